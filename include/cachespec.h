@@ -31,7 +31,20 @@
  *                          tree of drafted candidates is scored in one pass
  *                          (each node sees the prefix and its ancestors), one
  *                          root-to-node path is accepted, and its K/V rows
- *                          are moved next to the root.
+ *                          are moved next to the root;
+ *   cs_packed_kv_append,
+ *   cs_packed_kv_read,
+ *   cs_packed_verify_attention
+ *                       -- the same paged cache held in 4 bits a value: rows
+ *                          are quantised as they are appended, and verify
+ *                          attention (or single-token decoding) reads them;
+ *   cs_kv_fork,
+ *   cs_kv_release,
+ *   cs_kv_compact       -- the pages of any of these caches: rows of the page
+ *                          table share pages, give them back, and the pages in
+ *                          use move together;
+ *   cs_logprobs         -- log probabilities of given tokens with the entropy
+ *                          and the top alternatives of their rows.
  *
  * Conventions for every entry point
  *   - All tensor arguments are DEVICE pointers owned by the caller, dense
@@ -425,6 +438,191 @@ cs_status cs_tree_accept(const cs_accept_dims* dims, const void* target_logits, 
 cs_status cs_kv_commit_tree(const cs_attn_dims* dims, void* k_pages, void* v_pages, const int32_t* page_table,
                             int32_t* ctx_lens, const int32_t* path, const int32_t* n_accepted, int32_t n_nodes,
                             cs_stream_t stream);
+
+/*
+ * A paged K/V cache in 4 bits a value (the paper keeps its cache in the model's
+ * type; this is for servers whose contexts outgrow it: 144 bytes a token and KV
+ * head in place of 512).
+ *
+ * A row (one token, one KV head, 128 dims) is eight groups of 16 dims.  Group g
+ * has a scale s_g in e4m3 (8 bits: 4 exponent bits with bias 7, 3 mantissa
+ * bits), each dim a code in e2m1 (4 bits: a sign and one of the magnitudes 0,
+ * 0.5, 1, 1.5, 2, 3, 4, 6), and each KV head h a scale t_h in fp32 that its
+ * rows share (a calibration constant of the model, 1 where there is none).
+ * Dim d stands for  code_d * s_g * t_h.
+ *
+ *   k_codes, v_codes    uint8 [P, Hkv, ps, 64]: byte i holds dims 2i (low four
+ *                       bits) and 2i + 1; 16-byte aligned
+ *   k_scales, v_scales  e4m3 bytes [P, Hkv, ps, 8]; 16-byte aligned
+ *   k_head_scale,
+ *   v_head_scale        fp32 [Hkv], positive and finite, or NULL (all 1)
+ */
+typedef struct {
+    void* k_codes;
+    void* k_scales;
+    void* v_codes;
+    void* v_scales;
+    const float* k_head_scale;
+    const float* v_head_scale;
+} cs_packed_pool;
+
+/*
+ * cs_packed_kv_append: cs_kv_append into a packed cache.  The rows' positions,
+ * the clamping and the rows that are not written are those of cs_kv_append.
+ * For each group of a row x, in fp32 arithmetic with every operation rounded
+ * to nearest:
+ *     s = e4m3(max|x| / (6 t)), at most 448;
+ *     code_d = e2m1(x_d / (s t)), at most 6 in magnitude (0 where s t is 0),
+ * both conversions to nearest, ties to the even code.  A NaN is stored as 0, an
+ * infinity as the largest value of its group.
+ *
+ *   dims         the pool geometry (head_dim 128; n_q_heads and sm_scale unused)
+ *   new_k/new_v  bf16 [B, n_new, Hkv, 128], 16-byte aligned
+ *   page_table   int32 [B, max_pages_per_seq]; ctx_lens int32 [B]
+ *   n_new        in [1, 4096]
+ * Requests must not share the slots they write (cs_kv_fork gives each its own).
+ *
+ * cs_packed_kv_read: the newest n_rows rows of every request (positions
+ * L_b - n_rows + i) as bf16 [B, n_rows, Hkv, 128], 16-byte aligned: the values
+ * code * s * t rounded once.  A row that cs_packed_kv_append would not have
+ * written reads as zeros.  For what has no packed form (token trees, a prefix
+ * handed to another process).
+ *
+ * cs_packed_verify_attention: cs_verify_attention over a packed cache, with K
+ * and V the values that the codes stand for.  n_draft may be 0 (one new token a
+ * request), up to 16; (n_draft + 1) * G must not exceed 144.  q, out,
+ * page_table, ctx_lens, clamping, rows without a key, pages outside the pool,
+ * slots past L_b and the workspace as there, but that the workspace may start
+ * with any contents.  Arithmetic: q is taken to fp16 after a power of two has
+ * brought its row's largest entry below 2^15 (entries down to 2^-31 of it keep
+ * every bit), keys and values are code * s in fp16 (exact), the weights P are
+ * rounded to fp16 (11 bits), all products are summed in fp32, the softmax is
+ * fp32, and the head scales enter in fp32 with the softmax scale and the
+ * normalisation.
+ *
+ * Return CS_ERR_INVALID_ARG (null pointer, misalignment, bad dimension or
+ * count), CS_ERR_UNSUPPORTED (head_dim != 128, page size, query rows),
+ * CS_ERR_WORKSPACE or CS_ERR_CUDA.
+ */
+cs_status cs_packed_kv_append(const cs_attn_dims* dims, const cs_packed_pool* pool, const void* new_k,
+                              const void* new_v, const int32_t* page_table, const int32_t* ctx_lens, int32_t n_new,
+                              cs_stream_t stream);
+cs_status cs_packed_kv_read(const cs_attn_dims* dims, const cs_packed_pool* pool, const int32_t* page_table,
+                            const int32_t* ctx_lens, int32_t n_rows, void* out_k, void* out_v, cs_stream_t stream);
+size_t cs_packed_verify_attention_workspace_bytes(const cs_attn_dims* dims, int32_t n_draft);
+cs_status cs_packed_verify_attention(const cs_attn_dims* dims, const void* q, const cs_packed_pool* pool,
+                                     const int32_t* page_table, const int32_t* ctx_lens, int32_t n_draft, void* out,
+                                     void* workspace, size_t workspace_bytes, cs_stream_t stream);
+
+/*
+ * Pages of a cache, shared between rows of the page table.
+ *
+ * ref_counts int32 [P] says how many entries of the page table name each page;
+ * a page with 0 is free.  A page pool is any array of P pages of page_bytes
+ * each (the K or V pages of a layer, its codes or scales): all pools of a call
+ * follow the same page table.  Page ids outside [0, P) are carried along and
+ * neither counted nor copied.  Rows of a call lie in [0, R); an operation on a
+ * row outside it does nothing.
+ *
+ * cs_kv_fork: for each i in [0, n), row dst[i] becomes a copy of row src[i] of
+ * L = ctx_lens[src[i]] tokens (clamped to what the row can hold), or an empty
+ * row (L = 0) where src[i] is -1.  Full pages are shared: their counts grow by
+ * one.  A part-filled last page is copied into a page of the new row's own, and
+ * further pages of its own give it room for `room` more tokens (as many as the
+ * row can hold): ceil((L + room) / ps) - floor(L / ps) free pages in all, the lowest ids first, in
+ * the order of i.  Entries past them become -1, ctx_lens[dst[i]] = L and
+ * out_forked[i] = 1.  When the free pages do not suffice for i (with what the
+ * requests before it ask for), row dst[i] is left empty (entries -1, length 0)
+ * and out_forked[i] = 0; so it is for an i whose src is neither -1 nor a row
+ * (where dst[i] is no row either, nothing is written).  The dst rows must be
+ * distinct, none of them a src, and their former pages are not given back
+ * (cs_kv_release before).
+ *
+ * cs_kv_release: row rows[i] keeps the pages of its first keep_lens[i] tokens
+ * (negative: 0): every entry past them becomes -1 and its page's count falls by
+ * one; ctx_lens is at most keep_lens[i] from then on.  0 gives the whole row
+ * back; after a commit, keep_lens = ctx_lens gives back what the rejected drafts
+ * took.  The rows must be distinct.
+ *
+ * cs_kv_compact: with N the number of pages whose count is not 0, every such
+ * page with an id of N or more moves to a free id below N, both in ascending
+ * order; its contents, its count and the entries that name it follow (all
+ * max_pages_per_seq entries of all R rows).  out_live[0] = N: pages from N on
+ * are free.  Page contents at the old ids stay as they were.
+ *
+ *   pools        host array of n_pools in [0, CS_MAX_PAGE_POOLS]; data 16-byte
+ *                aligned, page_bytes a positive multiple of 16
+ *   page_table   int32 [R, max_pages_per_seq], ctx_lens int32 [R],
+ *                ref_counts int32 [P]: updated in place
+ *   src, dst, rows, keep_lens, out_forked   int32 [n], n >= 0
+ *   workspace    at least as many bytes as the query says, 256-byte aligned,
+ *                any initial contents; calls that share one must be ordered
+ *
+ * Return CS_ERR_INVALID_ARG (null pointer, misalignment, bad dimension or
+ * count), CS_ERR_WORKSPACE or CS_ERR_CUDA.
+ */
+typedef struct {
+    int32_t rows;               /* R > 0 rows of the page table */
+    int32_t max_pages_per_seq;  /* its columns (> 0) */
+    int32_t page_size;          /* ps > 0 tokens per page */
+    int32_t num_pages;          /* P > 0 pages of every pool */
+} cs_page_dims;
+
+typedef struct {
+    void* data;                 /* [P, page_bytes] */
+    size_t page_bytes;
+} cs_page_pool;
+#define CS_MAX_PAGE_POOLS 128
+
+size_t cs_kv_fork_workspace_bytes(const cs_page_dims* dims, int32_t n);
+cs_status cs_kv_fork(const cs_page_dims* dims, const cs_page_pool* pools, int32_t n_pools, int32_t* page_table,
+                     int32_t* ctx_lens, int32_t* ref_counts, const int32_t* src, const int32_t* dst, int32_t n,
+                     int32_t room, int32_t* out_forked, void* workspace, size_t workspace_bytes, cs_stream_t stream);
+cs_status cs_kv_release(const cs_page_dims* dims, int32_t* page_table, int32_t* ctx_lens, int32_t* ref_counts,
+                        const int32_t* rows, const int32_t* keep_lens, int32_t n, cs_stream_t stream);
+size_t cs_kv_compact_workspace_bytes(const cs_page_dims* dims);
+cs_status cs_kv_compact(const cs_page_dims* dims, const cs_page_pool* pools, int32_t n_pools, int32_t* page_table,
+                        int32_t* ref_counts, int32_t* out_live, void* workspace, size_t workspace_bytes,
+                        cs_stream_t stream);
+
+/*
+ * Log probabilities of given tokens (what a server answers beside the tokens
+ * that cs_spec_accept or cs_sample emitted, or scores a prompt's tokens by).
+ *
+ * For every row r with token x = tokens[r] >= 0, with p = softmax(logits[r,:] / T):
+ *   out_logprob[r] = ln p(x)                      (-inf for a masked token, for
+ *                    x >= V and where ln p(x) passes fp32)
+ *   out_entropy[r] = - sum_v p(v) ln p(v)
+ *   out_top_tokens[r, j], out_top_logprobs[r, j]: the j-th largest logit's id
+ *                    (the lowest id first on ties) and ln p of it, j < n_top;
+ *                    -1 and -inf past the logits above -inf
+ * A row whose token is negative is not read (the positions past those that an
+ * acceptance step emitted): it gets -inf, 0, -1 and -inf.  A row without a
+ * logit above -inf gets the same.
+ *
+ *   logits   [rows, V] fp32 or bf16, rows row_stride elements apart (>= V),
+ *            element-aligned; -inf marks a masked token, NaN and +inf are not allowed
+ *   tokens   int32 [rows]
+ *   T        > 0 and finite
+ *   n_top    in [0, CS_MAX_TOP]
+ *   out_entropy may be NULL; out_top_* may be NULL when n_top is 0
+ * Sums are fp32; the result is a deterministic function of the inputs.
+ *
+ * Returns CS_ERR_INVALID_ARG (null pointer, misalignment, bad dimension, bad
+ * temperature, n_top out of range), CS_ERR_UNSUPPORTED (vocab above
+ * CS_MAX_VOCAB) or CS_ERR_CUDA.
+ */
+typedef struct {
+    int32_t rows;               /* >= 0 (0: nothing to do) */
+    int32_t vocab;              /* V > 0 */
+    int32_t logit_dtype;        /* cs_dtype */
+    int32_t n_top;              /* alternatives a row */
+    int64_t row_stride;         /* elements from one row to the next */
+} cs_logprob_dims;
+#define CS_MAX_TOP 32
+cs_status cs_logprobs(const cs_logprob_dims* dims, const void* logits, const int32_t* tokens, float temperature,
+                      float* out_logprob, float* out_entropy, int32_t* out_top_tokens, float* out_top_logprobs,
+                      cs_stream_t stream);
 
 /*
  * Device status word of a verify-attention workspace: 0 when every call that

@@ -16,6 +16,7 @@ import importlib.machinery
 import importlib.util
 import os
 import threading
+from typing import NamedTuple
 
 import torch
 
@@ -33,7 +34,12 @@ EXPORTED_SYMBOLS = ("cs_abi_version", "cs_last_error", "cs_verify_attention_work
                     "cs_sample", "cs_kv_append", "cs_kv_commit", "cs_route_workspace_bytes",
                     "cs_route_norms", "cs_route", "cs_tree_verify_attention_workspace_bytes",
                     "cs_tree_verify_attention", "cs_tree_accept_workspace_bytes", "cs_tree_accept",
-                    "cs_kv_commit_tree", "cs_selftest_wait_timeout")
+                    "cs_kv_commit_tree", "cs_selftest_wait_timeout",
+                    "cs_packed_kv_append", "cs_packed_kv_read", "cs_packed_verify_attention_workspace_bytes",
+                    "cs_packed_verify_attention", "cs_kv_fork_workspace_bytes", "cs_kv_fork", "cs_kv_release",
+                    "cs_kv_compact_workspace_bytes", "cs_kv_compact", "cs_logprobs")
+CS_MAX_TOP = 32
+CS_MAX_PAGE_POOLS = 128
 
 
 class RouteDims(ctypes.Structure):
@@ -50,6 +56,37 @@ class AttnDims(ctypes.Structure):
 class AcceptDims(ctypes.Structure):
     _fields_ = [("batch", ctypes.c_int32), ("vocab", ctypes.c_int32),
                 ("logit_dtype", ctypes.c_int32)]
+
+
+class PackedPoolPtrs(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("k_codes", "k_scales", "v_codes", "v_scales", "k_head_scale",
+                                               "v_head_scale")]
+
+
+class PageDims(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int32), ("max_pages_per_seq", ctypes.c_int32), ("page_size", ctypes.c_int32),
+                ("num_pages", ctypes.c_int32)]
+
+
+class PagePool(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("page_bytes", ctypes.c_size_t)]
+
+
+class LogprobDims(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int32), ("vocab", ctypes.c_int32), ("logit_dtype", ctypes.c_int32),
+                ("n_top", ctypes.c_int32), ("row_stride", ctypes.c_int64)]
+
+
+class PackedPool(NamedTuple):
+    """A K/V cache in 4 bits a value: codes uint8 [P, Hkv, ps, 64] (two dims a byte, the even one in the low four
+    bits), scales float8_e4m3fn [P, Hkv, ps, 8] (one for 16 dims) and, optionally, fp32 [Hkv] scales of the heads.
+    See include/cachespec.h."""
+    k_codes: torch.Tensor
+    k_scales: torch.Tensor
+    v_codes: torch.Tensor
+    v_scales: torch.Tensor
+    k_head_scale: torch.Tensor | None = None
+    v_head_scale: torch.Tensor | None = None
 
 
 class CacheSpecError(RuntimeError):
@@ -125,6 +162,29 @@ def load_library(path: str | None = None):
         lib.cs_tree_accept.restype = ctypes.c_int
         lib.cs_tree_accept.argtypes = [ctypes.POINTER(AcceptDims), vp, vp, vp, vp, vp, i32, ctypes.c_float,
                                        vp, vp, vp, vp, sz, vp]
+        lib.cs_packed_kv_append.restype = ctypes.c_int
+        lib.cs_packed_kv_append.argtypes = [ctypes.POINTER(AttnDims), ctypes.POINTER(PackedPoolPtrs), vp, vp, vp, vp, i32,
+                                            vp]
+        lib.cs_packed_kv_read.restype = ctypes.c_int
+        lib.cs_packed_kv_read.argtypes = [ctypes.POINTER(AttnDims), ctypes.POINTER(PackedPoolPtrs), vp, vp, i32, vp, vp, vp]
+        lib.cs_packed_verify_attention_workspace_bytes.restype = sz
+        lib.cs_packed_verify_attention_workspace_bytes.argtypes = [ctypes.POINTER(AttnDims), i32]
+        lib.cs_packed_verify_attention.restype = ctypes.c_int
+        lib.cs_packed_verify_attention.argtypes = [ctypes.POINTER(AttnDims), vp, ctypes.POINTER(PackedPoolPtrs), vp, vp, i32,
+                                                   vp, vp, sz, vp]
+        lib.cs_kv_fork_workspace_bytes.restype = sz
+        lib.cs_kv_fork_workspace_bytes.argtypes = [ctypes.POINTER(PageDims), i32]
+        lib.cs_kv_fork.restype = ctypes.c_int
+        lib.cs_kv_fork.argtypes = [ctypes.POINTER(PageDims), ctypes.POINTER(PagePool), i32, vp, vp, vp, vp, vp, i32, i32, vp,
+                                   vp, sz, vp]
+        lib.cs_kv_release.restype = ctypes.c_int
+        lib.cs_kv_release.argtypes = [ctypes.POINTER(PageDims), vp, vp, vp, vp, vp, i32, vp]
+        lib.cs_kv_compact_workspace_bytes.restype = sz
+        lib.cs_kv_compact_workspace_bytes.argtypes = [ctypes.POINTER(PageDims)]
+        lib.cs_kv_compact.restype = ctypes.c_int
+        lib.cs_kv_compact.argtypes = [ctypes.POINTER(PageDims), ctypes.POINTER(PagePool), i32, vp, vp, vp, vp, sz, vp]
+        lib.cs_logprobs.restype = ctypes.c_int
+        lib.cs_logprobs.argtypes = [ctypes.POINTER(LogprobDims), vp, vp, ctypes.c_float, vp, vp, vp, vp, vp]
         lib.cs_kv_commit_tree.restype = ctypes.c_int
         lib.cs_kv_commit_tree.argtypes = [ctypes.POINTER(AttnDims), vp, vp, vp, vp, vp, vp, i32, vp]
         if path is None:
@@ -579,6 +639,226 @@ def cs_kv_commit_tree(k_pages, v_pages, page_table, ctx_lens, path, n_accepted, 
                                _stream(dev) if stream is None else stream)
     if st:
         _check(lib, st)
+
+
+def packed_pool(num_pages: int, n_kv_heads: int, page_size: int, device, k_head_scale=None,
+                v_head_scale=None) -> PackedPool:
+    """An empty (all zero) packed cache of ``num_pages`` pages."""
+    def zeros(width, dtype):
+        return torch.zeros((num_pages, n_kv_heads, page_size, width), dtype=dtype, device=device)
+    return PackedPool(zeros(64, torch.uint8), zeros(8, torch.float8_e4m3fn), zeros(64, torch.uint8),
+                      zeros(8, torch.float8_e4m3fn), k_head_scale, v_head_scale)
+
+
+def _packed(pool: PackedPool, dev):
+    """The pool's pointers, after the checks, and its geometry (P, Hkv, ps)."""
+    pool = PackedPool(*pool)
+    _need(pool.k_codes, "k_codes", torch.uint8, 4, dev)
+    P, Hkv, ps, width = pool.k_codes.shape
+    if width != 64:
+        raise ValueError(f"k_codes must be [P, Hkv, ps, 64], got {tuple(pool.k_codes.shape)}")
+    _need(pool.v_codes, "v_codes", torch.uint8, 4, dev)
+    if pool.v_codes.shape != pool.k_codes.shape:
+        raise ValueError("k_codes and v_codes must have the same shape")
+    for name in ("k_scales", "v_scales"):
+        t = getattr(pool, name)
+        _need(t, name, torch.float8_e4m3fn, 4, dev)
+        if tuple(t.shape) != (P, Hkv, ps, 8):
+            raise ValueError(f"{name} must be [{P}, {Hkv}, {ps}, 8], got {tuple(t.shape)}")
+    for name in ("k_head_scale", "v_head_scale"):
+        t = getattr(pool, name)
+        if t is not None:
+            _need(t, name, torch.float32, 1, dev)
+            if t.shape[0] != Hkv:
+                raise ValueError(f"{name} must be [{Hkv}], got {tuple(t.shape)}")
+    return PackedPoolPtrs(*(_ptr(t) for t in pool)), (P, Hkv, ps)
+
+
+def _rows_of(page_table, ctx_lens, B: int, dev) -> None:
+    _need(page_table, "page_table", torch.int32, 2, dev)
+    _need(ctx_lens, "ctx_lens", torch.int32, 1, dev)
+    if page_table.shape[0] != B or ctx_lens.shape[0] != B:
+        raise ValueError(f"page_table and ctx_lens must have {B} rows")
+
+
+def cs_packed_kv_append(new_k, new_v, pool, page_table, ctx_lens, stream: int | None = None):
+    """Quantise the K/V rows of the newest positions into a packed cache (in place).
+    new_k / new_v bf16 [B, n_new, Hkv, 128]; ``pool`` a PackedPool.  See include/cachespec.h."""
+    lib = load_library()
+    _need(new_k, "new_k", torch.bfloat16, 4, None)
+    dev = new_k.device
+    _need(new_v, "new_v", torch.bfloat16, 4, dev)
+    ptrs, (P, Hkv, ps) = _packed(pool, dev)
+    B, n_new, H, D = new_k.shape
+    if new_v.shape != new_k.shape or H != Hkv or D != 128:
+        raise ValueError("new rows and pool do not match")
+    _rows_of(page_table, ctx_lens, B, dev)
+    d = AttnDims(B, Hkv, Hkv, D, ps, page_table.shape[1], P, 0.0)
+    st = lib.cs_packed_kv_append(ctypes.byref(d), ctypes.byref(ptrs), new_k.data_ptr(), new_v.data_ptr(),
+                                 page_table.data_ptr(), ctx_lens.data_ptr(), int(n_new),
+                                 _stream(dev) if stream is None else stream)
+    if st:
+        _check(lib, st)
+
+
+def cs_packed_kv_read(pool, page_table, ctx_lens, n_rows: int, stream: int | None = None):
+    """The newest ``n_rows`` rows of every request from a packed cache; returns (k, v), bf16 [B, n_rows, Hkv, 128]."""
+    lib = load_library()
+    dev = page_table.device
+    ptrs, (P, Hkv, ps) = _packed(pool, dev)
+    B = page_table.shape[0]
+    _rows_of(page_table, ctx_lens, B, dev)
+    out = [torch.empty((B, max(int(n_rows), 0), Hkv, 128), dtype=torch.bfloat16, device=dev) for _ in range(2)]
+    d = AttnDims(B, Hkv, Hkv, 128, ps, page_table.shape[1], P, 0.0)
+    st = lib.cs_packed_kv_read(ctypes.byref(d), ctypes.byref(ptrs), page_table.data_ptr(), ctx_lens.data_ptr(),
+                               int(n_rows), out[0].data_ptr(), out[1].data_ptr(),
+                               _stream(dev) if stream is None else stream)
+    if st:
+        _check(lib, st)
+    return tuple(out)
+
+
+def cs_packed_verify_attention(q, pool, page_table, ctx_lens, n_draft, out=None, workspace=None, sm_scale: float = 0.0,
+                               stream: int | None = None):
+    """Verify attention over a packed cache, ``n_draft`` in [0, 16]; returns ``out`` (bf16 [B, k+1, Hq, 128]).
+    See include/cachespec.h."""
+    lib = load_library()
+    _need(q, "q", torch.bfloat16, 4, None)
+    dev = q.device
+    ptrs, (P, Hkv, ps) = _packed(pool, dev)
+    B, R, Hq, D = q.shape
+    if R != n_draft + 1:
+        raise ValueError(f"q has {R} rows per request, n_draft+1 = {n_draft + 1}")
+    _rows_of(page_table, ctx_lens, B, dev)
+    d = AttnDims(B, Hq, Hkv, D, ps, page_table.shape[1], P, float(sm_scale))
+    if out is None:
+        out = torch.empty_like(q)
+    else:
+        _need(out, "out", torch.bfloat16, 4, dev)
+        if out.shape != q.shape:
+            raise ValueError("out must have the shape of q")
+    if workspace is None:
+        n = lib.cs_packed_verify_attention_workspace_bytes(ctypes.byref(d), int(n_draft))
+        workspace = _cached_workspace("packed_attn", dev, n, stream)
+    st = lib.cs_packed_verify_attention(ctypes.byref(d), q.data_ptr(), ctypes.byref(ptrs), page_table.data_ptr(),
+                                        ctx_lens.data_ptr(), int(n_draft), out.data_ptr(), workspace.data_ptr(),
+                                        workspace.nbytes, _stream(dev) if stream is None else stream)
+    if st:
+        _check(lib, st)
+    return out
+
+
+def _page_call(page_table, ctx_lens, ref_counts, page_size, dev) -> PageDims:
+    _need(page_table, "page_table", torch.int32, 2, dev)
+    _need(ref_counts, "ref_counts", torch.int32, 1, dev)
+    R, cols = page_table.shape
+    if ctx_lens is not None:
+        _need(ctx_lens, "ctx_lens", torch.int32, 1, dev)
+        if ctx_lens.shape[0] != R:
+            raise ValueError(f"ctx_lens must be [{R}]")
+    return PageDims(R, cols, int(page_size), ref_counts.shape[0])
+
+
+def _page_pools(pools, P: int, dev):
+    pools = [t for t in pools if t is not None]
+    for i, t in enumerate(pools):
+        _need(t, f"pools[{i}]", t.dtype, t.dim(), dev)
+        if t.dim() < 2 or t.shape[0] != P:
+            raise ValueError(f"pools[{i}] must be [{P}, ...], a page a row, got {tuple(t.shape)}")
+    return (PagePool * len(pools))(*((t.data_ptr(), t.nbytes // P) for t in pools)), len(pools)
+
+
+def cs_kv_fork(pools, page_table, ctx_lens, ref_counts, src, dst, page_size: int, room: int = 0, workspace=None,
+               stream: int | None = None):
+    """Rows ``dst`` of the page table become copies of rows ``src`` (-1: empty rows) that share their full pages,
+    with room for ``room`` more tokens each; table, lengths and counts change in place.  ``pools``: the cache's
+    tensors, each [P, ...].  Returns int32 [n]: 1 where there were enough free pages.  See include/cachespec.h."""
+    lib = load_library()
+    dev = page_table.device
+    d = _page_call(page_table, ctx_lens, ref_counts, page_size, dev)
+    arr, n_pools = _page_pools(pools, d.num_pages, dev)
+    _need(src, "src", torch.int32, 1, dev)
+    _need(dst, "dst", torch.int32, 1, dev)
+    n = src.shape[0]
+    if dst.shape[0] != n:
+        raise ValueError("src and dst must have the same length")
+    out = src.new_empty((n,))
+    if workspace is None:
+        workspace = _cached_workspace("fork", dev, lib.cs_kv_fork_workspace_bytes(ctypes.byref(d), int(n)), stream)
+    st = lib.cs_kv_fork(ctypes.byref(d), arr, n_pools, page_table.data_ptr(), ctx_lens.data_ptr(),
+                        ref_counts.data_ptr(), src.data_ptr(), dst.data_ptr(), int(n), int(room), out.data_ptr(),
+                        workspace.data_ptr(), workspace.nbytes, _stream(dev) if stream is None else stream)
+    if st:
+        _check(lib, st)
+    return out
+
+
+def cs_kv_release(page_table, ctx_lens, ref_counts, rows, keep_lens, page_size: int, stream: int | None = None):
+    """Rows ``rows`` keep the pages of their first ``keep_lens`` tokens and give the others back (in place)."""
+    lib = load_library()
+    dev = page_table.device
+    d = _page_call(page_table, ctx_lens, ref_counts, page_size, dev)
+    _need(rows, "rows", torch.int32, 1, dev)
+    _need(keep_lens, "keep_lens", torch.int32, 1, dev)
+    if rows.shape != keep_lens.shape:
+        raise ValueError("rows and keep_lens must have the same length")
+    st = lib.cs_kv_release(ctypes.byref(d), page_table.data_ptr(), ctx_lens.data_ptr(), ref_counts.data_ptr(),
+                           rows.data_ptr(), keep_lens.data_ptr(), int(rows.shape[0]),
+                           _stream(dev) if stream is None else stream)
+    if st:
+        _check(lib, st)
+
+
+def cs_kv_compact(pools, page_table, ref_counts, workspace=None, stream: int | None = None):
+    """Moves the pages in use to the lowest ids; pools, table and counts change in place.
+    Returns int32 [1]: how many pages are in use.  See include/cachespec.h."""
+    lib = load_library()
+    dev = page_table.device
+    d = _page_call(page_table, None, ref_counts, 1, dev)
+    arr, n_pools = _page_pools(pools, d.num_pages, dev)
+    out = ref_counts.new_empty((1,))
+    if workspace is None:
+        workspace = _cached_workspace("compact", dev, lib.cs_kv_compact_workspace_bytes(ctypes.byref(d)), stream)
+    st = lib.cs_kv_compact(ctypes.byref(d), arr, n_pools, page_table.data_ptr(), ref_counts.data_ptr(),
+                           out.data_ptr(), workspace.data_ptr(), workspace.nbytes,
+                           _stream(dev) if stream is None else stream)
+    if st:
+        _check(lib, st)
+    return out
+
+
+def cs_logprobs(logits, tokens, temperature: float = 1.0, n_top: int = 0, stream: int | None = None):
+    """Log probabilities of ``tokens`` (int32 [N]; negative: the row is skipped) under ``logits`` [N, V], whose rows
+    may lie apart.  Returns (logprob [N], entropy [N], top tokens [N, n_top], their log probabilities [N, n_top]).
+    See include/cachespec.h."""
+    lib = load_library()
+    if not isinstance(logits, torch.Tensor):
+        raise TypeError("logits must be a torch.Tensor")
+    if logits.dtype not in (torch.float32, torch.bfloat16):
+        raise TypeError("logits must be float32 or bfloat16")
+    if logits.dim() != 2:
+        raise ValueError(f"logits must have 2 dims, got shape {tuple(logits.shape)}")
+    if not logits.is_cuda:
+        raise ValueError("logits must live on a CUDA device")
+    N, V = logits.shape
+    if V > 1 and logits.stride(1) != 1:
+        raise ValueError("the logits of a row must be contiguous")
+    dev = logits.device
+    _need(tokens, "tokens", torch.int32, 1, dev)
+    if tokens.shape[0] != N:
+        raise ValueError(f"tokens must be [{N}]")
+    top = max(int(n_top), 0)
+    lp, entropy = (torch.empty((N,), dtype=torch.float32, device=dev) for _ in range(2))
+    top_tokens = tokens.new_empty((N, top))
+    top_lp = lp.new_empty((N, top))
+    d = LogprobDims(N, V, CS_F32 if logits.dtype == torch.float32 else CS_BF16, int(n_top),
+                    logits.stride(0) if N > 1 else V)
+    st = lib.cs_logprobs(ctypes.byref(d), logits.data_ptr(), tokens.data_ptr(), float(temperature), lp.data_ptr(),
+                         entropy.data_ptr(), top_tokens.data_ptr(), top_lp.data_ptr(),
+                         _stream(dev) if stream is None else stream)
+    if st:
+        _check(lib, st)
+    return lp, entropy, top_tokens, top_lp
 
 
 def cs_verify_attention_noalloc(q, k_pages, v_pages, page_table, ctx_lens, n_draft, out=None,

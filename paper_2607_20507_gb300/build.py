@@ -19,7 +19,8 @@ BUILD_DIR = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libcachespec.so")
 MARSHAL = os.path.join(HERE, "_marshal.so")
 AGAINST = os.path.join(BUILD_DIR, "marshal.against")
-SOURCES = ["capi.cu", "verify_attention.cu", "spec_accept.cu", "noalloc.cu", "kv_cache.cu", "route.cu", "selftest.cu"]
+SOURCES = ["capi.cu", "verify_attention.cu", "spec_accept.cu", "noalloc.cu", "kv_cache.cu", "route.cu", "selftest.cu",
+           "packed_cache.cu", "packed_attention.cu", "pages.cu", "logprobs.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 
 

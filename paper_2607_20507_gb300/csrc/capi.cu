@@ -150,6 +150,62 @@ cs_status check_sample(const cs_accept_dims* d, float temperature) {
         return fail(CS_ERR_UNSUPPORTED, "vocab %d (this library implements up to %d)", d->vocab, CS_MAX_VOCAB);
     return CS_OK;
 }
+
+cs_status check_packed(const cs_attn_dims* d, const cs_packed_pool* pool) {
+    if (!d || !pool) return fail(CS_ERR_INVALID_ARG, "dims or pool is NULL");
+    if (d->batch < 0) return fail(CS_ERR_INVALID_ARG, "batch %d < 0", d->batch);
+    if (d->n_kv_heads <= 0 || d->page_size <= 0 || d->max_pages_per_seq <= 0 || d->num_pages <= 0)
+        return fail(CS_ERR_INVALID_ARG, "n_kv_heads, page_size, max_pages_per_seq and num_pages must be positive");
+    if (d->head_dim != 128) return fail(CS_ERR_UNSUPPORTED, "head_dim %d (this library implements 128)", d->head_dim);
+    if (!pow2_page(d->page_size))
+        return fail(CS_ERR_UNSUPPORTED, "page_size %d (supported: 8..256, powers of two)", d->page_size);
+    if ((long long)d->max_pages_per_seq * d->page_size > (1LL << 30))
+        return fail(CS_ERR_INVALID_ARG, "max_pages_per_seq * page_size exceeds 2^30 keys");
+    return CS_OK;
+}
+
+cs_status check_packed_pointers(const cs_packed_pool& p, const int32_t* page_table, const int32_t* ctx_lens) {
+    if (!p.k_codes || !p.k_scales || !p.v_codes || !p.v_scales || !page_table || !ctx_lens)
+        return fail(CS_ERR_INVALID_ARG, "a tensor pointer is NULL");
+    if (!aligned(p.k_codes, 16) || !aligned(p.k_scales, 16) || !aligned(p.v_codes, 16) || !aligned(p.v_scales, 16))
+        return fail(CS_ERR_INVALID_ARG, "codes and scales must be 16-byte aligned");
+    if (!aligned(p.k_head_scale, 4) || !aligned(p.v_head_scale, 4) || !aligned(page_table, 4) || !aligned(ctx_lens, 4))
+        return fail(CS_ERR_INVALID_ARG, "head scales, page_table and ctx_lens must be 4-byte aligned");
+    return CS_OK;
+}
+
+cs_status check_packed_attn(const cs_attn_dims* d, int32_t n_draft) {
+    if (!d) return fail(CS_ERR_INVALID_ARG, "dims is NULL");
+    if (n_draft < 0 || n_draft > 16) return fail(CS_ERR_INVALID_ARG, "n_draft %d not in [0, 16]", n_draft);
+    const cs_status st = check_attn_geometry(d);
+    if (st != CS_OK) return st;
+    const long long rows = (long long)(n_draft + 1) * (d->n_q_heads / d->n_kv_heads);
+    if (rows > 144) return fail(CS_ERR_UNSUPPORTED, "(k+1)*G = %lld query rows per KV head (max 144)", rows);
+    return CS_OK;
+}
+
+cs_status check_pages(const cs_page_dims* d) {
+    if (!d) return fail(CS_ERR_INVALID_ARG, "dims is NULL");
+    if (d->rows <= 0 || d->max_pages_per_seq <= 0 || d->page_size <= 0 || d->num_pages <= 0)
+        return fail(CS_ERR_INVALID_ARG, "rows, max_pages_per_seq, page_size and num_pages must be positive");
+    if ((long long)d->max_pages_per_seq * d->page_size > (1LL << 30))
+        return fail(CS_ERR_INVALID_ARG, "max_pages_per_seq * page_size exceeds 2^30 keys");
+    return CS_OK;
+}
+
+cs_status check_page_pools(const cs_page_pool* pools, int32_t n_pools) {
+    if (n_pools < 0 || n_pools > CS_MAX_PAGE_POOLS)
+        return fail(CS_ERR_INVALID_ARG, "n_pools %d not in [0, %d]", n_pools, CS_MAX_PAGE_POOLS);
+    if (n_pools > 0 && !pools) return fail(CS_ERR_INVALID_ARG, "pools is NULL");
+    for (int i = 0; i < n_pools; ++i) {
+        if (!pools[i].data) return fail(CS_ERR_INVALID_ARG, "pool %d is NULL", i);
+        if (!aligned(pools[i].data, 16)) return fail(CS_ERR_INVALID_ARG, "pool %d must be 16-byte aligned", i);
+        if (pools[i].page_bytes == 0 || pools[i].page_bytes % 16 != 0 || pools[i].page_bytes > (1ull << 32))
+            return fail(CS_ERR_INVALID_ARG, "pool %d: page_bytes %zu is not a positive multiple of 16 up to 2^32", i,
+                        pools[i].page_bytes);
+    }
+    return CS_OK;
+}
 }  // namespace
 
 StreamTurn::StreamTurn(cudaStream_t stream) : turn_(turn_of(stream)) { turn_.lock(); }
@@ -362,6 +418,162 @@ cs_status cs_kv_commit(int32_t batch, int32_t* ctx_lens, const int32_t* n_accept
     if (!aligned(ctx_lens, 4) || !aligned(n_accepted, 4))
         return fail(CS_ERR_INVALID_ARG, "ctx_lens and n_accepted must be 4-byte aligned");
     return launch_kv_commit(ctx_lens, n_accepted, batch, n_draft, reinterpret_cast<cudaStream_t>(stream));
+}
+
+cs_status cs_packed_kv_append(const cs_attn_dims* dims, const cs_packed_pool* pool, const void* new_k,
+                              const void* new_v, const int32_t* page_table, const int32_t* ctx_lens, int32_t n_new,
+                              cs_stream_t stream) {
+    cs_status st = check_packed(dims, pool);
+    if (st != CS_OK) return st;
+    if (n_new < 1 || n_new > 4096) return fail(CS_ERR_INVALID_ARG, "n_new %d not in [1, 4096]", n_new);
+    if (dims->batch == 0) return CS_OK;
+    st = check_packed_pointers(*pool, page_table, ctx_lens);
+    if (st != CS_OK) return st;
+    if (!new_k || !new_v) return fail(CS_ERR_INVALID_ARG, "a tensor pointer is NULL");
+    if (!aligned(new_k, 16) || !aligned(new_v, 16))
+        return fail(CS_ERR_INVALID_ARG, "new rows must be 16-byte aligned");
+    return launch_packed_append(*dims, *pool, new_k, new_v, page_table, ctx_lens, n_new,
+                                reinterpret_cast<cudaStream_t>(stream));
+}
+
+cs_status cs_packed_kv_read(const cs_attn_dims* dims, const cs_packed_pool* pool, const int32_t* page_table,
+                            const int32_t* ctx_lens, int32_t n_rows, void* out_k, void* out_v, cs_stream_t stream) {
+    cs_status st = check_packed(dims, pool);
+    if (st != CS_OK) return st;
+    if (n_rows < 1 || n_rows > (1 << 30)) return fail(CS_ERR_INVALID_ARG, "n_rows %d not in [1, 2^30]", n_rows);
+    if (dims->batch == 0) return CS_OK;
+    st = check_packed_pointers(*pool, page_table, ctx_lens);
+    if (st != CS_OK) return st;
+    if (!out_k || !out_v) return fail(CS_ERR_INVALID_ARG, "a tensor pointer is NULL");
+    if (!aligned(out_k, 16) || !aligned(out_v, 16))
+        return fail(CS_ERR_INVALID_ARG, "out_k and out_v must be 16-byte aligned");
+    return launch_packed_read(*dims, *pool, page_table, ctx_lens, n_rows, out_k, out_v,
+                              reinterpret_cast<cudaStream_t>(stream));
+}
+
+size_t cs_packed_verify_attention_workspace_bytes(const cs_attn_dims* dims, int32_t n_draft) {
+    if (check_packed_attn(dims, n_draft) != CS_OK) return 0;
+    return packed_attention_workspace_bytes(*dims, n_draft + 1, current_sm_count());
+}
+
+cs_status cs_packed_verify_attention(const cs_attn_dims* dims, const void* q, const cs_packed_pool* pool,
+                                     const int32_t* page_table, const int32_t* ctx_lens, int32_t n_draft, void* out,
+                                     void* workspace, size_t workspace_bytes, cs_stream_t stream) {
+    cs_status st = check_packed_attn(dims, n_draft);
+    if (st != CS_OK) return st;
+    if (!pool) return fail(CS_ERR_INVALID_ARG, "pool is NULL");
+    if (dims->batch == 0) return CS_OK;
+    st = check_packed_pointers(*pool, page_table, ctx_lens);
+    if (st != CS_OK) return st;
+    if (!q || !out) return fail(CS_ERR_INVALID_ARG, "a tensor pointer is NULL");
+    if (!aligned(q, 4) || !aligned(out, 8))
+        return fail(CS_ERR_INVALID_ARG, "q must be 4-byte and out 8-byte aligned");
+    const size_t need = packed_attention_workspace_bytes(*dims, n_draft + 1, current_sm_count());
+    if (!workspace || workspace_bytes < need)
+        return fail(CS_ERR_WORKSPACE, "workspace of %zu bytes given, %zu needed", workspace_bytes, need);
+    if (!aligned(workspace, 256)) return fail(CS_ERR_INVALID_ARG, "workspace must be 256-byte aligned");
+    const StreamTurn turn(reinterpret_cast<cudaStream_t>(stream));
+    return launch_packed_attention(*dims, q, *pool, page_table, ctx_lens, n_draft + 1, out, workspace,
+                                   reinterpret_cast<cudaStream_t>(stream));
+}
+
+size_t cs_kv_fork_workspace_bytes(const cs_page_dims* dims, int32_t n) {
+    if (check_pages(dims) != CS_OK || n < 0) return 0;
+    return fork_workspace_bytes(*dims, n);
+}
+
+cs_status cs_kv_fork(const cs_page_dims* dims, const cs_page_pool* pools, int32_t n_pools, int32_t* page_table,
+                     int32_t* ctx_lens, int32_t* ref_counts, const int32_t* src, const int32_t* dst, int32_t n,
+                     int32_t room, int32_t* out_forked, void* workspace, size_t workspace_bytes, cs_stream_t stream) {
+    cs_status st = check_pages(dims);
+    if (st != CS_OK) return st;
+    st = check_page_pools(pools, n_pools);
+    if (st != CS_OK) return st;
+    if (n < 0) return fail(CS_ERR_INVALID_ARG, "n %d < 0", n);
+    if (room < 0) return fail(CS_ERR_INVALID_ARG, "room %d < 0", room);
+    if (n == 0) return CS_OK;
+    if (!page_table || !ctx_lens || !ref_counts || !src || !dst || !out_forked)
+        return fail(CS_ERR_INVALID_ARG, "a tensor pointer is NULL");
+    if (!aligned(page_table, 4) || !aligned(ctx_lens, 4) || !aligned(ref_counts, 4) || !aligned(src, 4) ||
+        !aligned(dst, 4) || !aligned(out_forked, 4))
+        return fail(CS_ERR_INVALID_ARG, "int32 pointers must be 4-byte aligned");
+    const size_t need = fork_workspace_bytes(*dims, n);
+    if (!workspace || workspace_bytes < need)
+        return fail(CS_ERR_WORKSPACE, "workspace of %zu bytes given, %zu needed", workspace_bytes, need);
+    if (!aligned(workspace, 256)) return fail(CS_ERR_INVALID_ARG, "workspace must be 256-byte aligned");
+    const StreamTurn turn(reinterpret_cast<cudaStream_t>(stream));
+    return launch_kv_fork(*dims, pools, n_pools, page_table, ctx_lens, ref_counts, src, dst, n, room, out_forked,
+                          workspace, reinterpret_cast<cudaStream_t>(stream));
+}
+
+cs_status cs_kv_release(const cs_page_dims* dims, int32_t* page_table, int32_t* ctx_lens, int32_t* ref_counts,
+                        const int32_t* rows, const int32_t* keep_lens, int32_t n, cs_stream_t stream) {
+    const cs_status st = check_pages(dims);
+    if (st != CS_OK) return st;
+    if (n < 0) return fail(CS_ERR_INVALID_ARG, "n %d < 0", n);
+    if (n == 0) return CS_OK;
+    if (!page_table || !ctx_lens || !ref_counts || !rows || !keep_lens)
+        return fail(CS_ERR_INVALID_ARG, "a tensor pointer is NULL");
+    if (!aligned(page_table, 4) || !aligned(ctx_lens, 4) || !aligned(ref_counts, 4) || !aligned(rows, 4) ||
+        !aligned(keep_lens, 4))
+        return fail(CS_ERR_INVALID_ARG, "int32 pointers must be 4-byte aligned");
+    return launch_kv_release(*dims, page_table, ctx_lens, ref_counts, rows, keep_lens, n,
+                             reinterpret_cast<cudaStream_t>(stream));
+}
+
+size_t cs_kv_compact_workspace_bytes(const cs_page_dims* dims) {
+    if (check_pages(dims) != CS_OK) return 0;
+    return compact_workspace_bytes(*dims);
+}
+
+cs_status cs_kv_compact(const cs_page_dims* dims, const cs_page_pool* pools, int32_t n_pools, int32_t* page_table,
+                        int32_t* ref_counts, int32_t* out_live, void* workspace, size_t workspace_bytes,
+                        cs_stream_t stream) {
+    cs_status st = check_pages(dims);
+    if (st != CS_OK) return st;
+    st = check_page_pools(pools, n_pools);
+    if (st != CS_OK) return st;
+    if (!page_table || !ref_counts || !out_live) return fail(CS_ERR_INVALID_ARG, "a tensor pointer is NULL");
+    if (!aligned(page_table, 4) || !aligned(ref_counts, 4) || !aligned(out_live, 4))
+        return fail(CS_ERR_INVALID_ARG, "int32 pointers must be 4-byte aligned");
+    const size_t need = compact_workspace_bytes(*dims);
+    if (!workspace || workspace_bytes < need)
+        return fail(CS_ERR_WORKSPACE, "workspace of %zu bytes given, %zu needed", workspace_bytes, need);
+    if (!aligned(workspace, 256)) return fail(CS_ERR_INVALID_ARG, "workspace must be 256-byte aligned");
+    const StreamTurn turn(reinterpret_cast<cudaStream_t>(stream));
+    return launch_kv_compact(*dims, pools, n_pools, page_table, ref_counts, out_live, workspace,
+                             reinterpret_cast<cudaStream_t>(stream));
+}
+
+cs_status cs_logprobs(const cs_logprob_dims* dims, const void* logits, const int32_t* tokens, float temperature,
+                      float* out_logprob, float* out_entropy, int32_t* out_top_tokens, float* out_top_logprobs,
+                      cs_stream_t stream) {
+    if (!dims) return fail(CS_ERR_INVALID_ARG, "dims is NULL");
+    const cs_logprob_dims* d = dims;
+    if (d->rows < 0) return fail(CS_ERR_INVALID_ARG, "rows %d < 0", d->rows);
+    if (d->vocab <= 0) return fail(CS_ERR_INVALID_ARG, "vocab %d <= 0", d->vocab);
+    if (d->logit_dtype != CS_F32 && d->logit_dtype != CS_BF16)
+        return fail(CS_ERR_INVALID_ARG, "logit_dtype %d is neither CS_F32 nor CS_BF16", d->logit_dtype);
+    if (d->n_top < 0 || d->n_top > CS_MAX_TOP)
+        return fail(CS_ERR_INVALID_ARG, "n_top %d not in [0, %d]", d->n_top, CS_MAX_TOP);
+    if (d->rows > 1 && d->row_stride < d->vocab)
+        return fail(CS_ERR_INVALID_ARG, "row_stride %lld below the vocabulary", (long long)d->row_stride);
+    if (d->rows > 1 && d->row_stride > (1LL << 46) / d->rows)
+        return fail(CS_ERR_INVALID_ARG, "logit tensor too large");
+    if (!(temperature > 0.f) || isinf(temperature))
+        return fail(CS_ERR_INVALID_ARG, "temperature must be finite and > 0");
+    if (d->vocab > CS_MAX_VOCAB)
+        return fail(CS_ERR_UNSUPPORTED, "vocab %d (this library implements up to %d)", d->vocab, CS_MAX_VOCAB);
+    if (d->rows == 0) return CS_OK;
+    if (!logits || !tokens || !out_logprob || (d->n_top > 0 && (!out_top_tokens || !out_top_logprobs)))
+        return fail(CS_ERR_INVALID_ARG, "a tensor pointer is NULL");
+    if (!aligned(logits, d->logit_dtype == CS_F32 ? 4 : 2))
+        return fail(CS_ERR_INVALID_ARG, "logits must be aligned to their element size");
+    if (!aligned(tokens, 4) || !aligned(out_logprob, 4) || !aligned(out_entropy, 4) || !aligned(out_top_tokens, 4) ||
+        !aligned(out_top_logprobs, 4))
+        return fail(CS_ERR_INVALID_ARG, "int32/fp32 pointers must be 4-byte aligned");
+    return launch_logprobs(*d, logits, tokens, temperature, out_logprob, out_entropy, out_top_tokens,
+                           out_top_logprobs, reinterpret_cast<cudaStream_t>(stream));
 }
 
 size_t cs_route_workspace_bytes(const cs_route_dims* dims) {

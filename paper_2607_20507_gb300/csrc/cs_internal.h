@@ -106,6 +106,32 @@ cs_status launch_kv_commit_tree(const cs_attn_dims& d, void* k_pages, void* v_pa
                                 int32_t* ctx_lens, const int32_t* path, const int32_t* n_accepted, int n_nodes,
                                 cudaStream_t stream);
 
+// ---------------------------------------------------------- packed cache
+cs_status launch_packed_append(const cs_attn_dims& d, const cs_packed_pool& pool, const void* new_k, const void* new_v,
+                               const int32_t* page_table, const int32_t* ctx_lens, int n_new, cudaStream_t stream);
+cs_status launch_packed_read(const cs_attn_dims& d, const cs_packed_pool& pool, const int32_t* page_table,
+                             const int32_t* ctx_lens, int n_rows, void* out_k, void* out_v, cudaStream_t stream);
+size_t packed_attention_workspace_bytes(const cs_attn_dims& d, int rows, int sm_count);
+cs_status launch_packed_attention(const cs_attn_dims& d, const void* q, const cs_packed_pool& pool,
+                                  const int32_t* page_table, const int32_t* ctx_lens, int rows, void* out,
+                                  void* workspace, cudaStream_t stream);
+
+// ------------------------------------------------------------------ pages
+size_t fork_workspace_bytes(const cs_page_dims& d, int n);
+cs_status launch_kv_fork(const cs_page_dims& d, const cs_page_pool* pools, int n_pools, int32_t* page_table,
+                         int32_t* ctx_lens, int32_t* ref_counts, const int32_t* src, const int32_t* dst, int n,
+                         int room, int32_t* out_forked, void* workspace, cudaStream_t stream);
+cs_status launch_kv_release(const cs_page_dims& d, int32_t* page_table, int32_t* ctx_lens, int32_t* ref_counts,
+                            const int32_t* rows, const int32_t* keep_lens, int n, cudaStream_t stream);
+size_t compact_workspace_bytes(const cs_page_dims& d);
+cs_status launch_kv_compact(const cs_page_dims& d, const cs_page_pool* pools, int n_pools, int32_t* page_table,
+                            int32_t* ref_counts, int32_t* out_live, void* workspace, cudaStream_t stream);
+
+// ------------------------------------------------------ log probabilities
+cs_status launch_logprobs(const cs_logprob_dims& d, const void* logits, const int32_t* tokens, float temperature,
+                          float* out_logprob, float* out_entropy, int32_t* out_top_tokens, float* out_top_logprobs,
+                          cudaStream_t stream);
+
 // -------------------------------------------------------------- routing
 constexpr int kMaxRouteDim = CS_MAX_ROUTE_DIM;
 struct RoutePlan {

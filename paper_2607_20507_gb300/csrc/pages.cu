@@ -1,0 +1,388 @@
+// pages.cu -- pages of a cache that rows of the page table share, give back and
+// that move together (cs_kv_fork, cs_kv_release, cs_kv_compact).
+//
+// The counts alone say which pages are free, so there is no list to keep: a
+// fork takes the lowest free ids, found by a scan of the counts.  Every result
+// is a function of the inputs: places come from prefix sums, and the only
+// atomics are additions to whole numbers.
+//
+// What bounds them: a fork and a release are chains of a few dependent loads
+// and the launches; a compaction reads the counts twice and the table once and
+// then copies pages at the memory's rate.
+#include "cs_internal.h"
+#include "cs_device.cuh"
+
+namespace cs {
+namespace {
+
+struct PagePools {
+    uint4* data[CS_MAX_PAGE_POOLS];
+    uint32_t vecs[CS_MAX_PAGE_POOLS];   // 16-byte vectors of a page
+    int n;
+};
+
+struct PageParams {
+    int32_t* table;      // [R, max_pages]
+    int32_t* lens;       // [R]
+    int32_t* refs;       // [P]
+    int R, max_pages, ps, P;
+};
+
+__device__ __forceinline__ int clamped_len(const PageParams& p, int L) {
+    return max(0, min(L, p.max_pages * p.ps));
+}
+
+// Inclusive sum over the block's threads before this one, and the block's total.
+template <int kThreads>
+__device__ __forceinline__ int block_scan(int v, int* s_warp, int& total) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    int inc = v;
+#pragma unroll
+    for (int off = 1; off < 32; off <<= 1) {
+        const int y = __shfl_up_sync(0xffffffffu, inc, off);
+        if (lane >= off) inc += y;
+    }
+    __syncthreads();   // (s_warp of the scan before)
+    if (lane == 31) s_warp[warp] = inc;
+    __syncthreads();
+    int before = 0, all = 0;
+    for (int w = 0; w < kThreads / 32; ++w) {
+        const int x = s_warp[w];
+        if (w < warp) before += x;
+        all += x;
+    }
+    total = all;
+    return before + inc - v;
+}
+
+// Copies page `src` of every pool to page `dst`; thread t of n takes every n-th vector.
+__device__ __forceinline__ void copy_page(const PagePools& pools, long long src, long long dst, int t, int n) {
+    for (int i = 0; i < pools.n; ++i) {
+        const uint32_t vecs = pools.vecs[i];
+        const uint4* from = pools.data[i] + src * vecs;
+        uint4* to = pools.data[i] + dst * vecs;
+        for (uint32_t j = t; j < vecs; j += n) to[j] = __ldcg(from + j);
+    }
+}
+
+// ------------------------------------------------------------------- fork
+// What request i of a fork asks for.
+struct ForkRequest {
+    int L, full, own;    // tokens, shared full pages, pages of the new row's own
+    int src, dst;
+    bool valid;          // src is a row or -1, and dst a row
+};
+__device__ __forceinline__ ForkRequest fork_request(const PageParams& p, const int32_t* src, const int32_t* dst, int i,
+                                                    int room) {
+    ForkRequest f;
+    f.src = __ldcg(src + i);
+    f.dst = __ldcg(dst + i);
+    f.valid = f.src >= -1 && f.src < p.R && f.dst >= 0 && f.dst < p.R;
+    f.L = f.valid && f.src >= 0 ? clamped_len(p, __ldcg(p.lens + f.src)) : 0;
+    f.full = f.L / p.ps;
+    const long long end = min((long long)f.L + room, (long long)p.max_pages * p.ps);
+    f.own = f.valid ? (int)((end + p.ps - 1) / p.ps) - f.full : 0;
+    return f;
+}
+
+constexpr int kFindThreads = 1024;
+constexpr int kFindPer = 16;   // counts a thread takes at a time
+
+// One CTA: first[i], how many free pages the requests before i take, and the
+// lowest free pages, as many as all of them take (found: how many there were).
+__global__ void __launch_bounds__(kFindThreads) fork_find_kernel(const PageParams p, const int32_t* src,
+                                                                 const int32_t* dst, int n, int room,
+                                                                 long long* first, int32_t* free_ids, int* found) {
+    __shared__ int s_warp[kFindThreads / 32];
+    wait_prior_grid();
+    allow_dependent_launch();
+    long long want = 0;
+    for (int base = 0; base < n; base += kFindThreads) {
+        const int i = base + threadIdx.x;
+        const int own = i < n ? fork_request(p, src, dst, i, room).own : 0;
+        int total;
+        const int before = block_scan<kFindThreads>(own, s_warp, total);
+        if (i < n) first[i] = want + before;
+        want += total;
+    }
+    int have = 0;
+    for (long long base = 0; base < p.P && have < want; base += kFindThreads * kFindPer) {
+        const long long id = base + threadIdx.x * kFindPer;
+        uint32_t is_free = 0;
+#pragma unroll
+        for (int j = 0; j < kFindPer; ++j)
+            if (id + j < p.P && __ldcg(p.refs + id + j) == 0) is_free |= 1u << j;
+        int total;
+        int at = have + block_scan<kFindThreads>(__popc(is_free), s_warp, total);
+        for (; is_free; is_free &= is_free - 1, ++at)
+            if (at < want) free_ids[at] = (int)(id + __ffs(is_free) - 1);
+        have += total;
+    }
+    if (threadIdx.x == 0) *found = have;
+}
+
+constexpr int kForkThreads = 256;
+
+// CTA (request i, part y): part 0 writes the row; all parts copy the part-filled page.
+__global__ void __launch_bounds__(kForkThreads) fork_row_kernel(const PageParams p, const __grid_constant__ PagePools pools,
+                                                                const int32_t* src, const int32_t* dst, int room,
+                                                                const long long* first, const int32_t* free_ids,
+                                                                const int* found, int32_t* out_forked) {
+    const int i = blockIdx.x;
+    wait_prior_grid();
+    allow_dependent_launch();
+    const ForkRequest f = fork_request(p, src, dst, i, room);
+    const long long at = __ldcg(first + i);
+    const bool ok = f.valid && at + f.own <= __ldcg(found);
+    const int32_t* from = p.table + (size_t)max(f.src, 0) * p.max_pages;
+    if (blockIdx.y == 0) {
+        if (threadIdx.x == 0) out_forked[i] = ok;
+        if (f.dst >= 0 && f.dst < p.R) {
+            int32_t* to = p.table + (size_t)f.dst * p.max_pages;
+            if (threadIdx.x == 0) p.lens[f.dst] = ok ? f.L : 0;
+            for (int j = threadIdx.x; j < p.max_pages; j += kForkThreads) {
+                int id = -1;
+                if (ok && j < f.full) {
+                    id = __ldcg(from + j);
+                    if (id >= 0 && id < p.P) atomicAdd(p.refs + id, 1);
+                } else if (ok && j < f.full + f.own) {
+                    id = __ldcg(free_ids + at + (j - f.full));
+                    p.refs[id] = 1;
+                }
+                to[j] = id;
+            }
+        }
+    }
+    if (ok && f.L % p.ps != 0) {
+        const int old = __ldcg(from + f.full);
+        if (old >= 0 && old < p.P)
+            copy_page(pools, old, __ldcg(free_ids + at), blockIdx.y * kForkThreads + threadIdx.x,
+                      gridDim.y * kForkThreads);
+    }
+}
+
+// ---------------------------------------------------------------- release
+constexpr int kReleaseThreads = 256;
+
+__global__ void __launch_bounds__(kReleaseThreads) release_kernel(const PageParams p, const int32_t* rows,
+                                                                  const int32_t* keep_lens) {
+    wait_prior_grid();
+    allow_dependent_launch();
+    const int r = __ldcg(rows + blockIdx.x);
+    if (r < 0 || r >= p.R) return;
+    const int keep = clamped_len(p, __ldcg(keep_lens + blockIdx.x));
+    int32_t* row = p.table + (size_t)r * p.max_pages;
+    if (threadIdx.x == 0) p.lens[r] = min(__ldcg(p.lens + r), keep);
+    for (int j = (keep + p.ps - 1) / p.ps + threadIdx.x; j < p.max_pages; j += kReleaseThreads) {
+        const int id = __ldcg(row + j);
+        if (id >= 0 && id < p.P) atomicSub(p.refs + id, 1);
+        row[j] = -1;
+    }
+}
+
+// ---------------------------------------------------------------- compact
+constexpr int kCountThreads = 256;
+constexpr int kCountPer = 16;
+constexpr int kCountTile = kCountThreads * kCountPer;   // pages a CTA counts
+
+struct CompactParams {
+    int* tile_live;      // [tiles] pages in use in each tile of counts
+    int32_t* src;        // [P] the moving pages, ascending (as many as move)
+    int32_t* dst;        // [P] where they go
+    int32_t* rank;       // [P] of an id >= N: its place in src, -1 if it does not move
+    int* n_moved;
+    int tiles;
+};
+
+__device__ __forceinline__ uint32_t live_bits(const PageParams& p, long long id) {
+    uint32_t live = 0;
+#pragma unroll
+    for (int j = 0; j < kCountPer; ++j)
+        if (id + j < p.P && __ldcg(p.refs + id + j) != 0) live |= 1u << j;
+    return live;
+}
+
+__global__ void __launch_bounds__(kCountThreads) compact_count_kernel(const PageParams p, const CompactParams c) {
+    __shared__ int s_warp[kCountThreads / 32];
+    wait_prior_grid();
+    allow_dependent_launch();
+    int total;
+    block_scan<kCountThreads>(__popc(live_bits(p, (long long)blockIdx.x * kCountTile + threadIdx.x * kCountPer)), s_warp,
+                              total);
+    if (threadIdx.x == 0) c.tile_live[blockIdx.x] = total;
+}
+
+// The place of every page that moves and of every free page that takes one:
+// a page in use with id >= N is the (pages in use before it, less those below
+// N)-th of the first, a free page below N the (id less pages in use before it)-th
+// of the second.
+__global__ void __launch_bounds__(kCountThreads) compact_rank_kernel(const PageParams p, const CompactParams c,
+                                                                     int32_t* out_live) {
+    __shared__ int s_warp[kCountThreads / 32];
+    wait_prior_grid();
+    allow_dependent_launch();
+    auto sum = [&](int v) {
+        int total;
+        block_scan<kCountThreads>(v, s_warp, total);
+        return total;
+    };
+    int before = 0, all = 0;
+    for (int t = threadIdx.x; t < c.tiles; t += kCountThreads) {
+        const int x = __ldcg(c.tile_live + t);
+        all += x;
+        if (t < (int)blockIdx.x) before += x;
+    }
+    const int N = sum(all);
+    before = sum(before);
+    // pages in use below N: the tiles before N's, and N's tile up to it
+    const int tile_n = N / kCountTile;
+    int below = 0;
+    for (int t = threadIdx.x; t < tile_n; t += kCountThreads) below += __ldcg(c.tile_live + t);
+    {
+        const long long id = (long long)tile_n * kCountTile + threadIdx.x * kCountPer;
+        const uint32_t live = live_bits(p, id);
+#pragma unroll
+        for (int j = 0; j < kCountPer; ++j)
+            if (id + j < N && (live >> j & 1)) ++below;
+    }
+    below = sum(below);
+    const long long id0 = (long long)blockIdx.x * kCountTile + threadIdx.x * kCountPer;
+    const uint32_t live = live_bits(p, id0);
+    int total;
+    int at = before + block_scan<kCountThreads>(__popc(live), s_warp, total);
+#pragma unroll
+    for (int j = 0; j < kCountPer; ++j) {
+        const int id = (int)(id0 + j);
+        if (id0 + j >= p.P) break;
+        const bool on = live >> j & 1;
+        if (id < N && !on) c.dst[id - at] = id;
+        if (id >= N) {
+            c.rank[id] = on ? at - below : -1;
+            if (on) c.src[at - below] = id;
+        }
+        at += on;
+    }
+    if (blockIdx.x == 0 && threadIdx.x == 0) {
+        *out_live = N;
+        *c.n_moved = N - below;
+    }
+}
+
+constexpr int kMoveThreads = 256;
+
+// The first `copy_ctas` CTAs copy pages, the others rename table entries.
+__global__ void __launch_bounds__(kMoveThreads) compact_move_kernel(const PageParams p,
+                                                                    const __grid_constant__ PagePools pools,
+                                                                    const CompactParams c, const int32_t* live,
+                                                                    int copy_ctas) {
+    wait_prior_grid();
+    allow_dependent_launch();
+    if ((int)blockIdx.x < copy_ctas) {
+        const int moved = __ldcg(c.n_moved);
+        for (int r = blockIdx.x; r < moved; r += copy_ctas) {
+            const int from = __ldcg(c.src + r), to = __ldcg(c.dst + r);
+            copy_page(pools, from, to, threadIdx.x, kMoveThreads);
+            if (threadIdx.x == 0) {
+                p.refs[to] = __ldcg(p.refs + from);
+                p.refs[from] = 0;
+            }
+        }
+        return;
+    }
+    const int N = __ldcg(live);
+    const long long entries = (long long)p.R * p.max_pages;
+    for (long long e = (long long)(blockIdx.x - copy_ctas) * kMoveThreads + threadIdx.x; e < entries;
+         e += (long long)(gridDim.x - copy_ctas) * kMoveThreads) {
+        const int id = __ldcg(p.table + e);
+        if (id < N || id >= p.P) continue;
+        const int r = __ldcg(c.rank + id);
+        if (r >= 0) p.table[e] = __ldcg(c.dst + r);
+    }
+}
+
+size_t align256(size_t n) { return (n + 255) & ~size_t(255); }
+
+PageParams page_params(const cs_page_dims& d, int32_t* table, int32_t* lens, int32_t* refs) {
+    PageParams p{};
+    p.table = table;
+    p.lens = lens;
+    p.refs = refs;
+    p.R = d.rows;
+    p.max_pages = d.max_pages_per_seq;
+    p.ps = d.page_size;
+    p.P = d.num_pages;
+    return p;
+}
+
+PagePools page_pools(const cs_page_pool* pools, int n) {
+    PagePools q{};
+    for (int i = 0; i < n; ++i) {
+        q.data[i] = static_cast<uint4*>(pools[i].data);
+        q.vecs[i] = (uint32_t)(pools[i].page_bytes / 16);
+    }
+    q.n = n;
+    return q;
+}
+
+int tiles_of_counts(int P) { return (P + kCountTile - 1) / kCountTile; }
+
+}  // namespace
+
+// found (256 B), first [n], the free pages (at most all)
+size_t fork_workspace_bytes(const cs_page_dims& d, int n) {
+    return 256 + align256(sizeof(long long) * (size_t)n) + align256(sizeof(int32_t) * (size_t)d.num_pages);
+}
+
+cs_status launch_kv_fork(const cs_page_dims& d, const cs_page_pool* pools, int n_pools, int32_t* page_table,
+                         int32_t* ctx_lens, int32_t* ref_counts, const int32_t* src, const int32_t* dst, int n,
+                         int room, int32_t* out_forked, void* workspace, cudaStream_t stream) {
+    uint8_t* ws = static_cast<uint8_t*>(workspace);
+    int* found = reinterpret_cast<int*>(ws);
+    long long* first = reinterpret_cast<long long*>(ws + 256);
+    int32_t* free_ids = reinterpret_cast<int32_t*>(ws + 256 + align256(sizeof(long long) * (size_t)n));
+    const PageParams p = page_params(d, page_table, ctx_lens, ref_counts);
+    cudaError_t e = launch_dependent(fork_find_kernel, dim3(1), dim3(kFindThreads), 0, stream, p, src, dst, n, room,
+                                     first, free_ids, found);
+    if (e != cudaSuccess) return cuda_fail(e, "fork_find_kernel launch");
+    e = launch_dependent(fork_row_kernel, dim3(n, 4), dim3(kForkThreads), 0, stream, p, page_pools(pools, n_pools), src,
+                         dst, room, (const long long*)first, (const int32_t*)free_ids, (const int*)found, out_forked);
+    return e == cudaSuccess ? CS_OK : cuda_fail(e, "fork_row_kernel launch");
+}
+
+cs_status launch_kv_release(const cs_page_dims& d, int32_t* page_table, int32_t* ctx_lens, int32_t* ref_counts,
+                            const int32_t* rows, const int32_t* keep_lens, int n, cudaStream_t stream) {
+    const cudaError_t e = launch_dependent(release_kernel, dim3(n), dim3(kReleaseThreads), 0, stream,
+                                           page_params(d, page_table, ctx_lens, ref_counts), rows, keep_lens);
+    return e == cudaSuccess ? CS_OK : cuda_fail(e, "release_kernel launch");
+}
+
+// n_moved (256 B), tile counts, src, dst, rank
+size_t compact_workspace_bytes(const cs_page_dims& d) {
+    return 256 + align256(sizeof(int) * (size_t)tiles_of_counts(d.num_pages)) +
+           3 * align256(sizeof(int32_t) * (size_t)d.num_pages);
+}
+
+cs_status launch_kv_compact(const cs_page_dims& d, const cs_page_pool* pools, int n_pools, int32_t* page_table,
+                            int32_t* ref_counts, int32_t* out_live, void* workspace, cudaStream_t stream) {
+    uint8_t* ws = static_cast<uint8_t*>(workspace);
+    const size_t ids = align256(sizeof(int32_t) * (size_t)d.num_pages);
+    CompactParams c{};
+    c.tiles = tiles_of_counts(d.num_pages);
+    c.n_moved = reinterpret_cast<int*>(ws);
+    c.tile_live = reinterpret_cast<int*>(ws + 256);
+    ws += 256 + align256(sizeof(int) * (size_t)c.tiles);
+    c.src = reinterpret_cast<int32_t*>(ws);
+    c.dst = reinterpret_cast<int32_t*>(ws + ids);
+    c.rank = reinterpret_cast<int32_t*>(ws + 2 * ids);
+    const PageParams p = page_params(d, page_table, nullptr, ref_counts);
+    cudaError_t e = launch_dependent(compact_count_kernel, dim3(c.tiles), dim3(kCountThreads), 0, stream, p, c);
+    if (e != cudaSuccess) return cuda_fail(e, "compact_count_kernel launch");
+    e = launch_dependent(compact_rank_kernel, dim3(c.tiles), dim3(kCountThreads), 0, stream, p, c, out_live);
+    if (e != cudaSuccess) return cuda_fail(e, "compact_rank_kernel launch");
+    const int sms = current_sm_count();
+    e = launch_dependent(compact_move_kernel, dim3(8 * sms), dim3(kMoveThreads), 0, stream, p, page_pools(pools, n_pools),
+                         c, (const int32_t*)out_live, 7 * sms);
+    return e == cudaSuccess ? CS_OK : cuda_fail(e, "compact_move_kernel launch");
+}
+
+}  // namespace cs
