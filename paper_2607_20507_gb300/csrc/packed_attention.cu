@@ -2,10 +2,39 @@
 // (cs_packed_verify_attention): o = softmax_j(scale q . K_j) V_j with K and V
 // the values that the codes stand for (packed.cuh).
 //
-// One CTA per (request, query head, draft row); its warps take every fourth
-// key each, a lane four dims, with a running maximum and sum each, joined in
-// shared memory at the end.
+// Work split.  A span is one (request, KV head); its keys go in tiles of
+// kTeams x 16.  The grid holds the CTAs that are resident at once, and each
+// takes an equal share of all tiles (a span's start counts as `span_x` more).
+// A span that lies in one CTA is written there; one that is cut leaves each
+// piece's normalised output and (maximum, sum), which packed_merge_kernel joins.
+//
+// Per CTA: teams of kRG warps, each with a ring of kStages tiles of 16 keys in
+// shared memory, filled by cp.async (a page piece of 16 keys is 1 KB of codes
+// and 128 bytes of scales for K and for V: too little for a bulk copy each).
+// A warp holds up to 8 kNT query rows; kRG warps share a tile where there are
+// more.
+//
+// Per warp and tile, transposed products on mma.sync (m16n8k16, fp16 operands,
+// fp32 sums), so that the padding is to 8 query rows and not to 16:
+//   S^T [16 keys x 8 rows] = K Q^T   lane (r, c) = (lane / 4, lane % 4) takes keys
+//       r and r + 8 and dims 32 c .. 32 c + 31: 16 bytes of codes a key, which
+//       become the eight A fragments in registers.  The dims of a k-step are
+//       any 16, the same ones for K and Q, so no code moves between lanes.
+//   O^T [16 dims x 8 rows] += V^T P^T  lane (r, c) takes keys 2c, 2c+1, 2c+8, 2c+9
+//       and dims 16 r .. 16 r + 15, one scale group: 8 bytes of codes and one
+//       scale a key.  The codes of two keys are paired by nibbles (two shifts
+//       and two selections for 16 codes) before they become fp16 pairs.
+// P^T is S^T's accumulator after movmatrix.  Codes become fp16 by one
+// conversion a pair and one product with their scale, both exact.
+//
+// The running maximum of a row grows only when a score passes it by 2^3 (then
+// the sums are rescaled): P = 2^(s - m + 12) lies between 2^-14 and 2^15, where
+// fp16 has 11 bits, for weights down to 2^-26 of the largest.  A tile with
+// smaller ones takes another turn for them (faint, below): an output may rest
+// on them where the codes of the heavier keys are 0.
 #include <math.h>
+
+#include <type_traits>
 
 #include "cs_internal.h"
 #include "packed.cuh"
@@ -13,7 +42,20 @@
 namespace cs {
 namespace {
 
-constexpr int kWarps = 4;
+constexpr int kSub = 16;                            // keys of a team's tile
+constexpr int kStages = 4;
+constexpr int kCodes = kSub * kPackCodeBytes;       // 1024 bytes of codes of K or V
+constexpr int kScales = kSub * kPackGroups;         // 128 bytes of scales
+constexpr int kStageBytes = 2 * (kCodes + kScales);
+constexpr int kMaxBatchPerLaunch = 1024;            // requests whose schedule one launch holds
+constexpr int kMaxGrid = 1024;                      // CTAs of a launch at most
+constexpr float kPUp = 12.f;                        // P = 2^(s - m + kPUp)
+constexpr float kPMax = 15.f;                       // the maximum follows a score that passes 2^kPMax
+constexpr float kPMin = -14.f;                      // weights below 2^kPMin are faint: less than 11 bits in fp16
+
+struct Job {             // a cut span that starts in a CTA: its pieces lie in slot0 and the first slots of the CTAs after it
+    int b, h, slot0, n;
+};
 
 struct PackedAttnParams {
     const __nv_bfloat16* q;      // [B, R, Hq, D]
@@ -26,79 +68,708 @@ struct PackedAttnParams {
     const float* v_head;
     const int32_t* page_table;   // [B, max_pages]
     const int32_t* ctx_lens;     // [B]
-    int Hq, Hkv, G, R, ps, max_pages, P;
+    float* part_o;               // [2 grid, n_rows, D] a CTA's first and last piece
+    float2* part_ml;             // [2 grid, n_rows] (maximum in log2 units, sum)
+    Job* jobs;                   // [grid]
+    int Hq, Hkv, G, R, n_rows, ps, ps_log2, max_pages, P;
+    int b_base, n_batch, span_x;
     float scale_log2;            // sm_scale * log2(e)
 };
 
-__device__ __forceinline__ void four_dims(const uint8_t* codes, const uint8_t* scales, size_t slot, int lane,
-                                          float (&x)[4]) {
-    const uint32_t c = __ldcg(reinterpret_cast<const uint16_t*>(codes + slot * kPackCodeBytes) + lane);
-    const uint32_t s = __ldcg(scales + slot * kPackGroups + lane / 4);
-    const uint32_t sc = scales_f16x2(s | s << 8);
-    const uint32_t a = mul_f16x2(codes_f16x2<0>(c), sc), b = mul_f16x2(codes_f16x2<1>(c), sc);
-    x[0] = f16_lo(a);
-    x[1] = f16_hi(a);
-    x[2] = f16_lo(b);
-    x[3] = f16_hi(b);
+// warps that share a tile's keys by query rows, and what follows from the count
+template <int kNT, int kRG>
+struct Form {
+    static constexpr int kTeams = kRG <= 2 ? 4 : 2;
+    static constexpr int kThreads = kTeams * kRG * 32;
+    static constexpr int kTile = kTeams * kSub;
+    static constexpr int kRows = kRG * kNT * 8;
+    static constexpr int kMinBlocks = kRG == 1 ? (kNT == 1 ? 4 : kNT == 2 ? 3 : 2) : kRG == 3 ? 2 : 1;
+    static constexpr int kRing = kTeams * kStages * kStageBytes;
+    static constexpr int kQ = kRows * kPackDim * 2;
+    static constexpr int kFold = kTeams / 2 * kRows * kPackDim * 4 + kTeams / 2 * kRG * kNT * 32 * 16;
+    static constexpr int kSmem = kRing + kQ + kFold + kRows * 8 + kMaxBatchPerLaunch * 4;
+    static_assert(kRing >= (kMaxBatchPerLaunch + 1) * 8, "the prefix lies in the ring at the start");
+};
+
+struct Cursor {
+    int b, h, t, T;
+};
+
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool in) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(in ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int kLeft>
+__device__ __forceinline__ void cp_async_wait() {
+    asm volatile("cp.async.wait_group %0;" ::"n"(kLeft) : "memory");
 }
 
-__global__ void __launch_bounds__(kWarps * 32) packed_attention_kernel(const PackedAttnParams p) {
-    __shared__ float s_o[kWarps][kPackDim];
-    __shared__ float s_m[kWarps], s_l[kWarps];
+__device__ __forceinline__ void mma_f16_16816(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+    asm volatile(
+        "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, "
+        "{%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+// an 8 x 8 matrix of 16-bit values over the warp, transposed
+__device__ __forceinline__ uint32_t transpose_8x8(uint32_t x) {
+    uint32_t r;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(x));
+    return r;
+}
+__device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi) {
+    uint32_t r;
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+// the low four bits of every byte from a, the high four from b
+__device__ __forceinline__ uint32_t nibbles(uint32_t a, uint32_t b) { return (a & 0x0f0f0f0fu) | (b & 0xf0f0f0f0u); }
+
+// Byte offset of 16-byte part `part` of a key's V codes: with the rows and the
+// parts exchanged by the key's bits, the eight-byte loads of a half warp (keys
+// 0, 2, 4, 6 and one half of the dims) meet every bank once.
+__device__ __forceinline__ int v_at(int key, int part) {
+    return (key ^ (key >> 2 & 1)) * kPackCodeBytes + (part ^ (key & 2)) * 16;
+}
+
+// Tiles of a request of L keys, its spans' units before request b (prefix) and
+// the position of unit v.
+struct Share {
+    Cursor first;
+    int n_tiles;
+};
+__device__ __forceinline__ int tiles_of(int L, int tile) { return max(1, (L + tile - 1) / tile); }
+
+// The first unit of CTA c of G.
+__device__ __forceinline__ long long first_unit(int c, long long U, int G) { return div_pos((long long)c * U, G); }
+// The CTA that holds unit v.
+__device__ __forceinline__ int owner_of(long long v, long long U, int G) {
+    return (int)div_pos((v + 1) * G + U - 1, U) - 1;
+}
+
+// The share of CTA c of G, by one warp: even lanes place its first unit, odd
+// ones the unit past its last (lanes compare 32 requests' starts at a time).
+__device__ __forceinline__ Share share_of(int c, long long U, int G, const long long* prefix, const int* lens, int nb,
+                                          int Hkv, int X, int tile) {
+    const int lane = threadIdx.x & 31;
+    const long long v = first_unit(c + (lane & 1), U, G);
+    Cursor cur{};
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+        const long long ve = __shfl_sync(0xffffffffu, v, e);
+        const int far = lane * 32;
+        const int blk = nb > 32 ? 31 - __clz(__ballot_sync(0xffffffffu, far < nb && prefix[far] <= ve)) : 0;
+        const int b = blk * 32 + lane;
+        const int at = blk * 32 + 31 - __clz(__ballot_sync(0xffffffffu, b < nb && prefix[b] <= ve));
+        if ((lane & 1) == e) cur.b = at;
+    }
+    cur.T = tiles_of(lens[cur.b], tile);
+    const long long local = v - prefix[cur.b];
+    cur.h = (int)div_pos(local, cur.T + X);     // Hkv: past the last unit
+    const int in = (int)(local - (long long)cur.h * (cur.T + X));
+    cur.t = in > X ? in - X : 0;
+    const long long before = prefix[cur.b] - (long long)X * Hkv * cur.b + (long long)cur.h * cur.T + cur.t;
+    Share s;
+    s.n_tiles = (int)(__shfl_sync(0xffffffffu, before, 1) - __shfl_sync(0xffffffffu, before, 0));
+    s.first.b = __shfl_sync(0xffffffffu, cur.b, 0);
+    s.first.h = __shfl_sync(0xffffffffu, cur.h, 0);
+    s.first.t = __shfl_sync(0xffffffffu, cur.t, 0);
+    s.first.T = __shfl_sync(0xffffffffu, cur.T, 0);
+    return s;
+}
+
+__device__ __forceinline__ void advance(Cursor& c, const int* lens, int nb, int Hkv, int tile) {
+    if (++c.t < c.T) return;
+    c.t = 0;
+    if (++c.h < Hkv) return;
+    c.h = 0;
+    if (++c.b < nb) c.T = tiles_of(lens[c.b], tile);
+}
+
+template <int kNT, int kRG>
+__global__ void __launch_bounds__(Form<kNT, kRG>::kThreads, Form<kNT, kRG>::kMinBlocks)
+packed_attention_kernel(const PackedAttnParams p) {
+    using F = Form<kNT, kRG>;
+    extern __shared__ uint4 smem_raw[];
+    uint8_t* smem = reinterpret_cast<uint8_t*>(smem_raw);
+    uint4* s_q = reinterpret_cast<uint4*>(smem + F::kRing);                       // [row tile][4][lane] B fragments
+    float4* s_fold = reinterpret_cast<float4*>(smem + F::kRing + F::kQ);
+    float* s_scale = reinterpret_cast<float*>(smem + F::kRing + F::kQ + F::kFold);   // [row] of the scores
+    int* s_draft = reinterpret_cast<int*>(s_scale + F::kRows);                    // [row] draft position
+    int* s_len = s_draft + F::kRows;
+    long long* s_prefix = reinterpret_cast<long long*>(smem);
+    __shared__ long long s_wsum[F::kThreads / 32];
+
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int h = blockIdx.x, i = blockIdx.y, b = blockIdx.z;
-    const int hk = h / p.G;
+    const int team = warp / kRG, rg = warp % kRG;
+    const int r = lane >> 2, c = lane & 3;
+    const int nb = p.n_batch, X0 = p.span_x;
     wait_prior_grid();
     allow_dependent_launch();
-    const int L = max(0, min(__ldcg(p.ctx_lens + b), p.max_pages * p.ps));
-    const int n_keys = max(0, L - p.R + 1 + i);
-    const size_t row = (((size_t)b * p.R + i) * p.Hq + h) * kPackDim + 4 * lane;
-    const float c = p.scale_log2 * (p.k_head ? __ldcg(p.k_head + hk) : 1.f);
-    float q[4], o[4] = {0.f, 0.f, 0.f, 0.f}, m = kNegInf, l = 0.f;
-    for (int d = 0; d < 4; ++d) q[d] = __bfloat162float(p.q[row + d]);
-    for (int j = warp; j < n_keys; j += kWarps) {
-        const int page = __ldcg(p.page_table + (size_t)b * p.max_pages + j / p.ps);
-        const bool in = page >= 0 && page < p.P;
-        const size_t slot = in ? ((size_t)page * p.Hkv + hk) * p.ps + j % p.ps : 0;
-        float k[4] = {0.f, 0.f, 0.f, 0.f}, v[4] = {0.f, 0.f, 0.f, 0.f};
-        if (in) {
-            four_dims(p.k_codes, p.k_scales, slot, lane, k);
-            four_dims(p.v_codes, p.v_scales, slot, lane, v);
+
+    // ---- the requests' tiles: lengths, and where each request's units start
+    long long carry = 0, W = 0;
+    for (int base = 0; base < nb; base += F::kThreads) {
+        const int b = base + threadIdx.x;
+        long long v = 0;
+        if (b < nb) {
+            const int L = max(0, min(__ldcg(p.ctx_lens + p.b_base + b), p.max_pages * p.ps));
+            s_len[b] = L;
+            v = (long long)tiles_of(L, F::kTile) * p.Hkv;
         }
-        float s = q[0] * k[0] + q[1] * k[1] + q[2] * k[2] + q[3] * k[3];
-        for (int off = 16; off > 0; off >>= 1) s += __shfl_xor_sync(0xffffffffu, s, off);
-        s *= c;
-        const float mn = fmaxf(m, s), a = ex2(m - mn), w = ex2(s - mn);
-        l = l * a + w;
-        for (int d = 0; d < 4; ++d) o[d] = o[d] * a + w * v[d];
-        m = mn;
+        long long inc = v;
+#pragma unroll
+        for (int off = 1; off < 32; off <<= 1) {
+            const long long y = __shfl_up_sync(0xffffffffu, inc, off);
+            if (lane >= off) inc += y;
+        }
+        if (lane == 31) s_wsum[warp] = inc;
+        __syncthreads();
+        long long before = carry, all = 0;
+        for (int w = 0; w < F::kThreads / 32; ++w) {
+            if (w < warp) before += s_wsum[w];
+            all += s_wsum[w];
+        }
+        if (b < nb) s_prefix[b] = before + inc - v;
+        carry += all;
+        __syncthreads();
     }
-    for (int d = 0; d < 4; ++d) s_o[warp][4 * lane + d] = o[d];
-    if (lane == 0) {
-        s_m[warp] = m;
-        s_l[warp] = l;
+    W = carry;
+    // few tiles: one a CTA; else a span's start counts as X tiles
+    const int grid = gridDim.x, cta = blockIdx.x;
+    const bool few = W <= grid;
+    const int X = few ? 0 : X0, Gc = few ? (int)W : grid;
+    if (threadIdx.x == 0) p.jobs[cta].n = 0;
+    if (cta >= Gc) return;
+    if (X > 0) {
+        for (int b = threadIdx.x; b < nb; b += F::kThreads) s_prefix[b] += (long long)X * p.Hkv * b;
+        __syncthreads();
     }
-    __syncthreads();
-    if (warp != 0) return;
-    float M = kNegInf, sum = 0.f, r[4] = {0.f, 0.f, 0.f, 0.f};
-    for (int w = 0; w < kWarps; ++w) M = fmaxf(M, s_m[w]);
-    for (int w = 0; w < kWarps && M != kNegInf; ++w) {
-        const float a = ex2(s_m[w] - M);
-        sum += s_l[w] * a;
-        for (int d = 0; d < 4; ++d) r[d] += s_o[w][4 * lane + d] * a;
+    const long long U = W + (long long)X * p.Hkv * nb;
+    const Share share = share_of(cta, U, Gc, s_prefix, s_len, nb, p.Hkv, X, F::kTile);
+    const int n_tiles = share.n_tiles;
+    // where the span that ends this share starts, in units (for its pieces below)
+    __syncthreads();   // the prefix gives way to the ring
+    if (n_tiles <= 0) return;
+    for (int row = threadIdx.x; row < F::kRows; row += F::kThreads) s_draft[row] = row / p.G;
+
+    // ---- the ring
+    uint8_t* ring = smem + team * (kStages * kStageBytes);
+    const uint32_t ring_a = smem_u32(ring);
+    Cursor ci = share.first;     // of the next tile to load
+    Cursor cn = share.first;     // of the tile whose pages are looked up next
+    int next_a = -1, next_b = -1, next2_a = -1, next2_b = -1;   // the pages of the next two tiles to load
+    int looked = 0;
+    auto look_up = [&](int& pa, int& pb) {   // the pages of keys 0-7 and 8-15 of cn's tile
+        pa = pb = -1;
+        if (looked++ >= n_tiles) return;
+        const int key = cn.t * F::kTile + team * kSub, L = s_len[cn.b];
+        const int32_t* row = p.page_table + (size_t)(p.b_base + cn.b) * p.max_pages;
+        if (key < L) pa = __ldcg(row + (key >> p.ps_log2));
+        if (p.ps >= kSub) pb = pa;
+        else if (key + 8 < L) pb = __ldcg(row + ((key + 8) >> p.ps_log2));
+        advance(cn, s_len, nb, p.Hkv, F::kTile);
+    };
+    constexpr int kLoaders = kRG == 1 ? 1 : 2;
+    int issued = 0;
+    auto issue = [&]() {
+        if (rg < kLoaders && issued < n_tiles) {
+            const int pa = next_a, pb = next_b;
+            next_a = next2_a;
+            next_b = next2_b;
+            look_up(next2_a, next2_b);
+            const int key = ci.t * F::kTile + team * kSub;
+            if (key < s_len[ci.b]) {
+                const uint32_t st = ring_a + (issued % kStages) * kStageBytes;
+                const int slot = key & (p.ps - 1);
+                const bool in_a = pa >= 0 && pa < p.P, in_b = pb >= 0 && pb < p.P;
+                const size_t row_a = in_a ? ((size_t)pa * p.Hkv + ci.h) * p.ps + slot : 0;
+                const size_t row_b = in_b ? ((size_t)pb * p.Hkv + ci.h) * p.ps + (p.ps >= kSub ? slot + 8 : 0) : 0;
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    if (kLoaders == 2 && i != rg) continue;
+                    const size_t row = (i ? row_b : row_a) + r;
+                    const bool in = i ? in_b : in_a;
+                    cp_async16(st + (8 * i + r) * kPackCodeBytes + c * 16, p.k_codes + row * kPackCodeBytes + c * 16, in);
+                    cp_async16(st + kCodes + v_at(8 * i + r, c), p.v_codes + row * kPackCodeBytes + c * 16, in);
+                }
+                if (rg == 0 && lane < 16) {
+                    const bool second = lane & 4, in = second ? in_b : in_a;
+                    const size_t at = (second ? row_b : row_a) * kPackGroups + (lane & 3) * 16;
+                    cp_async16(st + 2 * kCodes + lane * 16, (lane & 8 ? p.v_scales : p.k_scales) + at, in);
+                }
+            }
+            advance(ci, s_len, nb, p.Hkv, F::kTile);
+        }
+        ++issued;
+        cp_async_commit();
+    };
+    auto team_sync = [&]() {
+        if constexpr (kRG == 1) __syncwarp();
+        else asm volatile("bar.sync %0, %1;" ::"r"(1 + team), "n"(kRG * 32) : "memory");
+    };
+    if (rg < kLoaders) {
+        look_up(next_a, next_b);
+        look_up(next2_a, next2_b);
     }
-    const float inv = sum > 0.f ? (p.v_head ? __ldcg(p.v_head + hk) : 1.f) / sum : 0.f;
-    *reinterpret_cast<uint2*>(p.out + row) =
-        make_uint2(pack_bf16x2(r[0] * inv, r[1] * inv), pack_bf16x2(r[2] * inv, r[3] * inv));
+    for (int i = 0; i < kStages - 1; ++i) issue();
+
+    // ---- spans
+    Cursor cur = share.first;
+    int done = 0;
+    bool first_piece = true;
+    while (done < n_tiles) {
+        const int n = min(cur.T - cur.t, n_tiles - done);
+        const int bg = p.b_base + cur.b, L = s_len[cur.b];
+        // the query rows in fp16, brought below 2^15 by a power of two each
+        for (int row = warp; row < F::kRows; row += F::kThreads / 32) {
+            uint2 x = make_uint2(0, 0);
+            if (row < p.n_rows) {
+                const int i = s_draft[row];
+                const uint32_t* src = reinterpret_cast<const uint32_t*>(
+                    p.q + (((size_t)bg * p.R + i) * p.Hq + (size_t)cur.h * p.G + (row - i * p.G)) * kPackDim + 4 * lane);
+                x.x = __ldcg(src);
+                x.y = __ldcg(src + 1);
+            }
+            float f[4] = {__uint_as_float(x.x << 16), __uint_as_float(x.x & 0xffff0000u), __uint_as_float(x.y << 16),
+                          __uint_as_float(x.y & 0xffff0000u)};
+            float top = fmaxf(fmaxf(fabsf(f[0]), fabsf(f[1])), fmaxf(fabsf(f[2]), fabsf(f[3])));
+#pragma unroll
+            for (int off = 16; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
+            // top = 1.m x 2^e -> 1.m x 2^14; the factors 2^(14 - e) in two halves,
+            // neither of which leaves fp32 for any e
+            const int e = (int)(__float_as_uint(top) >> 23) - 127;
+            const int up = top > 0.f ? 14 - e : 0, u0 = up / 2, u1 = up - u0;
+            const float s0 = __uint_as_float((uint32_t)(127 + u0) << 23), s1 = __uint_as_float((uint32_t)(127 + u1) << 23);
+            const uint2 y = make_uint2(pack_f16x2(f[0] * s0 * s1, f[1] * s0 * s1), pack_f16x2(f[2] * s0 * s1, f[3] * s0 * s1));
+            uint4* at = s_q + ((row >> 3) * 4 + ((lane & 7) >> 1)) * 32 + (row & 7) * 4 + (lane >> 3);
+            reinterpret_cast<uint2*>(at)[lane & 1] = y;
+            if (lane == 0) {
+                const float d0 = __uint_as_float((uint32_t)(127 - u0) << 23), d1 = __uint_as_float((uint32_t)(127 - u1) << 23);
+                s_scale[row] = p.scale_log2 * d0 * (p.k_head ? __ldcg(p.k_head + cur.h) : 1.f) * d1;
+            }
+        }
+        __syncthreads();
+
+        float o[kNT][8][4], m[kNT][2], l[kNT][2], sc_f[kNT][2];
+#pragma unroll
+        for (int nt = 0; nt < kNT; ++nt) {
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                m[nt][e] = kNegInf;
+                l[nt][e] = 0.f;
+                sc_f[nt][e] = s_scale[(rg * kNT + nt) * 8 + 2 * c + e];
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[nt][i][e] = 0.f;
+        }
+        const uint4* q_frag = s_q + rg * kNT * 4 * 32 + lane;
+
+        for (int t = 0; t < n; ++t) {
+            cp_async_wait<kStages - 2>();
+            team_sync();
+            const uint8_t* st = ring + ((done + t) % kStages) * kStageBytes;
+            issue();   // into the stage that the team left before the barrier
+            const int key0 = (cur.t + t) * F::kTile + team * kSub;
+            if (key0 >= L) continue;
+
+            // ---- S^T = K Q^T
+            float s[kNT][4];
+#pragma unroll
+            for (int nt = 0; nt < kNT; ++nt)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) s[nt][e] = 0.f;
+            {
+                const uint4 k0 = *reinterpret_cast<const uint4*>(st + r * kPackCodeBytes + c * 16);
+                const uint4 k1 = *reinterpret_cast<const uint4*>(st + (r + 8) * kPackCodeBytes + c * 16);
+                const uint8_t* ks = st + 2 * kCodes + r * kPackGroups + 2 * c;
+                const uint32_t f0 = scales_f16x2(*reinterpret_cast<const uint16_t*>(ks));
+                const uint32_t f1 = scales_f16x2(*reinterpret_cast<const uint16_t*>(ks + 8 * kPackGroups));
+                const uint32_t w0[4] = {k0.x, k0.y, k0.z, k0.w}, w1[4] = {k1.x, k1.y, k1.z, k1.w};
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {   // k-steps 2i, 2i + 1: dims 32 c + 8 i ...
+                    const uint32_t g0 = __byte_perm(f0, 0, i < 2 ? 0x1010 : 0x3232);
+                    const uint32_t g1 = __byte_perm(f1, 0, i < 2 ? 0x1010 : 0x3232);
+                    const uint32_t a[2][4] = {
+                        {mul_f16x2(codes_f16x2<0>(w0[i]), g0), mul_f16x2(codes_f16x2<0>(w1[i]), g1),
+                         mul_f16x2(codes_f16x2<1>(w0[i]), g0), mul_f16x2(codes_f16x2<1>(w1[i]), g1)},
+                        {mul_f16x2(codes_f16x2<2>(w0[i]), g0), mul_f16x2(codes_f16x2<2>(w1[i]), g1),
+                         mul_f16x2(codes_f16x2<3>(w0[i]), g0), mul_f16x2(codes_f16x2<3>(w1[i]), g1)}};
+#pragma unroll
+                    for (int nt = 0; nt < kNT; ++nt) {
+                        const uint4 qb = q_frag[(nt * 4 + i) * 32];
+                        mma_f16_16816(s[nt], a[0], qb.x, qb.y);
+                        mma_f16_16816(s[nt], a[1], qb.z, qb.w);
+                    }
+                }
+            }
+            // ---- P = 2^(s - m + 6); lane (r, c): keys r, r + 8 of rows 2c, 2c + 1
+            const bool edge = key0 + kSub > L - p.R + 1;   // some row does not see some key
+            auto hide = [&](float x, int nt, int e) {
+                const int row = (rg * kNT + nt) * 8 + 2 * c + (e & 1);
+                const int last = row < p.n_rows ? L - p.R + s_draft[row] : L - 1;
+                return key0 + r + (e & 2) * 4 <= last ? x : kNegInf;
+            };
+            bool grow = false;
+            float x[kNT][4];
+#pragma unroll
+            for (int nt = 0; nt < kNT; ++nt)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    x[nt][e] = fmaf(s[nt][e], sc_f[nt][e & 1], kPUp - m[nt][e & 1]);
+                    if (edge) x[nt][e] = hide(x[nt][e], nt, e);
+                    grow |= x[nt][e] > kPMax;
+                }
+            if (__any_sync(0xffffffffu, grow)) {
+#pragma unroll
+                for (int nt = 0; nt < kNT; ++nt)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        float z0 = s[nt][e] * sc_f[nt][e], z1 = s[nt][e + 2] * sc_f[nt][e];
+                        if (edge) {
+                            z0 = hide(z0, nt, e);
+                            z1 = hide(z1, nt, e + 2);
+                        }
+                        float top = fmaxf(z0, z1);
+#pragma unroll
+                        for (int off = 4; off < 32; off <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
+                        top = fmaxf(top, m[nt][e]);
+                        const float a = top == kNegInf ? 1.f : ex2(m[nt][e] - top);
+                        m[nt][e] = top;
+                        l[nt][e] *= a;
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) {
+                            o[nt][i][e] *= a;
+                            o[nt][i][e + 2] *= a;
+                        }
+                        // (a row that has seen no key yet: the exponents are -inf all the same)
+                        const float up = top == kNegInf ? 0.f : kPUp - top;
+                        x[nt][e] = fmaf(s[nt][e], sc_f[nt][e], up);
+                        x[nt][e + 2] = fmaf(s[nt][e + 2], sc_f[nt][e], up);
+                        if (edge) {
+                            x[nt][e] = hide(x[nt][e], nt, e);
+                            x[nt][e + 2] = hide(x[nt][e + 2], nt, e + 2);
+                        }
+                    }
+            }
+            // f(i, a): the A fragment of V^T for dims 16 r + 2i (rows r) and 16 r + 2i + 1 (rows r + 8)
+            auto with_values = [&](auto f) {
+                const uint8_t* vc = st + kCodes + 8 * (r & 1);
+                const uint2 v0 = *reinterpret_cast<const uint2*>(vc + v_at(2 * c, r >> 1));
+                const uint2 v1 = *reinterpret_cast<const uint2*>(vc + v_at(2 * c + 1, r >> 1));
+                const uint2 v2 = *reinterpret_cast<const uint2*>(vc + v_at(2 * c + 8, r >> 1));
+                const uint2 v3 = *reinterpret_cast<const uint2*>(vc + v_at(2 * c + 9, r >> 1));
+                const uint8_t* vs = st + 2 * kCodes + kScales + 2 * c * kPackGroups + r;
+                uint32_t b0 = vs[0], b1 = vs[kPackGroups], b2 = vs[8 * kPackGroups], b3 = vs[9 * kPackGroups];
+                if (key0 + kSub > L) {   // slots past the context hold anything
+                    if (key0 + 2 * c >= L) b0 = 0;
+                    if (key0 + 2 * c + 1 >= L) b1 = 0;
+                    if (key0 + 2 * c + 8 >= L) b2 = 0;
+                    if (key0 + 2 * c + 9 >= L) b3 = 0;
+                }
+                const uint32_t f01 = scales_f16x2(b0 | b1 << 8), f23 = scales_f16x2(b2 | b3 << 8);
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    const uint32_t w0 = half ? v0.y : v0.x, w1 = half ? v1.y : v1.x;
+                    const uint32_t w2 = half ? v2.y : v2.x, w3 = half ? v3.y : v3.x;
+                    const uint32_t e01 = nibbles(w0, w1 << 4), o01 = nibbles(w0 >> 4, w1);   // even and odd dims
+                    const uint32_t e23 = nibbles(w2, w3 << 4), o23 = nibbles(w2 >> 4, w3);
+                    auto dims = [&](auto byte) {
+                        constexpr int kByte = decltype(byte)::value;
+                        const uint32_t a[4] = {mul_f16x2(codes_f16x2<kByte>(e01), f01), mul_f16x2(codes_f16x2<kByte>(o01), f01),
+                                               mul_f16x2(codes_f16x2<kByte>(e23), f23), mul_f16x2(codes_f16x2<kByte>(o23), f23)};
+                        f(half * 4 + kByte, a);
+                    };
+                    dims(std::integral_constant<int, 0>{});
+                    dims(std::integral_constant<int, 1>{});
+                    dims(std::integral_constant<int, 2>{});
+                    dims(std::integral_constant<int, 3>{});
+                }
+            };
+            // faint weights, 28 powers of two at a time, each turn's product scaled back in fp32
+            bool faint = false;
+#pragma unroll
+            for (int nt = 0; nt < kNT; ++nt)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) faint |= x[nt][e] < kPMin && x[nt][e] > -126.f;
+            for (float up = 28.f; __any_sync(0xffffffffu, faint); up += 28.f) {
+                uint32_t pf[kNT][2];
+                faint = false;
+#pragma unroll
+                for (int nt = 0; nt < kNT; ++nt) {
+                    float w[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const bool now = x[nt][e] < kPMin && x[nt][e] + up >= kPMin;
+                        w[e] = now ? ex2(x[nt][e] + up) : 0.f;
+                        if (now) {
+                            l[nt][e & 1] += ex2(x[nt][e]);
+                            x[nt][e] = kNegInf;
+                        }
+                        faint |= x[nt][e] < kPMin && x[nt][e] > -126.f;
+                    }
+                    pf[nt][0] = transpose_8x8(pack_f16x2(w[0], w[1]));
+                    pf[nt][1] = transpose_8x8(pack_f16x2(w[2], w[3]));
+                }
+                const float down = ex2(-up);
+                with_values([&](int i, const uint32_t (&a)[4]) {
+#pragma unroll
+                    for (int nt = 0; nt < kNT; ++nt) {
+                        float d[4] = {0.f, 0.f, 0.f, 0.f};
+                        mma_f16_16816(d, a, pf[nt][0], pf[nt][1]);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) o[nt][i][e] = fmaf(d[e], down, o[nt][i][e]);
+                    }
+                });
+            }
+            uint32_t pb[kNT][2];
+#pragma unroll
+            for (int nt = 0; nt < kNT; ++nt) {
+                float w[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) w[e] = ex2(x[nt][e]);
+                l[nt][0] += w[0] + w[2];
+                l[nt][1] += w[1] + w[3];
+                pb[nt][0] = transpose_8x8(pack_f16x2(w[0], w[1]));
+                pb[nt][1] = transpose_8x8(pack_f16x2(w[2], w[3]));
+            }
+            // ---- O^T += V^T P^T
+            with_values([&](int i, const uint32_t (&a)[4]) {
+#pragma unroll
+                for (int nt = 0; nt < kNT; ++nt) mma_f16_16816(o[nt][i], a, pb[nt][0], pb[nt][1]);
+            });
+        }
+
+        // ---- the teams' states become one (team 0's)
+#pragma unroll
+        for (int nt = 0; nt < kNT; ++nt)
+#pragma unroll
+            for (int e = 0; e < 2; ++e)
+#pragma unroll
+                for (int off = 4; off < 32; off <<= 1) l[nt][e] += __shfl_xor_sync(0xffffffffu, l[nt][e], off);
+        float4* s_ml = s_fold + F::kTeams / 2 * kRG * kNT * 8 * 32;
+#pragma unroll
+        for (int half = F::kTeams / 2; half > 0; half >>= 1) {
+            __syncthreads();
+            const int at = (team % half) * kRG + rg;
+            if (team >= half && team < 2 * half) {
+#pragma unroll
+                for (int nt = 0; nt < kNT; ++nt) {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i)
+                        s_fold[((at * kNT + nt) * 8 + i) * 32 + lane] =
+                            make_float4(o[nt][i][0], o[nt][i][1], o[nt][i][2], o[nt][i][3]);
+                    s_ml[(at * kNT + nt) * 32 + lane] = make_float4(m[nt][0], m[nt][1], l[nt][0], l[nt][1]);
+                }
+            }
+            __syncthreads();
+            if (team < half) {
+#pragma unroll
+                for (int nt = 0; nt < kNT; ++nt) {
+                    const float4 ml = s_ml[(at * kNT + nt) * 32 + lane];
+                    const float om[2] = {ml.x, ml.y}, ol[2] = {ml.z, ml.w};
+                    float a[2], b[2];
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const float top = fmaxf(m[nt][e], om[e]), base = top == kNegInf ? 0.f : top;
+                        a[e] = ex2(m[nt][e] - base);
+                        b[e] = ex2(om[e] - base);
+                        l[nt][e] = l[nt][e] * a[e] + ol[e] * b[e];
+                        m[nt][e] = top;
+                    }
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const float4 v = s_fold[((at * kNT + nt) * 8 + i) * 32 + lane];
+                        o[nt][i][0] = o[nt][i][0] * a[0] + v.x * b[0];
+                        o[nt][i][1] = o[nt][i][1] * a[1] + v.y * b[1];
+                        o[nt][i][2] = o[nt][i][2] * a[0] + v.z * b[0];
+                        o[nt][i][3] = o[nt][i][3] * a[1] + v.w * b[1];
+                    }
+                }
+            }
+        }
+        const bool whole = n == cur.T;
+        if (team == 0) {
+            const float vh = p.v_head ? __ldcg(p.v_head + cur.h) : 1.f;
+            const int slot = 2 * cta + (first_piece ? 0 : 1);
+#pragma unroll
+            for (int nt = 0; nt < kNT; ++nt)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const int row = (rg * kNT + nt) * 8 + 2 * c + e;
+                    if (row >= p.n_rows) continue;
+                    const float inv = l[nt][e] > 0.f ? vh / l[nt][e] : l[nt][e] == 0.f ? 0.f : l[nt][e];   // (NaN stays)
+                    if (whole) {
+                        const int i = s_draft[row];
+                        uint2* dst = reinterpret_cast<uint2*>(
+                            p.out + (((size_t)bg * p.R + i) * p.Hq + (size_t)cur.h * p.G + (row - i * p.G)) * kPackDim + 16 * r);
+#pragma unroll
+                        for (int i2 = 0; i2 < 4; ++i2)
+                            dst[i2] = make_uint2(pack_bf16x2(o[nt][2 * i2][e] * inv, o[nt][2 * i2][e + 2] * inv),
+                                                 pack_bf16x2(o[nt][2 * i2 + 1][e] * inv, o[nt][2 * i2 + 1][e + 2] * inv));
+                    } else {
+                        float4* dst = reinterpret_cast<float4*>(p.part_o + ((size_t)slot * p.n_rows + row) * kPackDim + 16 * r);
+#pragma unroll
+                        for (int i2 = 0; i2 < 4; ++i2)
+                            dst[i2] = make_float4(o[nt][2 * i2][e] * inv, o[nt][2 * i2][e + 2] * inv,
+                                                  o[nt][2 * i2 + 1][e] * inv, o[nt][2 * i2 + 1][e + 2] * inv);
+                        if (r == 0) p.part_ml[(size_t)slot * p.n_rows + row] = make_float2(m[nt][e], l[nt][e]);
+                    }
+                }
+            // a cut span that starts here: its last tile's owner ends its pieces.
+            // This share's last unit is that of its last tile, so the span's
+            // last tile lies T - (cur.t + n) units past it.
+            if (threadIdx.x == 0 && !whole && cur.t == 0) {
+                const long long last = first_unit(cta + 1, U, Gc) - 1 + (cur.T - n);
+                p.jobs[cta] = Job{bg, cur.h, slot, owner_of(last, U, Gc) - cta + 1};
+            }
+        }
+        done += n;
+        cur.t += n - 1;
+        advance(cur, s_len, nb, p.Hkv, F::kTile);
+        first_piece = false;
+        __syncthreads();   // the query rows and the fold's room are free again
+    }
+    cp_async_wait<0>();
+}
+
+// ---------------------------------------------------------------------------
+// Joins the pieces of the span that starts in CTA c of the main kernel (if one
+// does): o = sum_j w_j o_j with w_j = l_j 2^(m_j - M) / sum, a warp for a row.
+// ---------------------------------------------------------------------------
+constexpr int kMergeThreads = 256;
+constexpr int kMergeRows = kMergeThreads / 32;
+constexpr int kMergePieces = 8;   // pieces requested together
+
+__global__ void __launch_bounds__(kMergeThreads) packed_merge_kernel(const PackedAttnParams p) {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    wait_prior_grid();
+    allow_dependent_launch();
+    const int4 jv = __ldcg(reinterpret_cast<const int4*>(p.jobs + blockIdx.x));
+    const Job job{jv.x, jv.y, jv.z, jv.w};
+    if (job.n < 2) return;
+    auto slot = [&](int j) { return (size_t)(j == 0 ? job.slot0 : 2 * ((int)blockIdx.x + j)); };
+    for (int row = blockIdx.y * kMergeRows + warp; row < p.n_rows; row += gridDim.y * kMergeRows) {
+        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+        float M = kNegInf, sum = 0.f;
+        for (int j0 = 0; j0 < job.n; j0 += kMergePieces) {
+            float4 v[kMergePieces];
+            float2 ml[kMergePieces];
+#pragma unroll
+            for (int j = 0; j < kMergePieces; ++j) {
+                ml[j] = make_float2(kNegInf, 0.f);
+                v[j] = make_float4(0.f, 0.f, 0.f, 0.f);
+                if (j0 + j < job.n) {
+                    const size_t at = slot(j0 + j) * p.n_rows + row;
+                    ml[j] = __ldcg(p.part_ml + at);
+                    v[j] = __ldcg(reinterpret_cast<const float4*>(p.part_o + at * kPackDim) + lane);
+                }
+            }
+            float top = M;
+#pragma unroll
+            for (int j = 0; j < kMergePieces; ++j) top = fmaxf(top, ml[j].x);
+            const float base = top == kNegInf ? 0.f : top, keep = ex2(M - base);
+            M = top;
+            sum *= keep;
+            acc.x *= keep;
+            acc.y *= keep;
+            acc.z *= keep;
+            acc.w *= keep;
+#pragma unroll
+            for (int j = 0; j < kMergePieces; ++j) {
+                const float w = ml[j].y * ex2(ml[j].x - base);   // (0 for a piece without a key)
+                sum += w;
+                acc.x = fmaf(w, v[j].x, acc.x);
+                acc.y = fmaf(w, v[j].y, acc.y);
+                acc.z = fmaf(w, v[j].z, acc.z);
+                acc.w = fmaf(w, v[j].w, acc.w);
+            }
+        }
+        const float inv = sum > 0.f ? 1.f / sum : sum == 0.f ? 0.f : sum;
+        const int i = row / p.G;
+        uint2* dst = reinterpret_cast<uint2*>(
+            p.out + (((size_t)job.b * p.R + i) * p.Hq + (size_t)job.h * p.G + (row - i * p.G)) * kPackDim + 4 * lane);
+        *dst = make_uint2(pack_bf16x2(acc.x * inv, acc.y * inv), pack_bf16x2(acc.z * inv, acc.w * inv));
+    }
+}
+
+size_t align256(size_t n) { return (n + 255) & ~size_t(255); }
+
+using Kernel = void (*)(const PackedAttnParams);
+struct Choice {
+    Kernel kern;
+    int threads, smem;
+};
+template <int kNT, int kRG>
+Choice choice() {
+    return {packed_attention_kernel<kNT, kRG>, Form<kNT, kRG>::kThreads, Form<kNT, kRG>::kSmem};
+}
+constexpr int kForms = 9;
+
+// The form for a number of query rows: one warp holds up to four tiles of 8
+// rows; more rows are spread over as few warps of three tiles as hold them.
+int form_of(int rows) {
+    const int nt = (rows + 7) / 8;
+    return nt <= 4 ? nt - 1 : 2 + (nt + 2) / 3;   // 4: two warps of three tiles, ... 8: six
+}
+Choice choice_of(int form) {
+    static const Choice all[kForms] = {choice<1, 1>(), choice<2, 1>(), choice<3, 1>(), choice<4, 1>(), choice<3, 2>(),
+                                       choice<3, 3>(), choice<3, 4>(), choice<3, 5>(), choice<3, 6>()};
+    return all[form];
+}
+
+// CTAs of a form that an SM holds at once (kept for each device), the limit of
+// dynamic shared memory set on the way.
+int resident_of(int form) {
+    static std::atomic<int> kept[64][kForms];
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) {
+        cudaGetLastError();
+        return 0;
+    }
+    if (!kept[dev][form]) {
+        const Choice c = choice_of(form);
+        int n = 0;
+        if (cudaFuncSetAttribute(c.kern, cudaFuncAttributeMaxDynamicSharedMemorySize, c.smem) != cudaSuccess ||
+            cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, c.kern, c.threads, c.smem) != cudaSuccess || n <= 0) {
+            cudaGetLastError();
+            return 0;
+        }
+        kept[dev][form] = n;
+    }
+    return kept[dev][form];
+}
+
+struct PackedPlan {
+    int form, rows, grid;
+    size_t off_ml, off_o, bytes;
+};
+PackedPlan plan_packed(const cs_attn_dims& d, int rows, int sm_count) {
+    PackedPlan pl{};
+    pl.rows = rows * (d.n_q_heads / d.n_kv_heads);
+    pl.form = form_of(pl.rows);
+    const int res = resident_of(pl.form);
+    pl.grid = sm_count * (res > 0 ? res : 1);
+    if (pl.grid > kMaxGrid) pl.grid = kMaxGrid;
+    pl.off_ml = align256(sizeof(Job) * (size_t)pl.grid);
+    pl.off_o = pl.off_ml + align256(sizeof(float2) * 2 * (size_t)pl.grid * pl.rows);
+    pl.bytes = pl.off_o + align256(sizeof(float) * kPackDim * 2 * (size_t)pl.grid * pl.rows);
+    return pl;
 }
 
 }  // namespace
 
-size_t packed_attention_workspace_bytes(const cs_attn_dims&, int, int) { return 256; }
+size_t packed_attention_workspace_bytes(const cs_attn_dims& d, int rows, int sm_count) {
+    return plan_packed(d, rows, sm_count).bytes;
+}
 
 cs_status launch_packed_attention(const cs_attn_dims& d, const void* q, const cs_packed_pool& pool,
                                   const int32_t* page_table, const int32_t* ctx_lens, int rows, void* out,
-                                  void*, cudaStream_t stream) {
+                                  void* workspace, cudaStream_t stream) {
+    const PackedPlan pl = plan_packed(d, rows, current_sm_count());
+    uint8_t* ws = static_cast<uint8_t*>(workspace);
     PackedAttnParams p{};
     p.q = static_cast<const __nv_bfloat16*>(q);
     p.out = static_cast<__nv_bfloat16*>(out);
@@ -110,18 +781,32 @@ cs_status launch_packed_attention(const cs_attn_dims& d, const void* q, const cs
     p.v_head = pool.v_head_scale;
     p.page_table = page_table;
     p.ctx_lens = ctx_lens;
+    p.jobs = reinterpret_cast<Job*>(ws);
+    p.part_ml = reinterpret_cast<float2*>(ws + pl.off_ml);
+    p.part_o = reinterpret_cast<float*>(ws + pl.off_o);
     p.Hq = d.n_q_heads;
     p.Hkv = d.n_kv_heads;
     p.G = d.n_q_heads / d.n_kv_heads;
     p.R = rows;
+    p.n_rows = pl.rows;
     p.ps = d.page_size;
+    while ((1 << p.ps_log2) < d.page_size) ++p.ps_log2;
     p.max_pages = d.max_pages_per_seq;
     p.P = d.num_pages;
+    p.span_x = 1;
     p.scale_log2 = (d.sm_scale > 0.f ? d.sm_scale : 1.0f / sqrtf((float)d.head_dim)) * 1.4426950408889634f;
-    if (d.batch > 65535) return fail(CS_ERR_UNSUPPORTED, "batch %d too large for one call", d.batch);
-    const cudaError_t e = launch_dependent(packed_attention_kernel, dim3(d.n_q_heads, rows, d.batch), dim3(kWarps * 32),
-                                           0, stream, p);
-    return e == cudaSuccess ? CS_OK : cuda_fail(e, "packed_attention_kernel launch");
+    const Choice k = choice_of(pl.form);
+    if (resident_of(pl.form) <= 0) return fail(CS_ERR_CUDA, "packed_attention_kernel does not fit this device");
+    const unsigned chunks = (unsigned)((pl.rows + kMergeRows - 1) / kMergeRows);
+    for (int b0 = 0; b0 < d.batch; b0 += kMaxBatchPerLaunch) {
+        p.b_base = b0;
+        p.n_batch = d.batch - b0 < kMaxBatchPerLaunch ? d.batch - b0 : kMaxBatchPerLaunch;
+        cudaError_t e = launch_dependent(k.kern, dim3(pl.grid), dim3(k.threads), (size_t)k.smem, stream, p);
+        if (e != cudaSuccess) return cuda_fail(e, "packed_attention_kernel launch");
+        e = launch_dependent(packed_merge_kernel, dim3(pl.grid, chunks), dim3(kMergeThreads), 0, stream, p);
+        if (e != cudaSuccess) return cuda_fail(e, "packed_merge_kernel launch");
+    }
+    return CS_OK;
 }
 
 }  // namespace cs
