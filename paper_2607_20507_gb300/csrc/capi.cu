@@ -181,6 +181,8 @@ cs_status check_packed_attn(const cs_attn_dims* d, int32_t n_draft) {
     if (st != CS_OK) return st;
     const long long rows = (long long)(n_draft + 1) * (d->n_q_heads / d->n_kv_heads);
     if (rows > 144) return fail(CS_ERR_UNSUPPORTED, "(k+1)*G = %lld query rows per KV head (max 144)", rows);
+    if ((long long)d->num_pages * d->n_kv_heads > 0x7fffffffLL / d->page_size)
+        return fail(CS_ERR_UNSUPPORTED, "a pool of more than 2^31 rows");
     return CS_OK;
 }
 

@@ -32,6 +32,7 @@
 // fp16 has 11 bits, for weights down to 2^-26 of the largest.  A tile with
 // smaller ones takes another turn for them (faint, below): an output may rest
 // on them where the codes of the heavier keys are 0.
+#include <limits.h>
 #include <math.h>
 
 #include <type_traits>
@@ -42,16 +43,18 @@
 namespace cs {
 namespace {
 
-constexpr int kSub = 16;                            // keys of a team's tile
-constexpr int kStages = 4;
-constexpr int kCodes = kSub * kPackCodeBytes;       // 1024 bytes of codes of K or V
-constexpr int kScales = kSub * kPackGroups;         // 128 bytes of scales
+constexpr int kSub = 32;                            // keys of a team's tile
+constexpr int kHalves = kSub / 16;                  // MMA tiles of 16 keys in it
+constexpr int kStages = 2;
+constexpr int kCodes = kSub * kPackCodeBytes;       // 2048 bytes of codes of K or V
+constexpr int kScales = kSub * kPackGroups;         // 256 bytes of scales
 constexpr int kStageBytes = 2 * (kCodes + kScales);
 constexpr int kMaxBatchPerLaunch = 1024;            // requests whose schedule one launch holds
 constexpr int kMaxGrid = 1024;                      // CTAs of a launch at most
 constexpr float kPUp = 12.f;                        // P = 2^(s - m + kPUp)
 constexpr float kPMax = 15.f;                       // the maximum follows a score that passes 2^kPMax
 constexpr float kPMin = -14.f;                      // weights below 2^kPMin are faint: less than 11 bits in fp16
+constexpr float kPGone = -126.f;                    // and those below 2^kPGone count as 0
 
 struct Job {             // a cut span that starts in a CTA: its pieces lie in slot0 and the first slots of the CTAs after it
     int b, h, slot0, n;
@@ -253,66 +256,59 @@ packed_attention_kernel(const PackedAttnParams p) {
     if (n_tiles <= 0) return;
     for (int row = threadIdx.x; row < F::kRows; row += F::kThreads) s_draft[row] = row / p.G;
 
-    // ---- the ring
+    // ---- the ring.  Lane g (mod 4) looks up the page of keys 8 g .. 8 g + 7 of
+    // the next tile to load, one tile ahead.
     uint8_t* ring = smem + team * (kStages * kStageBytes);
     const uint32_t ring_a = smem_u32(ring);
-    Cursor ci = share.first;     // of the next tile to load
-    Cursor cn = share.first;     // of the tile whose pages are looked up next
-    int next_a = -1, next_b = -1, next2_a = -1, next2_b = -1;   // the pages of the next two tiles to load
-    int looked = 0;
-    auto look_up = [&](int& pa, int& pb) {   // the pages of keys 0-7 and 8-15 of cn's tile
-        pa = pb = -1;
-        if (looked++ >= n_tiles) return;
-        const int key = cn.t * F::kTile + team * kSub, L = s_len[cn.b];
-        const int32_t* row = p.page_table + (size_t)(p.b_base + cn.b) * p.max_pages;
-        if (key < L) pa = __ldcg(row + (key >> p.ps_log2));
-        if (p.ps >= kSub) pb = pa;
-        else if (key + 8 < L) pb = __ldcg(row + ((key + 8) >> p.ps_log2));
+    constexpr int kLoaders = kRG == 1 ? 1 : 2;
+    const int page_rows = p.Hkv * p.ps;
+    Cursor cn = share.first;
+    int left = n_tiles, stage_in = 0;                 // tiles not looked up yet, the stage that is filled next
+    int next_page = -1, next_row = 0;                 // the page of this lane's group, and the row of its keys on it
+    bool pending = false;                             // whether a tile is looked up
+    auto look_up = [&]() {
+        pending = left > 0;
+        if (!pending) return;
+        --left;
+        const int key = cn.t * F::kTile + team * kSub + 8 * c;
+        next_page = -1;
+        next_row = cn.h * p.ps + (key & (p.ps - 1));
+        if (key < s_len[cn.b])
+            next_page = __ldcg(p.page_table + (size_t)(p.b_base + cn.b) * p.max_pages + (key >> p.ps_log2));
         advance(cn, s_len, nb, p.Hkv, F::kTile);
     };
-    constexpr int kLoaders = kRG == 1 ? 1 : 2;
-    int issued = 0;
+    const uint8_t* k_lane = p.k_codes + r * kPackCodeBytes + c * 16;
+    const uint8_t* v_lane = p.v_codes + r * kPackCodeBytes + c * 16;
+    const uint8_t* s_lane = (lane < 16 ? p.k_scales : p.v_scales) + c * 16;
+    const uint32_t k_to = ring_a + r * kPackCodeBytes + c * 16, v_to = ring_a + kCodes + v_at(r, c);
+    const uint32_t s_to = ring_a + 2 * kCodes + lane * 16;
     auto issue = [&]() {
-        if (rg < kLoaders && issued < n_tiles) {
-            const int pa = next_a, pb = next_b;
-            next_a = next2_a;
-            next_b = next2_b;
-            look_up(next2_a, next2_b);
-            const int key = ci.t * F::kTile + team * kSub;
-            if (key < s_len[ci.b]) {
-                const uint32_t st = ring_a + (issued % kStages) * kStageBytes;
-                const int slot = key & (p.ps - 1);
-                const bool in_a = pa >= 0 && pa < p.P, in_b = pb >= 0 && pb < p.P;
-                const size_t row_a = in_a ? ((size_t)pa * p.Hkv + ci.h) * p.ps + slot : 0;
-                const size_t row_b = in_b ? ((size_t)pb * p.Hkv + ci.h) * p.ps + (p.ps >= kSub ? slot + 8 : 0) : 0;
+        if (rg < kLoaders && pending) {
+            const bool in = next_page >= 0 && next_page < p.P;
+            const int row = in ? next_page * page_rows + next_row : -1;
+            const uint32_t st = stage_in * kStageBytes;
+            look_up();
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    if (kLoaders == 2 && i != rg) continue;
-                    const size_t row = (i ? row_b : row_a) + r;
-                    const bool in = i ? in_b : in_a;
-                    cp_async16(st + (8 * i + r) * kPackCodeBytes + c * 16, p.k_codes + row * kPackCodeBytes + c * 16, in);
-                    cp_async16(st + kCodes + v_at(8 * i + r, c), p.v_codes + row * kPackCodeBytes + c * 16, in);
-                }
-                if (rg == 0 && lane < 16) {
-                    const bool second = lane & 4, in = second ? in_b : in_a;
-                    const size_t at = (second ? row_b : row_a) * kPackGroups + (lane & 3) * 16;
-                    cp_async16(st + 2 * kCodes + lane * 16, (lane & 8 ? p.v_scales : p.k_scales) + at, in);
-                }
+            for (int g = 0; g < 4; ++g) {
+                const int rw = __shfl_sync(0xffffffffu, row, g);
+                if (kLoaders == 2 && g / 2 != rg) continue;
+                const size_t at = (size_t)max(rw, 0) * kPackCodeBytes;
+                cp_async16(k_to + st + g * 8 * kPackCodeBytes, k_lane + at, rw >= 0);
+                cp_async16(v_to + st + g * 8 * kPackCodeBytes, v_lane + at, rw >= 0);
             }
-            advance(ci, s_len, nb, p.Hkv, F::kTile);
+            const int rw = __shfl_sync(0xffffffffu, row, lane >> 2 & 3);
+            if (rg == 0) cp_async16(s_to + st, s_lane + (size_t)max(rw, 0) * kPackGroups, rw >= 0);
         }
-        ++issued;
+        stage_in = stage_in + 1 == kStages ? 0 : stage_in + 1;
         cp_async_commit();
     };
     auto team_sync = [&]() {
         if constexpr (kRG == 1) __syncwarp();
         else asm volatile("bar.sync %0, %1;" ::"r"(1 + team), "n"(kRG * 32) : "memory");
     };
-    if (rg < kLoaders) {
-        look_up(next_a, next_b);
-        look_up(next2_a, next2_b);
-    }
+    if (rg < kLoaders) look_up();
     for (int i = 0; i < kStages - 1; ++i) issue();
+    int stage = 0;
 
     // ---- spans
     Cursor cur = share.first;
@@ -366,25 +362,32 @@ packed_attention_kernel(const PackedAttnParams p) {
                 for (int e = 0; e < 4; ++e) o[nt][i][e] = 0.f;
         }
         const uint4* q_frag = s_q + rg * kNT * 4 * 32 + lane;
+        uint4 q_kept[4];   // one row tile's fragments stay in registers
+        if constexpr (kNT == 1)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) q_kept[i] = q_frag[i * 32];
 
         for (int t = 0; t < n; ++t) {
             cp_async_wait<kStages - 2>();
             team_sync();
-            const uint8_t* st = ring + ((done + t) % kStages) * kStageBytes;
+            const uint8_t* st = ring + stage * kStageBytes;
+            stage = stage + 1 == kStages ? 0 : stage + 1;
             issue();   // into the stage that the team left before the barrier
             const int key0 = (cur.t + t) * F::kTile + team * kSub;
             if (key0 >= L) continue;
 
             // ---- S^T = K Q^T
-            float s[kNT][4];
+            float s[kHalves][kNT][4];
 #pragma unroll
-            for (int nt = 0; nt < kNT; ++nt)
+            for (int hf = 0; hf < kHalves; ++hf) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) s[nt][e] = 0.f;
-            {
-                const uint4 k0 = *reinterpret_cast<const uint4*>(st + r * kPackCodeBytes + c * 16);
-                const uint4 k1 = *reinterpret_cast<const uint4*>(st + (r + 8) * kPackCodeBytes + c * 16);
-                const uint8_t* ks = st + 2 * kCodes + r * kPackGroups + 2 * c;
+                for (int nt = 0; nt < kNT; ++nt)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) s[hf][nt][e] = 0.f;
+                const uint8_t* kc = st + (16 * hf + r) * kPackCodeBytes + c * 16;
+                const uint4 k0 = *reinterpret_cast<const uint4*>(kc);
+                const uint4 k1 = *reinterpret_cast<const uint4*>(kc + 8 * kPackCodeBytes);
+                const uint8_t* ks = st + 2 * kCodes + (16 * hf + r) * kPackGroups + 2 * c;
                 const uint32_t f0 = scales_f16x2(*reinterpret_cast<const uint16_t*>(ks));
                 const uint32_t f1 = scales_f16x2(*reinterpret_cast<const uint16_t*>(ks + 8 * kPackGroups));
                 const uint32_t w0[4] = {k0.x, k0.y, k0.z, k0.w}, w1[4] = {k1.x, k1.y, k1.z, k1.w};
@@ -399,75 +402,84 @@ packed_attention_kernel(const PackedAttnParams p) {
                          mul_f16x2(codes_f16x2<3>(w0[i]), g0), mul_f16x2(codes_f16x2<3>(w1[i]), g1)}};
 #pragma unroll
                     for (int nt = 0; nt < kNT; ++nt) {
-                        const uint4 qb = q_frag[(nt * 4 + i) * 32];
-                        mma_f16_16816(s[nt], a[0], qb.x, qb.y);
-                        mma_f16_16816(s[nt], a[1], qb.z, qb.w);
+                        const uint4 qb = kNT == 1 ? q_kept[i] : q_frag[(nt * 4 + i) * 32];
+                        mma_f16_16816(s[hf][nt], a[0], qb.x, qb.y);
+                        mma_f16_16816(s[hf][nt], a[1], qb.z, qb.w);
                     }
                 }
             }
-            // ---- P = 2^(s - m + 6); lane (r, c): keys r, r + 8 of rows 2c, 2c + 1
-            const bool edge = key0 + kSub > L - p.R + 1;   // some row does not see some key
-            auto hide = [&](float x, int nt, int e) {
-                const int row = (rg * kNT + nt) * 8 + 2 * c + (e & 1);
-                const int last = row < p.n_rows ? L - p.R + s_draft[row] : L - 1;
-                return key0 + r + (e & 2) * 4 <= last ? x : kNegInf;
-            };
-            bool grow = false;
-            float x[kNT][4];
+            // ---- x = s - m + 12; lane (r, c): keys r, r + 8 of rows 2c, 2c + 1.
+            // Most tiles need no more than that; the others (a key that a row
+            // does not see, a maximum that grows, faint weights) branch off here
+            // and leave x in s (ready)
+            float top = -1.f, low = 0.f;
 #pragma unroll
             for (int nt = 0; nt < kNT; ++nt)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    x[nt][e] = fmaf(s[nt][e], sc_f[nt][e & 1], kPUp - m[nt][e & 1]);
-                    if (edge) x[nt][e] = hide(x[nt][e], nt, e);
-                    grow |= x[nt][e] > kPMax;
-                }
-            if (__any_sync(0xffffffffu, grow)) {
+                for (int e = 0; e < 4; ++e)
+#pragma unroll
+                    for (int hf = 0; hf < kHalves; ++hf) {
+                        const float v = fmaf(s[hf][nt][e], sc_f[nt][e & 1], kPUp - m[nt][e & 1]);
+                        top = fmaxf(top, v);
+                        low = fminf(low, v);
+                    }
+            const bool edge = key0 + kSub > L - p.R + 1;   // some row does not see some key
+            const bool ready = __any_sync(0xffffffffu, top > kPMax || low < kPMin || edge);
+            if (ready) {
+                low = 0.f;
 #pragma unroll
                 for (int nt = 0; nt < kNT; ++nt)
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
-                        float z0 = s[nt][e] * sc_f[nt][e], z1 = s[nt][e + 2] * sc_f[nt][e];
-                        if (edge) {
-                            z0 = hide(z0, nt, e);
-                            z1 = hide(z1, nt, e + 2);
-                        }
-                        float top = fmaxf(z0, z1);
+                        const int row = (rg * kNT + nt) * 8 + 2 * c + e;
+                        const int last = !edge ? INT_MAX : row < p.n_rows ? L - p.R + s_draft[row] : L - 1;
+                        float now = kNegInf;
 #pragma unroll
-                        for (int off = 4; off < 32; off <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
-                        top = fmaxf(top, m[nt][e]);
-                        const float a = top == kNegInf ? 1.f : ex2(m[nt][e] - top);
-                        m[nt][e] = top;
-                        l[nt][e] *= a;
+                        for (int hf = 0; hf < kHalves; ++hf)
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) {
-                            o[nt][i][e] *= a;
-                            o[nt][i][e + 2] *= a;
+                            for (int k = e; k < 4; k += 2) {
+                                const bool seen = key0 + 16 * hf + r + (k & 2) * 4 <= last;
+                                s[hf][nt][k] = seen ? s[hf][nt][k] * sc_f[nt][e] : kNegInf;
+                                now = fmaxf(now, s[hf][nt][k]);
+                            }
+#pragma unroll
+                        for (int off = 4; off < 32; off <<= 1) now = fmaxf(now, __shfl_xor_sync(0xffffffffu, now, off));
+                        if (now - m[nt][e] > kPMax - kPUp) {   // (true for a row's first key: m is -inf)
+                            const float a = ex2(m[nt][e] - now);
+                            m[nt][e] = now;
+                            l[nt][e] *= a;
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) {
+                                o[nt][i][e] *= a;
+                                o[nt][i][e + 2] *= a;
+                            }
                         }
-                        // (a row that has seen no key yet: the exponents are -inf all the same)
-                        const float up = top == kNegInf ? 0.f : kPUp - top;
-                        x[nt][e] = fmaf(s[nt][e], sc_f[nt][e], up);
-                        x[nt][e + 2] = fmaf(s[nt][e + 2], sc_f[nt][e], up);
-                        if (edge) {
-                            x[nt][e] = hide(x[nt][e], nt, e);
-                            x[nt][e + 2] = hide(x[nt][e + 2], nt, e + 2);
-                        }
+                        // (a row that has seen no key yet: every score is -inf)
+                        const float up = m[nt][e] == kNegInf ? 0.f : kPUp - m[nt][e];
+#pragma unroll
+                        for (int hf = 0; hf < kHalves; ++hf)
+#pragma unroll
+                            for (int k = e; k < 4; k += 2) {
+                                s[hf][nt][k] += up;
+                                if (s[hf][nt][k] > kPGone) low = fminf(low, s[hf][nt][k]);
+                            }
                     }
             }
             // f(i, a): the A fragment of V^T for dims 16 r + 2i (rows r) and 16 r + 2i + 1 (rows r + 8)
-            auto with_values = [&](auto f) {
-                const uint8_t* vc = st + kCodes + 8 * (r & 1);
+            auto with_values = [&](int hf, auto f) {
+                const uint8_t* vc = st + kCodes + hf * 16 * kPackCodeBytes + 8 * (r & 1);
+                const int kv = key0 + 16 * hf;
                 const uint2 v0 = *reinterpret_cast<const uint2*>(vc + v_at(2 * c, r >> 1));
                 const uint2 v1 = *reinterpret_cast<const uint2*>(vc + v_at(2 * c + 1, r >> 1));
                 const uint2 v2 = *reinterpret_cast<const uint2*>(vc + v_at(2 * c + 8, r >> 1));
                 const uint2 v3 = *reinterpret_cast<const uint2*>(vc + v_at(2 * c + 9, r >> 1));
-                const uint8_t* vs = st + 2 * kCodes + kScales + 2 * c * kPackGroups + r;
+                const uint8_t* vs = st + 2 * kCodes + kScales + (16 * hf + 2 * c) * kPackGroups + r;
                 uint32_t b0 = vs[0], b1 = vs[kPackGroups], b2 = vs[8 * kPackGroups], b3 = vs[9 * kPackGroups];
-                if (key0 + kSub > L) {   // slots past the context hold anything
-                    if (key0 + 2 * c >= L) b0 = 0;
-                    if (key0 + 2 * c + 1 >= L) b1 = 0;
-                    if (key0 + 2 * c + 8 >= L) b2 = 0;
-                    if (key0 + 2 * c + 9 >= L) b3 = 0;
+                if (kv + 16 > L) {   // slots past the context hold anything
+                    if (kv + 2 * c >= L) b0 = 0;
+                    if (kv + 2 * c + 1 >= L) b1 = 0;
+                    if (kv + 2 * c + 8 >= L) b2 = 0;
+                    if (kv + 2 * c + 9 >= L) b3 = 0;
                 }
                 const uint32_t f01 = scales_f16x2(b0 | b1 << 8), f23 = scales_f16x2(b2 | b3 << 8);
 #pragma unroll
@@ -489,57 +501,69 @@ packed_attention_kernel(const PackedAttnParams p) {
                 }
             };
             // faint weights, 28 powers of two at a time, each turn's product scaled back in fp32
-            bool faint = false;
+            if (ready && __any_sync(0xffffffffu, low < kPMin)) {
+                auto is_faint = [&](float v) { return v < kPMin && v > kPGone; };
 #pragma unroll
-            for (int nt = 0; nt < kNT; ++nt)
+                for (int hf = 0; hf < kHalves; ++hf) {
+                    bool faint = false;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) faint |= x[nt][e] < kPMin && x[nt][e] > -126.f;
-            for (float up = 28.f; __any_sync(0xffffffffu, faint); up += 28.f) {
-                uint32_t pf[kNT][2];
-                faint = false;
+                    for (int nt = 0; nt < kNT; ++nt)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) faint |= is_faint(s[hf][nt][e]);
+#pragma unroll 1
+                    for (float up = 28.f; __any_sync(0xffffffffu, faint); up += 28.f) {
+                        uint32_t pf[kNT][2];
+                        faint = false;
+#pragma unroll
+                        for (int nt = 0; nt < kNT; ++nt) {
+                            float w[4];
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) {
+                                float& v = s[hf][nt][e];
+                                const bool now = v < kPMin && v + up >= kPMin;
+                                w[e] = now ? ex2(v + up) : 0.f;
+                                if (now) {
+                                    l[nt][e & 1] += ex2(v);
+                                    v = kNegInf;
+                                }
+                                faint |= is_faint(v);
+                            }
+                            pf[nt][0] = transpose_8x8(pack_f16x2(w[0], w[1]));
+                            pf[nt][1] = transpose_8x8(pack_f16x2(w[2], w[3]));
+                        }
+                        const float down = ex2(-up);
+                        with_values(hf, [&](int i, const uint32_t (&a)[4]) {
+#pragma unroll
+                            for (int nt = 0; nt < kNT; ++nt) {
+                                float d[4] = {0.f, 0.f, 0.f, 0.f};
+                                mma_f16_16816(d, a, pf[nt][0], pf[nt][1]);
+#pragma unroll
+                                for (int e = 0; e < 4; ++e) o[nt][i][e] = fmaf(d[e], down, o[nt][i][e]);
+                            }
+                        });
+                    }
+                }
+            }
+            // ---- P = 2^x and O^T += V^T P^T
+#pragma unroll
+            for (int hf = 0; hf < kHalves; ++hf) {
+                uint32_t pb[kNT][2];
 #pragma unroll
                 for (int nt = 0; nt < kNT; ++nt) {
                     float w[4];
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const bool now = x[nt][e] < kPMin && x[nt][e] + up >= kPMin;
-                        w[e] = now ? ex2(x[nt][e] + up) : 0.f;
-                        if (now) {
-                            l[nt][e & 1] += ex2(x[nt][e]);
-                            x[nt][e] = kNegInf;
-                        }
-                        faint |= x[nt][e] < kPMin && x[nt][e] > -126.f;
-                    }
-                    pf[nt][0] = transpose_8x8(pack_f16x2(w[0], w[1]));
-                    pf[nt][1] = transpose_8x8(pack_f16x2(w[2], w[3]));
+                    for (int e = 0; e < 4; ++e)
+                        w[e] = ex2(fmaf(s[hf][nt][e], ready ? 1.f : sc_f[nt][e & 1], ready ? 0.f : kPUp - m[nt][e & 1]));
+                    l[nt][0] += w[0] + w[2];
+                    l[nt][1] += w[1] + w[3];
+                    pb[nt][0] = transpose_8x8(pack_f16x2(w[0], w[1]));
+                    pb[nt][1] = transpose_8x8(pack_f16x2(w[2], w[3]));
                 }
-                const float down = ex2(-up);
-                with_values([&](int i, const uint32_t (&a)[4]) {
+                with_values(hf, [&](int i, const uint32_t (&a)[4]) {
 #pragma unroll
-                    for (int nt = 0; nt < kNT; ++nt) {
-                        float d[4] = {0.f, 0.f, 0.f, 0.f};
-                        mma_f16_16816(d, a, pf[nt][0], pf[nt][1]);
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) o[nt][i][e] = fmaf(d[e], down, o[nt][i][e]);
-                    }
+                    for (int nt = 0; nt < kNT; ++nt) mma_f16_16816(o[nt][i], a, pb[nt][0], pb[nt][1]);
                 });
             }
-            uint32_t pb[kNT][2];
-#pragma unroll
-            for (int nt = 0; nt < kNT; ++nt) {
-                float w[4];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) w[e] = ex2(x[nt][e]);
-                l[nt][0] += w[0] + w[2];
-                l[nt][1] += w[1] + w[3];
-                pb[nt][0] = transpose_8x8(pack_f16x2(w[0], w[1]));
-                pb[nt][1] = transpose_8x8(pack_f16x2(w[2], w[3]));
-            }
-            // ---- O^T += V^T P^T
-            with_values([&](int i, const uint32_t (&a)[4]) {
-#pragma unroll
-                for (int nt = 0; nt < kNT; ++nt) mma_f16_16816(o[nt][i], a, pb[nt][0], pb[nt][1]);
-            });
         }
 
         // ---- the teams' states become one (team 0's)
