@@ -501,8 +501,9 @@ typedef struct {
  * normalisation.
  *
  * Return CS_ERR_INVALID_ARG (null pointer, misalignment, bad dimension or
- * count), CS_ERR_UNSUPPORTED (head_dim != 128, page size, query rows),
- * CS_ERR_WORKSPACE or CS_ERR_CUDA.
+ * count), CS_ERR_UNSUPPORTED (head_dim != 128, page size, query rows, attention
+ * over a pool of more than 2^31 rows P * Hkv * ps), CS_ERR_WORKSPACE or
+ * CS_ERR_CUDA.
  */
 cs_status cs_packed_kv_append(const cs_attn_dims* dims, const cs_packed_pool* pool, const void* new_k,
                               const void* new_v, const int32_t* page_table, const int32_t* ctx_lens, int32_t n_new,
@@ -603,7 +604,7 @@ cs_status cs_kv_compact(const cs_page_dims* dims, const cs_page_pool* pools, int
  *   logits   [rows, V] fp32 or bf16, rows row_stride elements apart (>= V),
  *            element-aligned; -inf marks a masked token, NaN and +inf are not allowed
  *   tokens   int32 [rows]
- *   T        > 0 and finite
+ *   T        in [1e-30, 1e30]
  *   n_top    in [0, CS_MAX_TOP]
  *   out_entropy may be NULL; out_top_* may be NULL when n_top is 0
  * Sums are fp32; the result is a deterministic function of the inputs.

@@ -562,8 +562,8 @@ cs_status cs_logprobs(const cs_logprob_dims* dims, const void* logits, const int
         return fail(CS_ERR_INVALID_ARG, "row_stride %lld below the vocabulary", (long long)d->row_stride);
     if (d->rows > 1 && d->row_stride > (1LL << 46) / d->rows)
         return fail(CS_ERR_INVALID_ARG, "logit tensor too large");
-    if (!(temperature > 0.f) || isinf(temperature))
-        return fail(CS_ERR_INVALID_ARG, "temperature must be finite and > 0");
+    if (!(temperature >= 1e-30f && temperature <= 1e30f))
+        return fail(CS_ERR_INVALID_ARG, "temperature must lie in [1e-30, 1e30]");
     if (d->vocab > CS_MAX_VOCAB)
         return fail(CS_ERR_UNSUPPORTED, "vocab %d (this library implements up to %d)", d->vocab, CS_MAX_VOCAB);
     if (d->rows == 0) return CS_OK;

@@ -1,9 +1,23 @@
 // logprobs.cu -- log probabilities of given tokens, the entropy and the top
-// alternatives of their rows (cs_logprobs).
+// alternatives of their rows (cs_logprobs), in one pass over the logits.
 //
-// One CTA per row: the maximum; the sums S = sum w and U = sum w ln w of the
-// weights w = exp((z - max) / T); then the alternatives one after another, each
-// the largest logit below the one before it (ties by id).
+// A cluster of 1 to 8 CTAs takes a row, each a contiguous slice in tiles of
+// kTile 16-byte vectors (rows of any alignment are read in 16-byte blocks of
+// memory, what lies outside the row counts as -inf).  A thread keeps a running
+// maximum m, and with it S = sum w and U = sum w d of the weights
+// w = 2^(d log2(e) / T), d = z - m; so
+//     ln sum exp(z / T) = m / T + ln S,   H = ln S - U / (S T).
+//
+// The alternatives: a logit and its id are one ordered number (the larger
+// logit, then the lower id).  A CTA keeps a bound no higher than its n-th best
+// and puts the keys above it into a list in shared memory; when the list has
+// grown, its n best stay and the last of them is the new bound.  The first bound
+// is the n-th largest of the threads' best keys of the first tile (of 8192 bf16
+// logits some 25 lie above it).  A tile with more keys above the bound than the
+// list takes is taken again with such a bound of its own, which at most n
+// threads have keys above.  Keys are unique, so the order in which they arrive
+// changes nothing.  The first CTA of the cluster merges the slices' sums and
+// lists through distributed shared memory.
 #include "cs_internal.h"
 #include "cs_device.cuh"
 
@@ -11,6 +25,15 @@ namespace cs {
 namespace {
 
 constexpr int kThreads = 256;
+constexpr int kVecs = 4;                       // 16-byte vectors of a thread's tile
+constexpr int kTile = kThreads * kVecs;
+constexpr int kMaxCluster = 8;
+constexpr int kListFull = 192;                 // from here on the list is cut to the n best
+constexpr int kList = 2048;                    // what it takes: kListFull, and the keys of CS_MAX_TOP threads
+static_assert(kList >= kListFull + CS_MAX_TOP * kVecs * 8, "a tile's keys above its threads' n-th best fit");
+static_assert(kListFull <= kThreads && kMaxCluster * CS_MAX_TOP <= kThreads, "a thread a key");
+
+using Key = unsigned long long;
 
 struct LogprobParams {
     const void* logits;
@@ -21,91 +44,354 @@ struct LogprobParams {
     float* top_logprobs;
     int V, n_top;
     long long stride;
-    float c_hi, c_lo;            // log2(e) / T
+    float c;                     // log2(e) / T
     float i_hi, i_lo;            // 1 / T
     float d_min;                 // weights of logits further below the maximum are 0
 };
 
-template <bool kF32>
-__device__ __forceinline__ float logit(const void* row, int v) {
-    if constexpr (kF32) return __ldcg(static_cast<const float*>(row) + v);
-    else return bf16_bits_to_float(__ldcg(static_cast<const uint16_t*>(row) + v));
+// Larger logit, then lower id (-0 is 0).
+__device__ __forceinline__ Key key_of(float z, int v) {
+    const uint32_t b = __float_as_uint(z + 0.f);
+    return (Key)(b & 0x80000000u ? ~b : b | 0x80000000u) << 32 | (uint32_t)~v;
+}
+__device__ __forceinline__ float logit_of(Key k) {
+    const uint32_t b = (uint32_t)(k >> 32);
+    return __uint_as_float(b & 0x80000000u ? b & 0x7fffffffu : ~b);
+}
+__device__ __forceinline__ int id_of(Key k) { return (int)~(uint32_t)k; }
+
+__device__ __forceinline__ uint32_t cluster_rank() {
+    uint32_t r;
+    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ void cluster_sync() {
+    asm volatile("barrier.cluster.arrive.aligned;\n\tbarrier.cluster.wait.aligned;" ::: "memory");
+}
+// the same shared-memory word of CTA `rank` of the cluster
+__device__ __forceinline__ uint32_t at_rank(const void* p, uint32_t rank) {
+    uint32_t a;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(smem_u32(p)), "r"(rank));
+    return a;
+}
+__device__ __forceinline__ Key load_key(uint32_t a) {
+    Key k;
+    asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(k) : "r"(a) : "memory");
+    return k;
+}
+__device__ __forceinline__ float load_float(uint32_t a) {
+    float f;
+    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(f) : "r"(a) : "memory");
+    return f;
 }
 
-// A logit and its id as one number: the larger logit, then the lower id, is the larger.
-__device__ __forceinline__ unsigned long long key_of(float z, int v) {
-    const uint32_t b = __float_as_uint(z + 0.f);   // (-0 is 0)
-    return (unsigned long long)(b & 0x80000000u ? ~b : b | 0x80000000u) << 32 | (uint32_t)~v;
-}
-
-template <typename T, typename F>
-__device__ __forceinline__ T block_reduce(T v, T* s, F f) {
-    for (int off = 16; off > 0; off >>= 1) v = f(v, __shfl_xor_sync(0xffffffffu, v, off));
-    __syncthreads();
-    if ((threadIdx.x & 31) == 0) s[threadIdx.x >> 5] = v;
-    __syncthreads();
-    T r = s[0];
-    for (int w = 1; w < kThreads / 32; ++w) r = f(r, s[w]);
+struct Sums {
+    float m, S, U;
+};
+// Sums of two sets of weights under the larger of their maxima.
+__device__ __forceinline__ Sums join(const Sums& a, const Sums& b, float c, float d_min) {
+    Sums r;
+    r.m = fmaxf(a.m, b.m);
+    if (r.m == kNegInf) return a;
+    const float da = fmaxf(a.m - r.m, d_min), db = fmaxf(b.m - r.m, d_min);
+    const float wa = ex2(da * c), wb = ex2(db * c);
+    r.S = a.S * wa + b.S * wb;
+    r.U = wa * fmaf(a.S, da, a.U) + wb * fmaf(b.S, db, b.U);
     return r;
 }
 
 template <bool kF32>
-__global__ void __launch_bounds__(kThreads) logprobs_kernel(const LogprobParams p) {
-    __shared__ unsigned long long s_red[kThreads / 32];
-    const int r = blockIdx.x;
+__device__ __forceinline__ float element(const uint4& v, int i) {
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+    if constexpr (kF32) return __uint_as_float(w[i]);
+    else return __uint_as_float(i & 1 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16);
+}
+
+__device__ __forceinline__ uint32_t max_bf16x2(uint32_t a, uint32_t b) {
+    uint32_t r;
+    asm("max.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
+
+template <bool kF32, bool kTop>
+__global__ void __launch_bounds__(kThreads, 4) logprobs_kernel(const LogprobParams p) {
+    constexpr int kPer = kF32 ? 4 : 8;          // logits of a vector
+    __shared__ Key s_list[kTop ? kList : 1];
+    __shared__ Key s_best[kTop ? kThreads : 1];
+    __shared__ Key s_kept[kTop ? CS_MAX_TOP * (kList / kThreads) : 1];
+    __shared__ int s_kept_count;
+    __shared__ Key s_top[CS_MAX_TOP];           // the slice's best, in order
+    __shared__ Key s_bound;
+    __shared__ int s_count;
+    __shared__ Sums s_sums[kThreads / 32];
+    __shared__ Sums s_slice;
+
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    uint32_t ranks;
+    asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(ranks));
+    const uint32_t rank = cluster_rank();
+    const int r = blockIdx.x / ranks, n = p.n_top;
     wait_prior_grid();
     allow_dependent_launch();
-    const void* row = static_cast<const char*>(p.logits) + (size_t)r * p.stride * (kF32 ? 4 : 2);
     const int tok = __ldcg(p.tokens + r);
-    float* s_f = reinterpret_cast<float*>(s_red);
-    float m = kNegInf;
-    if (tok >= 0)
-        for (int v = threadIdx.x; v < p.V; v += kThreads) m = fmaxf(m, logit<kF32>(row, v));
-    m = block_reduce(m, s_f, [](float a, float b) { return fmaxf(a, b); });
-    if (m == kNegInf) {   // not wanted, or nothing but masked tokens
-        if (threadIdx.x == 0) {
-            p.logprob[r] = kNegInf;
-            if (p.entropy) p.entropy[r] = 0.f;
-        }
-        if (threadIdx.x < p.n_top) {
-            p.top_tokens[(size_t)r * p.n_top + threadIdx.x] = -1;
-            p.top_logprobs[(size_t)r * p.n_top + threadIdx.x] = kNegInf;
+    if (tok < 0) {   // (the whole cluster leaves)
+        if (rank == 0) {
+            if (tid == 0) {
+                p.logprob[r] = kNegInf;
+                if (p.entropy) p.entropy[r] = 0.f;
+            }
+            if (tid < n) {
+                p.top_tokens[(size_t)r * n + tid] = -1;
+                p.top_logprobs[(size_t)r * n + tid] = kNegInf;
+            }
         }
         return;
     }
-    float S = 0.f, U = 0.f;
-    for (int v = threadIdx.x; v < p.V; v += kThreads) {
-        const float d = fmaxf(logit<kF32>(row, v) - m, p.d_min), w = ex2_scaled(d, p.c_hi, p.c_lo);
-        S += w;
-        U = fmaf(w, d, U);
+    const char* row = static_cast<const char*>(p.logits) + (size_t)r * p.stride * (kF32 ? 4 : 2);
+    // the row in 16-byte blocks of memory: logit 0 is number `skip` of the first one
+    const uint4* blocks = reinterpret_cast<const uint4*>(reinterpret_cast<uintptr_t>(row) & ~uintptr_t(15));
+    const int skip = (int)((reinterpret_cast<uintptr_t>(row) & 15) / (kF32 ? 4 : 2));
+    const int n_blocks = (skip + p.V + kPer - 1) / kPer;
+    const int per = ((n_blocks + ranks - 1) / ranks + 31) / 32 * 32;     // whole 512-byte pieces a slice
+    const int first = min((int)rank * per, n_blocks), last = min(first + per, n_blocks);
+    float z_tok = 0.f;
+    if (rank == 0 && tid == 0 && tok < p.V)
+        z_tok = kF32 ? __ldcg(reinterpret_cast<const float*>(row) + tok)
+                     : bf16_bits_to_float(__ldcg(reinterpret_cast<const uint16_t*>(row) + tok));
+    if (kTop && tid == 0) {
+        s_bound = 0;
+        s_count = 0;
     }
-    S = block_reduce(S, s_f, [](float a, float b) { return a + b; });
-    U = block_reduce(U, s_f, [](float a, float b) { return a + b; });
-    const float lse = lg2(S) * kLn2;
-    auto lp = [&](float z) {
-        const float d = z - m;   // (-inf where the difference, or d / T, passes fp32)
-        return d * p.i_hi == kNegInf ? kNegInf : fmaf(d, p.i_hi, fmaf(d, p.i_lo, -lse));
+
+    constexpr uint32_t kNone = kF32 ? 0xff800000u : 0xff80ff80u;        // -inf
+    auto load = [&](int base, uint4 (&v)[kVecs]) {
+#pragma unroll
+        for (int u = 0; u < kVecs; ++u) {
+            const int b = base + u * kThreads + tid;
+            v[u] = b < last ? __ldcg(blocks + b) : make_uint4(kNone, kNone, kNone, kNone);
+        }
     };
-    if (threadIdx.x == 0) {
-        p.logprob[r] = tok < p.V ? lp(logit<kF32>(row, tok)) : kNegInf;
-        if (p.entropy) p.entropy[r] = fmaxf(0.f, lse - U / S * p.i_hi);
-    }
-    unsigned long long last = ~0ull;
-    for (int j = 0; j < p.n_top; ++j) {
-        unsigned long long best = 0;
-        for (int v = threadIdx.x; v < p.V; v += kThreads) {
-            const float z = logit<kF32>(row, v);
-            const unsigned long long k = z == kNegInf ? 0 : key_of(z, v);
-            if (k < last && k > best) best = k;
+    // -inf for what a row's first and last block hold of others
+    auto trim = [&](int base, uint4 (&v)[kVecs]) {
+#pragma unroll
+        for (int u = 0; u < kVecs; ++u) {
+            const int b = base + u * kThreads + tid;
+            if ((b != 0 || skip == 0) && (b + 1 != n_blocks || (b + 1) * kPer - skip == p.V)) continue;
+            uint32_t w[4] = {v[u].x, v[u].y, v[u].z, v[u].w};
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) {
+                const int id = b * kPer - skip + i;
+                if (id >= 0 && id < p.V) continue;
+                if (kF32) w[i & 3] = kNone;
+                else if (i & 1) w[i / 2] = (w[i / 2] & 0xffffu) | 0xff800000u;
+                else w[i / 2] = (w[i / 2] & 0xffff0000u) | 0xff80u;
+            }
+            v[u] = make_uint4(w[0], w[1], w[2], w[3]);
         }
-        best = block_reduce(best, s_red, [](unsigned long long a, unsigned long long b) { return a > b ? a : b; });
-        if (threadIdx.x == 0) {
-            const int id = best ? (int)~(uint32_t)best : -1;
-            p.top_tokens[(size_t)r * p.n_top + j] = id;
-            p.top_logprobs[(size_t)r * p.n_top + j] = best ? lp(logit<kF32>(row, id)) : kNegInf;
+    };
+    auto place = [&](Key k, const Key* keys, int count) {   // how many of the keys are larger
+        int at = 0;
+#pragma unroll 4
+        for (int j = 0; j < count; ++j) at += keys[j] > k;
+        return at;
+    };
+    // the n best of the list, in order, into s_top and the front of the list; the
+    // last of them is the bound.  Between barriers.
+    auto cut = [&]() {
+        int count = min(s_count, kList);
+        const Key* keys = s_list;
+        Key mine = 0;
+        if (count > kThreads) {
+            // the n best lie with the threads whose own best is among the n best of those
+            for (int j = tid; j < count; j += kThreads) mine = s_list[j] > mine ? s_list[j] : mine;
+            s_best[tid] = mine;
+            __syncthreads();
+            const bool in = mine != 0 && place(mine, s_best, kThreads) < n;
+            if (tid == 0) s_kept_count = 0;
+            __syncthreads();
+            if (in)
+                for (int j = tid; j < count; j += kThreads) s_kept[atomicAdd(&s_kept_count, 1)] = s_list[j];
+            __syncthreads();
+            count = s_kept_count;
+            keys = s_kept;
         }
-        last = best;
+        mine = tid < count ? keys[tid] : 0;
+        const int at = mine ? place(mine, keys, count) : n;
+        if (tid < n) s_top[tid] = 0;
+        __syncthreads();
+        if (at < n) s_top[at] = mine;
+        __syncthreads();
+        if (tid < n) s_list[tid] = s_top[tid];
+        if (tid == 0) {
+            s_count = min(count, n);
+            if (s_top[n - 1] > s_bound) s_bound = s_top[n - 1];
+        }
+        __syncthreads();
+    };
+
+    Sums t{kNegInf, 0.f, 0.f};
+    uint4 v[kVecs], ahead[kVecs];
+    load(first, v);
+    if (kTop) __syncthreads();   // (the empty list)
+    for (int base = first; base < last; base += kTile) {
+        load(base + kTile, ahead);
+        if ((base == 0 && skip > 0) || base + kTile >= n_blocks) trim(base, v);
+        // ---- the tile's maximum and sums
+        float top;
+        if constexpr (kF32) {
+            top = kNegInf;
+#pragma unroll
+            for (int u = 0; u < kVecs; ++u)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) top = fmaxf(top, element<true>(v[u], i));
+        } else {
+            uint32_t t2 = kNone;
+#pragma unroll
+            for (int u = 0; u < kVecs; ++u)
+                t2 = max_bf16x2(t2, max_bf16x2(max_bf16x2(v[u].x, v[u].y), max_bf16x2(v[u].z, v[u].w)));
+            top = fmaxf(__uint_as_float(t2 << 16), __uint_as_float(t2 & 0xffff0000u));
+        }
+        if (top > t.m) {
+            const float d = fmaxf(t.m - top, p.d_min), w = ex2(d * p.c);
+            t.U = w * fmaf(t.S, d, t.U);
+            t.S *= w;
+            t.m = top;
+        }
+        if (top > kNegInf) {
+            float S[2] = {0.f, 0.f}, U[2] = {0.f, 0.f};
+#pragma unroll
+            for (int u = 0; u < kVecs; ++u)
+#pragma unroll
+                for (int i = 0; i < kPer; ++i) {
+                    const float d = fmaxf(element<kF32>(v[u], i) - t.m, p.d_min), w = ex2(d * p.c);
+                    S[i & 1] += w;
+                    U[i & 1] = fmaf(w, d, U[i & 1]);
+                }
+            t.S += S[0] + S[1];
+            t.U += U[0] + U[1];
+        }
+        // ---- the keys above the bound
+        if constexpr (kTop) {
+            const int id0 = base * kPer - skip;   // the tile's first id
+            auto id_at = [&](int u, int i) { return id0 + (u * kThreads + tid) * kPer + i; };
+            auto append = [&](Key k) {
+                const int at = atomicAdd(&s_count, 1);
+                if (at < kList) s_list[at] = k;
+                return at + 1 >= kListFull;
+            };
+            auto push = [&]() {   // whether the list is to be cut
+                const Key bound = s_bound;
+                bool full = false;
+                if (top == kNegInf || key_of(top, 0) <= bound) return false;
+                const float least = bound ? logit_of(bound) : kNegInf;
+#pragma unroll
+                for (int u = 0; u < kVecs; ++u)
+#pragma unroll
+                    for (int i = 0; i < kPer; ++i) {
+                        const float z = element<kF32>(v[u], i);
+                        if (z < least || z == kNegInf) continue;
+                        const Key k = key_of(z, id_at(u, i));
+                        if (k > bound) full |= append(k);
+                    }
+                return full;
+            };
+            const bool begin = base == first;
+            if (begin || __syncthreads_or(push())) {
+                if (begin || s_count > kList) {
+                    // a bound from this tile alone, under which the list takes it (again);
+                    // what lies in the list from the tiles before came first
+                    Key best = 0, kept = tid < min(s_count, kListFull) ? s_list[tid] : 0;
+                    if (kept && id_of(kept) >= id0) kept = 0;
+#pragma unroll
+                    for (int u = 0; u < kVecs; ++u)
+#pragma unroll
+                        for (int i = 0; i < kPer; ++i) {
+                            const float z = element<kF32>(v[u], i);
+                            const Key k = z == kNegInf ? 0 : key_of(z, id_at(u, i));
+                            best = k > best ? k : best;
+                        }
+                    s_best[tid] = best;
+                    __syncthreads();
+                    if (tid == 0) s_count = 0;
+                    if (best > s_bound && place(best, s_best, kThreads) == n - 1) s_bound = best - 1;   // (one thread)
+                    __syncthreads();
+                    if (kept) append(kept);
+                    push();
+                    __syncthreads();
+                }
+                cut();
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < kVecs; ++u) v[u] = ahead[u];
     }
+
+    // ---- the slice's sums and best keys
+#pragma unroll
+    for (int off = 16; off > 0; off >>= 1) {
+        const Sums o{__shfl_xor_sync(0xffffffffu, t.m, off), __shfl_xor_sync(0xffffffffu, t.S, off),
+                     __shfl_xor_sync(0xffffffffu, t.U, off)};
+        t = join(t, o, p.c, p.d_min);
+    }
+    if (lane == 0) s_sums[warp] = t;
+    __syncthreads();
+    if (kTop) cut();
+    if (tid == 0) {
+        for (int w = 1; w < kThreads / 32; ++w) t = join(t, s_sums[w], p.c, p.d_min);
+        s_slice = t;
+    }
+    if (ranks > 1) {
+        cluster_sync();
+        if (rank == 0 && tid == 0) {
+            for (uint32_t k = 1; k < ranks; ++k) {
+                const Sums o{load_float(at_rank(&s_slice.m, k)), load_float(at_rank(&s_slice.S, k)),
+                             load_float(at_rank(&s_slice.U, k))};
+                t = join(t, o, p.c, p.d_min);
+            }
+            s_sums[0] = t;
+        }
+        if (kTop && rank == 0) {
+            const int count = (int)ranks * n;
+            Key mine = 0;
+            if (tid < count) mine = load_key(at_rank(&s_top[tid % n], tid / n));
+            s_best[tid] = mine;
+            __syncthreads();
+            const int at = mine ? place(mine, s_best, count) : n;
+            __syncthreads();   // (its own s_top is read above)
+            if (tid < n) s_top[tid] = 0;
+            __syncthreads();
+            if (at < n) s_top[at] = mine;
+        }
+        cluster_sync();
+        if (rank != 0) return;
+    } else if (tid == 0) {
+        s_sums[0] = t;
+    }
+    __syncthreads();
+    const Sums all = s_sums[0];
+    const float lse = lg2(all.S) * kLn2;
+    auto lp = [&](float z) {
+        const float d = z - all.m;   // (-inf where the difference, or d / T, passes fp32)
+        return all.m == kNegInf || d * p.i_hi == kNegInf ? kNegInf : fmaf(d, p.i_hi, fmaf(d, p.i_lo, -lse));
+    };
+    if (tid == 0) {
+        p.logprob[r] = tok < p.V ? lp(z_tok) : kNegInf;
+        if (p.entropy) p.entropy[r] = all.m == kNegInf ? 0.f : fmaxf(0.f, lse - all.U / all.S * p.i_hi);
+    }
+    if (kTop && tid < n) {
+        const Key k = s_top[tid];
+        p.top_tokens[(size_t)r * n + tid] = k ? id_of(k) : -1;
+        p.top_logprobs[(size_t)r * n + tid] = k ? lp(logit_of(k)) : kNegInf;
+    }
+}
+
+// CTAs a row: as many as leave each some 16 KB, while there are fewer CTAs than
+// the GPU holds at once.
+int cluster_of(const cs_logprob_dims& d) {
+    const size_t bytes = (size_t)d.vocab * (d.logit_dtype == CS_F32 ? 4 : 2);
+    int c = 1;
+    while (c < kMaxCluster && (long long)d.rows * c < 4LL * current_sm_count() && bytes / (2 * c) >= 16384) c *= 2;
+    return c;
 }
 
 }  // namespace
@@ -123,15 +409,29 @@ cs_status launch_logprobs(const cs_logprob_dims& d, const void* logits, const in
     p.V = d.vocab;
     p.n_top = d.n_top;
     p.stride = d.row_stride;
-    // (below 1e-37 a temperature picks the largest logits alone, as 1e-37 does)
-    const double i = 1.0 / (double)(temperature < 1e-37f ? 1e-37f : temperature), c = 1.4426950408889634073599 * i;
+    const double i = 1.0 / (double)temperature, c = 1.4426950408889634073599 * i;
+    p.c = (float)c;
     p.i_hi = (float)i;
     p.i_lo = (float)(i - (double)p.i_hi);
-    p.c_hi = (float)c;
-    p.c_lo = (float)(c - (double)p.c_hi);
     p.d_min = (float)(-300.0 / c);
-    const cudaError_t e = launch_dependent(d.logit_dtype == CS_F32 ? logprobs_kernel<true> : logprobs_kernel<false>,
-                                           dim3(d.rows), dim3(kThreads), 0, stream, p);
+    using Kern = void (*)(const LogprobParams);
+    static const Kern kerns[2][2] = {{logprobs_kernel<false, false>, logprobs_kernel<false, true>},
+                                     {logprobs_kernel<true, false>, logprobs_kernel<true, true>}};
+    const int cluster = cluster_of(d);
+    if ((long long)d.rows * cluster > 0x7fffffffLL) return fail(CS_ERR_UNSUPPORTED, "too many rows in one call");
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = cluster;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(d.rows * cluster));
+    cfg.blockDim = dim3(kThreads);
+    cfg.stream = stream;
+    cfg.attrs = attr;
+    cfg.numAttrs = 2;
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, kerns[d.logit_dtype == CS_F32][d.n_top > 0], p);
     return e == cudaSuccess ? CS_OK : cuda_fail(e, "logprobs_kernel launch");
 }
 
