@@ -14,8 +14,8 @@
 // grown, its n best stay and the last of them is the new bound.  The first bound
 // is the n-th largest of the threads' best keys of the first tile (of 8192 bf16
 // logits some 25 lie above it).  A tile with more keys above the bound than the
-// list takes is taken again with such a bound of its own, which at most n
-// threads have keys above.  Keys are unique, so the order in which they arrive
+// list takes is taken again with such a bound of its own, which little more
+// than n threads have keys above.  Keys are unique, so the order in which they arrive
 // changes nothing.  The first CTA of the cluster merges the slices' sums and
 // lists through distributed shared memory.
 #include "cs_internal.h"
@@ -29,8 +29,9 @@ constexpr int kVecs = 4;                       // 16-byte vectors of a thread's 
 constexpr int kTile = kThreads * kVecs;
 constexpr int kMaxCluster = 8;
 constexpr int kListFull = 192;                 // from here on the list is cut to the n best
-constexpr int kList = 2048;                    // what it takes: kListFull, and the keys of CS_MAX_TOP threads
-static_assert(kList >= kListFull + CS_MAX_TOP * kVecs * 8, "a tile's keys above its threads' n-th best fit");
+constexpr int kSlack = 8;                      // more keys than n that a bound may let through
+constexpr int kList = 2048;                    // what the list takes
+static_assert(kList >= kListFull + (CS_MAX_TOP + kSlack) * kVecs * 8, "a tile's keys above its threads' n-th best fit");
 static_assert(kListFull <= kThreads && kMaxCluster * CS_MAX_TOP <= kThreads, "a thread a key");
 
 using Key = unsigned long long;
@@ -195,11 +196,24 @@ __global__ void __launch_bounds__(kThreads, 4) logprobs_kernel(const LogprobPara
         for (int j = 0; j < count; ++j) at += keys[j] > k;
         return at;
     };
-    // the n best of the list, in order, into s_top and the front of the list; the
-    // last of them is the bound.  Between barriers.
-    auto cut = [&]() {
+    // The largest T for which n or more of the threads' numbers reach T (0 where
+    // fewer than n are not 0), or one that n + kSlack do at most; and how many do.
+    auto nth_of = [&](uint32_t o, int& reach) {
+        uint32_t T = 0;
+        reach = kThreads;
+        for (int bit = 31; bit >= (kF32 ? 0 : 16); --bit) {   // (a bf16's low half is 0, or all ones)
+            const int c = __syncthreads_count(o >= (T | 1u << bit));
+            if (c < n) continue;
+            T |= 1u << bit;
+            reach = c;
+            if (c <= n + kSlack) break;
+        }
+        return T;
+    };
+    // Cuts the list; the bound follows.  `last_cut`: to the n best, in order in
+    // s_top; else to as many as reach the n-th best logit (or a few more).  Between barriers.
+    auto cut = [&](bool last_cut) {
         int count = min(s_count, kList);
-        const Key* keys = s_list;
         Key mine = 0;
         if (count > kThreads) {
             // the n best lie with the threads whose own best is among the n best of those
@@ -213,18 +227,38 @@ __global__ void __launch_bounds__(kThreads, 4) logprobs_kernel(const LogprobPara
                 for (int j = tid; j < count; j += kThreads) s_kept[atomicAdd(&s_kept_count, 1)] = s_list[j];
             __syncthreads();
             count = s_kept_count;
-            keys = s_kept;
+            mine = tid < count ? s_kept[tid] : 0;
+            __syncthreads();
+        } else {
+            mine = tid < count ? s_list[tid] : 0;
         }
-        mine = tid < count ? keys[tid] : 0;
-        const int at = mine ? place(mine, keys, count) : n;
-        if (tid < n) s_top[tid] = 0;
-        __syncthreads();
-        if (at < n) s_top[at] = mine;
-        __syncthreads();
-        if (tid < n) s_list[tid] = s_top[tid];
-        if (tid == 0) {
-            s_count = min(count, n);
-            if (s_top[n - 1] > s_bound) s_bound = s_top[n - 1];
+        int reach = count;
+        uint32_t T = 0;
+        if (count > n) T = nth_of((uint32_t)(mine >> 32), reach);
+        if (tid == 0) s_kept_count = 0;
+        __syncthreads();   // (and s_list, s_kept are read)
+        const bool keep = mine != 0 && (uint32_t)(mine >> 32) >= T;
+        if (last_cut || reach > kListFull / 2) {   // (many equal logits: by their ids)
+            if (keep) s_best[atomicAdd(&s_kept_count, 1)] = mine;
+            if (tid < n) s_top[tid] = 0;
+            __syncthreads();
+            count = s_kept_count;
+            mine = tid < count ? s_best[tid] : 0;
+            const int at = mine ? place(mine, s_best, count) : n;
+            if (at < n) s_top[at] = mine;
+            __syncthreads();
+            if (tid < n) s_list[tid] = s_top[tid];
+            if (tid == 0) {
+                s_count = min(count, n);
+                if (s_top[n - 1] > s_bound) s_bound = s_top[n - 1];
+            }
+        } else {
+            if (keep) s_list[atomicAdd(&s_kept_count, 1)] = mine;
+            if (tid == 0) {
+                s_count = reach;
+                const Key bound = T ? ((Key)T << 32) - 1 : 0;
+                if (bound > s_bound) s_bound = bound;
+            }
         }
         __syncthreads();
     };
@@ -285,7 +319,16 @@ __global__ void __launch_bounds__(kThreads, 4) logprobs_kernel(const LogprobPara
                 if (top == kNegInf || key_of(top, 0) <= bound) return false;
                 const float least = bound ? logit_of(bound) : kNegInf;
 #pragma unroll
-                for (int u = 0; u < kVecs; ++u)
+                for (int u = 0; u < kVecs; ++u) {
+                    float most;
+                    if constexpr (kF32) {
+                        most = fmaxf(fmaxf(element<true>(v[u], 0), element<true>(v[u], 1)),
+                                     fmaxf(element<true>(v[u], 2), element<true>(v[u], 3)));
+                    } else {
+                        const uint32_t m2 = max_bf16x2(max_bf16x2(v[u].x, v[u].y), max_bf16x2(v[u].z, v[u].w));
+                        most = fmaxf(__uint_as_float(m2 << 16), __uint_as_float(m2 & 0xffff0000u));
+                    }
+                    if (most < least || most == kNegInf) continue;
 #pragma unroll
                     for (int i = 0; i < kPer; ++i) {
                         const float z = element<kF32>(v[u], i);
@@ -293,6 +336,7 @@ __global__ void __launch_bounds__(kThreads, 4) logprobs_kernel(const LogprobPara
                         const Key k = key_of(z, id_at(u, i));
                         if (k > bound) full |= append(k);
                     }
+                }
                 return full;
             };
             const bool begin = base == first;
@@ -310,16 +354,22 @@ __global__ void __launch_bounds__(kThreads, 4) logprobs_kernel(const LogprobPara
                             const Key k = z == kNegInf ? 0 : key_of(z, id_at(u, i));
                             best = k > best ? k : best;
                         }
+                    int reach;
+                    const uint32_t T = nth_of((uint32_t)(best >> 32), reach);
                     s_best[tid] = best;
                     __syncthreads();
                     if (tid == 0) s_count = 0;
-                    if (best > s_bound && place(best, s_best, kThreads) == n - 1) s_bound = best - 1;   // (one thread)
+                    if (reach <= n + kSlack) {
+                        if (tid == 0 && T && ((Key)T << 32) - 1 > s_bound) s_bound = ((Key)T << 32) - 1;
+                    } else if (best > s_bound && place(best, s_best, kThreads) == n - 1) {
+                        s_bound = best - 1;   // (one thread's)
+                    }
                     __syncthreads();
                     if (kept) append(kept);
                     push();
                     __syncthreads();
                 }
-                cut();
+                cut(false);
             }
         }
 #pragma unroll
@@ -335,7 +385,7 @@ __global__ void __launch_bounds__(kThreads, 4) logprobs_kernel(const LogprobPara
     }
     if (lane == 0) s_sums[warp] = t;
     __syncthreads();
-    if (kTop) cut();
+    if (kTop) cut(true);
     if (tid == 0) {
         for (int w = 1; w < kThreads / 32; ++w) t = join(t, s_sums[w], p.c, p.d_min);
         s_slice = t;
