@@ -9,15 +9,16 @@
 //     ln sum exp(z / T) = m / T + ln S,   H = ln S - U / (S T).
 //
 // The alternatives: a logit and its id are one ordered number (the larger
-// logit, then the lower id).  A CTA keeps a bound no higher than its n-th best
-// and puts the keys above it into a list in shared memory; when the list has
-// grown, its n best stay and the last of them is the new bound.  The first bound
-// is the n-th largest of the threads' best keys of the first tile (of 8192 bf16
-// logits some 25 lie above it).  A tile with more keys above the bound than the
-// list takes is taken again with such a bound of its own, which little more
-// than n threads have keys above.  Keys are unique, so the order in which they arrive
-// changes nothing.  The first CTA of the cluster merges the slices' sums and
-// lists through distributed shared memory.
+// logit, then the lower id).  While it streams, a thread keeps the maximum of
+// each sixteenth of its logits (a cell) in shared memory.  At the end the n-th
+// largest of the threads' maxima is a bound that at least n logits reach, and
+// few more do (n = 20 of 128256: 21 on average): the cells that reach it are
+// read again, from L2, and their keys ranked.  Rows on which too many cells or
+// keys reach the bound (ties by the thousand, rows made to that end) are read
+// again tile by tile, with a list that is cut to the n best and a bound that
+// grows.  Keys are unique, so the order in which they arrive changes nothing.
+// The first CTA of the cluster merges the slices' sums and keys through
+// distributed shared memory.
 #include "cs_internal.h"
 #include "cs_device.cuh"
 
@@ -28,7 +29,9 @@ constexpr int kThreads = 256;
 constexpr int kVecs = 4;                       // 16-byte vectors of a thread's tile
 constexpr int kTile = kThreads * kVecs;
 constexpr int kMaxCluster = 8;
-constexpr int kListFull = 192;                 // from here on the list is cut to the n best
+constexpr int kListFull = 2 * CS_MAX_TOP + 24;  // a list of 2 n + 24 keys is cut to the n best
+constexpr int kCells = 16;                     // parts of a thread's logits
+constexpr int kMaxCells = 512;                 // of the CTA's cells that are read again
 constexpr int kSlack = 8;                      // more keys than n that a bound may let through
 constexpr int kList = 2048;                    // what the list takes
 static_assert(kList >= kListFull + (CS_MAX_TOP + kSlack) * kVecs * 8, "a tile's keys above its threads' n-th best fit");
@@ -119,6 +122,9 @@ __global__ void __launch_bounds__(kThreads, 4) logprobs_kernel(const LogprobPara
     constexpr int kPer = kF32 ? 4 : 8;          // logits of a vector
     __shared__ Key s_list[kTop ? kList : 1];
     __shared__ Key s_best[kTop ? kThreads : 1];
+    __shared__ float s_cell[kTop ? kCells : 1][kTop ? kThreads : 1];
+    __shared__ int s_cells[kTop ? kMaxCells : 1];
+    __shared__ int s_cell_count;
     __shared__ Key s_kept[kTop ? CS_MAX_TOP * (kList / kThreads) : 1];
     __shared__ int s_kept_count;
     __shared__ Key s_top[CS_MAX_TOP];           // the slice's best, in order
@@ -131,7 +137,7 @@ __global__ void __launch_bounds__(kThreads, 4) logprobs_kernel(const LogprobPara
     uint32_t ranks;
     asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(ranks));
     const uint32_t rank = cluster_rank();
-    const int r = blockIdx.x / ranks, n = p.n_top;
+    const int r = blockIdx.x / ranks, n = p.n_top, full_at = 2 * n + 24;
     wait_prior_grid();
     allow_dependent_launch();
     const int tok = __ldcg(p.tokens + r);
@@ -162,6 +168,7 @@ __global__ void __launch_bounds__(kThreads, 4) logprobs_kernel(const LogprobPara
     if (kTop && tid == 0) {
         s_bound = 0;
         s_count = 0;
+        s_cell_count = 0;
     }
 
     constexpr uint32_t kNone = kF32 ? 0xff800000u : 0xff80ff80u;        // -inf
@@ -173,21 +180,24 @@ __global__ void __launch_bounds__(kThreads, 4) logprobs_kernel(const LogprobPara
         }
     };
     // -inf for what a row's first and last block hold of others
+    auto trim_vector = [&](int b, uint4& x) {
+        if ((b != 0 || skip == 0) && (b + 1 != n_blocks || (b + 1) * kPer - skip == p.V)) return;
+        uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+            const int id = b * kPer - skip + i;
+            if (id >= 0 && id < p.V) continue;
+            if (kF32) w[i & 3] = kNone;
+            else if (i & 1) w[i / 2] = (w[i / 2] & 0xffffu) | 0xff800000u;
+            else w[i / 2] = (w[i / 2] & 0xffff0000u) | 0xff80u;
+        }
+        x = make_uint4(w[0], w[1], w[2], w[3]);
+    };
     auto trim = [&](int base, uint4 (&v)[kVecs]) {
 #pragma unroll
         for (int u = 0; u < kVecs; ++u) {
             const int b = base + u * kThreads + tid;
-            if ((b != 0 || skip == 0) && (b + 1 != n_blocks || (b + 1) * kPer - skip == p.V)) continue;
-            uint32_t w[4] = {v[u].x, v[u].y, v[u].z, v[u].w};
-#pragma unroll
-            for (int i = 0; i < kPer; ++i) {
-                const int id = b * kPer - skip + i;
-                if (id >= 0 && id < p.V) continue;
-                if (kF32) w[i & 3] = kNone;
-                else if (i & 1) w[i / 2] = (w[i / 2] & 0xffffu) | 0xff800000u;
-                else w[i / 2] = (w[i / 2] & 0xffff0000u) | 0xff80u;
-            }
-            v[u] = make_uint4(w[0], w[1], w[2], w[3]);
+            if (b < last) trim_vector(b, v[u]);
         }
     };
     auto place = [&](Key k, const Key* keys, int count) {   // how many of the keys are larger
@@ -238,7 +248,7 @@ __global__ void __launch_bounds__(kThreads, 4) logprobs_kernel(const LogprobPara
         if (tid == 0) s_kept_count = 0;
         __syncthreads();   // (and s_list, s_kept are read)
         const bool keep = mine != 0 && (uint32_t)(mine >> 32) >= T;
-        if (last_cut || reach > kListFull / 2) {   // (many equal logits: by their ids)
+        if (last_cut || reach > n + kSlack) {   // (many equal logits: by their ids)
             if (keep) s_best[atomicAdd(&s_kept_count, 1)] = mine;
             if (tid < n) s_top[tid] = 0;
             __syncthreads();
@@ -263,10 +273,49 @@ __global__ void __launch_bounds__(kThreads, 4) logprobs_kernel(const LogprobPara
         __syncthreads();
     };
 
+    auto top_of = [&](const uint4& x) {   // a vector's largest logit
+        if constexpr (kF32) {
+            return fmaxf(fmaxf(element<true>(x, 0), element<true>(x, 1)), fmaxf(element<true>(x, 2), element<true>(x, 3)));
+        } else {
+            const uint32_t m2 = max_bf16x2(max_bf16x2(x.x, x.y), max_bf16x2(x.z, x.w));
+            return fmaxf(__uint_as_float(m2 << 16), __uint_as_float(m2 & 0xffff0000u));
+        }
+    };
+    auto append = [&](Key k) {   // whether the list is to be cut
+        const int at = atomicAdd(&s_count, 1);
+        if (at < kList) s_list[at] = k;
+        return at + 1 >= full_at;
+    };
+    // the keys of a vector that reach `least` and lie above the bound, in a rolled
+    // loop: little code for few threads
+    auto push_vector = [&](uint4 w, int id, float least, Key bound) {
+        bool full = false;
+#pragma unroll 1
+        for (int i = 0; i < kPer; ++i) {
+            const float z = element<kF32>(w, 0);
+            if (kF32) {
+                w.x = w.y;
+                w.y = w.z;
+                w.z = w.w;
+            } else {
+                w.x = __byte_perm(w.x, w.y, 0x5432);
+                w.y = __byte_perm(w.y, w.z, 0x5432);
+                w.z = __byte_perm(w.z, w.w, 0x5432);
+                w.w >>= 16;
+            }
+            if (z < least || z == kNegInf) continue;
+            const Key k = key_of(z, id + i);
+            if (k > bound) full |= append(k);
+        }
+        return full;
+    };
+
     Sums t{kNegInf, 0.f, 0.f};
     uint4 v[kVecs], ahead[kVecs];
+    const int tiles = (last - first + kTile - 1) / kTile, cell_tiles = (tiles + kCells - 1) / kCells;
+    int cell = 0, in_cell = 0;
+    float cell_top = kNegInf;
     load(first, v);
-    if (kTop) __syncthreads();   // (the empty list)
     for (int base = first; base < last; base += kTile) {
         load(base + kTile, ahead);
         if ((base == 0 && skip > 0) || base + kTile >= n_blocks) trim(base, v);
@@ -292,55 +341,83 @@ __global__ void __launch_bounds__(kThreads, 4) logprobs_kernel(const LogprobPara
             t.m = top;
         }
         if (top > kNegInf) {
-            float S[2] = {0.f, 0.f}, U[2] = {0.f, 0.f};
+            const uint64_t m2 = f2_pack(t.m, t.m), c2 = f2_pack(p.c, p.c);
+            uint64_t S2 = 0, U2 = 0;
 #pragma unroll
             for (int u = 0; u < kVecs; ++u)
 #pragma unroll
-                for (int i = 0; i < kPer; ++i) {
-                    const float d = fmaxf(element<kF32>(v[u], i) - t.m, p.d_min), w = ex2(d * p.c);
-                    S[i & 1] += w;
-                    U[i & 1] = fmaf(w, d, U[i & 1]);
+                for (int i = 0; i < kPer; i += 2) {
+                    float d0, d1, w0, w1;
+                    f2_unpack(f2_sub(f2_pack(element<kF32>(v[u], i), element<kF32>(v[u], i + 1)), m2), d0, d1);
+                    const uint64_t d2 = f2_pack(fmaxf(d0, p.d_min), fmaxf(d1, p.d_min));   // (a -inf too)
+                    f2_unpack(f2_mul(d2, c2), w0, w1);
+                    const uint64_t w2 = f2_pack(ex2(w0), ex2(w1));
+                    S2 = f2_add(S2, w2);
+                    U2 = f2_fma(w2, d2, U2);
                 }
-            t.S += S[0] + S[1];
-            t.U += U[0] + U[1];
+            float S0, S1, U0, U1;
+            f2_unpack(S2, S0, S1);
+            f2_unpack(U2, U0, U1);
+            t.S += S0 + S1;
+            t.U += U0 + U1;
         }
-        // ---- the keys above the bound
         if constexpr (kTop) {
-            const int id0 = base * kPer - skip;   // the tile's first id
-            auto id_at = [&](int u, int i) { return id0 + (u * kThreads + tid) * kPer + i; };
-            auto append = [&](Key k) {
-                const int at = atomicAdd(&s_count, 1);
-                if (at < kList) s_list[at] = k;
-                return at + 1 >= kListFull;
-            };
-            auto push = [&]() {   // whether the list is to be cut
-                const Key bound = s_bound;
-                bool full = false;
-                if (top == kNegInf || key_of(top, 0) <= bound) return false;
-                const float least = bound ? logit_of(bound) : kNegInf;
+            cell_top = fmaxf(cell_top, top);
+            if (++in_cell == cell_tiles || base + kTile >= last) {
+                s_cell[cell++][tid] = cell_top;
+                cell_top = kNegInf;
+                in_cell = 0;
+            }
+        }
 #pragma unroll
-                for (int u = 0; u < kVecs; ++u) {
-                    float most;
-                    if constexpr (kF32) {
-                        most = fmaxf(fmaxf(element<true>(v[u], 0), element<true>(v[u], 1)),
-                                     fmaxf(element<true>(v[u], 2), element<true>(v[u], 3)));
-                    } else {
-                        const uint32_t m2 = max_bf16x2(max_bf16x2(v[u].x, v[u].y), max_bf16x2(v[u].z, v[u].w));
-                        most = fmaxf(__uint_as_float(m2 << 16), __uint_as_float(m2 & 0xffff0000u));
-                    }
-                    if (most < least || most == kNegInf) continue;
-#pragma unroll
-                    for (int i = 0; i < kPer; ++i) {
-                        const float z = element<kF32>(v[u], i);
-                        if (z < least || z == kNegInf) continue;
-                        const Key k = key_of(z, id_at(u, i));
-                        if (k > bound) full |= append(k);
-                    }
+        for (int u = 0; u < kVecs; ++u) v[u] = ahead[u];
+    }
+
+    if constexpr (kTop) {
+        __syncthreads();   // (the counts of 0)
+        const uint32_t mine = t.m == kNegInf ? 0 : (uint32_t)(key_of(t.m, 0) >> 32);
+        int reach;
+        const uint32_t T = nth_of(mine, reach);
+        const float least = T ? logit_of((Key)T << 32) : -3.4028235e38f;   // (fewer than n threads have any: all of theirs)
+        if (t.m >= least)
+            for (int j = 0; j < cell; ++j)
+                if (s_cell[j][tid] >= least) {
+                    const int at = atomicAdd(&s_cell_count, 1);
+                    if (at < kMaxCells) s_cells[at] = j * kThreads + tid;
                 }
-                return full;
-            };
-            const bool begin = base == first;
-            if (begin || __syncthreads_or(push())) {
+        __syncthreads();
+        const int cells = s_cell_count, cell_vecs = cell_tiles * kVecs;
+        if (cells <= kMaxCells) {
+            for (int j = tid; j < cells * cell_vecs; j += kThreads) {
+                const int of = s_cells[j / cell_vecs], k = j % cell_vecs;   // vector k of the cell
+                const int b = first + (of / kThreads * cell_vecs + k) * kThreads + of % kThreads;
+                if (b >= last) continue;
+                uint4 x[kVecs] = {__ldcg(blocks + b)};
+                trim_vector(b, x[0]);
+                if (top_of(x[0]) >= least) push_vector(x[0], b * kPer - skip, least, 0);
+            }
+        }
+        __syncthreads();
+        if (cells > kMaxCells || s_count > kList) {
+            __syncthreads();
+            if (tid == 0) s_count = 0;
+            __syncthreads();
+            for (int base = first; base < last; base += kTile) {
+                load(base, v);
+                if ((base == 0 && skip > 0) || base + kTile >= n_blocks) trim(base, v);
+                const int id0 = base * kPer - skip;   // the tile's first id
+                auto id_at = [&](int u) { return id0 + (u * kThreads + tid) * kPer; };
+                auto push = [&]() {
+                    const Key bound = s_bound;
+                    const float at_least = bound ? logit_of(bound) : kNegInf;
+                    bool full = false;
+#pragma unroll
+                    for (int u = 0; u < kVecs; ++u)
+                        if (top_of(v[u]) >= at_least) full |= push_vector(v[u], id_at(u), at_least, bound);
+                    return full;
+                };
+                const bool begin = base == first;
+                if (!begin && !__syncthreads_or(push())) continue;
                 if (begin || s_count > kList) {
                     // a bound from this tile alone, under which the list takes it (again);
                     // what lies in the list from the tiles before came first
@@ -351,19 +428,13 @@ __global__ void __launch_bounds__(kThreads, 4) logprobs_kernel(const LogprobPara
 #pragma unroll
                         for (int i = 0; i < kPer; ++i) {
                             const float z = element<kF32>(v[u], i);
-                            const Key k = z == kNegInf ? 0 : key_of(z, id_at(u, i));
+                            const Key k = z == kNegInf ? 0 : key_of(z, id_at(u) + i);
                             best = k > best ? k : best;
                         }
-                    int reach;
-                    const uint32_t T = nth_of((uint32_t)(best >> 32), reach);
                     s_best[tid] = best;
                     __syncthreads();
                     if (tid == 0) s_count = 0;
-                    if (reach <= n + kSlack) {
-                        if (tid == 0 && T && ((Key)T << 32) - 1 > s_bound) s_bound = ((Key)T << 32) - 1;
-                    } else if (best > s_bound && place(best, s_best, kThreads) == n - 1) {
-                        s_bound = best - 1;   // (one thread's)
-                    }
+                    if (best > s_bound && place(best, s_best, kThreads) == n - 1) s_bound = best - 1;   // (one thread's)
                     __syncthreads();
                     if (kept) append(kept);
                     push();
@@ -372,8 +443,6 @@ __global__ void __launch_bounds__(kThreads, 4) logprobs_kernel(const LogprobPara
                 cut(false);
             }
         }
-#pragma unroll
-        for (int u = 0; u < kVecs; ++u) v[u] = ahead[u];
     }
 
     // ---- the slice's sums and best keys
