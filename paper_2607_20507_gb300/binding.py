@@ -684,6 +684,10 @@ def _rows_of(page_table, ctx_lens, B: int, dev) -> None:
 def cs_packed_kv_append(new_k, new_v, pool, page_table, ctx_lens, stream: int | None = None):
     """Quantise the K/V rows of the newest positions into a packed cache (in place).
     new_k / new_v bf16 [B, n_new, Hkv, 128]; ``pool`` a PackedPool.  See include/cachespec.h."""
+    r = (_fast or _load_fast()).packed_kv_append(new_k, new_v, pool, page_table, ctx_lens, stream)
+    if r is not None:
+        _done(r)
+        return
     lib = load_library()
     _need(new_k, "new_k", torch.bfloat16, 4, None)
     dev = new_k.device
@@ -703,6 +707,9 @@ def cs_packed_kv_append(new_k, new_v, pool, page_table, ctx_lens, stream: int | 
 
 def cs_packed_kv_read(pool, page_table, ctx_lens, n_rows: int, stream: int | None = None):
     """The newest ``n_rows`` rows of every request from a packed cache; returns (k, v), bf16 [B, n_rows, Hkv, 128]."""
+    r = (_fast or _load_fast()).packed_kv_read(pool, page_table, ctx_lens, n_rows, stream)
+    if r is not None:
+        return _done(r)
     lib = load_library()
     dev = page_table.device
     ptrs, (P, Hkv, ps) = _packed(pool, dev)
@@ -722,6 +729,10 @@ def cs_packed_verify_attention(q, pool, page_table, ctx_lens, n_draft, out=None,
                                stream: int | None = None):
     """Verify attention over a packed cache, ``n_draft`` in [0, 16]; returns ``out`` (bf16 [B, k+1, Hq, 128]).
     See include/cachespec.h."""
+    r = (_fast or _load_fast()).packed_verify_attention(q, pool, page_table, ctx_lens, n_draft, out, workspace, sm_scale,
+                                                        stream)
+    if r is not None:
+        return _done(r)
     lib = load_library()
     _need(q, "q", torch.bfloat16, 4, None)
     dev = q.device
@@ -773,6 +784,9 @@ def cs_kv_fork(pools, page_table, ctx_lens, ref_counts, src, dst, page_size: int
     """Rows ``dst`` of the page table become copies of rows ``src`` (-1: empty rows) that share their full pages,
     with room for ``room`` more tokens each; table, lengths and counts change in place.  ``pools``: the cache's
     tensors, each [P, ...].  Returns int32 [n]: 1 where there were enough free pages.  See include/cachespec.h."""
+    r = (_fast or _load_fast()).kv_fork(pools, page_table, ctx_lens, ref_counts, src, dst, page_size, room, workspace, stream)
+    if r is not None:
+        return _done(r)
     lib = load_library()
     dev = page_table.device
     d = _page_call(page_table, ctx_lens, ref_counts, page_size, dev)
@@ -795,6 +809,10 @@ def cs_kv_fork(pools, page_table, ctx_lens, ref_counts, src, dst, page_size: int
 
 def cs_kv_release(page_table, ctx_lens, ref_counts, rows, keep_lens, page_size: int, stream: int | None = None):
     """Rows ``rows`` keep the pages of their first ``keep_lens`` tokens and give the others back (in place)."""
+    r = (_fast or _load_fast()).kv_release(page_table, ctx_lens, ref_counts, rows, keep_lens, page_size, stream)
+    if r is not None:
+        _done(r)
+        return
     lib = load_library()
     dev = page_table.device
     d = _page_call(page_table, ctx_lens, ref_counts, page_size, dev)
@@ -812,6 +830,9 @@ def cs_kv_release(page_table, ctx_lens, ref_counts, rows, keep_lens, page_size: 
 def cs_kv_compact(pools, page_table, ref_counts, workspace=None, stream: int | None = None):
     """Moves the pages in use to the lowest ids; pools, table and counts change in place.
     Returns int32 [1]: how many pages are in use.  See include/cachespec.h."""
+    r = (_fast or _load_fast()).kv_compact(pools, page_table, ref_counts, workspace, stream)
+    if r is not None:
+        return _done(r)
     lib = load_library()
     dev = page_table.device
     d = _page_call(page_table, None, ref_counts, 1, dev)
@@ -831,6 +852,9 @@ def cs_logprobs(logits, tokens, temperature: float = 1.0, n_top: int = 0, stream
     """Log probabilities of ``tokens`` (int32 [N]; negative: the row is skipped) under ``logits`` [N, V], whose rows
     may lie apart.  Returns (logprob [N], entropy [N], top tokens [N, n_top], their log probabilities [N, n_top]).
     See include/cachespec.h."""
+    r = (_fast or _load_fast()).logprobs(logits, tokens, temperature, n_top, stream)
+    if r is not None:
+        return _done(r)
     lib = load_library()
     if not isinstance(logits, torch.Tensor):
         raise TypeError("logits must be a torch.Tensor")

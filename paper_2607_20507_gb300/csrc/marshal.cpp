@@ -81,8 +81,9 @@ bool stream_of(PyObject* o, c10::Device dev, cs_stream_t* s) {
     return false;
 }
 
-enum Kind { kAttn, kTreeAttn, kAccept, kTreeAccept, kSample, kRoute };
-const char* const kKinds[] = {"attn", "tree_attn", "accept", "tree_accept", "sample", "route"};
+enum Kind { kAttn, kTreeAttn, kAccept, kTreeAccept, kSample, kRoute, kPackedAttn, kFork, kCompact };
+const char* const kKinds[] = {"attn", "tree_attn", "accept", "tree_accept", "sample", "route", "packed_attn", "fork",
+                              "compact"};
 
 // Scratch of a call; `hold` is the kept workspace it lies in.
 struct Scratch {
@@ -382,6 +383,232 @@ CALL(kv_commit_tree, 7)
     Py_RETURN_TRUE;
 CALL_END
 
+// A PackedPool (a tuple of four tensors and two that may be None): its pointers and its shape [P, Hkv, ps].
+bool packed(PyObject* o, c10::Device dev, cs_packed_pool* p, const at::Tensor** codes) {
+    if (!PyTuple_Check(o) || PyTuple_GET_SIZE(o) != 6) return false;
+    const at::Tensor *kc, *ks, *vc, *vs, *h;
+    if (!need(PyTuple_GET_ITEM(o, 0), at::kByte, 4, dev, &kc) || !need(PyTuple_GET_ITEM(o, 1), at::kFloat8_e4m3fn, 4, dev, &ks) ||
+        !need(PyTuple_GET_ITEM(o, 2), at::kByte, 4, dev, &vc) || !need(PyTuple_GET_ITEM(o, 3), at::kFloat8_e4m3fn, 4, dev, &vs) ||
+        kc->size(3) != 64 || vc->sizes() != kc->sizes())
+        return false;
+    for (const at::Tensor* s : {ks, vs})
+        if (s->size(0) != kc->size(0) || s->size(1) != kc->size(1) || s->size(2) != kc->size(2) || s->size(3) != 8) return false;
+    const float* head[2] = {nullptr, nullptr};
+    for (int i = 0; i < 2; ++i) {
+        PyObject* t = PyTuple_GET_ITEM(o, 4 + i);
+        if (t == Py_None) continue;
+        if (!need(t, at::kFloat, 1, dev, &h) || h->size(0) != kc->size(1)) return false;
+        head[i] = (const float*)h->data_ptr();
+    }
+    *p = cs_packed_pool{kc->data_ptr(), ks->data_ptr(), vc->data_ptr(), vs->data_ptr(), head[0], head[1]};
+    *codes = kc;
+    return true;
+}
+
+// page_table [B, ...] and ctx_lens [B]
+bool rows_of(PyObject* t, PyObject* l, int64_t B, c10::Device dev, const at::Tensor** table, const at::Tensor** lens) {
+    return need(t, at::kInt, 2, dev, table) && need(l, at::kInt, 1, dev, lens) && (*table)->size(0) == B && (*lens)->size(0) == B;
+}
+
+cs_attn_dims packed_dims(int64_t B, int64_t hq, const at::Tensor* codes, const at::Tensor* table, float scale) {
+    return cs_attn_dims{(int32_t)B, (int32_t)hq, (int32_t)codes->size(1), 128, (int32_t)codes->size(2),
+                        (int32_t)table->size(1), (int32_t)codes->size(0), scale};
+}
+
+// new_k, new_v, pool, page_table, ctx_lens, stream.  True when done.
+CALL(packed_kv_append, 6)
+    const at::Tensor *nk, *nv, *codes, *table, *lens;
+    cs_packed_pool pool;
+    c10::Device dev(c10::kCPU);
+    cs_stream_t s;
+    if (!first(a[0], at::kBFloat16, 4, &dev, &nk) || !need(a[1], at::kBFloat16, 4, dev, &nv) ||
+        !packed(a[2], dev, &pool, &codes) || !rows_of(a[3], a[4], nk->size(0), dev, &table, &lens) ||
+        !stream_of(a[5], dev, &s) || nk->sizes() != nv->sizes() || nk->size(2) != codes->size(1) || nk->size(3) != 128)
+        Py_RETURN_NONE;
+    const cs_attn_dims d = packed_dims(nk->size(0), codes->size(1), codes, table, 0.f);
+    const cs_status st = launch([&] {
+        return cs_packed_kv_append(&d, &pool, nk->data_ptr(), nv->data_ptr(), (const int32_t*)table->data_ptr(),
+                                   (const int32_t*)lens->data_ptr(), (int32_t)nk->size(1), s);
+    });
+    if (st != CS_OK) return status(st);
+    Py_RETURN_TRUE;
+CALL_END
+
+// pool, page_table, ctx_lens, n_rows, stream
+CALL(packed_kv_read, 5)
+    const at::Tensor *codes, *table, *lens;
+    cs_packed_pool pool;
+    c10::Device dev(c10::kCPU);
+    int32_t n;
+    cs_stream_t s;
+    if (!first(a[1], at::kInt, 2, &dev, &table) || !rows_of(a[1], a[2], table->size(0), dev, &table, &lens) ||
+        !packed(a[0], dev, &pool, &codes) || !small_int(a[3], &n) || n < 1 || !stream_of(a[4], dev, &s))
+        Py_RETURN_NONE;
+    const cs_attn_dims d = packed_dims(table->size(0), codes->size(1), codes, table, 0.f);
+    at::Tensor k, v;
+    const cs_status st = launch([&] {
+        const auto o = at::TensorOptions(at::kBFloat16).device(dev);
+        k = at::empty({table->size(0), n, codes->size(1), 128}, o);
+        v = at::empty({table->size(0), n, codes->size(1), 128}, o);
+        return cs_packed_kv_read(&d, &pool, (const int32_t*)table->data_ptr(), (const int32_t*)lens->data_ptr(), n,
+                                 k.data_ptr(), v.data_ptr(), s);
+    });
+    return st != CS_OK ? status(st) : pair(k, v);
+CALL_END
+
+// q, pool, page_table, ctx_lens, n_draft, out, workspace, sm_scale, stream
+CALL(packed_verify_attention, 9)
+    const at::Tensor *q, *codes, *table, *lens, *o;
+    cs_packed_pool pool;
+    c10::Device dev(c10::kCPU);
+    int32_t k;
+    float scale;
+    cs_stream_t s;
+    if (!first(a[0], at::kBFloat16, 4, &dev, &q) || !packed(a[1], dev, &pool, &codes) ||
+        !rows_of(a[2], a[3], q->size(0), dev, &table, &lens) || !small_int(a[4], &k) || q->size(1) != (int64_t)k + 1 ||
+        q->size(3) != 128 || !number(a[7], &scale) || !stream_of(a[8], dev, &s))
+        Py_RETURN_NONE;
+    if (a[5] != Py_None && (!need(a[5], at::kBFloat16, 4, dev, &o) || o->sizes() != q->sizes())) Py_RETURN_NONE;
+    const cs_attn_dims d = packed_dims(q->size(0), q->size(2), codes, table, scale);
+    Scratch ws;
+    const size_t bytes = a[6] == Py_None ? cs_packed_verify_attention_workspace_bytes(&d, k) : 0;
+    if (!workspace(a[6], kPackedAttn, dev, bytes, s, &ws)) Py_RETURN_NONE;
+    at::Tensor out;
+    const cs_status st = launch([&] {
+        out = a[5] == Py_None ? at::empty_like(*q) : *o;
+        return cs_packed_verify_attention(&d, q->data_ptr(), &pool, (const int32_t*)table->data_ptr(),
+                                          (const int32_t*)lens->data_ptr(), k, out.data_ptr(), ws.ptr, ws.bytes, s);
+    });
+    if (st != CS_OK) return status(st);
+    return a[5] == Py_None ? THPVariable_Wrap(out) : Py_NewRef(a[5]);
+CALL_END
+
+// page_table, ctx_lens (or none), ref_counts, page_size
+bool pages(PyObject* t, PyObject* l, PyObject* c, int32_t ps, c10::Device* dev, cs_page_dims* d, int32_t** table,
+           int32_t** lens, int32_t** refs) {
+    const at::Tensor *x, *y;
+    if (!first(t, at::kInt, 2, dev, &x) || !need(c, at::kInt, 1, *dev, &y)) return false;
+    *table = (int32_t*)x->data_ptr();
+    *refs = (int32_t*)y->data_ptr();
+    *d = cs_page_dims{(int32_t)x->size(0), (int32_t)x->size(1), ps, (int32_t)y->size(0)};
+    if (!l) return true;
+    if (!need(l, at::kInt, 1, *dev, &y) || y->size(0) != x->size(0)) return false;
+    *lens = (int32_t*)y->data_ptr();
+    return true;
+}
+
+// A list or tuple of tensors [P, ...], a page a row.
+bool page_pools(PyObject* o, int32_t P, c10::Device dev, cs_page_pool* pools, int32_t* n) {
+    if (!PyList_CheckExact(o) && !PyTuple_Check(o)) return false;
+    const Py_ssize_t count = PySequence_Fast_GET_SIZE(o);
+    if (count > CS_MAX_PAGE_POOLS || P <= 0) return false;
+    for (Py_ssize_t i = 0; i < count; ++i) {
+        PyObject* t = PySequence_Fast_GET_ITEM(o, i);
+        if (!THPVariable_CheckExact(t)) return false;
+        const at::Tensor& x = THPVariable_Unpack(t);
+        if (x.dim() < 2 || x.size(0) != P || !x.is_cuda() || x.device() != dev || !x.is_contiguous()) return false;
+        pools[i] = cs_page_pool{x.data_ptr(), (size_t)x.nbytes() / P};
+    }
+    *n = (int32_t)count;
+    return true;
+}
+
+// pools, page_table, ctx_lens, ref_counts, src, dst, page_size, room, workspace, stream
+CALL(kv_fork, 10)
+    const at::Tensor *src, *dst;
+    c10::Device dev(c10::kCPU);
+    cs_page_dims d;
+    cs_page_pool pools[CS_MAX_PAGE_POOLS];
+    int32_t n_pools, ps, room, *table, *lens, *refs;
+    cs_stream_t s;
+    if (!small_int(a[6], &ps) || !small_int(a[7], &room) || !pages(a[1], a[2], a[3], ps, &dev, &d, &table, &lens, &refs) ||
+        !page_pools(a[0], d.num_pages, dev, pools, &n_pools) || !need(a[4], at::kInt, 1, dev, &src) ||
+        !need(a[5], at::kInt, 1, dev, &dst) || src->size(0) != dst->size(0) || !stream_of(a[9], dev, &s))
+        Py_RETURN_NONE;
+    const int32_t n = (int32_t)src->size(0);
+    Scratch ws;
+    const size_t bytes = a[8] == Py_None ? cs_kv_fork_workspace_bytes(&d, n) : 0;
+    if (!workspace(a[8], kFork, dev, bytes, s, &ws)) Py_RETURN_NONE;
+    at::Tensor out;
+    const cs_status st = launch([&] {
+        make(&out, {n}, dev);
+        return cs_kv_fork(&d, pools, n_pools, table, lens, refs, (const int32_t*)src->data_ptr(),
+                          (const int32_t*)dst->data_ptr(), n, room, (int32_t*)out.data_ptr(), ws.ptr, ws.bytes, s);
+    });
+    return st != CS_OK ? status(st) : THPVariable_Wrap(out);
+CALL_END
+
+// page_table, ctx_lens, ref_counts, rows, keep_lens, page_size, stream.  True when done.
+CALL(kv_release, 7)
+    const at::Tensor *rows, *keep;
+    c10::Device dev(c10::kCPU);
+    cs_page_dims d;
+    int32_t ps, *table, *lens, *refs;
+    cs_stream_t s;
+    if (!small_int(a[5], &ps) || !pages(a[0], a[1], a[2], ps, &dev, &d, &table, &lens, &refs) ||
+        !need(a[3], at::kInt, 1, dev, &rows) || !need(a[4], at::kInt, 1, dev, &keep) || rows->size(0) != keep->size(0) ||
+        !stream_of(a[6], dev, &s))
+        Py_RETURN_NONE;
+    const cs_status st = launch([&] {
+        return cs_kv_release(&d, table, lens, refs, (const int32_t*)rows->data_ptr(), (const int32_t*)keep->data_ptr(),
+                             (int32_t)rows->size(0), s);
+    });
+    if (st != CS_OK) return status(st);
+    Py_RETURN_TRUE;
+CALL_END
+
+// pools, page_table, ref_counts, workspace, stream
+CALL(kv_compact, 5)
+    c10::Device dev(c10::kCPU);
+    cs_page_dims d;
+    cs_page_pool pools[CS_MAX_PAGE_POOLS];
+    int32_t n_pools, *table, *lens, *refs;
+    cs_stream_t s;
+    if (!pages(a[1], nullptr, a[2], 1, &dev, &d, &table, &lens, &refs) ||
+        !page_pools(a[0], d.num_pages, dev, pools, &n_pools) || !stream_of(a[4], dev, &s))
+        Py_RETURN_NONE;
+    Scratch ws;
+    const size_t bytes = a[3] == Py_None ? cs_kv_compact_workspace_bytes(&d) : 0;
+    if (!workspace(a[3], kCompact, dev, bytes, s, &ws)) Py_RETURN_NONE;
+    at::Tensor out;
+    const cs_status st = launch([&] {
+        make(&out, {1}, dev);
+        return cs_kv_compact(&d, pools, n_pools, table, refs, (int32_t*)out.data_ptr(), ws.ptr, ws.bytes, s);
+    });
+    return st != CS_OK ? status(st) : THPVariable_Wrap(out);
+CALL_END
+
+// logits (rows may lie apart), tokens, temperature, n_top, stream
+CALL(logprobs, 5)
+    if (!THPVariable_CheckExact(a[0])) Py_RETURN_NONE;
+    const at::Tensor& z = THPVariable_Unpack(a[0]);
+    const at::Tensor* tok;
+    const c10::Device dev = z.device();
+    float T;
+    int32_t n_top;
+    cs_stream_t s;
+    if ((z.scalar_type() != at::kFloat && z.scalar_type() != at::kBFloat16) || z.dim() != 2 || !z.is_cuda() ||
+        (z.size(1) > 1 && z.stride(1) != 1) || !need(a[1], at::kInt, 1, dev, &tok) || tok->size(0) != z.size(0) ||
+        !number(a[2], &T) || !small_int(a[3], &n_top) || n_top < 0 || n_top > CS_MAX_TOP || !stream_of(a[4], dev, &s))
+        Py_RETURN_NONE;
+    const int64_t N = z.size(0);
+    const cs_logprob_dims d{(int32_t)N, (int32_t)z.size(1), z.scalar_type() == at::kFloat ? CS_F32 : CS_BF16, n_top,
+                            N > 1 ? z.stride(0) : z.size(1)};
+    at::Tensor lp, entropy, top, top_lp;
+    const cs_status st = launch([&] {
+        const auto f = at::TensorOptions(at::kFloat).device(dev);
+        lp = at::empty({N}, f);
+        entropy = at::empty({N}, f);
+        make(&top, {N, n_top}, dev);
+        top_lp = at::empty({N, n_top}, f);
+        return cs_logprobs(&d, z.data_ptr(), (const int32_t*)tok->data_ptr(), T, (float*)lp.data_ptr(),
+                           (float*)entropy.data_ptr(), (int32_t*)top.data_ptr(), (float*)top_lp.data_ptr(), s);
+    });
+    if (st != CS_OK) return status(st);
+    return Py_BuildValue("(NNNN)", THPVariable_Wrap(lp), THPVariable_Wrap(entropy), THPVariable_Wrap(top),
+                         THPVariable_Wrap(top_lp));
+CALL_END
+
 PyObject* use_workspaces(PyObject*, PyObject* f) {
     Py_XSETREF(g_workspace_of, Py_NewRef(f));
     Py_RETURN_NONE;
@@ -390,6 +617,8 @@ PyObject* use_workspaces(PyObject*, PyObject* f) {
 #define FAST(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(name)), METH_FASTCALL, nullptr}
 PyMethodDef g_methods[] = {FAST(verify_attention), FAST(tree_verify_attention), FAST(spec_accept), FAST(tree_accept),
                            FAST(sample), FAST(route), FAST(kv_append), FAST(kv_commit), FAST(kv_commit_tree),
+                           FAST(packed_kv_append), FAST(packed_kv_read), FAST(packed_verify_attention), FAST(kv_fork),
+                           FAST(kv_release), FAST(kv_compact), FAST(logprobs),
                            {"use_workspaces", use_workspaces, METH_O, nullptr}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
 
