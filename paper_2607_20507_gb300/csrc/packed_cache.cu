@@ -11,91 +11,130 @@ namespace cs {
 namespace {
 
 constexpr int kThreads = 256;
+constexpr uint32_t kLarge = 0x5d80;     // bf16 bits of 2^60: groups from there on, and units up to
+constexpr float kSmall = 0x1p-60f;      // 2^-60, are divided (no remainder leaves fp32's range between)
 
+// Quotients by a divisor that the host knows, of numbers below 2^31: one high
+// product and a shift (Granlund and Montgomery, 1994).
+struct Divisor {
+    uint32_t d, mul;
+    int shift;
+    explicit Divisor(uint32_t d_ = 1) : d(d_), mul(0), shift(0) {
+        while ((1ull << shift) < d) ++shift;
+        if (shift > 0) mul = (uint32_t)(((1ull << (31 + shift)) + d - 1) / d);
+    }
+    __device__ __forceinline__ uint32_t operator()(uint32_t n) const {
+        return shift > 0 ? __umulhi(n, mul) >> (shift - 1) : n;
+    }
+};
+
+struct PackedSide {
+    uint4* rows;               // [B, n, Hkv, 128] bf16: read by the append, written by the read
+    uint8_t* codes;            // [P, Hkv, ps, 64]
+    uint8_t* scales;           // [P, Hkv, ps, 8]
+    const float* head;         // [Hkv] or NULL
+};
 struct PackedRowsParams {
-    const uint4* rows[2];      // append: [B, n, Hkv, 128] bf16 of K and V
-    uint4* out[2];             // read: the same
-    uint8_t* codes[2];         // [P, Hkv, ps, 64]
-    uint8_t* scales[2];        // [P, Hkv, ps, 8]
-    const float* head[2];      // [Hkv] or NULL
+    PackedSide k, v;
     const int32_t* page_table; // [B, max_pages]
     const int32_t* ctx_lens;   // [B]
-    long long groups;          // B * n * Hkv * 8
-    int n, Hkv, ps, max_pages, P;
+    uint32_t rows;             // B * n * Hkv
+    Divisor Hkv, n;
+    int ps_log2, max_pages, P;
 };
 
-// The row and group of this thread, and the pool row (page, head, slot) that
-// it lies in; -1 for a row before the first key or on a page outside the pool.
+// The row and group of a thread.
 struct Place {
+    uint32_t row;              // (b, i, h)
     int b, i, h, g;
-    long long row;             // (b, i, h)
 };
-__device__ __forceinline__ Place place_of(const PackedRowsParams& p, long long t) {
+__device__ __forceinline__ Place place_of(const PackedRowsParams& p) {
     Place a;
-    a.g = (int)(t & (kPackGroups - 1));
-    a.row = t / kPackGroups;
-    const long long bi = div_pos(a.row, p.Hkv);
-    a.h = (int)(a.row - bi * p.Hkv);
-    a.b = (int)div_pos(bi, p.n);
-    a.i = (int)(bi - (long long)a.b * p.n);
+    a.g = threadIdx.x & (kPackGroups - 1);
+    a.row = blockIdx.x * (kThreads / kPackGroups) + threadIdx.x / kPackGroups;
+    const uint32_t bi = p.Hkv(a.row);
+    a.h = (int)(a.row - bi * p.Hkv.d);
+    a.b = (int)p.n(bi);
+    a.i = (int)(bi - (uint32_t)a.b * p.n.d);
     return a;
 }
+// The pool row (page, head, slot) that it lies in; -1 for a row before the first
+// key or on a page outside the pool.
 __device__ __forceinline__ long long slot_of(const PackedRowsParams& p, const Place& a, int L) {
-    const int pos = max(0, min(L, p.max_pages * p.ps)) - p.n + a.i;
+    const int pos = max(0, min(L, p.max_pages << p.ps_log2)) - (int)p.n.d + a.i;
     if (pos < 0) return -1;
-    const int page = __ldcg(p.page_table + (size_t)a.b * p.max_pages + pos / p.ps);
+    const int page = __ldcg(p.page_table + (size_t)a.b * p.max_pages + (pos >> p.ps_log2));
     if (page < 0 || page >= p.P) return -1;
-    return ((long long)page * p.Hkv + a.h) * p.ps + pos % p.ps;
+    return (((long long)page * p.Hkv.d + a.h) << p.ps_log2) + (pos & ((1 << p.ps_log2) - 1));
 }
 
 __global__ void __launch_bounds__(kThreads) packed_append_kernel(const PackedRowsParams p) {
-    const long long t = (long long)blockIdx.x * kThreads + threadIdx.x;
-    const int kv = blockIdx.y;
-    const Place a = place_of(p, t);
+    const PackedSide& side = blockIdx.y ? p.v : p.k;
+    const Place a = place_of(p);
     wait_prior_grid();
     allow_dependent_launch();
-    if (t >= p.groups) return;
-    const uint4* src = p.rows[kv] + 2 * t;
+    if (a.row >= p.rows) return;
+    const uint4* src = side.rows + 2 * ((size_t)a.row * kPackGroups + a.g);
     const int L = __ldcg(p.ctx_lens + a.b);
     const uint4 x0 = __ldcg(src), x1 = __ldcg(src + 1);
-    const float head = p.head[kv] ? __ldcg(p.head[kv] + a.h) : 1.f;
+    const float head = side.head ? __ldcg(side.head + a.h) : 1.f;
     const long long slot = slot_of(p, a, L);
     if (slot < 0) return;
     const uint32_t w[8] = {x0.x, x0.y, x0.z, x0.w, x1.x, x1.y, x1.z, x1.w};
-    float x[16], top = 0.f;
+    uint32_t top2 = 0;   // the larger magnitudes of the even and odd dims, NaN where one is
 #pragma unroll
-    for (int j = 0; j < 16; ++j) {
-        x[j] = __uint_as_float(j & 1 ? w[j / 2] & 0xffff0000u : w[j / 2] << 16);
-        top = fmaxf(top, fabsf(x[j]));   // (passes over a NaN)
-        if (x[j] != x[j]) x[j] = 0.f;
+    for (int j = 0; j < 8; ++j) asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(top2) : "r"(top2), "r"(w[j] & 0x7fff7fffu));
+    float top = fmaxf(__uint_as_float(top2 << 16), __uint_as_float(top2 & 0xffff0000u));
+    const bool plain = top2 << 16 < kLarge << 16 && top2 < kLarge << 16;   // (bits of magnitudes are in their order)
+    float x[16];
+#pragma unroll
+    for (int j = 0; j < 16; ++j) x[j] = __uint_as_float(j & 1 ? w[j / 2] & 0xffff0000u : w[j / 2] << 16);
+    if (!plain) {   // (a NaN is stored as 0)
+        top = 0.f;
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+            if (x[j] != x[j]) x[j] = 0.f;
+            top = fmaxf(top, fabsf(x[j]));
+        }
     }
     const uint32_t scale = to_e4m3(fminf(__fdiv_rn(top, __fmul_rn(6.f, head)), 448.f));
     const float unit = __fmul_rn(f16_lo(scales_f16x2(scale)), head);
-    uint2 c = make_uint2(0, 0);
-    if (unit > 0.f) {
+    if (plain && unit > kSmall) {
+        // x / unit correctly rounded from the correctly rounded reciprocal: one
+        // step from x * (1 / unit) with the remainder (Markstein, 1990), three
+        // operations in place of a division
+        const float inv = __frcp_rn(unit);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            c.x |= to_e2m1x2(__fdiv_rn(x[2 * j], unit), __fdiv_rn(x[2 * j + 1], unit)) << (8 * j);
-            c.y |= to_e2m1x2(__fdiv_rn(x[8 + 2 * j], unit), __fdiv_rn(x[8 + 2 * j + 1], unit)) << (8 * j);
+        for (int j = 0; j < 16; ++j) {
+            const float q = __fmul_rn(x[j], inv);
+            x[j] = __fmaf_rn(__fmaf_rn(-q, unit, x[j]), inv, q);
         }
+    } else {
+#pragma unroll
+        for (int j = 0; j < 16; ++j) x[j] = unit > 0.f ? __fdiv_rn(x[j], unit) : 0.f;
     }
-    *reinterpret_cast<uint2*>(p.codes[kv] + (size_t)slot * kPackCodeBytes + a.g * 8) = c;
-    p.scales[kv][(size_t)slot * kPackGroups + a.g] = (uint8_t)scale;
+    uint2 c = make_uint2(0, 0);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        c.x |= to_e2m1x2(x[2 * j], x[2 * j + 1]) << (8 * j);
+        c.y |= to_e2m1x2(x[8 + 2 * j], x[8 + 2 * j + 1]) << (8 * j);
+    }
+    *reinterpret_cast<uint2*>(side.codes + (size_t)slot * kPackCodeBytes + a.g * 8) = c;
+    side.scales[(size_t)slot * kPackGroups + a.g] = (uint8_t)scale;
 }
 
 __global__ void __launch_bounds__(kThreads) packed_read_kernel(const PackedRowsParams p) {
-    const long long t = (long long)blockIdx.x * kThreads + threadIdx.x;
-    const int kv = blockIdx.y;
-    const Place a = place_of(p, t);
+    const PackedSide& side = blockIdx.y ? p.v : p.k;
+    const Place a = place_of(p);
     wait_prior_grid();
     allow_dependent_launch();
-    if (t >= p.groups) return;
+    if (a.row >= p.rows) return;
     const long long slot = slot_of(p, a, __ldcg(p.ctx_lens + a.b));
     uint4 o[2] = {make_uint4(0, 0, 0, 0), make_uint4(0, 0, 0, 0)};
     if (slot >= 0) {
-        const uint2 c = __ldcg(reinterpret_cast<const uint2*>(p.codes[kv] + (size_t)slot * kPackCodeBytes + a.g * 8));
-        const uint32_t s = __ldcg(p.scales[kv] + (size_t)slot * kPackGroups + a.g);
-        const float head = p.head[kv] ? __ldcg(p.head[kv] + a.h) : 1.f;
+        const uint2 c = __ldcg(reinterpret_cast<const uint2*>(side.codes + (size_t)slot * kPackCodeBytes + a.g * 8));
+        const uint32_t s = __ldcg(side.scales + (size_t)slot * kPackGroups + a.g);
+        const float head = side.head ? __ldcg(side.head + a.h) : 1.f;
         const uint32_t sc = scales_f16x2(s | s << 8);
         const uint32_t v[8] = {codes_f16x2<0>(c.x), codes_f16x2<1>(c.x), codes_f16x2<2>(c.x), codes_f16x2<3>(c.x),
                                codes_f16x2<0>(c.y), codes_f16x2<1>(c.y), codes_f16x2<2>(c.y), codes_f16x2<3>(c.y)};
@@ -108,35 +147,32 @@ __global__ void __launch_bounds__(kThreads) packed_read_kernel(const PackedRowsP
         o[0] = make_uint4(r[0], r[1], r[2], r[3]);
         o[1] = make_uint4(r[4], r[5], r[6], r[7]);
     }
-    p.out[kv][2 * t] = o[0];
-    p.out[kv][2 * t + 1] = o[1];
+    uint4* dst = side.rows + 2 * ((size_t)a.row * kPackGroups + a.g);
+    dst[0] = o[0];
+    dst[1] = o[1];
 }
 
-PackedRowsParams rows_params(const cs_attn_dims& d, const cs_packed_pool& pool, const int32_t* page_table,
-                             const int32_t* ctx_lens, int n) {
+cs_status launch_rows(void (*kern)(const PackedRowsParams), const cs_attn_dims& d, const cs_packed_pool& pool,
+                      void* k_rows, void* v_rows, const int32_t* page_table, const int32_t* ctx_lens, int n,
+                      const char* what, cudaStream_t stream) {
+    const long long rows = (long long)d.batch * n * d.n_kv_heads;
+    if ((long long)d.batch * n > 0x7fffffffLL || rows > 0x7fffffffLL)
+        return fail(CS_ERR_UNSUPPORTED, "more than 2^31 rows in one call");
     PackedRowsParams p{};
-    p.codes[0] = static_cast<uint8_t*>(pool.k_codes);
-    p.codes[1] = static_cast<uint8_t*>(pool.v_codes);
-    p.scales[0] = static_cast<uint8_t*>(pool.k_scales);
-    p.scales[1] = static_cast<uint8_t*>(pool.v_scales);
-    p.head[0] = pool.k_head_scale;
-    p.head[1] = pool.v_head_scale;
+    p.k = PackedSide{static_cast<uint4*>(k_rows), static_cast<uint8_t*>(pool.k_codes), static_cast<uint8_t*>(pool.k_scales),
+                     pool.k_head_scale};
+    p.v = PackedSide{static_cast<uint4*>(v_rows), static_cast<uint8_t*>(pool.v_codes), static_cast<uint8_t*>(pool.v_scales),
+                     pool.v_head_scale};
     p.page_table = page_table;
     p.ctx_lens = ctx_lens;
-    p.groups = (long long)d.batch * n * d.n_kv_heads * kPackGroups;
-    p.n = n;
-    p.Hkv = d.n_kv_heads;
-    p.ps = d.page_size;
+    p.rows = (uint32_t)rows;
+    p.Hkv = Divisor((uint32_t)d.n_kv_heads);
+    p.n = Divisor((uint32_t)n);
+    while ((1 << p.ps_log2) < d.page_size) ++p.ps_log2;
     p.max_pages = d.max_pages_per_seq;
     p.P = d.num_pages;
-    return p;
-}
-
-cs_status launch_rows(void (*kern)(const PackedRowsParams), const PackedRowsParams& p, const char* what,
-                      cudaStream_t stream) {
-    const long long blocks = (p.groups + kThreads - 1) / kThreads;
-    if (blocks > 0x7fffffffLL) return fail(CS_ERR_UNSUPPORTED, "too many rows in one call");
-    const cudaError_t e = launch_dependent(kern, dim3((unsigned)blocks, 2), dim3(kThreads), 0, stream, p);
+    const unsigned blocks = (unsigned)((rows + kThreads / kPackGroups - 1) / (kThreads / kPackGroups));
+    const cudaError_t e = launch_dependent(kern, dim3(blocks, 2), dim3(kThreads), 0, stream, p);
     return e == cudaSuccess ? CS_OK : cuda_fail(e, what);
 }
 
@@ -144,18 +180,14 @@ cs_status launch_rows(void (*kern)(const PackedRowsParams), const PackedRowsPara
 
 cs_status launch_packed_append(const cs_attn_dims& d, const cs_packed_pool& pool, const void* new_k, const void* new_v,
                                const int32_t* page_table, const int32_t* ctx_lens, int n_new, cudaStream_t stream) {
-    PackedRowsParams p = rows_params(d, pool, page_table, ctx_lens, n_new);
-    p.rows[0] = static_cast<const uint4*>(new_k);
-    p.rows[1] = static_cast<const uint4*>(new_v);
-    return launch_rows(packed_append_kernel, p, "packed_append_kernel launch", stream);
+    return launch_rows(packed_append_kernel, d, pool, const_cast<void*>(new_k), const_cast<void*>(new_v), page_table,
+                       ctx_lens, n_new, "packed_append_kernel launch", stream);
 }
 
 cs_status launch_packed_read(const cs_attn_dims& d, const cs_packed_pool& pool, const int32_t* page_table,
                              const int32_t* ctx_lens, int n_rows, void* out_k, void* out_v, cudaStream_t stream) {
-    PackedRowsParams p = rows_params(d, pool, page_table, ctx_lens, n_rows);
-    p.out[0] = static_cast<uint4*>(out_k);
-    p.out[1] = static_cast<uint4*>(out_v);
-    return launch_rows(packed_read_kernel, p, "packed_read_kernel launch", stream);
+    return launch_rows(packed_read_kernel, d, pool, out_k, out_v, page_table, ctx_lens, n_rows,
+                       "packed_read_kernel launch", stream);
 }
 
 }  // namespace cs
