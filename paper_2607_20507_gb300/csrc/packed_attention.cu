@@ -74,6 +74,7 @@ struct PackedAttnParams {
     float* part_o;               // [2 grid, n_rows, D] a CTA's first and last piece
     float2* part_ml;             // [2 grid, n_rows] (maximum in log2 units, sum)
     Job* jobs;                   // [grid]
+    int* status;                 // device status word
     int Hq, Hkv, G, R, n_rows, ps, ps_log2, max_pages, P;
     int b_base, n_batch, span_x;
     float scale_log2;            // sm_scale * log2(e)
@@ -189,6 +190,57 @@ __device__ __forceinline__ void advance(Cursor& c, const int* lens, int nb, int 
     if (++c.b < nb) c.T = tiles_of(lens[c.b], tile);
 }
 
+// The requests' clamped lengths and their spans' tiles before each, into shared
+// memory (ends with a block barrier); all tiles.
+template <int kThreads>
+__device__ __forceinline__ long long build_prefix(const PackedAttnParams& p, int tile, int* lens, long long* prefix,
+                                                  long long* wsum) {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    long long carry = 0;
+    for (int base = 0; base < p.n_batch; base += kThreads) {
+        const int b = base + threadIdx.x;
+        long long v = 0;
+        if (b < p.n_batch) {
+            const int L = max(0, min(__ldcg(p.ctx_lens + p.b_base + b), p.max_pages * p.ps));
+            lens[b] = L;
+            v = (long long)tiles_of(L, tile) * p.Hkv;
+        }
+        long long inc = v;
+#pragma unroll
+        for (int off = 1; off < 32; off <<= 1) {
+            const long long y = __shfl_up_sync(0xffffffffu, inc, off);
+            if (lane >= off) inc += y;
+        }
+        if (lane == 31) wsum[warp] = inc;
+        __syncthreads();
+        long long before = carry, all = 0;
+        for (int w = 0; w < kThreads / 32; ++w) {
+            if (w < warp) before += wsum[w];
+            all += wsum[w];
+        }
+        if (b < p.n_batch) prefix[b] = before + inc - v;
+        carry += all;
+        __syncthreads();
+    }
+    return carry;
+}
+
+// Four of a query row's dims (a lane's, of the warp that has the row) as fp16,
+// brought below 2^15 by a power of two that the whole row shares; back: its inverse.
+__device__ __forceinline__ uint2 query_f16(uint2 x, float& back) {
+    const float f[4] = {__uint_as_float(x.x << 16), __uint_as_float(x.x & 0xffff0000u), __uint_as_float(x.y << 16),
+                        __uint_as_float(x.y & 0xffff0000u)};
+    float top = fmaxf(fmaxf(fabsf(f[0]), fabsf(f[1])), fmaxf(fabsf(f[2]), fabsf(f[3])));
+#pragma unroll
+    for (int off = 16; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
+    // top = 1.m x 2^e -> 1.m x 2^14; 2^(14 - e) in two halves, neither of which leaves fp32
+    const int e = (int)(__float_as_uint(top) >> 23) - 127;
+    const int up = top > 0.f ? 14 - e : 0, u0 = up / 2, u1 = up - u0;
+    const float s0 = __uint_as_float((uint32_t)(127 + u0) << 23), s1 = __uint_as_float((uint32_t)(127 + u1) << 23);
+    back = __uint_as_float((uint32_t)(127 - u0) << 23) * __uint_as_float((uint32_t)(127 - u1) << 23);
+    return make_uint2(pack_f16x2(f[0] * s0 * s1, f[1] * s0 * s1), pack_f16x2(f[2] * s0 * s1, f[3] * s0 * s1));
+}
+
 template <int kNT, int kRG>
 __global__ void __launch_bounds__(Form<kNT, kRG>::kThreads, Form<kNT, kRG>::kMinBlocks)
 packed_attention_kernel(const PackedAttnParams p) {
@@ -210,39 +262,15 @@ packed_attention_kernel(const PackedAttnParams p) {
     wait_prior_grid();
     allow_dependent_launch();
 
-    // ---- the requests' tiles: lengths, and where each request's units start
-    long long carry = 0, W = 0;
-    for (int base = 0; base < nb; base += F::kThreads) {
-        const int b = base + threadIdx.x;
-        long long v = 0;
-        if (b < nb) {
-            const int L = max(0, min(__ldcg(p.ctx_lens + p.b_base + b), p.max_pages * p.ps));
-            s_len[b] = L;
-            v = (long long)tiles_of(L, F::kTile) * p.Hkv;
-        }
-        long long inc = v;
-#pragma unroll
-        for (int off = 1; off < 32; off <<= 1) {
-            const long long y = __shfl_up_sync(0xffffffffu, inc, off);
-            if (lane >= off) inc += y;
-        }
-        if (lane == 31) s_wsum[warp] = inc;
-        __syncthreads();
-        long long before = carry, all = 0;
-        for (int w = 0; w < F::kThreads / 32; ++w) {
-            if (w < warp) before += s_wsum[w];
-            all += s_wsum[w];
-        }
-        if (b < nb) s_prefix[b] = before + inc - v;
-        carry += all;
-        __syncthreads();
-    }
-    W = carry;
+    const long long W = build_prefix<F::kThreads>(p, F::kTile, s_len, s_prefix, s_wsum);
     // few tiles: one a CTA; else a span's start counts as X tiles
     const int grid = gridDim.x, cta = blockIdx.x;
     const bool few = W <= grid;
     const int X = few ? 0 : X0, Gc = few ? (int)W : grid;
-    if (threadIdx.x == 0) p.jobs[cta].n = 0;
+    if (threadIdx.x == 0) {
+        p.jobs[cta].n = 0;
+        if (cta == 0 && p.b_base == 0) *p.status = 0;
+    }
     if (cta >= Gc) return;
     if (X > 0) {
         for (int b = threadIdx.x; b < nb; b += F::kThreads) s_prefix[b] += (long long)X * p.Hkv * b;
@@ -251,7 +279,6 @@ packed_attention_kernel(const PackedAttnParams p) {
     const long long U = W + (long long)X * p.Hkv * nb;
     const Share share = share_of(cta, U, Gc, s_prefix, s_len, nb, p.Hkv, X, F::kTile);
     const int n_tiles = share.n_tiles;
-    // where the span that ends this share starts, in units (for its pieces below)
     __syncthreads();   // the prefix gives way to the ring
     if (n_tiles <= 0) return;
     for (int row = threadIdx.x; row < F::kRows; row += F::kThreads) s_draft[row] = row / p.G;
@@ -327,23 +354,11 @@ packed_attention_kernel(const PackedAttnParams p) {
                 x.x = __ldcg(src);
                 x.y = __ldcg(src + 1);
             }
-            float f[4] = {__uint_as_float(x.x << 16), __uint_as_float(x.x & 0xffff0000u), __uint_as_float(x.y << 16),
-                          __uint_as_float(x.y & 0xffff0000u)};
-            float top = fmaxf(fmaxf(fabsf(f[0]), fabsf(f[1])), fmaxf(fabsf(f[2]), fabsf(f[3])));
-#pragma unroll
-            for (int off = 16; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
-            // top = 1.m x 2^e -> 1.m x 2^14; the factors 2^(14 - e) in two halves,
-            // neither of which leaves fp32 for any e
-            const int e = (int)(__float_as_uint(top) >> 23) - 127;
-            const int up = top > 0.f ? 14 - e : 0, u0 = up / 2, u1 = up - u0;
-            const float s0 = __uint_as_float((uint32_t)(127 + u0) << 23), s1 = __uint_as_float((uint32_t)(127 + u1) << 23);
-            const uint2 y = make_uint2(pack_f16x2(f[0] * s0 * s1, f[1] * s0 * s1), pack_f16x2(f[2] * s0 * s1, f[3] * s0 * s1));
+            float back;
+            const uint2 y = query_f16(x, back);
             uint4* at = s_q + ((row >> 3) * 4 + ((lane & 7) >> 1)) * 32 + (row & 7) * 4 + (lane >> 3);
             reinterpret_cast<uint2*>(at)[lane & 1] = y;
-            if (lane == 0) {
-                const float d0 = __uint_as_float((uint32_t)(127 - u0) << 23), d1 = __uint_as_float((uint32_t)(127 - u1) << 23);
-                s_scale[row] = p.scale_log2 * d0 * (p.k_head ? __ldcg(p.k_head + cur.h) : 1.f) * d1;
-            }
+            if (lane == 0) s_scale[row] = p.scale_log2 * back * (p.k_head ? __ldcg(p.k_head + cur.h) : 1.f);
         }
         __syncthreads();
 
@@ -659,6 +674,8 @@ packed_attention_kernel(const PackedAttnParams p) {
     cp_async_wait<0>();
 }
 
+#include "packed_attention_tc.cuh"
+
 // ---------------------------------------------------------------------------
 // Joins the pieces of the span that starts in CTA c of the main kernel (if one
 // does): o = sum_j w_j o_j with w_j = l_j 2^(m_j - M) / sum, a warp for a row.
@@ -730,17 +747,23 @@ template <int kNT, int kRG>
 Choice choice() {
     return {packed_attention_kernel<kNT, kRG>, Form<kNT, kRG>::kThreads, Form<kNT, kRG>::kSmem};
 }
-constexpr int kForms = 9;
+template <int kN>
+Choice choice_tc() {
+    return {packed_attention_tc_kernel<kN>, kTcThreads, TcForm<kN>::kSmem};
+}
+constexpr int kSyncForms = 9, kForms = kSyncForms + 7;
 
-// The form for a number of query rows: one warp holds up to four tiles of 8
-// rows; more rows are spread over as few warps of three tiles as hold them.
-int form_of(int rows) {
+// The form for a number of query rows; tc: whether the tcgen05 form may be chosen.
+int form_of(int rows, bool tc) {
+    if (tc && rows >= kTcMinRows && rows <= kTcMaxRows) return kSyncForms + (rows + 15) / 16 - 2;
     const int nt = (rows + 7) / 8;
     return nt <= 4 ? nt - 1 : 2 + (nt + 2) / 3;   // 4: two warps of three tiles, ... 8: six
 }
 Choice choice_of(int form) {
     static const Choice all[kForms] = {choice<1, 1>(), choice<2, 1>(), choice<3, 1>(), choice<4, 1>(), choice<3, 2>(),
-                                       choice<3, 3>(), choice<3, 4>(), choice<3, 5>(), choice<3, 6>()};
+                                       choice<3, 3>(), choice<3, 4>(), choice<3, 5>(), choice<3, 6>(),
+                                       choice_tc<32>(), choice_tc<48>(), choice_tc<64>(), choice_tc<80>(),
+                                       choice_tc<96>(), choice_tc<112>(), choice_tc<128>()};
     return all[form];
 }
 
@@ -756,6 +779,14 @@ int resident_of(int form) {
     if (!kept[dev][form]) {
         const Choice c = choice_of(form);
         int n = 0;
+        if (form >= kSyncForms) {
+            // the warp groups' shares of registers have to be what the block was launched with
+            cudaFuncAttributes a;
+            if (cudaFuncGetAttributes(&a, c.kern) != cudaSuccess || a.numRegs != kTcRegisters) {
+                cudaGetLastError();
+                return 0;
+            }
+        }
         if (cudaFuncSetAttribute(c.kern, cudaFuncAttributeMaxDynamicSharedMemorySize, c.smem) != cudaSuccess ||
             cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, c.kern, c.threads, c.smem) != cudaSuccess || n <= 0) {
             cudaGetLastError();
@@ -766,18 +797,19 @@ int resident_of(int form) {
     return kept[dev][form];
 }
 
+// Workspace: the status word (256 B), the jobs, then the pieces' (maximum, sum) and outputs.
 struct PackedPlan {
     int form, rows, grid;
     size_t off_ml, off_o, bytes;
 };
-PackedPlan plan_packed(const cs_attn_dims& d, int rows, int sm_count) {
+PackedPlan plan_packed(const cs_attn_dims& d, int rows, int sm_count, bool tc) {
     PackedPlan pl{};
     pl.rows = rows * (d.n_q_heads / d.n_kv_heads);
-    pl.form = form_of(pl.rows);
+    pl.form = form_of(pl.rows, tc);
     const int res = resident_of(pl.form);
     pl.grid = sm_count * (res > 0 ? res : 1);
     if (pl.grid > kMaxGrid) pl.grid = kMaxGrid;
-    pl.off_ml = align256(sizeof(Job) * (size_t)pl.grid);
+    pl.off_ml = 256 + align256(sizeof(Job) * (size_t)pl.grid);
     pl.off_o = pl.off_ml + align256(sizeof(float2) * 2 * (size_t)pl.grid * pl.rows);
     pl.bytes = pl.off_o + align256(sizeof(float) * kPackDim * 2 * (size_t)pl.grid * pl.rows);
     return pl;
@@ -786,13 +818,16 @@ PackedPlan plan_packed(const cs_attn_dims& d, int rows, int sm_count) {
 }  // namespace
 
 size_t packed_attention_workspace_bytes(const cs_attn_dims& d, int rows, int sm_count) {
-    return plan_packed(d, rows, sm_count).bytes;
+    const size_t a = plan_packed(d, rows, sm_count, true).bytes, b = plan_packed(d, rows, sm_count, false).bytes;
+    return a > b ? a : b;
 }
 
 cs_status launch_packed_attention(const cs_attn_dims& d, const void* q, const cs_packed_pool& pool,
                                   const int32_t* page_table, const int32_t* ctx_lens, int rows, void* out,
                                   void* workspace, cudaStream_t stream) {
-    const PackedPlan pl = plan_packed(d, rows, current_sm_count());
+    // the tcgen05 form loads 32 bytes of codes at a time
+    const bool tc = ((reinterpret_cast<uintptr_t>(pool.k_codes) | reinterpret_cast<uintptr_t>(pool.v_codes)) & 31) == 0;
+    const PackedPlan pl = plan_packed(d, rows, current_sm_count(), tc);
     uint8_t* ws = static_cast<uint8_t*>(workspace);
     PackedAttnParams p{};
     p.q = static_cast<const __nv_bfloat16*>(q);
@@ -805,7 +840,8 @@ cs_status launch_packed_attention(const cs_attn_dims& d, const void* q, const cs
     p.v_head = pool.v_head_scale;
     p.page_table = page_table;
     p.ctx_lens = ctx_lens;
-    p.jobs = reinterpret_cast<Job*>(ws);
+    p.status = reinterpret_cast<int*>(ws);
+    p.jobs = reinterpret_cast<Job*>(ws + 256);
     p.part_ml = reinterpret_cast<float2*>(ws + pl.off_ml);
     p.part_o = reinterpret_cast<float*>(ws + pl.off_o);
     p.Hq = d.n_q_heads;
