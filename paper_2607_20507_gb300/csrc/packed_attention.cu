@@ -779,14 +779,6 @@ int resident_of(int form) {
     if (!kept[dev][form]) {
         const Choice c = choice_of(form);
         int n = 0;
-        if (form >= kSyncForms) {
-            // the warp groups' shares of registers have to be what the block was launched with
-            cudaFuncAttributes a;
-            if (cudaFuncGetAttributes(&a, c.kern) != cudaSuccess || a.numRegs != kTcRegisters) {
-                cudaGetLastError();
-                return 0;
-            }
-        }
         if (cudaFuncSetAttribute(c.kern, cudaFuncAttributeMaxDynamicSharedMemorySize, c.smem) != cudaSuccess ||
             cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, c.kern, c.threads, c.smem) != cudaSuccess || n <= 0) {
             cudaGetLastError();

@@ -13,17 +13,19 @@
 // bytes, where 18 KB of codes take 800 at the memory's rate, the MMAs 640, the
 // exponentials 640.  K goes by tensor memory, which takes it off that path.
 //
-// One CTA an SM of twelve warps.  Warps 0-3 (side 0) decode the K rows of a tile,
-// warps 4-7 (side 1) its V rows, one tile ahead of the softmax, with the codes
-// of the tile after that already requested into registers (two 32-byte loads a
-// row).  Then all eight do the softmax of the tile, each side a share of its
-// columns (query rows), a thread one key.  Warp 8 issues the MMAs: S of the next
-// tile beside the softmax of this one, O of the last.  Warps 9-11 are there for
-// their registers, which the workers take over.
+// One CTA an SM of 17 warps.  Sixteen workers are four groups of four warps, a
+// thread of a group one key of the tile: groups 0 and 2 decode the halves of
+// its K row, groups 1 and 3 those of its V row, one tile ahead of the softmax,
+// with the codes of the tile after that already requested into registers.  Then
+// all do the softmax of the tile, each group a quarter of the columns (query
+// rows).  (With eight warps, whole rows and half the columns each, a tile of 72
+// rows took 3600 cycles, most of them waits on the warps' own results.)  Warp 16
+// issues the MMAs: S of the next tile beside the softmax of this one, O of the
+// last.
 //
 // As in the other form P = 2^(s - m + 12), and the tile is taken the short way
 // unless some weight leaves [2^-14, 2^15] or some key is hidden from some row
-// (a vote of the eight warps).  Then the columns' maxima are found, and O is
+// (a vote of the workers).  Then the columns' maxima are found, and O is
 // rescaled where one grows by more than 2^3; weights below 2^-14 (faint) are
 // taken 28 powers of two at a time by products of their own into the place of
 // the tile's S, which the workers add to O.
@@ -32,11 +34,8 @@
 // issued any more, every warp still meets every block barrier, and the status
 // word says so.
 
-constexpr int kTcThreads = 384;                    // two groups of workers, and one whose first warp issues the MMAs
-constexpr int kTcWorkers = 256;
-constexpr int kTcRegisters = 168;                  // of a thread at launch; the groups then share them
-constexpr int kTcWorkerRegs = 232, kTcOtherRegs = 40;
-static_assert(256 * kTcWorkerRegs + 128 * kTcOtherRegs <= kTcThreads * kTcRegisters, "more registers than the block has");
+constexpr int kTcThreads = 544;
+constexpr int kTcWorkers = 512;
 constexpr int kTcTile = 128;                       // keys of a tile: the MMAs' M (S) and K (O)
 constexpr int kTcVBytes = kTcTile * 256;           // V of a tile in fp16
 constexpr int kTcVBufs = 3;
@@ -44,7 +43,8 @@ constexpr int kTcMinRows = 17, kTcMaxRows = 128;   // query rows that it takes
 
 template <int kN>
 struct TcForm {
-    static constexpr int kH0 = (kN / 16 + 1) / 2 * 16, kH1 = kN - kH0;   // columns of side 0 and 1
+    // columns of groups 0 and 1, and of groups 2 and 3: multiples of 8
+    static constexpr int kH0 = (kN + 31) / 32 * 8, kH1 = kN / 2 - kH0;
     static constexpr int kNHalves = kN > 64 ? 2 : 1;                     // 64-column atoms of P
     static constexpr int kPGroup = kNHalves * 1024;                      // bytes of P for 8 keys
     static constexpr int kPBytes = kTcTile / 8 * kPGroup;
@@ -64,13 +64,16 @@ __device__ __forceinline__ void tc_wait_st() { asm volatile("tcgen05.wait::st.sy
 __device__ __forceinline__ void tc_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void fence_async_smem() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
-// 16 columns of the warp's 32 lanes (complete after tc_wait_ld)
-__device__ __forceinline__ void tc_ld16(uint32_t addr, float* v) {
-    asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
-        : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]), "=f"(v[8]),
-          "=f"(v[9]), "=f"(v[10]), "=f"(v[11]), "=f"(v[12]), "=f"(v[13]), "=f"(v[14]), "=f"(v[15])
-        : "r"(addr));
+// 8 columns of the warp's 32 lanes (complete after tc_wait_ld)
+__device__ __forceinline__ void tc_ld8(uint32_t addr, float* v) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+                 : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7])
+                 : "r"(addr));
+}
+__device__ __forceinline__ void tc_st8(uint32_t addr, const uint32_t* r) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"r"(addr), "r"(r[0]), "r"(r[1]),
+                 "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
+                 : "memory");
 }
 __device__ __forceinline__ void tc_st16(uint32_t addr, const uint32_t* r) {
     asm volatile(
@@ -116,18 +119,18 @@ __device__ __forceinline__ uint32_t min_f16x2(uint32_t a, uint32_t b) {
     asm("min.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
     return r;
 }
-// Whether any of the eight worker warps' threads says so; a barrier of theirs.
+// Whether any of the workers' threads says so; a barrier of theirs.
 __device__ __forceinline__ bool workers_any(bool x) {
     uint32_t r;
     asm volatile(
-        "{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbarrier.cta.red.or.pred q, 1, 256, p;\n\t"
+        "{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbarrier.cta.red.or.pred q, 1, 512, p;\n\t"
         "selp.u32 %0, 1, 0, q;\n\t}\n"
         : "=r"(r)
         : "r"((uint32_t)x)
         : "memory");
     return r != 0;
 }
-__device__ __forceinline__ void workers_sync() { asm volatile("barrier.cta.sync 1, 256;" ::: "memory"); }
+__device__ __forceinline__ void workers_sync() { asm volatile("barrier.cta.sync 1, 512;" ::: "memory"); }
 
 // A float's bits as an integer of the same order, and back.
 __device__ __forceinline__ int ordered(float x) {
@@ -148,9 +151,9 @@ __device__ __forceinline__ void tc_wait(uint64_t* bar, uint32_t parity, volatile
 __device__ __forceinline__ bool alive(volatile int* dead) { return !__any_sync(0xffffffffu, *dead); }
 
 struct TcBars {
-    uint64_t k_full[2];    // K of a tile decoded (4 warps)
+    uint64_t k_full[2];    // K of a tile decoded (8 warps)
     uint64_t s_full[2];    // S of a tile done; its K is read
-    uint64_t p_full[2];    // P and V of a tile written, its S read (8 warps)
+    uint64_t p_full[2];    // P and V of a tile written, its S read (16 warps)
     uint64_t o_done[2];    // O of a tile done; its P and V are read
     uint64_t f_done;       // a product of faint weights done
 };
@@ -167,13 +170,15 @@ __device__ __forceinline__ void tc_mma_values(uint32_t d, uint8_t* smem, int j, 
         tc_mma_ss(d, v + (uint64_t)(kk * (4096 >> 4)), x + (uint64_t)(kk * 2 * F::kPGroup >> 4), id, add || kk > 0 ? 1u : 0u);
 }
 
-template <int kN, int kSide>
+// kH columns from kC0 on; group: what of a row this warp decodes.
+template <int kN, int kH>
 __device__ __forceinline__ void tc_worker(const PackedAttnParams& p, uint8_t* smem, TcBars& bars, uint32_t tmem,
                                           volatile int* dead, int* s_info, const int* s_len, const Cursor start,
-                                          const int n_tiles, int* s_draft_off) {
+                                          const int n_tiles, const int* s_draft, const int kC0) {
     using F = TcForm<kN>;
-    constexpr int kH = kSide ? F::kH1 : F::kH0, kC0 = kSide ? F::kH0 : 0;   // this side's columns
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, quad = warp & 3;
+    const bool v_side = warp & 4;
+    const int half = warp >> 3;                          // of the row: dims 64 half ..
     const int key = 32 * quad + lane;                    // of a tile; also the lane of tensor memory
     const uint32_t lanes = (uint32_t)(32 * quad) << 16;
     const int nb = p.n_batch, cta = blockIdx.x;
@@ -186,16 +191,14 @@ __device__ __forceinline__ void tc_worker(const PackedAttnParams& p, uint8_t* sm
     int* s_red = reinterpret_cast<int*>(s_l + kN);       // [4][N] the quads' maxima, or sums
     uint8_t* s_p = smem + F::kOffP;
     uint8_t* s_q = smem + F::kOffQ;
-    auto draft_of = [&](int row) { return s_draft_off[row]; };
 
     // ---- the codes and scales of a tile's row, two tiles ahead
-    const uint8_t* codes = kSide ? p.v_codes : p.k_codes;
-    const uint8_t* scales = kSide ? p.v_scales : p.k_scales;
+    const uint8_t* codes = (v_side ? p.v_codes : p.k_codes) + half * (kPackCodeBytes / 2);
+    const uint8_t* scales = (v_side ? p.v_scales : p.k_scales) + half * (kPackGroups / 2);
     Cursor cl = start;           // the tile whose page is looked up next
     int left = n_tiles;
     int page = -1, slot = 0;     // of the tile whose row is loaded next
-    uint32_t w[16];
-    uint2 sc8 = make_uint2(0, 0);
+    uint32_t w[8], sc4 = 0;
     auto look_up = [&]() {
         page = -1;
         if (left <= 0) return;
@@ -210,20 +213,20 @@ __device__ __forceinline__ void tc_worker(const PackedAttnParams& p, uint8_t* sm
         if (page >= 0 && page < p.P) {
             const size_t row = (size_t)page * p.Hkv * p.ps + slot;
             load32(codes + row * kPackCodeBytes, w);
-            load32(codes + row * kPackCodeBytes + 32, w + 8);
-            sc8 = __ldcg(reinterpret_cast<const uint2*>(scales + row * kPackGroups));
+            sc4 = __ldcg(reinterpret_cast<const uint32_t*>(scales + row * kPackGroups));
         } else {
 #pragma unroll
-            for (int i = 0; i < 16; ++i) w[i] = 0;
-            sc8 = make_uint2(0, 0);
+            for (int i = 0; i < 8; ++i) w[i] = 0;
+            sc4 = 0;
         }
         look_up();
     };
-    // the row as fp16, into tensor memory (K) or shared memory (V)
+    // half a row as fp16, into tensor memory (K) or shared memory (V)
+    uint8_t* const v_row = smem + (key >> 3) * 2048 + half * 1024 + (key & 7) * 128;
     auto decode = [&](int tile) {
-        uint32_t f[4] = {scales_f16x2(sc8.x), scales_f16x2(sc8.x >> 16), scales_f16x2(sc8.y), scales_f16x2(sc8.y >> 16)};
+        const uint32_t f[2] = {scales_f16x2(sc4), scales_f16x2(sc4 >> 16)};
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {   // 32 dims: 16 pairs
+        for (int i = 0; i < 2; ++i) {   // 32 dims: 16 pairs
             uint32_t x[16];
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
@@ -233,17 +236,17 @@ __device__ __forceinline__ void tc_worker(const PackedAttnParams& p, uint8_t* sm
                 x[4 * j + 2] = mul_f16x2(codes_f16x2<2>(w[4 * i + j]), s);
                 x[4 * j + 3] = mul_f16x2(codes_f16x2<3>(w[4 * i + j]), s);
             }
-            if (kSide == 0) {
-                tc_st16(tmem + lanes + (tile & 1) * 64 + 16 * i, x);
+            if (!v_side) {
+                tc_st16(tmem + lanes + (tile & 1) * 64 + half * 32 + 16 * i, x);
             } else {
-                uint8_t* v = smem + (tile % kTcVBufs) * kTcVBytes + (key >> 3) * 2048 + (i >> 1) * 1024 + (key & 7) * 128;
+                uint8_t* v = v_row + (tile % kTcVBufs) * kTcVBytes;
 #pragma unroll
                 for (int j = 0; j < 4; ++j)
-                    *reinterpret_cast<uint4*>(v + ((((i & 1) * 4 + j) ^ (key & 7)) << 4)) =
+                    *reinterpret_cast<uint4*>(v + (((i * 4 + j) ^ (key & 7)) << 4)) =
                         make_uint4(x[4 * j], x[4 * j + 1], x[4 * j + 2], x[4 * j + 3]);
             }
         }
-        if (kSide == 0) {
+        if (!v_side) {
             tc_wait_st();
             tc_fence_before();
         } else {
@@ -252,7 +255,7 @@ __device__ __forceinline__ void tc_worker(const PackedAttnParams& p, uint8_t* sm
     };
     auto k_arrive = [&](int tile) {
         __syncwarp();
-        if (kSide == 0 && lane == 0) mbar_arrive(&bars.k_full[tile & 1]);
+        if (!v_side && lane == 0) mbar_arrive(&bars.k_full[tile & 1]);
     };
     // a key's columns of P into the buffer
     auto store_p = [&](uint8_t* buf, const uint32_t (&x)[kH / 2]) {
@@ -284,21 +287,31 @@ __device__ __forceinline__ void tc_worker(const PackedAttnParams& p, uint8_t* sm
             piece_t0 = cur.t;
 #pragma unroll
             for (int i = 0; i < kH; ++i) l[i] = 0.f;
-            for (int row = warp; row < kN; row += kTcWorkers / 32) {
-                uint2 x = make_uint2(0, 0);
+            constexpr int kMine = (kN + 15) / 16;   // rows of a warp, requested together
+            uint2 x[kMine];
+            const float head = p.k_head ? __ldcg(p.k_head + cur.h) : 1.f;
+#pragma unroll
+            for (int k = 0; k < kMine; ++k) {
+                const int row = warp + 16 * k;
+                x[k] = make_uint2(0, 0);
                 if (row < p.n_rows) {
-                    const int i = draft_of(row);
+                    const int i = s_draft[row];
                     const uint32_t* src = reinterpret_cast<const uint32_t*>(
                         p.q + (((size_t)bg * p.R + i) * p.Hq + (size_t)cur.h * p.G + (row - i * p.G)) * kPackDim + 4 * lane);
-                    x.x = __ldcg(src);
-                    x.y = __ldcg(src + 1);
+                    x[k].x = __ldcg(src);
+                    x[k].y = __ldcg(src + 1);
                 }
+            }
+#pragma unroll
+            for (int k = 0; k < kMine; ++k) {
+                const int row = warp + 16 * k;
                 float back;
-                const uint2 y = query_f16(x, back);
+                const uint2 y = query_f16(x[k], back);
+                if (row >= kN) continue;
                 *reinterpret_cast<uint2*>(s_q + (lane >> 4) * F::kQHalf + row * 128 +
                                           ((((lane & 15) >> 1) ^ (row & 7)) << 4) + (lane & 1) * 8) = y;
                 if (lane == 0) {
-                    s_sc[row] = row < p.n_rows ? p.scale_log2 * back * (p.k_head ? __ldcg(p.k_head + cur.h) : 1.f) : 0.f;
+                    s_sc[row] = row < p.n_rows ? p.scale_log2 * back * head : 0.f;
                     s_up[row] = row < p.n_rows ? -kNegInf : 0.f;
                     s_m[row] = row < p.n_rows ? kNegInf : kPUp;
                 }
@@ -320,7 +333,7 @@ __device__ __forceinline__ void tc_worker(const PackedAttnParams& p, uint8_t* sm
         float s[kH];
         const uint32_t s_at = tmem + lanes + F::kColS + b2 * kN + kC0;
 #pragma unroll
-        for (int i = 0; i < kH; i += 16) tc_ld16(s_at + i, s + i);
+        for (int i = 0; i < kH; i += 8) tc_ld8(s_at + i, s + i);
         tc_wait_ld();
         const int key0 = cur.t * kTcTile;
         const bool edge = key0 + kTcTile > L - p.R + 1;
@@ -345,12 +358,12 @@ __device__ __forceinline__ void tc_worker(const PackedAttnParams& p, uint8_t* sm
         int info = first ? 1 : 0;
         if (workers_any(odd || edge)) {
 #pragma unroll
-            for (int i = 0; i < kH; i += 16) tc_ld16(s_at + i, s + i);
+            for (int i = 0; i < kH; i += 8) tc_ld8(s_at + i, s + i);
             tc_wait_ld();
 #pragma unroll
             for (int i = 0; i < kH; ++i) {
                 const int row = kC0 + i;
-                const int end = row < p.n_rows ? L - p.R + draft_of(row) : L - 1;
+                const int end = row < p.n_rows ? L - p.R + s_draft[row] : L - 1;
                 s[i] = key0 + key <= end ? s[i] * s_sc[row] : kNegInf;
                 const int top = __reduce_max_sync(0xffffffffu, ordered(s[i]));
                 if (lane == 0) s_red[quad * kN + row] = top;
@@ -387,14 +400,14 @@ __device__ __forceinline__ void tc_worker(const PackedAttnParams& p, uint8_t* sm
             const uint32_t o_at = tmem + lanes + F::kColO + kC0;
             if (rescale) {
 #pragma unroll 1
-                for (int i = 0; i < kH; i += 16) {
-                    float o[16];
-                    uint32_t r[16];
-                    tc_ld16(o_at + i, o);
+                for (int i = 0; i < kH; i += 8) {
+                    float o[8];
+                    uint32_t r[8];
+                    tc_ld8(o_at + i, o);
                     tc_wait_ld();
 #pragma unroll
-                    for (int k = 0; k < 16; ++k) r[k] = __float_as_uint(o[k] * s_alpha[kC0 + i + k]);
-                    tc_st16(o_at + i, r);
+                    for (int k = 0; k < 8; ++k) r[k] = __float_as_uint(o[k] * s_alpha[kC0 + i + k]);
+                    tc_st8(o_at + i, r);
                 }
                 tc_wait_st();
             }
@@ -431,16 +444,16 @@ __device__ __forceinline__ void tc_worker(const PackedAttnParams& p, uint8_t* sm
                 tc_fence_after();
                 const float down = ex2(-up);
 #pragma unroll 1
-                for (int i = 0; i < kH; i += 16) {
-                    float o[16], f[16];
-                    uint32_t r[16];
-                    tc_ld16(s_at + i, f);
-                    tc_ld16(o_at + i, o);
+                for (int i = 0; i < kH; i += 8) {
+                    float o[8], f[8];
+                    uint32_t r[8];
+                    tc_ld8(s_at + i, f);
+                    tc_ld8(o_at + i, o);
                     tc_wait_ld();
                     // (a piece's first tile finds no sums yet)
 #pragma unroll
-                    for (int k = 0; k < 16; ++k) r[k] = __float_as_uint(info ? f[k] * down : fmaf(f[k], down, o[k]));
-                    tc_st16(o_at + i, r);
+                    for (int k = 0; k < 8; ++k) r[k] = __float_as_uint(info ? f[k] * down : fmaf(f[k], down, o[k]));
+                    tc_st8(o_at + i, r);
                 }
                 tc_wait_st();
                 info = 0;
@@ -490,16 +503,16 @@ __device__ __forceinline__ void tc_worker(const PackedAttnParams& p, uint8_t* sm
         tc_fence_after();
         workers_sync();   // (s_inv)
 #pragma unroll 1
-        for (int i = 0; i < kH; i += 16) {
-            float o[16];
-            tc_ld16(tmem + lanes + F::kColO + kC0 + i, o);
+        for (int i = 0; i < kH; i += 8) {
+            float o[8];
+            tc_ld8(tmem + lanes + F::kColO + kC0 + i, o);
             tc_wait_ld();
 #pragma unroll
-            for (int k = 0; k < 16; ++k) {
+            for (int k = 0; k < 8; ++k) {
                 const int row = kC0 + i + k;
                 if (row >= p.n_rows) continue;
                 const float v = o[k] * s_inv[row];
-                const int d = draft_of(row);
+                const int d = s_draft[row];
                 if (whole)
                     p.out[(((size_t)bg * p.R + d) * p.Hq + (size_t)cur.h * p.G + (row - d * p.G)) * kPackDim + key] =
                         __float2bfloat16(v);
@@ -539,9 +552,9 @@ __global__ void __launch_bounds__(kTcThreads, 1) packed_attention_tc_kernel(cons
     if (threadIdx.x == 0) {
         s_dead = 0;
         for (int i = 0; i < 2; ++i) {
-            mbar_init(&bars.k_full[i], 4);
+            mbar_init(&bars.k_full[i], 8);
             mbar_init(&bars.s_full[i], 1);
-            mbar_init(&bars.p_full[i], 8);
+            mbar_init(&bars.p_full[i], 16);
             mbar_init(&bars.o_done[i], 1);
         }
         mbar_init(&bars.f_done, 1);
@@ -570,7 +583,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) packed_attention_tc_kernel(cons
         *reinterpret_cast<long long*>(s_info + 2) = U;
         s_info[4] = Gc;
     }
-    if (warp == 8) {
+    if (warp == 16) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(&s_tmem)) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
@@ -579,16 +592,13 @@ __global__ void __launch_bounds__(kTcThreads, 1) packed_attention_tc_kernel(cons
     tc_fence_after();
     const uint32_t tmem = s_tmem;
 
-    if (warp < 4) {
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kTcWorkerRegs));
-        tc_worker<kN, 0>(p, smem, bars, tmem, &s_dead, s_info, s_len, share.first, n_tiles, s_draft);
-    } else if (warp < 8) {
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kTcWorkerRegs));
-        tc_worker<kN, 1>(p, smem, bars, tmem, &s_dead, s_info, s_len, share.first, n_tiles, s_draft);
+    const int group = warp >> 2;
+    if (group < 2) {
+        tc_worker<kN, F::kH0>(p, smem, bars, tmem, &s_dead, s_info, s_len, share.first, n_tiles, s_draft, group * F::kH0);
+    } else if (group < 4) {
+        tc_worker<kN, F::kH1>(p, smem, bars, tmem, &s_dead, s_info, s_len, share.first, n_tiles, s_draft,
+                              2 * F::kH0 + (group - 2) * F::kH1);
     } else {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kTcOtherRegs));
-    }
-    if (warp == 8) {
         // ---- the MMAs: S of tile j as soon as its K is there, O of tile j - 1
         // after it -- or before it where tile j opens a piece, whose query rows
         // wait for the end of the one before.  (Each wait names the phase that
@@ -639,5 +649,5 @@ __global__ void __launch_bounds__(kTcThreads, 1) packed_attention_tc_kernel(cons
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    if (warp == 8) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
+    if (warp == 16) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
 }
