@@ -742,16 +742,17 @@ using Kernel = void (*)(const PackedAttnParams);
 struct Choice {
     Kernel kern;
     int threads, smem;
+    int blocks;   // of an SM, where the occupancy query is not asked; 0: it is
 };
 template <int kNT, int kRG>
 Choice choice() {
-    return {packed_attention_kernel<kNT, kRG>, Form<kNT, kRG>::kThreads, Form<kNT, kRG>::kSmem};
+    return {packed_attention_kernel<kNT, kRG>, Form<kNT, kRG>::kThreads, Form<kNT, kRG>::kSmem, 0};
 }
 template <int kN>
 Choice choice_tc() {
-    return {packed_attention_tc_kernel<kN>, kTcThreads, TcForm<kN>::kSmem};
+    return {packed_attention_tc_kernel<kN>, kTcThreads, TcForm<kN>::kSmem, TcForm<kN>::kMinBlocks};
 }
-constexpr int kSyncForms = 9, kForms = kSyncForms + 7;
+constexpr int kSyncForms = 9, kForms = kSyncForms + 4;
 
 // The form for a number of query rows; tc: whether the tcgen05 form may be chosen.
 int form_of(int rows, bool tc) {
@@ -762,8 +763,7 @@ int form_of(int rows, bool tc) {
 Choice choice_of(int form) {
     static const Choice all[kForms] = {choice<1, 1>(), choice<2, 1>(), choice<3, 1>(), choice<4, 1>(), choice<3, 2>(),
                                        choice<3, 3>(), choice<3, 4>(), choice<3, 5>(), choice<3, 6>(),
-                                       choice_tc<32>(), choice_tc<48>(), choice_tc<64>(), choice_tc<80>(),
-                                       choice_tc<96>(), choice_tc<112>(), choice_tc<128>()};
+                                       choice_tc<32>(), choice_tc<48>(), choice_tc<64>(), choice_tc<80>()};
     return all[form];
 }
 
@@ -784,6 +784,9 @@ int resident_of(int form) {
             cudaGetLastError();
             return 0;
         }
+        // (the query answers 1 for a kernel that allocates tensor memory, whatever
+        // it allocates)
+        if (c.blocks) n = c.blocks;
         kept[dev][form] = n;
     }
     return kept[dev][form];

@@ -1,4 +1,4 @@
-// packed_attention_tc.cuh -- the tcgen05 form of packed attention, for 17 to 128
+// packed_attention_tc.cuh -- the tcgen05 form of packed attention, for 17 to 80
 // query rows per KV head (included by packed_attention.cu inside its anonymous
 // namespace: the same split of the keys, pieces and merge).
 //
@@ -8,54 +8,49 @@
 //       the row of its key, its lane), Q a K-major shared-memory operand;
 //   O^T [128 dims x N] += V^T P^T  V as fp16 and P in shared memory, both
 //       MN-major: a thread writes the row of its key as it is.
-// What bounds it: shared memory.  A tile of 128 keys writes V (32 KB) and P and
-// lets the tensor core read V, P and Q: with N = 80 some 1200 cycles at 128
-// bytes, where 18 KB of codes take 800 at the memory's rate, the MMAs 640, the
-// exponentials 640.  K goes by tensor memory, which takes it off that path.
 //
-// One CTA an SM of 17 warps.  Sixteen workers are four groups of four warps, a
-// thread of a group one key of the tile: groups 0 and 2 decode the halves of
-// its K row, groups 1 and 3 those of its V row, one tile ahead of the softmax,
-// with the codes of the tile after that already requested into registers.  Then
-// all do the softmax of the tile, each group a quarter of the columns (query
-// rows).  (With eight warps, whole rows and half the columns each, a tile of 72
-// rows took 3600 cycles, most of them waits on the warps' own results.)  Warp 16
-// issues the MMAs: S of the next tile beside the softmax of this one, O of the
-// last.
+// Two CTAs an SM of eight warps, each with one buffer of
+// everything: while one waits for a product, a fence or a vote, the other has
+// the SM.  (A ninth warp for the MMAs counts as four when the SM's registers
+// are shared out: one CTA fits then.)  Warps 0-3 decode the K rows of a tile, warps 4-7 its V rows; the
+// codes of the next tile come by cp.async meanwhile, every thread's own row.
+// Then all eight do the softmax, a thread one key and each four warps a share
+// of the columns (query rows).  Warp 0 issues the product for S, warp 4 that for
+// O: each would wait for it next.
 //
 // As in the other form P = 2^(s - m + 12), and the tile is taken the short way
-// unless some weight leaves [2^-14, 2^15] or some key is hidden from some row
-// (a vote of the workers).  Then the columns' maxima are found, and O is
-// rescaled where one grows by more than 2^3; weights below 2^-14 (faint) are
-// taken 28 powers of two at a time by products of their own into the place of
-// the tile's S, which the workers add to O.
+// unless some weight would leave [2^-14, 2^15] or some key is hidden from some
+// row (a vote of the workers).  Then (mend) the columns' maxima are found, O is
+// rescaled where one grows by more than 2^3, hidden scores become -inf where they
+// lie, and weights below 2^-14 (faint) are taken 28 powers of two at a time by
+// products of their own, which the workers add to O.  Mending is rolled up, for
+// the instruction cache's sake.
 //
 // Every mbarrier wait is bounded; after one that gives up nothing waits or is
 // issued any more, every warp still meets every block barrier, and the status
 // word says so.
 
-constexpr int kTcThreads = 544;
-constexpr int kTcWorkers = 512;
+constexpr int kTcThreads = 256;
 constexpr int kTcTile = 128;                       // keys of a tile: the MMAs' M (S) and K (O)
 constexpr int kTcVBytes = kTcTile * 256;           // V of a tile in fp16
-constexpr int kTcVBufs = 3;
-constexpr int kTcMinRows = 17, kTcMaxRows = 128;   // query rows that it takes
+constexpr int kTcRawBytes = 2 * kTcTile * kPackCodeBytes;   // codes of K and V of a tile
+constexpr int kTcMinRows = 17, kTcMaxRows = 80;    // query rows that it takes
 
 template <int kN>
 struct TcForm {
-    // columns of groups 0 and 1, and of groups 2 and 3: multiples of 8
-    static constexpr int kH0 = (kN + 31) / 32 * 8, kH1 = kN / 2 - kH0;
-    static constexpr int kNHalves = kN > 64 ? 2 : 1;                     // 64-column atoms of P
-    static constexpr int kPGroup = kNHalves * 1024;                      // bytes of P for 8 keys
-    static constexpr int kPBytes = kTcTile / 8 * kPGroup;
+    static constexpr int kMinBlocks = 2;
+    static constexpr int kH = (kN + 15) / 16 * 8, kH1 = kN - kH;         // columns of warps 0-3, of warps 4-7: multiples of 8
+    static constexpr int kAtoms = kN > 64 ? 2 : 1;                       // 64-column atoms of P
+    static constexpr int kPGroup = kAtoms * 1024;                        // bytes of P for 8 keys
     static constexpr int kQHalf = kN * 128;                              // bytes of a dim half of Q
-    static constexpr int kColS = 128, kColO = kColS + 2 * kN;            // tensor memory: K [0, 128), S twice, O
-    static_assert(kColO + kN <= 512, "tensor memory");
-    // V ring | P twice | Q | columns | lengths
-    static constexpr int kOffP = kTcVBufs * kTcVBytes, kOffQ = kOffP + 2 * kPBytes, kOffCol = kOffQ + 2 * kQHalf;
-    static constexpr int kOffLen = kOffCol + kN * 4 * (6 + 4);
+    static constexpr int kColS = 64, kColO = kColS + kN;                 // tensor memory: K [0, 64), S, O
+    static constexpr int kCols = kColO + kN <= 128 ? 128 : 256;
+    static_assert(kColO + kN <= kCols && kCols * kMinBlocks <= 512, "tensor memory");
+    // V | P | Q | raw codes | columns | lengths
+    static constexpr int kOffP = kTcVBytes, kOffQ = kOffP + kTcTile / 8 * kPGroup, kOffRaw = kOffQ + 2 * kQHalf;
+    static constexpr int kOffCol = kOffRaw + kTcRawBytes, kOffLen = kOffCol + kN * 4 * (5 + 8);
     static constexpr int kSmem = kOffLen + kMaxBatchPerLaunch * 4 + 1024;
-    static_assert(kSmem <= 232448 - 1024, "shared memory");
+    static_assert((kSmem + 2048) * kMinBlocks <= 233472, "shared memory");
 };
 
 __device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
@@ -103,34 +98,28 @@ __host__ __device__ constexpr uint32_t tc_idesc(int n, bool a_mn, bool b_mn) {
     return (1u << 4) | (a_mn ? 1u << 15 : 0u) | (b_mn ? 1u << 16 : 0u) | ((uint32_t)(n >> 3) << 17) | (8u << 24);
 }
 
-__device__ __forceinline__ void load32(const uint8_t* p, uint32_t* r) {   // 32 bytes, 32-byte aligned
-    asm volatile("ld.global.cg.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
-                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
-                 : "l"(p)
-                 : "memory");
+__device__ __forceinline__ float fmax3(float a, float b, float c) {
+    float d;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    return d;
 }
-__device__ __forceinline__ uint32_t max_f16x2(uint32_t a, uint32_t b) {
-    uint32_t r;
-    asm("max.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
-    return r;
-}
-__device__ __forceinline__ uint32_t min_f16x2(uint32_t a, uint32_t b) {
-    uint32_t r;
-    asm("min.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
-    return r;
+__device__ __forceinline__ float fmin3(float a, float b, float c) {
+    float d;
+    asm("min.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    return d;
 }
 // Whether any of the workers' threads says so; a barrier of theirs.
 __device__ __forceinline__ bool workers_any(bool x) {
     uint32_t r;
     asm volatile(
-        "{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbarrier.cta.red.or.pred q, 1, 512, p;\n\t"
+        "{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbarrier.cta.red.or.pred q, 1, 256, p;\n\t"
         "selp.u32 %0, 1, 0, q;\n\t}\n"
         : "=r"(r)
         : "r"((uint32_t)x)
         : "memory");
     return r != 0;
 }
-__device__ __forceinline__ void workers_sync() { asm volatile("barrier.cta.sync 1, 512;" ::: "memory"); }
+__device__ __forceinline__ void workers_sync() { asm volatile("barrier.cta.sync 1, 256;" ::: "memory"); }
 
 // A float's bits as an integer of the same order, and back.
 __device__ __forceinline__ int ordered(float x) {
@@ -139,46 +128,51 @@ __device__ __forceinline__ int ordered(float x) {
 }
 __device__ __forceinline__ float unordered(int b) { return __int_as_float(b < 0 ? b ^ 0x7fffffff : b); }
 
-// Bounded; returns at once when another wait has given up.
-__device__ __forceinline__ void tc_wait(uint64_t* bar, uint32_t parity, volatile int* dead, int* status) {
-    if (mbar_test_wait(bar, parity) || *dead) return;
-    if (mbar_wait_bounded(bar, parity)) return;
+// Bounded; returns at once when another wait has given up.  (Out of line: the loop's code is long.)
+__device__ __noinline__ void tc_wait_long(uint64_t* bar, uint32_t parity, volatile int* dead, int* status) {
+    if (*dead || mbar_wait_bounded(bar, parity)) return;
     *dead = 1;
     atomicOr(status, CS_DEVICE_WAIT_TIMEOUT);
+}
+__device__ __forceinline__ void tc_wait(uint64_t* bar, uint32_t parity, volatile int* dead, int* status) {
+    if (!mbar_test_wait(bar, parity)) tc_wait_long(bar, parity, dead, status);
 }
 
 // Whether no wait has given up, the same answer in the whole warp.
 __device__ __forceinline__ bool alive(volatile int* dead) { return !__any_sync(0xffffffffu, *dead); }
 
 struct TcBars {
-    uint64_t k_full[2];    // K of a tile decoded (8 warps)
-    uint64_t s_full[2];    // S of a tile done; its K is read
-    uint64_t p_full[2];    // P and V of a tile written, its S read (16 warps)
-    uint64_t o_done[2];    // O of a tile done; its P and V are read
+    uint64_t k_full;       // K of a tile decoded (4 warps)
+    uint64_t s_full;       // S of a tile done; its K is read
+    uint64_t p_full;       // P and V of a tile written, its S read (8 warps)
+    uint64_t o_done;       // O of a tile done; its P and V are read
     uint64_t f_done;       // a product of faint weights done
 };
 
-// V^T P^T of tile j into the columns from d on (one thread issues): 8 steps of 16 keys.
+// V^T P^T, n columns of P from an atom's first on, into the columns from d on
+// (one thread issues): 8 steps of 16 keys.
 template <int kN>
-__device__ __forceinline__ void tc_mma_values(uint32_t d, uint8_t* smem, int j, bool add) {
+__device__ __forceinline__ void tc_mma_values(uint32_t d, uint8_t* smem, int atom, int n, bool add) {
     using F = TcForm<kN>;
-    constexpr uint32_t id = tc_idesc(kN, true, true);
-    const uint64_t v = tc_desc(smem_u32(smem + (j % kTcVBufs) * kTcVBytes), 2048, 1024);
-    const uint64_t x = tc_desc(smem_u32(smem + F::kOffP + (j & 1) * F::kPBytes), F::kPGroup, 1024);
+    const uint32_t id = tc_idesc(n, true, true);
+    const uint64_t v = tc_desc(smem_u32(smem), 2048, 1024);
+    const uint64_t x = tc_desc(smem_u32(smem + F::kOffP + atom * 1024), F::kPGroup, 1024);
 #pragma unroll
     for (int kk = 0; kk < kTcTile / 16; ++kk)
         tc_mma_ss(d, v + (uint64_t)(kk * (4096 >> 4)), x + (uint64_t)(kk * 2 * F::kPGroup >> 4), id, add || kk > 0 ? 1u : 0u);
 }
 
-// kH columns from kC0 on; group: what of a row this warp decodes.
-template <int kN, int kH>
+template <int kN>
 __device__ __forceinline__ void tc_worker(const PackedAttnParams& p, uint8_t* smem, TcBars& bars, uint32_t tmem,
-                                          volatile int* dead, int* s_info, const int* s_len, const Cursor start,
-                                          const int n_tiles, const int* s_draft, const int kC0) {
+                                          volatile int* dead, const int* s_info, const int* s_len, const Cursor start,
+                                          const int n_tiles, const int* s_draft) {
     using F = TcForm<kN>;
+    constexpr int kH = F::kH;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, quad = warp & 3;
-    const bool v_side = warp & 4;
-    const int half = warp >> 3;                          // of the row: dims 64 half ..
+    const bool v_side = warp >= 4;
+    // this side's columns: kH of them, or fewer (one body of code for both)
+    const int kC0 = v_side ? kH : 0, n_cols = v_side ? F::kH1 : kH;
+    auto mine = [&](int i) { return kH == F::kH1 || i < n_cols; };
     const int key = 32 * quad + lane;                    // of a tile; also the lane of tensor memory
     const uint32_t lanes = (uint32_t)(32 * quad) << 16;
     const int nb = p.n_batch, cta = blockIdx.x;
@@ -187,18 +181,21 @@ __device__ __forceinline__ void tc_worker(const PackedAttnParams& p, uint8_t* sm
     float* s_alpha = s_up + kN;                          // [N] what a column's sums are rescaled by
     float* s_m = s_alpha + kN;                           // [N] running maxima
     float* s_inv = s_m + kN;                             // [N] 1 / l at the end
-    float* s_l = s_inv + kN;                             // [N]
-    int* s_red = reinterpret_cast<int*>(s_l + kN);       // [4][N] the quads' maxima, or sums
-    uint8_t* s_p = smem + F::kOffP;
+    int* s_red = reinterpret_cast<int*>(s_inv + kN);     // [4][N] the quads' maxima, or sums
+    float* s_faint = reinterpret_cast<float*>(s_red + 4 * kN);   // [4][N] the quads' sums of faint weights
+
     uint8_t* s_q = smem + F::kOffQ;
 
-    // ---- the codes and scales of a tile's row, two tiles ahead
-    const uint8_t* codes = (v_side ? p.v_codes : p.k_codes) + half * (kPackCodeBytes / 2);
-    const uint8_t* scales = (v_side ? p.v_scales : p.k_scales) + half * (kPackGroups / 2);
+    // ---- the next tile's row: codes into shared memory (parts exchanged by the
+    // key's bits, so that the threads' 16-byte loads meet every bank once), scales
+    const uint8_t* codes = v_side ? p.v_codes : p.k_codes;
+    const uint8_t* scales = v_side ? p.v_scales : p.k_scales;
+    uint8_t* const raw = smem + F::kOffRaw + (v_side ? kTcRawBytes / 2 : 0) + key * kPackCodeBytes;
+    const int raw_x = (key >> 1) & 3;
     Cursor cl = start;           // the tile whose page is looked up next
     int left = n_tiles;
     int page = -1, slot = 0;     // of the tile whose row is loaded next
-    uint32_t w[8], sc4 = 0;
+    uint2 sc8 = make_uint2(0, 0);
     auto look_up = [&]() {
         page = -1;
         if (left <= 0) return;
@@ -210,62 +207,47 @@ __device__ __forceinline__ void tc_worker(const PackedAttnParams& p, uint8_t* sm
         advance(cl, s_len, nb, p.Hkv, kTcTile);
     };
     auto load_row = [&]() {      // zeros for a key past the context or on no page
-        if (page >= 0 && page < p.P) {
-            const size_t row = (size_t)page * p.Hkv * p.ps + slot;
-            load32(codes + row * kPackCodeBytes, w);
-            sc4 = __ldcg(reinterpret_cast<const uint32_t*>(scales + row * kPackGroups));
-        } else {
+        const bool in = page >= 0 && page < p.P;
+        const size_t row = in ? (size_t)page * p.Hkv * p.ps + slot : 0;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) w[i] = 0;
-            sc4 = 0;
-        }
+        for (int i = 0; i < 4; ++i) cp_async16(smem_u32(raw + ((i ^ raw_x) << 4)), codes + row * kPackCodeBytes + 16 * i, in);
+        cp_async_commit();
+        sc8 = in ? __ldcg(reinterpret_cast<const uint2*>(scales + row * kPackGroups)) : make_uint2(0, 0);
         look_up();
     };
-    // half a row as fp16, into tensor memory (K) or shared memory (V)
-    uint8_t* const v_row = smem + (key >> 3) * 2048 + half * 1024 + (key & 7) * 128;
-    auto decode = [&](int tile) {
-        const uint32_t f[2] = {scales_f16x2(sc4), scales_f16x2(sc4 >> 16)};
+    // the row as fp16, into tensor memory (K) or shared memory (V)
+    uint8_t* const v_row = smem + (key >> 3) * 2048 + (key & 7) * 128;
+    auto decode = [&]() {
+        cp_async_wait<0>();
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {   // 32 dims: 16 pairs
+        for (int i = 0; i < 4; ++i) {   // 32 dims: 16 pairs
+            const uint4 w4 = *reinterpret_cast<const uint4*>(raw + ((i ^ raw_x) << 4));
+            const uint32_t w[4] = {w4.x, w4.y, w4.z, w4.w};
+            const uint32_t f = scales_f16x2((i & 2 ? sc8.y : sc8.x) >> (i & 1 ? 16 : 0));
             uint32_t x[16];
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const uint32_t s = __byte_perm(f[i], 0, j < 2 ? 0x1010 : 0x3232);
-                x[4 * j] = mul_f16x2(codes_f16x2<0>(w[4 * i + j]), s);
-                x[4 * j + 1] = mul_f16x2(codes_f16x2<1>(w[4 * i + j]), s);
-                x[4 * j + 2] = mul_f16x2(codes_f16x2<2>(w[4 * i + j]), s);
-                x[4 * j + 3] = mul_f16x2(codes_f16x2<3>(w[4 * i + j]), s);
+                const uint32_t s = __byte_perm(f, 0, j < 2 ? 0x1010 : 0x3232);
+                x[4 * j] = mul_f16x2(codes_f16x2<0>(w[j]), s);
+                x[4 * j + 1] = mul_f16x2(codes_f16x2<1>(w[j]), s);
+                x[4 * j + 2] = mul_f16x2(codes_f16x2<2>(w[j]), s);
+                x[4 * j + 3] = mul_f16x2(codes_f16x2<3>(w[j]), s);
             }
             if (!v_side) {
-                tc_st16(tmem + lanes + (tile & 1) * 64 + half * 32 + 16 * i, x);
+                tc_st16(tmem + lanes + 16 * i, x);
             } else {
-                uint8_t* v = v_row + (tile % kTcVBufs) * kTcVBytes;
 #pragma unroll
                 for (int j = 0; j < 4; ++j)
-                    *reinterpret_cast<uint4*>(v + (((i * 4 + j) ^ (key & 7)) << 4)) =
+                    *reinterpret_cast<uint4*>(v_row + (i >> 1) * 1024 + ((((i & 1) * 4 + j) ^ (key & 7)) << 4)) =
                         make_uint4(x[4 * j], x[4 * j + 1], x[4 * j + 2], x[4 * j + 3]);
             }
         }
-        if (!v_side) {
-            tc_wait_st();
-            tc_fence_before();
-        } else {
-            fence_async_smem();
-        }
     };
-    auto k_arrive = [&](int tile) {
-        __syncwarp();
-        if (!v_side && lane == 0) mbar_arrive(&bars.k_full[tile & 1]);
-    };
-    // a key's columns of P into the buffer
-    auto store_p = [&](uint8_t* buf, const uint32_t (&x)[kH / 2]) {
-        uint8_t* row = buf + (key >> 3) * F::kPGroup + (key & 7) * 128;
-#pragma unroll
-        for (int i = 0; i < kH / 8; ++i) {
-            const int col = kC0 + 8 * i;
-            *reinterpret_cast<uint4*>(row + (col >> 6) * 1024 + ((((col & 63) >> 3) ^ (key & 7)) << 4)) =
-                make_uint4(x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]);
-        }
+    // eight of a key's columns of P, from `col` on
+    uint8_t* const p_row = smem + F::kOffP + (key >> 3) * F::kPGroup + (key & 7) * 128;
+    auto store_p = [&](int col, uint32_t x0, uint32_t x1, uint32_t x2, uint32_t x3) {
+        *reinterpret_cast<uint4*>(p_row + (col >> 6) * 1024 + ((((col & 63) >> 3) ^ (key & 7)) << 4)) =
+            make_uint4(x0, x1, x2, x3);
     };
 
     look_up();
@@ -275,24 +257,22 @@ __device__ __forceinline__ void tc_worker(const PackedAttnParams& p, uint8_t* sm
     bool first_piece = true;
     uint32_t f_phase = 0;
     int piece_t0 = cur.t;
-    decode(0);
-    load_row();
+#pragma unroll 1
     for (int j = 0; j < n_tiles; ++j) {
         const int L = s_len[cur.b], bg = p.b_base + cur.b;
-        const int b2 = j & 1;
-        const uint32_t ph = (uint32_t)(j >> 1) & 1;
+        const uint32_t ph = (uint32_t)j & 1;
         const bool first = j == 0 || cur.t == 0, last = j + 1 == n_tiles || cur.t + 1 == cur.T;
         if (first) {
             // ---- a new piece: its query rows as fp16 below 2^15 (as in the other form)
             piece_t0 = cur.t;
 #pragma unroll
             for (int i = 0; i < kH; ++i) l[i] = 0.f;
-            constexpr int kMine = (kN + 15) / 16;   // rows of a warp, requested together
+            constexpr int kMine = kN / 8;   // rows of a warp, requested together
             uint2 x[kMine];
             const float head = p.k_head ? __ldcg(p.k_head + cur.h) : 1.f;
 #pragma unroll
             for (int k = 0; k < kMine; ++k) {
-                const int row = warp + 16 * k;
+                const int row = warp + 8 * k;
                 x[k] = make_uint2(0, 0);
                 if (row < p.n_rows) {
                     const int i = s_draft[row];
@@ -304,73 +284,77 @@ __device__ __forceinline__ void tc_worker(const PackedAttnParams& p, uint8_t* sm
             }
 #pragma unroll
             for (int k = 0; k < kMine; ++k) {
-                const int row = warp + 16 * k;
+                const int row = warp + 8 * k;
                 float back;
                 const uint2 y = query_f16(x[k], back);
-                if (row >= kN) continue;
                 *reinterpret_cast<uint2*>(s_q + (lane >> 4) * F::kQHalf + row * 128 +
                                           ((((lane & 15) >> 1) ^ (row & 7)) << 4) + (lane & 1) * 8) = y;
                 if (lane == 0) {
-                    s_sc[row] = row < p.n_rows ? p.scale_log2 * back * head : 0.f;
+                    // (not 0, under which a hidden score would be NaN)
+                    s_sc[row] = row < p.n_rows ? fmaxf(p.scale_log2 * back * head, 0x1p-126f) : 0x1p-126f;
                     s_up[row] = row < p.n_rows ? -kNegInf : 0.f;
                     s_m[row] = row < p.n_rows ? kNegInf : kPUp;
+                    for (int k4 = 0; k4 < 4; ++k4) s_faint[k4 * kN + row] = 0.f;
                 }
             }
             fence_async_smem();
             workers_sync();
-            k_arrive(j);
         }
-        // ---- the next tile's row, once P and V of two tiles before are read
-        if (j >= 2) tc_wait(&bars.o_done[b2], ph ^ 1, dead, p.status);
-        if (j + 1 < n_tiles) {
-            decode(j + 1);
-            load_row();
-            if (!last) k_arrive(j + 1);   // (a new piece's waits for its query rows)
+        // ---- this tile's row (V once the product of the tile before has read its buffer),
+        // and the request of the next one's
+        if (v_side && j > 0) tc_wait(&bars.o_done, ph ^ 1, dead, p.status);
+        decode();
+        load_row();
+        if (!v_side) {
+            tc_wait_st();
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&bars.k_full);
+            if (warp == 0) {
+                // (each wait names the phase that follows the last one seen of its barrier)
+                tc_wait(&bars.k_full, ph, dead, p.status);
+                tc_fence_after();
+                __syncwarp();
+                if (alive(dead) && elect_one()) {
+                    const uint64_t dq = tc_desc(smem_u32(s_q), 1024, 0);
+#pragma unroll
+                    for (int ks = 0; ks < kPackDim / 16; ++ks)
+                        tc_mma_ts(tmem + F::kColS, tmem + ks * 8,
+                                  dq + (uint64_t)((ks >> 2) * (F::kQHalf >> 4) + (ks & 3) * 2), tc_idesc(kN, false, false),
+                                  ks > 0 ? 1u : 0u);
+                    tc_commit(&bars.s_full);
+                }
+                __syncwarp();
+            }
         }
         // ---- softmax: this key's scores
-        tc_wait(&bars.s_full[b2], ph, dead, p.status);
+        tc_wait(&bars.s_full, ph, dead, p.status);
         tc_fence_after();
-        float s[kH];
-        const uint32_t s_at = tmem + lanes + F::kColS + b2 * kN + kC0;
-#pragma unroll
-        for (int i = 0; i < kH; i += 8) tc_ld8(s_at + i, s + i);
-        tc_wait_ld();
+        const uint32_t s_at = tmem + lanes + F::kColS + kC0, o_at = tmem + lanes + F::kColO + kC0;
         const int key0 = cur.t * kTcTile;
         const bool edge = key0 + kTcTile > L - p.R + 1;
-        uint32_t pk[kH / 2], most = 0, least = 0x7c007c00u;
+        bool starts = first;   // whether the tile's product starts O
+        // what a tile needs before it can go the short way
+        auto mend = [&]() {
+#pragma unroll 1
+            for (int i = 0; i < n_cols; i += 8) {
+                float z[8];
+                tc_ld8(s_at + i, z);
+                tc_wait_ld();
 #pragma unroll
-        for (int i = 0; i < kH; i += 4) {
-            const float4 c = *reinterpret_cast<const float4*>(s_sc + kC0 + i), u = *reinterpret_cast<const float4*>(s_up + kC0 + i);
-            float x0, x1, x2, x3;
-            f2_unpack(f2_fma(f2_pack(s[i], s[i + 1]), f2_pack(c.x, c.y), f2_pack(u.x, u.y)), x0, x1);
-            f2_unpack(f2_fma(f2_pack(s[i + 2], s[i + 3]), f2_pack(c.z, c.w), f2_pack(u.z, u.w)), x2, x3);
-            s[i] = ex2(x0);
-            s[i + 1] = ex2(x1);
-            s[i + 2] = ex2(x2);
-            s[i + 3] = ex2(x3);
-            pk[i / 2] = pack_f16x2(s[i], s[i + 1]);
-            pk[i / 2 + 1] = pack_f16x2(s[i + 2], s[i + 3]);
-            most = max_f16x2(most, max_f16x2(pk[i / 2], pk[i / 2 + 1]));
-            least = min_f16x2(least, min_f16x2(pk[i / 2], pk[i / 2 + 1]));
-        }
-        // (bits of positive fp16 numbers are in their order) above 2^15, below 2^-14
-        const bool odd = max(most & 0xffffu, most >> 16) > 0x7800u || min(least & 0xffffu, least >> 16) < 0x0400u;
-        int info = first ? 1 : 0;
-        if (workers_any(odd || edge)) {
-#pragma unroll
-            for (int i = 0; i < kH; i += 8) tc_ld8(s_at + i, s + i);
-            tc_wait_ld();
-#pragma unroll
-            for (int i = 0; i < kH; ++i) {
-                const int row = kC0 + i;
-                const int end = row < p.n_rows ? L - p.R + s_draft[row] : L - 1;
-                s[i] = key0 + key <= end ? s[i] * s_sc[row] : kNegInf;
-                const int top = __reduce_max_sync(0xffffffffu, ordered(s[i]));
-                if (lane == 0) s_red[quad * kN + row] = top;
+                for (int k = 0; k < 8; ++k) {
+                    const int row = kC0 + i + k;
+                    const int end = row < p.n_rows ? L - p.R + s_draft[row] : L - 1;
+                    if (key0 + key > end) z[k] = kNegInf;
+                    const int top = __reduce_max_sync(0xffffffffu, ordered(z[k] * s_sc[row]));
+                    if (lane == 0) s_red[quad * kN + row] = top;
+                }
+                if (edge) tc_st8(s_at + i, reinterpret_cast<const uint32_t*>(z));
             }
+            tc_wait_st();
             workers_sync();
             bool grew = false;
-            if (key < kH) {
+            if (key < n_cols) {
                 const int row = kC0 + key;
                 const float now = unordered(max(max(s_red[row], s_red[kN + row]), max(s_red[2 * kN + row], s_red[3 * kN + row])));
                 const float m = s_m[row];
@@ -379,105 +363,165 @@ __device__ __forceinline__ void tc_worker(const PackedAttnParams& p, uint8_t* sm
                     a = ex2(m - now);
                     s_m[row] = now;
                     s_up[row] = kPUp - now;
+                    for (int k = 0; k < 4; ++k) s_faint[k * kN + row] *= a;
                     grew = !first;
+                } else if (m == kNegInf) {
+                    s_up[row] = 0.f;   // (no key for this row in the piece: those that a row sees come first)
                 }
                 s_alpha[row] = a;
             }
             const bool rescale = workers_any(grew);
+#pragma unroll
+            for (int i = 0; i < kH; i += 4) {
+                if (!mine(i)) continue;
+                const float4 a = *reinterpret_cast<const float4*>(s_alpha + kC0 + i);
+                l[i] *= a.x;
+                l[i + 1] *= a.y;
+                l[i + 2] *= a.z;
+                l[i + 3] *= a.w;
+            }
             auto is_faint = [&](float x) { return x < kPMin && x > kPGone; };
             bool faint = false;
+#pragma unroll 1
+            for (int i = 0; i < n_cols; i += 8) {
+                float z[8];
+                tc_ld8(s_at + i, z);
+                tc_wait_ld();
 #pragma unroll
-            for (int i = 0; i < kH; ++i) {
-                l[i] *= s_alpha[kC0 + i];
-                s[i] = s[i] == kNegInf ? kNegInf : s[i] + s_up[kC0 + i];
-                faint |= is_faint(s[i]);
+                for (int k = 0; k < 8; ++k) faint |= is_faint(fmaf(z[k], s_sc[kC0 + i + k], s_up[kC0 + i + k]));
             }
             faint = workers_any(faint);
             if ((rescale || faint) && j > 0) {
-                tc_wait(&bars.o_done[b2 ^ 1], (uint32_t)((j - 1) >> 1) & 1, dead, p.status);
+                tc_wait(&bars.o_done, ph ^ 1, dead, p.status);
                 tc_fence_after();
             }
-            const uint32_t o_at = tmem + lanes + F::kColO + kC0;
             if (rescale) {
 #pragma unroll 1
-                for (int i = 0; i < kH; i += 8) {
+                for (int i = 0; i < n_cols; i += 8) {
                     float o[8];
-                    uint32_t r[8];
                     tc_ld8(o_at + i, o);
                     tc_wait_ld();
 #pragma unroll
-                    for (int k = 0; k < 8; ++k) r[k] = __float_as_uint(o[k] * s_alpha[kC0 + i + k]);
-                    tc_st8(o_at + i, r);
+                    for (int k = 0; k < 8; ++k) o[k] *= s_alpha[kC0 + i + k];
+                    tc_st8(o_at + i, reinterpret_cast<const uint32_t*>(o));
                 }
                 tc_wait_st();
             }
+#pragma unroll 1
             for (float up = 28.f; faint; up += 28.f) {
-                // this turn's weights through the tile's P, their product into its S (both free yet)
-                uint32_t pf[kH / 2];
+                bool more = false;
+#pragma unroll 1
+                for (int i = 0; i < n_cols; i += 8) {   // this turn's weights, which then are done
+                    float z[8], f[8];
+                    tc_ld8(s_at + i, z);
+                    tc_wait_ld();
 #pragma unroll
-                for (int i = 0; i < kH; i += 2) {
-                    float f[2];
-#pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        const float x = s[i + e];
+                    for (int k = 0; k < 8; ++k) {
+                        const int row = kC0 + i + k;
+                        const float x = fmaf(z[k], s_sc[row], s_up[row]);
                         const bool now = x < kPMin && x + up >= kPMin;
-                        f[e] = now ? ex2(x + up) : 0.f;
-                        if (now) {
-                            l[i + e] += ex2(x);
-                            s[i + e] = kNegInf;
-                        }
+                        f[k] = now ? ex2(x + up) : 0.f;
+                        more |= !now && is_faint(x);
+                        if (now) z[k] = kNegInf;
+                        float sum = now ? ex2(x) : 0.f;
+#pragma unroll
+                        for (int off = 16; off > 0; off >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
+                        if (lane == 0) s_faint[quad * kN + row] += sum;
                     }
-                    pf[i / 2] = pack_f16x2(f[0], f[1]);
+                    tc_st8(s_at + i, reinterpret_cast<const uint32_t*>(z));
+                    store_p(kC0 + i, pack_f16x2(f[0], f[1]), pack_f16x2(f[2], f[3]), pack_f16x2(f[4], f[5]),
+                            pack_f16x2(f[6], f[7]));
                 }
-                store_p(s_p + b2 * F::kPBytes, pf);
+                tc_wait_st();
                 fence_async_smem();
-                tc_fence_before();
-                workers_sync();
-                tc_fence_after();
-                if (warp == 0 && alive(dead) && elect_one()) {
-                    tc_mma_values<kN>(tmem + F::kColS + b2 * kN, smem, j, false);
-                    tc_commit(&bars.f_done);
-                }
-                __syncwarp();
-                tc_wait(&bars.f_done, f_phase, dead, p.status);
-                f_phase ^= 1;
-                tc_fence_after();
                 const float down = ex2(-up);
 #pragma unroll 1
-                for (int i = 0; i < kH; i += 8) {
-                    float o[8], f[8];
-                    uint32_t r[8];
-                    tc_ld8(s_at + i, f);
-                    tc_ld8(o_at + i, o);
-                    tc_wait_ld();
-                    // (a piece's first tile finds no sums yet)
+                for (int atom = 0; atom < F::kAtoms; ++atom) {   // 64 columns at a time, into the place of this tile's K
+                    tc_fence_before();
+                    workers_sync();
+                    tc_fence_after();
+                    if (warp == 0 && alive(dead) && elect_one()) {
+                        tc_mma_values<kN>(tmem, smem, atom, min(64, kN - 64 * atom), false);
+                        tc_commit(&bars.f_done);
+                    }
+                    __syncwarp();
+                    tc_wait(&bars.f_done, f_phase, dead, p.status);
+                    f_phase ^= 1;
+                    tc_fence_after();
+#pragma unroll 1
+                    for (int i = 0; i < n_cols; i += 8) {
+                        if ((kC0 + i) >> 6 != atom) continue;
+                        float o[8], f[8];
+                        tc_ld8(tmem + lanes + ((kC0 + i) & 63), f);
+                        tc_ld8(o_at + i, o);
+                        tc_wait_ld();
+                        // (a piece's first tile finds no sums yet)
 #pragma unroll
-                    for (int k = 0; k < 8; ++k) r[k] = __float_as_uint(info ? f[k] * down : fmaf(f[k], down, o[k]));
-                    tc_st8(o_at + i, r);
+                        for (int k = 0; k < 8; ++k) o[k] = starts ? f[k] * down : fmaf(f[k], down, o[k]);
+                        tc_st8(o_at + i, reinterpret_cast<const uint32_t*>(o));
+                    }
+                    tc_wait_st();
                 }
-                tc_wait_st();
-                info = 0;
-                bool more = false;
-#pragma unroll
-                for (int i = 0; i < kH; ++i) more |= is_faint(s[i]);
+                starts = false;
                 tc_fence_before();
                 faint = workers_any(more);
+                tc_fence_after();
             }
+        };
+        // x = s - m + 12 of this side's columns, eight at a time
+        auto scores = [&](int i, float (&x)[8]) {
+            tc_ld8(s_at + i, x);
+            float c[8], u[8];
 #pragma unroll
-            for (int i = 0; i < kH; i += 2) {
-                s[i] = ex2(s[i]);
-                s[i + 1] = ex2(s[i + 1]);
-                pk[i / 2] = pack_f16x2(s[i], s[i + 1]);
+            for (int k = 0; k < 8; k += 4) {
+                *reinterpret_cast<float4*>(c + k) = *reinterpret_cast<const float4*>(s_sc + kC0 + i + k);
+                *reinterpret_cast<float4*>(u + k) = *reinterpret_cast<const float4*>(s_up + kC0 + i + k);
+            }
+            tc_wait_ld();
+#pragma unroll
+            for (int k = 0; k < 8; k += 2)
+                f2_unpack(f2_fma(f2_pack(x[k], x[k + 1]), f2_pack(c[k], c[k + 1]), f2_pack(u[k], u[k + 1])), x[k], x[k + 1]);
+        };
+        float most = 0.f, least = 0.f;
+#pragma unroll
+        for (int i = 0; i < kH; i += 8) {
+            if (!mine(i)) continue;
+            float x[8];
+            scores(i, x);
+#pragma unroll
+            for (int k = 0; k < 8; k += 2) {
+                most = fmax3(most, x[k], x[k + 1]);
+                least = fmin3(least, x[k], x[k + 1]);
             }
         }
+        if (workers_any(most > kPMax || least < kPMin || edge)) mend();
+        if (!v_side && j > 0) tc_wait(&bars.o_done, ph ^ 1, dead, p.status);   // P is free
 #pragma unroll
-        for (int i = 0; i < kH; i += 2) f2_unpack(f2_add(f2_pack(l[i], l[i + 1]), f2_pack(s[i], s[i + 1])), l[i], l[i + 1]);
-        store_p(s_p + b2 * F::kPBytes, pk);
-        if (threadIdx.x == 0) s_info[b2] = info;
+        for (int i = 0; i < kH; i += 8) {
+            if (!mine(i)) continue;
+            float x[8];
+            scores(i, x);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) x[k] = ex2(x[k]);
+            store_p(kC0 + i, pack_f16x2(x[0], x[1]), pack_f16x2(x[2], x[3]), pack_f16x2(x[4], x[5]), pack_f16x2(x[6], x[7]));
+#pragma unroll
+            for (int k = 0; k < 8; k += 2)
+                f2_unpack(f2_add(f2_pack(l[i + k], l[i + k + 1]), f2_pack(x[k], x[k + 1])), l[i + k], l[i + k + 1]);
+        }
         fence_async_smem();
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive(&bars.p_full[b2]);
+        if (lane == 0) mbar_arrive(&bars.p_full);
+        if (warp == 4) {
+            tc_wait(&bars.p_full, ph, dead, p.status);
+            tc_fence_after();
+            __syncwarp();
+            if (alive(dead) && elect_one()) {
+                tc_mma_values<kN>(tmem + F::kColO, smem, 0, kN, !starts);
+                tc_commit(&bars.o_done);
+            }
+            __syncwarp();
+        }
         if (!last) {
             advance(cur, s_len, nb, p.Hkv, kTcTile);
             continue;
@@ -488,22 +532,24 @@ __device__ __forceinline__ void tc_worker(const PackedAttnParams& p, uint8_t* sm
         float* s_sum = reinterpret_cast<float*>(s_red);
 #pragma unroll
         for (int i = 0; i < kH; ++i) {
+            if (!mine(i)) continue;
 #pragma unroll
             for (int off = 16; off > 0; off >>= 1) l[i] += __shfl_xor_sync(0xffffffffu, l[i], off);
             if (lane == 0) s_sum[quad * kN + kC0 + i] = l[i];
         }
         workers_sync();
-        if (key < kH) {
+        if (key < n_cols) {
             const int row = kC0 + key;
-            const float sum = s_sum[row] + s_sum[kN + row] + s_sum[2 * kN + row] + s_sum[3 * kN + row];
+            float sum = 0.f;
+            for (int k = 0; k < 4; ++k) sum += s_sum[k * kN + row] + s_faint[k * kN + row];
             s_inv[row] = sum > 0.f ? (p.v_head ? __ldcg(p.v_head + cur.h) : 1.f) / sum : sum == 0.f ? 0.f : sum;
             if (!whole && row < p.n_rows) p.part_ml[(size_t)out_slot * p.n_rows + row] = make_float2(s_m[row], sum);
         }
-        tc_wait(&bars.o_done[b2], ph, dead, p.status);
+        tc_wait(&bars.o_done, ph, dead, p.status);
         tc_fence_after();
         workers_sync();   // (s_inv)
 #pragma unroll 1
-        for (int i = 0; i < kH; i += 8) {
+        for (int i = 0; i < n_cols; i += 8) {
             float o[8];
             tc_ld8(tmem + lanes + F::kColO + kC0 + i, o);
             tc_wait_ld();
@@ -532,16 +578,17 @@ __device__ __forceinline__ void tc_worker(const PackedAttnParams& p, uint8_t* sm
         advance(cur, s_len, nb, p.Hkv, kTcTile);
         workers_sync();   // (the columns' words are free)
     }
+    cp_async_wait<0>();
 }
 
 template <int kN>
-__global__ void __launch_bounds__(kTcThreads, 1) packed_attention_tc_kernel(const PackedAttnParams p) {
+__global__ void __launch_bounds__(kTcThreads, TcForm<kN>::kMinBlocks) packed_attention_tc_kernel(const PackedAttnParams p) {
     using F = TcForm<kN>;
     extern __shared__ uint4 smem_raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     __shared__ TcBars bars;
     __shared__ long long s_wsum[kTcThreads / 32];
-    __shared__ alignas(16) int s_info[8];      // [2] whether a tile's product starts O; then U and the CTAs
+    __shared__ alignas(16) int s_info[8];      // [2], [3] U; [4] the CTAs
     __shared__ uint32_t s_tmem;
     __shared__ volatile int s_dead;
     __shared__ int s_draft[kN];
@@ -551,12 +598,10 @@ __global__ void __launch_bounds__(kTcThreads, 1) packed_attention_tc_kernel(cons
     const int nb = p.n_batch;
     if (threadIdx.x == 0) {
         s_dead = 0;
-        for (int i = 0; i < 2; ++i) {
-            mbar_init(&bars.k_full[i], 8);
-            mbar_init(&bars.s_full[i], 1);
-            mbar_init(&bars.p_full[i], 16);
-            mbar_init(&bars.o_done[i], 1);
-        }
+        mbar_init(&bars.k_full, 4);
+        mbar_init(&bars.s_full, 1);
+        mbar_init(&bars.p_full, 8);
+        mbar_init(&bars.o_done, 1);
         mbar_init(&bars.f_done, 1);
         fence_barrier_init();
     }
@@ -583,8 +628,10 @@ __global__ void __launch_bounds__(kTcThreads, 1) packed_attention_tc_kernel(cons
         *reinterpret_cast<long long*>(s_info + 2) = U;
         s_info[4] = Gc;
     }
-    if (warp == 16) {
-        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(&s_tmem)) : "memory");
+    if (warp == 0) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&s_tmem)),
+                     "n"(F::kCols)
+                     : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
     tc_fence_before();
@@ -592,62 +639,13 @@ __global__ void __launch_bounds__(kTcThreads, 1) packed_attention_tc_kernel(cons
     tc_fence_after();
     const uint32_t tmem = s_tmem;
 
-    const int group = warp >> 2;
-    if (group < 2) {
-        tc_worker<kN, F::kH0>(p, smem, bars, tmem, &s_dead, s_info, s_len, share.first, n_tiles, s_draft, group * F::kH0);
-    } else if (group < 4) {
-        tc_worker<kN, F::kH1>(p, smem, bars, tmem, &s_dead, s_info, s_len, share.first, n_tiles, s_draft,
-                              2 * F::kH0 + (group - 2) * F::kH1);
-    } else {
-        // ---- the MMAs: S of tile j as soon as its K is there, O of tile j - 1
-        // after it -- or before it where tile j opens a piece, whose query rows
-        // wait for the end of the one before.  (Each wait names the phase that
-        // follows the last one this warp has seen of its barrier.)
-        const uint64_t dq = tc_desc(smem_u32(smem + F::kOffQ), 1024, 0);
-        constexpr uint32_t id_s = tc_idesc(kN, false, false);
-        uint64_t* open = nullptr;     // the latest commit
-        uint32_t open_ph = 0;
-        auto scores = [&](int j) {
-            tc_wait(&bars.k_full[j & 1], (uint32_t)(j >> 1) & 1, &s_dead, p.status);
-            tc_fence_after();
-            __syncwarp();
-            if (alive(&s_dead) && elect_one()) {
-#pragma unroll
-                for (int ks = 0; ks < kPackDim / 16; ++ks)
-                    tc_mma_ts(tmem + F::kColS + (j & 1) * kN, tmem + (j & 1) * 64 + ks * 8,
-                              dq + (uint64_t)((ks >> 2) * (F::kQHalf >> 4) + (ks & 3) * 2), id_s, ks > 0 ? 1u : 0u);
-                tc_commit(&bars.s_full[j & 1]);
-            }
-            __syncwarp();
-            open = &bars.s_full[j & 1];
-            open_ph = (uint32_t)(j >> 1) & 1;
-        };
-        auto sums = [&](int j) {
-            tc_wait(&bars.p_full[j & 1], (uint32_t)(j >> 1) & 1, &s_dead, p.status);
-            tc_fence_after();
-            const int info = *reinterpret_cast<volatile int*>(s_info + (j & 1));
-            __syncwarp();
-            if (alive(&s_dead) && elect_one()) {
-                tc_mma_values<kN>(tmem + F::kColO, smem, j, !(info & 1));
-                tc_commit(&bars.o_done[j & 1]);
-            }
-            __syncwarp();
-            open = &bars.o_done[j & 1];
-            open_ph = (uint32_t)(j >> 1) & 1;
-        };
-        Cursor cur = share.first;
-        for (int j = 0; j < n_tiles; ++j) {
-            if (j > 0) advance(cur, s_len, nb, p.Hkv, kTcTile);
-            if (j > 0 && cur.t == 0) sums(j - 1);
-            scores(j);
-            if (j > 0 && cur.t != 0) sums(j - 1);
-        }
-        sums(n_tiles - 1);
-        // every MMA completes before the tensor memory is given back
-        if (!mbar_wait_bounded(open, open_ph) && (threadIdx.x & 31) == 0) atomicOr(p.status, CS_DEVICE_WAIT_TIMEOUT);
-    }
+    tc_worker<kN>(p, smem, bars, tmem, &s_dead, s_info, s_len, share.first, n_tiles, s_draft);
+    // every MMA completes before the tensor memory is given back
+    if (warp == 0 && !mbar_wait_bounded(&bars.o_done, (uint32_t)(n_tiles - 1) & 1) && threadIdx.x == 0)
+        atomicOr(p.status, CS_DEVICE_WAIT_TIMEOUT);
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    if (warp == 16) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
+    if (warp == 0)
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(F::kCols) : "memory");
 }
