@@ -19,10 +19,9 @@
 // O: each would wait for it next.
 //
 // As in the other form P = 2^(s - m + 12), and the tile is taken the short way
-// unless some weight would leave [2^-14, 2^15] or some key is hidden from some
-// row (a vote of the workers).  Then (mend) the columns' maxima are found, O is
-// rescaled where one grows by more than 2^3, hidden scores become -inf where they
-// lie, and weights below 2^-14 (faint) are taken 28 powers of two at a time by
+// unless some weight would leave [2^-14, 2^15] (a vote of the workers).  Then
+// (mend) the columns' maxima are found, O is rescaled where one grows by more than
+// 2^3, and weights below 2^-14 (faint) are taken 28 powers of two at a time by
 // products of their own, which the workers add to O.  Mending is rolled up, for
 // the instruction cache's sake.
 //
@@ -34,7 +33,7 @@ constexpr int kTcThreads = 256;
 constexpr int kTcTile = 128;                       // keys of a tile: the MMAs' M (S) and K (O)
 constexpr int kTcVBytes = kTcTile * 256;           // V of a tile in fp16
 constexpr int kTcRawBytes = 2 * kTcTile * kPackCodeBytes;   // codes of K and V of a tile
-constexpr int kTcMinRows = 17, kTcMaxRows = 80;    // query rows that it takes
+constexpr int kTcMinRows = 33, kTcMaxRows = 80;    // query rows that it takes
 
 template <int kN>
 struct TcForm {
@@ -332,7 +331,10 @@ __device__ __forceinline__ void tc_worker(const PackedAttnParams& p, uint8_t* sm
         tc_fence_after();
         const uint32_t s_at = tmem + lanes + F::kColS + kC0, o_at = tmem + lanes + F::kColO + kC0;
         const int key0 = cur.t * kTcTile;
+        // the columns that do not see this thread's key: all past the context, else those
+        // of the drafts before it (columns are drafts in order, G query heads each)
         const bool edge = key0 + kTcTile > L - p.R + 1;
+        const int hidden = !edge ? 0 : key0 + key >= L ? kN : (key0 + key - (L - p.R)) * p.G;
         bool starts = first;   // whether the tile's product starts O
         // what a tile needs before it can go the short way
         auto mend = [&]() {
@@ -344,14 +346,10 @@ __device__ __forceinline__ void tc_worker(const PackedAttnParams& p, uint8_t* sm
 #pragma unroll
                 for (int k = 0; k < 8; ++k) {
                     const int row = kC0 + i + k;
-                    const int end = row < p.n_rows ? L - p.R + s_draft[row] : L - 1;
-                    if (key0 + key > end) z[k] = kNegInf;
-                    const int top = __reduce_max_sync(0xffffffffu, ordered(z[k] * s_sc[row]));
+                    const int top = __reduce_max_sync(0xffffffffu, ordered(row < hidden ? kNegInf : z[k] * s_sc[row]));
                     if (lane == 0) s_red[quad * kN + row] = top;
                 }
-                if (edge) tc_st8(s_at + i, reinterpret_cast<const uint32_t*>(z));
             }
-            tc_wait_st();
             workers_sync();
             bool grew = false;
             if (key < n_cols) {
@@ -388,7 +386,8 @@ __device__ __forceinline__ void tc_worker(const PackedAttnParams& p, uint8_t* sm
                 tc_ld8(s_at + i, z);
                 tc_wait_ld();
 #pragma unroll
-                for (int k = 0; k < 8; ++k) faint |= is_faint(fmaf(z[k], s_sc[kC0 + i + k], s_up[kC0 + i + k]));
+                for (int k = 0; k < 8; ++k)
+                    faint |= kC0 + i + k >= hidden && is_faint(fmaf(z[k], s_sc[kC0 + i + k], s_up[kC0 + i + k]));
             }
             faint = workers_any(faint);
             if ((rescale || faint) && j > 0) {
@@ -419,9 +418,9 @@ __device__ __forceinline__ void tc_worker(const PackedAttnParams& p, uint8_t* sm
                     for (int k = 0; k < 8; ++k) {
                         const int row = kC0 + i + k;
                         const float x = fmaf(z[k], s_sc[row], s_up[row]);
-                        const bool now = x < kPMin && x + up >= kPMin;
+                        const bool seen = row >= hidden, now = seen && x < kPMin && x + up >= kPMin;
                         f[k] = now ? ex2(x + up) : 0.f;
-                        more |= !now && is_faint(x);
+                        more |= seen && !now && is_faint(x);
                         if (now) z[k] = kNegInf;
                         float sum = now ? ex2(x) : 0.f;
 #pragma unroll
@@ -488,19 +487,25 @@ __device__ __forceinline__ void tc_worker(const PackedAttnParams& p, uint8_t* sm
             if (!mine(i)) continue;
             float x[8];
             scores(i, x);
+            if (edge)
+#pragma unroll
+                for (int k = 0; k < 8; ++k) x[k] = kC0 + i + k < hidden ? 0.f : x[k];
 #pragma unroll
             for (int k = 0; k < 8; k += 2) {
                 most = fmax3(most, x[k], x[k + 1]);
                 least = fmin3(least, x[k], x[k + 1]);
             }
         }
-        if (workers_any(most > kPMax || least < kPMin || edge)) mend();
+        if (workers_any(most > kPMax || least < kPMin)) mend();
         if (!v_side && j > 0) tc_wait(&bars.o_done, ph ^ 1, dead, p.status);   // P is free
 #pragma unroll
         for (int i = 0; i < kH; i += 8) {
             if (!mine(i)) continue;
             float x[8];
             scores(i, x);
+            if (edge)
+#pragma unroll
+                for (int k = 0; k < 8; ++k) x[k] = kC0 + i + k < hidden ? kNegInf : x[k];
 #pragma unroll
             for (int k = 0; k < 8; ++k) x[k] = ex2(x[k]);
             store_p(kC0 + i, pack_f16x2(x[0], x[1]), pack_f16x2(x[2], x[3]), pack_f16x2(x[4], x[5]), pack_f16x2(x[6], x[7]));
@@ -548,6 +553,9 @@ __device__ __forceinline__ void tc_worker(const PackedAttnParams& p, uint8_t* sm
         tc_wait(&bars.o_done, ph, dead, p.status);
         tc_fence_after();
         workers_sync();   // (s_inv)
+        // row (i, g) of the span lies i Hq + g rows past its first one
+        __nv_bfloat16* const dst = p.out + ((size_t)bg * p.R * p.Hq + (size_t)cur.h * p.G) * kPackDim + key;
+        float* const part = p.part_o + (size_t)out_slot * p.n_rows * kPackDim + key;
 #pragma unroll 1
         for (int i = 0; i < n_cols; i += 8) {
             float o[8];
@@ -558,12 +566,8 @@ __device__ __forceinline__ void tc_worker(const PackedAttnParams& p, uint8_t* sm
                 const int row = kC0 + i + k;
                 if (row >= p.n_rows) continue;
                 const float v = o[k] * s_inv[row];
-                const int d = s_draft[row];
-                if (whole)
-                    p.out[(((size_t)bg * p.R + d) * p.Hq + (size_t)cur.h * p.G + (row - d * p.G)) * kPackDim + key] =
-                        __float2bfloat16(v);
-                else
-                    p.part_o[((size_t)out_slot * p.n_rows + row) * kPackDim + key] = v;
+                if (whole) dst[(s_draft[row] * (p.Hq - p.G) + row) * kPackDim] = __float2bfloat16(v);
+                else part[row * kPackDim] = v;
             }
         }
         if (threadIdx.x == 0 && !whole && piece_t0 == 0) {
