@@ -127,16 +127,33 @@ __device__ __forceinline__ int ordered(float x) {
 }
 __device__ __forceinline__ float unordered(int b) { return __int_as_float(b < 0 ? b ^ 0x7fffffff : b); }
 
-// Bounded; returns at once when another wait has given up.  (Out of line: the loop's code is long.)
+// Waits for the phase of the given parity, asleep for up to 20 us.
+__device__ __forceinline__ bool tc_asleep(uint64_t* bar, uint32_t parity) {
+    uint32_t done;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, 20000;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}\n"
+        : "=r"(done)
+        : "r"(smem_u32(bar)), "r"(parity)
+        : "memory");
+    return done != 0;
+}
+// Bounded (about one second); returns at once when another wait has given up.
+// (Out of line: the loop's code is long.)
 __device__ __noinline__ void tc_wait_long(uint64_t* bar, uint32_t parity, volatile int* dead, int* status) {
-    if (*dead || mbar_wait_bounded(bar, parity)) return;
-    *dead = 1;
-    atomicOr(status, CS_DEVICE_WAIT_TIMEOUT);
+    const uint64_t t0 = global_timer_ns();
+    while (!*dead) {
+        if (tc_asleep(bar, parity)) return;
+        if (global_timer_ns() - t0 > 1000000000ull) {
+            *dead = 1;
+            atomicOr(status, CS_DEVICE_WAIT_TIMEOUT);
+        }
+    }
 }
 __device__ __forceinline__ void tc_wait(uint64_t* bar, uint32_t parity, volatile int* dead, int* status) {
-    if (!mbar_test_wait(bar, parity)) tc_wait_long(bar, parity, dead, status);
+    if (!tc_asleep(bar, parity)) tc_wait_long(bar, parity, dead, status);
 }
-
 // Whether no wait has given up, the same answer in the whole warp.
 __device__ __forceinline__ bool alive(volatile int* dead) { return !__any_sync(0xffffffffu, *dead); }
 
