@@ -52,6 +52,17 @@ __device__ __forceinline__ float f16_hi(uint32_t w) {
     return f;
 }
 
+__device__ __forceinline__ float fmax3(float a, float b, float c) {
+    float d;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    return d;
+}
+__device__ __forceinline__ float fmin3(float a, float b, float c) {
+    float d;
+    asm("min.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    return d;
+}
+
 // The e4m3 byte nearest to 0 <= x (ties to even, at most 448).
 __device__ __forceinline__ uint32_t to_e4m3(float x) {
     uint16_t r;

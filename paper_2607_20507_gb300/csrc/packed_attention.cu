@@ -431,13 +431,13 @@ packed_attention_kernel(const PackedAttnParams p) {
 #pragma unroll
             for (int nt = 0; nt < kNT; ++nt)
 #pragma unroll
-                for (int e = 0; e < 4; ++e)
-#pragma unroll
-                    for (int hf = 0; hf < kHalves; ++hf) {
-                        const float v = fmaf(s[hf][nt][e], sc_f[nt][e & 1], kPUp - m[nt][e & 1]);
-                        top = fmaxf(top, v);
-                        low = fminf(low, v);
-                    }
+                for (int e = 0; e < 4; ++e) {
+                    static_assert(kHalves == 2, "");
+                    const float up = kPUp - m[nt][e & 1];
+                    const float v0 = fmaf(s[0][nt][e], sc_f[nt][e & 1], up), v1 = fmaf(s[1][nt][e], sc_f[nt][e & 1], up);
+                    top = fmax3(top, v0, v1);
+                    low = fmin3(low, v0, v1);
+                }
             const bool edge = key0 + kSub > L - p.R + 1;   // some row does not see some key
             const bool ready = __any_sync(0xffffffffu, top > kPMax || low < kPMin || edge);
             if (ready) {

@@ -97,16 +97,6 @@ __host__ __device__ constexpr uint32_t tc_idesc(int n, bool a_mn, bool b_mn) {
     return (1u << 4) | (a_mn ? 1u << 15 : 0u) | (b_mn ? 1u << 16 : 0u) | ((uint32_t)(n >> 3) << 17) | (8u << 24);
 }
 
-__device__ __forceinline__ float fmax3(float a, float b, float c) {
-    float d;
-    asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
-    return d;
-}
-__device__ __forceinline__ float fmin3(float a, float b, float c) {
-    float d;
-    asm("min.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
-    return d;
-}
 // Whether any of the workers' threads says so; a barrier of theirs.
 __device__ __forceinline__ bool workers_any(bool x) {
     uint32_t r;
