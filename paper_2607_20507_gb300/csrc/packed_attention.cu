@@ -2,17 +2,20 @@
 // (cs_packed_verify_attention): o = softmax_j(scale q . K_j) V_j with K and V
 // the values that the codes stand for (packed.cuh).
 //
-// Work split.  A span is one (request, KV head); its keys go in tiles of
-// kTeams x 16.  The grid holds the CTAs that are resident at once, and each
-// takes an equal share of all tiles (a span's start counts as `span_x` more).
-// A span that lies in one CTA is written there; one that is cut leaves each
-// piece's normalised output and (maximum, sum), which packed_merge_kernel joins.
+// Up to 32 query rows per KV head take the form below, more the tcgen05 form
+// (packed_attention_tc.cuh).
 //
-// Per CTA: teams of kRG warps, each with a ring of kStages tiles of 16 keys in
-// shared memory, filled by cp.async (a page piece of 16 keys is 1 KB of codes
-// and 128 bytes of scales for K and for V: too little for a bulk copy each).
-// A warp holds up to 8 kNT query rows; kRG warps share a tile where there are
-// more.
+// Work split.  A span is one (request, KV head) -- with more than 80 query rows
+// one of two blocks of them; its keys go in tiles of 128.  The grid holds the
+// CTAs that are resident at once, and each takes an equal share of all tiles (a
+// span's start counts as `span_x` more).  A span that lies in one CTA is written
+// there; one that is cut leaves each piece's normalised output and (maximum,
+// sum), which packed_merge_kernel joins.
+//
+// Per CTA: four warps, each with a quarter of a tile's keys and a ring of its
+// own in shared memory for them, filled by cp.async (a page piece of 16 keys is
+// 1 KB of codes and 128 bytes of scales for K and for V: too little for a bulk
+// copy each).  A warp holds all query rows, 8 kNT of them.
 //
 // Per warp and tile, transposed products on mma.sync (m16n8k16, fp16 operands,
 // fp32 sums), so that the padding is to 8 query rows and not to 16:
@@ -43,7 +46,7 @@
 namespace cs {
 namespace {
 
-constexpr int kSub = 32;                            // keys of a team's tile
+constexpr int kSub = 32;                            // keys of a warp's tile
 constexpr int kHalves = kSub / 16;                  // MMA tiles of 16 keys in it
 constexpr int kStages = 2;
 constexpr int kCodes = kSub * kPackCodeBytes;       // 2048 bytes of codes of K or V
@@ -75,22 +78,24 @@ struct PackedAttnParams {
     float2* part_ml;             // [2 grid, n_rows] (maximum in log2 units, sum)
     Job* jobs;                   // [grid]
     int* status;                 // device status word
-    int Hq, Hkv, G, R, n_rows, ps, ps_log2, max_pages, P;
+    int Hq, Hkv, G, R, ps, ps_log2, max_pages, P;
+    int n_rows, n_all;           // query rows of a span, and of a KV head
+    int n_rb, n_spans;           // row blocks of a KV head, spans of a request (Hkv n_rb)
     int b_base, n_batch, span_x;
     float scale_log2;            // sm_scale * log2(e)
 };
 
 // warps that share a tile's keys by query rows, and what follows from the count
-template <int kNT, int kRG>
+template <int kNT>
 struct Form {
-    static constexpr int kTeams = kRG <= 2 ? 4 : 2;
-    static constexpr int kThreads = kTeams * kRG * 32;
-    static constexpr int kTile = kTeams * kSub;
-    static constexpr int kRows = kRG * kNT * 8;
-    static constexpr int kMinBlocks = kRG == 1 ? (kNT == 1 ? 4 : kNT == 2 ? 3 : 2) : kRG == 3 ? 2 : 1;
-    static constexpr int kRing = kTeams * kStages * kStageBytes;
+    static constexpr int kWarps = 4;
+    static constexpr int kThreads = kWarps * 32;
+    static constexpr int kTile = kWarps * kSub;
+    static constexpr int kRows = kNT * 8;
+    static constexpr int kMinBlocks = kNT == 1 ? 4 : kNT == 2 ? 3 : 2;
+    static constexpr int kRing = kWarps * kStages * kStageBytes;
     static constexpr int kQ = kRows * kPackDim * 2;
-    static constexpr int kFold = kTeams / 2 * kRows * kPackDim * 4 + kTeams / 2 * kRG * kNT * 32 * 16;
+    static constexpr int kFold = kWarps / 2 * (kRows * kPackDim * 4 + kNT * 32 * 16);
     static constexpr int kSmem = kRing + kQ + kFold + kRows * 8 + kMaxBatchPerLaunch * 4;
     static_assert(kRing >= (kMaxBatchPerLaunch + 1) * 8, "the prefix lies in the ring at the start");
 };
@@ -154,7 +159,7 @@ __device__ __forceinline__ int owner_of(long long v, long long U, int G) {
 // The share of CTA c of G, by one warp: even lanes place its first unit, odd
 // ones the unit past its last (lanes compare 32 requests' starts at a time).
 __device__ __forceinline__ Share share_of(int c, long long U, int G, const long long* prefix, const int* lens, int nb,
-                                          int Hkv, int X, int tile) {
+                                          int n_spans, int X, int tile) {
     const int lane = threadIdx.x & 31;
     const long long v = first_unit(c + (lane & 1), U, G);
     Cursor cur{};
@@ -169,10 +174,10 @@ __device__ __forceinline__ Share share_of(int c, long long U, int G, const long 
     }
     cur.T = tiles_of(lens[cur.b], tile);
     const long long local = v - prefix[cur.b];
-    cur.h = (int)div_pos(local, cur.T + X);     // Hkv: past the last unit
+    cur.h = (int)div_pos(local, cur.T + X);     // n_spans: past the last unit
     const int in = (int)(local - (long long)cur.h * (cur.T + X));
     cur.t = in > X ? in - X : 0;
-    const long long before = prefix[cur.b] - (long long)X * Hkv * cur.b + (long long)cur.h * cur.T + cur.t;
+    const long long before = prefix[cur.b] - (long long)X * n_spans * cur.b + (long long)cur.h * cur.T + cur.t;
     Share s;
     s.n_tiles = (int)(__shfl_sync(0xffffffffu, before, 1) - __shfl_sync(0xffffffffu, before, 0));
     s.first.b = __shfl_sync(0xffffffffu, cur.b, 0);
@@ -182,10 +187,10 @@ __device__ __forceinline__ Share share_of(int c, long long U, int G, const long 
     return s;
 }
 
-__device__ __forceinline__ void advance(Cursor& c, const int* lens, int nb, int Hkv, int tile) {
+__device__ __forceinline__ void advance(Cursor& c, const int* lens, int nb, int n_spans, int tile) {
     if (++c.t < c.T) return;
     c.t = 0;
-    if (++c.h < Hkv) return;
+    if (++c.h < n_spans) return;
     c.h = 0;
     if (++c.b < nb) c.T = tiles_of(lens[c.b], tile);
 }
@@ -203,7 +208,7 @@ __device__ __forceinline__ long long build_prefix(const PackedAttnParams& p, int
         if (b < p.n_batch) {
             const int L = max(0, min(__ldcg(p.ctx_lens + p.b_base + b), p.max_pages * p.ps));
             lens[b] = L;
-            v = (long long)tiles_of(L, tile) * p.Hkv;
+            v = (long long)tiles_of(L, tile) * p.n_spans;
         }
         long long inc = v;
 #pragma unroll
@@ -241,10 +246,10 @@ __device__ __forceinline__ uint2 query_f16(uint2 x, float& back) {
     return make_uint2(pack_f16x2(f[0] * s0 * s1, f[1] * s0 * s1), pack_f16x2(f[2] * s0 * s1, f[3] * s0 * s1));
 }
 
-template <int kNT, int kRG>
-__global__ void __launch_bounds__(Form<kNT, kRG>::kThreads, Form<kNT, kRG>::kMinBlocks)
+template <int kNT>
+__global__ void __launch_bounds__(Form<kNT>::kThreads, Form<kNT>::kMinBlocks)
 packed_attention_kernel(const PackedAttnParams p) {
-    using F = Form<kNT, kRG>;
+    using F = Form<kNT>;
     extern __shared__ uint4 smem_raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>(smem_raw);
     uint4* s_q = reinterpret_cast<uint4*>(smem + F::kRing);                       // [row tile][4][lane] B fragments
@@ -256,7 +261,6 @@ packed_attention_kernel(const PackedAttnParams p) {
     __shared__ long long s_wsum[F::kThreads / 32];
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int team = warp / kRG, rg = warp % kRG;
     const int r = lane >> 2, c = lane & 3;
     const int nb = p.n_batch, X0 = p.span_x;
     wait_prior_grid();
@@ -273,11 +277,11 @@ packed_attention_kernel(const PackedAttnParams p) {
     }
     if (cta >= Gc) return;
     if (X > 0) {
-        for (int b = threadIdx.x; b < nb; b += F::kThreads) s_prefix[b] += (long long)X * p.Hkv * b;
+        for (int b = threadIdx.x; b < nb; b += F::kThreads) s_prefix[b] += (long long)X * p.n_spans * b;
         __syncthreads();
     }
-    const long long U = W + (long long)X * p.Hkv * nb;
-    const Share share = share_of(cta, U, Gc, s_prefix, s_len, nb, p.Hkv, X, F::kTile);
+    const long long U = W + (long long)X * p.n_spans * nb;
+    const Share share = share_of(cta, U, Gc, s_prefix, s_len, nb, p.n_spans, X, F::kTile);
     const int n_tiles = share.n_tiles;
     __syncthreads();   // the prefix gives way to the ring
     if (n_tiles <= 0) return;
@@ -285,9 +289,8 @@ packed_attention_kernel(const PackedAttnParams p) {
 
     // ---- the ring.  Lane g (mod 4) looks up the page of keys 8 g .. 8 g + 7 of
     // the next tile to load, one tile ahead.
-    uint8_t* ring = smem + team * (kStages * kStageBytes);
+    uint8_t* ring = smem + warp * (kStages * kStageBytes);
     const uint32_t ring_a = smem_u32(ring);
-    constexpr int kLoaders = kRG == 1 ? 1 : 2;
     const int page_rows = p.Hkv * p.ps;
     Cursor cn = share.first;
     int left = n_tiles, stage_in = 0;                 // tiles not looked up yet, the stage that is filled next
@@ -297,12 +300,12 @@ packed_attention_kernel(const PackedAttnParams p) {
         pending = left > 0;
         if (!pending) return;
         --left;
-        const int key = cn.t * F::kTile + team * kSub + 8 * c;
+        const int key = cn.t * F::kTile + warp * kSub + 8 * c;
         next_page = -1;
         next_row = cn.h * p.ps + (key & (p.ps - 1));
         if (key < s_len[cn.b])
             next_page = __ldcg(p.page_table + (size_t)(p.b_base + cn.b) * p.max_pages + (key >> p.ps_log2));
-        advance(cn, s_len, nb, p.Hkv, F::kTile);
+        advance(cn, s_len, nb, p.n_spans, F::kTile);
     };
     const uint8_t* k_lane = p.k_codes + r * kPackCodeBytes + c * 16;
     const uint8_t* v_lane = p.v_codes + r * kPackCodeBytes + c * 16;
@@ -310,7 +313,7 @@ packed_attention_kernel(const PackedAttnParams p) {
     const uint32_t k_to = ring_a + r * kPackCodeBytes + c * 16, v_to = ring_a + kCodes + v_at(r, c);
     const uint32_t s_to = ring_a + 2 * kCodes + lane * 16;
     auto issue = [&]() {
-        if (rg < kLoaders && pending) {
+        if (pending) {
             const bool in = next_page >= 0 && next_page < p.P;
             const int row = in ? next_page * page_rows + next_row : -1;
             const uint32_t st = stage_in * kStageBytes;
@@ -318,22 +321,17 @@ packed_attention_kernel(const PackedAttnParams p) {
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
                 const int rw = __shfl_sync(0xffffffffu, row, g);
-                if (kLoaders == 2 && g / 2 != rg) continue;
                 const size_t at = (size_t)max(rw, 0) * kPackCodeBytes;
                 cp_async16(k_to + st + g * 8 * kPackCodeBytes, k_lane + at, rw >= 0);
                 cp_async16(v_to + st + g * 8 * kPackCodeBytes, v_lane + at, rw >= 0);
             }
             const int rw = __shfl_sync(0xffffffffu, row, lane >> 2 & 3);
-            if (rg == 0) cp_async16(s_to + st, s_lane + (size_t)max(rw, 0) * kPackGroups, rw >= 0);
+            cp_async16(s_to + st, s_lane + (size_t)max(rw, 0) * kPackGroups, rw >= 0);
         }
         stage_in = stage_in + 1 == kStages ? 0 : stage_in + 1;
         cp_async_commit();
     };
-    auto team_sync = [&]() {
-        if constexpr (kRG == 1) __syncwarp();
-        else asm volatile("bar.sync %0, %1;" ::"r"(1 + team), "n"(kRG * 32) : "memory");
-    };
-    if (rg < kLoaders) look_up();
+    look_up();
     for (int i = 0; i < kStages - 1; ++i) issue();
     int stage = 0;
 
@@ -369,14 +367,14 @@ packed_attention_kernel(const PackedAttnParams p) {
             for (int e = 0; e < 2; ++e) {
                 m[nt][e] = kNegInf;
                 l[nt][e] = 0.f;
-                sc_f[nt][e] = s_scale[(rg * kNT + nt) * 8 + 2 * c + e];
+                sc_f[nt][e] = s_scale[nt * 8 + 2 * c + e];
             }
 #pragma unroll
             for (int i = 0; i < 8; ++i)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) o[nt][i][e] = 0.f;
         }
-        const uint4* q_frag = s_q + rg * kNT * 4 * 32 + lane;
+        const uint4* q_frag = s_q + lane;
         uint4 q_kept[4];   // one row tile's fragments stay in registers
         if constexpr (kNT == 1)
 #pragma unroll
@@ -384,11 +382,11 @@ packed_attention_kernel(const PackedAttnParams p) {
 
         for (int t = 0; t < n; ++t) {
             cp_async_wait<kStages - 2>();
-            team_sync();
+            __syncwarp();
             const uint8_t* st = ring + stage * kStageBytes;
             stage = stage + 1 == kStages ? 0 : stage + 1;
-            issue();   // into the stage that the team left before the barrier
-            const int key0 = (cur.t + t) * F::kTile + team * kSub;
+            issue();   // into the stage that the warp has left
+            const int key0 = (cur.t + t) * F::kTile + warp * kSub;
             if (key0 >= L) continue;
 
             // ---- S^T = K Q^T
@@ -446,7 +444,7 @@ packed_attention_kernel(const PackedAttnParams p) {
                 for (int nt = 0; nt < kNT; ++nt)
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
-                        const int row = (rg * kNT + nt) * 8 + 2 * c + e;
+                        const int row = nt * 8 + 2 * c + e;
                         const int last = !edge ? INT_MAX : row < p.n_rows ? L - p.R + s_draft[row] : L - 1;
                         float now = kNegInf;
 #pragma unroll
@@ -581,19 +579,19 @@ packed_attention_kernel(const PackedAttnParams p) {
             }
         }
 
-        // ---- the teams' states become one (team 0's)
+        // ---- the warps' states become one (warp 0's)
 #pragma unroll
         for (int nt = 0; nt < kNT; ++nt)
 #pragma unroll
             for (int e = 0; e < 2; ++e)
 #pragma unroll
                 for (int off = 4; off < 32; off <<= 1) l[nt][e] += __shfl_xor_sync(0xffffffffu, l[nt][e], off);
-        float4* s_ml = s_fold + F::kTeams / 2 * kRG * kNT * 8 * 32;
+        float4* s_ml = s_fold + F::kWarps / 2 * kNT * 8 * 32;
 #pragma unroll
-        for (int half = F::kTeams / 2; half > 0; half >>= 1) {
+        for (int half = F::kWarps / 2; half > 0; half >>= 1) {
             __syncthreads();
-            const int at = (team % half) * kRG + rg;
-            if (team >= half && team < 2 * half) {
+            const int at = warp % half;
+            if (warp >= half && warp < 2 * half) {
 #pragma unroll
                 for (int nt = 0; nt < kNT; ++nt) {
 #pragma unroll
@@ -604,7 +602,7 @@ packed_attention_kernel(const PackedAttnParams p) {
                 }
             }
             __syncthreads();
-            if (team < half) {
+            if (warp < half) {
 #pragma unroll
                 for (int nt = 0; nt < kNT; ++nt) {
                     const float4 ml = s_ml[(at * kNT + nt) * 32 + lane];
@@ -630,14 +628,14 @@ packed_attention_kernel(const PackedAttnParams p) {
             }
         }
         const bool whole = n == cur.T;
-        if (team == 0) {
+        if (warp == 0) {
             const float vh = p.v_head ? __ldcg(p.v_head + cur.h) : 1.f;
             const int slot = 2 * cta + (first_piece ? 0 : 1);
 #pragma unroll
             for (int nt = 0; nt < kNT; ++nt)
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    const int row = (rg * kNT + nt) * 8 + 2 * c + e;
+                    const int row = nt * 8 + 2 * c + e;
                     if (row >= p.n_rows) continue;
                     const float inv = l[nt][e] > 0.f ? vh / l[nt][e] : l[nt][e] == 0.f ? 0.f : l[nt][e];   // (NaN stays)
                     if (whole) {
@@ -667,7 +665,7 @@ packed_attention_kernel(const PackedAttnParams p) {
         }
         done += n;
         cur.t += n - 1;
-        advance(cur, s_len, nb, p.Hkv, F::kTile);
+        advance(cur, s_len, nb, p.n_spans, F::kTile);
         first_piece = false;
         __syncthreads();   // the query rows and the fold's room are free again
     }
@@ -729,9 +727,10 @@ __global__ void __launch_bounds__(kMergeThreads) packed_merge_kernel(const Packe
             }
         }
         const float inv = sum > 0.f ? 1.f / sum : sum == 0.f ? 0.f : sum;
-        const int i = row / p.G;
+        const int head = job.h / p.n_rb, of = (job.h - head * p.n_rb) * p.n_rows + row, i = of / p.G;
+        if (of >= p.n_all) continue;
         uint2* dst = reinterpret_cast<uint2*>(
-            p.out + (((size_t)job.b * p.R + i) * p.Hq + (size_t)job.h * p.G + (row - i * p.G)) * kPackDim + 4 * lane);
+            p.out + (((size_t)job.b * p.R + i) * p.Hq + (size_t)head * p.G + (of - i * p.G)) * kPackDim + 4 * lane);
         *dst = make_uint2(pack_bf16x2(acc.x * inv, acc.y * inv), pack_bf16x2(acc.z * inv, acc.w * inv));
     }
 }
@@ -744,26 +743,26 @@ struct Choice {
     int threads, smem;
     int blocks;   // of an SM, where the occupancy query is not asked; 0: it is
 };
-template <int kNT, int kRG>
+template <int kNT>
 Choice choice() {
-    return {packed_attention_kernel<kNT, kRG>, Form<kNT, kRG>::kThreads, Form<kNT, kRG>::kSmem, 0};
+    return {packed_attention_kernel<kNT>, Form<kNT>::kThreads, Form<kNT>::kSmem, 0};
 }
 template <int kN>
 Choice choice_tc() {
     return {packed_attention_tc_kernel<kN>, kTcThreads, TcForm<kN>::kSmem, TcForm<kN>::kMinBlocks};
 }
-constexpr int kSyncForms = 9, kForms = kSyncForms + 4;
+constexpr int kForms = 7;
 
-// The form for a number of query rows; tc: whether the tcgen05 form may be chosen.
-int form_of(int rows, bool tc) {
-    if (tc && rows >= kTcMinRows && rows <= kTcMaxRows) return kSyncForms + (rows + 15) / 16 - 2;
-    const int nt = (rows + 7) / 8;
-    return nt <= 4 ? nt - 1 : 2 + (nt + 2) / 3;   // 4: two warps of three tiles, ... 8: six
+// The form for a number of query rows of a span: up to 32 the one above (32 rows, 64
+// requests of 4096 keys, 8 KV heads: 172 us; 36 rows in the tcgen05 form 189, and
+// 20 rows 82 against 104 in it at 2048 keys), from 33 on the tcgen05 form (36 rows
+// in the other one 200, 72 rows 269 against 152 at 32 requests).
+int form_of(int rows) {
+    return rows <= 32 ? (rows + 7) / 8 - 1 : rows <= 48 ? 4 : rows <= 64 ? 5 : 6;
 }
 Choice choice_of(int form) {
-    static const Choice all[kForms] = {choice<1, 1>(), choice<2, 1>(), choice<3, 1>(), choice<4, 1>(), choice<3, 2>(),
-                                       choice<3, 3>(), choice<3, 4>(), choice<3, 5>(), choice<3, 6>(),
-                                       choice_tc<32>(), choice_tc<48>(), choice_tc<64>(), choice_tc<80>()};
+    static const Choice all[kForms] = {choice<1>(), choice<2>(), choice<3>(), choice<4>(), choice_tc<48>(), choice_tc<64>(),
+                                       choice_tc<80>()};
     return all[form];
 }
 
@@ -794,13 +793,17 @@ int resident_of(int form) {
 
 // Workspace: the status word (256 B), the jobs, then the pieces' (maximum, sum) and outputs.
 struct PackedPlan {
-    int form, rows, grid;
+    int form, n_all, n_rb, rows, grid;
     size_t off_ml, off_o, bytes;
 };
-PackedPlan plan_packed(const cs_attn_dims& d, int rows, int sm_count, bool tc) {
+PackedPlan plan_packed(const cs_attn_dims& d, int rows, int sm_count) {
     PackedPlan pl{};
-    pl.rows = rows * (d.n_q_heads / d.n_kv_heads);
-    pl.form = form_of(pl.rows, tc);
+    pl.n_all = rows * (d.n_q_heads / d.n_kv_heads);
+    // more rows than the widest form's in blocks of equal size, each reading the keys
+    // again (136 rows in two blocks 519 us, in one block of the other form 870)
+    pl.n_rb = (pl.n_all + kTcMaxRows - 1) / kTcMaxRows;
+    pl.rows = (pl.n_all + pl.n_rb - 1) / pl.n_rb;
+    pl.form = form_of(pl.rows);
     const int res = resident_of(pl.form);
     pl.grid = sm_count * (res > 0 ? res : 1);
     if (pl.grid > kMaxGrid) pl.grid = kMaxGrid;
@@ -813,16 +816,13 @@ PackedPlan plan_packed(const cs_attn_dims& d, int rows, int sm_count, bool tc) {
 }  // namespace
 
 size_t packed_attention_workspace_bytes(const cs_attn_dims& d, int rows, int sm_count) {
-    const size_t a = plan_packed(d, rows, sm_count, true).bytes, b = plan_packed(d, rows, sm_count, false).bytes;
-    return a > b ? a : b;
+    return plan_packed(d, rows, sm_count).bytes;
 }
 
 cs_status launch_packed_attention(const cs_attn_dims& d, const void* q, const cs_packed_pool& pool,
                                   const int32_t* page_table, const int32_t* ctx_lens, int rows, void* out,
                                   void* workspace, cudaStream_t stream) {
-    // the tcgen05 form loads 32 bytes of codes at a time
-    const bool tc = ((reinterpret_cast<uintptr_t>(pool.k_codes) | reinterpret_cast<uintptr_t>(pool.v_codes)) & 31) == 0;
-    const PackedPlan pl = plan_packed(d, rows, current_sm_count(), tc);
+    const PackedPlan pl = plan_packed(d, rows, current_sm_count());
     uint8_t* ws = static_cast<uint8_t*>(workspace);
     PackedAttnParams p{};
     p.q = static_cast<const __nv_bfloat16*>(q);
@@ -844,6 +844,9 @@ cs_status launch_packed_attention(const cs_attn_dims& d, const void* q, const cs
     p.G = d.n_q_heads / d.n_kv_heads;
     p.R = rows;
     p.n_rows = pl.rows;
+    p.n_all = pl.n_all;
+    p.n_rb = pl.n_rb;
+    p.n_spans = d.n_kv_heads * pl.n_rb;
     p.ps = d.page_size;
     while ((1 << p.ps_log2) < d.page_size) ++p.ps_log2;
     p.max_pages = d.max_pages_per_seq;

@@ -1,5 +1,5 @@
-// packed_attention_tc.cuh -- the tcgen05 form of packed attention, for 17 to 80
-// query rows per KV head (included by packed_attention.cu inside its anonymous
+// packed_attention_tc.cuh -- the tcgen05 form of packed attention, for 33 to 80
+// query rows of a span (included by packed_attention.cu inside its anonymous
 // namespace: the same split of the keys, pieces and merge).
 //
 // Transposed products, so that the padding is to 16 query rows (N) and the keys
@@ -33,7 +33,7 @@ constexpr int kTcThreads = 256;
 constexpr int kTcTile = 128;                       // keys of a tile: the MMAs' M (S) and K (O)
 constexpr int kTcVBytes = kTcTile * 256;           // V of a tile in fp16
 constexpr int kTcRawBytes = 2 * kTcTile * kPackCodeBytes;   // codes of K and V of a tile
-constexpr int kTcMinRows = 33, kTcMaxRows = 80;    // query rows that it takes
+constexpr int kTcMaxRows = 80;                     // query rows of a span at most
 
 template <int kN>
 struct TcForm {
@@ -207,10 +207,10 @@ __device__ __forceinline__ void tc_worker(const PackedAttnParams& p, uint8_t* sm
         if (left <= 0) return;
         --left;
         const int pos = cl.t * kTcTile + key;
-        slot = cl.h * p.ps + (pos & (p.ps - 1));
+        slot = (p.n_rb == 1 ? cl.h : cl.h / p.n_rb) * p.ps + (pos & (p.ps - 1));
         if (pos < s_len[cl.b])
             page = __ldcg(p.page_table + (size_t)(p.b_base + cl.b) * p.max_pages + (pos >> p.ps_log2));
-        advance(cl, s_len, nb, p.Hkv, kTcTile);
+        advance(cl, s_len, nb, p.n_spans, kTcTile);
     };
     auto load_row = [&]() {      // zeros for a key past the context or on no page
         const bool in = page >= 0 && page < p.P;
@@ -266,6 +266,9 @@ __device__ __forceinline__ void tc_worker(const PackedAttnParams& p, uint8_t* sm
 #pragma unroll 1
     for (int j = 0; j < n_tiles; ++j) {
         const int L = s_len[cur.b], bg = p.b_base + cur.b;
+        // the KV head of the span, and its row block's first row
+        const int head = p.n_rb == 1 ? cur.h : cur.h / p.n_rb, row0 = (cur.h - head * p.n_rb) * p.n_rows;
+        const int n_live = min(p.n_rows, p.n_all - row0);
         const uint32_t ph = (uint32_t)j & 1;
         const bool first = j == 0 || cur.t == 0, last = j + 1 == n_tiles || cur.t + 1 == cur.T;
         if (first) {
@@ -275,15 +278,15 @@ __device__ __forceinline__ void tc_worker(const PackedAttnParams& p, uint8_t* sm
             for (int i = 0; i < kH; ++i) l[i] = 0.f;
             constexpr int kMine = kN / 8;   // rows of a warp, requested together
             uint2 x[kMine];
-            const float head = p.k_head ? __ldcg(p.k_head + cur.h) : 1.f;
+            const float scale = p.scale_log2 * (p.k_head ? __ldcg(p.k_head + head) : 1.f);
 #pragma unroll
             for (int k = 0; k < kMine; ++k) {
                 const int row = warp + 8 * k;
                 x[k] = make_uint2(0, 0);
-                if (row < p.n_rows) {
-                    const int i = s_draft[row];
+                if (row < n_live) {
+                    const int i = s_draft[row0 + row];
                     const uint32_t* src = reinterpret_cast<const uint32_t*>(
-                        p.q + (((size_t)bg * p.R + i) * p.Hq + (size_t)cur.h * p.G + (row - i * p.G)) * kPackDim + 4 * lane);
+                        p.q + (((size_t)bg * p.R + i) * p.Hq + (size_t)head * p.G + (row0 + row - i * p.G)) * kPackDim + 4 * lane);
                     x[k].x = __ldcg(src);
                     x[k].y = __ldcg(src + 1);
                 }
@@ -297,9 +300,9 @@ __device__ __forceinline__ void tc_worker(const PackedAttnParams& p, uint8_t* sm
                                           ((((lane & 15) >> 1) ^ (row & 7)) << 4) + (lane & 1) * 8) = y;
                 if (lane == 0) {
                     // (not 0, under which a hidden score would be NaN)
-                    s_sc[row] = row < p.n_rows ? fmaxf(p.scale_log2 * back * head, 0x1p-126f) : 0x1p-126f;
-                    s_up[row] = row < p.n_rows ? -kNegInf : 0.f;
-                    s_m[row] = row < p.n_rows ? kNegInf : kPUp;
+                    s_sc[row] = row < n_live ? fmaxf(scale * back, 0x1p-126f) : 0x1p-126f;
+                    s_up[row] = row < n_live ? -kNegInf : 0.f;
+                    s_m[row] = row < n_live ? kNegInf : kPUp;
                     for (int k4 = 0; k4 < 4; ++k4) s_faint[k4 * kN + row] = 0.f;
                 }
             }
@@ -341,7 +344,7 @@ __device__ __forceinline__ void tc_worker(const PackedAttnParams& p, uint8_t* sm
         // the columns that do not see this thread's key: all past the context, else those
         // of the drafts before it (columns are drafts in order, G query heads each)
         const bool edge = key0 + kTcTile > L - p.R + 1;
-        const int hidden = !edge ? 0 : key0 + key >= L ? kN : (key0 + key - (L - p.R)) * p.G;
+        const int hidden = !edge ? 0 : key0 + key >= L ? kN : (key0 + key - (L - p.R)) * p.G - row0;
         bool starts = first;   // whether the tile's product starts O
         // what a tile needs before it can go the short way
         auto mend = [&]() {
@@ -364,7 +367,7 @@ __device__ __forceinline__ void tc_worker(const PackedAttnParams& p, uint8_t* sm
                 const float now = unordered(max(max(s_red[row], s_red[kN + row]), max(s_red[2 * kN + row], s_red[3 * kN + row])));
                 const float m = s_m[row];
                 float a = 1.f;
-                if (row < p.n_rows && now - m > kPMax - kPUp) {   // (true for the first key: m is -inf)
+                if (row < n_live && now - m > kPMax - kPUp) {   // (true for the first key: m is -inf)
                     a = ex2(m - now);
                     s_m[row] = now;
                     s_up[row] = kPUp - now;
@@ -535,7 +538,7 @@ __device__ __forceinline__ void tc_worker(const PackedAttnParams& p, uint8_t* sm
             __syncwarp();
         }
         if (!last) {
-            advance(cur, s_len, nb, p.Hkv, kTcTile);
+            advance(cur, s_len, nb, p.n_spans, kTcTile);
             continue;
         }
         // ---- the end of a piece: sums over the keys, then a dim a thread
@@ -554,14 +557,14 @@ __device__ __forceinline__ void tc_worker(const PackedAttnParams& p, uint8_t* sm
             const int row = kC0 + key;
             float sum = 0.f;
             for (int k = 0; k < 4; ++k) sum += s_sum[k * kN + row] + s_faint[k * kN + row];
-            s_inv[row] = sum > 0.f ? (p.v_head ? __ldcg(p.v_head + cur.h) : 1.f) / sum : sum == 0.f ? 0.f : sum;
-            if (!whole && row < p.n_rows) p.part_ml[(size_t)out_slot * p.n_rows + row] = make_float2(s_m[row], sum);
+            s_inv[row] = sum > 0.f ? (p.v_head ? __ldcg(p.v_head + head) : 1.f) / sum : sum == 0.f ? 0.f : sum;
+            if (!whole && row < n_live) p.part_ml[(size_t)out_slot * p.n_rows + row] = make_float2(s_m[row], sum);
         }
         tc_wait(&bars.o_done, ph, dead, p.status);
         tc_fence_after();
         workers_sync();   // (s_inv)
         // row (i, g) of the span lies i Hq + g rows past its first one
-        __nv_bfloat16* const dst = p.out + ((size_t)bg * p.R * p.Hq + (size_t)cur.h * p.G) * kPackDim + key;
+        __nv_bfloat16* const dst = p.out + ((size_t)bg * p.R * p.Hq + (size_t)head * p.G + row0) * kPackDim + key;
         float* const part = p.part_o + (size_t)out_slot * p.n_rows * kPackDim + key;
 #pragma unroll 1
         for (int i = 0; i < n_cols; i += 8) {
@@ -571,9 +574,9 @@ __device__ __forceinline__ void tc_worker(const PackedAttnParams& p, uint8_t* sm
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
                 const int row = kC0 + i + k;
-                if (row >= p.n_rows) continue;
+                if (row >= n_live) continue;
                 const float v = o[k] * s_inv[row];
-                if (whole) dst[(s_draft[row] * (p.Hq - p.G) + row) * kPackDim] = __float2bfloat16(v);
+                if (whole) dst[(s_draft[row0 + row] * (p.Hq - p.G) + row) * kPackDim] = __float2bfloat16(v);
                 else part[row * kPackDim] = v;
             }
         }
@@ -586,7 +589,7 @@ __device__ __forceinline__ void tc_worker(const PackedAttnParams& p, uint8_t* sm
         }
         tc_fence_before();
         first_piece = false;
-        advance(cur, s_len, nb, p.Hkv, kTcTile);
+        advance(cur, s_len, nb, p.n_spans, kTcTile);
         workers_sync();   // (the columns' words are free)
     }
     cp_async_wait<0>();
@@ -602,7 +605,7 @@ __global__ void __launch_bounds__(kTcThreads, TcForm<kN>::kMinBlocks) packed_att
     __shared__ alignas(16) int s_info[8];      // [2], [3] U; [4] the CTAs
     __shared__ uint32_t s_tmem;
     __shared__ volatile int s_dead;
-    __shared__ int s_draft[kN];
+    __shared__ int s_draft[2 * kTcMaxRows];   // of the KV head's query rows
     int* s_len = reinterpret_cast<int*>(smem + F::kOffLen);
     long long* s_prefix = reinterpret_cast<long long*>(smem);
     const int warp = threadIdx.x >> 5, cta = blockIdx.x, grid = gridDim.x;
@@ -616,7 +619,7 @@ __global__ void __launch_bounds__(kTcThreads, TcForm<kN>::kMinBlocks) packed_att
         mbar_init(&bars.f_done, 1);
         fence_barrier_init();
     }
-    for (int row = threadIdx.x; row < kN; row += kTcThreads) s_draft[row] = row / p.G;
+    for (int row = threadIdx.x; row < 2 * kTcMaxRows; row += kTcThreads) s_draft[row] = row / p.G;
     wait_prior_grid();
     allow_dependent_launch();
     const long long W = build_prefix<kTcThreads>(p, kTcTile, s_len, s_prefix, s_wsum);
@@ -628,11 +631,11 @@ __global__ void __launch_bounds__(kTcThreads, TcForm<kN>::kMinBlocks) packed_att
     }
     if (cta >= Gc) return;
     if (X > 0) {
-        for (int b = threadIdx.x; b < nb; b += kTcThreads) s_prefix[b] += (long long)X * p.Hkv * b;
+        for (int b = threadIdx.x; b < nb; b += kTcThreads) s_prefix[b] += (long long)X * p.n_spans * b;
         __syncthreads();
     }
-    const long long U = W + (long long)X * p.Hkv * nb;
-    const Share share = share_of(cta, U, Gc, s_prefix, s_len, nb, p.Hkv, X, kTcTile);
+    const long long U = W + (long long)X * p.n_spans * nb;
+    const Share share = share_of(cta, U, Gc, s_prefix, s_len, nb, p.n_spans, X, kTcTile);
     const int n_tiles = share.n_tiles;
     if (n_tiles <= 0) return;
     if (threadIdx.x == 0) {
