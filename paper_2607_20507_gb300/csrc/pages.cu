@@ -15,9 +15,13 @@
 namespace cs {
 namespace {
 
+constexpr int kPiece = 128;             // 16-byte vectors that a warp copies at a time, four a lane in flight
+
 struct PagePools {
     uint4* data[CS_MAX_PAGE_POOLS];
     uint32_t vecs[CS_MAX_PAGE_POOLS];   // 16-byte vectors of a page
+    uint32_t first[CS_MAX_PAGE_POOLS];  // a page's pieces in the pools before
+    uint32_t pieces;                    // and in all
     int n;
 };
 
@@ -55,14 +59,20 @@ __device__ __forceinline__ int block_scan(int v, int* s_warp, int& total) {
     return before + inc - v;
 }
 
-// Copies page `src` of every pool to page `dst`; thread t of n takes every n-th vector.
-__device__ __forceinline__ void copy_page(const PagePools& pools, long long src, long long dst, int t, int n) {
-    for (int i = 0; i < pools.n; ++i) {
-        const uint32_t vecs = pools.vecs[i];
-        const uint4* from = pools.data[i] + src * vecs;
-        uint4* to = pools.data[i] + dst * vecs;
-        for (uint32_t j = t; j < vecs; j += n) to[j] = __ldcg(from + j);
-    }
+// A warp copies piece `piece` of page `src` to page `dst`.
+__device__ __forceinline__ void copy_piece(const PagePools& pools, long long src, long long dst, uint32_t piece) {
+    int i = 0;
+    while (i + 1 < pools.n && pools.first[i + 1] <= piece) ++i;
+    const uint32_t vecs = pools.vecs[i], j = (piece - pools.first[i]) * kPiece + (threadIdx.x & 31);
+    const uint4* from = pools.data[i] + src * vecs;
+    uint4* to = pools.data[i] + dst * vecs;
+    uint4 v[kPiece / 32];
+#pragma unroll
+    for (int k = 0; k < kPiece / 32; ++k)
+        if (j + 32 * k < vecs) v[k] = __ldcg(from + j + 32 * k);
+#pragma unroll
+    for (int k = 0; k < kPiece / 32; ++k)
+        if (j + 32 * k < vecs) to[j + 32 * k] = v[k];
 }
 
 // ------------------------------------------------------------------- fork
@@ -155,9 +165,12 @@ __global__ void __launch_bounds__(kForkThreads) fork_row_kernel(const PageParams
     }
     if (ok && f.L % p.ps != 0) {
         const int old = __ldcg(from + f.full);
-        if (old >= 0 && old < p.P)
-            copy_page(pools, old, __ldcg(free_ids + at), blockIdx.y * kForkThreads + threadIdx.x,
-                      gridDim.y * kForkThreads);
+        if (old >= 0 && old < p.P) {
+            const int to = __ldcg(free_ids + at);
+            constexpr int kWarps = kForkThreads / 32;
+            for (uint32_t k = blockIdx.y * kWarps + threadIdx.x / 32; k < pools.pieces; k += gridDim.y * kWarps)
+                copy_piece(pools, old, to, k);
+        }
     }
 }
 
@@ -270,7 +283,9 @@ __global__ void __launch_bounds__(kCountThreads) compact_rank_kernel(const PageP
 
 constexpr int kMoveThreads = 256;
 
-// The first `copy_ctas` CTAs copy pages, the others rename table entries.
+// The first `copy_ctas` CTAs copy pages, a warp a piece at a time (a CTA a page:
+// 239 pages of 128 KB took 28 us, 26,637 of 18 KB 250), the others rename table
+// entries.
 __global__ void __launch_bounds__(kMoveThreads) compact_move_kernel(const PageParams p,
                                                                     const __grid_constant__ PagePools pools,
                                                                     const CompactParams c, const int32_t* live,
@@ -279,10 +294,14 @@ __global__ void __launch_bounds__(kMoveThreads) compact_move_kernel(const PagePa
     allow_dependent_launch();
     if ((int)blockIdx.x < copy_ctas) {
         const int moved = __ldcg(c.n_moved);
-        for (int r = blockIdx.x; r < moved; r += copy_ctas) {
+        const uint32_t pieces = max(pools.pieces, 1u);   // (no pool: the counts alone)
+        const long long items = (long long)moved * pieces, step = (long long)copy_ctas * (kMoveThreads / 32);
+        for (long long it = (long long)blockIdx.x * (kMoveThreads / 32) + threadIdx.x / 32; it < items; it += step) {
+            const long long r = div_pos(it, pieces);
+            const uint32_t k = (uint32_t)(it - r * pieces);
             const int from = __ldcg(c.src + r), to = __ldcg(c.dst + r);
-            copy_page(pools, from, to, threadIdx.x, kMoveThreads);
-            if (threadIdx.x == 0) {
+            if (k < pools.pieces) copy_piece(pools, from, to, k);
+            if (k == 0 && (threadIdx.x & 31) == 0) {
                 p.refs[to] = __ldcg(p.refs + from);
                 p.refs[from] = 0;
             }
@@ -319,6 +338,8 @@ PagePools page_pools(const cs_page_pool* pools, int n) {
     for (int i = 0; i < n; ++i) {
         q.data[i] = static_cast<uint4*>(pools[i].data);
         q.vecs[i] = (uint32_t)(pools[i].page_bytes / 16);
+        q.first[i] = q.pieces;
+        q.pieces += (q.vecs[i] + kPiece - 1) / kPiece;
     }
     q.n = n;
     return q;
@@ -344,7 +365,10 @@ cs_status launch_kv_fork(const cs_page_dims& d, const cs_page_pool* pools, int n
     cudaError_t e = launch_dependent(fork_find_kernel, dim3(1), dim3(kFindThreads), 0, stream, p, src, dst, n, room,
                                      first, free_ids, found);
     if (e != cudaSuccess) return cuda_fail(e, "fork_find_kernel launch");
-    e = launch_dependent(fork_row_kernel, dim3(n, 4), dim3(kForkThreads), 0, stream, p, page_pools(pools, n_pools), src,
+    const PagePools q = page_pools(pools, n_pools);
+    // a warp some four pieces of the page that is copied
+    const unsigned parts = q.pieces / 32 < 1 ? 1 : q.pieces / 32 > 32 ? 32 : q.pieces / 32;
+    e = launch_dependent(fork_row_kernel, dim3(n, parts), dim3(kForkThreads), 0, stream, p, q, src,
                          dst, room, (const long long*)first, (const int32_t*)free_ids, (const int*)found, out_forked);
     return e == cudaSuccess ? CS_OK : cuda_fail(e, "fork_row_kernel launch");
 }
