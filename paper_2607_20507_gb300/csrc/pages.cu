@@ -199,7 +199,7 @@ constexpr int kCountPer = 16;
 constexpr int kCountTile = kCountThreads * kCountPer;   // pages a CTA counts
 
 struct CompactParams {
-    int* tile_live;      // [tiles] pages in use in each tile of counts
+    int* tile_live;      // [tiles] pages in use in each tile of counts; NULL: not counted before
     int32_t* src;        // [P] the moving pages, ascending (as many as move)
     int32_t* dst;        // [P] where they go
     int32_t* rank;       // [P] of an id >= N: its place in src, -1 if it does not move
@@ -239,21 +239,32 @@ __global__ void __launch_bounds__(kCountThreads) compact_rank_kernel(const PageP
         block_scan<kCountThreads>(v, s_warp, total);
         return total;
     };
+    // f(the pages in use of a stretch, its first id): stretches of a tile, or, where
+    // they are not counted before, of a thread's counts
+    auto each = [&](auto f) {
+        if (c.tile_live) {
+            for (int t = threadIdx.x; t < c.tiles; t += kCountThreads) f(__ldcg(c.tile_live + t), (long long)t * kCountTile);
+        } else {
+            for (long long id = threadIdx.x * kCountPer; id < p.P; id += kCountTile) f(__popc(live_bits(p, id)), id);
+        }
+    };
+    const long long mine = (long long)blockIdx.x * kCountTile;
     int before = 0, all = 0;
-    for (int t = threadIdx.x; t < c.tiles; t += kCountThreads) {
-        const int x = __ldcg(c.tile_live + t);
-        all += x;
-        if (t < (int)blockIdx.x) before += x;
-    }
+    each([&](int live, long long id) {
+        all += live;
+        if (id < mine) before += live;
+    });
     const int N = sum(all);
     before = sum(before);
-    // pages in use below N: the tiles before N's, and N's tile up to it
-    const int tile_n = N / kCountTile;
+    // pages in use below N: the stretches that end there, and the one that N lies in
+    const int stretch = c.tile_live ? kCountTile : kCountPer;
     int below = 0;
-    for (int t = threadIdx.x; t < tile_n; t += kCountThreads) below += __ldcg(c.tile_live + t);
+    each([&](int live, long long id) {
+        if (id + stretch <= N) below += live;
+    });
     {
-        const long long id = (long long)tile_n * kCountTile + threadIdx.x * kCountPer;
-        const uint32_t live = live_bits(p, id);
+        const long long id = (long long)N / stretch * stretch + threadIdx.x * kCountPer;
+        const uint32_t live = id < N ? live_bits(p, id) : 0;
 #pragma unroll
         for (int j = 0; j < kCountPer; ++j)
             if (id + j < N && (live >> j & 1)) ++below;
@@ -399,8 +410,14 @@ cs_status launch_kv_compact(const cs_page_dims& d, const cs_page_pool* pools, in
     c.dst = reinterpret_cast<int32_t*>(ws + ids);
     c.rank = reinterpret_cast<int32_t*>(ws + 2 * ids);
     const PageParams p = page_params(d, page_table, nullptr, ref_counts);
-    cudaError_t e = launch_dependent(compact_count_kernel, dim3(c.tiles), dim3(kCountThreads), 0, stream, p, c);
-    if (e != cudaSuccess) return cuda_fail(e, "compact_count_kernel launch");
+    cudaError_t e = cudaSuccess;
+    // up to four tiles the ranking counts them itself: a launch less
+    if (c.tiles <= 4) {
+        c.tile_live = nullptr;
+    } else {
+        e = launch_dependent(compact_count_kernel, dim3(c.tiles), dim3(kCountThreads), 0, stream, p, c);
+        if (e != cudaSuccess) return cuda_fail(e, "compact_count_kernel launch");
+    }
     e = launch_dependent(compact_rank_kernel, dim3(c.tiles), dim3(kCountThreads), 0, stream, p, c, out_live);
     if (e != cudaSuccess) return cuda_fail(e, "compact_rank_kernel launch");
     const int sms = current_sm_count();
