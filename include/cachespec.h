@@ -483,7 +483,8 @@ typedef struct {
  * Requests must not share the slots they write (cs_kv_fork gives each its own).
  *
  * cs_packed_kv_read: the newest n_rows rows of every request (positions
- * L_b - n_rows + i) as bf16 [B, n_rows, Hkv, 128], 16-byte aligned: the values
+ * L_b - n_rows + i; n_rows in [1, 2^30]) as bf16 [B, n_rows, Hkv, 128], 16-byte
+ * aligned: the values
  * code * s * t rounded once.  A row that cs_packed_kv_append would not have
  * written reads as zeros.  For what has no packed form (token trees, a prefix
  * handed to another process).
@@ -493,11 +494,14 @@ typedef struct {
  * request), up to 16; (n_draft + 1) * G must not exceed 144.  q, out,
  * page_table, ctx_lens, clamping, rows without a key, pages outside the pool,
  * slots past L_b and the workspace as there, but that the workspace may start
- * with any contents.  Arithmetic: q is taken to fp16 after a power of two has
- * brought its row's largest entry below 2^15 (entries down to 2^-31 of it keep
- * every bit), keys and values are code * s in fp16 (exact), the weights P are
- * rounded to fp16 (11 bits), all products are summed in fp32, the softmax is
- * fp32, and the head scales enter in fp32 with the softmax scale and the
+ * with any contents: its first 4 bytes are the device status word, which every
+ * call clears first (so cs_read_device_status tells of the latest call).
+ * Arithmetic: q is taken to fp16 after a power of two has brought its row's
+ * largest entry below 2^15 (entries down to 2^-31 of it keep every bit), keys
+ * and values are code * s in fp16 (exact), the weights are rounded to 11 bits
+ * (those below some 2^-138 of the row's largest count as 0), all products are
+ * summed in fp32, the softmax is fp32, and the head scales enter in fp32 with
+ * the softmax scale and the
  * normalisation.
  *
  * Return CS_ERR_INVALID_ARG (null pointer, misalignment, bad dimension or

@@ -776,7 +776,7 @@ def _page_pools(pools, P: int, dev):
         _need(t, f"pools[{i}]", t.dtype, t.dim(), dev)
         if t.dim() < 2 or t.shape[0] != P:
             raise ValueError(f"pools[{i}] must be [{P}, ...], a page a row, got {tuple(t.shape)}")
-    return (PagePool * len(pools))(*((t.data_ptr(), t.nbytes // P) for t in pools)), len(pools)
+    return (PagePool * len(pools))(*((t.data_ptr(), t.nbytes // max(P, 1)) for t in pools)), len(pools)
 
 
 def cs_kv_fork(pools, page_table, ctx_lens, ref_counts, src, dst, page_size: int, room: int = 0, workspace=None,
