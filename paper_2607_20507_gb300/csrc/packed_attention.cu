@@ -107,6 +107,12 @@ struct Cursor {
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool in) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(in ? 16 : 0) : "memory");
 }
+__device__ __forceinline__ void cp_async8(uint32_t dst, const void* src, bool in) {
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(dst), "l"(src), "r"(in ? 8 : 0) : "memory");
+}
+__device__ __forceinline__ void cp_async4(uint32_t dst, const void* src, bool in) {
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(in ? 4 : 0) : "memory");
+}
 __device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int kLeft>
 __device__ __forceinline__ void cp_async_wait() {
@@ -749,7 +755,7 @@ Choice choice() {
 }
 template <int kN>
 Choice choice_tc() {
-    return {packed_attention_tc_kernel<kN>, kTcThreads, TcForm<kN>::kSmem, TcForm<kN>::kMinBlocks};
+    return {packed_attention_tc_kernel<kN>, kTcThreads, TcForm<kN>::kSmem, 1};
 }
 constexpr int kForms = 7;
 

@@ -9,14 +9,14 @@
 //   O^T [128 dims x N] += V^T P^T  V as fp16 and P in shared memory, both
 //       MN-major: a thread writes the row of its key as it is.
 //
-// Two CTAs an SM of eight warps, each with one buffer of
-// everything: while one waits for a product, a fence or a vote, the other has
-// the SM.  (A ninth warp for the MMAs counts as four when the SM's registers
-// are shared out: one CTA fits then.)  Warps 0-3 decode the K rows of a tile, warps 4-7 its V rows; the
-// codes of the next tile come by cp.async meanwhile, every thread's own row.
-// Then all eight do the softmax, a thread one key and each four warps a share
-// of the columns (query rows).  Warp 0 issues the product for S, warp 4 that for
-// O: each would wait for it next.
+// One CTA an SM, every one of its buffers twice, so that the stages of a tile
+// overlap those of the tiles beside it: warps 0-3 decode K rows, warps 4-7 V rows,
+// warps 8-15 do the softmax, four warps a half of the columns (query rows), and
+// warps 16 and 17 issue the products for S and for O (an issue takes as long as its
+// product).  The codes of the next two tiles come by cp.async meanwhile, every
+// warp's own rows.  Scores are read as the fragments that stmatrix writes, so that
+// a thread needs the scales of a quarter of the columns.  The sums of P are products
+// too, with a matrix of ones: sums in registers took the softmax warps' room.
 //
 // As in the other form P = 2^(s - m + 12), and the tile is taken the short way
 // unless some weight would leave [2^-14, 2^15] (a vote of the workers).  Then
@@ -29,27 +29,30 @@
 // issued any more, every warp still meets every block barrier, and the status
 // word says so.
 
-constexpr int kTcThreads = 256;
+constexpr int kTcThreads = 640;                    // (the last two warps only take part in block barriers)
+constexpr int kTcSoft = 256, kTcSoftWarps = 8;     // the softmax warps: their first thread, their count
 constexpr int kTcTile = 128;                       // keys of a tile: the MMAs' M (S) and K (O)
 constexpr int kTcVBytes = kTcTile * 256;           // V of a tile in fp16
-constexpr int kTcRawBytes = 2 * kTcTile * kPackCodeBytes;   // codes of K and V of a tile
+constexpr int kTcRowBytes = kTcTile * (kPackCodeBytes + kPackGroups);   // codes and scales of K or V of a tile
+constexpr long long kTcPatience = 2000000000;      // cycles: a second or so
 constexpr int kTcMaxRows = 80;                     // query rows of a span at most
 
 template <int kN>
 struct TcForm {
-    static constexpr int kMinBlocks = 2;
-    static constexpr int kH = (kN + 15) / 16 * 8, kH1 = kN - kH;         // columns of warps 0-3, of warps 4-7: multiples of 8
+    static constexpr int kH = kN / 2;                                    // columns of four softmax warps
+    static_assert(kH % 8 == 0, "chunks of eight columns");
     static constexpr int kAtoms = kN > 64 ? 2 : 1;                       // 64-column atoms of P
     static constexpr int kPGroup = kAtoms * 1024;                        // bytes of P for 8 keys
+    static constexpr int kPBytes = kTcTile / 8 * kPGroup;
     static constexpr int kQHalf = kN * 128;                              // bytes of a dim half of Q
-    static constexpr int kColS = 64, kColO = kColS + kN;                 // tensor memory: K [0, 64), S, O
-    static constexpr int kCols = kColO + kN <= 128 ? 128 : 256;
-    static_assert(kColO + kN <= kCols && kCols * kMinBlocks <= 512, "tensor memory");
-    // V | P | Q | raw codes | columns | lengths
-    static constexpr int kOffP = kTcVBytes, kOffQ = kOffP + kTcTile / 8 * kPGroup, kOffRaw = kOffQ + 2 * kQHalf;
-    static constexpr int kOffCol = kOffRaw + kTcRawBytes, kOffLen = kOffCol + kN * 4 * (5 + 8);
+    // tensor memory: K twice, S twice, O, the sums of P, the product of faint weights
+    static constexpr int kColK = 0, kColS = 128, kColO = kColS + 2 * kN, kColL = kColO + kN, kColF = kColL + kN, kCols = 512;
+    static_assert(kColF + 64 <= kCols, "tensor memory");
+    // V | P | Q | raw rows, all twice | ones | columns | lengths
+    static constexpr int kOffP = 2 * kTcVBytes, kOffQ = kOffP + 2 * kPBytes, kOffRaw = kOffQ + 4 * kQHalf;
+    static constexpr int kOffOnes = kOffRaw + 4 * kTcRowBytes, kOffCol = kOffOnes + 2048, kOffLen = kOffCol + kN * 4 * (6 + 8);
     static constexpr int kSmem = kOffLen + kMaxBatchPerLaunch * 4 + 1024;
-    static_assert((kSmem + 2048) * kMinBlocks <= 233472, "shared memory");
+    static_assert(kOffOnes % 1024 == 0 && kSmem + 2048 <= 232448, "shared memory");
 };
 
 __device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
@@ -63,6 +66,22 @@ __device__ __forceinline__ void tc_ld8(uint32_t addr, float* v) {
     asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
                  : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7])
                  : "r"(addr));
+}
+// 8 columns of 16 lanes: a thread columns 2c and 2c + 1 (c = lane % 4) of lanes lane / 4
+// and lane / 4 + 8 (complete after tc_wait_ld)
+__device__ __forceinline__ void tc_ld16(uint32_t addr, float* v) {
+    asm volatile("tcgen05.ld.sync.aligned.16x256b.x1.b32 {%0,%1,%2,%3}, [%4];"
+                 : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3])
+                 : "r"(addr));
+}
+// Four 8 x 8 matrices of 16-bit values from their fragments; `addr`: the lane's row.
+__device__ __forceinline__ void store_matrices(uint32_t addr, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+    asm volatile("stmatrix.sync.aligned.m8n8.x4.shared.b16 [%0], {%1,%2,%3,%4};" ::"r"(addr), "r"(a), "r"(b), "r"(c), "r"(d)
+                 : "memory");
+}
+// (after tc_wait_ld: nothing that uses them is moved before it)
+__device__ __forceinline__ void tc_loaded8(float* v) {
+    asm volatile("" : "+f"(v[0]), "+f"(v[1]), "+f"(v[2]), "+f"(v[3]), "+f"(v[4]), "+f"(v[5]), "+f"(v[6]), "+f"(v[7]));
 }
 __device__ __forceinline__ void tc_st8(uint32_t addr, const uint32_t* r) {
     asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"r"(addr), "r"(r[0]), "r"(r[1]),
@@ -92,12 +111,12 @@ __device__ __forceinline__ uint64_t tc_desc(uint32_t addr, uint32_t group, uint3
     return (uint64_t)((addr >> 4) & 0x3FFF) | ((uint64_t)(atom >> 4) << 16) | ((uint64_t)(group >> 4) << 32) |
            (1ull << 46) | (2ull << 61);
 }
-// kind::f16, both operands fp16, fp32 sums, M = 128, N = n
-__host__ __device__ constexpr uint32_t tc_idesc(int n, bool a_mn, bool b_mn) {
-    return (1u << 4) | (a_mn ? 1u << 15 : 0u) | (b_mn ? 1u << 16 : 0u) | ((uint32_t)(n >> 3) << 17) | (8u << 24);
+// kind::f16, both operands fp16, fp32 sums, M = m, N = n
+__host__ __device__ constexpr uint32_t tc_idesc(int m, int n, bool a_mn, bool b_mn) {
+    return (1u << 4) | (a_mn ? 1u << 15 : 0u) | (b_mn ? 1u << 16 : 0u) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(m >> 4) << 24);
 }
 
-// Whether any of the workers' threads says so; a barrier of theirs.
+// Whether any of the softmax warps' threads says so; a barrier of theirs.
 __device__ __forceinline__ bool workers_any(bool x) {
     uint32_t r;
     asm volatile(
@@ -130,12 +149,15 @@ __device__ __forceinline__ bool tc_asleep(uint64_t* bar, uint32_t parity) {
     return done != 0;
 }
 // Bounded (about one second); returns at once when another wait has given up.
-// (Out of line: the loop's code is long.)
+// (Out of line: the loop's code is long.  try_wait sleeps for some 150 cycles at
+// most, whatever it is told: between looks at the clock, 64 of them.)
 __device__ __noinline__ void tc_wait_long(uint64_t* bar, uint32_t parity, volatile int* dead, int* status) {
-    const uint64_t t0 = global_timer_ns();
+    const long long t0 = clock64();
     while (!*dead) {
-        if (tc_asleep(bar, parity)) return;
-        if (global_timer_ns() - t0 > 1000000000ull) {
+#pragma unroll 1
+        for (int i = 0; i < 64; ++i)
+            if (tc_asleep(bar, parity)) return;
+        if (clock64() - t0 > kTcPatience) {
             *dead = 1;
             atomicOr(status, CS_DEVICE_WAIT_TIMEOUT);
         }
@@ -147,61 +169,68 @@ __device__ __forceinline__ void tc_wait(uint64_t* bar, uint32_t parity, volatile
 // Whether no wait has given up, the same answer in the whole warp.
 __device__ __forceinline__ bool alive(volatile int* dead) { return !__any_sync(0xffffffffu, *dead); }
 
+// Tile j uses those of j % 2, whose phase j / 2 is its own.
 struct TcBars {
-    uint64_t k_full;       // K of a tile decoded (4 warps)
-    uint64_t s_full;       // S of a tile done; its K is read
-    uint64_t p_full;       // P and V of a tile written, its S read (8 warps)
-    uint64_t o_done;       // O of a tile done; its P and V are read
+    uint64_t q_full[2];    // Q of a piece written (4 warps)
+    uint64_t k_full[2];    // K of a tile decoded (4 warps)
+    uint64_t v_full[2];    // V of a tile decoded (4 warps)
+    uint64_t s_full[2];    // S of a tile done; its K is read
+    uint64_t s_free[2];    // S of a tile read (8 warps)
+    uint64_t p_full[2];    // P of a tile written (8 warps)
+    uint64_t o_done[2];    // O of a tile done; its P and V are read
     uint64_t f_done;       // a product of faint weights done
+    int starts[2];         // whether a tile's products start O (1) and the sums (2); written before p_full
 };
 
 // V^T P^T, n columns of P from an atom's first on, into the columns from d on
 // (one thread issues): 8 steps of 16 keys.
 template <int kN>
-__device__ __forceinline__ void tc_mma_values(uint32_t d, uint8_t* smem, int atom, int n, bool add) {
+__device__ __forceinline__ void tc_mma_values(uint32_t d, uint8_t* smem, int buffer, int atom, int n, bool add) {
     using F = TcForm<kN>;
-    const uint32_t id = tc_idesc(n, true, true);
-    const uint64_t v = tc_desc(smem_u32(smem), 2048, 1024);
-    const uint64_t x = tc_desc(smem_u32(smem + F::kOffP + atom * 1024), F::kPGroup, 1024);
+    const uint32_t id = tc_idesc(128, n, true, true);
+    const uint64_t v = tc_desc(smem_u32(smem + buffer * kTcVBytes), 2048, 1024);
+    const uint64_t x = tc_desc(smem_u32(smem + F::kOffP + buffer * F::kPBytes + atom * 1024), F::kPGroup, 1024);
 #pragma unroll
     for (int kk = 0; kk < kTcTile / 16; ++kk)
         tc_mma_ss(d, v + (uint64_t)(kk * (4096 >> 4)), x + (uint64_t)(kk * 2 * F::kPGroup >> 4), id, add || kk > 0 ? 1u : 0u);
 }
 
+// The sums of P over the keys: 64 equal rows of ones times P, n columns.
 template <int kN>
-__device__ __forceinline__ void tc_worker(const PackedAttnParams& p, uint8_t* smem, TcBars& bars, uint32_t tmem,
-                                          volatile int* dead, const int* s_info, const int* s_len, const Cursor start,
-                                          const int n_tiles, const int* s_draft) {
+__device__ __forceinline__ void tc_mma_sums(uint32_t d, uint8_t* smem, int buffer, bool add) {
     using F = TcForm<kN>;
-    constexpr int kH = F::kH;
+    const uint32_t id = tc_idesc(64, kN, true, true);
+    const uint64_t ones = tc_desc(smem_u32(smem + F::kOffOnes), 1024, 1024);
+    const uint64_t x = tc_desc(smem_u32(smem + F::kOffP + buffer * F::kPBytes), F::kPGroup, 1024);
+#pragma unroll
+    for (int kk = 0; kk < kTcTile / 16; ++kk)
+        tc_mma_ss(d, ones, x + (uint64_t)(kk * 2 * F::kPGroup >> 4), id, add || kk > 0 ? 1u : 0u);
+}
+
+// Warps 0-3: K rows, and the query rows of a piece.  Warps 4-7: V rows.
+template <int kN>
+__device__ __forceinline__ void tc_decode(const PackedAttnParams& p, uint8_t* smem, TcBars& bars, uint32_t tmem,
+                                          volatile int* dead, const int* s_len, const Cursor start, const int n_tiles,
+                                          const int* s_draft) {
+    using F = TcForm<kN>;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, quad = warp & 3;
-    const bool v_side = warp >= 4;
-    // this side's columns: kH of them, or fewer (one body of code for both)
-    const int kC0 = v_side ? kH : 0, n_cols = v_side ? F::kH1 : kH;
-    auto mine = [&](int i) { return kH == F::kH1 || i < n_cols; };
+    const bool v_side = warp >= 4;   // (one body of code for both: the instruction cache is small)
     const int key = 32 * quad + lane;                    // of a tile; also the lane of tensor memory
     const uint32_t lanes = (uint32_t)(32 * quad) << 16;
-    const int nb = p.n_batch, cta = blockIdx.x;
-    float* s_sc = reinterpret_cast<float*>(smem + F::kOffCol);   // [N] scale of a column's scores
-    float* s_up = s_sc + kN;                             // [N] 12 - m
-    float* s_alpha = s_up + kN;                          // [N] what a column's sums are rescaled by
-    float* s_m = s_alpha + kN;                           // [N] running maxima
-    float* s_inv = s_m + kN;                             // [N] 1 / l at the end
-    int* s_red = reinterpret_cast<int*>(s_inv + kN);     // [4][N] the quads' maxima, or sums
-    float* s_faint = reinterpret_cast<float*>(s_red + 4 * kN);   // [4][N] the quads' sums of faint weights
+    const int nb = p.n_batch;
+    float* s_sc = reinterpret_cast<float*>(smem + F::kOffCol);   // [2][N] scale of a column's scores
 
-    uint8_t* s_q = smem + F::kOffQ;
-
-    // ---- the next tile's row: codes into shared memory (parts exchanged by the
-    // key's bits, so that the threads' 16-byte loads meet every bank once), scales
+    // ---- the rows of the next two tiles: codes and scales into shared memory (parts
+    // of the codes exchanged by the key's bits, so that the threads' 16-byte loads meet
+    // every bank once)
     const uint8_t* codes = v_side ? p.v_codes : p.k_codes;
     const uint8_t* scales = v_side ? p.v_scales : p.k_scales;
-    uint8_t* const raw = smem + F::kOffRaw + (v_side ? kTcRawBytes / 2 : 0) + key * kPackCodeBytes;
+    uint8_t* const raw = smem + F::kOffRaw + (v_side ? 2 * kTcRowBytes : 0);
     const int raw_x = (key >> 1) & 3;
     Cursor cl = start;           // the tile whose page is looked up next
     int left = n_tiles;
     int page = -1, slot = 0;     // of the tile whose row is loaded next
-    uint2 sc8 = make_uint2(0, 0);
+    const int page_rows = p.Hkv * p.ps;
     auto look_up = [&]() {
         page = -1;
         if (left <= 0) return;
@@ -212,22 +241,28 @@ __device__ __forceinline__ void tc_worker(const PackedAttnParams& p, uint8_t* sm
             page = __ldcg(p.page_table + (size_t)(p.b_base + cl.b) * p.max_pages + (pos >> p.ps_log2));
         advance(cl, s_len, nb, p.n_spans, kTcTile);
     };
-    auto load_row = [&]() {      // zeros for a key past the context or on no page
-        const bool in = page >= 0 && page < p.P;
-        const size_t row = in ? (size_t)page * p.Hkv * p.ps + slot : 0;
+    auto load_rows = [&](int buffer) {   // zeros for a key past the context or on no page
+        const int row = page >= 0 && page < p.P ? page * page_rows + slot : -1;
+        uint8_t* const to = raw + buffer * kTcRowBytes;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) cp_async16(smem_u32(raw + ((i ^ raw_x) << 4)), codes + row * kPackCodeBytes + 16 * i, in);
+        for (int i = 0; i < 4; ++i) {    // four lanes a row: keys of a page lie side by side
+            const int of = 8 * i + (lane >> 2), r = __shfl_sync(0xffffffffu, row, of);
+            cp_async16(smem_u32(to + (32 * quad + of) * kPackCodeBytes + (((lane & 3) ^ (of >> 1 & 3)) << 4)),
+                       codes + (size_t)max(r, 0) * kPackCodeBytes + 16 * (lane & 3), r >= 0);
+        }
+        cp_async8(smem_u32(to + kTcTile * kPackCodeBytes + key * kPackGroups), scales + (size_t)max(row, 0) * kPackGroups,
+                  row >= 0);
         cp_async_commit();
-        sc8 = in ? __ldcg(reinterpret_cast<const uint2*>(scales + row * kPackGroups)) : make_uint2(0, 0);
         look_up();
     };
-    // the row as fp16, into tensor memory (K) or shared memory (V)
-    uint8_t* const v_row = smem + (key >> 3) * 2048 + (key & 7) * 128;
-    auto decode = [&]() {
-        cp_async_wait<0>();
+    // a row as fp16, into tensor memory (K) or shared memory (V)
+    auto decode = [&](int buffer) {
+        const uint8_t* const from = raw + buffer * kTcRowBytes;
+        const uint2 sc8 = *reinterpret_cast<const uint2*>(from + kTcTile * kPackCodeBytes + key * kPackGroups);
+        uint8_t* const v_row = smem + buffer * kTcVBytes + (key >> 3) * 2048 + (key & 7) * 128;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {   // 32 dims: 16 pairs
-            const uint4 w4 = *reinterpret_cast<const uint4*>(raw + ((i ^ raw_x) << 4));
+            const uint4 w4 = *reinterpret_cast<const uint4*>(from + key * kPackCodeBytes + ((i ^ raw_x) << 4));
             const uint32_t w[4] = {w4.x, w4.y, w4.z, w4.w};
             const uint32_t f = scales_f16x2((i & 2 ? sc8.y : sc8.x) >> (i & 1 ? 16 : 0));
             uint32_t x[16];
@@ -240,7 +275,7 @@ __device__ __forceinline__ void tc_worker(const PackedAttnParams& p, uint8_t* sm
                 x[4 * j + 3] = mul_f16x2(codes_f16x2<3>(w[j]), s);
             }
             if (!v_side) {
-                tc_st16(tmem + lanes + 16 * i, x);
+                tc_st16(tmem + lanes + F::kColK + buffer * 64 + 16 * i, x);
             } else {
 #pragma unroll
                 for (int j = 0; j < 4; ++j)
@@ -249,97 +284,189 @@ __device__ __forceinline__ void tc_worker(const PackedAttnParams& p, uint8_t* sm
             }
         }
     };
-    // eight of a key's columns of P, from `col` on
-    uint8_t* const p_row = smem + F::kOffP + (key >> 3) * F::kPGroup + (key & 7) * 128;
-    auto store_p = [&](int col, uint32_t x0, uint32_t x1, uint32_t x2, uint32_t x3) {
-        *reinterpret_cast<uint4*>(p_row + (col >> 6) * 1024 + ((((col & 63) >> 3) ^ (key & 7)) << 4)) =
-            make_uint4(x0, x1, x2, x3);
-    };
-
     look_up();
-    load_row();
+    load_rows(0);
+    load_rows(1);
     Cursor cur = start;
-    float l[kH];
-    bool first_piece = true;
-    uint32_t f_phase = 0;
-    int piece_t0 = cur.t;
+    int piece = 0;
 #pragma unroll 1
     for (int j = 0; j < n_tiles; ++j) {
-        const int L = s_len[cur.b], bg = p.b_base + cur.b;
-        // the KV head of the span, and its row block's first row
-        const int head = p.n_rb == 1 ? cur.h : cur.h / p.n_rb, row0 = (cur.h - head * p.n_rb) * p.n_rows;
-        const int n_live = min(p.n_rows, p.n_all - row0);
-        const uint32_t ph = (uint32_t)j & 1;
-        const bool first = j == 0 || cur.t == 0, last = j + 1 == n_tiles || cur.t + 1 == cur.T;
-        if (first) {
-            // ---- a new piece: its query rows as fp16 below 2^15 (as in the other form)
-            piece_t0 = cur.t;
-#pragma unroll
-            for (int i = 0; i < kH; ++i) l[i] = 0.f;
-            constexpr int kMine = kN / 8;   // rows of a warp, requested together
-            uint2 x[kMine];
+        const int buf = j & 1;
+        const uint32_t ph = (uint32_t)(j >> 1) & 1;
+        if (!v_side && (j == 0 || cur.t == 0)) {
+            // ---- a new piece: its query rows as fp16 below 2^15 (as in the other form),
+            // a lane its four dims of a row, converted where they arrive.  (Their buffer was
+            // read last by the tile two before, or an earlier one.)
+            if (j >= 2) tc_wait(&bars.s_free[buf], ph ^ 1, dead, p.status);
+            // the KV head of the span, and its row block's first row
+            const int bg = p.b_base + cur.b;
+            const int head = p.n_rb == 1 ? cur.h : cur.h / p.n_rb, row0 = (cur.h - head * p.n_rb) * p.n_rows;
+            const int n_live = min(p.n_rows, p.n_all - row0);
+            uint8_t* const s_q = smem + F::kOffQ + (piece & 1) * 2 * F::kQHalf + (lane >> 4) * F::kQHalf + (lane & 1) * 8;
             const float scale = p.scale_log2 * (p.k_head ? __ldcg(p.k_head + head) : 1.f);
-#pragma unroll
-            for (int k = 0; k < kMine; ++k) {
-                const int row = warp + 8 * k;
-                x[k] = make_uint2(0, 0);
-                if (row < n_live) {
-                    const int i = s_draft[row0 + row];
-                    const uint32_t* src = reinterpret_cast<const uint32_t*>(
-                        p.q + (((size_t)bg * p.R + i) * p.Hq + (size_t)head * p.G + (row0 + row - i * p.G)) * kPackDim + 4 * lane);
-                    x[k].x = __ldcg(src);
-                    x[k].y = __ldcg(src + 1);
-                }
+            const __nv_bfloat16* const from =
+                p.q + ((size_t)bg * p.R * p.Hq + (size_t)head * p.G + row0) * kPackDim + 4 * lane;
+            auto place = [&](int row) { return s_q + row * 128 + ((((lane & 15) >> 1) ^ (row & 7)) << 4); };
+#pragma unroll 1
+            for (int row = warp; row < kN; row += 4) {
+                const bool in = row < n_live;   // row (i, g) lies i Hq + g rows past its head's first one
+                const __nv_bfloat16* src = from + (in ? (size_t)(s_draft[row0 + row] * (p.Hq - p.G) + row) * kPackDim : 0);
+                const uint32_t to = smem_u32(place(row));
+                cp_async4(to, src, in);
+                cp_async4(to + 4, src + 2, in);
             }
-#pragma unroll
-            for (int k = 0; k < kMine; ++k) {
-                const int row = warp + 8 * k;
+            cp_async_commit();
+            cp_async_wait<0>();
+#pragma unroll 1
+            for (int row = warp; row < kN; row += 4) {
                 float back;
-                const uint2 y = query_f16(x[k], back);
-                *reinterpret_cast<uint2*>(s_q + (lane >> 4) * F::kQHalf + row * 128 +
-                                          ((((lane & 15) >> 1) ^ (row & 7)) << 4) + (lane & 1) * 8) = y;
-                if (lane == 0) {
-                    // (not 0, under which a hidden score would be NaN)
-                    s_sc[row] = row < n_live ? fmaxf(scale * back, 0x1p-126f) : 0x1p-126f;
-                    s_up[row] = row < n_live ? -kNegInf : 0.f;
-                    s_m[row] = row < n_live ? kNegInf : kPUp;
-                    for (int k4 = 0; k4 < 4; ++k4) s_faint[k4 * kN + row] = 0.f;
-                }
+                uint2* const at = reinterpret_cast<uint2*>(place(row));
+                *at = query_f16(*at, back);
+                // (not 0, under which a hidden score would be NaN)
+                if (lane == 0) s_sc[(piece & 1) * kN + row] = row < n_live ? fmaxf(scale * back, 0x1p-126f) : 0x1p-126f;
             }
             fence_async_smem();
-            workers_sync();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&bars.q_full[piece & 1]);
+            ++piece;
         }
-        // ---- this tile's row (V once the product of the tile before has read its buffer),
-        // and the request of the next one's
-        if (v_side && j > 0) tc_wait(&bars.o_done, ph ^ 1, dead, p.status);
-        decode();
-        load_row();
-        if (!v_side) {
+        // ---- this tile's row, once what was in its place is read, and the request of
+        // that two tiles on
+        if (j >= 2) tc_wait(v_side ? &bars.o_done[buf] : &bars.s_full[buf], ph ^ 1, dead, p.status);
+        tc_fence_after();
+        cp_async_wait<1>();
+        __syncwarp();
+        decode(buf);
+        __syncwarp();
+        load_rows(buf);
+        if (v_side) {
+            fence_async_smem();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&bars.v_full[buf]);
+        } else {
             tc_wait_st();
             tc_fence_before();
             __syncwarp();
-            if (lane == 0) mbar_arrive(&bars.k_full);
-            if (warp == 0) {
-                // (each wait names the phase that follows the last one seen of its barrier)
-                tc_wait(&bars.k_full, ph, dead, p.status);
-                tc_fence_after();
-                __syncwarp();
-                if (alive(dead) && elect_one()) {
-                    const uint64_t dq = tc_desc(smem_u32(s_q), 1024, 0);
+            if (lane == 0) mbar_arrive(&bars.k_full[buf]);
+        }
+        advance(cur, s_len, nb, p.n_spans, kTcTile);
+    }
+    cp_async_wait<0>();
+}
+
+// Warp 16: the products for S.
+template <int kN>
+__device__ __forceinline__ void tc_issue_scores(const PackedAttnParams& p, uint8_t* smem, TcBars& bars, uint32_t tmem,
+                                                volatile int* dead, const int* s_len, const Cursor start, const int n_tiles) {
+    using F = TcForm<kN>;
+    Cursor cur = start;
+    int piece = -1;
+#pragma unroll 1
+    for (int j = 0; j < n_tiles; ++j) {
+        const int buf = j & 1;
+        const uint32_t ph = (uint32_t)(j >> 1) & 1;
+        if (j == 0 || cur.t == 0) ++piece;
+        tc_wait(&bars.k_full[buf], ph, dead, p.status);
+        if (j >= 2) tc_wait(&bars.s_free[buf], ph ^ 1, dead, p.status);
+        tc_fence_after();
+        __syncwarp();
+        if (alive(dead) && elect_one()) {
+            const uint64_t dq = tc_desc(smem_u32(smem + F::kOffQ + (piece & 1) * 2 * F::kQHalf), 1024, 0);
 #pragma unroll
-                    for (int ks = 0; ks < kPackDim / 16; ++ks)
-                        tc_mma_ts(tmem + F::kColS, tmem + ks * 8,
-                                  dq + (uint64_t)((ks >> 2) * (F::kQHalf >> 4) + (ks & 3) * 2), tc_idesc(kN, false, false),
-                                  ks > 0 ? 1u : 0u);
-                    tc_commit(&bars.s_full);
-                }
-                __syncwarp();
+            for (int ks = 0; ks < kPackDim / 16; ++ks)
+                tc_mma_ts(tmem + F::kColS + buf * kN, tmem + F::kColK + buf * 64 + ks * 8,
+                          dq + (uint64_t)((ks >> 2) * (F::kQHalf >> 4) + (ks & 3) * 2), tc_idesc(128, kN, false, false),
+                          ks > 0 ? 1u : 0u);
+            tc_commit(&bars.s_full[buf]);
+        }
+        __syncwarp();
+        advance(cur, s_len, p.n_batch, p.n_spans, kTcTile);
+    }
+}
+
+// Warp 17: the products for O and the sums.
+template <int kN>
+__device__ __forceinline__ void tc_issue_values(const PackedAttnParams& p, uint8_t* smem, TcBars& bars, uint32_t tmem,
+                                                volatile int* dead, const int n_tiles) {
+    using F = TcForm<kN>;
+#pragma unroll 1
+    for (int j = 0; j < n_tiles; ++j) {
+        const int buf = j & 1;
+        const uint32_t ph = (uint32_t)(j >> 1) & 1;
+        tc_wait(&bars.v_full[buf], ph, dead, p.status);
+        tc_wait(&bars.p_full[buf], ph, dead, p.status);
+        tc_fence_after();
+        const int starts = *reinterpret_cast<volatile int*>(&bars.starts[buf]);
+        __syncwarp();
+        if (alive(dead) && elect_one()) {
+            tc_mma_values<kN>(tmem + F::kColO, smem, buf, 0, kN, !(starts & 1));
+            tc_mma_sums<kN>(tmem + F::kColL, smem, buf, !(starts & 2));
+            tc_commit(&bars.o_done[buf]);
+        }
+        __syncwarp();
+    }
+}
+
+// Warps 8-15: the softmax and the results.
+template <int kN>
+__device__ __forceinline__ void tc_softmax(const PackedAttnParams& p, uint8_t* smem, TcBars& bars, uint32_t tmem,
+                                           volatile int* dead, const int* s_info, const int* s_len, const Cursor start,
+                                           const int n_tiles, const int* s_draft) {
+    using F = TcForm<kN>;
+    constexpr int kH = F::kH;
+    const int warp = (threadIdx.x >> 5) - 8, lane = threadIdx.x & 31, quad = warp & 3;
+    const int kC0 = warp >= 4 ? kH : 0;                  // this warp's columns
+    constexpr int n_cols = kH;
+    const int key = 32 * quad + lane;                    // of a tile; also the lane of tensor memory
+    const uint32_t lanes = (uint32_t)(32 * quad) << 16;
+    const int nb = p.n_batch, cta = blockIdx.x;
+    float* s_sc = reinterpret_cast<float*>(smem + F::kOffCol);   // [N] scale of a column's scores (of two pieces)
+    float* s_up = s_sc + 2 * kN;                         // [N] 12 - m
+    float* s_alpha = s_up + kN;                          // [N] what a column's sums are rescaled by
+    float* s_m = s_alpha + kN;                           // [N] running maxima
+    float* s_inv = s_m + kN;                             // [N] 1 / l at the end
+    int* s_red = reinterpret_cast<int*>(s_inv + kN);     // [4][N] the quads' maxima, or sums
+    float* s_faint = reinterpret_cast<float*>(s_red + 4 * kN);   // [4][N] the quads' sums of faint weights
+    const uint32_t o_at = tmem + lanes + F::kColO + kC0, l_at = tmem + lanes + F::kColL + kC0;
+
+    // eight of a key's columns of P, from `col` on
+    auto store_p = [&](int buf, int col, uint32_t x0, uint32_t x1, uint32_t x2, uint32_t x3) {
+        uint8_t* const p_row = smem + F::kOffP + buf * F::kPBytes + (key >> 3) * F::kPGroup + (key & 7) * 128;
+        *reinterpret_cast<uint4*>(p_row + (col >> 6) * 1024 + ((((col & 63) >> 3) ^ (key & 7)) << 4)) =
+            make_uint4(x0, x1, x2, x3);
+    };
+    Cursor cur = start;
+    bool first_piece = true;
+    uint32_t f_phase = 0;
+    int piece_t0 = cur.t, piece = 0;
+    int L = 0, bg = 0, head = 0, row0 = 0, n_live = 0;   // of the piece
+#pragma unroll 1
+    for (int j = 0; j < n_tiles; ++j) {
+        const int buf = j & 1;
+        const uint32_t ph = (uint32_t)(j >> 1) & 1;
+        const bool first = j == 0 || cur.t == 0, last = j + 1 == n_tiles || cur.t + 1 == cur.T;
+        if (first) {
+            piece_t0 = cur.t;
+            L = s_len[cur.b];
+            bg = p.b_base + cur.b;
+            head = p.n_rb == 1 ? cur.h : cur.h / p.n_rb;
+            row0 = (cur.h - head * p.n_rb) * p.n_rows;
+            n_live = min(p.n_rows, p.n_all - row0);
+            const int row = threadIdx.x - kTcSoft;
+            if (row < kN) {
+                s_up[row] = row < n_live ? -kNegInf : 0.f;
+                s_m[row] = row < n_live ? kNegInf : kPUp;
+                for (int k4 = 0; k4 < 4; ++k4) s_faint[k4 * kN + row] = 0.f;
             }
+            tc_wait(&bars.q_full[piece & 1], (uint32_t)(piece >> 1) & 1, dead, p.status);
+            s_sc = reinterpret_cast<float*>(smem + F::kOffCol) + (piece & 1) * kN;
+            ++piece;
+            workers_sync();
         }
         // ---- softmax: this key's scores
-        tc_wait(&bars.s_full, ph, dead, p.status);
+        tc_wait(&bars.s_full[buf], ph, dead, p.status);
         tc_fence_after();
-        const uint32_t s_at = tmem + lanes + F::kColS + kC0, o_at = tmem + lanes + F::kColO + kC0;
+        const uint32_t s_at = tmem + lanes + F::kColS + buf * kN + kC0;
         const int key0 = cur.t * kTcTile;
         // the columns that do not see this thread's key: all past the context, else those
         // of the drafts before it (columns are drafts in order, G query heads each)
@@ -353,6 +480,7 @@ __device__ __forceinline__ void tc_worker(const PackedAttnParams& p, uint8_t* sm
                 float z[8];
                 tc_ld8(s_at + i, z);
                 tc_wait_ld();
+                tc_loaded8(z);
 #pragma unroll
                 for (int k = 0; k < 8; ++k) {
                     const int row = kC0 + i + k;
@@ -379,15 +507,6 @@ __device__ __forceinline__ void tc_worker(const PackedAttnParams& p, uint8_t* sm
                 s_alpha[row] = a;
             }
             const bool rescale = workers_any(grew);
-#pragma unroll
-            for (int i = 0; i < kH; i += 4) {
-                if (!mine(i)) continue;
-                const float4 a = *reinterpret_cast<const float4*>(s_alpha + kC0 + i);
-                l[i] *= a.x;
-                l[i + 1] *= a.y;
-                l[i + 2] *= a.z;
-                l[i + 3] *= a.w;
-            }
             auto is_faint = [&](float x) { return x < kPMin && x > kPGone; };
             bool faint = false;
 #pragma unroll 1
@@ -395,24 +514,29 @@ __device__ __forceinline__ void tc_worker(const PackedAttnParams& p, uint8_t* sm
                 float z[8];
                 tc_ld8(s_at + i, z);
                 tc_wait_ld();
+                tc_loaded8(z);
 #pragma unroll
                 for (int k = 0; k < 8; ++k)
                     faint |= kC0 + i + k >= hidden && is_faint(fmaf(z[k], s_sc[kC0 + i + k], s_up[kC0 + i + k]));
             }
             faint = workers_any(faint);
-            if ((rescale || faint) && j > 0) {
-                tc_wait(&bars.o_done, ph ^ 1, dead, p.status);
+            if ((rescale || faint) && !first) {
+                tc_wait(&bars.o_done[buf ^ 1], (uint32_t)((j - 1) >> 1) & 1, dead, p.status);
                 tc_fence_after();
             }
+            if (faint && j >= 2) tc_wait(&bars.o_done[buf], ph ^ 1, dead, p.status);   // P is free
             if (rescale) {
 #pragma unroll 1
-                for (int i = 0; i < n_cols; i += 8) {
+                for (int i = 0; i < (quad == 0 ? 2 : 1) * n_cols; i += 8) {   // (the sums: in the first quad's lanes)
+                    const int col = i < n_cols ? i : i - n_cols;
+                    const uint32_t at = (i < n_cols ? o_at : l_at) + col;
                     float o[8];
-                    tc_ld8(o_at + i, o);
+                    tc_ld8(at, o);
                     tc_wait_ld();
+                    tc_loaded8(o);
 #pragma unroll
-                    for (int k = 0; k < 8; ++k) o[k] *= s_alpha[kC0 + i + k];
-                    tc_st8(o_at + i, reinterpret_cast<const uint32_t*>(o));
+                    for (int k = 0; k < 8; ++k) o[k] *= s_alpha[kC0 + col + k];
+                    tc_st8(at, reinterpret_cast<const uint32_t*>(o));
                 }
                 tc_wait_st();
             }
@@ -424,6 +548,7 @@ __device__ __forceinline__ void tc_worker(const PackedAttnParams& p, uint8_t* sm
                     float z[8], f[8];
                     tc_ld8(s_at + i, z);
                     tc_wait_ld();
+                    tc_loaded8(z);
 #pragma unroll
                     for (int k = 0; k < 8; ++k) {
                         const int row = kC0 + i + k;
@@ -438,22 +563,26 @@ __device__ __forceinline__ void tc_worker(const PackedAttnParams& p, uint8_t* sm
                         if (lane == 0) s_faint[quad * kN + row] += sum;
                     }
                     tc_st8(s_at + i, reinterpret_cast<const uint32_t*>(z));
-                    store_p(kC0 + i, pack_f16x2(f[0], f[1]), pack_f16x2(f[2], f[3]), pack_f16x2(f[4], f[5]),
+                    store_p(buf, kC0 + i, pack_f16x2(f[0], f[1]), pack_f16x2(f[2], f[3]), pack_f16x2(f[4], f[5]),
                             pack_f16x2(f[6], f[7]));
                 }
                 tc_wait_st();
                 fence_async_smem();
                 const float down = ex2(-up);
 #pragma unroll 1
-                for (int atom = 0; atom < F::kAtoms; ++atom) {   // 64 columns at a time, into the place of this tile's K
+                for (int atom = 0; atom < F::kAtoms; ++atom) {   // 64 columns at a time
                     tc_fence_before();
                     workers_sync();
                     tc_fence_after();
-                    if (warp == 0 && alive(dead) && elect_one()) {
-                        tc_mma_values<kN>(tmem, smem, atom, min(64, kN - 64 * atom), false);
-                        tc_commit(&bars.f_done);
+                    if (warp == 0) {
+                        tc_wait(&bars.v_full[buf], ph, dead, p.status);
+                        __syncwarp();
+                        if (alive(dead) && elect_one()) {
+                            tc_mma_values<kN>(tmem + F::kColF, smem, buf, atom, min(64, kN - 64 * atom), false);
+                            tc_commit(&bars.f_done);
+                        }
+                        __syncwarp();
                     }
-                    __syncwarp();
                     tc_wait(&bars.f_done, f_phase, dead, p.status);
                     f_phase ^= 1;
                     tc_fence_after();
@@ -461,9 +590,11 @@ __device__ __forceinline__ void tc_worker(const PackedAttnParams& p, uint8_t* sm
                     for (int i = 0; i < n_cols; i += 8) {
                         if ((kC0 + i) >> 6 != atom) continue;
                         float o[8], f[8];
-                        tc_ld8(tmem + lanes + ((kC0 + i) & 63), f);
+                        tc_ld8(tmem + lanes + F::kColF + ((kC0 + i) & 63), f);
                         tc_ld8(o_at + i, o);
                         tc_wait_ld();
+                        tc_loaded8(f);
+                        tc_loaded8(o);
                         // (a piece's first tile finds no sums yet)
 #pragma unroll
                         for (int k = 0; k < 8; ++k) o[k] = starts ? f[k] * down : fmaf(f[k], down, o[k]);
@@ -477,91 +608,103 @@ __device__ __forceinline__ void tc_worker(const PackedAttnParams& p, uint8_t* sm
                 tc_fence_after();
             }
         };
-        // x = s - m + 12 of this side's columns, eight at a time
-        auto scores = [&](int i, float (&x)[8]) {
-            tc_ld8(s_at + i, x);
-            float c[8], u[8];
+        // x = s - m + 12 of this warp's columns: eight of a chunk c, columns col(c) and
+        // col(c) + 1 of the keys row(0) .. row(3) of the warp's 32
+        float x[kH];
+        auto col = [&](int c) { return kC0 + 8 * c + 2 * (lane & 3); };
+        auto row = [&](int h) { return 8 * h + (lane >> 2); };
+        auto scores = [&]() {
 #pragma unroll
-            for (int k = 0; k < 8; k += 4) {
-                *reinterpret_cast<float4*>(c + k) = *reinterpret_cast<const float4*>(s_sc + kC0 + i + k);
-                *reinterpret_cast<float4*>(u + k) = *reinterpret_cast<const float4*>(s_up + kC0 + i + k);
+            for (int c = 0; c < kH / 8; ++c) {
+                tc_ld16(s_at + 8 * c, x + 8 * c);
+                tc_ld16(s_at + (16u << 16) + 8 * c, x + 8 * c + 4);
             }
             tc_wait_ld();
 #pragma unroll
-            for (int k = 0; k < 8; k += 2)
-                f2_unpack(f2_fma(f2_pack(x[k], x[k + 1]), f2_pack(c[k], c[k + 1]), f2_pack(u[k], u[k + 1])), x[k], x[k + 1]);
+            for (int c = 0; c < kH / 8; ++c) {
+                tc_loaded8(x + 8 * c);
+                const float2 m = *reinterpret_cast<const float2*>(s_sc + col(c)), u = *reinterpret_cast<const float2*>(s_up + col(c));
+#pragma unroll
+                for (int k = 8 * c; k < 8 * c + 8; k += 2)
+                    f2_unpack(f2_fma(f2_pack(x[k], x[k + 1]), f2_pack(m.x, m.y), f2_pack(u.x, u.y)), x[k], x[k + 1]);
+            }
         };
+        // what is hidden becomes `with`
+        auto hide = [&](float with) {
+#pragma unroll
+            for (int h = 0; h < 4; ++h) {
+                const int of = key0 + 32 * quad + row(h);
+                const int none = of >= L ? kN : (of - (L - p.R)) * p.G - row0;   // columns below it
+#pragma unroll
+                for (int c = 0; c < kH / 8; ++c)
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) x[8 * c + 2 * h + k] = col(c) + k < none ? with : x[8 * c + 2 * h + k];
+            }
+        };
+        scores();
+        if (edge) hide(0.f);
         float most = 0.f, least = 0.f;
 #pragma unroll
-        for (int i = 0; i < kH; i += 8) {
-            if (!mine(i)) continue;
-            float x[8];
-            scores(i, x);
-            if (edge)
-#pragma unroll
-                for (int k = 0; k < 8; ++k) x[k] = kC0 + i + k < hidden ? 0.f : x[k];
-#pragma unroll
-            for (int k = 0; k < 8; k += 2) {
-                most = fmax3(most, x[k], x[k + 1]);
-                least = fmin3(least, x[k], x[k + 1]);
-            }
+        for (int i = 0; i < kH; i += 2) {
+            most = fmax3(most, x[i], x[i + 1]);
+            least = fmin3(least, x[i], x[i + 1]);
         }
-        if (workers_any(most > kPMax || least < kPMin)) mend();
-        if (!v_side && j > 0) tc_wait(&bars.o_done, ph ^ 1, dead, p.status);   // P is free
+        const bool bad = workers_any(most > kPMax || least < kPMin);
+        if (bad) {
+            mend();
+            scores();
+        }
+        // S is read
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&bars.s_free[buf]);
+        if (edge) hide(kNegInf);
+        if (j >= 2) tc_wait(&bars.o_done[buf], ph ^ 1, dead, p.status);   // P is free
+        const uint32_t p_row = smem_u32(smem + F::kOffP + buf * F::kPBytes + (key >> 3) * F::kPGroup + (key & 7) * 128);
 #pragma unroll
-        for (int i = 0; i < kH; i += 8) {
-            if (!mine(i)) continue;
-            float x[8];
-            scores(i, x);
-            if (edge)
+        for (int c = 0; c < kH / 8; ++c) {
+            uint32_t f[4];
 #pragma unroll
-                for (int k = 0; k < 8; ++k) x[k] = kC0 + i + k < hidden ? kNegInf : x[k];
-#pragma unroll
-            for (int k = 0; k < 8; ++k) x[k] = ex2(x[k]);
-            store_p(kC0 + i, pack_f16x2(x[0], x[1]), pack_f16x2(x[2], x[3]), pack_f16x2(x[4], x[5]), pack_f16x2(x[6], x[7]));
-#pragma unroll
-            for (int k = 0; k < 8; k += 2)
-                f2_unpack(f2_add(f2_pack(l[i + k], l[i + k + 1]), f2_pack(x[k], x[k + 1])), l[i + k], l[i + k + 1]);
+            for (int h = 0; h < 4; ++h) f[h] = pack_f16x2(ex2(x[8 * c + 2 * h]), ex2(x[8 * c + 2 * h + 1]));
+            const int at = kC0 + 8 * c;
+            store_matrices(p_row + (at >> 6) * 1024 + ((((at & 63) >> 3) ^ (key & 7)) << 4), f[0], f[1], f[2], f[3]);
         }
         fence_async_smem();
         tc_fence_before();
+        if (threadIdx.x == kTcSoft) bars.starts[buf] = (starts ? 1 : 0) | (first ? 2 : 0);
         __syncwarp();
-        if (lane == 0) mbar_arrive(&bars.p_full);
-        if (warp == 4) {
-            tc_wait(&bars.p_full, ph, dead, p.status);
-            tc_fence_after();
-            __syncwarp();
-            if (alive(dead) && elect_one()) {
-                tc_mma_values<kN>(tmem + F::kColO, smem, 0, kN, !starts);
-                tc_commit(&bars.o_done);
-            }
-            __syncwarp();
-        }
+        if (lane == 0) mbar_arrive(&bars.p_full[buf]);
         if (!last) {
             advance(cur, s_len, nb, p.n_spans, kTcTile);
             continue;
         }
-        // ---- the end of a piece: sums over the keys, then a dim a thread
+        // ---- the end of a piece: a dim a thread
         const bool whole = piece_t0 == 0 && cur.t + 1 == cur.T;
         const int out_slot = 2 * cta + (first_piece ? 0 : 1);
         float* s_sum = reinterpret_cast<float*>(s_red);
-#pragma unroll
-        for (int i = 0; i < kH; ++i) {
-            if (!mine(i)) continue;
-#pragma unroll
-            for (int off = 16; off > 0; off >>= 1) l[i] += __shfl_xor_sync(0xffffffffu, l[i], off);
-            if (lane == 0) s_sum[quad * kN + kC0 + i] = l[i];
+        tc_wait(&bars.o_done[buf], ph, dead, p.status);
+        tc_fence_after();
+        if (quad == 0) {
+#pragma unroll 1
+            for (int i = 0; i < n_cols; i += 8) {
+                float o[8];
+                tc_ld8(l_at + i, o);
+                tc_wait_ld();
+                tc_loaded8(o);
+                if (lane == 0) {
+                    *reinterpret_cast<float4*>(s_sum + kC0 + i) = make_float4(o[0], o[1], o[2], o[3]);
+                    *reinterpret_cast<float4*>(s_sum + kC0 + i + 4) = make_float4(o[4], o[5], o[6], o[7]);
+                }
+            }
         }
         workers_sync();
         if (key < n_cols) {
             const int row = kC0 + key;
-            float sum = 0.f;
-            for (int k = 0; k < 4; ++k) sum += s_sum[k * kN + row] + s_faint[k * kN + row];
+            float sum = s_sum[row];
+            for (int k = 0; k < 4; ++k) sum += s_faint[k * kN + row];
             s_inv[row] = sum > 0.f ? (p.v_head ? __ldcg(p.v_head + head) : 1.f) / sum : sum == 0.f ? 0.f : sum;
             if (!whole && row < n_live) p.part_ml[(size_t)out_slot * p.n_rows + row] = make_float2(s_m[row], sum);
         }
-        tc_wait(&bars.o_done, ph, dead, p.status);
-        tc_fence_after();
         workers_sync();   // (s_inv)
         // row (i, g) of the span lies i Hq + g rows past its first one
         __nv_bfloat16* const dst = p.out + ((size_t)bg * p.R * p.Hq + (size_t)head * p.G + row0) * kPackDim + key;
@@ -569,8 +712,9 @@ __device__ __forceinline__ void tc_worker(const PackedAttnParams& p, uint8_t* sm
 #pragma unroll 1
         for (int i = 0; i < n_cols; i += 8) {
             float o[8];
-            tc_ld8(tmem + lanes + F::kColO + kC0 + i, o);
+            tc_ld8(o_at + i, o);
             tc_wait_ld();
+            tc_loaded8(o);
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
                 const int row = kC0 + i + k;
@@ -580,7 +724,7 @@ __device__ __forceinline__ void tc_worker(const PackedAttnParams& p, uint8_t* sm
                 else part[row * kPackDim] = v;
             }
         }
-        if (threadIdx.x == 0 && !whole && piece_t0 == 0) {
+        if (threadIdx.x == kTcSoft && !whole && piece_t0 == 0) {
             const long long U = *reinterpret_cast<const long long*>(s_info + 2);
             const int Gc = s_info[4];
             const int n = cur.t + 1;   // the piece's tiles (it starts the span)
@@ -592,11 +736,10 @@ __device__ __forceinline__ void tc_worker(const PackedAttnParams& p, uint8_t* sm
         advance(cur, s_len, nb, p.n_spans, kTcTile);
         workers_sync();   // (the columns' words are free)
     }
-    cp_async_wait<0>();
 }
 
 template <int kN>
-__global__ void __launch_bounds__(kTcThreads, TcForm<kN>::kMinBlocks) packed_attention_tc_kernel(const PackedAttnParams p) {
+__global__ void __launch_bounds__(kTcThreads, 1) packed_attention_tc_kernel(const PackedAttnParams p) {
     using F = TcForm<kN>;
     extern __shared__ uint4 smem_raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
@@ -612,10 +755,15 @@ __global__ void __launch_bounds__(kTcThreads, TcForm<kN>::kMinBlocks) packed_att
     const int nb = p.n_batch;
     if (threadIdx.x == 0) {
         s_dead = 0;
-        mbar_init(&bars.k_full, 4);
-        mbar_init(&bars.s_full, 1);
-        mbar_init(&bars.p_full, 8);
-        mbar_init(&bars.o_done, 1);
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(&bars.q_full[i], 4);
+            mbar_init(&bars.k_full[i], 4);
+            mbar_init(&bars.v_full[i], 4);
+            mbar_init(&bars.s_full[i], 1);
+            mbar_init(&bars.s_free[i], kTcSoftWarps);
+            mbar_init(&bars.p_full[i], kTcSoftWarps);
+            mbar_init(&bars.o_done[i], 1);
+        }
         mbar_init(&bars.f_done, 1);
         fence_barrier_init();
     }
@@ -648,14 +796,21 @@ __global__ void __launch_bounds__(kTcThreads, TcForm<kN>::kMinBlocks) packed_att
                      : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
+    uint32_t* const ones = reinterpret_cast<uint32_t*>(smem + F::kOffOnes);
+    if (threadIdx.x < 512) ones[threadIdx.x] = 0x3c003c00u;
+    fence_async_smem();
     tc_fence_before();
     __syncthreads();   // the prefix gives way to V
     tc_fence_after();
     const uint32_t tmem = s_tmem;
 
-    tc_worker<kN>(p, smem, bars, tmem, &s_dead, s_info, s_len, share.first, n_tiles, s_draft);
-    // every MMA completes before the tensor memory is given back
-    if (warp == 0 && !mbar_wait_bounded(&bars.o_done, (uint32_t)(n_tiles - 1) & 1) && threadIdx.x == 0)
+    if (warp < 8) tc_decode<kN>(p, smem, bars, tmem, &s_dead, s_len, share.first, n_tiles, s_draft);
+    else if (warp == 16) tc_issue_scores<kN>(p, smem, bars, tmem, &s_dead, s_len, share.first, n_tiles);
+    else if (warp == 17) tc_issue_values<kN>(p, smem, bars, tmem, &s_dead, n_tiles);
+    else if (warp < 16) tc_softmax<kN>(p, smem, bars, tmem, &s_dead, s_info, s_len, share.first, n_tiles, s_draft);
+    // every MMA completes before the tensor memory is given back (where a wait gave up
+    // and the last one was not issued, this wait gives those in flight a second)
+    if (warp == 0 && !mbar_wait_bounded(&bars.o_done[(n_tiles - 1) & 1], (uint32_t)((n_tiles - 1) >> 1) & 1) && threadIdx.x == 0)
         atomicOr(p.status, CS_DEVICE_WAIT_TIMEOUT);
     tc_fence_before();
     __syncthreads();
