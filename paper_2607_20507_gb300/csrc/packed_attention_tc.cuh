@@ -29,7 +29,7 @@
 // issued any more, every warp still meets every block barrier, and the status
 // word says so.
 
-constexpr int kTcThreads = 640;                    // (the last two warps only take part in block barriers)
+constexpr int kTcThreads = 640;                    // (the last warp only takes part in block barriers)
 constexpr int kTcSoft = 256, kTcSoftWarps = 8;     // the softmax warps: their first thread, their count
 constexpr int kTcTile = 128;                       // keys of a tile: the MMAs' M (S) and K (O)
 constexpr int kTcVBytes = kTcTile * 256;           // V of a tile in fp16
@@ -127,6 +127,17 @@ __device__ __forceinline__ bool workers_any(bool x) {
         : "memory");
     return r != 0;
 }
+// The same, and with warp 18.
+__device__ __forceinline__ bool vote(bool x) {
+    uint32_t r;
+    asm volatile(
+        "{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbarrier.cta.red.or.pred q, 2, 288, p;\n\t"
+        "selp.u32 %0, 1, 0, q;\n\t}\n"
+        : "=r"(r)
+        : "r"((uint32_t)x)
+        : "memory");
+    return r != 0;
+}
 __device__ __forceinline__ void workers_sync() { asm volatile("barrier.cta.sync 1, 256;" ::: "memory"); }
 
 // A float's bits as an integer of the same order, and back.
@@ -175,8 +186,7 @@ struct TcBars {
     uint64_t k_full[2];    // K of a tile decoded (4 warps)
     uint64_t v_full[2];    // V of a tile decoded (4 warps)
     uint64_t s_full[2];    // S of a tile done; its K is read
-    uint64_t s_free[2];    // S of a tile read (8 warps)
-    uint64_t p_full[2];    // P of a tile written (8 warps)
+    uint64_t p_full[2];    // P of a tile written, its S read (8 warps)
     uint64_t o_done[2];    // O of a tile done; its P and V are read
     uint64_t f_done;       // a product of faint weights done
     int starts[2];         // whether a tile's products start O (1) and the sums (2); written before p_full
@@ -297,7 +307,7 @@ __device__ __forceinline__ void tc_decode(const PackedAttnParams& p, uint8_t* sm
             // ---- a new piece: its query rows as fp16 below 2^15 (as in the other form),
             // a lane its four dims of a row, converted where they arrive.  (Their buffer was
             // read last by the tile two before, or an earlier one.)
-            if (j >= 2) tc_wait(&bars.s_free[buf], ph ^ 1, dead, p.status);
+            if (j >= 2) tc_wait(&bars.p_full[buf], ph ^ 1, dead, p.status);
             // the KV head of the span, and its row block's first row
             const int bg = p.b_base + cur.b;
             const int head = p.n_rb == 1 ? cur.h : cur.h / p.n_rb, row0 = (cur.h - head * p.n_rb) * p.n_rows;
@@ -367,7 +377,7 @@ __device__ __forceinline__ void tc_issue_scores(const PackedAttnParams& p, uint8
         const uint32_t ph = (uint32_t)(j >> 1) & 1;
         if (j == 0 || cur.t == 0) ++piece;
         tc_wait(&bars.k_full[buf], ph, dead, p.status);
-        if (j >= 2) tc_wait(&bars.s_free[buf], ph ^ 1, dead, p.status);
+        if (j >= 2) tc_wait(&bars.p_full[buf], ph ^ 1, dead, p.status);
         tc_fence_after();
         __syncwarp();
         if (alive(dead) && elect_one()) {
@@ -407,6 +417,17 @@ __device__ __forceinline__ void tc_issue_values(const PackedAttnParams& p, uint8
     }
 }
 
+// Warp 18: takes part in a tile's vote once the place of its P is free, so that the
+// softmax warps do not each look.
+__device__ __forceinline__ void tc_watch(const PackedAttnParams& p, TcBars& bars, volatile int* dead, const int n_tiles) {
+#pragma unroll 1
+    for (int j = 0; j < n_tiles; ++j) {
+        if (j >= 2) tc_wait(&bars.o_done[j & 1], (uint32_t)((j >> 1) & 1) ^ 1, dead, p.status);
+        __syncwarp();
+        vote(false);
+    }
+}
+
 // Warps 8-15: the softmax and the results.
 template <int kN>
 __device__ __forceinline__ void tc_softmax(const PackedAttnParams& p, uint8_t* smem, TcBars& bars, uint32_t tmem,
@@ -439,14 +460,15 @@ __device__ __forceinline__ void tc_softmax(const PackedAttnParams& p, uint8_t* s
     bool first_piece = true;
     uint32_t f_phase = 0;
     int piece_t0 = cur.t, piece = 0;
-    int L = 0, bg = 0, head = 0, row0 = 0, n_live = 0;   // of the piece
+    int L = 0, bg = 0, head = 0, row0 = 0, n_live = 0, left = 0;   // of the piece; its tiles from the next on
 #pragma unroll 1
     for (int j = 0; j < n_tiles; ++j) {
         const int buf = j & 1;
         const uint32_t ph = (uint32_t)(j >> 1) & 1;
-        const bool first = j == 0 || cur.t == 0, last = j + 1 == n_tiles || cur.t + 1 == cur.T;
+        const bool first = left == 0;
         if (first) {
             piece_t0 = cur.t;
+            left = min(cur.T - cur.t, n_tiles - j);
             L = s_len[cur.b];
             bg = p.b_base + cur.b;
             head = p.n_rb == 1 ? cur.h : cur.h / p.n_rb;
@@ -524,7 +546,6 @@ __device__ __forceinline__ void tc_softmax(const PackedAttnParams& p, uint8_t* s
                 tc_wait(&bars.o_done[buf ^ 1], (uint32_t)((j - 1) >> 1) & 1, dead, p.status);
                 tc_fence_after();
             }
-            if (faint && j >= 2) tc_wait(&bars.o_done[buf], ph ^ 1, dead, p.status);   // P is free
             if (rescale) {
 #pragma unroll 1
                 for (int i = 0; i < (quad == 0 ? 2 : 1) * n_cols; i += 8) {   // (the sums: in the first quad's lanes)
@@ -649,17 +670,12 @@ __device__ __forceinline__ void tc_softmax(const PackedAttnParams& p, uint8_t* s
             most = fmax3(most, x[i], x[i + 1]);
             least = fmin3(least, x[i], x[i + 1]);
         }
-        const bool bad = workers_any(most > kPMax || least < kPMin);
+        const bool bad = vote(most > kPMax || least < kPMin);   // (P is free, too)
         if (bad) {
             mend();
             scores();
         }
-        // S is read
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&bars.s_free[buf]);
         if (edge) hide(kNegInf);
-        if (j >= 2) tc_wait(&bars.o_done[buf], ph ^ 1, dead, p.status);   // P is free
         const uint32_t p_row = smem_u32(smem + F::kOffP + buf * F::kPBytes + (key >> 3) * F::kPGroup + (key & 7) * 128);
 #pragma unroll
         for (int c = 0; c < kH / 8; ++c) {
@@ -674,8 +690,8 @@ __device__ __forceinline__ void tc_softmax(const PackedAttnParams& p, uint8_t* s
         if (threadIdx.x == kTcSoft) bars.starts[buf] = (starts ? 1 : 0) | (first ? 2 : 0);
         __syncwarp();
         if (lane == 0) mbar_arrive(&bars.p_full[buf]);
-        if (!last) {
-            advance(cur, s_len, nb, p.n_spans, kTcTile);
+        if (--left > 0) {
+            ++cur.t;
             continue;
         }
         // ---- the end of a piece: a dim a thread
@@ -760,7 +776,6 @@ __global__ void __launch_bounds__(kTcThreads, 1) packed_attention_tc_kernel(cons
             mbar_init(&bars.k_full[i], 4);
             mbar_init(&bars.v_full[i], 4);
             mbar_init(&bars.s_full[i], 1);
-            mbar_init(&bars.s_free[i], kTcSoftWarps);
             mbar_init(&bars.p_full[i], kTcSoftWarps);
             mbar_init(&bars.o_done[i], 1);
         }
@@ -807,6 +822,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) packed_attention_tc_kernel(cons
     if (warp < 8) tc_decode<kN>(p, smem, bars, tmem, &s_dead, s_len, share.first, n_tiles, s_draft);
     else if (warp == 16) tc_issue_scores<kN>(p, smem, bars, tmem, &s_dead, s_len, share.first, n_tiles);
     else if (warp == 17) tc_issue_values<kN>(p, smem, bars, tmem, &s_dead, n_tiles);
+    else if (warp == 18) tc_watch(p, bars, &s_dead, n_tiles);
     else if (warp < 16) tc_softmax<kN>(p, smem, bars, tmem, &s_dead, s_info, s_len, share.first, n_tiles, s_draft);
     // every MMA completes before the tensor memory is given back (where a wait gave up
     // and the last one was not issued, this wait gives those in flight a second)
