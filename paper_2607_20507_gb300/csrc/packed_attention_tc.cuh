@@ -270,10 +270,13 @@ __device__ __forceinline__ void tc_decode(const PackedAttnParams& p, uint8_t* sm
         const uint8_t* const from = raw + buffer * kTcRowBytes;
         const uint2 sc8 = *reinterpret_cast<const uint2*>(from + kTcTile * kPackCodeBytes + key * kPackGroups);
         uint8_t* const v_row = smem + buffer * kTcVBytes + (key >> 3) * 2048 + (key & 7) * 128;
+        uint4 all[4];   // (requested together: no load is moved before a store below)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            all[i] = *reinterpret_cast<const uint4*>(from + key * kPackCodeBytes + ((i ^ raw_x) << 4));
 #pragma unroll
         for (int i = 0; i < 4; ++i) {   // 32 dims: 16 pairs
-            const uint4 w4 = *reinterpret_cast<const uint4*>(from + key * kPackCodeBytes + ((i ^ raw_x) << 4));
-            const uint32_t w[4] = {w4.x, w4.y, w4.z, w4.w};
+            const uint32_t w[4] = {all[i].x, all[i].y, all[i].z, all[i].w};
             const uint32_t f = scales_f16x2((i & 2 ? sc8.y : sc8.x) >> (i & 1 ? 16 : 0));
             uint32_t x[16];
 #pragma unroll
