@@ -2,7 +2,7 @@
 // (cs_packed_verify_attention): o = softmax_j(scale q . K_j) V_j with K and V
 // the values that the codes stand for (packed.cuh).
 //
-// Up to 32 query rows per KV head take the form below, more the tcgen05 form
+// Up to 24 query rows per KV head take the form below, more the tcgen05 form
 // (packed_attention_tc.cuh).
 //
 // Work split.  A span is one (request, KV head) -- with more than 80 query rows
@@ -755,19 +755,18 @@ Choice choice() {
 }
 template <int kN>
 Choice choice_tc() {
-    return {packed_attention_tc_kernel<kN>, kTcThreads, TcForm<kN>::kSmem, 1};
+    return {packed_attention_tc_kernel<kN>, TcForm<kN>::kThreads, TcForm<kN>::kSmem, 1};
 }
 constexpr int kForms = 7;
 
-// The form for a number of query rows of a span: up to 32 the one above (32 rows, 64
-// requests of 4096 keys, 8 KV heads: 172 us; 36 rows in the tcgen05 form 189, and
-// 20 rows 82 against 104 in it at 2048 keys), from 33 on the tcgen05 form (36 rows
-// in the other one 200, 72 rows 269 against 152 at 32 requests).
+// The form for a number of query rows of a span: up to 24 the one above (24 rows, 64
+// requests of 4096 keys, 8 KV heads: 129 us, 138 in the tcgen05 form), from 25 on the
+// tcgen05 form (28 rows: 137 us, 170 in the other one).
 int form_of(int rows) {
-    return rows <= 32 ? (rows + 7) / 8 - 1 : rows <= 48 ? 4 : rows <= 64 ? 5 : 6;
+    return rows <= 24 ? (rows + 7) / 8 - 1 : rows <= 32 ? 3 : rows <= 48 ? 4 : rows <= 64 ? 5 : 6;
 }
 Choice choice_of(int form) {
-    static const Choice all[kForms] = {choice<1>(), choice<2>(), choice<3>(), choice<4>(), choice_tc<48>(), choice_tc<64>(),
+    static const Choice all[kForms] = {choice<1>(), choice<2>(), choice<3>(), choice_tc<32>(), choice_tc<48>(), choice_tc<64>(),
                                        choice_tc<80>()};
     return all[form];
 }

@@ -1,4 +1,4 @@
-// packed_attention_tc.cuh -- the tcgen05 form of packed attention, for 33 to 80
+// packed_attention_tc.cuh -- the tcgen05 form of packed attention, for 25 to 80
 // query rows of a span (included by packed_attention.cu inside its anonymous
 // namespace: the same split of the keys, pieces and merge).
 //
@@ -10,13 +10,13 @@
 //       MN-major: a thread writes the row of its key as it is.
 //
 // One CTA an SM, every one of its buffers twice, so that the stages of a tile
-// overlap those of the tiles beside it: warps 0-3 decode K rows, warps 4-7 V rows,
-// warps 8-15 do the softmax, four warps a half of the columns (query rows), and
-// warps 16 and 17 issue the products for S and for O (an issue takes as long as its
-// product).  The codes of the next two tiles come by cp.async meanwhile, every
-// warp's own rows.  Scores are read as the fragments that stmatrix writes, so that
-// a thread needs the scales of a quarter of the columns.  The sums of P are products
-// too, with a matrix of ones: sums in registers took the softmax warps' room.
+// overlap those of the tiles beside it, each with warps of its own: K rows are
+// decoded, V rows are, the softmax is done, and two warps issue the products for S
+// and for O (an issue takes as long as its product).  The codes of the next two
+// tiles come by cp.async meanwhile, every warp's own rows.  Scores are read as the
+// fragments that stmatrix writes, so that a thread needs the scales of a quarter of
+// the columns.  The sums of P are products too, with a matrix of ones: sums in
+// registers took the softmax warps' room.
 //
 // As in the other form P = 2^(s - m + 12), and the tile is taken the short way
 // unless some weight would leave [2^-14, 2^15] (a vote of the workers).  Then
@@ -29,8 +29,6 @@
 // issued any more, every warp still meets every block barrier, and the status
 // word says so.
 
-constexpr int kTcThreads = 640;                    // (the last warp only takes part in block barriers)
-constexpr int kTcSoft = 256, kTcSoftWarps = 8;     // the softmax warps: their first thread, their count
 constexpr int kTcTile = 128;                       // keys of a tile: the MMAs' M (S) and K (O)
 constexpr int kTcVBytes = kTcTile * 256;           // V of a tile in fp16
 constexpr int kTcRowBytes = kTcTile * (kPackCodeBytes + kPackGroups);   // codes and scales of K or V of a tile
@@ -39,6 +37,13 @@ constexpr int kTcMaxRows = 80;                     // query rows of a span at mo
 
 template <int kN>
 struct TcForm {
+    // Warps: eight decoders a set, one set or (up to 48 columns, where they are what
+    // takes longest: 36 rows 162 us with one set, 151 with two; 56 rows 99 and 108,
+    // for want of registers) two in turn; eight for the softmax; two that issue, one
+    // that watches.
+    static constexpr int kSets = kN <= 48 ? 2 : 1;
+    static constexpr int kSoft = 8 * kSets, kIssueS = kSoft + 8, kIssueO = kIssueS + 1, kWatch = kIssueS + 2;
+    static constexpr int kThreads = (kWatch + 4) / 4 * 4 * 32;           // (registers are given to four warps at a time)
     static constexpr int kH = kN / 2;                                    // columns of four softmax warps
     static_assert(kH % 8 == 0, "chunks of eight columns");
     static constexpr int kAtoms = kN > 64 ? 2 : 1;                       // 64-column atoms of P
@@ -127,7 +132,7 @@ __device__ __forceinline__ bool workers_any(bool x) {
         : "memory");
     return r != 0;
 }
-// The same, and with warp 18.
+// The same, and with the watching warp.
 __device__ __forceinline__ bool vote(bool x) {
     uint32_t r;
     asm volatile(
@@ -217,13 +222,14 @@ __device__ __forceinline__ void tc_mma_sums(uint32_t d, uint8_t* smem, int buffe
         tc_mma_ss(d, ones, x + (uint64_t)(kk * 2 * F::kPGroup >> 4), id, add || kk > 0 ? 1u : 0u);
 }
 
-// Warps 0-3: K rows, and the query rows of a piece.  Warps 4-7: V rows.
+// Of the eight warps of a set the first four: K rows, and the query rows of a piece;
+// the others: V rows.
 template <int kN>
 __device__ __forceinline__ void tc_decode(const PackedAttnParams& p, uint8_t* smem, TcBars& bars, uint32_t tmem,
                                           volatile int* dead, const int* s_len, const Cursor start, const int n_tiles,
                                           const int* s_draft) {
     using F = TcForm<kN>;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, quad = warp & 3;
+    const int warp = (threadIdx.x >> 5) & 7, lane = threadIdx.x & 31, quad = warp & 3, set = threadIdx.x >> 8;
     const bool v_side = warp >= 4;   // (one body of code for both: the instruction cache is small)
     const int key = 32 * quad + lane;                    // of a tile; also the lane of tensor memory
     const uint32_t lanes = (uint32_t)(32 * quad) << 16;
@@ -237,19 +243,24 @@ __device__ __forceinline__ void tc_decode(const PackedAttnParams& p, uint8_t* sm
     const uint8_t* scales = v_side ? p.v_scales : p.k_scales;
     uint8_t* const raw = smem + F::kOffRaw + (v_side ? 2 * kTcRowBytes : 0);
     const int raw_x = (key >> 1) & 3;
-    Cursor cl = start;           // the tile whose page is looked up next
-    int left = n_tiles;
+    Cursor cl = start, cur = start;   // the tile whose page is looked up next, and tile j
+    int next = set, piece = 0;        // cl's tile, j's piece
+    for (int i = 0; i < set; ++i) {
+        advance(cl, s_len, nb, p.n_spans, kTcTile);
+        advance(cur, s_len, nb, p.n_spans, kTcTile);
+        piece += cur.t == 0;
+    }
     int page = -1, slot = 0;     // of the tile whose row is loaded next
     const int page_rows = p.Hkv * p.ps;
     auto look_up = [&]() {
         page = -1;
-        if (left <= 0) return;
-        --left;
+        if (next >= n_tiles) return;
+        next += F::kSets;
         const int pos = cl.t * kTcTile + key;
         slot = (p.n_rb == 1 ? cl.h : cl.h / p.n_rb) * p.ps + (pos & (p.ps - 1));
         if (pos < s_len[cl.b])
             page = __ldcg(p.page_table + (size_t)(p.b_base + cl.b) * p.max_pages + (pos >> p.ps_log2));
-        advance(cl, s_len, nb, p.n_spans, kTcTile);
+        for (int i = 0; i < F::kSets; ++i) advance(cl, s_len, nb, p.n_spans, kTcTile);
     };
     auto load_rows = [&](int buffer) {   // zeros for a key past the context or on no page
         const int row = page >= 0 && page < p.P ? page * page_rows + slot : -1;
@@ -298,12 +309,10 @@ __device__ __forceinline__ void tc_decode(const PackedAttnParams& p, uint8_t* sm
         }
     };
     look_up();
-    load_rows(0);
-    load_rows(1);
-    Cursor cur = start;
-    int piece = 0;
+    load_rows(set);
+    if (F::kSets == 1) load_rows(1);
 #pragma unroll 1
-    for (int j = 0; j < n_tiles; ++j) {
+    for (int j = set; j < n_tiles; j += F::kSets) {
         const int buf = j & 1;
         const uint32_t ph = (uint32_t)(j >> 1) & 1;
         if (!v_side && (j == 0 || cur.t == 0)) {
@@ -341,13 +350,12 @@ __device__ __forceinline__ void tc_decode(const PackedAttnParams& p, uint8_t* sm
             fence_async_smem();
             __syncwarp();
             if (lane == 0) mbar_arrive(&bars.q_full[piece & 1]);
-            ++piece;
         }
         // ---- this tile's row, once what was in its place is read, and the request of
         // that two tiles on
         if (j >= 2) tc_wait(v_side ? &bars.o_done[buf] : &bars.s_full[buf], ph ^ 1, dead, p.status);
         tc_fence_after();
-        cp_async_wait<1>();
+        cp_async_wait<2 - F::kSets>();
         __syncwarp();
         decode(buf);
         __syncwarp();
@@ -362,12 +370,15 @@ __device__ __forceinline__ void tc_decode(const PackedAttnParams& p, uint8_t* sm
             __syncwarp();
             if (lane == 0) mbar_arrive(&bars.k_full[buf]);
         }
-        advance(cur, s_len, nb, p.n_spans, kTcTile);
+        for (int i = 0; i < F::kSets; ++i) {
+            advance(cur, s_len, nb, p.n_spans, kTcTile);
+            piece += cur.t == 0;
+        }
     }
     cp_async_wait<0>();
 }
 
-// Warp 16: the products for S.
+// A warp: the products for S.
 template <int kN>
 __device__ __forceinline__ void tc_issue_scores(const PackedAttnParams& p, uint8_t* smem, TcBars& bars, uint32_t tmem,
                                                 volatile int* dead, const int* s_len, const Cursor start, const int n_tiles) {
@@ -397,7 +408,7 @@ __device__ __forceinline__ void tc_issue_scores(const PackedAttnParams& p, uint8
     }
 }
 
-// Warp 17: the products for O and the sums.
+// A warp: the products for O and the sums.
 template <int kN>
 __device__ __forceinline__ void tc_issue_values(const PackedAttnParams& p, uint8_t* smem, TcBars& bars, uint32_t tmem,
                                                 volatile int* dead, const int n_tiles) {
@@ -420,7 +431,7 @@ __device__ __forceinline__ void tc_issue_values(const PackedAttnParams& p, uint8
     }
 }
 
-// Warp 18: takes part in a tile's vote once the place of its P is free, so that the
+// A warp: takes part in a tile's vote once the place of its P is free, so that the
 // softmax warps do not each look.
 __device__ __forceinline__ void tc_watch(const PackedAttnParams& p, TcBars& bars, volatile int* dead, const int n_tiles) {
 #pragma unroll 1
@@ -431,14 +442,14 @@ __device__ __forceinline__ void tc_watch(const PackedAttnParams& p, TcBars& bars
     }
 }
 
-// Warps 8-15: the softmax and the results.
+// The softmax and the results.
 template <int kN>
 __device__ __forceinline__ void tc_softmax(const PackedAttnParams& p, uint8_t* smem, TcBars& bars, uint32_t tmem,
                                            volatile int* dead, const int* s_info, const int* s_len, const Cursor start,
                                            const int n_tiles, const int* s_draft) {
     using F = TcForm<kN>;
     constexpr int kH = F::kH;
-    const int warp = (threadIdx.x >> 5) - 8, lane = threadIdx.x & 31, quad = warp & 3;
+    const int warp = (threadIdx.x >> 5) - F::kSoft, lane = threadIdx.x & 31, quad = warp & 3;
     const int kC0 = warp >= 4 ? kH : 0;                  // this warp's columns
     constexpr int n_cols = kH;
     const int key = 32 * quad + lane;                    // of a tile; also the lane of tensor memory
@@ -477,7 +488,7 @@ __device__ __forceinline__ void tc_softmax(const PackedAttnParams& p, uint8_t* s
             head = p.n_rb == 1 ? cur.h : cur.h / p.n_rb;
             row0 = (cur.h - head * p.n_rb) * p.n_rows;
             n_live = min(p.n_rows, p.n_all - row0);
-            const int row = threadIdx.x - kTcSoft;
+            const int row = threadIdx.x - 32 * F::kSoft;
             if (row < kN) {
                 s_up[row] = row < n_live ? -kNegInf : 0.f;
                 s_m[row] = row < n_live ? kNegInf : kPUp;
@@ -690,7 +701,7 @@ __device__ __forceinline__ void tc_softmax(const PackedAttnParams& p, uint8_t* s
         }
         fence_async_smem();
         tc_fence_before();
-        if (threadIdx.x == kTcSoft) bars.starts[buf] = (starts ? 1 : 0) | (first ? 2 : 0);
+        if (threadIdx.x == 32 * F::kSoft) bars.starts[buf] = (starts ? 1 : 0) | (first ? 2 : 0);
         __syncwarp();
         if (lane == 0) mbar_arrive(&bars.p_full[buf]);
         if (--left > 0) {
@@ -743,7 +754,7 @@ __device__ __forceinline__ void tc_softmax(const PackedAttnParams& p, uint8_t* s
                 else part[row * kPackDim] = v;
             }
         }
-        if (threadIdx.x == kTcSoft && !whole && piece_t0 == 0) {
+        if (threadIdx.x == 32 * F::kSoft && !whole && piece_t0 == 0) {
             const long long U = *reinterpret_cast<const long long*>(s_info + 2);
             const int Gc = s_info[4];
             const int n = cur.t + 1;   // the piece's tiles (it starts the span)
@@ -758,12 +769,12 @@ __device__ __forceinline__ void tc_softmax(const PackedAttnParams& p, uint8_t* s
 }
 
 template <int kN>
-__global__ void __launch_bounds__(kTcThreads, 1) packed_attention_tc_kernel(const PackedAttnParams p) {
+__global__ void __launch_bounds__(TcForm<kN>::kThreads, 1) packed_attention_tc_kernel(const PackedAttnParams p) {
     using F = TcForm<kN>;
     extern __shared__ uint4 smem_raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     __shared__ TcBars bars;
-    __shared__ long long s_wsum[kTcThreads / 32];
+    __shared__ long long s_wsum[F::kThreads / 32];
     __shared__ alignas(16) int s_info[8];      // [2], [3] U; [4] the CTAs
     __shared__ uint32_t s_tmem;
     __shared__ volatile int s_dead;
@@ -779,16 +790,16 @@ __global__ void __launch_bounds__(kTcThreads, 1) packed_attention_tc_kernel(cons
             mbar_init(&bars.k_full[i], 4);
             mbar_init(&bars.v_full[i], 4);
             mbar_init(&bars.s_full[i], 1);
-            mbar_init(&bars.p_full[i], kTcSoftWarps);
+            mbar_init(&bars.p_full[i], 8);
             mbar_init(&bars.o_done[i], 1);
         }
         mbar_init(&bars.f_done, 1);
         fence_barrier_init();
     }
-    for (int row = threadIdx.x; row < 2 * kTcMaxRows; row += kTcThreads) s_draft[row] = row / p.G;
+    for (int row = threadIdx.x; row < 2 * kTcMaxRows; row += F::kThreads) s_draft[row] = row / p.G;
     wait_prior_grid();
     allow_dependent_launch();
-    const long long W = build_prefix<kTcThreads>(p, kTcTile, s_len, s_prefix, s_wsum);
+    const long long W = build_prefix<F::kThreads>(p, kTcTile, s_len, s_prefix, s_wsum);
     const bool few = W <= grid;
     const int X = few ? 0 : p.span_x, Gc = few ? (int)W : grid;
     if (threadIdx.x == 0) {
@@ -797,7 +808,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) packed_attention_tc_kernel(cons
     }
     if (cta >= Gc) return;
     if (X > 0) {
-        for (int b = threadIdx.x; b < nb; b += kTcThreads) s_prefix[b] += (long long)X * p.n_spans * b;
+        for (int b = threadIdx.x; b < nb; b += F::kThreads) s_prefix[b] += (long long)X * p.n_spans * b;
         __syncthreads();
     }
     const long long U = W + (long long)X * p.n_spans * nb;
@@ -822,11 +833,11 @@ __global__ void __launch_bounds__(kTcThreads, 1) packed_attention_tc_kernel(cons
     tc_fence_after();
     const uint32_t tmem = s_tmem;
 
-    if (warp < 8) tc_decode<kN>(p, smem, bars, tmem, &s_dead, s_len, share.first, n_tiles, s_draft);
-    else if (warp == 16) tc_issue_scores<kN>(p, smem, bars, tmem, &s_dead, s_len, share.first, n_tiles);
-    else if (warp == 17) tc_issue_values<kN>(p, smem, bars, tmem, &s_dead, n_tiles);
-    else if (warp == 18) tc_watch(p, bars, &s_dead, n_tiles);
-    else if (warp < 16) tc_softmax<kN>(p, smem, bars, tmem, &s_dead, s_info, s_len, share.first, n_tiles, s_draft);
+    if (warp < F::kSoft) tc_decode<kN>(p, smem, bars, tmem, &s_dead, s_len, share.first, n_tiles, s_draft);
+    else if (warp == F::kIssueS) tc_issue_scores<kN>(p, smem, bars, tmem, &s_dead, s_len, share.first, n_tiles);
+    else if (warp == F::kIssueO) tc_issue_values<kN>(p, smem, bars, tmem, &s_dead, n_tiles);
+    else if (warp == F::kWatch) tc_watch(p, bars, &s_dead, n_tiles);
+    else if (warp < F::kIssueS) tc_softmax<kN>(p, smem, bars, tmem, &s_dead, s_info, s_len, share.first, n_tiles, s_draft);
     // every MMA completes before the tensor memory is given back (where a wait gave up
     // and the last one was not issued, this wait gives those in flight a second)
     if (warp == 0 && !mbar_wait_bounded(&bars.o_done[(n_tiles - 1) & 1], (uint32_t)((n_tiles - 1) >> 1) & 1) && threadIdx.x == 0)
