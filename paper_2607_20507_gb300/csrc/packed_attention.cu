@@ -241,9 +241,9 @@ __device__ __forceinline__ long long build_prefix(const PackedAttnParams& p, int
 __device__ __forceinline__ uint2 query_f16(uint2 x, float& back) {
     const float f[4] = {__uint_as_float(x.x << 16), __uint_as_float(x.x & 0xffff0000u), __uint_as_float(x.y << 16),
                         __uint_as_float(x.y & 0xffff0000u)};
-    float top = fmaxf(fmaxf(fabsf(f[0]), fabsf(f[1])), fmaxf(fabsf(f[2]), fabsf(f[3])));
-#pragma unroll
-    for (int off = 16; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
+    // (of magnitudes, whose order is that of their bits)
+    const float top = __uint_as_float(__reduce_max_sync(
+        0xffffffffu, __float_as_uint(fmaxf(fmaxf(fabsf(f[0]), fabsf(f[1])), fmaxf(fabsf(f[2]), fabsf(f[3]))))));
     // top = 1.m x 2^e -> 1.m x 2^14; 2^(14 - e) in two halves, neither of which leaves fp32
     const int e = (int)(__float_as_uint(top) >> 23) - 127;
     const int up = top > 0.f ? 14 - e : 0, u0 = up / 2, u1 = up - u0;

@@ -329,7 +329,7 @@ __device__ __forceinline__ void tc_decode(const PackedAttnParams& p, uint8_t* sm
             const __nv_bfloat16* const from =
                 p.q + ((size_t)bg * p.R * p.Hq + (size_t)head * p.G + row0) * kPackDim + 4 * lane;
             auto place = [&](int row) { return s_q + row * 128 + ((((lane & 15) >> 1) ^ (row & 7)) << 4); };
-#pragma unroll 1
+#pragma unroll 4
             for (int row = warp; row < kN; row += 4) {
                 const bool in = row < n_live;   // row (i, g) lies i Hq + g rows past its head's first one
                 const __nv_bfloat16* src = from + (in ? (size_t)(s_draft[row0 + row] * (p.Hq - p.G) + row) * kPackDim : 0);
@@ -339,7 +339,7 @@ __device__ __forceinline__ void tc_decode(const PackedAttnParams& p, uint8_t* sm
             }
             cp_async_commit();
             cp_async_wait<0>();
-#pragma unroll 1
+#pragma unroll 4
             for (int row = warp; row < kN; row += 4) {
                 float back;
                 uint2* const at = reinterpret_cast<uint2*>(place(row));
