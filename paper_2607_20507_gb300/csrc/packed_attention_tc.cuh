@@ -315,10 +315,15 @@ __device__ __forceinline__ void tc_decode(const PackedAttnParams& p, uint8_t* sm
     for (int j = set; j < n_tiles; j += F::kSets) {
         const int buf = j & 1;
         const uint32_t ph = (uint32_t)(j >> 1) & 1;
+        // ---- what was in the place of this tile's row is read
+        if (j >= 2) tc_wait(v_side ? &bars.o_done[buf] : &bars.s_full[buf], ph ^ 1, dead, p.status);
+        tc_fence_after();
         if (!v_side && (j == 0 || cur.t == 0)) {
             // ---- a new piece: its query rows as fp16 below 2^15 (as in the other form),
             // a lane its four dims of a row, converted where they arrive.  (Their buffer was
-            // read last by the tile two before, or an earlier one.)
+            // read last by the tile two before, or an earlier one.  This wait is right only
+            // after the one above: S of that tile is issued after P of the tile two before it,
+            // and a parity does not tell a phase from the one two before.)
             if (j >= 2) tc_wait(&bars.p_full[buf], ph ^ 1, dead, p.status);
             // the KV head of the span, and its row block's first row
             const int bg = p.b_base + cur.b;
@@ -351,10 +356,7 @@ __device__ __forceinline__ void tc_decode(const PackedAttnParams& p, uint8_t* sm
             __syncwarp();
             if (lane == 0) mbar_arrive(&bars.q_full[piece & 1]);
         }
-        // ---- this tile's row, once what was in its place is read, and the request of
-        // that two tiles on
-        if (j >= 2) tc_wait(v_side ? &bars.o_done[buf] : &bars.s_full[buf], ph ^ 1, dead, p.status);
-        tc_fence_after();
+        // ---- this tile's row, and the request of that two tiles on
         cp_async_wait<2 - F::kSets>();
         __syncwarp();
         decode(buf);
