@@ -269,6 +269,8 @@ packed_attention_kernel(const PackedAttnParams p) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int r = lane >> 2, c = lane & 3;
     const int nb = p.n_batch, X0 = p.span_x;
+    // (read from the first span on, after the barriers below)
+    for (int row = threadIdx.x; row < F::kRows; row += F::kThreads) s_draft[row] = row / p.G;
     wait_prior_grid();
     allow_dependent_launch();
 
@@ -291,7 +293,6 @@ packed_attention_kernel(const PackedAttnParams p) {
     const int n_tiles = share.n_tiles;
     __syncthreads();   // the prefix gives way to the ring
     if (n_tiles <= 0) return;
-    for (int row = threadIdx.x; row < F::kRows; row += F::kThreads) s_draft[row] = row / p.G;
 
     // ---- the ring.  Lane g (mod 4) looks up the page of keys 8 g .. 8 g + 7 of
     // the next tile to load, one tile ahead.
