@@ -25,11 +25,11 @@
 // products of their own, which the softmax warps add to O.  Mending is rolled up, for
 // the instruction cache's sake.
 //
-// What bounds it: up to 48 columns the decoding warps, above the softmax warps, each
-// at some 2400 to 3300 cycles a tile where its instructions alone would take 1100:
-// chains of waits (a try_wait that succeeds costs 160 cycles, a vote 60 and the
-// warps' drift), shared-memory and conversion latencies; the tensor pipe is 20%
-// busy, DRAM 20%.  64 requests of 4096 keys and 8 KV heads: 32 rows 138 us, 36 148;
+// What bounds it: the softmax warps, at some 2300 (48 columns) to 3200 cycles (80) a
+// tile (one set of decoding warps takes 2400), where the SM's instructions alone would
+// take 1100 to 1500: chains of waits (a try_wait that succeeds costs 160 cycles, a vote
+// 60 and the warps' drift), shared-memory and conversion latencies; the tensor pipe is
+// 23 to 30% busy, DRAM 21 to 27%.  64 requests of 4096 keys and 8 KV heads: 32 rows 138 us, 36 148;
 // 32 requests: 56 rows 96, 72 104; 256 requests of up to 16384 keys, 72 rows: 1.33 ms
 // for 2.8 GB (the same attention over a bf16 cache: 1.72 ms for 10 GB).  A CTA that
 // does everything in turn, two an SM, took 2.03 ms.
