@@ -7,10 +7,10 @@
 // atomics are additions to whole numbers.
 //
 // What bounds them: a fork and a release are chains of a few dependent loads
-// and the launches (a release and a fork of 4 rows 10 us, of 192 rows 19); a
+// and the launches (a release and a fork of 4 rows 10 us, of 192 rows 16); a
 // compaction reads the counts twice and the table once and then copies pages at
-// the memory's rate: 26,637 pages of 18 KB take 181 us, 5.4 TB/s; 239 of 128 KB,
-// 22.6 us, three launches and 31 MB each way.
+// the memory's rate: 26,637 pages of 18 KB take 178 us, 5.5 TB/s; 239 of 128 KB,
+// 20.5 us, two launches and 31 MB each way.
 #include "cs_internal.h"
 #include "cs_device.cuh"
 
@@ -61,6 +61,26 @@ __device__ __forceinline__ int block_scan(int v, int* s_warp, int& total) {
     return before + inc - v;
 }
 
+// Of the 16 pages from base + 16 threadIdx.x on, which have a count of 0 (kFree) or
+// another (else): a bit each.  A warp reads its 512 counts 32 at a time (a thread its
+// own 16 would touch every sector eight times); all of it takes part.
+constexpr int kPer = 16;
+template <bool kFree>
+__device__ __forceinline__ uint32_t pages_of(const PageParams& p, long long base) {
+    const int lane = threadIdx.x & 31;
+    const long long first = base + (long long)(threadIdx.x & ~31) * kPer + lane;
+    int v[kPer];
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) v[j] = first + 32 * j < p.P ? __ldcg(p.refs + first + 32 * j) : kFree ? 1 : 0;
+    uint32_t mine = 0;
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) {
+        const uint32_t all = __ballot_sync(0xffffffffu, (v[j] == 0) == kFree);
+        if (lane >> 1 == j) mine = all;
+    }
+    return lane & 1 ? mine >> 16 : mine & 0xffffu;
+}
+
 // A warp copies piece `piece` of page `src` to page `dst`.
 __device__ __forceinline__ void copy_piece(const PagePools& pools, long long src, long long dst, uint32_t piece) {
     int i = 0;
@@ -98,7 +118,6 @@ __device__ __forceinline__ ForkRequest fork_request(const PageParams& p, const i
 }
 
 constexpr int kFindThreads = 1024;
-constexpr int kFindPer = 16;   // counts a thread takes at a time
 
 // One CTA: first[i], how many free pages the requests before i take, and the
 // lowest free pages, as many as all of them take (found: how many there were).
@@ -118,12 +137,9 @@ __global__ void __launch_bounds__(kFindThreads) fork_find_kernel(const PageParam
         want += total;
     }
     int have = 0;
-    for (long long base = 0; base < p.P && have < want; base += kFindThreads * kFindPer) {
-        const long long id = base + threadIdx.x * kFindPer;
-        uint32_t is_free = 0;
-#pragma unroll
-        for (int j = 0; j < kFindPer; ++j)
-            if (id + j < p.P && __ldcg(p.refs + id + j) == 0) is_free |= 1u << j;
+    for (long long base = 0; base < p.P && have < want; base += kFindThreads * kPer) {
+        const long long id = base + threadIdx.x * kPer;
+        uint32_t is_free = pages_of<true>(p, base);
         int total;
         int at = have + block_scan<kFindThreads>(__popc(is_free), s_warp, total);
         for (; is_free; is_free &= is_free - 1, ++at)
@@ -197,8 +213,7 @@ __global__ void __launch_bounds__(kReleaseThreads) release_kernel(const PagePara
 
 // ---------------------------------------------------------------- compact
 constexpr int kCountThreads = 256;
-constexpr int kCountPer = 16;
-constexpr int kCountTile = kCountThreads * kCountPer;   // pages a CTA counts
+constexpr int kCountTile = kCountThreads * kPer;   // pages a CTA counts
 
 struct CompactParams {
     int* tile_live;      // [tiles] pages in use in each tile of counts; NULL: not counted before
@@ -209,20 +224,12 @@ struct CompactParams {
     int tiles;
 };
 
-__device__ __forceinline__ uint32_t live_bits(const PageParams& p, long long id) {
-    uint32_t live = 0;
-#pragma unroll
-    for (int j = 0; j < kCountPer; ++j)
-        if (id + j < p.P && __ldcg(p.refs + id + j) != 0) live |= 1u << j;
-    return live;
-}
-
 __global__ void __launch_bounds__(kCountThreads) compact_count_kernel(const PageParams p, const CompactParams c) {
     __shared__ int s_warp[kCountThreads / 32];
     wait_prior_grid();
     allow_dependent_launch();
     int total;
-    block_scan<kCountThreads>(__popc(live_bits(p, (long long)blockIdx.x * kCountTile + threadIdx.x * kCountPer)), s_warp,
+    block_scan<kCountThreads>(__popc(pages_of<false>(p, (long long)blockIdx.x * kCountTile)), s_warp,
                               total);
     if (threadIdx.x == 0) c.tile_live[blockIdx.x] = total;
 }
@@ -241,16 +248,18 @@ __global__ void __launch_bounds__(kCountThreads) compact_rank_kernel(const PageP
         block_scan<kCountThreads>(v, s_warp, total);
         return total;
     };
+    const long long mine = (long long)blockIdx.x * kCountTile, id0 = mine + threadIdx.x * kPer;
+    const uint32_t own = pages_of<false>(p, mine);
+    auto live_of = [&](long long base) { return base == mine ? own : pages_of<false>(p, base); };
     // f(the pages in use of a stretch, its first id): stretches of a tile, or, where
     // they are not counted before, of a thread's counts
     auto each = [&](auto f) {
         if (c.tile_live) {
             for (int t = threadIdx.x; t < c.tiles; t += kCountThreads) f(__ldcg(c.tile_live + t), (long long)t * kCountTile);
         } else {
-            for (long long id = threadIdx.x * kCountPer; id < p.P; id += kCountTile) f(__popc(live_bits(p, id)), id);
+            for (long long base = 0; base < p.P; base += kCountTile) f(__popc(live_of(base)), base + threadIdx.x * kPer);
         }
     };
-    const long long mine = (long long)blockIdx.x * kCountTile;
     int before = 0, all = 0;
     each([&](int live, long long id) {
         all += live;
@@ -259,28 +268,26 @@ __global__ void __launch_bounds__(kCountThreads) compact_rank_kernel(const PageP
     const int N = sum(all);
     before = sum(before);
     // pages in use below N: the stretches that end there, and the one that N lies in
-    const int stretch = c.tile_live ? kCountTile : kCountPer;
+    const int stretch = c.tile_live ? kCountTile : kPer;
     int below = 0;
     each([&](int live, long long id) {
         if (id + stretch <= N) below += live;
     });
     {
-        const long long id = (long long)N / stretch * stretch + threadIdx.x * kCountPer;
-        const uint32_t live = id < N ? live_bits(p, id) : 0;
+        const long long base = (long long)N / kCountTile * kCountTile, id = base + threadIdx.x * kPer;
+        const uint32_t live = live_of(base);
 #pragma unroll
-        for (int j = 0; j < kCountPer; ++j)
-            if (id + j < N && (live >> j & 1)) ++below;
+        for (int j = 0; j < kPer; ++j)
+            if (id + j >= (long long)N / stretch * stretch && id + j < N && (live >> j & 1)) ++below;
     }
     below = sum(below);
-    const long long id0 = (long long)blockIdx.x * kCountTile + threadIdx.x * kCountPer;
-    const uint32_t live = live_bits(p, id0);
     int total;
-    int at = before + block_scan<kCountThreads>(__popc(live), s_warp, total);
+    int at = before + block_scan<kCountThreads>(__popc(own), s_warp, total);
 #pragma unroll
-    for (int j = 0; j < kCountPer; ++j) {
+    for (int j = 0; j < kPer; ++j) {
         const int id = (int)(id0 + j);
         if (id0 + j >= p.P) break;
-        const bool on = live >> j & 1;
+        const bool on = own >> j & 1;
         if (id < N && !on) c.dst[id - at] = id;
         if (id >= N) {
             c.rank[id] = on ? at - below : -1;
