@@ -38,22 +38,22 @@ __device__ __forceinline__ int clamped_len(const PageParams& p, int L) {
     return max(0, min(L, p.max_pages * p.ps));
 }
 
-// Inclusive sum over the block's threads before this one, and the block's total.
-template <int kThreads>
-__device__ __forceinline__ int block_scan(int v, int* s_warp, int& total) {
+// Sum over the block's threads before this one, and the block's total.
+template <int kThreads, class T>
+__device__ __forceinline__ T block_scan(T v, T* s_warp, T& total) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    int inc = v;
+    T inc = v;
 #pragma unroll
     for (int off = 1; off < 32; off <<= 1) {
-        const int y = __shfl_up_sync(0xffffffffu, inc, off);
+        const T y = __shfl_up_sync(0xffffffffu, inc, off);
         if (lane >= off) inc += y;
     }
     __syncthreads();   // (s_warp of the scan before)
     if (lane == 31) s_warp[warp] = inc;
     __syncthreads();
-    int before = 0, all = 0;
+    T before = 0, all = 0;
     for (int w = 0; w < kThreads / 32; ++w) {
-        const int x = s_warp[w];
+        const T x = s_warp[w];
         if (w < warp) before += x;
         all += x;
     }
@@ -119,20 +119,23 @@ __device__ __forceinline__ ForkRequest fork_request(const PageParams& p, const i
 
 constexpr int kFindThreads = 1024;
 
-// One CTA: first[i], how many free pages the requests before i take, and the
-// lowest free pages, as many as all of them take (found: how many there were).
+// One CTA: first[i], how many free pages the requests before i ask for, and the
+// lowest free pages, as many as all of them ask for (found: how many are listed).
+// What is asked for is summed in 64 bits: a request may want 2^30 pages, whatever
+// the pool holds.
 __global__ void __launch_bounds__(kFindThreads) fork_find_kernel(const PageParams p, const int32_t* src,
                                                                  const int32_t* dst, int n, int room,
                                                                  long long* first, int32_t* free_ids, int* found) {
     __shared__ int s_warp[kFindThreads / 32];
+    __shared__ long long s_asked[kFindThreads / 32];
     wait_prior_grid();
     allow_dependent_launch();
     long long want = 0;
-    for (int base = 0; base < n; base += kFindThreads) {
-        const int i = base + threadIdx.x;
-        const int own = i < n ? fork_request(p, src, dst, i, room).own : 0;
-        int total;
-        const int before = block_scan<kFindThreads>(own, s_warp, total);
+    for (long long base = 0; base < n; base += kFindThreads) {
+        const long long i = base + threadIdx.x;
+        const long long own = i < n ? fork_request(p, src, dst, (int)i, room).own : 0;
+        long long total;
+        const long long before = block_scan<kFindThreads>(own, s_asked, total);
         if (i < n) first[i] = want + before;
         want += total;
     }
@@ -146,7 +149,7 @@ __global__ void __launch_bounds__(kFindThreads) fork_find_kernel(const PageParam
             if (at < want) free_ids[at] = (int)(id + __ffs(is_free) - 1);
         have += total;
     }
-    if (threadIdx.x == 0) *found = have;
+    if (threadIdx.x == 0) *found = (int)min((long long)have, want);
 }
 
 constexpr int kForkThreads = 256;
