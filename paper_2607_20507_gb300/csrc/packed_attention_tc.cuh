@@ -761,7 +761,7 @@ __device__ __forceinline__ void tc_softmax(const PackedAttnParams& p, uint8_t* s
                 const int row = kC0 + i + k;
                 if (row >= n_live) continue;
                 const float v = o[k] * s_inv[row];
-                if (whole) dst[(s_draft[row0 + row] * (p.Hq - p.G) + row) * kPackDim] = __float2bfloat16(v);
+                if (whole) dst[(size_t)(s_draft[row0 + row] * (p.Hq - p.G) + row) * kPackDim] = __float2bfloat16(v);
                 else part[row * kPackDim] = v;
             }
         }
