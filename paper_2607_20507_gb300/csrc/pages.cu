@@ -368,7 +368,7 @@ PagePools page_pools(const cs_page_pool* pools, int n) {
     return q;
 }
 
-int tiles_of_counts(int P) { return (P + kCountTile - 1) / kCountTile; }
+int tiles_of_counts(int P) { return (int)(((long long)P + kCountTile - 1) / kCountTile); }
 
 }  // namespace
 
