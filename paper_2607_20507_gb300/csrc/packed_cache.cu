@@ -116,12 +116,13 @@ __device__ __forceinline__ void append_group(const PackedSide& side, const uint4
     if (plain && unit > kSmall) {
         // x / unit correctly rounded from the correctly rounded reciprocal: one
         // step from x * (1 / unit) with the remainder (Markstein, 1990), three
-        // operations in place of a division
+        // operations in place of a division.  (The remainder as q unit - x: with it a
+        // quotient of -0 stays one.)
         const float inv = __frcp_rn(unit);
 #pragma unroll
         for (int j = 0; j < 16; ++j) {
             const float q = __fmul_rn(x[j], inv);
-            x[j] = __fmaf_rn(__fmaf_rn(-q, unit, x[j]), inv, q);
+            x[j] = __fmaf_rn(-__fmaf_rn(q, unit, -x[j]), inv, q);
         }
     } else {
 #pragma unroll
