@@ -156,6 +156,13 @@ __global__ void __launch_bounds__(kThreads) packed_append_kernel(const PackedRow
     append_group(p.v, v0, v1, v_head, slot, a.g);
 }
 
+// a b rounded to odd: the odd one of its two neighbours in fp32, or itself.  What is
+// then rounded to fewer bits is as if rounded once.
+__device__ __forceinline__ float mul_to_odd(float a, float b) {
+    const float lo = __fmul_rd(a, b), hi = __fmul_ru(a, b);
+    return __float_as_uint(lo) & 1u ? lo : hi;
+}
+
 // The values of a group's codes, in bf16.
 __device__ __forceinline__ void group_values(const uint2& c, uint32_t s, float head, uint4& x, uint4& y) {
     const uint32_t sc = scales_f16x2(s | s << 8);
@@ -165,7 +172,7 @@ __device__ __forceinline__ void group_values(const uint2& c, uint32_t s, float h
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
         const uint32_t z = mul_f16x2(v[j], sc);
-        r[j] = pack_bf16x2(__fmul_rn(f16_lo(z), head), __fmul_rn(f16_hi(z), head));
+        r[j] = pack_bf16x2(mul_to_odd(f16_lo(z), head), mul_to_odd(f16_hi(z), head));
     }
     x = make_uint4(r[0], r[1], r[2], r[3]);
     y = make_uint4(r[4], r[5], r[6], r[7]);
