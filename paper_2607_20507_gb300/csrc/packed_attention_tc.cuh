@@ -36,7 +36,8 @@
 //
 // Every mbarrier wait is bounded; after one that gives up nothing waits or is
 // issued any more, every warp still meets every block barrier, and the status
-// word says so.
+// word says so.  A warp that issues products waits for its own at its end, so that
+// none is in flight when the tensor memory is given back (drain).
 
 constexpr int kTcTile = 128;                       // keys of a tile: the MMAs' M (S) and K (O)
 constexpr int kTcVBytes = kTcTile * 256;           // V of a tile in fp16
@@ -203,8 +204,18 @@ struct TcBars {
     uint64_t p_full[2];    // P of a tile written, its S read (8 warps)
     uint64_t o_done[2];    // O of a tile done; its P and V are read
     uint64_t f_done;       // a product of faint weights done
+    uint64_t drained[3];   // a warp's products done, at its end: one phase each
     int starts[2];         // whether a tile's products start O (1) and the sums (2); written before p_full
 };
+
+// The end of a warp that issued products: all of them are done, or a second has
+// passed.  (On a barrier of a single phase: where a wait gave up, those of the buffers
+// may be a phase behind, which a parity does not tell.)
+__device__ __forceinline__ void tc_drain(uint64_t* drained, int* status) {
+    if (elect_one()) tc_commit(drained);
+    __syncwarp();
+    if (!mbar_wait_bounded(drained, 0) && elect_one()) atomicOr(status, CS_DEVICE_WAIT_TIMEOUT);
+}
 
 // V^T P^T, n columns of P from an atom's first on, into the columns from d on
 // (one thread issues): 8 steps of 16 keys.
@@ -417,6 +428,7 @@ __device__ __forceinline__ void tc_issue_scores(const PackedAttnParams& p, uint8
         __syncwarp();
         advance(cur, s_len, p.n_batch, p.n_spans, kTcTile);
     }
+    tc_drain(&bars.drained[0], p.status);
 }
 
 // A warp: the products for O and the sums.
@@ -440,6 +452,7 @@ __device__ __forceinline__ void tc_issue_values(const PackedAttnParams& p, uint8
         }
         __syncwarp();
     }
+    tc_drain(&bars.drained[1], p.status);
 }
 
 // A warp: takes part in a tile's vote once the place of its P is free, so that the
@@ -777,6 +790,8 @@ __device__ __forceinline__ void tc_softmax(const PackedAttnParams& p, uint8_t* s
         advance(cur, s_len, nb, p.n_spans, kTcTile);
         workers_sync();   // (the columns' words are free)
     }
+    // (faint weights' products are waited for one by one, unless a wait gave up)
+    if (warp == 0 && !alive(dead)) tc_drain(&bars.drained[2], p.status);
 }
 
 template <int kN>
@@ -805,6 +820,7 @@ __global__ void __launch_bounds__(TcForm<kN>::kThreads, 1) packed_attention_tc_k
             mbar_init(&bars.o_done[i], 1);
         }
         mbar_init(&bars.f_done, 1);
+        for (int i = 0; i < 3; ++i) mbar_init(&bars.drained[i], 1);
         fence_barrier_init();
     }
     for (int row = threadIdx.x; row < 2 * kTcMaxRows; row += F::kThreads) s_draft[row] = row / p.G;
@@ -849,10 +865,6 @@ __global__ void __launch_bounds__(TcForm<kN>::kThreads, 1) packed_attention_tc_k
     else if (warp == F::kIssueO) tc_issue_values<kN>(p, smem, bars, tmem, &s_dead, n_tiles);
     else if (warp == F::kWatch) tc_watch(p, bars, &s_dead, n_tiles);
     else if (warp < F::kIssueS) tc_softmax<kN>(p, smem, bars, tmem, &s_dead, s_info, s_len, share.first, n_tiles, s_draft);
-    // every MMA completes before the tensor memory is given back (where a wait gave up
-    // and the last one was not issued, this wait gives those in flight a second)
-    if (warp == 0 && !mbar_wait_bounded(&bars.o_done[(n_tiles - 1) & 1], (uint32_t)((n_tiles - 1) >> 1) & 1) && threadIdx.x == 0)
-        atomicOr(p.status, CS_DEVICE_WAIT_TIMEOUT);
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
