@@ -640,10 +640,10 @@ cs_status cs_logprobs(const cs_logprob_dims* dims, const void* logits, const int
 cs_status cs_read_device_status(const void* workspace, int32_t* status_out, cs_stream_t stream);
 
 /*
- * Failure-detection self-test.  Enqueues one kernel whose single thread runs
- * the bounded mbarrier wait that every wait of the attention kernels uses, on
- * a barrier that nothing completes.  After about one second the wait gives up
- * and the thread sets CS_DEVICE_WAIT_TIMEOUT in the status word, the first 4
+ * Failure-detection self-test.  Enqueues one kernel that runs the bounded
+ * mbarrier wait of the attention kernels and that of packed attention, each on
+ * a barrier that nothing completes.  After about one second both give up
+ * and the kernel sets CS_DEVICE_WAIT_TIMEOUT in the status word, the first 4
  * bytes of `workspace` (a device buffer of at least 4 bytes, 4-byte aligned,
  * owned by the caller; nothing else in it is touched).  Read the word with
  * cs_read_device_status.  No fault, trap or hang: the context stays usable.

@@ -48,6 +48,7 @@
 
 #include <type_traits>
 
+#include "bounded_wait.cuh"
 #include "cs_internal.h"
 #include "packed.cuh"
 

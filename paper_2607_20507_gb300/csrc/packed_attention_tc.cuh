@@ -42,7 +42,6 @@
 constexpr int kTcTile = 128;                       // keys of a tile: the MMAs' M (S) and K (O)
 constexpr int kTcVBytes = kTcTile * 256;           // V of a tile in fp16
 constexpr int kTcRowBytes = kTcTile * (kPackCodeBytes + kPackGroups);   // codes and scales of K or V of a tile
-constexpr long long kTcPatience = 2000000000;      // cycles: a second or so
 constexpr int kTcMaxRows = 80;                     // query rows of a span at most
 
 template <int kN>
@@ -161,39 +160,6 @@ __device__ __forceinline__ int ordered(float x) {
     return b < 0 ? b ^ 0x7fffffff : b;
 }
 __device__ __forceinline__ float unordered(int b) { return __int_as_float(b < 0 ? b ^ 0x7fffffff : b); }
-
-// Waits for the phase of the given parity, asleep for up to 20 us.
-__device__ __forceinline__ bool tc_asleep(uint64_t* bar, uint32_t parity) {
-    uint32_t done;
-    asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, 20000;\n\t"
-        "selp.u32 %0, 1, 0, p;\n\t}\n"
-        : "=r"(done)
-        : "r"(smem_u32(bar)), "r"(parity)
-        : "memory");
-    return done != 0;
-}
-// Bounded (about one second); returns at once when another wait has given up.
-// (Out of line: the loop's code is long.  try_wait sleeps for some 150 cycles at
-// most, whatever it is told: between looks at the clock, 64 of them.)
-__device__ __noinline__ void tc_wait_long(uint64_t* bar, uint32_t parity, volatile int* dead, int* status) {
-    const long long t0 = clock64();
-    while (!*dead) {
-#pragma unroll 1
-        for (int i = 0; i < 64; ++i)
-            if (tc_asleep(bar, parity)) return;
-        if (clock64() - t0 > kTcPatience) {
-            *dead = 1;
-            atomicOr(status, CS_DEVICE_WAIT_TIMEOUT);
-        }
-    }
-}
-__device__ __forceinline__ void tc_wait(uint64_t* bar, uint32_t parity, volatile int* dead, int* status) {
-    if (!tc_asleep(bar, parity)) tc_wait_long(bar, parity, dead, status);
-}
-// Whether no wait has given up, the same answer in the whole warp.
-__device__ __forceinline__ bool alive(volatile int* dead) { return !__any_sync(0xffffffffu, *dead); }
 
 // Tile j uses those of j % 2, whose phase j / 2 is its own.
 struct TcBars {

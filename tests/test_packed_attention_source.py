@@ -21,3 +21,11 @@ def test_warps_that_issue_products_wait_for_them_at_their_end():
     kernel = text[text.index("packed_attention_tc_kernel(const"):]
     assert kernel.index("tc_softmax<") < kernel.rindex("__syncthreads()") < kernel.index("tcgen05.dealloc")
     assert len(re.findall(r"mbar_init\(&bars\.drained\[i\], 1\)", kernel)) == 1
+
+
+def test_the_self_test_runs_the_bounded_waits():
+    """Packed attention waits on mbarriers by two functions alone, and the self-test lets both run out."""
+    selftest = (SOURCE.parent / "selftest.cu").read_text()
+    assert "!mbar_wait_bounded(" in selftest and re.search(r"\btc_wait\(", selftest)
+    for f in (SOURCE, SOURCE.with_name("packed_attention.cu")):
+        assert not re.search(r"mbarrier\.|mbar_(try|test)_wait|tc_asleep|tc_wait_long", f.read_text()), f.name
