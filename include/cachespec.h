@@ -634,7 +634,8 @@ cs_status cs_logprobs(const cs_logprob_dims* dims, const void* logits, const int
  * used it finished normally; otherwise a bit set of CS_DEVICE_* flags (a
  * bounded wait inside a kernel gave up, so that call's output is invalid).
  * Copies 4 bytes to the host and SYNCHRONISES `stream`.  The word is sticky
- * until the caller zero-fills the workspace again.
+ * until the caller zero-fills the workspace again; in a workspace of
+ * cs_packed_verify_attention it tells of the latest call alone.
  */
 #define CS_DEVICE_WAIT_TIMEOUT 1
 cs_status cs_read_device_status(const void* workspace, int32_t* status_out, cs_stream_t stream);

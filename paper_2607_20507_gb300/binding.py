@@ -725,6 +725,17 @@ def cs_packed_kv_read(pool, page_table, ctx_lens, n_rows: int, stream: int | Non
     return tuple(out)
 
 
+def packed_attn_dims(q: torch.Tensor, pool: PackedPool, page_table: torch.Tensor, sm_scale: float = 0.0) -> AttnDims:
+    return attn_dims(q, pool[0], page_table, sm_scale)
+
+
+def packed_verify_attention_workspace(dims: AttnDims, n_draft: int, device, stream: int | None = None) -> torch.Tensor:
+    """The default workspace of the (current) stream's calls of cs_packed_verify_attention with these dims: after one,
+    cs_read_device_status of it tells whether it finished normally."""
+    n = load_library().cs_packed_verify_attention_workspace_bytes(ctypes.byref(dims), int(n_draft))
+    return _cached_workspace("packed_attn", device, n, stream)
+
+
 def cs_packed_verify_attention(q, pool, page_table, ctx_lens, n_draft, out=None, workspace=None, sm_scale: float = 0.0,
                                stream: int | None = None):
     """Verify attention over a packed cache, ``n_draft`` in [0, 16]; returns ``out`` (bf16 [B, k+1, Hq, 128]).
@@ -918,7 +929,7 @@ def cs_selftest_wait_timeout(workspace: torch.Tensor, stream: int | None = None)
 
 
 def cs_read_device_status(workspace: torch.Tensor, stream: int | None = None) -> int:
-    """Status word of a verify-attention workspace (synchronises the stream)."""
+    """Status word of a verify-attention workspace, packed attention's among them (synchronises the stream)."""
     lib = load_library()
     v = ctypes.c_int32(0)
     _check(lib, lib.cs_read_device_status(_ptr(workspace), ctypes.byref(v),
