@@ -55,9 +55,17 @@ class Server:
     def rows(self, ids):
         return torch.tensor(ids, dtype=torch.int32, device=self.model.dev)
 
+    def pool_groups(self):
+        """The cache's tensors, as many at a time as a call takes."""
+        m = cs.CS_MAX_PAGE_POOLS
+        return [self.page_pools[i:i + m] for i in range(0, len(self.page_pools), m)]
+
     def fork(self, src, dst, room):
-        return cs.cs_kv_fork(self.page_pools, self.table, self.lens, self.counts, self.rows(src), self.rows(dst),
-                             self.page_size, room)
+        first, *rest = self.pool_groups()
+        ok = cs.cs_kv_fork(first, self.table, self.lens, self.counts, self.rows(src), self.rows(dst), self.page_size, room)
+        for pools in rest:
+            cs.cs_kv_fork_more(pools, self.table, self.counts, len(src))
+        return ok
 
     def prefill(self, row, n):
         """An empty row with pages for a prompt of n tokens, and the prompt's keys and values."""
@@ -96,7 +104,11 @@ class Server:
         cs.cs_kv_release(self.table, self.lens, self.counts, self.rows(ids), self.rows([0] * len(ids)), self.page_size)
 
     def compact(self):
-        return cs.cs_kv_compact(self.page_pools, self.table, self.counts)
+        first, *rest = self.pool_groups()
+        live = cs.cs_kv_compact(first, self.table, self.counts)
+        for pools in rest:
+            cs.cs_kv_compact_more(pools, self.table, self.counts)
+        return live
 
 
 def main(argv=None):

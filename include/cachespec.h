@@ -38,9 +38,10 @@
  *                       -- the same paged cache held in 4 bits a value: rows
  *                          are quantised as they are appended, and verify
  *                          attention (or single-token decoding) reads them;
- *   cs_kv_fork,
+ *   cs_kv_fork, cs_kv_fork_more,
  *   cs_kv_release,
- *   cs_kv_compact       -- the pages of any of these caches: rows of the page
+ *   cs_kv_compact, cs_kv_compact_more
+ *                       -- the pages of any of these caches: rows of the page
  *                          table share pages, give them back, and the pages in
  *                          use move together;
  *   cs_logprobs         -- log probabilities of given tokens with the entropy
@@ -555,6 +556,12 @@ cs_status cs_packed_verify_attention(const cs_attn_dims* dims, const void* q, co
  * max_pages_per_seq entries of all R rows).  out_live[0] = N: pages from N on
  * are free.  Page contents at the old ids stay as they were.
  *
+ * cs_kv_fork_more, cs_kv_compact_more: the page copies of the latest cs_kv_fork
+ * (cs_kv_compact) that used this workspace, in further pools: for caches of more
+ * than CS_MAX_PAGE_POOLS arrays.  As many calls as it takes, with the dims (and n) of
+ * that call, ordered after it on the stream and before anything that reads those
+ * pools; no other call may use the workspace in between.
+ *
  *   pools        host array of n_pools in [0, CS_MAX_PAGE_POOLS]; data 16-byte
  *                aligned, page_bytes a positive multiple of 16
  *   page_table   int32 [R, max_pages_per_seq], ctx_lens int32 [R],
@@ -583,12 +590,16 @@ size_t cs_kv_fork_workspace_bytes(const cs_page_dims* dims, int32_t n);
 cs_status cs_kv_fork(const cs_page_dims* dims, const cs_page_pool* pools, int32_t n_pools, int32_t* page_table,
                      int32_t* ctx_lens, int32_t* ref_counts, const int32_t* src, const int32_t* dst, int32_t n,
                      int32_t room, int32_t* out_forked, void* workspace, size_t workspace_bytes, cs_stream_t stream);
+cs_status cs_kv_fork_more(const cs_page_dims* dims, const cs_page_pool* pools, int32_t n_pools, int32_t n,
+                          void* workspace, size_t workspace_bytes, cs_stream_t stream);
 cs_status cs_kv_release(const cs_page_dims* dims, int32_t* page_table, int32_t* ctx_lens, int32_t* ref_counts,
                         const int32_t* rows, const int32_t* keep_lens, int32_t n, cs_stream_t stream);
 size_t cs_kv_compact_workspace_bytes(const cs_page_dims* dims);
 cs_status cs_kv_compact(const cs_page_dims* dims, const cs_page_pool* pools, int32_t n_pools, int32_t* page_table,
                         int32_t* ref_counts, int32_t* out_live, void* workspace, size_t workspace_bytes,
                         cs_stream_t stream);
+cs_status cs_kv_compact_more(const cs_page_dims* dims, const cs_page_pool* pools, int32_t n_pools, void* workspace,
+                             size_t workspace_bytes, cs_stream_t stream);
 
 /*
  * Log probabilities of given tokens (what a server answers beside the tokens

@@ -37,7 +37,8 @@ EXPORTED_SYMBOLS = ("cs_abi_version", "cs_last_error", "cs_verify_attention_work
                     "cs_kv_commit_tree", "cs_selftest_wait_timeout",
                     "cs_packed_kv_append", "cs_packed_kv_read", "cs_packed_verify_attention_workspace_bytes",
                     "cs_packed_verify_attention", "cs_kv_fork_workspace_bytes", "cs_kv_fork", "cs_kv_release",
-                    "cs_kv_compact_workspace_bytes", "cs_kv_compact", "cs_logprobs")
+                    "cs_kv_compact_workspace_bytes", "cs_kv_compact", "cs_logprobs", "cs_kv_fork_more",
+                    "cs_kv_compact_more")
 CS_MAX_TOP = 32
 CS_MAX_PAGE_POOLS = 128
 
@@ -183,6 +184,10 @@ def load_library(path: str | None = None):
         lib.cs_kv_compact_workspace_bytes.argtypes = [ctypes.POINTER(PageDims)]
         lib.cs_kv_compact.restype = ctypes.c_int
         lib.cs_kv_compact.argtypes = [ctypes.POINTER(PageDims), ctypes.POINTER(PagePool), i32, vp, vp, vp, vp, sz, vp]
+        lib.cs_kv_fork_more.restype = ctypes.c_int
+        lib.cs_kv_fork_more.argtypes = [ctypes.POINTER(PageDims), ctypes.POINTER(PagePool), i32, i32, vp, sz, vp]
+        lib.cs_kv_compact_more.restype = ctypes.c_int
+        lib.cs_kv_compact_more.argtypes = [ctypes.POINTER(PageDims), ctypes.POINTER(PagePool), i32, vp, sz, vp]
         lib.cs_logprobs.restype = ctypes.c_int
         lib.cs_logprobs.argtypes = [ctypes.POINTER(LogprobDims), vp, vp, ctypes.c_float, vp, vp, vp, vp, vp]
         lib.cs_kv_commit_tree.restype = ctypes.c_int
@@ -818,6 +823,22 @@ def cs_kv_fork(pools, page_table, ctx_lens, ref_counts, src, dst, page_size: int
     return out
 
 
+def cs_kv_fork_more(pools, page_table, ref_counts, n: int, workspace=None, stream: int | None = None):
+    """The page copies of the fork of ``n`` rows before, in further pools: a cache of more than CS_MAX_PAGE_POOLS
+    tensors goes through cs_kv_fork with the first of them and through this with the others, up to that many a call.
+    ``workspace`` is that call's (None: the stream's default one, as there).  See include/cachespec.h."""
+    lib = load_library()
+    dev = page_table.device
+    d = _page_call(page_table, None, ref_counts, 1, dev)
+    arr, n_pools = _page_pools(pools, d.num_pages, dev)
+    if workspace is None:
+        workspace = _cached_workspace("fork", dev, lib.cs_kv_fork_workspace_bytes(ctypes.byref(d), int(n)), stream)
+    st = lib.cs_kv_fork_more(ctypes.byref(d), arr, n_pools, int(n), workspace.data_ptr(), workspace.nbytes,
+                             _stream(dev) if stream is None else stream)
+    if st:
+        _check(lib, st)
+
+
 def cs_kv_release(page_table, ctx_lens, ref_counts, rows, keep_lens, page_size: int, stream: int | None = None):
     """Rows ``rows`` keep the pages of their first ``keep_lens`` tokens and give the others back (in place)."""
     r = (_fast or _load_fast()).kv_release(page_table, ctx_lens, ref_counts, rows, keep_lens, page_size, stream)
@@ -857,6 +878,20 @@ def cs_kv_compact(pools, page_table, ref_counts, workspace=None, stream: int | N
     if st:
         _check(lib, st)
     return out
+
+
+def cs_kv_compact_more(pools, page_table, ref_counts, workspace=None, stream: int | None = None):
+    """The page copies of the compaction before, in further pools (as cs_kv_fork_more those of a fork)."""
+    lib = load_library()
+    dev = page_table.device
+    d = _page_call(page_table, None, ref_counts, 1, dev)
+    arr, n_pools = _page_pools(pools, d.num_pages, dev)
+    if workspace is None:
+        workspace = _cached_workspace("compact", dev, lib.cs_kv_compact_workspace_bytes(ctypes.byref(d)), stream)
+    st = lib.cs_kv_compact_more(ctypes.byref(d), arr, n_pools, workspace.data_ptr(), workspace.nbytes,
+                                _stream(dev) if stream is None else stream)
+    if st:
+        _check(lib, st)
 
 
 def cs_logprobs(logits, tokens, temperature: float = 1.0, n_top: int = 0, stream: int | None = None):

@@ -547,6 +547,35 @@ cs_status cs_kv_compact(const cs_page_dims* dims, const cs_page_pool* pools, int
                              reinterpret_cast<cudaStream_t>(stream));
 }
 
+cs_status cs_kv_fork_more(const cs_page_dims* dims, const cs_page_pool* pools, int32_t n_pools, int32_t n,
+                          void* workspace, size_t workspace_bytes, cs_stream_t stream) {
+    cs_status st = check_pages(dims);
+    if (st != CS_OK) return st;
+    st = check_page_pools(pools, n_pools);
+    if (st != CS_OK) return st;
+    if (n < 0) return fail(CS_ERR_INVALID_ARG, "n %d < 0", n);
+    if (n == 0 || n_pools == 0) return CS_OK;
+    const size_t need = fork_workspace_bytes(*dims, n);
+    if (!workspace || workspace_bytes < need)
+        return fail(CS_ERR_WORKSPACE, "workspace of %zu bytes given, %zu needed", workspace_bytes, need);
+    if (!aligned(workspace, 256)) return fail(CS_ERR_INVALID_ARG, "workspace must be 256-byte aligned");
+    return launch_kv_fork_more(*dims, pools, n_pools, n, workspace, reinterpret_cast<cudaStream_t>(stream));
+}
+
+cs_status cs_kv_compact_more(const cs_page_dims* dims, const cs_page_pool* pools, int32_t n_pools, void* workspace,
+                             size_t workspace_bytes, cs_stream_t stream) {
+    cs_status st = check_pages(dims);
+    if (st != CS_OK) return st;
+    st = check_page_pools(pools, n_pools);
+    if (st != CS_OK) return st;
+    if (n_pools == 0) return CS_OK;
+    const size_t need = compact_workspace_bytes(*dims);
+    if (!workspace || workspace_bytes < need)
+        return fail(CS_ERR_WORKSPACE, "workspace of %zu bytes given, %zu needed", workspace_bytes, need);
+    if (!aligned(workspace, 256)) return fail(CS_ERR_INVALID_ARG, "workspace must be 256-byte aligned");
+    return launch_kv_compact_more(*dims, pools, n_pools, workspace, reinterpret_cast<cudaStream_t>(stream));
+}
+
 cs_status cs_logprobs(const cs_logprob_dims* dims, const void* logits, const int32_t* tokens, float temperature,
                       float* out_logprob, float* out_entropy, int32_t* out_top_tokens, float* out_top_logprobs,
                       cs_stream_t stream) {

@@ -123,9 +123,13 @@ cs_status launch_kv_fork(const cs_page_dims& d, const cs_page_pool* pools, int n
                          int room, int32_t* out_forked, void* workspace, cudaStream_t stream);
 cs_status launch_kv_release(const cs_page_dims& d, int32_t* page_table, int32_t* ctx_lens, int32_t* ref_counts,
                             const int32_t* rows, const int32_t* keep_lens, int n, cudaStream_t stream);
+cs_status launch_kv_fork_more(const cs_page_dims& d, const cs_page_pool* pools, int n_pools, int n, void* workspace,
+                              cudaStream_t stream);
 size_t compact_workspace_bytes(const cs_page_dims& d);
 cs_status launch_kv_compact(const cs_page_dims& d, const cs_page_pool* pools, int n_pools, int32_t* page_table,
                             int32_t* ref_counts, int32_t* out_live, void* workspace, cudaStream_t stream);
+cs_status launch_kv_compact_more(const cs_page_dims& d, const cs_page_pool* pools, int n_pools, void* workspace,
+                                 cudaStream_t stream);
 
 // ------------------------------------------------------ log probabilities
 cs_status launch_logprobs(const cs_logprob_dims& d, const void* logits, const int32_t* tokens, float temperature,

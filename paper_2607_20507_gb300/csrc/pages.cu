@@ -1,5 +1,7 @@
 // pages.cu -- pages of a cache that rows of the page table share, give back and
-// that move together (cs_kv_fork, cs_kv_release, cs_kv_compact).
+// that move together (cs_kv_fork, cs_kv_release, cs_kv_compact; the copies of a fork
+// or a compaction in more pools than one call takes: cs_kv_fork_more,
+// cs_kv_compact_more).
 //
 // The counts alone say which pages are free, so there is no list to keep: a
 // fork takes the lowest free ids, found by a scan of the counts.  Every result
@@ -154,11 +156,13 @@ __global__ void __launch_bounds__(kFindThreads) fork_find_kernel(const PageParam
 
 constexpr int kForkThreads = 256;
 
-// CTA (request i, part y): part 0 writes the row; all parts copy the part-filled page.
+// CTA (request i, part y): part 0 writes the row, and which page it copies to which
+// (-1: none); all parts copy the part-filled page.
 __global__ void __launch_bounds__(kForkThreads) fork_row_kernel(const PageParams p, const __grid_constant__ PagePools pools,
                                                                 const int32_t* src, const int32_t* dst, int room,
                                                                 const long long* first, const int32_t* free_ids,
-                                                                const int* found, int32_t* out_forked) {
+                                                                const int* found, int32_t* copy_from, int32_t* copy_to,
+                                                                int32_t* out_forked) {
     const int i = blockIdx.x;
     wait_prior_grid();
     allow_dependent_launch();
@@ -184,14 +188,19 @@ __global__ void __launch_bounds__(kForkThreads) fork_row_kernel(const PageParams
             }
         }
     }
+    int old = -1, to = -1;
     if (ok && f.L % p.ps != 0) {
-        const int old = __ldcg(from + f.full);
+        old = __ldcg(from + f.full);
         if (old >= 0 && old < p.P) {
-            const int to = __ldcg(free_ids + at);
+            to = __ldcg(free_ids + at);
             constexpr int kWarps = kForkThreads / 32;
             for (uint32_t k = blockIdx.y * kWarps + threadIdx.x / 32; k < pools.pieces; k += gridDim.y * kWarps)
                 copy_piece(pools, old, to, k);
         }
+    }
+    if (blockIdx.y == 0 && threadIdx.x == 0) {
+        copy_from[i] = old;
+        copy_to[i] = to;
     }
 }
 
@@ -342,6 +351,22 @@ __global__ void __launch_bounds__(kMoveThreads) compact_move_kernel(const PagePa
     }
 }
 
+// The copies of a fork or a compaction in further pools: page from[r] to page to[r], r
+// below n and *count (NULL: n).  What is no page is left out, whatever the lists hold.
+__global__ void __launch_bounds__(kMoveThreads) copy_more_kernel(const __grid_constant__ PagePools pools,
+                                                                 const int32_t* from, const int32_t* to,
+                                                                 const int* count, int n, int P) {
+    wait_prior_grid();
+    allow_dependent_launch();
+    const int copies = count ? min(n, __ldcg(count)) : n;
+    const long long items = (long long)copies * pools.pieces, step = (long long)gridDim.x * (kMoveThreads / 32);
+    for (long long it = (long long)blockIdx.x * (kMoveThreads / 32) + threadIdx.x / 32; it < items; it += step) {
+        const long long r = div_pos(it, pools.pieces);
+        const int a = __ldcg(from + r), b = __ldcg(to + r);
+        if (a >= 0 && a < P && b >= 0 && b < P && a != b) copy_piece(pools, a, b, (uint32_t)(it - r * pools.pieces));
+    }
+}
+
 size_t align256(size_t n) { return (n + 255) & ~size_t(255); }
 
 PageParams page_params(const cs_page_dims& d, int32_t* table, int32_t* lens, int32_t* refs) {
@@ -372,28 +397,58 @@ int tiles_of_counts(int P) { return (int)(((long long)P + kCountTile - 1) / kCou
 
 }  // namespace
 
-// found (256 B), first [n], the free pages (at most all)
+// found (256 B), first [n], the copied pages and where they go [n], the free pages (at most all)
 size_t fork_workspace_bytes(const cs_page_dims& d, int n) {
-    return 256 + align256(sizeof(long long) * (size_t)n) + align256(sizeof(int32_t) * (size_t)d.num_pages);
+    return 256 + align256(sizeof(long long) * (size_t)n) + 2 * align256(sizeof(int32_t) * (size_t)n) +
+           align256(sizeof(int32_t) * (size_t)d.num_pages);
 }
+
+namespace {
+struct ForkSpace {
+    int* found;
+    long long* first;
+    int32_t *copy_from, *copy_to, *free_ids;
+    ForkSpace(void* workspace, int n) {
+        uint8_t* ws = static_cast<uint8_t*>(workspace);
+        const size_t ids = align256(sizeof(int32_t) * (size_t)n);
+        found = reinterpret_cast<int*>(ws);
+        first = reinterpret_cast<long long*>(ws + 256);
+        ws += 256 + align256(sizeof(long long) * (size_t)n);
+        copy_from = reinterpret_cast<int32_t*>(ws);
+        copy_to = reinterpret_cast<int32_t*>(ws + ids);
+        free_ids = reinterpret_cast<int32_t*>(ws + 2 * ids);
+    }
+};
+
+cs_status launch_copy_more(const cs_page_dims& d, const cs_page_pool* pools, int n_pools, const int32_t* from,
+                           const int32_t* to, const int* count, int n, cudaStream_t stream) {
+    const cudaError_t e = launch_dependent(copy_more_kernel, dim3(7 * current_sm_count()), dim3(kMoveThreads), 0, stream,
+                                           page_pools(pools, n_pools), from, to, count, n, (int)d.num_pages);
+    return e == cudaSuccess ? CS_OK : cuda_fail(e, "copy_more_kernel launch");
+}
+}  // namespace
 
 cs_status launch_kv_fork(const cs_page_dims& d, const cs_page_pool* pools, int n_pools, int32_t* page_table,
                          int32_t* ctx_lens, int32_t* ref_counts, const int32_t* src, const int32_t* dst, int n,
                          int room, int32_t* out_forked, void* workspace, cudaStream_t stream) {
-    uint8_t* ws = static_cast<uint8_t*>(workspace);
-    int* found = reinterpret_cast<int*>(ws);
-    long long* first = reinterpret_cast<long long*>(ws + 256);
-    int32_t* free_ids = reinterpret_cast<int32_t*>(ws + 256 + align256(sizeof(long long) * (size_t)n));
+    const ForkSpace ws(workspace, n);
     const PageParams p = page_params(d, page_table, ctx_lens, ref_counts);
     cudaError_t e = launch_dependent(fork_find_kernel, dim3(1), dim3(kFindThreads), 0, stream, p, src, dst, n, room,
-                                     first, free_ids, found);
+                                     ws.first, ws.free_ids, ws.found);
     if (e != cudaSuccess) return cuda_fail(e, "fork_find_kernel launch");
     const PagePools q = page_pools(pools, n_pools);
     // a warp some four pieces of the page that is copied
     const unsigned parts = q.pieces / 32 < 1 ? 1 : q.pieces / 32 > 32 ? 32 : q.pieces / 32;
     e = launch_dependent(fork_row_kernel, dim3(n, parts), dim3(kForkThreads), 0, stream, p, q, src,
-                         dst, room, (const long long*)first, (const int32_t*)free_ids, (const int*)found, out_forked);
+                         dst, room, (const long long*)ws.first, (const int32_t*)ws.free_ids, (const int*)ws.found,
+                         ws.copy_from, ws.copy_to, out_forked);
     return e == cudaSuccess ? CS_OK : cuda_fail(e, "fork_row_kernel launch");
+}
+
+cs_status launch_kv_fork_more(const cs_page_dims& d, const cs_page_pool* pools, int n_pools, int n, void* workspace,
+                              cudaStream_t stream) {
+    const ForkSpace ws(workspace, n);
+    return launch_copy_more(d, pools, n_pools, ws.copy_from, ws.copy_to, nullptr, n, stream);
 }
 
 cs_status launch_kv_release(const cs_page_dims& d, int32_t* page_table, int32_t* ctx_lens, int32_t* ref_counts,
@@ -409,8 +464,8 @@ size_t compact_workspace_bytes(const cs_page_dims& d) {
            3 * align256(sizeof(int32_t) * (size_t)d.num_pages);
 }
 
-cs_status launch_kv_compact(const cs_page_dims& d, const cs_page_pool* pools, int n_pools, int32_t* page_table,
-                            int32_t* ref_counts, int32_t* out_live, void* workspace, cudaStream_t stream) {
+namespace {
+CompactParams compact_params(const cs_page_dims& d, void* workspace) {
     uint8_t* ws = static_cast<uint8_t*>(workspace);
     const size_t ids = align256(sizeof(int32_t) * (size_t)d.num_pages);
     CompactParams c{};
@@ -421,6 +476,13 @@ cs_status launch_kv_compact(const cs_page_dims& d, const cs_page_pool* pools, in
     c.src = reinterpret_cast<int32_t*>(ws);
     c.dst = reinterpret_cast<int32_t*>(ws + ids);
     c.rank = reinterpret_cast<int32_t*>(ws + 2 * ids);
+    return c;
+}
+}  // namespace
+
+cs_status launch_kv_compact(const cs_page_dims& d, const cs_page_pool* pools, int n_pools, int32_t* page_table,
+                            int32_t* ref_counts, int32_t* out_live, void* workspace, cudaStream_t stream) {
+    CompactParams c = compact_params(d, workspace);
     const PageParams p = page_params(d, page_table, nullptr, ref_counts);
     cudaError_t e = cudaSuccess;
     // up to four tiles the ranking counts them itself: a launch less
@@ -436,6 +498,12 @@ cs_status launch_kv_compact(const cs_page_dims& d, const cs_page_pool* pools, in
     e = launch_dependent(compact_move_kernel, dim3(8 * sms), dim3(kMoveThreads), 0, stream, p, page_pools(pools, n_pools),
                          c, (const int32_t*)out_live, 7 * sms);
     return e == cudaSuccess ? CS_OK : cuda_fail(e, "compact_move_kernel launch");
+}
+
+cs_status launch_kv_compact_more(const cs_page_dims& d, const cs_page_pool* pools, int n_pools, void* workspace,
+                                 cudaStream_t stream) {
+    const CompactParams c = compact_params(d, workspace);
+    return launch_copy_more(d, pools, n_pools, c.src, c.dst, c.n_moved, d.num_pages, stream);
 }
 
 }  // namespace cs
