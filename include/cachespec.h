@@ -535,11 +535,13 @@ cs_status cs_packed_verify_attention(const cs_attn_dims* dims, const void* q, co
  * row (L = 0) where src[i] is -1.  Full pages are shared: their counts grow by
  * one.  A part-filled last page is copied into a page of the new row's own, and
  * further pages of its own give it room for `room` more tokens (as many as the
- * row can hold): ceil((L + room) / ps) - floor(L / ps) free pages in all, the lowest ids first, in
- * the order of i.  Entries past them become -1, ctx_lens[dst[i]] = L and
- * out_forked[i] = 1.  When the free pages do not suffice for i (with what the
- * requests before it ask for), row dst[i] is left empty (entries -1, length 0)
- * and out_forked[i] = 0; so it is for an i whose src is neither -1 nor a row
+ * row can hold): ceil((L + room) / ps) - floor(L / ps) free pages in all, the
+ * lowest ids first, in the order of i.  Entries past them become -1,
+ * ctx_lens[dst[i]] = L and out_forked[i] = 1.  When the free pages do not suffice
+ * for what requests 0 .. i ask for together, row dst[i] is left empty (entries
+ * -1, length 0) and out_forked[i] = 0: from the first request that goes without
+ * on, all do, also one that asks for none.  So it is for an i whose src is
+ * neither -1 nor a row
  * (where dst[i] is no row either, nothing is written).  The dst rows must be
  * distinct, none of them a src, and their former pages are not given back
  * (cs_kv_release before).

@@ -1,4 +1,4 @@
-"""Forks and compactions of caches with more arrays than one call takes."""
+"""Forks and compactions of caches with more arrays than one call takes, and forks past a shortage."""
 import importlib.util
 import os
 
@@ -88,3 +88,25 @@ def test_the_example_with_a_model_of_many_layers():
     s.release([0, 1, 2])
     assert int(s.compact()) == -(-(prompt + room) // ps)
     assert all(torch.equal(a, b) for a, b in zip(read(3), want))
+
+
+@pytest.mark.parametrize("lens,free,want", [((9, 8), 0, (0, 0)), ((8, 9), 0, (1, 0)), ((8, 9, 8, 16, 9), 1, (1, 1, 1, 1, 0)),
+                                            ((9, 17, 8, 8), 1, (1, 0, 0, 0))])
+def test_from_a_shortage_on_no_row_is_forked(lens, free, want):
+    """Rows of whole pages ask for none, but not past a request that went without."""
+    ps, cols, n = 8, 3, len(lens)
+    used = [-(-L // ps) for L in lens]
+    P = sum(used) + free
+    table, at = np.full((2 * n, cols), -1, np.int32), 0
+    for r, u in enumerate(used):
+        table[r, :u] = range(at, at + u)
+        at += u
+    lens = np.array(lens + (0,) * n, np.int32)
+    refs = (np.arange(P) < at).astype(np.int32)
+    pools = [np.random.default_rng(n).integers(0, 256, (P, 32), dtype=np.uint8)]
+    dev = [torch.from_numpy(a.copy()).to(DEV) for a in (pools[0], table, lens, refs)]
+    src, dst = list(range(n)), list(range(n, 2 * n))
+    done = binding.cs_kv_fork([dev[0]], *dev[1:], ints(src), ints(dst), ps)
+    assert tuple(done.tolist()) == want == tuple(ref.fork(pools, table, lens, refs, src, dst, ps, 0))
+    for d, h in zip(dev, (pools[0], table, lens, refs)):
+        np.testing.assert_array_equal(d.cpu().numpy(), h)
