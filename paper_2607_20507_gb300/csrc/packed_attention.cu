@@ -39,10 +39,16 @@
 //
 // What bounds it: turning codes into fp16 pairs and these into scaled ones, an
 // instruction each on pipes of 64 lanes a clock, with the address and selection
-// work around them (issue 53-60% busy, ALU 54%), not the memory: 256 requests of
-// 2048 keys, 4 rows, 8 KV heads, 276 us for 1.36 GB, 4.9 TB/s (the bytes alone take 200).
-// 64 requests of 4096 keys: 4 rows 71 us, 8 73, 12 97, 16 98, 20 127, 24 129: one
-// row tile more costs its own products and fewer CTAs an SM (registers).
+// work around them, and the latencies that 16 warps an SM leave in the open (issue 60%
+// busy, ALU 53%: neither at its limit), not the memory: 256 requests of 1024 to 8192
+// keys, 4 rows, 8 KV heads, 276 us for 1.37 GB, 4.9 TB/s (the bytes alone take 200).
+// 64 requests of 4096 keys: 4 rows 71 us, 8 72, 12 96, 16 98, 20 125, 24 128 (their
+// bytes take 44): one row tile more costs its own products and accumulators, so fewer
+// CTAs an SM (four, three and two at 128, 168 and 255 registers).
+// These are scores that lie within some 2^26 of their row's largest weight.  Each
+// turn for faint weights decodes the values again: with scores of 3, 5 and 8 nats'
+// deviation 4 rows take 103, 114 and 147 us and 20 rows 234, 286 and 396; with one key 20, 40
+// and 60 nats above the rest 108, 124 and 142, and 250, 318 and 392.
 #include <limits.h>
 #include <math.h>
 
@@ -770,8 +776,8 @@ Choice choice_tc() {
 constexpr int kForms = 7;
 
 // The form for a number of query rows of a span: up to 24 the one above (24 rows, 64
-// requests of 4096 keys, 8 KV heads: 129 us, 138 in the tcgen05 form), from 25 on the
-// tcgen05 form (28 rows: 137 us, 170 in the other one).
+// requests of 4096 keys, 8 KV heads: 128 us, 138 in the tcgen05 form), from 25 on the
+// tcgen05 form (28 rows: 138 us, 170 in the other one).
 int form_of(int rows) {
     return rows <= 24 ? (rows + 7) / 8 - 1 : rows <= 32 ? 3 : rows <= 48 ? 4 : rows <= 64 ? 5 : 6;
 }
@@ -814,8 +820,10 @@ struct PackedPlan {
 PackedPlan plan_packed(const cs_attn_dims& d, int rows, int sm_count) {
     PackedPlan pl{};
     pl.n_all = rows * (d.n_q_heads / d.n_kv_heads);
-    // more rows than the widest form's in blocks of equal size, each reading the keys
-    // again (136 rows in two blocks 519 us, in one block of the other form 870)
+    // more rows than the widest form's in blocks of equal size, each reading and decoding
+    // the keys again (64 requests of 4096 keys, 8 KV heads: 80 rows 186 us, 88 288, 136 344,
+    // where the bytes take 44; before the tcgen05 form's later steps 136 rows took 519 us in
+    // two blocks, 870 in one of the other form)
     pl.n_rb = (pl.n_all + kTcMaxRows - 1) / kTcMaxRows;
     pl.rows = (pl.n_all + pl.n_rb - 1) / pl.n_rb;
     pl.form = form_of(pl.rows);

@@ -29,10 +29,16 @@
 // tile (one set of decoding warps takes 2400), where the SM's instructions alone would
 // take 1100 to 1500: chains of waits (a try_wait that succeeds costs 160 cycles, a vote
 // 60 and the warps' drift), shared-memory and conversion latencies; the tensor pipe is
-// 23 to 30% busy, DRAM 21 to 27%.  64 requests of 4096 keys and 8 KV heads: 32 rows 138 us, 36 148;
-// 32 requests: 56 rows 96, 72 104; 256 requests of up to 16384 keys, 72 rows: 1.33 ms
-// for 2.8 GB (the same attention over a bf16 cache: 1.72 ms for 10 GB).  A CTA that
-// does everything in turn, two an SM, took 2.03 ms.
+// 23 to 30% busy, DRAM 21 to 27%.  Every warp has the same 96 registers (72 up to 48
+// columns), also those that issue and watch.  64 requests of 4096 keys and 8 KV heads:
+// 32 rows 138 us, 36 148; 32 requests: 56 rows 98, 72 111; 256 requests of up to 16384
+// keys, 72 rows: 1.34 ms for 2.8 GB (the same attention over a bf16 cache: 1.72 ms for
+// 10 GB).  A CTA that does everything in turn, two an SM, took 2.03 ms.
+// A tile that is mended costs several times one that is not, and peaked scores mend
+// most tiles: with scores of 3, 5 and 8 nats' deviation 36 rows (64 requests) take 0.79,
+// 1.08 and 1.58 ms and 72 rows (32 requests) 0.64, 0.96 and 1.36; with one key 20, 40 and 60
+// nats above the rest 0.76, 1.18 and 1.59, and 0.61, 0.97 and 1.33.  A piece's first tile is
+// always mended (m starts at -inf).
 //
 // Every mbarrier wait is bounded; after one that gives up nothing waits or is
 // issued any more, every warp still meets every block barrier, and the status

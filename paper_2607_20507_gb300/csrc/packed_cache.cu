@@ -7,9 +7,9 @@
 // contiguous segments.  Two neighbours bring in (or store) the four 16-byte
 // vectors of their groups in order and exchange the middle ones: every access of
 // a warp covers whole sectors.
-// 16 requests of 2049 rows, 8 KV heads (172 MB in all): append 38.5 us, 4.5 TB/s,
+// 16 requests of 2049 rows, 8 KV heads (172 MB in all): append 38.0 us, 4.5 TB/s,
 // bound by the instructions of the rounding (a quotient each, in the definition);
-// read 40.5 us, 4.3 TB/s, by the chain of loads that leads to a row.  (A thread a
+// read 40.0 us, 4.3 TB/s, by the chain of loads that leads to a row.  (A thread a
 // group of K or of V, its vectors loaded as they lie: 49 and 55.)
 #include "cs_internal.h"
 #include "packed.cuh"

@@ -11,8 +11,8 @@
 // What bounds them: a fork and a release are chains of a few dependent loads
 // and the launches (a release and a fork of 4 rows 10 us, of 192 rows 16); a
 // compaction reads the counts twice and the table once and then copies pages at
-// the memory's rate: 26,637 pages of 18 KB take 178 us, 5.5 TB/s; 239 of 128 KB,
-// 20.5 us, two launches and 31 MB each way.
+// the memory's rate: 26,637 pages of 18 KB take 178 us, 5.5 TB/s; 239 of 64 KB,
+// 20.5 us, two launches and 16 MB each way.
 #include "cs_internal.h"
 #include "cs_device.cuh"
 
@@ -316,7 +316,7 @@ __global__ void __launch_bounds__(kCountThreads) compact_rank_kernel(const PageP
 constexpr int kMoveThreads = 256;
 
 // The first `copy_ctas` CTAs copy pages, a warp a piece at a time (a CTA a page:
-// 239 pages of 128 KB took 28 us, 26,637 of 18 KB 250), the others rename table
+// 239 pages of 64 KB took 28 us, 26,637 of 18 KB 250), the others rename table
 // entries.
 __global__ void __launch_bounds__(kMoveThreads) compact_move_kernel(const PageParams p,
                                                                     const __grid_constant__ PagePools pools,
