@@ -500,10 +500,9 @@ typedef struct {
  * Arithmetic: q is taken to fp16 after a power of two has brought its row's
  * largest entry below 2^15 (entries down to 2^-31 of it keep every bit), keys
  * and values are code * s in fp16 (exact), the weights are rounded to 11 bits
- * (those below some 2^-138 of the row's largest count as 0), all products are
+ * (those below 2^-126 of the row's largest may count as 0), all products are
  * summed in fp32, the softmax is fp32, and the head scales enter in fp32 with
- * the softmax scale and the
- * normalisation.
+ * the softmax scale and the normalisation.
  *
  * Return CS_ERR_INVALID_ARG (null pointer, misalignment, bad dimension or
  * count), CS_ERR_UNSUPPORTED (head_dim != 128, page size, query rows, attention
