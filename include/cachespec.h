@@ -45,7 +45,14 @@
  *                          table share pages, give them back, and the pages in
  *                          use move together;
  *   cs_logprobs         -- log probabilities of given tokens with the entropy
- *                          and the top alternatives of their rows.
+ *                          and the top alternatives of their rows;
+ *   cs_rope_kv_append,
+ *   cs_packed_rope_kv_append,
+ *   cs_chunk_attention  -- the tokens of prompts, and of requests that decode
+ *                          beside them, on their way through the cache: rotated
+ *                          by their positions and appended (to either cache),
+ *                          and attended, each request with a number of new
+ *                          tokens of its own.
  *
  * Conventions for every entry point
  *   - All tensor arguments are DEVICE pointers owned by the caller, dense
@@ -520,6 +527,105 @@ cs_status cs_packed_verify_attention(const cs_attn_dims* dims, const void* q, co
                                      void* workspace, size_t workspace_bytes, cs_stream_t stream);
 
 /*
+ * Batches whose requests have different numbers of new tokens: the tokens of all
+ * requests are rows of one array, request b's the rows q_starts[b] ..
+ * q_starts[b+1] - 1 (n_b of them, from 0 on), its newest ones: row i of them sits
+ * at key position L_b - n_b + i, with L_b = ctx_lens[b], which counts them, clamped
+ * to [0, max_pages_per_seq * page_size].
+ *
+ *   q_starts   int32 [B + 1], not decreasing, from 0 on at most `tokens`; or NULL:
+ *              tokens / B rows a request (B has to divide tokens).  Rows in front of
+ *              q_starts[0] and from q_starts[B] on belong to nobody: they are not
+ *              computed and what stands in their place in outputs stays.
+ *   strides    rows of q, new_k and new_v may lie apart, as where a projection wrote
+ *              queries, keys and values side by side: elements from one token's heads
+ *              to the next token's, a multiple of 8; the heads of a token lie together.
+ *
+ * cs_rope_kv_append: cs_kv_append with the position rotation on the way.  For the
+ * row of each token, at rotation position t = positions[row], or its key position
+ * where positions is NULL, every head x of q and new_k:
+ *     x <- x * w / sqrt(mean(x^2) + norm_eps)   where there is a norm weight w;
+ *     (x_a, x_c) <- (x_a cos - x_c sin, x_c cos + x_a sin) for each pair of dims
+ * with the cosine and sine i of row t of cos_sin for pair i = 0 .. rot_dim / 2 - 1:
+ * dims (i, i + rot_dim / 2), or (2i, 2i + 1) where `interleaved` is set.  Dims from
+ * rot_dim on do not turn.  All in fp32, rounded once.  Queries go to q_out, keys and
+ * (as they are) values to the token's slot: slot j % ps of page page_table[b][j / ps]
+ * for key position j.
+ *
+ *   dims       the pool geometry and the head counts (head_dim 128; sm_scale unused)
+ *   q          bf16 [tokens, Hq, 128], 16-byte aligned; NULL (with q_out): none
+ *   new_k, new_v   bf16 [tokens, Hkv, 128], 16-byte aligned
+ *   cos_sin    fp32 [n_positions, rot_dim]: the cosines of a position, then its
+ *              sines; 16-byte aligned.  (Whatever scaling of frequencies a model
+ *              has is in the table, which a program fills once.)
+ *   positions  int32 [tokens] or NULL.  For token trees: a node's depth below the
+ *              root counts, not its slot.
+ *   q_norm, k_norm   bf16 [128], 16-byte aligned, or NULL
+ *   q_out      bf16 [tokens, Hq, 128], 16-byte aligned; may be q itself (with its stride)
+ *   rope->tokens         at most 2^31 - 1
+ *   rope->rot_dim        32, 64, 96 or 128
+ * A token whose rotation position lies outside [0, n_positions) is left out: its
+ * row of q_out stays, and so does the cache.  Keys and values of a token whose key
+ * position is negative or whose page lies outside the pool are not written.  Rows
+ * must not share the slots that they write.
+ *
+ * cs_packed_rope_kv_append: the same into a packed cache; the rotated keys are
+ * quantised from fp32, by the rule of cs_packed_kv_append.
+ *
+ * cs_chunk_attention: for the row of token i of request b and query head h,
+ *     out[row, h, :] = softmax_j( sm_scale * q[row, h, :] . K_j ) V_j
+ * over the keys j = 0 .. L_b - n_b + i of KV head h / G; from single tokens to whole
+ * prompts, in one call.  Page table, clamping, pages outside the pool (their keys and
+ * values read as zeros) and sm_scale are as for cs_verify_attention, and so is a row
+ * without a key (L_b - n_b + i < 0): zeros.
+ *
+ *   q          bf16 [tokens, Hq, 128], 16-byte aligned, q_stride elements from a
+ *              token to the next
+ *   out        bf16 [tokens, Hq, 128], dense, 16-byte aligned (must not alias the inputs)
+ *   tokens     >= 0, G = Hq / Hkv at most 128
+ *   workspace  at least cs_chunk_attention_workspace_bytes(dims, tokens) bytes,
+ *              256-byte aligned, any initial contents; its first 4 bytes are the
+ *              device status word, which every call clears first.  Calls that share
+ *              one must be ordered.
+ * Slots from L_b on may hold any bits.  Keys and values in front of L_b have to be
+ * finite: one that is not may reach every row of its request.
+ * Arithmetic: q.K in bf16 with fp32 accumulation, the softmax in fp32, its weights
+ * rounded to bf16 for the product with V, which is summed in fp32 (the sum that
+ * divides it is that of the unrounded weights); scaled by 2^-64 on the way as in
+ * cs_verify_attention, so that every finite V gives a finite output.
+ *
+ * Return CS_ERR_INVALID_ARG (null pointer, misalignment, bad dimension, stride or
+ * count), CS_ERR_UNSUPPORTED (head_dim != 128, page size, rot_dim, G > 128, a pool of
+ * more than 2^34 rows P * Hkv * ps), CS_ERR_WORKSPACE or CS_ERR_CUDA.
+ */
+typedef struct {
+    int32_t tokens;             /* rows of q, new_k and new_v (0: nothing to do) */
+    int32_t rot_dim;            /* dims of a head that turn */
+    int32_t interleaved;        /* 0: dims i and i + rot_dim / 2; 1: dims 2i and 2i + 1 */
+    int32_t n_positions;        /* rows of cos_sin (> 0) */
+    float norm_eps;             /* >= 0 and finite; read where there is a norm weight */
+    int64_t q_stride;           /* >= Hq * 128 */
+    int64_t k_stride;           /* >= Hkv * 128 */
+    int64_t v_stride;           /* >= Hkv * 128 */
+    int64_t q_out_stride;       /* >= Hq * 128 */
+} cs_rope_dims;
+
+cs_status cs_rope_kv_append(const cs_attn_dims* dims, const cs_rope_dims* rope, const void* q, const void* new_k,
+                            const void* new_v, const float* cos_sin, const int32_t* positions, const void* q_norm,
+                            const void* k_norm, void* q_out, void* k_pages, void* v_pages, const int32_t* page_table,
+                            const int32_t* ctx_lens, const int32_t* q_starts, cs_stream_t stream);
+cs_status cs_packed_rope_kv_append(const cs_attn_dims* dims, const cs_rope_dims* rope, const void* q,
+                                   const void* new_k, const void* new_v, const float* cos_sin,
+                                   const int32_t* positions, const void* q_norm, const void* k_norm, void* q_out,
+                                   const cs_packed_pool* pool, const int32_t* page_table, const int32_t* ctx_lens,
+                                   const int32_t* q_starts, cs_stream_t stream);
+size_t cs_chunk_attention_workspace_bytes(const cs_attn_dims* dims, int32_t tokens);
+cs_status cs_chunk_attention(const cs_attn_dims* dims, const void* q, int64_t q_stride, int32_t tokens,
+                             const void* k_pages, const void* v_pages, const int32_t* page_table,
+                             const int32_t* ctx_lens, const int32_t* q_starts, void* out, void* workspace,
+                             size_t workspace_bytes, cs_stream_t stream);
+
+/*
  * Pages of a cache, shared between rows of the page table.
  *
  * ref_counts int32 [P] says how many entries of the page table name each page;
@@ -647,7 +753,8 @@ cs_status cs_logprobs(const cs_logprob_dims* dims, const void* logits, const int
  * bounded wait inside a kernel gave up, so that call's output is invalid).
  * Copies 4 bytes to the host and SYNCHRONISES `stream`.  The word is sticky
  * until the caller zero-fills the workspace again; in a workspace of
- * cs_packed_verify_attention it tells of the latest call alone.
+ * cs_packed_verify_attention or cs_chunk_attention it tells of the latest call
+ * alone.
  */
 #define CS_DEVICE_WAIT_TIMEOUT 1
 cs_status cs_read_device_status(const void* workspace, int32_t* status_out, cs_stream_t stream);

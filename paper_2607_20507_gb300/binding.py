@@ -38,7 +38,8 @@ EXPORTED_SYMBOLS = ("cs_abi_version", "cs_last_error", "cs_verify_attention_work
                     "cs_packed_kv_append", "cs_packed_kv_read", "cs_packed_verify_attention_workspace_bytes",
                     "cs_packed_verify_attention", "cs_kv_fork_workspace_bytes", "cs_kv_fork", "cs_kv_release",
                     "cs_kv_compact_workspace_bytes", "cs_kv_compact", "cs_logprobs", "cs_kv_fork_more",
-                    "cs_kv_compact_more")
+                    "cs_kv_compact_more", "cs_rope_kv_append", "cs_packed_rope_kv_append",
+                    "cs_chunk_attention_workspace_bytes", "cs_chunk_attention")
 CS_MAX_TOP = 32
 CS_MAX_PAGE_POOLS = 128
 
@@ -76,6 +77,12 @@ class PagePool(ctypes.Structure):
 class LogprobDims(ctypes.Structure):
     _fields_ = [("rows", ctypes.c_int32), ("vocab", ctypes.c_int32), ("logit_dtype", ctypes.c_int32),
                 ("n_top", ctypes.c_int32), ("row_stride", ctypes.c_int64)]
+
+
+class RopeDims(ctypes.Structure):
+    _fields_ = [("tokens", ctypes.c_int32), ("rot_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32),
+                ("n_positions", ctypes.c_int32), ("norm_eps", ctypes.c_float), ("q_stride", ctypes.c_int64),
+                ("k_stride", ctypes.c_int64), ("v_stride", ctypes.c_int64), ("q_out_stride", ctypes.c_int64)]
 
 
 class PackedPool(NamedTuple):
@@ -190,6 +197,16 @@ def load_library(path: str | None = None):
         lib.cs_kv_compact_more.argtypes = [ctypes.POINTER(PageDims), ctypes.POINTER(PagePool), i32, vp, sz, vp]
         lib.cs_logprobs.restype = ctypes.c_int
         lib.cs_logprobs.argtypes = [ctypes.POINTER(LogprobDims), vp, vp, ctypes.c_float, vp, vp, vp, vp, vp]
+        lib.cs_rope_kv_append.restype = ctypes.c_int
+        lib.cs_rope_kv_append.argtypes = [ctypes.POINTER(AttnDims), ctypes.POINTER(RopeDims), *[vp] * 14]
+        lib.cs_packed_rope_kv_append.restype = ctypes.c_int
+        lib.cs_packed_rope_kv_append.argtypes = [ctypes.POINTER(AttnDims), ctypes.POINTER(RopeDims), *[vp] * 8,
+                                                 ctypes.POINTER(PackedPoolPtrs), *[vp] * 4]
+        lib.cs_chunk_attention_workspace_bytes.restype = sz
+        lib.cs_chunk_attention_workspace_bytes.argtypes = [ctypes.POINTER(AttnDims), i32]
+        lib.cs_chunk_attention.restype = ctypes.c_int
+        lib.cs_chunk_attention.argtypes = [ctypes.POINTER(AttnDims), vp, ctypes.c_int64, i32, vp, vp, vp, vp, vp, vp, vp,
+                                           sz, vp]
         lib.cs_kv_commit_tree.restype = ctypes.c_int
         lib.cs_kv_commit_tree.argtypes = [ctypes.POINTER(AttnDims), vp, vp, vp, vp, vp, vp, i32, vp]
         if path is None:
@@ -770,6 +787,167 @@ def cs_packed_verify_attention(q, pool, page_table, ctx_lens, n_draft, out=None,
     st = lib.cs_packed_verify_attention(ctypes.byref(d), q.data_ptr(), ctypes.byref(ptrs), page_table.data_ptr(),
                                         ctx_lens.data_ptr(), int(n_draft), out.data_ptr(), workspace.data_ptr(),
                                         workspace.nbytes, _stream(dev) if stream is None else stream)
+    if st:
+        _check(lib, st)
+    return out
+
+
+def _token_rows(t: torch.Tensor, name: str, dev) -> int:
+    """Checks rows of heads [T, H, 128], a token's heads side by side; returns the stride from token to token."""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch.Tensor")
+    if t.dtype != torch.bfloat16:
+        raise TypeError(f"{name} must be {torch.bfloat16}, got {t.dtype}")
+    if t.dim() != 3 or t.shape[2] != 128:
+        raise ValueError(f"{name} must be [tokens, heads, 128], got shape {tuple(t.shape)}")
+    if not t.is_cuda or (dev is not None and t.device != dev):
+        raise ValueError(f"{name} must live on {dev or 'a CUDA device'}")
+    T, H, D = t.shape
+    if T and H and (t.stride(2) != 1 or (H > 1 and t.stride(1) != D)):
+        raise ValueError(f"the heads of a token of {name} must lie together")
+    if T <= 1 or H == 0:
+        return H * D
+    if t.stride(0) < H * D or t.stride(0) % 8:
+        raise ValueError(f"the tokens of {name} must lie a multiple of 8 elements apart, at least {H * D}")
+    return t.stride(0)
+
+
+def _ragged(page_table, ctx_lens, q_starts, T: int, dev) -> int:
+    """Checks the arrays of a batch whose requests have rows of their own; returns the number of requests."""
+    _need(ctx_lens, "ctx_lens", torch.int32, 1, dev)
+    B = ctx_lens.shape[0]
+    _rows_of(page_table, ctx_lens, B, dev)
+    if q_starts is not None:
+        _need(q_starts, "q_starts", torch.int32, 1, dev)
+        if q_starts.shape[0] != B + 1:
+            raise ValueError(f"q_starts must be [{B + 1}]")
+    elif T % max(B, 1):
+        raise ValueError(f"{T} tokens of {B} requests without q_starts")
+    return B
+
+
+def _rope_call(q, new_k, new_v, cos_sin, page_table, ctx_lens, q_starts, positions, q_norm, k_norm, norm_eps, interleaved,
+               q_out, Hkv: int, ps: int, P: int, dev):
+    """The checks of the two rotated appends; returns (dims, rope dims, q_out)."""
+    k_stride, v_stride = _token_rows(new_k, "new_k", dev), _token_rows(new_v, "new_v", dev)
+    T, H, D = new_k.shape
+    if new_v.shape != new_k.shape or H != Hkv:
+        raise ValueError("new rows and pools do not match")
+    q_stride = out_stride = 0
+    if q is not None:
+        q_stride = _token_rows(q, "q", dev)
+        if q.shape[0] != T:
+            raise ValueError(f"q has {q.shape[0]} tokens, new_k {T}")
+        if q_out is None:
+            q_out = q.new_empty(q.shape)
+        out_stride = _token_rows(q_out, "q_out", dev)
+        if q_out.shape != q.shape:
+            raise ValueError("q_out must have the shape of q")
+    elif q_out is not None:
+        raise ValueError("q_out without q")
+    _need(cos_sin, "cos_sin", torch.float32, 2, dev)
+    B = _ragged(page_table, ctx_lens, q_starts, T, dev)
+    if positions is not None:
+        _need(positions, "positions", torch.int32, 1, dev)
+        if positions.shape[0] != T:
+            raise ValueError(f"positions must be [{T}]")
+    for name, t in (("q_norm", q_norm), ("k_norm", k_norm)):
+        if t is not None:
+            _need(t, name, torch.bfloat16, 1, dev)
+            if t.shape[0] != D:
+                raise ValueError(f"{name} must be [{D}]")
+    return (AttnDims(B, Hkv if q is None else q.shape[1], Hkv, D, ps, page_table.shape[1], P, 0.0),
+            RopeDims(T, cos_sin.shape[1], int(bool(interleaved)), cos_sin.shape[0], float(norm_eps), q_stride, k_stride,
+                     v_stride, out_stride), q_out)
+
+
+def cs_rope_kv_append(q, new_k, new_v, cos_sin, k_pages, v_pages, page_table, ctx_lens, q_starts=None, positions=None,
+                      q_norm=None, k_norm=None, norm_eps: float = 1e-6, interleaved: bool = False, q_out=None,
+                      stream: int | None = None):
+    """Turn the queries and keys of new tokens by their positions and append keys and values to the page pools (in
+    place).  q bf16 [tokens, Hq, 128] or None, new_k / new_v [tokens, Hkv, 128], whose tokens may lie apart; request b's
+    are the rows q_starts[b] .. q_starts[b+1] - 1 (None: as many each).  cos_sin fp32 [positions, rot_dim].  Returns
+    q_out.  See include/cachespec.h."""
+    lib = load_library()
+    _need(k_pages, "k_pages", torch.bfloat16, 4, None)
+    dev = k_pages.device
+    _need(v_pages, "v_pages", torch.bfloat16, 4, dev)
+    P, Hkv, ps, D = k_pages.shape
+    if v_pages.shape != k_pages.shape or D != 128:
+        raise ValueError("k_pages and v_pages must have the same shape [P, Hkv, ps, 128]")
+    d, r, q_out = _rope_call(q, new_k, new_v, cos_sin, page_table, ctx_lens, q_starts, positions, q_norm, k_norm,
+                             norm_eps, interleaved, q_out, Hkv, ps, P, dev)
+    with torch.cuda.device(dev):
+        st = lib.cs_rope_kv_append(ctypes.byref(d), ctypes.byref(r), _ptr(q), new_k.data_ptr(), new_v.data_ptr(),
+                                   cos_sin.data_ptr(), _ptr(positions), _ptr(q_norm), _ptr(k_norm), _ptr(q_out),
+                                   k_pages.data_ptr(), v_pages.data_ptr(), page_table.data_ptr(), ctx_lens.data_ptr(),
+                                   _ptr(q_starts), _stream(dev) if stream is None else stream)
+    if st:
+        _check(lib, st)
+    return q_out
+
+
+def cs_packed_rope_kv_append(q, new_k, new_v, cos_sin, pool, page_table, ctx_lens, q_starts=None, positions=None,
+                             q_norm=None, k_norm=None, norm_eps: float = 1e-6, interleaved: bool = False, q_out=None,
+                             stream: int | None = None):
+    """cs_rope_kv_append into a packed cache; ``pool`` a PackedPool.  Returns q_out.  See include/cachespec.h."""
+    lib = load_library()
+    _need(pool[0], "k_codes", torch.uint8, 4, None)
+    dev = pool[0].device
+    ptrs, (P, Hkv, ps) = _packed(pool, dev)
+    d, r, q_out = _rope_call(q, new_k, new_v, cos_sin, page_table, ctx_lens, q_starts, positions, q_norm, k_norm,
+                             norm_eps, interleaved, q_out, Hkv, ps, P, dev)
+    with torch.cuda.device(dev):
+        st = lib.cs_packed_rope_kv_append(ctypes.byref(d), ctypes.byref(r), _ptr(q), new_k.data_ptr(), new_v.data_ptr(),
+                                          cos_sin.data_ptr(), _ptr(positions), _ptr(q_norm), _ptr(k_norm), _ptr(q_out),
+                                          ctypes.byref(ptrs), page_table.data_ptr(), ctx_lens.data_ptr(), _ptr(q_starts),
+                                          _stream(dev) if stream is None else stream)
+    if st:
+        _check(lib, st)
+    return q_out
+
+
+def chunk_attn_dims(q: torch.Tensor, k_pages: torch.Tensor, page_table: torch.Tensor, sm_scale: float = 0.0) -> AttnDims:
+    P, Hkv, ps, D = k_pages.shape
+    return AttnDims(page_table.shape[0], q.shape[1], Hkv, D, ps, page_table.shape[1], P, float(sm_scale))
+
+
+def chunk_attention_workspace(dims: AttnDims, tokens: int, device, stream: int | None = None) -> torch.Tensor:
+    """The default workspace of the (current) stream's calls of cs_chunk_attention with these dims: after one,
+    cs_read_device_status of it tells whether it finished normally."""
+    n = load_library().cs_chunk_attention_workspace_bytes(ctypes.byref(dims), int(tokens))
+    return _cached_workspace("chunk_attn", device, n, stream)
+
+
+def cs_chunk_attention(q, k_pages, v_pages, page_table, ctx_lens, q_starts=None, out=None, workspace=None,
+                       sm_scale: float = 0.0, stream: int | None = None):
+    """Attention of every request's newest tokens over the paged cache, causal among them.  q bf16 [tokens, Hq, 128],
+    whose tokens may lie apart; request b's are the rows q_starts[b] .. q_starts[b+1] - 1 (None: as many each).
+    Returns ``out`` (bf16 [tokens, Hq, 128]; rows of no request stay as they are).  See include/cachespec.h."""
+    lib = load_library()
+    q_stride = _token_rows(q, "q", None)
+    dev = q.device
+    _need(k_pages, "k_pages", torch.bfloat16, 4, dev)
+    _need(v_pages, "v_pages", torch.bfloat16, 4, dev)
+    if v_pages.shape != k_pages.shape:
+        raise ValueError("k_pages and v_pages must have the same shape")
+    _ragged(page_table, ctx_lens, q_starts, q.shape[0], dev)
+    d = chunk_attn_dims(q, k_pages, page_table, sm_scale)
+    if out is None:
+        out = q.new_empty(q.shape)
+    else:
+        _need(out, "out", torch.bfloat16, 3, dev)
+        if out.shape != q.shape:
+            raise ValueError("out must have the shape of q")
+    T = q.shape[0]
+    with torch.cuda.device(dev):
+        if workspace is None:
+            n = lib.cs_chunk_attention_workspace_bytes(ctypes.byref(d), int(T))
+            workspace = _cached_workspace("chunk_attn", dev, n, stream)
+        st = lib.cs_chunk_attention(ctypes.byref(d), q.data_ptr(), q_stride, int(T), k_pages.data_ptr(),
+                                    v_pages.data_ptr(), page_table.data_ptr(), ctx_lens.data_ptr(), _ptr(q_starts),
+                                    out.data_ptr(), workspace.data_ptr(), workspace.nbytes,
+                                    _stream(dev) if stream is None else stream)
     if st:
         _check(lib, st)
     return out

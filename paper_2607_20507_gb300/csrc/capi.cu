@@ -186,6 +186,79 @@ cs_status check_packed_attn(const cs_attn_dims* d, int32_t n_draft) {
     return CS_OK;
 }
 
+// Head counts, pool and the rows of a batch with rows of its own for each request.
+cs_status check_ragged(const cs_attn_dims* d, int32_t tokens) {
+    const cs_status st = check_attn_geometry(d);
+    if (st != CS_OK) return st;
+    if (tokens < 0) return fail(CS_ERR_INVALID_ARG, "tokens %d < 0", tokens);
+    if ((long long)d->num_pages * d->n_kv_heads > (1LL << 34) / d->page_size)
+        return fail(CS_ERR_UNSUPPORTED, "a pool of more than 2^34 rows");
+    return CS_OK;
+}
+
+// (once there is something to do)
+cs_status check_ragged_pointers(const cs_attn_dims* d, int32_t tokens, const int32_t* page_table,
+                                const int32_t* ctx_lens, const int32_t* q_starts) {
+    if (!page_table || !ctx_lens) return fail(CS_ERR_INVALID_ARG, "a tensor pointer is NULL");
+    if (!aligned(page_table, 4) || !aligned(ctx_lens, 4) || !aligned(q_starts, 4))
+        return fail(CS_ERR_INVALID_ARG, "page_table, ctx_lens and q_starts must be 4-byte aligned");
+    if (!q_starts && tokens % d->batch != 0)
+        return fail(CS_ERR_INVALID_ARG, "%d tokens of %d requests without q_starts", tokens, d->batch);
+    return CS_OK;
+}
+
+cs_status check_stride(const char* name, int64_t stride, int heads) {
+    if (stride < (int64_t)heads * 128 || stride % 8 != 0 || stride > (1LL << 36))
+        return fail(CS_ERR_INVALID_ARG, "%s %lld is not a multiple of 8 from %lld to 2^36", name, (long long)stride,
+                    (long long)heads * 128);
+    return CS_OK;
+}
+
+// nothing: set where there is nothing to do
+cs_status check_rope(const cs_attn_dims* d, const cs_rope_dims* r, const void* q, const void* new_k, const void* new_v,
+                     const float* cos_sin, const int32_t* positions, const void* q_norm, const void* k_norm,
+                     const void* q_out, const int32_t* page_table, const int32_t* ctx_lens, const int32_t* q_starts,
+                     bool* nothing) {
+    if (!d || !r) return fail(CS_ERR_INVALID_ARG, "dims or rope is NULL");
+    cs_status st = check_ragged(d, r->tokens);
+    if (st != CS_OK) return st;
+    if (r->rot_dim != 32 && r->rot_dim != 64 && r->rot_dim != 96 && r->rot_dim != 128)
+        return fail(CS_ERR_UNSUPPORTED, "rot_dim %d (supported: 32, 64, 96, 128)", r->rot_dim);
+    if (r->interleaved != 0 && r->interleaved != 1)
+        return fail(CS_ERR_INVALID_ARG, "interleaved %d is neither 0 nor 1", r->interleaved);
+    if (r->n_positions <= 0) return fail(CS_ERR_INVALID_ARG, "n_positions %d <= 0", r->n_positions);
+    if (!(r->norm_eps >= 0.f) || isinf(r->norm_eps))
+        return fail(CS_ERR_INVALID_ARG, "norm_eps must be finite and >= 0");
+    if ((q == nullptr) != (q_out == nullptr)) return fail(CS_ERR_INVALID_ARG, "q and q_out go together");
+    if (q && ((st = check_stride("q_stride", r->q_stride, d->n_q_heads)) != CS_OK ||
+              (st = check_stride("q_out_stride", r->q_out_stride, d->n_q_heads)) != CS_OK))
+        return st;
+    if ((st = check_stride("k_stride", r->k_stride, d->n_kv_heads)) != CS_OK ||
+        (st = check_stride("v_stride", r->v_stride, d->n_kv_heads)) != CS_OK)
+        return st;
+    *nothing = d->batch == 0 || r->tokens == 0;
+    if (*nothing) return CS_OK;
+    st = check_ragged_pointers(d, r->tokens, page_table, ctx_lens, q_starts);
+    if (st != CS_OK) return st;
+    if (!new_k || !new_v || !cos_sin) return fail(CS_ERR_INVALID_ARG, "a tensor pointer is NULL");
+    if (!aligned(q, 16) || !aligned(new_k, 16) || !aligned(new_v, 16) || !aligned(q_out, 16) || !aligned(cos_sin, 16) ||
+        !aligned(q_norm, 16) || !aligned(k_norm, 16))
+        return fail(CS_ERR_INVALID_ARG, "rows, cos_sin and norm weights must be 16-byte aligned");
+    if (!aligned(positions, 4)) return fail(CS_ERR_INVALID_ARG, "positions must be 4-byte aligned");
+    return CS_OK;
+}
+
+cs_status check_chunk(const cs_attn_dims* d, int32_t tokens) {
+    if (!d) return fail(CS_ERR_INVALID_ARG, "dims is NULL");
+    const cs_status st = check_ragged(d, tokens);
+    if (st != CS_OK) return st;
+    if (d->n_q_heads / d->n_kv_heads > 128)
+        return fail(CS_ERR_UNSUPPORTED, "%d query heads a KV head (max 128)", d->n_q_heads / d->n_kv_heads);
+    if ((long long)tokens * d->n_q_heads > 0x7fffffffLL - (1 << 20))
+        return fail(CS_ERR_UNSUPPORTED, "%d tokens of %d heads in one call", tokens, d->n_q_heads);
+    return CS_OK;
+}
+
 cs_status check_pages(const cs_page_dims* d) {
     if (!d) return fail(CS_ERR_INVALID_ARG, "dims is NULL");
     if (d->rows <= 0 || d->max_pages_per_seq <= 0 || d->page_size <= 0 || d->num_pages <= 0)
@@ -477,6 +550,65 @@ cs_status cs_packed_verify_attention(const cs_attn_dims* dims, const void* q, co
     const StreamTurn turn(reinterpret_cast<cudaStream_t>(stream));
     return launch_packed_attention(*dims, q, *pool, page_table, ctx_lens, n_draft + 1, out, workspace,
                                    reinterpret_cast<cudaStream_t>(stream));
+}
+
+cs_status cs_rope_kv_append(const cs_attn_dims* dims, const cs_rope_dims* rope, const void* q, const void* new_k,
+                            const void* new_v, const float* cos_sin, const int32_t* positions, const void* q_norm,
+                            const void* k_norm, void* q_out, void* k_pages, void* v_pages, const int32_t* page_table,
+                            const int32_t* ctx_lens, const int32_t* q_starts, cs_stream_t stream) {
+    bool nothing = false;
+    const cs_status st = check_rope(dims, rope, q, new_k, new_v, cos_sin, positions, q_norm, k_norm, q_out, page_table,
+                                    ctx_lens, q_starts, &nothing);
+    if (st != CS_OK || nothing) return st;
+    if (!k_pages || !v_pages) return fail(CS_ERR_INVALID_ARG, "a tensor pointer is NULL");
+    if (!aligned(k_pages, 16) || !aligned(v_pages, 16))
+        return fail(CS_ERR_INVALID_ARG, "k_pages and v_pages must be 16-byte aligned");
+    return launch_rope_append(*dims, *rope, q, new_k, new_v, cos_sin, positions, q_norm, k_norm, q_out, k_pages,
+                              v_pages, page_table, ctx_lens, q_starts, reinterpret_cast<cudaStream_t>(stream));
+}
+
+cs_status cs_packed_rope_kv_append(const cs_attn_dims* dims, const cs_rope_dims* rope, const void* q,
+                                   const void* new_k, const void* new_v, const float* cos_sin,
+                                   const int32_t* positions, const void* q_norm, const void* k_norm, void* q_out,
+                                   const cs_packed_pool* pool, const int32_t* page_table, const int32_t* ctx_lens,
+                                   const int32_t* q_starts, cs_stream_t stream) {
+    if (!pool) return fail(CS_ERR_INVALID_ARG, "pool is NULL");
+    bool nothing = false;
+    cs_status st = check_rope(dims, rope, q, new_k, new_v, cos_sin, positions, q_norm, k_norm, q_out, page_table,
+                              ctx_lens, q_starts, &nothing);
+    if (st != CS_OK || nothing) return st;
+    st = check_packed_pointers(*pool, page_table, ctx_lens);
+    if (st != CS_OK) return st;
+    return launch_packed_rope_append(*dims, *rope, q, new_k, new_v, cos_sin, positions, q_norm, k_norm, q_out, *pool,
+                                     page_table, ctx_lens, q_starts, reinterpret_cast<cudaStream_t>(stream));
+}
+
+size_t cs_chunk_attention_workspace_bytes(const cs_attn_dims* dims, int32_t tokens) {
+    if (check_chunk(dims, tokens) != CS_OK) return 0;
+    return chunk_attention_workspace_bytes(*dims, tokens, current_sm_count());
+}
+
+cs_status cs_chunk_attention(const cs_attn_dims* dims, const void* q, int64_t q_stride, int32_t tokens,
+                             const void* k_pages, const void* v_pages, const int32_t* page_table,
+                             const int32_t* ctx_lens, const int32_t* q_starts, void* out, void* workspace,
+                             size_t workspace_bytes, cs_stream_t stream) {
+    cs_status st = check_chunk(dims, tokens);
+    if (st != CS_OK) return st;
+    st = check_stride("q_stride", q_stride, dims->n_q_heads);
+    if (st != CS_OK) return st;
+    if (dims->batch == 0 || tokens == 0) return CS_OK;
+    st = check_ragged_pointers(dims, tokens, page_table, ctx_lens, q_starts);
+    if (st != CS_OK) return st;
+    if (!q || !k_pages || !v_pages || !out) return fail(CS_ERR_INVALID_ARG, "a tensor pointer is NULL");
+    if (!aligned(q, 16) || !aligned(k_pages, 16) || !aligned(v_pages, 16) || !aligned(out, 16))
+        return fail(CS_ERR_INVALID_ARG, "q, k_pages, v_pages and out must be 16-byte aligned");
+    const size_t need = chunk_attention_workspace_bytes(*dims, tokens, current_sm_count());
+    if (!workspace || workspace_bytes < need)
+        return fail(CS_ERR_WORKSPACE, "workspace of %zu bytes given, %zu needed", workspace_bytes, need);
+    if (!aligned(workspace, 256)) return fail(CS_ERR_INVALID_ARG, "workspace must be 256-byte aligned");
+    const StreamTurn turn(reinterpret_cast<cudaStream_t>(stream));
+    return launch_chunk_attention(*dims, q, q_stride, tokens, k_pages, v_pages, page_table, ctx_lens, q_starts, out,
+                                  workspace, reinterpret_cast<cudaStream_t>(stream));
 }
 
 size_t cs_kv_fork_workspace_bytes(const cs_page_dims* dims, int32_t n) {

@@ -116,6 +116,22 @@ cs_status launch_packed_attention(const cs_attn_dims& d, const void* q, const cs
                                   const int32_t* page_table, const int32_t* ctx_lens, int rows, void* out,
                                   void* workspace, cudaStream_t stream);
 
+// ------------------------------------------- requests with rows of their own
+cs_status launch_rope_append(const cs_attn_dims& d, const cs_rope_dims& r, const void* q, const void* new_k,
+                             const void* new_v, const float* cos_sin, const int32_t* positions, const void* q_norm,
+                             const void* k_norm, void* q_out, void* k_pages, void* v_pages, const int32_t* page_table,
+                             const int32_t* ctx_lens, const int32_t* q_starts, cudaStream_t stream);
+cs_status launch_packed_rope_append(const cs_attn_dims& d, const cs_rope_dims& r, const void* q, const void* new_k,
+                                    const void* new_v, const float* cos_sin, const int32_t* positions,
+                                    const void* q_norm, const void* k_norm, void* q_out, const cs_packed_pool& pool,
+                                    const int32_t* page_table, const int32_t* ctx_lens, const int32_t* q_starts,
+                                    cudaStream_t stream);
+size_t chunk_attention_workspace_bytes(const cs_attn_dims& d, int tokens, int sm_count);
+cs_status launch_chunk_attention(const cs_attn_dims& d, const void* q, int64_t q_stride, int tokens,
+                                 const void* k_pages, const void* v_pages, const int32_t* page_table,
+                                 const int32_t* ctx_lens, const int32_t* q_starts, void* out, void* workspace,
+                                 cudaStream_t stream);
+
 // ------------------------------------------------------------------ pages
 size_t fork_workspace_bytes(const cs_page_dims& d, int n);
 cs_status launch_kv_fork(const cs_page_dims& d, const cs_page_pool* pools, int n_pools, int32_t* page_table,

@@ -1,0 +1,45 @@
+// ragged.cuh -- the rows of a batch whose requests have different numbers of new
+// tokens (cs_rope_kv_append, cs_chunk_attention): which request a token belongs to.
+#pragma once
+
+#include "cs_device.cuh"
+
+namespace cs {
+
+struct RaggedBatch {
+    const int32_t* ctx_lens;   // [B]
+    const int32_t* q_starts;   // [B + 1], or NULL: n rows each
+    int B, tokens, n;
+    int max_keys;              // keys that a row of the page table can hold
+
+    // Request b's rows, [start, start + n), in [0, tokens], and its length
+    __device__ __forceinline__ void rows_of(int b, int& start, int& count, int& len) const {
+        len = max(0, min(__ldcg(ctx_lens + b), max_keys));
+        if (!q_starts) {
+            start = b * n;
+            count = n;
+            return;
+        }
+        start = max(0, min(__ldcg(q_starts + b), tokens));
+        count = max(0, min(__ldcg(q_starts + b + 1), tokens) - start);
+    }
+
+    // The request that token t belongs to (the whole warp asks for one token); -1: none.
+    // 32 places of the array at a time: two loads up to 1024 requests.
+    __device__ __forceinline__ int request_of(int t, int lane) const {
+        if (!q_starts) return t / n < B ? t / n : -1;
+        int lo = 0, len = B + 1;   // the last b with q_starts[b] <= t lies in [lo, lo + len), if anywhere
+        while (len > 1) {
+            const int step = (len + 31) / 32;
+            const int at = lo + lane * step;
+            const unsigned before = __ballot_sync(0xffffffffu, lane * step < len && __ldcg(q_starts + at) <= t);
+            if (before == 0) return -1;
+            const int last = 31 - __clz(before);
+            lo += last * step;
+            len = min(step, len - last * step);
+        }
+        return lo < B && __ldcg(q_starts + lo) <= t && t < __ldcg(q_starts + lo + 1) ? lo : -1;
+    }
+};
+
+}  // namespace cs
