@@ -1,10 +1,33 @@
 // chunk_attention.cu -- attention of every request's newest tokens over the paged
 // bf16 cache, causal among them (cs_chunk_attention; the formula is in cachespec.h).
 //
-// A CTA takes 32 query rows of one request and KV head (row r of a request is token
-// r / G, query head h G + r % G) and passes once over their keys, 32 at a time, with
-// the running maximum and sum of the softmax; four threads share a row, each 32 of
-// its dims.
+// Work.  The query rows of a request and KV head (row r: token r / G, query head
+// h G + r % G) are cut into blocks of whole tokens, up to 256 rows, and a block's
+// keys into tiles of 128.  A block weighs its keys and what it costs to begin and
+// end one; a persistent grid of one CTA an SM takes equal contiguous ranges of the
+// whole weight, whatever the requests' sizes: blocks are cut between tiles where the
+// ranges end, and a second kernel joins the pieces of cut blocks.  The weights have
+// closed forms, so a CTA finds its range from the lengths alone.
+//
+// A CTA (twelve warps):
+//   warps 0-3, 4-7  softmax of query rows 0-127 and 128-255, a row a thread;
+//   warp 8          issues the products: S = Q K^T (M 128, N 128 keys, 8 steps of 16
+//                   dims) and O += P V (N 128 dims, 8 steps of 16 keys), tcgen05 with
+//                   S, P (over S) and O in tensor memory: 2 x (128 + 128) columns;
+//   warp 9          brings K and V tiles (TMA, one box a page piece) into a ring of
+//                   five 32 KB stages;
+//   warp 10         brings a block's query rows (TMA).
+// The products of one half run while the softmax of the other does: the issuer goes
+// round P0 V, Q0 K', P1 V, Q1 K', and a half's S_j+1 being complete says that its
+// P_j V_j is too (one thread's products complete in order), so O may be rescaled
+// then.  The running maximum moves only for a growth of more than 2^8.
+// Every wait on a barrier is bounded; one that gives up sets the status word and a flag
+// that ends every warp's loop.
+#include <cudaTypedefs.h>
+#include <math.h>
+
+#include <atomic>
+
 #include "cs_internal.h"
 #include "ragged.cuh"
 
@@ -12,123 +35,833 @@ namespace cs {
 namespace {
 
 constexpr int kD = 128;
-constexpr int kRows = 32, kKeys = 32, kThreads = 128;
+constexpr int kRows = 256;                         // query rows of a block
+constexpr int kHalf = 128;                         // ... of one of its two MMA tiles
+constexpr int kKeys = 128;                         // keys of a tile
+constexpr int kThreads = 384;
+constexpr int kMmaWarp = 8, kKvWarp = 9, kQWarp = 10;
+constexpr int kStages = 5;
+constexpr int kTileBytes = kKeys * kD * 2;
+constexpr int kQBytes = kRows * kD * 2;
+constexpr int kSmem = kQBytes + kStages * kTileBytes;
+constexpr int kSmallQRows = 32;                    // blocks of few rows bring in no more than these
+constexpr int kBeginKeys = 128;                    // what beginning and ending a block costs, in keys
+constexpr int kMaxBatch = 1024;                    // requests of a launch
+constexpr float kRescale = 8.f;                    // log2 growth of the maximum that moves it
 
 struct ChunkParams {
     RaggedBatch batch;
-    const __nv_bfloat16 *q, *k_pages, *v_pages;
     const int32_t* page_table;
     __nv_bfloat16* out;
-    int64_t q_stride;
-    int Hq, Hkv, G, ps_log2, max_pages, P;
+    int* status;
+    int4* slots;               // [2 grid]: request, head, block, flags of the pieces of cut blocks
+    float2* part_ml;           // [2 grid, rows] maximum (in powers of two) and sum
+    float* part_o;             // [2 grid, rows, 128], divided by the sum
+    int b0, nb;                // requests of this launch
+    int Hq, Hkv, G, ps, ps_log2, max_pages, P;
+    int block_tokens;          // whole tokens of a block
+    int small_tokens;          // ... of the small query box
+    int rows;                  // rows of a slot
     float scale_log2;
 };
+constexpr int kLeads = 1, kEnds = 2;               // flags of a piece: it has its block's first tile, last tile
 
-__global__ void __launch_bounds__(kThreads) chunk_attention_kernel(const ChunkParams p) {
-    __shared__ float sk[kKeys][kD + 4], sv[kKeys][kD + 4];
-    __shared__ int s_b, s_block;
-    wait_prior_grid();
-    allow_dependent_launch();
-    if (threadIdx.x == 0) {
-        long long left = blockIdx.x;
-        int b = 0;
-        for (; b < p.batch.B; ++b) {
-            int start, n, L;
-            p.batch.rows_of(b, start, n, L);
-            const long long blocks = ((long long)n * p.G + kRows - 1) / kRows;
-            if (left < blocks) break;
-            left -= blocks;
+// A request's blocks: block i has tokens [i T, min(n, (i+1) T)) and the keys in front
+// of and at the last of them; it weighs its keys + kBeginKeys.
+struct Blocks {
+    int n, L, T, count;
+    __device__ __forceinline__ Blocks(int n_, int L_, int T_) : n(n_), L(L_), T(T_), count((n_ + T_ - 1) / T_) {}
+    __device__ __forceinline__ int keys(int i) const { return max(0, L - n + min(n, (i + 1) * T)); }
+    // the weight of blocks 0 .. i-1
+    __device__ __forceinline__ long long before(int i) const {
+        const long long first = (long long)L - n;   // keys in front of the new tokens
+        const int full = min(i, count - 1);
+        // blocks without a key (more new tokens than keys): all in front
+        const int none = first < 0 ? (int)min((long long)full, -first / T) : 0;
+        const long long a = none, b = full;
+        long long w = (b - a) * first + T * ((b * (b + 1) - a * (a + 1)) / 2) + (long long)full * kBeginKeys;
+        if (i == count) w += L + kBeginKeys;
+        return w;
+    }
+};
+
+// The tile at place x of a block's weight w = keys + kBeginKeys
+__device__ __forceinline__ int tile_at(long long x, int keys) {
+    const int tiles = (keys + kKeys - 1) / kKeys;
+    if (x <= 0) return 0;
+    if (x >= keys + kBeginKeys) return tiles;
+    return (int)min((long long)tiles, max(0ll, (x - kBeginKeys + kKeys / 2) / kKeys));
+}
+
+// One piece after the other of a CTA's range.
+struct Pieces {
+    const ChunkParams* p;
+    int b, h, i;               // where the next piece begins
+    long long off, left;       // ... in its block; what is left of the range
+    int start, n, L;           // the request
+    // the piece
+    int t0, t1, tiles, keys, token0, tokens;
+    int pb, ph, pi, pL, pstart;
+
+    __device__ __forceinline__ void load() {
+        for (; b < p->nb; ++b) {
+            p->batch.rows_of(p->b0 + b, start, n, L);
+            if (n > 0) return;
         }
-        s_b = b;
-        s_block = (int)left;
+        left = 0;
     }
-    __syncthreads();
-    const int b = s_b, h = blockIdx.y;
-    if (b >= p.batch.B) return;
-    int start, n, L;
-    p.batch.rows_of(b, start, n, L);
-    const int r = s_block * kRows + (int)threadIdx.x / 4, part = threadIdx.x & 3;
-    const int i = min(r / p.G, n - 1), g = r % p.G;
-    const bool live = r < n * p.G;
-    const int last_i = min((s_block * kRows + kRows - 1) / p.G, n - 1);
-    const int seen = L - n + i + 1, most = L - n + last_i + 1;   // keys of this row, and of the block's last
-    float q[32], o[32];
-    const __nv_bfloat16* qrow = p.q + (int64_t)(start + i) * p.q_stride + (h * p.G + g) * kD + part * 32;
-#pragma unroll
-    for (int d = 0; d < 32; ++d) {
-        q[d] = __bfloat162float(qrow[d]);
-        o[d] = 0.f;
+    __device__ __forceinline__ Pieces(const ChunkParams* p_, int b_, int h_, int i_, long long off_, long long left_)
+        : p(p_), b(b_), h(h_), i(i_), off(off_), left(left_) {
+        if (left > 0) load();
     }
-    float m = kNegInf, l = 0.f;
-    for (int j0 = 0; j0 < most; j0 += kKeys) {
-        __syncthreads();
-        for (int e = threadIdx.x; e < kKeys * kD; e += kThreads) {
-            const int j = j0 + e / kD, d = e % kD;
-            float k = 0.f, v = 0.f;
-            if (j < most) {
-                const int page = __ldcg(p.page_table + (size_t)b * p.max_pages + (j >> p.ps_log2));
-                if (page >= 0 && page < p.P) {
-                    const size_t at = (((((size_t)page * p.Hkv + h) << p.ps_log2) + (j & ((1 << p.ps_log2) - 1)))) * kD + d;
-                    k = __bfloat162float(p.k_pages[at]);
-                    v = __bfloat162float(p.v_pages[at]);
+    // false: no more
+    __device__ __forceinline__ bool next() {
+        while (left > 0) {
+            const Blocks blocks(n, L, p->block_tokens);
+            keys = blocks.keys(i);
+            const long long w = keys + kBeginKeys, end = min(w, off + left);
+            tiles = (keys + kKeys - 1) / kKeys;
+            t0 = tile_at(off, keys);
+            t1 = tile_at(end, keys);
+            const bool there = t1 > t0 || (tiles == 0 && off == 0);
+            token0 = i * blocks.T;
+            tokens = min(n - token0, blocks.T);
+            pb = p->b0 + b;
+            ph = h;
+            pi = i;
+            pL = L;
+            pstart = start;
+            left -= end - off;
+            off = 0;
+            if (left > 0 && ++i == blocks.count) {
+                i = 0;
+                if (++h == p->Hkv) {
+                    h = 0;
+                    ++b;
+                    load();
                 }
             }
-            sk[e / kD][d] = k;
-            sv[e / kD][d] = v;
+            if (there) return true;
         }
-        __syncthreads();
-        for (int j = 0; j < kKeys; ++j) {
-            float s = 0.f;
+        return false;
+    }
+};
+
+// ------------------------------------------------------------- tensor memory
+__device__ __forceinline__ void tmem_ld32(uint32_t addr, float (&v)[32]) {
+    uint32_t r[32];
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
+        "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+          "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]),
+          "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]),
+          "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+        : "r"(addr));
 #pragma unroll
-            for (int d = 0; d < 32; ++d) s += q[d] * sk[j][part * 32 + d];
-            s += __shfl_xor_sync(0xffffffffu, s, 1);
-            s += __shfl_xor_sync(0xffffffffu, s, 2);
-            s *= p.scale_log2;
-            if (j0 + j >= seen) continue;
-            const float m_new = fmaxf(m, s);
-            const float keep = exp2f(m - m_new), w = exp2f(s - m_new);
-            l = l * keep + w;
-            m = m_new;
+    for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
+}
+__device__ __forceinline__ void tmem_ld16(uint32_t addr, uint32_t (&r)[16]) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+          "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+        : "r"(addr));
+}
+__device__ __forceinline__ void tmem_st16(uint32_t addr, const uint32_t (&r)[16]) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(
+            addr),
+        "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
+        "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+        : "memory");
+}
+// Waits for the loads so far; the values go through it, so that nothing that uses them
+// moves in front of it.
+__device__ __forceinline__ void tmem_ld_done(float (&v)[32]) {
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+f"(v[0]), "+f"(v[1]), "+f"(v[2]), "+f"(v[3]), "+f"(v[4]), "+f"(v[5]), "+f"(v[6]), "+f"(v[7]),
+                   "+f"(v[8]), "+f"(v[9]), "+f"(v[10]), "+f"(v[11]), "+f"(v[12]), "+f"(v[13]), "+f"(v[14]),
+                   "+f"(v[15]), "+f"(v[16]), "+f"(v[17]), "+f"(v[18]), "+f"(v[19]), "+f"(v[20]), "+f"(v[21]),
+                   "+f"(v[22]), "+f"(v[23]), "+f"(v[24]), "+f"(v[25]), "+f"(v[26]), "+f"(v[27]), "+f"(v[28]),
+                   "+f"(v[29]), "+f"(v[30]), "+f"(v[31])
+                 :: "memory");
+}
+__device__ __forceinline__ void tmem_ld_done(uint32_t (&v)[16]) {
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+r"(v[0]), "+r"(v[1]), "+r"(v[2]), "+r"(v[3]), "+r"(v[4]), "+r"(v[5]), "+r"(v[6]), "+r"(v[7]),
+                   "+r"(v[8]), "+r"(v[9]), "+r"(v[10]), "+r"(v[11]), "+r"(v[12]), "+r"(v[13]), "+r"(v[14]), "+r"(v[15])
+                 :: "memory");
+}
+__device__ __forceinline__ void tmem_st_done() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+
+// D[128 x n] (+)= A B, both in shared memory
+__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t acc) {
+    asm volatile(
+        "{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, q;\n\t}\n" ::"r"(d),
+        "l"(a), "l"(b), "r"(idesc), "r"(acc)
+        : "memory");
+}
+
+// Shared-memory operands with a 128-byte swizzle, in groups of 8 rows of 128 bytes:
+// query rows [dim half][row][64 dims], K-major, groups 1024 bytes apart;
+__device__ __forceinline__ uint64_t q_desc(uint32_t addr) {
+    return (uint64_t)((addr >> 4) & 0x3FFF) | ((uint64_t)1 << 16) | ((uint64_t)(1024 >> 4) << 32) | (1ull << 46) | (2ull << 61);
+}
+// K and V tiles [8-key group][dim half][key][64 dims], groups 2048 bytes apart: K
+// K-major, V MN-major (its dim halves 1024 bytes apart).
+__device__ __forceinline__ uint64_t k_desc(uint32_t addr) {
+    return (uint64_t)((addr >> 4) & 0x3FFF) | ((uint64_t)1 << 16) | ((uint64_t)(2048 >> 4) << 32) | (1ull << 46) | (2ull << 61);
+}
+__device__ __forceinline__ uint64_t v_desc(uint32_t addr) {
+    return (uint64_t)((addr >> 4) & 0x3FFF) | ((uint64_t)(1024 >> 4) << 16) | ((uint64_t)(2048 >> 4) << 32) | (1ull << 46) |
+           (2ull << 61);
+}
+// bf16 operands, fp32 sums, M = N = 128; b_mn: B's N index is the contiguous one
+__host__ __device__ constexpr uint32_t idesc_of(bool b_mn) {
+    return (1u << 4) | (1u << 7) | (1u << 10) | (b_mn ? (1u << 16) : 0u) | ((128u >> 3) << 17) | ((128u >> 4) << 24);
+}
+
+__device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* map, uint64_t* bar, int c0, int c1, int c2) {
+    asm volatile(
+        "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes"
+        " [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst),
+        "l"(reinterpret_cast<uint64_t>(map)), "r"(c0), "r"(c1), "r"(c2), "r"(smem_u32(bar))
+        : "memory");
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float d;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    return d;
+}
+// Keys from lim on are hidden.
+__device__ __forceinline__ void hide(float (&s)[32], int lim) {
+    if (lim < 32) {
 #pragma unroll
-            for (int d = 0; d < 32; ++d) o[d] = o[d] * keep + w * sv[j][part * 32 + d];
+        for (int e = 0; e < 32; ++e)
+            if (e >= lim) s[e] = kNegInf;
+    }
+}
+__device__ __forceinline__ float top_of(const float (&s)[32]) {
+    float a[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) a[j] = max3(s[j], s[j + 4], s[j + 8]);
+#pragma unroll
+    for (int e = 12; e < 28; e += 8)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) a[j] = max3(a[j], s[e + j], s[e + 4 + j]);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) a[j] = fmaxf(a[j], s[28 + j]);
+    return fmaxf(max3(a[0], a[1], a[2]), a[3]);
+}
+// 32 bytes at once
+__device__ __forceinline__ void store32(void* p, const uint32_t (&r)[8]) {
+    asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]),
+                 "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
+                 : "memory");
+}
+
+struct Bars {
+    uint64_t kv_full[kStages], kv_empty[kStages];
+    uint64_t q_full, q_empty;
+    uint64_t s_full[2], p_full[2], o_full[2], o_empty[2];
+    uint64_t drained;
+};
+
+// Waits for the phase of the given parity, the whole warp; false, at once, after any
+// wait of the block has given up.  (In line: registers are moved between warps, and a
+// function has those of a call's convention.)
+__device__ __forceinline__ bool wait(uint64_t* bar, uint32_t parity, volatile int* dead, int* status) {
+    bool done = mbar_test_wait(bar, parity);
+    if (!done && !*dead) {
+        done = mbar_wait_bounded(bar, parity);
+        if (!done) {
+            *dead = 1;
+            atomicOr(status, CS_DEVICE_WAIT_TIMEOUT);
         }
     }
-    if (!live) return;
-    const float inv = l > 0.f ? 1.f / l : 0.f;
-    __nv_bfloat16* dst = p.out + ((int64_t)(start + i) * p.Hq + h * p.G + g) * kD + part * 32;
+    return __all_sync(0xffffffffu, done);
+}
+
+__global__ void __launch_bounds__(kThreads, 1)
+chunk_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
+                       const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_q_small,
+                       const ChunkParams p) {
+    extern __shared__ __align__(1024) uint8_t smem[];
+    uint8_t* const sq = smem;                      // [dim half][row][128 B]
+    uint8_t* const ring = smem + kQBytes;
+    __shared__ Bars bars;
+    __shared__ long long s_part[kThreads / 32], s_off;
+    __shared__ int s_b, s_h, s_i;
+    __shared__ uint32_t s_tmem;
+    __shared__ volatile int s_dead;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+
+    if (warp == kMmaWarp) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(&s_tmem)) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    if (threadIdx.x == 0) {
+        s_dead = 0;
+        for (int i = 0; i < kStages; ++i) {
+            mbar_init(&bars.kv_full[i], 1);
+            mbar_init(&bars.kv_empty[i], 1);
+        }
+        mbar_init(&bars.q_full, 1);
+        mbar_init(&bars.q_empty, 1);
+        for (int m = 0; m < 2; ++m) {
+            mbar_init(&bars.s_full[m], 1);
+            mbar_init(&bars.p_full[m], 4);
+            mbar_init(&bars.o_full[m], 1);
+            mbar_init(&bars.o_empty[m], 4);
+        }
+        mbar_init(&bars.drained, 1);
+        fence_barrier_init();
+    }
+    // (rows that no block fills: zeros are cheaper to multiply than noise)
+    for (int i = threadIdx.x; i < kQBytes / 16; i += kThreads) reinterpret_cast<uint4*>(sq)[i] = make_uint4(0, 0, 0, 0);
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    wait_prior_grid();
+    allow_dependent_launch();
+
+    // ---- the range: three requests a thread, their weights' running sum
+    constexpr int kEach = (kMaxBatch + kThreads - 1) / kThreads;
+    long long weight[kEach], mine = 0;
 #pragma unroll
-    for (int d = 0; d < 32; ++d) dst[d] = __float2bfloat16(o[d] * inv);
+    for (int e = 0; e < kEach; ++e) {
+        const int b = threadIdx.x * kEach + e;
+        weight[e] = 0;
+        if (b < p.nb) {
+            int start, n, L;
+            p.batch.rows_of(p.b0 + b, start, n, L);
+            const Blocks blocks(n, L, p.block_tokens);
+            if (n > 0) weight[e] = blocks.before(blocks.count) * p.Hkv;
+        }
+        mine += weight[e];
+    }
+    long long upto = mine;
+#pragma unroll
+    for (int d = 1; d < 32; d *= 2) {
+        const long long x = __shfl_up_sync(0xffffffffu, upto, d);
+        if (lane >= d) upto += x;
+    }
+    if (lane == 31) s_part[warp] = upto;
+    if (threadIdx.x < 2) p.slots[2 * blockIdx.x + threadIdx.x] = make_int4(-1, 0, 0, 0);
+    if (blockIdx.x == 0 && threadIdx.x == 0 && p.b0 == 0) *p.status = 0;
+    fence_before();
+    __syncthreads();
+    fence_after();
+    const uint32_t tmem = s_tmem;
+    long long total = 0, at = upto - mine;
+    for (int w = 0; w < kThreads / 32; ++w) {
+        if (w < warp) at += s_part[w];
+        total += s_part[w];
+    }
+    const long long lo = total / gridDim.x * blockIdx.x + total % gridDim.x * blockIdx.x / gridDim.x;
+    const long long hi = total / gridDim.x * (blockIdx.x + 1) + total % gridDim.x * (blockIdx.x + 1) / gridDim.x;
+#pragma unroll
+    for (int e = 0; e < kEach; ++e) {
+        if (weight[e] > 0 && at <= lo && lo < at + weight[e]) {
+            int start, n, L;
+            p.batch.rows_of(p.b0 + threadIdx.x * kEach + e, start, n, L);
+            const Blocks blocks(n, L, p.block_tokens);
+            const long long head = weight[e] / p.Hkv, in = (lo - at) % head;
+            int i = 0;
+            for (int step = 1 << 30; step > 0; step >>= 1)
+                if (i + step < blocks.count && blocks.before(i + step) <= in) i += step;
+            s_b = threadIdx.x * kEach + e;
+            s_h = (int)((lo - at) / head);
+            s_i = i;
+            s_off = in - blocks.before(i);
+        }
+        at += weight[e];
+    }
+    __syncthreads();
+    Pieces pc(&p, s_b, s_h, s_i, s_off, hi - lo);
+    const uint32_t ring_at = smem_u32(ring);
+
+    if (warp >= kMmaWarp) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+        if (warp == kKvWarp) {
+            // --------------------------------------------------- K and V tiles
+            if (lane == 0) {
+                tma_prefetch_desc(&map_k);
+                tma_prefetch_desc(&map_v);
+            }
+            const int box = min(p.ps, kKeys), pieces = kKeys / box;
+            uint32_t at_stage = 0;   // stages used so far
+            bool ok = true;
+            while (ok && pc.next()) {
+                const int32_t* row = p.page_table + (size_t)pc.pb * p.max_pages;
+                auto page_of = [&](int t) {
+                    const int key = t * kKeys + lane * box;
+                    return lane < pieces && key < pc.pL ? __ldcg(row + (key >> p.ps_log2)) : -1;
+                };
+                int page = pc.t0 < pc.t1 ? page_of(pc.t0) : -1;
+                for (int t = pc.t0; ok && t < pc.t1; ++t) {
+                    const int key = t * kKeys + lane * box;
+                    const int live = min(pieces, (pc.pL - t * kKeys + box - 1) / box);
+                    // (a page outside the pool reads as zeros, from in front of it)
+                    const int group = (unsigned)page < (unsigned)p.P
+                                          ? (int)(((long long)page * p.Hkv + pc.ph) * (p.ps >> 3) + ((key & (p.ps - 1)) >> 3))
+                                          : -(box >> 3);
+                    if (t + 1 < pc.t1) page = page_of(t + 1);
+#pragma unroll
+                    for (int v = 0; v < 2; ++v) {
+                        const uint32_t st = at_stage % kStages, round = at_stage / kStages;
+                        ++at_stage;
+                        if (round > 0 && !(ok = wait(&bars.kv_empty[st], (round - 1) & 1, &s_dead, p.status))) {
+                            --at_stage;
+                            break;
+                        }
+                        if (lane == 0) mbar_arrive_expect_tx(&bars.kv_full[st], (uint32_t)live * box * (kD * 2));
+                        __syncwarp();
+                        if (lane < live)
+                            tma_load_4d(ring_at + st * kTileBytes + lane * box * (kD * 2), v ? &map_v : &map_k,
+                                        &bars.kv_full[st], 0, 0, 0, group);
+                    }
+                }
+            }
+            // no copy in flight at the end: every stage that was filled has landed
+            for (uint32_t j = at_stage > kStages ? at_stage - kStages : 0; j < at_stage; ++j)
+                if (!mbar_wait_bounded(&bars.kv_full[j % kStages], (j / kStages) & 1) && lane == 0)
+                    atomicOr(p.status, CS_DEVICE_WAIT_TIMEOUT);
+        } else if (warp == kQWarp) {
+            // ------------------------------------------------------ query rows
+            if (lane == 0) {
+                tma_prefetch_desc(&map_q);
+                tma_prefetch_desc(&map_q_small);
+            }
+            uint32_t piece = 0;
+            while (pc.next()) {
+                if (pc.tiles == 0) continue;
+                if (piece > 0 && !wait(&bars.q_empty, (piece - 1) & 1, &s_dead, p.status)) break;
+                ++piece;
+                const bool few = pc.tokens <= p.small_tokens;
+                const int box = few ? p.small_tokens : p.block_tokens;
+                if (lane == 0) mbar_arrive_expect_tx(&bars.q_full, (uint32_t)box * p.G * (kD * 2));
+                __syncwarp();
+                if (lane < 2)
+                    tma_load_3d(smem_u32(sq) + lane * (kQBytes / 2), few ? &map_q_small : &map_q, &bars.q_full, lane * 64,
+                                pc.ph * p.G, pc.pstart + pc.token0);
+            }
+            if (piece > 0 && !mbar_wait_bounded(&bars.q_full, (piece - 1) & 1) && lane == 0)
+                atomicOr(p.status, CS_DEVICE_WAIT_TIMEOUT);
+        } else if (warp == kMmaWarp) {
+            // -------------------------------------------------------- products
+            const uint64_t dq = q_desc(smem_u32(sq)), dk = k_desc(ring_at), dv = v_desc(ring_at);
+            constexpr uint32_t id_s = idesc_of(false), id_o = idesc_of(true);
+            auto scores = [&](int m, uint32_t st) {
+                const uint64_t a = dq + (uint64_t)(m * (kHalf * 128) >> 4), b = dk + (uint64_t)(st * kTileBytes >> 4);
+#pragma unroll
+                for (int s = 0; s < 8; ++s)
+                    mma_ss(tmem + m * 128, a + (s >> 2) * (uint64_t)(kQBytes / 2 >> 4) + (s & 3) * 2,
+                           b + (s >> 2) * (uint64_t)(1024 >> 4) + (s & 3) * 2, id_s, s > 0);
+                tc_commit(&bars.s_full[m]);
+            };
+            uint32_t stage = 0, piece = 0, n_p[2] = {0, 0}, n_o[2] = {0, 0};   // (as many phases as there were)
+            bool ok = true;
+            while (ok && pc.next()) {
+                if (pc.tiles == 0) continue;
+                const int halves = pc.tokens * p.G > kHalf ? 2 : 1;
+                if (!(ok = wait(&bars.q_full, piece & 1, &s_dead, p.status))) break;
+                ++piece;
+                const uint32_t st = stage % kStages;
+                if (!(ok = wait(&bars.kv_full[st], (stage / kStages) & 1, &s_dead, p.status))) break;
+                ++stage;
+                if (elect_one()) {
+                    for (int m = 0; m < halves; ++m) scores(m, st);
+                    tc_commit(&bars.kv_empty[st]);
+                    if (pc.t0 + 1 == pc.t1) tc_commit(&bars.q_empty);
+                }
+                __syncwarp();
+                for (int t = pc.t0; ok && t < pc.t1; ++t) {
+                    const bool last = t + 1 == pc.t1;
+                    const uint32_t sv = stage % kStages, sk = (stage + 1) % kStages;
+                    const uint32_t pv = (stage / kStages) & 1, pk = ((stage + 1) / kStages) & 1;
+                    if (!(ok = wait(&bars.kv_full[sv], pv, &s_dead, p.status))) break;
+                    // slots past the context's end may hold any bits, and their weights are 0
+                    const int live = pc.pL - t * kKeys;
+                    if (live < kKeys) {
+                        uint4* v = reinterpret_cast<uint4*>(ring + sv * kTileBytes);
+                        for (int i = lane; i < kTileBytes / 16; i += 32) {
+                            const int r = i >> 3;   // [group][half][key]
+                            if ((r >> 4) * 8 + (r & 7) >= live) v[i] = make_uint4(0, 0, 0, 0);
+                        }
+                        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                        __syncwarp();
+                    }
+                    for (int m = 0; m < halves; ++m) {
+                        if (!(ok = wait(&bars.p_full[m], n_p[m] & 1, &s_dead, p.status))) break;
+                        ++n_p[m];
+                        if (t == pc.t0) {
+                            if (n_o[m] > 0 && !(ok = wait(&bars.o_empty[m], (n_o[m] - 1) & 1, &s_dead, p.status))) break;
+                            ++n_o[m];
+                        }
+                        if (m == 0 && !last && !(ok = wait(&bars.kv_full[sk], pk, &s_dead, p.status))) break;
+                        fence_after();
+                        if (elect_one()) {
+                            const uint64_t b = dv + (uint64_t)(sv * kTileBytes >> 4);
+#pragma unroll
+                            for (int s = 0; s < 8; ++s)
+                                tc_mma_ts(tmem + 256 + m * 128, tmem + m * 128 + s * 8, b + s * (uint64_t)(4096 >> 4), id_o,
+                                          t > pc.t0 || s > 0);
+                            if (last) tc_commit(&bars.o_full[m]);
+                            else scores(m, sk);
+                        }
+                        __syncwarp();
+                    }
+                    if (!ok) break;
+                    if (elect_one()) {
+                        tc_commit(&bars.kv_empty[sv]);
+                        if (!last) tc_commit(&bars.kv_empty[sk]);
+                        if (t + 2 == pc.t1) tc_commit(&bars.q_empty);
+                    }
+                    __syncwarp();
+                    stage += last ? 1 : 2;
+                }
+            }
+            // every product is complete before tensor memory is given back
+            if (elect_one()) tc_commit(&bars.drained);
+            __syncwarp();
+            if (!mbar_wait_bounded(&bars.drained, 0) && lane == 0) atomicOr(p.status, CS_DEVICE_WAIT_TIMEOUT);
+        }
+    } else {
+        // ------------------------------------------------- softmax, a row a thread
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
+        const int m = warp >> 2;
+        const int row = threadIdx.x;               // of the block
+        const uint32_t t_s = tmem + ((uint32_t)(warp & 3) << 21) + m * 128, t_o = t_s + 256;
+        const int my_token = row / p.G, my_head = row - my_token * p.G;
+        const float c = p.scale_log2;
+        uint32_t n_s = 0, n_o = 0;
+        bool ok = true;
+        while (ok && pc.next()) {
+            const bool mine_ = my_token < pc.tokens;
+            const size_t out_row = (size_t)(pc.pstart + pc.token0 + my_token) * p.Hq + (size_t)pc.ph * p.G + my_head;
+            if (pc.tiles == 0) {   // no key at all
+                if (mine_) {
+                    const uint32_t zero[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+                    for (int j = 0; j < 8; ++j) store32(p.out + out_row * kD + j * 16, zero);
+                }
+                continue;
+            }
+            if (m == 1 && pc.tokens * p.G <= kHalf) continue;
+            const bool any = __any_sync(0xffffffffu, mine_);
+            // keys that the row sees
+            const int seen = max(0, pc.keys - (pc.tokens - 1 - min(my_token, pc.tokens - 1)));
+            float m_run = kNegInf, l_run = 0.f;
+            for (int t = pc.t0; t < pc.t1; ++t) {
+                if (!(ok = wait(&bars.s_full[m], n_s & 1, &s_dead, p.status))) break;
+                ++n_s;
+                fence_after();
+                if (any) {
+                    // the row's maximum over the tile; its last half stays in registers
+                    const int lim = seen - t * kKeys;
+                    float x[32], y[32], z[32];
+                    tmem_ld32(t_s, x);
+                    tmem_ld32(t_s + 32, y);
+                    tmem_ld_done(x);
+                    tmem_ld_done(y);
+                    tmem_ld32(t_s + 64, z);
+                    hide(x, lim);
+                    hide(y, lim - 32);
+                    float mt = fmaxf(top_of(x), top_of(y));
+                    tmem_ld_done(z);
+                    tmem_ld32(t_s + 96, y);
+                    hide(z, lim - 64);
+                    mt = fmaxf(mt, top_of(z));
+                    tmem_ld_done(y);
+                    tmem_ld32(t_s, x);
+                    hide(y, lim - 96);
+                    mt = fmaxf(mt, top_of(y));
+                    float alpha = 1.f;
+                    if (mt != kNegInf && (m_run == kNegInf || (mt - m_run) * c > kRescale)) {
+                        alpha = m_run == kNegInf ? 0.f : ex2((m_run - mt) * c);
+                        m_run = mt;
+                    }
+                    if (__any_sync(0xffffffffu, alpha != 1.f) && t != pc.t0) {
+                        // P V of the tile before is complete (see above)
+#pragma unroll 1
+                        for (int q = 0; q < 8; ++q) {
+                            uint32_t o[16];
+                            tmem_ld16(t_o + q * 16, o);
+                            tmem_ld_done(o);
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * alpha);
+                            tmem_st16(t_o + q * 16, o);
+                        }
+                    }
+                    const float neg = m_run == kNegInf ? 0.f : -m_run * c - kPShift;
+                    const uint64_t c2 = f2_pack(c, c), n2 = f2_pack(neg, neg);
+                    uint64_t sum[2] = {0ull, 0ull};
+                    auto weights = [&](const float (&s)[32], uint32_t (&w)[16]) {
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) {
+                            float x0, x1;
+                            f2_unpack(f2_fma(f2_pack(s[2 * e], s[2 * e + 1]), c2, n2), x0, x1);
+                            const float p0 = ex2(x0), p1 = ex2(x1);
+                            sum[e & 1] = f2_add(sum[e & 1], f2_pack(p0, p1));
+                            w[e] = pack_bf16x2(p0, p1);
+                        }
+                    };
+                    // (weights of keys 32 q .. go over scores of keys 16 q ..: the second
+                    // quarter has to be out before the third's weights go in)
+                    uint32_t wz[16], w[16];
+                    weights(z, wz);
+                    tmem_ld_done(x);
+                    tmem_ld32(t_s + 32, z);
+                    hide(x, lim);
+                    weights(x, w);
+                    tmem_ld_done(z);
+                    tmem_st16(t_s, w);
+                    tmem_st16(t_s + 32, wz);
+                    weights(y, w);
+                    tmem_st16(t_s + 48, w);
+                    hide(z, lim - 32);
+                    weights(z, w);
+                    tmem_st16(t_s + 16, w);
+                    float a0, a1;
+                    f2_unpack(f2_add(sum[0], sum[1]), a0, a1);
+                    l_run = l_run * alpha + (a0 + a1);
+                    tmem_st_done();
+                }
+                fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&bars.p_full[m]);
+            }
+            if (!ok) break;
+            // ---- the piece's end
+            if (!(ok = wait(&bars.o_full[m], n_o & 1, &s_dead, p.status))) break;
+            ++n_o;
+            fence_after();
+            const bool whole = pc.t0 == 0 && pc.t1 == pc.tiles;
+            const float inv = l_run > 0.f ? 1.f / l_run : 0.f;
+            const size_t slot = 2 * (size_t)blockIdx.x + (pc.t0 == 0);
+            if (any) {
+#pragma unroll 1
+                for (int q = 0; q < 4; ++q) {
+                    float o[32];
+                    tmem_ld32(t_o + q * 32, o);
+                    tmem_ld_done(o);
+                    if (!mine_) continue;
+                    if (whole) {
+#pragma unroll
+                        for (int j = 0; j < 2; ++j) {
+                            uint32_t r[8];
+#pragma unroll
+                            for (int e = 0; e < 8; ++e)
+                                r[e] = pack_bf16x2(o[16 * j + 2 * e] * inv, o[16 * j + 2 * e + 1] * inv);
+                            store32(p.out + out_row * kD + q * 32 + j * 16, r);
+                        }
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            uint32_t r[8];
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) r[e] = __float_as_uint(o[8 * j + e] * inv);
+                            store32(p.part_o + (slot * p.rows + row) * kD + q * 32 + j * 8, r);
+                        }
+                    }
+                }
+                if (!whole) {
+                    if (mine_) p.part_ml[slot * p.rows + row] = make_float2(m_run == kNegInf ? kNegInf : m_run * c, l_run);
+                    if (threadIdx.x == 0)
+                        p.slots[slot] = make_int4(pc.pb, pc.ph, pc.pi,
+                                                  (pc.t0 == 0 ? kLeads : 0) | (pc.t1 == pc.tiles ? kEnds : 0));
+                }
+            }
+            fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&bars.o_empty[m]);
+        }
+    }
+    fence_before();
+    __syncthreads();
+    fence_after();
+    if (warp == kMmaWarp)
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
+}
+
+// ------------------------------------------------------------------ the join
+// CTA (c, y): the block that begins in main CTA c and ends in a later one, rows 32 y
+// and on, a row a warp at a time: the pieces' outputs weighted by their sums.
+constexpr int kJoinThreads = 256;
+constexpr int kJoinRows = 32;
+
+__global__ void __launch_bounds__(kJoinThreads) chunk_join_kernel(const ChunkParams p, int grid) {
+    __shared__ int s_slot[2];
+    wait_prior_grid();
+    allow_dependent_launch();
+    const int first = 2 * blockIdx.x + 1;
+    const int4 head = __ldcg(p.slots + first);
+    if (head.x < 0) return;
+    int start, n, L;
+    p.batch.rows_of(head.x, start, n, L);
+    const int token0 = head.z * p.block_tokens;
+    const int rows = min(n - token0, p.block_tokens) * p.G;
+    if ((int)blockIdx.y * kJoinRows >= rows) return;
+    // its other pieces are the first ones of the CTAs behind (those that have one), up to
+    // the one that ends the block
+    if (threadIdx.x < 32) {
+        int last = -1;
+        for (int c = blockIdx.x + 1; last < 0 && c < grid; c += 32) {
+            const int at = c + (int)threadIdx.x;
+            const bool ends = at < grid && (__ldcg(p.slots + 2 * at).x >= 0) && (__ldcg(p.slots + 2 * at).w & kEnds);
+            const unsigned found = __ballot_sync(0xffffffffu, ends);
+            if (found) last = c + __ffs(found) - 1;
+        }
+        if (threadIdx.x == 0) s_slot[0] = last;
+    }
+    __syncthreads();
+    const int last = s_slot[0];
+    if (last < 0) return;   // (a wait gave up; the status says so)
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    for (int r = blockIdx.y * kJoinRows + warp; r < min(rows, ((int)blockIdx.y + 1) * kJoinRows); r += kJoinThreads / 32) {
+        float4 o = __ldcg(reinterpret_cast<const float4*>(p.part_o + ((size_t)first * p.rows + r) * kD) + lane);
+        float2 ml = __ldcg(p.part_ml + (size_t)first * p.rows + r);
+        for (int c = blockIdx.x + 1; c <= last; ++c) {
+            if (__ldcg(p.slots + 2 * c).x < 0) continue;
+            const size_t at = (size_t)(2 * c) * p.rows + r;
+            const float2 x = __ldcg(p.part_ml + at);
+            const float4 y = __ldcg(reinterpret_cast<const float4*>(p.part_o + at * kD) + lane);
+            const float top = fmaxf(ml.x, x.x);
+            if (top == kNegInf) continue;
+            const float a = ml.y * ex2(ml.x - top), b = x.y * ex2(x.x - top), inv = a + b > 0.f ? 1.f / (a + b) : 0.f;
+            const float fa = a * inv, fb = b * inv;
+            o.x = o.x * fa + y.x * fb;
+            o.y = o.y * fa + y.y * fb;
+            o.z = o.z * fa + y.z * fb;
+            o.w = o.w * fa + y.w * fb;
+            ml = make_float2(top, a + b);
+        }
+        const int token = token0 + r / p.G;
+        uint2* dst = reinterpret_cast<uint2*>(p.out + ((size_t)(start + token) * p.Hq + (size_t)head.y * p.G + r % p.G) * kD);
+        dst[lane] = make_uint2(pack_bf16x2(o.x, o.y), pack_bf16x2(o.z, o.w));
+    }
+}
+
+// ------------------------------------------------------------------ the host
+PFN_cuTensorMapEncodeTiled_v12000 encoder() {
+    static std::atomic<PFN_cuTensorMapEncodeTiled_v12000> fn{nullptr};
+    if (!fn) {
+        void* ptr = nullptr;
+        cudaDriverEntryPointQueryResult q;
+        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &ptr, 12000, cudaEnableDefault, &q) == cudaSuccess &&
+            q == cudaDriverEntryPointSuccess)
+            fn = reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(ptr);
+    }
+    return fn;
+}
+
+cs_status encode(CUtensorMap* map, const void* data, int rank, const cuuint64_t* dims, const cuuint64_t* strides,
+                 const cuuint32_t* box) {
+    auto enc = encoder();
+    if (!enc) return fail(CS_ERR_CUDA, "cuTensorMapEncodeTiled is not available from the driver");
+    const cuuint32_t ones[5] = {1, 1, 1, 1, 1};
+    const CUresult r = enc(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, rank, const_cast<void*>(data), dims, strides, box, ones,
+                           CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                           CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS ? CS_OK : fail(CS_ERR_CUDA, "cuTensorMapEncodeTiled failed (CUresult %d)", (int)r);
+}
+
+// A pool as 8-key groups (64 dims, 8 keys, 2 dim halves, groups), so that a box of a
+// page's keys lands as [group][half][8 keys][64 dims]
+cs_status encode_pool(CUtensorMap* map, const void* pool, const cs_attn_dims& d) {
+    const cuuint64_t dims[4] = {64, 8, 2, (cuuint64_t)d.num_pages * d.n_kv_heads * (d.page_size / 8)};
+    const cuuint64_t strides[3] = {256, 128, 2048};
+    const cuuint32_t box[4] = {64, 8, 2, (cuuint32_t)(d.page_size < kKeys ? d.page_size : kKeys) / 8};
+    return encode(map, pool, 4, dims, strides, box);
+}
+
+// Query rows of one KV head of some tokens, a dim half at a time: [token][head][64 dims]
+cs_status encode_rows(CUtensorMap* map, const void* q, const cs_attn_dims& d, int tokens, int64_t stride, int box_tokens) {
+    const cuuint64_t dims[3] = {kD, (cuuint64_t)d.n_q_heads, (cuuint64_t)tokens};
+    const cuuint64_t strides[2] = {kD * 2, (cuuint64_t)stride * 2};
+    const cuuint32_t box[3] = {64, (cuuint32_t)(d.n_q_heads / d.n_kv_heads), (cuuint32_t)box_tokens};
+    return encode(map, q, 3, dims, strides, box);
+}
+
+struct Layout {
+    int rows;
+    size_t slots, ml, o, bytes;
+};
+size_t align_up(size_t x) { return (x + 255) / 256 * 256; }
+Layout layout(const cs_attn_dims& d, int tokens, int grid) {
+    Layout l;
+    const long long all = (long long)tokens * (d.n_q_heads / d.n_kv_heads);
+    l.rows = all < kRows ? (int)all : kRows;
+    l.slots = 256;
+    l.ml = align_up(l.slots + sizeof(int4) * 2 * grid);
+    l.o = align_up(l.ml + sizeof(float2) * 2 * grid * l.rows);
+    l.bytes = align_up(l.o + sizeof(float) * kD * 2 * grid * l.rows);
+    return l;
 }
 
 }  // namespace
 
-size_t chunk_attention_workspace_bytes(const cs_attn_dims&, int, int) { return 256; }
+size_t chunk_attention_workspace_bytes(const cs_attn_dims& d, int tokens, int sm_count) {
+    return layout(d, tokens, sm_count).bytes;
+}
 
 cs_status launch_chunk_attention(const cs_attn_dims& d, const void* q, int64_t q_stride, int tokens,
                                  const void* k_pages, const void* v_pages, const int32_t* page_table,
                                  const int32_t* ctx_lens, const int32_t* q_starts, void* out, void* workspace,
                                  cudaStream_t stream) {
+    const int grid = current_sm_count();
+    const Layout l = layout(d, tokens, grid);
+    uint8_t* ws = static_cast<uint8_t*>(workspace);
     ChunkParams p{};
     p.batch = RaggedBatch{ctx_lens, q_starts, d.batch, tokens, q_starts ? 0 : tokens / d.batch,
                           d.max_pages_per_seq * d.page_size};
-    p.q = static_cast<const __nv_bfloat16*>(q);
-    p.k_pages = static_cast<const __nv_bfloat16*>(k_pages);
-    p.v_pages = static_cast<const __nv_bfloat16*>(v_pages);
     p.page_table = page_table;
     p.out = static_cast<__nv_bfloat16*>(out);
-    p.q_stride = q_stride;
+    p.status = reinterpret_cast<int*>(ws);
+    p.slots = reinterpret_cast<int4*>(ws + l.slots);
+    p.part_ml = reinterpret_cast<float2*>(ws + l.ml);
+    p.part_o = reinterpret_cast<float*>(ws + l.o);
     p.Hq = d.n_q_heads;
     p.Hkv = d.n_kv_heads;
     p.G = d.n_q_heads / d.n_kv_heads;
+    p.ps = d.page_size;
     while ((1 << p.ps_log2) < d.page_size) ++p.ps_log2;
     p.max_pages = d.max_pages_per_seq;
     p.P = d.num_pages;
+    p.block_tokens = kRows / p.G;
+    p.small_tokens = p.G < kSmallQRows ? kSmallQRows / p.G : 1;
+    p.rows = l.rows;
     p.scale_log2 = (d.sm_scale > 0.f ? d.sm_scale : 1.0f / sqrtf((float)kD)) * 1.4426950408889634f;
-    cudaError_t e = cudaMemsetAsync(workspace, 0, 4, stream);
-    if (e != cudaSuccess) return cuda_fail(e, "cudaMemsetAsync");
-    const long long blocks = ((long long)tokens * p.G) / kRows + d.batch + 1;
-    e = launch_dependent(chunk_attention_kernel, dim3((unsigned)blocks, (unsigned)p.Hkv), dim3(kThreads), 0, stream, p);
-    return e == cudaSuccess ? CS_OK : cuda_fail(e, "chunk_attention_kernel launch");
+
+    CUtensorMap mk, mv, mq, ms;
+    cs_status st = encode_pool(&mk, k_pages, d);
+    if (st == CS_OK) st = encode_pool(&mv, v_pages, d);
+    if (st == CS_OK) st = encode_rows(&mq, q, d, tokens, q_stride, p.block_tokens);
+    if (st == CS_OK) st = encode_rows(&ms, q, d, tokens, q_stride, p.small_tokens);
+    if (st != CS_OK) return st;
+    {
+        static std::atomic<bool> done[64];
+        int dev = 0;
+        cudaError_t e = cudaGetDevice(&dev);
+        if (e != cudaSuccess) return cuda_fail(e, "cudaGetDevice");
+        if (dev < 0 || dev >= 64 || !done[dev]) {
+            e = cudaFuncSetAttribute(chunk_attention_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
+            if (e != cudaSuccess) return cuda_fail(e, "cudaFuncSetAttribute(chunk_attention_kernel)");
+            if (dev >= 0 && dev < 64) done[dev] = true;
+        }
+    }
+    for (p.b0 = 0; p.b0 < d.batch; p.b0 += kMaxBatch) {
+        p.nb = d.batch - p.b0 < kMaxBatch ? d.batch - p.b0 : kMaxBatch;
+        cudaError_t e = launch_dependent(chunk_attention_kernel, dim3(grid), dim3(kThreads), (size_t)kSmem, stream, mk, mv,
+                                         mq, ms, p);
+        if (e != cudaSuccess) return cuda_fail(e, "chunk_attention_kernel launch");
+        e = launch_dependent(chunk_join_kernel, dim3(grid, (l.rows + kJoinRows - 1) / kJoinRows), dim3(kJoinThreads), 0, stream,
+                             p, grid);
+        if (e != cudaSuccess) return cuda_fail(e, "chunk_join_kernel launch");
+    }
+    return CS_OK;
 }
 
 }  // namespace cs
