@@ -868,6 +868,10 @@ def cs_rope_kv_append(q, new_k, new_v, cos_sin, k_pages, v_pages, page_table, ct
     place).  q bf16 [tokens, Hq, 128] or None, new_k / new_v [tokens, Hkv, 128], whose tokens may lie apart; request b's
     are the rows q_starts[b] .. q_starts[b+1] - 1 (None: as many each).  cos_sin fp32 [positions, rot_dim].  Returns
     q_out.  See include/cachespec.h."""
+    r = (_fast or _load_fast()).rope_kv_append(q, new_k, new_v, cos_sin, k_pages, v_pages, page_table, ctx_lens, q_starts,
+                                               positions, q_norm, k_norm, norm_eps, interleaved, q_out, stream)
+    if r is not None:
+        return None if r is True else _done(r)
     lib = load_library()
     _need(k_pages, "k_pages", torch.bfloat16, 4, None)
     dev = k_pages.device
@@ -891,6 +895,10 @@ def cs_packed_rope_kv_append(q, new_k, new_v, cos_sin, pool, page_table, ctx_len
                              q_norm=None, k_norm=None, norm_eps: float = 1e-6, interleaved: bool = False, q_out=None,
                              stream: int | None = None):
     """cs_rope_kv_append into a packed cache; ``pool`` a PackedPool.  Returns q_out.  See include/cachespec.h."""
+    r = (_fast or _load_fast()).packed_rope_kv_append(q, new_k, new_v, cos_sin, pool, page_table, ctx_lens, q_starts,
+                                                      positions, q_norm, k_norm, norm_eps, interleaved, q_out, stream)
+    if r is not None:
+        return None if r is True else _done(r)
     lib = load_library()
     _need(pool[0], "k_codes", torch.uint8, 4, None)
     dev = pool[0].device
@@ -924,6 +932,10 @@ def cs_chunk_attention(q, k_pages, v_pages, page_table, ctx_lens, q_starts=None,
     """Attention of every request's newest tokens over the paged cache, causal among them.  q bf16 [tokens, Hq, 128],
     whose tokens may lie apart; request b's are the rows q_starts[b] .. q_starts[b+1] - 1 (None: as many each).
     Returns ``out`` (bf16 [tokens, Hq, 128]; rows of no request stay as they are).  See include/cachespec.h."""
+    r = (_fast or _load_fast()).chunk_attention(q, k_pages, v_pages, page_table, ctx_lens, q_starts, out, workspace,
+                                                sm_scale, stream)
+    if r is not None:
+        return _done(r)
     lib = load_library()
     q_stride = _token_rows(q, "q", None)
     dev = q.device

@@ -13,6 +13,7 @@
 
 #include <ATen/ops/empty.h>
 #include <ATen/ops/empty_like.h>
+#include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -81,9 +82,9 @@ bool stream_of(PyObject* o, c10::Device dev, cs_stream_t* s) {
     return false;
 }
 
-enum Kind { kAttn, kTreeAttn, kAccept, kTreeAccept, kSample, kRoute, kPackedAttn, kFork, kCompact };
+enum Kind { kAttn, kTreeAttn, kAccept, kTreeAccept, kSample, kRoute, kPackedAttn, kFork, kCompact, kChunkAttn };
 const char* const kKinds[] = {"attn", "tree_attn", "accept", "tree_accept", "sample", "route", "packed_attn", "fork",
-                              "compact"};
+                              "compact", "chunk_attn"};
 
 // Scratch of a call; `hold` is the kept workspace it lies in.
 struct Scratch {
@@ -609,6 +610,143 @@ CALL(logprobs, 5)
                          THPVariable_Wrap(top_lp));
 CALL_END
 
+// Rows of heads [T, H, 128], a token's heads side by side; `dev` is set by the first tensor
+// of a call (where it is the CPU).
+bool token_rows(PyObject* o, c10::Device* dev, const at::Tensor** t, int64_t* stride) {
+    if (!THPVariable_CheckExact(o)) return false;
+    const at::Tensor& x = THPVariable_Unpack(o);
+    if (!x.is_cuda() || x.scalar_type() != at::kBFloat16 || x.dim() != 3 || x.size(2) != 128) return false;
+    if (dev->is_cpu()) *dev = x.device();
+    const int64_t T = x.size(0), H = x.size(1);
+    if (x.device() != *dev || (T && H && (x.stride(2) != 1 || (H > 1 && x.stride(1) != 128)))) return false;
+    *stride = H * 128;
+    if (T > 1 && H > 0) *stride = x.stride(0);
+    *t = &x;
+    return *stride >= H * 128 && *stride % 8 == 0;
+}
+
+// page_table [B, ..], ctx_lens [B], q_starts [B + 1] or None, of T tokens
+bool ragged(PyObject* t, PyObject* l, PyObject* s, int64_t T, c10::Device dev, const at::Tensor** table,
+            const at::Tensor** lens, const int32_t** starts) {
+    const at::Tensor* x;
+    if (!need(l, at::kInt, 1, dev, lens) || !rows_of(t, l, (*lens)->size(0), dev, table, lens)) return false;
+    const int64_t B = (*lens)->size(0);
+    *starts = nullptr;
+    if (s == Py_None) return T % (B > 0 ? B : 1) == 0;
+    if (!need(s, at::kInt, 1, dev, &x) || x->size(0) != B + 1) return false;
+    *starts = (const int32_t*)x->data_ptr();
+    return true;
+}
+
+// An optional array of n entries: its data, or NULL
+template <typename T>
+bool maybe(PyObject* o, at::ScalarType type, int64_t n, c10::Device dev, const T** data) {
+    const at::Tensor* x;
+    *data = nullptr;
+    if (o == Py_None) return true;
+    if (!need(o, type, 1, dev, &x) || x->size(0) != n) return false;
+    *data = static_cast<const T*>(x->data_ptr());
+    return true;
+}
+
+// q, new_k, new_v, cos_sin, k_pages, v_pages (or pool), page_table, ctx_lens, q_starts, positions, q_norm, k_norm,
+// norm_eps, interleaved, q_out, stream
+PyObject* rope_append(PyObject* const* a, bool packed_pool) {
+    const at::Tensor *q = nullptr, *nk, *nv, *cos, *k, *v = nullptr, *table, *lens, *o;
+    c10::Device dev(c10::kCPU);
+    cs_packed_pool pool;
+    cs_rope_dims r{};
+    cs_stream_t s;
+    const int32_t *starts, *positions;
+    const void *q_norm, *k_norm;
+    if (!token_rows(a[1], &dev, &nk, &r.k_stride) || !token_rows(a[2], &dev, &nv, &r.v_stride) ||
+        nk->sizes() != nv->sizes() || !need(a[3], at::kFloat, 2, dev, &cos))
+        Py_RETURN_NONE;
+    if (packed_pool) {
+        if (!packed(a[4], dev, &pool, &k)) Py_RETURN_NONE;
+    } else if (!need(a[4], at::kBFloat16, 4, dev, &k) || !need(a[5], at::kBFloat16, 4, dev, &v) ||
+               k->sizes() != v->sizes() || k->size(3) != 128) {
+        Py_RETURN_NONE;
+    }
+    a += packed_pool ? 5 : 6;
+    const int64_t T = nk->size(0);
+    PyObject* const q_in = a[packed_pool ? -5 : -6];
+    if (nk->size(1) != k->size(1) || !ragged(a[0], a[1], a[2], T, dev, &table, &lens, &starts) ||
+        !maybe(a[3], at::kInt, T, dev, &positions) || !maybe(a[4], at::kBFloat16, 128, dev, &q_norm) ||
+        !maybe(a[5], at::kBFloat16, 128, dev, &k_norm) || !number(a[6], &r.norm_eps) || !PyBool_Check(a[7]) ||
+        !stream_of(a[9], dev, &s))
+        Py_RETURN_NONE;
+    if (q_in != Py_None) {
+        if (!token_rows(q_in, &dev, &q, &r.q_stride) || q->size(0) != T) Py_RETURN_NONE;
+        r.q_out_stride = q->size(1) * 128;
+        if (a[8] != Py_None && (!token_rows(a[8], &dev, &o, &r.q_out_stride) || o->sizes() != q->sizes())) Py_RETURN_NONE;
+    } else if (a[8] != Py_None) {
+        Py_RETURN_NONE;
+    }
+    r.tokens = (int32_t)T;
+    r.rot_dim = (int32_t)cos->size(1);
+    r.interleaved = a[7] == Py_True;
+    r.n_positions = (int32_t)cos->size(0);
+    const cs_attn_dims d{(int32_t)lens->size(0), (int32_t)(q ? q->size(1) : k->size(1)), (int32_t)k->size(1), 128,
+                         (int32_t)k->size(2), (int32_t)table->size(1), (int32_t)k->size(0), 0.f};
+    const c10::cuda::CUDAGuard guard(dev);
+    at::Tensor out;
+    const cs_status st = launch([&] {
+        if (q) out = a[8] == Py_None ? at::empty(q->sizes(), at::TensorOptions(at::kBFloat16).device(dev)) : *o;
+        const void *qp = q ? q->data_ptr() : nullptr, *kp = nk->data_ptr(), *vp = nv->data_ptr();
+        void* op = q ? out.data_ptr() : nullptr;
+        const float* cp = (const float*)cos->data_ptr();
+        const int32_t *tp = (const int32_t*)table->data_ptr(), *lp = (const int32_t*)lens->data_ptr();
+        return packed_pool ? cs_packed_rope_kv_append(&d, &r, qp, kp, vp, cp, positions, q_norm, k_norm, op, &pool, tp, lp,
+                                                      starts, s)
+                           : cs_rope_kv_append(&d, &r, qp, kp, vp, cp, positions, q_norm, k_norm, op, k->data_ptr(),
+                                               v->data_ptr(), tp, lp, starts, s);
+    });
+    if (st != CS_OK) return status(st);
+    if (!q) Py_RETURN_TRUE;
+    return a[8] == Py_None ? THPVariable_Wrap(out) : Py_NewRef(a[8]);
+}
+
+// (with no queries: True when done)
+CALL(rope_kv_append, 16)
+    return rope_append(a, false);
+CALL_END
+
+CALL(packed_rope_kv_append, 15)
+    return rope_append(a, true);
+CALL_END
+
+// q, k_pages, v_pages, page_table, ctx_lens, q_starts, out, workspace, sm_scale, stream
+CALL(chunk_attention, 10)
+    const at::Tensor *q, *k, *v, *table, *lens, *o;
+    c10::Device dev(c10::kCPU);
+    const int32_t* starts;
+    int64_t stride;
+    float scale;
+    cs_stream_t s;
+    if (!token_rows(a[0], &dev, &q, &stride) || !need(a[1], at::kBFloat16, 4, dev, &k) ||
+        !need(a[2], at::kBFloat16, 4, dev, &v) || k->sizes() != v->sizes() ||
+        !ragged(a[3], a[4], a[5], q->size(0), dev, &table, &lens, &starts) || !number(a[8], &scale) ||
+        !stream_of(a[9], dev, &s) || (a[6] != Py_None && (!need(a[6], at::kBFloat16, 3, dev, &o) || o->sizes() != q->sizes())))
+        Py_RETURN_NONE;
+    const int32_t T = (int32_t)q->size(0);
+    const cs_attn_dims d{(int32_t)lens->size(0), (int32_t)q->size(1), (int32_t)k->size(1), (int32_t)k->size(3),
+                         (int32_t)k->size(2), (int32_t)table->size(1), (int32_t)k->size(0), scale};
+    const c10::cuda::CUDAGuard guard(dev);
+    Scratch ws;
+    const size_t bytes = a[7] == Py_None ? cs_chunk_attention_workspace_bytes(&d, T) : 0;
+    if (!workspace(a[7], kChunkAttn, dev, bytes, s, &ws)) Py_RETURN_NONE;
+    at::Tensor out;
+    const cs_status st = launch([&] {
+        out = a[6] == Py_None ? at::empty(q->sizes(), at::TensorOptions(at::kBFloat16).device(dev)) : *o;
+        return cs_chunk_attention(&d, q->data_ptr(), stride, T, k->data_ptr(), v->data_ptr(),
+                                  (const int32_t*)table->data_ptr(), (const int32_t*)lens->data_ptr(), starts,
+                                  out.data_ptr(), ws.ptr, ws.bytes, s);
+    });
+    if (st != CS_OK) return status(st);
+    return a[6] == Py_None ? THPVariable_Wrap(out) : Py_NewRef(a[6]);
+CALL_END
+
 PyObject* use_workspaces(PyObject*, PyObject* f) {
     Py_XSETREF(g_workspace_of, Py_NewRef(f));
     Py_RETURN_NONE;
@@ -618,7 +756,8 @@ PyObject* use_workspaces(PyObject*, PyObject* f) {
 PyMethodDef g_methods[] = {FAST(verify_attention), FAST(tree_verify_attention), FAST(spec_accept), FAST(tree_accept),
                            FAST(sample), FAST(route), FAST(kv_append), FAST(kv_commit), FAST(kv_commit_tree),
                            FAST(packed_kv_append), FAST(packed_kv_read), FAST(packed_verify_attention), FAST(kv_fork),
-                           FAST(kv_release), FAST(kv_compact), FAST(logprobs),
+                           FAST(kv_release), FAST(kv_compact), FAST(logprobs), FAST(rope_kv_append),
+                           FAST(packed_rope_kv_append), FAST(chunk_attention),
                            {"use_workspaces", use_workspaces, METH_O, nullptr}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
 
