@@ -559,25 +559,17 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_c
                 ++n_s;
                 fence_after();
                 if (any) {
-                    // the row's maximum over the tile; its last half stays in registers
+                    float s[4][32];
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) tmem_ld32(t_s + q * 32, s[q]);
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) tmem_ld_done(s[q]);
                     const int lim = seen - t * kKeys;
-                    float x[32], y[32], z[32];
-                    tmem_ld32(t_s, x);
-                    tmem_ld32(t_s + 32, y);
-                    tmem_ld_done(x);
-                    tmem_ld_done(y);
-                    tmem_ld32(t_s + 64, z);
-                    hide(x, lim);
-                    hide(y, lim - 32);
-                    float mt = fmaxf(top_of(x), top_of(y));
-                    tmem_ld_done(z);
-                    tmem_ld32(t_s + 96, y);
-                    hide(z, lim - 64);
-                    mt = fmaxf(mt, top_of(z));
-                    tmem_ld_done(y);
-                    tmem_ld32(t_s, x);
-                    hide(y, lim - 96);
-                    mt = fmaxf(mt, top_of(y));
+                    if (lim < kKeys) {
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) hide(s[q], lim - 32 * q);
+                    }
+                    const float mt = fmaxf(max3(top_of(s[0]), top_of(s[1]), top_of(s[2])), top_of(s[3]));
                     float alpha = 1.f;
                     if (mt != kNegInf && (m_run == kNegInf || (mt - m_run) * c > kRescale)) {
                         alpha = m_run == kNegInf ? 0.f : ex2((m_run - mt) * c);
@@ -598,32 +590,19 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_c
                     const float neg = m_run == kNegInf ? 0.f : -m_run * c - kPShift;
                     const uint64_t c2 = f2_pack(c, c), n2 = f2_pack(neg, neg);
                     uint64_t sum[2] = {0ull, 0ull};
-                    auto weights = [&](const float (&s)[32], uint32_t (&w)[16]) {
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        uint32_t w[16];
 #pragma unroll
                         for (int e = 0; e < 16; ++e) {
                             float x0, x1;
-                            f2_unpack(f2_fma(f2_pack(s[2 * e], s[2 * e + 1]), c2, n2), x0, x1);
+                            f2_unpack(f2_fma(f2_pack(s[q][2 * e], s[q][2 * e + 1]), c2, n2), x0, x1);
                             const float p0 = ex2(x0), p1 = ex2(x1);
                             sum[e & 1] = f2_add(sum[e & 1], f2_pack(p0, p1));
                             w[e] = pack_bf16x2(p0, p1);
                         }
-                    };
-                    // (weights of keys 32 q .. go over scores of keys 16 q ..: the second
-                    // quarter has to be out before the third's weights go in)
-                    uint32_t wz[16], w[16];
-                    weights(z, wz);
-                    tmem_ld_done(x);
-                    tmem_ld32(t_s + 32, z);
-                    hide(x, lim);
-                    weights(x, w);
-                    tmem_ld_done(z);
-                    tmem_st16(t_s, w);
-                    tmem_st16(t_s + 32, wz);
-                    weights(y, w);
-                    tmem_st16(t_s + 48, w);
-                    hide(z, lim - 32);
-                    weights(z, w);
-                    tmem_st16(t_s + 16, w);
+                        tmem_st16(t_s + q * 16, w);
+                    }
                     float a0, a1;
                     f2_unpack(f2_add(sum[0], sum[1]), a0, a1);
                     l_run = l_run * alpha + (a0 + a1);
