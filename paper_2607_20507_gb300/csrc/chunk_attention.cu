@@ -9,14 +9,15 @@
 // ranges end, and a second kernel joins the pieces of cut blocks.  The weights have
 // closed forms, so a CTA finds its range from the lengths alone.
 //
-// A CTA (twelve warps):
-//   warps 0-3, 4-7  softmax of query rows 0-127 and 128-255, a row a thread;
-//   warp 8          issues the products: S = Q K^T (M 128, N 128 keys, 8 steps of 16
+// A CTA (twenty warps):
+//   warps 0-15      softmax, of query rows 0-127 and then 128-255 of a tile: a warp takes
+//                   16 rows and half of a tile's keys, two threads a row;
+//   warp 16         issues the products: S = Q K^T (M 128, N 128 keys, 8 steps of 16
 //                   dims) and O += P V (N 128 dims, 8 steps of 16 keys), tcgen05 with
 //                   S, P (over S) and O in tensor memory: 2 x (128 + 128) columns;
-//   warp 9          brings K and V tiles (TMA, one box a page piece) into a ring of
+//   warp 17         brings K and V tiles (TMA, one box a page piece) into a ring of
 //                   five 32 KB stages;
-//   warp 10         brings a block's query rows (TMA).
+//   warp 18         brings a block's query rows (TMA).
 // The products of one half run while the softmax of the other does: the issuer goes
 // round P0 V, Q0 K', P1 V, Q1 K', and a half's S_j+1 being complete says that its
 // P_j V_j is too (one thread's products complete in order), so O may be rescaled
@@ -38,8 +39,8 @@ constexpr int kD = 128;
 constexpr int kRows = 256;                         // query rows of a block
 constexpr int kHalf = 128;                         // ... of one of its two MMA tiles
 constexpr int kKeys = 128;                         // keys of a tile
-constexpr int kThreads = 384;
-constexpr int kMmaWarp = 8, kKvWarp = 9, kQWarp = 10;
+constexpr int kThreads = 640;
+constexpr int kMmaWarp = 16, kKvWarp = 17, kQWarp = 18;
 constexpr int kStages = 5;
 constexpr int kTileBytes = kKeys * kD * 2;
 constexpr int kQBytes = kRows * kD * 2;
@@ -47,7 +48,7 @@ constexpr int kSmem = kQBytes + kStages * kTileBytes;
 constexpr int kSmallQRows = 32;                    // blocks of few rows bring in no more than these
 constexpr int kBeginKeys = 128;                    // what beginning and ending a block costs, in keys
 constexpr int kMaxBatch = 1024;                    // requests of a launch
-constexpr float kRescale = 8.f;                    // log2 growth of the maximum that moves it
+constexpr float kMostSum = 0x1p-56f;               // 2^8 times 2^-kPShift
 
 struct ChunkParams {
     RaggedBatch batch;
@@ -148,32 +149,38 @@ struct Pieces {
 };
 
 // ------------------------------------------------------------- tensor memory
+// 16 lanes, twice: threads 0-15 have lanes l .. l+15 of the address at its columns,
+// threads 16-31 the same lanes kSplit columns on (32 or 16 columns a thread).
+template <int kSplit>
 __device__ __forceinline__ void tmem_ld32(uint32_t addr, float (&v)[32]) {
     uint32_t r[32];
     asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
-        "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+        "tcgen05.ld.sync.aligned.16x32bx2.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
+        "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32], %33;"
         : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
-          "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]),
-          "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]),
-          "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
-        : "r"(addr));
+          "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]),
+          "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]),
+          "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]),
+          "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+        : "r"(addr), "n"(kSplit));
 #pragma unroll
     for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
 }
+template <int kSplit>
 __device__ __forceinline__ void tmem_ld16(uint32_t addr, uint32_t (&r)[16]) {
     asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+        "tcgen05.ld.sync.aligned.16x32bx2.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16], %17;"
         : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
           "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
-        : "r"(addr));
+        : "r"(addr), "n"(kSplit));
 }
+template <int kSplit>
 __device__ __forceinline__ void tmem_st16(uint32_t addr, const uint32_t (&r)[16]) {
     asm volatile(
-        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(
+        "tcgen05.st.sync.aligned.16x32bx2.x16.b32 [%0], %1, {%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17};" ::"r"(
             addr),
-        "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
-        "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+        "n"(kSplit), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]),
+        "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
         : "memory");
 }
 // Waits for the loads so far; the values go through it, so that nothing that uses them
@@ -264,6 +271,19 @@ __device__ __forceinline__ void store32(void* p, const uint32_t (&r)[8]) {
                  : "memory");
 }
 
+// The two warps of a pair: whether any of their threads says so; and a barrier.
+__device__ __forceinline__ bool pair_any(int id, bool x) {
+    uint32_t r;
+    asm volatile(
+        "{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\t"
+        "barrier.cta.red.or.pred q, %2, 64, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+        : "=r"(r)
+        : "r"((uint32_t)x), "r"(id)
+        : "memory");
+    return r != 0;
+}
+__device__ __forceinline__ void pair_sync(int id) { asm volatile("barrier.cta.sync %0, 64;" ::"r"(id) : "memory"); }
+
 struct Bars {
     uint64_t kv_full[kStages], kv_empty[kStages];
     uint64_t q_full, q_empty;
@@ -296,6 +316,10 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_c
     __shared__ Bars bars;
     __shared__ long long s_part[kThreads / 32], s_off;
     __shared__ int s_b, s_h, s_i;
+    // for the warp of the other keys: a warp's rows' maxima and sums, and whether none of
+    // its waits gave up
+    __shared__ float s_top[16][16], s_sum[16][16];
+    __shared__ int s_going[16];
     __shared__ uint32_t s_tmem;
     __shared__ volatile int s_dead;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -314,9 +338,9 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_c
         mbar_init(&bars.q_empty, 1);
         for (int m = 0; m < 2; ++m) {
             mbar_init(&bars.s_full[m], 1);
-            mbar_init(&bars.p_full[m], 4);
+            mbar_init(&bars.p_full[m], 16);
             mbar_init(&bars.o_full[m], 1);
-            mbar_init(&bars.o_empty[m], 4);
+            mbar_init(&bars.o_empty[m], 16);
         }
         mbar_init(&bars.drained, 1);
         fence_barrier_init();
@@ -384,7 +408,6 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_c
     const uint32_t ring_at = smem_u32(ring);
 
     if (warp >= kMmaWarp) {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
         if (warp == kKvWarp) {
             // --------------------------------------------------- K and V tiles
             if (lane == 0) {
@@ -494,17 +517,17 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_c
                         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                         __syncwarp();
                     }
+                    if (!last && !(ok = wait(&bars.kv_full[sk], pk, &s_dead, p.status))) break;
+                    const uint64_t b = dv + (uint64_t)(sv * kTileBytes >> 4);
                     for (int m = 0; m < halves; ++m) {
-                        if (!(ok = wait(&bars.p_full[m], n_p[m] & 1, &s_dead, p.status))) break;
-                        ++n_p[m];
                         if (t == pc.t0) {
                             if (n_o[m] > 0 && !(ok = wait(&bars.o_empty[m], (n_o[m] - 1) & 1, &s_dead, p.status))) break;
                             ++n_o[m];
                         }
-                        if (m == 0 && !last && !(ok = wait(&bars.kv_full[sk], pk, &s_dead, p.status))) break;
+                        if (!(ok = wait(&bars.p_full[m], n_p[m] & 1, &s_dead, p.status))) break;
+                        ++n_p[m];
                         fence_after();
                         if (elect_one()) {
-                            const uint64_t b = dv + (uint64_t)(sv * kTileBytes >> 4);
 #pragma unroll
                             for (int s = 0; s < 8; ++s)
                                 tc_mma_ts(tmem + 256 + m * 128, tmem + m * 128 + s * 8, b + s * (uint64_t)(4096 >> 4), id_o,
@@ -530,132 +553,168 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_c
             if (!mbar_wait_bounded(&bars.drained, 0) && lane == 0) atomicOr(p.status, CS_DEVICE_WAIT_TIMEOUT);
         }
     } else {
-        // ------------------------------------------------- softmax, a row a thread
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
-        const int m = warp >> 2;
-        const int row = threadIdx.x;               // of the block
-        const uint32_t t_s = tmem + ((uint32_t)(warp & 3) << 21) + m * 128, t_o = t_s + 256;
-        const int my_token = row / p.G, my_head = row - my_token * p.G;
+        // ------------------------------------------- softmax, four threads a row
+        // Warps w and w + 8 take lanes 32 (w % 4) + 16 (w / 4 % 2) .. of either half, the
+        // first keys 0-63 of a tile, the second 64-127; threads i and i + 16 share a row,
+        // 32 keys each (and as many dims of O).  The two warps agree at a barrier of their
+        // own whether the weights stand, after which each may write over the other's scores.
+        const int part = (warp >> 3) * 2 + (lane >> 4);     // the thread's quarter of keys and dims
+        const int lane0 = (warp & 3) * 32 + ((warp >> 2) & 1) * 16;
+        const int pair = 1 + (warp & 7);
+        const uint32_t t_row = tmem + ((uint32_t)lane0 << 16);
         const float c = p.scale_log2;
-        uint32_t n_s = 0, n_o = 0;
+        int token[2], head[2];
+#pragma unroll
+        for (int m = 0; m < 2; ++m) {
+            token[m] = (m * kHalf + lane0 + (lane & 15)) / p.G;
+            head[m] = m * kHalf + lane0 + (lane & 15) - token[m] * p.G;
+        }
+        uint32_t n_s[2] = {0, 0}, n_o[2] = {0, 0};
         bool ok = true;
-        while (ok && pc.next()) {
-            const bool mine_ = my_token < pc.tokens;
-            const size_t out_row = (size_t)(pc.pstart + pc.token0 + my_token) * p.Hq + (size_t)pc.ph * p.G + my_head;
+        while (pc.next()) {
+            const size_t out_at = ((size_t)(pc.pstart + pc.token0) * p.Hq + (size_t)pc.ph * p.G) * kD + part * 32;
+            const int halves = pc.tokens * p.G > kHalf ? 2 : 1;
             if (pc.tiles == 0) {   // no key at all
-                if (mine_) {
-                    const uint32_t zero[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-                    for (int j = 0; j < 8; ++j) store32(p.out + out_row * kD + j * 16, zero);
-                }
+                const uint32_t zero[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+#pragma unroll
+                for (int m = 0; m < 2; ++m)
+                    if (token[m] < pc.tokens)
+                        for (int j = 0; j < 2; ++j)
+                            store32(p.out + out_at + ((size_t)token[m] * p.Hq + head[m]) * kD + j * 16, zero);
                 continue;
             }
-            if (m == 1 && pc.tokens * p.G <= kHalf) continue;
-            const bool any = __any_sync(0xffffffffu, mine_);
-            // keys that the row sees
-            const int seen = max(0, pc.keys - (pc.tokens - 1 - min(my_token, pc.tokens - 1)));
-            float m_run = kNegInf, l_run = 0.f;
-            for (int t = pc.t0; t < pc.t1; ++t) {
-                if (!(ok = wait(&bars.s_full[m], n_s & 1, &s_dead, p.status))) break;
-                ++n_s;
-                fence_after();
-                if (any) {
-                    float s[4][32];
+            // the maximum that the weights go by, what takes a score to its weight's exponent,
+            // the sum of this thread's weights
+            float m_run[2] = {kNegInf, kNegInf}, neg[2] = {0.f, 0.f}, l_run[2] = {0.f, 0.f};
+            bool any[2];   // (the same in both warps of a pair)
 #pragma unroll
-                    for (int q = 0; q < 4; ++q) tmem_ld32(t_s + q * 32, s[q]);
+            for (int m = 0; m < 2; ++m) any[m] = __any_sync(0xffffffffu, token[m] < pc.tokens);
+            // (a wait that gave up: the two warps leave the loop together, and meet at as many
+            // barriers, whichever of them it was)
+            bool stop = false;
+            for (int t = pc.t0; !stop && t < pc.t1; ++t) {
 #pragma unroll
-                    for (int q = 0; q < 4; ++q) tmem_ld_done(s[q]);
-                    const int lim = seen - t * kKeys;
-                    if (lim < kKeys) {
-#pragma unroll
-                        for (int q = 0; q < 4; ++q) hide(s[q], lim - 32 * q);
-                    }
-                    const float mt = fmaxf(max3(top_of(s[0]), top_of(s[1]), top_of(s[2])), top_of(s[3]));
-                    float alpha = 1.f;
-                    if (mt != kNegInf && (m_run == kNegInf || (mt - m_run) * c > kRescale)) {
-                        alpha = m_run == kNegInf ? 0.f : ex2((m_run - mt) * c);
-                        m_run = mt;
-                    }
-                    if (__any_sync(0xffffffffu, alpha != 1.f) && t != pc.t0) {
-                        // P V of the tile before is complete (see above)
-#pragma unroll 1
-                        for (int q = 0; q < 8; ++q) {
-                            uint32_t o[16];
-                            tmem_ld16(t_o + q * 16, o);
-                            tmem_ld_done(o);
-#pragma unroll
-                            for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * alpha);
-                            tmem_st16(t_o + q * 16, o);
-                        }
-                    }
-                    const float neg = m_run == kNegInf ? 0.f : -m_run * c - kPShift;
-                    const uint64_t c2 = f2_pack(c, c), n2 = f2_pack(neg, neg);
-                    uint64_t sum[2] = {0ull, 0ull};
-#pragma unroll
-                    for (int q = 0; q < 4; ++q) {
+                for (int m = 0; m < 2; ++m) {
+                    if (m == halves || stop) break;
+                    ok = wait(&bars.s_full[m], n_s[m] & 1, &s_dead, p.status) && ok;
+                    ++n_s[m];
+                    fence_after();
+                    if (any[m]) {
+                        const uint32_t t_s = t_row + m * 128, t_o = t_row + 256 + m * 128 + (warp >> 3) * 64;
+                        float s[32];
+                        tmem_ld32<32>(t_s + (warp >> 3) * 64, s);
+                        tmem_ld_done(s);
+                        // keys that the row sees, from this thread's first one on
+                        const int lim = pc.keys - (pc.tokens - 1 - min(token[m], pc.tokens - 1)) - t * kKeys - part * 32;
+                        if (__builtin_expect(lim < 32, 0)) hide(s, lim);
+                        // The weights by the maximum so far.  A sum within 2^8 says that no score
+                        // passed it by more than 8; otherwise, and where there is none, the
+                        // maximum of the tile is found and the weights are taken again.
                         uint32_t w[16];
+                        float sum;
+                        auto weights = [&] {
+                            const uint64_t c2 = f2_pack(c, c), n2 = f2_pack(neg[m], neg[m]);
+                            uint64_t sums[2] = {0ull, 0ull};
 #pragma unroll
-                        for (int e = 0; e < 16; ++e) {
-                            float x0, x1;
-                            f2_unpack(f2_fma(f2_pack(s[q][2 * e], s[q][2 * e + 1]), c2, n2), x0, x1);
-                            const float p0 = ex2(x0), p1 = ex2(x1);
-                            sum[e & 1] = f2_add(sum[e & 1], f2_pack(p0, p1));
-                            w[e] = pack_bf16x2(p0, p1);
+                            for (int e = 0; e < 16; ++e) {
+                                float x0, x1;
+                                f2_unpack(f2_fma(f2_pack(s[2 * e], s[2 * e + 1]), c2, n2), x0, x1);
+                                const float p0 = ex2(x0), p1 = ex2(x1);
+                                sums[e & 1] = f2_add(sums[e & 1], f2_pack(p0, p1));
+                                w[e] = pack_bf16x2(p0, p1);
+                            }
+                            float a0, a1;
+                            f2_unpack(f2_add(sums[0], sums[1]), a0, a1);
+                            sum = a0 + a1;
+                        };
+                        weights();
+                        if (__builtin_expect(pair_any(pair, !ok || !(sum <= kMostSum) || m_run[m] == kNegInf), 0)) {
+                            const float mh = top_of(s);
+                            const float mw = fmaxf(mh, __shfl_xor_sync(0xffffffffu, mh, 16));
+                            if (lane < 16) s_top[warp][lane] = mw;
+                            if (lane == 0) s_going[warp] = ok;
+                            pair_sync(pair);
+                            stop = !ok || !s_going[warp ^ 8];
+                            if (stop) break;
+                            const float mt = fmaxf(m_run[m], fmaxf(mw, s_top[warp ^ 8][lane & 15]));
+                            const float alpha = mt > m_run[m] ? ex2((m_run[m] - mt) * c) : 1.f;   // (0 where there was none)
+                            m_run[m] = mt;
+                            neg[m] = mt == kNegInf ? 0.f : -mt * c - kPShift;
+                            l_run[m] *= alpha;
+                            if (t != pc.t0) {
+                                // P V of the tile before is complete (see above)
+#pragma unroll 1
+                                for (int q = 0; q < 2; ++q) {
+                                    uint32_t o[16];
+                                    tmem_ld16<32>(t_o + q * 16, o);
+                                    tmem_ld_done(o);
+#pragma unroll
+                                    for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * alpha);
+                                    tmem_st16<32>(t_o + q * 16, o);
+                                }
+                            }
+                            weights();
                         }
-                        tmem_st16(t_s + q * 16, w);
+                        tmem_st16<16>(t_s + (warp >> 3) * 32, w);
+                        l_run[m] += sum;
+                        tmem_st_done();
                     }
-                    float a0, a1;
-                    f2_unpack(f2_add(sum[0], sum[1]), a0, a1);
-                    l_run = l_run * alpha + (a0 + a1);
-                    tmem_st_done();
+                    fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&bars.p_full[m]);
+                }
+            }
+            // ---- the piece's end
+            const bool whole = pc.t0 == 0 && pc.t1 == pc.tiles;
+            const size_t slot = 2 * (size_t)blockIdx.x + (pc.t0 == 0);
+#pragma unroll
+            for (int m = 0; m < 2; ++m) {
+                if (m == halves) break;
+                ok = wait(&bars.o_full[m], n_o[m] & 1, &s_dead, p.status) && ok;
+                ++n_o[m];
+                fence_after();
+                if (any[m]) {
+                    float l = l_run[m];
+                    l += __shfl_xor_sync(0xffffffffu, l, 16);
+                    if (lane < 16) s_sum[warp][lane] = l;
+                    pair_sync(pair);
+                    l += s_sum[warp ^ 8][lane & 15];
+                    const float inv = l > 0.f ? 1.f / l : 0.f;
+                    float o[32];
+                    tmem_ld32<32>(t_row + 256 + m * 128 + (warp >> 3) * 64, o);
+                    tmem_ld_done(o);
+                    if (ok && token[m] < pc.tokens) {
+                        if (whole) {
+                            __nv_bfloat16* dst = p.out + out_at + ((size_t)token[m] * p.Hq + head[m]) * kD;
+#pragma unroll
+                            for (int j = 0; j < 2; ++j) {
+                                uint32_t r[8];
+#pragma unroll
+                                for (int e = 0; e < 8; ++e)
+                                    r[e] = pack_bf16x2(o[16 * j + 2 * e] * inv, o[16 * j + 2 * e + 1] * inv);
+                                store32(dst + j * 16, r);
+                            }
+                        } else {
+                            const size_t row = slot * p.rows + m * kHalf + lane0 + (lane & 15);
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) {
+                                uint32_t r[8];
+#pragma unroll
+                                for (int e = 0; e < 8; ++e) r[e] = __float_as_uint(o[8 * j + e] * inv);
+                                store32(p.part_o + row * kD + part * 32 + j * 8, r);
+                            }
+                            if (part == 0)
+                                p.part_ml[row] = make_float2(m_run[m] == kNegInf ? kNegInf : m_run[m] * c, l);
+                        }
+                    }
+                    pair_sync(pair);   // (its sums have been read)
                 }
                 fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(&bars.p_full[m]);
+                if (lane == 0) mbar_arrive(&bars.o_empty[m]);
             }
-            if (!ok) break;
-            // ---- the piece's end
-            if (!(ok = wait(&bars.o_full[m], n_o & 1, &s_dead, p.status))) break;
-            ++n_o;
-            fence_after();
-            const bool whole = pc.t0 == 0 && pc.t1 == pc.tiles;
-            const float inv = l_run > 0.f ? 1.f / l_run : 0.f;
-            const size_t slot = 2 * (size_t)blockIdx.x + (pc.t0 == 0);
-            if (any) {
-#pragma unroll 1
-                for (int q = 0; q < 4; ++q) {
-                    float o[32];
-                    tmem_ld32(t_o + q * 32, o);
-                    tmem_ld_done(o);
-                    if (!mine_) continue;
-                    if (whole) {
-#pragma unroll
-                        for (int j = 0; j < 2; ++j) {
-                            uint32_t r[8];
-#pragma unroll
-                            for (int e = 0; e < 8; ++e)
-                                r[e] = pack_bf16x2(o[16 * j + 2 * e] * inv, o[16 * j + 2 * e + 1] * inv);
-                            store32(p.out + out_row * kD + q * 32 + j * 16, r);
-                        }
-                    } else {
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            uint32_t r[8];
-#pragma unroll
-                            for (int e = 0; e < 8; ++e) r[e] = __float_as_uint(o[8 * j + e] * inv);
-                            store32(p.part_o + (slot * p.rows + row) * kD + q * 32 + j * 8, r);
-                        }
-                    }
-                }
-                if (!whole) {
-                    if (mine_) p.part_ml[slot * p.rows + row] = make_float2(m_run == kNegInf ? kNegInf : m_run * c, l_run);
-                    if (threadIdx.x == 0)
-                        p.slots[slot] = make_int4(pc.pb, pc.ph, pc.pi,
-                                                  (pc.t0 == 0 ? kLeads : 0) | (pc.t1 == pc.tiles ? kEnds : 0));
-                }
-            }
-            fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&bars.o_empty[m]);
+            if (!whole && threadIdx.x == 0)
+                p.slots[slot] = make_int4(pc.pb, pc.ph, pc.pi, (pc.t0 == 0 ? kLeads : 0) | (pc.t1 == pc.tiles ? kEnds : 0));
         }
     }
     fence_before();
