@@ -10,20 +10,19 @@
 // closed forms, so a CTA finds its range from the lengths alone.
 //
 // A CTA (twenty warps):
-//   warps 0-15      softmax, of query rows 0-127 and then 128-255 of a tile: a warp takes
+//   warps 4-19      softmax, of query rows 0-127 and then 128-255 of a tile: a warp takes
 //                   16 rows and half of a tile's keys, two threads a row;
-//   warp 16         issues the products: S = Q K^T (M 128, N 128 keys, 8 steps of 16
+//   warp 0          issues the products: S = Q K^T (M 128, N 128 keys, 8 steps of 16
 //                   dims) and O += P V (N 128 dims, 8 steps of 16 keys), tcgen05 with
 //                   S, P (over S) and O in tensor memory: 2 x (128 + 128) columns;
-//   warp 17         brings K and V tiles (TMA, one box a page piece) into a ring of
+//   warp 1          brings K and V tiles (TMA, one box a page piece) into a ring of
 //                   five 32 KB stages;
-//   warp 18         brings a block's query rows (TMA).
+//   warp 2          brings a block's query rows (TMA).
 // The products of one half run while the softmax of the other does: the issuer goes
 // round P0 V, Q0 K', P1 V, Q1 K', and a half's S_j+1 being complete says that its
 // P_j V_j is too (one thread's products complete in order), so O may be rescaled
 // then.  The running maximum moves only for a growth of more than 2^8.
-// Every wait on a barrier is bounded; one that gives up sets the status word and a flag
-// that ends every warp's loop.
+// Every wait on a barrier is bounded; one that gives up sets the status word.
 #include <cudaTypedefs.h>
 #include <math.h>
 
@@ -40,7 +39,7 @@ constexpr int kRows = 256;                         // query rows of a block
 constexpr int kHalf = 128;                         // ... of one of its two MMA tiles
 constexpr int kKeys = 128;                         // keys of a tile
 constexpr int kThreads = 640;
-constexpr int kMmaWarp = 16, kKvWarp = 17, kQWarp = 18;
+constexpr int kMmaWarp = 0, kKvWarp = 1, kQWarp = 2, kFirstSoftmax = 4;
 constexpr int kStages = 5;
 constexpr int kTileBytes = kKeys * kD * 2;
 constexpr int kQBytes = kRows * kD * 2;
@@ -291,19 +290,17 @@ struct Bars {
     uint64_t drained;
 };
 
-// Waits for the phase of the given parity, the whole warp; false, at once, after any
-// wait of the block has given up.  (In line: registers are moved between warps, and a
-// function has those of a call's convention.)
-__device__ __forceinline__ bool wait(uint64_t* bar, uint32_t parity, volatile int* dead, int* status) {
-    bool done = mbar_test_wait(bar, parity);
-    if (!done && !*dead) {
-        done = mbar_wait_bounded(bar, parity);
-        if (!done) {
-            *dead = 1;
-            atomicOr(status, CS_DEVICE_WAIT_TIMEOUT);
-        }
+// Waits for the phase of the given parity, the whole warp; any wait returns at once
+// after one of the block has given up.  (What follows then works on whatever is there,
+// within the same bounds, to the end, and the status says so: no warp leaves before
+// another that it meets at a barrier.)
+__device__ __forceinline__ void wait(uint64_t* bar, uint32_t parity, volatile int* dead, int* status) {
+    if (mbar_try_wait(bar, parity)) return;
+    if (!*dead && !mbar_wait_bounded(bar, parity)) {
+        *dead = 1;
+        atomicOr(status, CS_DEVICE_WAIT_TIMEOUT);
     }
-    return __all_sync(0xffffffffu, done);
+    __syncwarp();
 }
 
 __global__ void __launch_bounds__(kThreads, 1)
@@ -316,10 +313,7 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_c
     __shared__ Bars bars;
     __shared__ long long s_part[kThreads / 32], s_off;
     __shared__ int s_b, s_h, s_i;
-    // for the warp of the other keys: a warp's rows' maxima and sums, and whether none of
-    // its waits gave up
-    __shared__ float s_top[16][16], s_sum[16][16];
-    __shared__ int s_going[16];
+    __shared__ float s_top[16][16], s_sum[16][16];   // a warp's rows' maxima and sums, for the warp of the other keys
     __shared__ uint32_t s_tmem;
     __shared__ volatile int s_dead;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -407,7 +401,7 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_c
     Pieces pc(&p, s_b, s_h, s_i, s_off, hi - lo);
     const uint32_t ring_at = smem_u32(ring);
 
-    if (warp >= kMmaWarp) {
+    if (warp < kFirstSoftmax) {
         if (warp == kKvWarp) {
             // --------------------------------------------------- K and V tiles
             if (lane == 0) {
@@ -416,15 +410,14 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_c
             }
             const int box = min(p.ps, kKeys), pieces = kKeys / box;
             uint32_t at_stage = 0;   // stages used so far
-            bool ok = true;
-            while (ok && pc.next()) {
+            while (pc.next()) {
                 const int32_t* row = p.page_table + (size_t)pc.pb * p.max_pages;
                 auto page_of = [&](int t) {
                     const int key = t * kKeys + lane * box;
                     return lane < pieces && key < pc.pL ? __ldcg(row + (key >> p.ps_log2)) : -1;
                 };
                 int page = pc.t0 < pc.t1 ? page_of(pc.t0) : -1;
-                for (int t = pc.t0; ok && t < pc.t1; ++t) {
+                for (int t = pc.t0; t < pc.t1; ++t) {
                     const int key = t * kKeys + lane * box;
                     const int live = min(pieces, (pc.pL - t * kKeys + box - 1) / box);
                     // (a page outside the pool reads as zeros, from in front of it)
@@ -436,10 +429,7 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_c
                     for (int v = 0; v < 2; ++v) {
                         const uint32_t st = at_stage % kStages, round = at_stage / kStages;
                         ++at_stage;
-                        if (round > 0 && !(ok = wait(&bars.kv_empty[st], (round - 1) & 1, &s_dead, p.status))) {
-                            --at_stage;
-                            break;
-                        }
+                        if (round > 0) wait(&bars.kv_empty[st], (round - 1) & 1, &s_dead, p.status);
                         if (lane == 0) mbar_arrive_expect_tx(&bars.kv_full[st], (uint32_t)live * box * (kD * 2));
                         __syncwarp();
                         if (lane < live)
@@ -461,7 +451,7 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_c
             uint32_t piece = 0;
             while (pc.next()) {
                 if (pc.tiles == 0) continue;
-                if (piece > 0 && !wait(&bars.q_empty, (piece - 1) & 1, &s_dead, p.status)) break;
+                if (piece > 0) wait(&bars.q_empty, (piece - 1) & 1, &s_dead, p.status);
                 ++piece;
                 const bool few = pc.tokens <= p.small_tokens;
                 const int box = few ? p.small_tokens : p.block_tokens;
@@ -485,27 +475,33 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_c
                            b + (s >> 2) * (uint64_t)(1024 >> 4) + (s & 3) * 2, id_s, s > 0);
                 tc_commit(&bars.s_full[m]);
             };
-            uint32_t stage = 0, piece = 0, n_p[2] = {0, 0}, n_o[2] = {0, 0};   // (as many phases as there were)
-            bool ok = true;
-            while (ok && pc.next()) {
+            // A tile's waits come while the products before it still run, where what they wait
+            // for is there; its V, and the K of the tile behind it:
+            uint32_t stage = 0, piece = 0, n_p = 0, n_p1 = 0, n_o = 0, n_o1 = 0;   // (as many phases as there were)
+            auto landed = [&](uint32_t n) { return mbar_test_wait(&bars.kv_full[n % kStages], (n / kStages) & 1); };
+            auto need = [&](uint32_t n) { wait(&bars.kv_full[n % kStages], (n / kStages) & 1, &s_dead, p.status); };
+            while (pc.next()) {
                 if (pc.tiles == 0) continue;
-                const int halves = pc.tokens * p.G > kHalf ? 2 : 1;
-                if (!(ok = wait(&bars.q_full, piece & 1, &s_dead, p.status))) break;
+                const bool two = pc.tokens * p.G > kHalf;
+                wait(&bars.q_full, piece & 1, &s_dead, p.status);
                 ++piece;
-                const uint32_t st = stage % kStages;
-                if (!(ok = wait(&bars.kv_full[st], (stage / kStages) & 1, &s_dead, p.status))) break;
-                ++stage;
+                need(stage);
                 if (elect_one()) {
-                    for (int m = 0; m < halves; ++m) scores(m, st);
-                    tc_commit(&bars.kv_empty[st]);
+                    scores(0, stage % kStages);
+                    if (two) scores(1, stage % kStages);
+                    tc_commit(&bars.kv_empty[stage % kStages]);
                     if (pc.t0 + 1 == pc.t1) tc_commit(&bars.q_empty);
                 }
                 __syncwarp();
-                for (int t = pc.t0; ok && t < pc.t1; ++t) {
-                    const bool last = t + 1 == pc.t1;
+                ++stage;
+                bool there = false;
+                for (int t = pc.t0; t < pc.t1; ++t) {
+                    const bool first = t == pc.t0, last = t + 1 == pc.t1;
                     const uint32_t sv = stage % kStages, sk = (stage + 1) % kStages;
-                    const uint32_t pv = (stage / kStages) & 1, pk = ((stage + 1) / kStages) & 1;
-                    if (!(ok = wait(&bars.kv_full[sv], pv, &s_dead, p.status))) break;
+                    if (!there) {
+                        need(stage);
+                        if (!last) need(stage + 1);
+                    }
                     // slots past the context's end may hold any bits, and their weights are 0
                     const int live = pc.pL - t * kKeys;
                     if (live < kKeys) {
@@ -517,27 +513,32 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_c
                         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                         __syncwarp();
                     }
-                    if (!last && !(ok = wait(&bars.kv_full[sk], pk, &s_dead, p.status))) break;
                     const uint64_t b = dv + (uint64_t)(sv * kTileBytes >> 4);
-                    for (int m = 0; m < halves; ++m) {
-                        if (t == pc.t0) {
-                            if (n_o[m] > 0 && !(ok = wait(&bars.o_empty[m], (n_o[m] - 1) & 1, &s_dead, p.status))) break;
-                            ++n_o[m];
-                        }
-                        if (!(ok = wait(&bars.p_full[m], n_p[m] & 1, &s_dead, p.status))) break;
-                        ++n_p[m];
+                    auto values = [&](int m) {
+#pragma unroll
+                        for (int s = 0; s < 8; ++s)
+                            tc_mma_ts(tmem + 256 + m * 128, tmem + m * 128 + s * 8, b + s * (uint64_t)(4096 >> 4), id_o,
+                                      !first || s > 0);
+                        if (last) tc_commit(&bars.o_full[m]);
+                    };
+                    if (first && n_o++ > 0) wait(&bars.o_empty[0], n_o & 1, &s_dead, p.status);
+                    wait(&bars.p_full[0], n_p++ & 1, &s_dead, p.status);
+                    fence_after();
+                    if (elect_one()) {
+                        values(0);
+                        if (!last) scores(0, sk);
+                    }
+                    __syncwarp();
+                    if (two) {
+                        if (first && n_o1++ > 0) wait(&bars.o_empty[1], n_o1 & 1, &s_dead, p.status);
+                        wait(&bars.p_full[1], n_p1++ & 1, &s_dead, p.status);
                         fence_after();
                         if (elect_one()) {
-#pragma unroll
-                            for (int s = 0; s < 8; ++s)
-                                tc_mma_ts(tmem + 256 + m * 128, tmem + m * 128 + s * 8, b + s * (uint64_t)(4096 >> 4), id_o,
-                                          t > pc.t0 || s > 0);
-                            if (last) tc_commit(&bars.o_full[m]);
-                            else scores(m, sk);
+                            values(1);
+                            if (!last) scores(1, sk);
                         }
                         __syncwarp();
                     }
-                    if (!ok) break;
                     if (elect_one()) {
                         tc_commit(&bars.kv_empty[sv]);
                         if (!last) tc_commit(&bars.kv_empty[sk]);
@@ -545,6 +546,7 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_c
                     }
                     __syncwarp();
                     stage += last ? 1 : 2;
+                    there = !last && __all_sync(0xffffffffu, landed(stage) && (t + 2 == pc.t1 || landed(stage + 1)));
                 }
             }
             // every product is complete before tensor memory is given back
@@ -554,13 +556,14 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_c
         }
     } else {
         // ------------------------------------------- softmax, four threads a row
-        // Warps w and w + 8 take lanes 32 (w % 4) + 16 (w / 4 % 2) .. of either half, the
+        // Of these, warps w and w + 8 take lanes 32 (w % 4) + 16 (w / 4 % 2) .. of either half, the
         // first keys 0-63 of a tile, the second 64-127; threads i and i + 16 share a row,
         // 32 keys each (and as many dims of O).  The two warps agree at a barrier of their
         // own whether the weights stand, after which each may write over the other's scores.
-        const int part = (warp >> 3) * 2 + (lane >> 4);     // the thread's quarter of keys and dims
-        const int lane0 = (warp & 3) * 32 + ((warp >> 2) & 1) * 16;
-        const int pair = 1 + (warp & 7);
+        const int sw = warp - kFirstSoftmax;
+        const int part = (sw >> 3) * 2 + (lane >> 4);     // the thread's quarter of keys and dims
+        const int lane0 = (sw & 3) * 32 + ((sw >> 2) & 1) * 16;
+        const int pair = 1 + (sw & 7);
         const uint32_t t_row = tmem + ((uint32_t)lane0 << 16);
         const float c = p.scale_log2;
         int token[2], head[2];
@@ -570,7 +573,6 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_c
             head[m] = m * kHalf + lane0 + (lane & 15) - token[m] * p.G;
         }
         uint32_t n_s[2] = {0, 0}, n_o[2] = {0, 0};
-        bool ok = true;
         while (pc.next()) {
             const size_t out_at = ((size_t)(pc.pstart + pc.token0) * p.Hq + (size_t)pc.ph * p.G) * kD + part * 32;
             const int halves = pc.tokens * p.G > kHalf ? 2 : 1;
@@ -589,20 +591,17 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_c
             bool any[2];   // (the same in both warps of a pair)
 #pragma unroll
             for (int m = 0; m < 2; ++m) any[m] = __any_sync(0xffffffffu, token[m] < pc.tokens);
-            // (a wait that gave up: the two warps leave the loop together, and meet at as many
-            // barriers, whichever of them it was)
-            bool stop = false;
-            for (int t = pc.t0; !stop && t < pc.t1; ++t) {
+            for (int t = pc.t0; t < pc.t1; ++t) {
 #pragma unroll
                 for (int m = 0; m < 2; ++m) {
-                    if (m == halves || stop) break;
-                    ok = wait(&bars.s_full[m], n_s[m] & 1, &s_dead, p.status) && ok;
+                    if (m == halves) break;
+                    wait(&bars.s_full[m], n_s[m] & 1, &s_dead, p.status);
                     ++n_s[m];
                     fence_after();
                     if (any[m]) {
-                        const uint32_t t_s = t_row + m * 128, t_o = t_row + 256 + m * 128 + (warp >> 3) * 64;
+                        const uint32_t t_s = t_row + m * 128, t_o = t_row + 256 + m * 128 + (sw >> 3) * 64;
                         float s[32];
-                        tmem_ld32<32>(t_s + (warp >> 3) * 64, s);
+                        tmem_ld32<32>(t_s + (sw >> 3) * 64, s);
                         tmem_ld_done(s);
                         // keys that the row sees, from this thread's first one on
                         const int lim = pc.keys - (pc.tokens - 1 - min(token[m], pc.tokens - 1)) - t * kKeys - part * 32;
@@ -628,15 +627,12 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_c
                             sum = a0 + a1;
                         };
                         weights();
-                        if (__builtin_expect(pair_any(pair, !ok || !(sum <= kMostSum) || m_run[m] == kNegInf), 0)) {
+                        if (__builtin_expect(pair_any(pair, !(sum <= kMostSum) || m_run[m] == kNegInf), 0)) {
                             const float mh = top_of(s);
                             const float mw = fmaxf(mh, __shfl_xor_sync(0xffffffffu, mh, 16));
-                            if (lane < 16) s_top[warp][lane] = mw;
-                            if (lane == 0) s_going[warp] = ok;
+                            if (lane < 16) s_top[sw][lane] = mw;
                             pair_sync(pair);
-                            stop = !ok || !s_going[warp ^ 8];
-                            if (stop) break;
-                            const float mt = fmaxf(m_run[m], fmaxf(mw, s_top[warp ^ 8][lane & 15]));
+                            const float mt = fmaxf(m_run[m], fmaxf(mw, s_top[sw ^ 8][lane & 15]));
                             const float alpha = mt > m_run[m] ? ex2((m_run[m] - mt) * c) : 1.f;   // (0 where there was none)
                             m_run[m] = mt;
                             neg[m] = mt == kNegInf ? 0.f : -mt * c - kPShift;
@@ -655,7 +651,7 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_c
                             }
                             weights();
                         }
-                        tmem_st16<16>(t_s + (warp >> 3) * 32, w);
+                        tmem_st16<16>(t_s + (sw >> 3) * 32, w);
                         l_run[m] += sum;
                         tmem_st_done();
                     }
@@ -670,20 +666,20 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_c
 #pragma unroll
             for (int m = 0; m < 2; ++m) {
                 if (m == halves) break;
-                ok = wait(&bars.o_full[m], n_o[m] & 1, &s_dead, p.status) && ok;
+                wait(&bars.o_full[m], n_o[m] & 1, &s_dead, p.status);
                 ++n_o[m];
                 fence_after();
                 if (any[m]) {
                     float l = l_run[m];
                     l += __shfl_xor_sync(0xffffffffu, l, 16);
-                    if (lane < 16) s_sum[warp][lane] = l;
+                    if (lane < 16) s_sum[sw][lane] = l;
                     pair_sync(pair);
-                    l += s_sum[warp ^ 8][lane & 15];
+                    l += s_sum[sw ^ 8][lane & 15];
                     const float inv = l > 0.f ? 1.f / l : 0.f;
                     float o[32];
-                    tmem_ld32<32>(t_row + 256 + m * 128 + (warp >> 3) * 64, o);
+                    tmem_ld32<32>(t_row + 256 + m * 128 + (sw >> 3) * 64, o);
                     tmem_ld_done(o);
-                    if (ok && token[m] < pc.tokens) {
+                    if (token[m] < pc.tokens) {
                         if (whole) {
                             __nv_bfloat16* dst = p.out + out_at + ((size_t)token[m] * p.Hq + head[m]) * kD;
 #pragma unroll
@@ -713,7 +709,7 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_c
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&bars.o_empty[m]);
             }
-            if (!whole && threadIdx.x == 0)
+            if (!whole && threadIdx.x == kFirstSoftmax * 32)
                 p.slots[slot] = make_int4(pc.pb, pc.ph, pc.pi, (pc.t0 == 0 ? kLeads : 0) | (pc.t1 == pc.tiles ? kEnds : 0));
         }
     }
