@@ -12,7 +12,7 @@
 // A CTA (twenty warps):
 //   warps 4-19      softmax, of query rows 0-127 and then 128-255 of a tile: a warp takes
 //                   16 rows and half of a tile's keys, two threads a row;
-//   warp 0          issues the products: S = Q K^T (M 128, N 128 keys, 8 steps of 16
+//   warps 0, 3      issue the products of either: S = Q K^T (M 128, N 128 keys, 8 steps of 16
 //                   dims) and O += P V (N 128 dims, 8 steps of 16 keys), tcgen05 with
 //                   S, P (over S) and O in tensor memory: 2 x (128 + 128) columns;
 //   warp 1          brings K and V tiles (TMA, one box a page piece) into a ring of
@@ -39,7 +39,7 @@ constexpr int kRows = 256;                         // query rows of a block
 constexpr int kHalf = 128;                         // ... of one of its two MMA tiles
 constexpr int kKeys = 128;                         // keys of a tile
 constexpr int kThreads = 640;
-constexpr int kMmaWarp = 0, kKvWarp = 1, kQWarp = 2, kFirstSoftmax = 4;
+constexpr int kMmaWarp = 0, kKvWarp = 1, kQWarp = 2, kMmaWarp1 = 3, kFirstSoftmax = 4;
 constexpr int kStages = 5;
 constexpr int kTileBytes = kKeys * kD * 2;
 constexpr int kQBytes = kRows * kD * 2;
@@ -66,79 +66,102 @@ struct ChunkParams {
 };
 constexpr int kLeads = 1, kEnds = 2;               // flags of a piece: it has its block's first tile, last tile
 
+// a / b for a >= 0, b > 0
+__device__ __forceinline__ long long quotient(long long a, long long b) { return div_pos(a, b); }
+
 // A request's blocks: block i has tokens [i T, min(n, (i+1) T)) and the keys in front
 // of and at the last of them; it weighs its keys + kBeginKeys.
 struct Blocks {
     int n, L, T, count;
     __device__ __forceinline__ Blocks(int n_, int L_, int T_) : n(n_), L(L_), T(T_), count((n_ + T_ - 1) / T_) {}
-    __device__ __forceinline__ int keys(int i) const { return max(0, L - n + min(n, (i + 1) * T)); }
     // the weight of blocks 0 .. i-1
     __device__ __forceinline__ long long before(int i) const {
         const long long first = (long long)L - n;   // keys in front of the new tokens
         const int full = min(i, count - 1);
         // blocks without a key (more new tokens than keys): all in front
-        const int none = first < 0 ? (int)min((long long)full, -first / T) : 0;
+        const int none = first < 0 ? min(full, (int)(n - L) / T) : 0;
         const long long a = none, b = full;
         long long w = (b - a) * first + T * ((b * (b + 1) - a * (a + 1)) / 2) + (long long)full * kBeginKeys;
         if (i == count) w += L + kBeginKeys;
         return w;
     }
+    // the block that place x of the whole weight lies in
+    __device__ __forceinline__ int at(long long x) const {
+        // i (a + T / 2) + i^2 T / 2 = x, nearly; then exactly
+        const float a = (float)(L - n) + kBeginKeys + 0.5f * (float)T, y = (float)x;
+        int i = L < n ? 0 : (int)(2.f * y / (a + sqrtf(a * a + 2.f * (float)T * y)));
+        i = max(0, min(i, count - 1));
+        while (i > 0 && before(i) > x) --i;
+        while (i + 1 < count && before(i + 1) <= x) ++i;
+        return i;
+    }
 };
 
 // The tile at place x of a block's weight w = keys + kBeginKeys
-__device__ __forceinline__ int tile_at(long long x, int keys) {
+__device__ __forceinline__ int tile_at(int x, int keys) {
     const int tiles = (keys + kKeys - 1) / kKeys;
     if (x <= 0) return 0;
     if (x >= keys + kBeginKeys) return tiles;
-    return (int)min((long long)tiles, max(0ll, (x - kBeginKeys + kKeys / 2) / kKeys));
+    return min(tiles, max(0, x - kBeginKeys + kKeys / 2) / kKeys);
 }
 
-// One piece after the other of a CTA's range.
-struct Pieces {
-    const ChunkParams* p;
-    int b, h, i;               // where the next piece begins
-    long long off, left;       // ... in its block; what is left of the range
-    int start, n, L;           // the request
-    // the piece
-    int t0, t1, tiles, keys, token0, tokens;
-    int pb, ph, pi, pL, pstart;
+// Where a CTA's range begins.
+struct Begin {
+    int b, h, i;               // request of the launch, KV head, block
+    int start, n, L;           // the request's rows and length
+    int off;                   // how far into the block's weight
+};
 
-    __device__ __forceinline__ void load() {
-        for (; b < p->nb; ++b) {
-            p->batch.rows_of(p->b0 + b, start, n, L);
-            if (n > 0) return;
-        }
-        left = 0;
+// One piece after the other of a CTA's range; every warp goes through them by itself.
+struct Pieces {
+    const ChunkParams& p;
+    Begin at;                  // where the next piece begins
+    int count;                 // blocks of its request
+    long long left;            // what is left of the range
+    int next_start, next_n, next_L;   // the request behind (read early)
+    // the piece: tiles [t0, t1) of `tiles`, the block's keys and tokens, its request, KV
+    // head and place
+    int t0, t1, tiles, keys, token0, tokens;
+    int b, h, i, L, start;
+
+    __device__ __forceinline__ Pieces(const ChunkParams& p_, const Begin& begin, long long size)
+        : p(p_), at(begin), count(0), left(begin.b >= 0 ? size : 0), next_start(0), next_n(0), next_L(0) {
+        if (left > 0) arrive();
     }
-    __device__ __forceinline__ Pieces(const ChunkParams* p_, int b_, int h_, int i_, long long off_, long long left_)
-        : p(p_), b(b_), h(h_), i(i_), off(off_), left(left_) {
-        if (left > 0) load();
+    __device__ __forceinline__ void arrive() {
+        count = (at.n + p.block_tokens - 1) / p.block_tokens;
+        if (at.b + 1 < p.nb) p.batch.rows_of(p.b0 + at.b + 1, next_start, next_n, next_L);
     }
     // false: no more
     __device__ __forceinline__ bool next() {
         while (left > 0) {
-            const Blocks blocks(n, L, p->block_tokens);
-            keys = blocks.keys(i);
-            const long long w = keys + kBeginKeys, end = min(w, off + left);
+            token0 = at.i * p.block_tokens;
+            tokens = min(at.n - token0, p.block_tokens);
+            keys = max(0, at.L - at.n + token0 + tokens);
             tiles = (keys + kKeys - 1) / kKeys;
-            t0 = tile_at(off, keys);
-            t1 = tile_at(end, keys);
-            const bool there = t1 > t0 || (tiles == 0 && off == 0);
-            token0 = i * blocks.T;
-            tokens = min(n - token0, blocks.T);
-            pb = p->b0 + b;
-            ph = h;
-            pi = i;
-            pL = L;
-            pstart = start;
-            left -= end - off;
-            off = 0;
-            if (left > 0 && ++i == blocks.count) {
-                i = 0;
-                if (++h == p->Hkv) {
-                    h = 0;
-                    ++b;
-                    load();
+            const int w = keys + kBeginKeys - at.off, take = left < w ? (int)left : w;
+            t0 = tile_at(at.off, keys);
+            t1 = tile_at(at.off + take, keys);
+            const bool there = t1 > t0 || (tiles == 0 && at.off == 0);
+            b = p.b0 + at.b;
+            h = at.h;
+            i = at.i;
+            L = at.L;
+            start = at.start;
+            left -= take;
+            at.off = 0;
+            if (left > 0 && ++at.i == count) {
+                at.i = 0;
+                if (++at.h == p.Hkv) {
+                    at.h = 0;
+                    do {
+                        ++at.b;
+                        at.start = next_start;
+                        at.n = next_n;
+                        at.L = next_L;
+                        if (at.b < p.nb) arrive();
+                    } while (at.n == 0 && at.b < p.nb);
+                    if (at.b >= p.nb) left = 0;
                 }
             }
             if (there) return true;
@@ -270,6 +293,15 @@ __device__ __forceinline__ void store32(void* p, const uint32_t (&r)[8]) {
                  : "memory");
 }
 
+// (one lane)
+__device__ __forceinline__ void wait_lane(uint64_t* bar, uint32_t parity, volatile int* dead, int* status) {
+    if (mbar_try_wait(bar, parity)) return;
+    if (!*dead && !mbar_wait_bounded(bar, parity)) {
+        *dead = 1;
+        atomicOr(status, CS_DEVICE_WAIT_TIMEOUT);
+    }
+}
+
 // The two warps of a pair: whether any of their threads says so; and a barrier.
 __device__ __forceinline__ bool pair_any(int id, bool x) {
     uint32_t r;
@@ -311,8 +343,8 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_c
     uint8_t* const sq = smem;                      // [dim half][row][128 B]
     uint8_t* const ring = smem + kQBytes;
     __shared__ Bars bars;
-    __shared__ long long s_part[kThreads / 32], s_off;
-    __shared__ int s_b, s_h, s_i;
+    __shared__ long long s_part[kThreads / 32];
+    __shared__ Begin s_begin;
     __shared__ float s_top[16][16], s_sum[16][16];   // a warp's rows' maxima and sums, for the warp of the other keys
     __shared__ uint32_t s_tmem;
     __shared__ volatile int s_dead;
@@ -322,21 +354,30 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_c
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(&s_tmem)) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
-    if (threadIdx.x == 0) {
+    if (warp == kKvWarp && lane == 0) {
+        tma_prefetch_desc(&map_k);
+        tma_prefetch_desc(&map_v);
+    }
+    if (warp == kQWarp && lane == 0) {
+        tma_prefetch_desc(&map_q);
+        tma_prefetch_desc(&map_q_small);
+    }
+    if (threadIdx.x == 3 * 32) {
         s_dead = 0;
+        s_begin.b = -1;
         for (int i = 0; i < kStages; ++i) {
             mbar_init(&bars.kv_full[i], 1);
-            mbar_init(&bars.kv_empty[i], 1);
+            mbar_init(&bars.kv_empty[i], 2);
         }
         mbar_init(&bars.q_full, 1);
-        mbar_init(&bars.q_empty, 1);
+        mbar_init(&bars.q_empty, 2);
         for (int m = 0; m < 2; ++m) {
             mbar_init(&bars.s_full[m], 1);
             mbar_init(&bars.p_full[m], 16);
             mbar_init(&bars.o_full[m], 1);
             mbar_init(&bars.o_empty[m], 16);
         }
-        mbar_init(&bars.drained, 1);
+        mbar_init(&bars.drained, 2);
         fence_barrier_init();
     }
     // (rows that no block fills: zeros are cheaper to multiply than noise)
@@ -345,20 +386,20 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_c
     wait_prior_grid();
     allow_dependent_launch();
 
-    // ---- the range: three requests a thread, their weights' running sum
+    // ---- the range: two requests a thread, their weights' running sum
     constexpr int kEach = (kMaxBatch + kThreads - 1) / kThreads;
-    long long weight[kEach], mine = 0;
+    long long weight[kEach], mine = 0;   // (of one KV head)
+    Begin own[kEach];
 #pragma unroll
     for (int e = 0; e < kEach; ++e) {
-        const int b = threadIdx.x * kEach + e;
+        own[e].b = threadIdx.x * kEach + e;
         weight[e] = 0;
-        if (b < p.nb) {
-            int start, n, L;
-            p.batch.rows_of(p.b0 + b, start, n, L);
-            const Blocks blocks(n, L, p.block_tokens);
-            if (n > 0) weight[e] = blocks.before(blocks.count) * p.Hkv;
+        if (own[e].b < p.nb) {
+            p.batch.rows_of(p.b0 + own[e].b, own[e].start, own[e].n, own[e].L);
+            const Blocks blocks(own[e].n, own[e].L, p.block_tokens);
+            if (own[e].n > 0) weight[e] = blocks.before(blocks.count);
         }
-        mine += weight[e];
+        mine += weight[e] * p.Hkv;
     }
     long long upto = mine;
 #pragma unroll
@@ -378,51 +419,46 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_c
         if (w < warp) at += s_part[w];
         total += s_part[w];
     }
-    const long long lo = total / gridDim.x * blockIdx.x + total % gridDim.x * blockIdx.x / gridDim.x;
-    const long long hi = total / gridDim.x * (blockIdx.x + 1) + total % gridDim.x * (blockIdx.x + 1) / gridDim.x;
+    // the first CTAs take one more of what is over
+    const long long each = quotient(total, gridDim.x);
+    const int over = (int)(total - each * gridDim.x), cta = blockIdx.x;
+    const long long lo = each * cta + min(cta, over), size = each + (cta < over);
 #pragma unroll
     for (int e = 0; e < kEach; ++e) {
-        if (weight[e] > 0 && at <= lo && lo < at + weight[e]) {
-            int start, n, L;
-            p.batch.rows_of(p.b0 + threadIdx.x * kEach + e, start, n, L);
-            const Blocks blocks(n, L, p.block_tokens);
-            const long long head = weight[e] / p.Hkv, in = (lo - at) % head;
-            int i = 0;
-            for (int step = 1 << 30; step > 0; step >>= 1)
-                if (i + step < blocks.count && blocks.before(i + step) <= in) i += step;
-            s_b = threadIdx.x * kEach + e;
-            s_h = (int)((lo - at) / head);
-            s_i = i;
-            s_off = in - blocks.before(i);
+        const long long in = lo - at;
+        if (size > 0 && in >= 0 && in < weight[e] * p.Hkv) {
+            Begin& a = own[e];
+            a.h = (int)quotient(in, weight[e]);
+            const long long x = in - a.h * weight[e];
+            const Blocks blocks(a.n, a.L, p.block_tokens);
+            a.i = blocks.at(x);
+            a.off = (int)(x - blocks.before(a.i));
+            s_begin = a;
         }
-        at += weight[e];
+        at += weight[e] * p.Hkv;
     }
     __syncthreads();
-    Pieces pc(&p, s_b, s_h, s_i, s_off, hi - lo);
+    Pieces pc(p, s_begin, size);
     const uint32_t ring_at = smem_u32(ring);
 
     if (warp < kFirstSoftmax) {
         if (warp == kKvWarp) {
             // --------------------------------------------------- K and V tiles
-            if (lane == 0) {
-                tma_prefetch_desc(&map_k);
-                tma_prefetch_desc(&map_v);
-            }
             const int box = min(p.ps, kKeys), pieces = kKeys / box;
             uint32_t at_stage = 0;   // stages used so far
             while (pc.next()) {
-                const int32_t* row = p.page_table + (size_t)pc.pb * p.max_pages;
+                const int32_t* row = p.page_table + (size_t)pc.b * p.max_pages;
                 auto page_of = [&](int t) {
                     const int key = t * kKeys + lane * box;
-                    return lane < pieces && key < pc.pL ? __ldcg(row + (key >> p.ps_log2)) : -1;
+                    return lane < pieces && key < pc.L ? __ldcg(row + (key >> p.ps_log2)) : -1;
                 };
                 int page = pc.t0 < pc.t1 ? page_of(pc.t0) : -1;
                 for (int t = pc.t0; t < pc.t1; ++t) {
                     const int key = t * kKeys + lane * box;
-                    const int live = min(pieces, (pc.pL - t * kKeys + box - 1) / box);
+                    const int live = min(pieces, (pc.L - t * kKeys + box - 1) / box);
                     // (a page outside the pool reads as zeros, from in front of it)
                     const int group = (unsigned)page < (unsigned)p.P
-                                          ? (int)(((long long)page * p.Hkv + pc.ph) * (p.ps >> 3) + ((key & (p.ps - 1)) >> 3))
+                                          ? (int)(((long long)page * p.Hkv + pc.h) * (p.ps >> 3) + ((key & (p.ps - 1)) >> 3))
                                           : -(box >> 3);
                     if (t + 1 < pc.t1) page = page_of(t + 1);
 #pragma unroll
@@ -444,10 +480,6 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_c
                     atomicOr(p.status, CS_DEVICE_WAIT_TIMEOUT);
         } else if (warp == kQWarp) {
             // ------------------------------------------------------ query rows
-            if (lane == 0) {
-                tma_prefetch_desc(&map_q);
-                tma_prefetch_desc(&map_q_small);
-            }
             uint32_t piece = 0;
             while (pc.next()) {
                 if (pc.tiles == 0) continue;
@@ -459,51 +491,59 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_c
                 __syncwarp();
                 if (lane < 2)
                     tma_load_3d(smem_u32(sq) + lane * (kQBytes / 2), few ? &map_q_small : &map_q, &bars.q_full, lane * 64,
-                                pc.ph * p.G, pc.pstart + pc.token0);
+                                pc.h * p.G, pc.start + pc.token0);
             }
             if (piece > 0 && !mbar_wait_bounded(&bars.q_full, (piece - 1) & 1) && lane == 0)
                 atomicOr(p.status, CS_DEVICE_WAIT_TIMEOUT);
-        } else if (warp == kMmaWarp) {
+        } else {
             // -------------------------------------------------------- products
-            const uint64_t dq = q_desc(smem_u32(sq)), dk = k_desc(ring_at), dv = v_desc(ring_at);
+            const int m = warp == kMmaWarp ? 0 : 1;
+            const uint64_t dq = q_desc(smem_u32(sq)) + (uint64_t)(m * (kHalf * 128) >> 4);
+            const uint64_t dk = k_desc(ring_at), dv = v_desc(ring_at);
+            const uint32_t t_s = tmem + m * 128, t_o = t_s + 256;
             constexpr uint32_t id_s = idesc_of(false), id_o = idesc_of(true);
-            auto scores = [&](int m, uint32_t st) {
-                const uint64_t a = dq + (uint64_t)(m * (kHalf * 128) >> 4), b = dk + (uint64_t)(st * kTileBytes >> 4);
+            auto scores = [&](uint32_t st) {
+                const uint64_t b = dk + (uint64_t)(st * kTileBytes >> 4);
 #pragma unroll
                 for (int s = 0; s < 8; ++s)
-                    mma_ss(tmem + m * 128, a + (s >> 2) * (uint64_t)(kQBytes / 2 >> 4) + (s & 3) * 2,
+                    mma_ss(t_s, dq + (s >> 2) * (uint64_t)(kQBytes / 2 >> 4) + (s & 3) * 2,
                            b + (s >> 2) * (uint64_t)(1024 >> 4) + (s & 3) * 2, id_s, s > 0);
                 tc_commit(&bars.s_full[m]);
             };
-            // A tile's waits come while the products before it still run, where what they wait
-            // for is there; its V, and the K of the tile behind it:
-            uint32_t stage = 0, piece = 0, n_p = 0, n_p1 = 0, n_o = 0, n_o1 = 0;   // (as many phases as there were)
-            auto landed = [&](uint32_t n) { return mbar_test_wait(&bars.kv_full[n % kStages], (n / kStages) & 1); };
+            uint32_t stage = 0, piece = 0, n_p = 0, n_o = 0;   // (as many phases as there were)
             auto need = [&](uint32_t n) { wait(&bars.kv_full[n % kStages], (n / kStages) & 1, &s_dead, p.status); };
             while (pc.next()) {
                 if (pc.tiles == 0) continue;
-                const bool two = pc.tokens * p.G > kHalf;
                 wait(&bars.q_full, piece & 1, &s_dead, p.status);
                 ++piece;
+                if (m == 1 && pc.tokens * p.G <= kHalf) {   // no row of this half
+                    if (lane == 0) {
+                        mbar_arrive(&bars.q_empty);
+                        for (int t = 2 * (pc.t1 - pc.t0); t > 0; --t) {
+                            const uint32_t n = stage++;
+                            wait_lane(&bars.kv_full[n % kStages], (n / kStages) & 1, &s_dead, p.status);
+                            mbar_arrive(&bars.kv_empty[n % kStages]);
+                        }
+                    }
+                    stage = __shfl_sync(0xffffffffu, stage, 0);
+                    continue;
+                }
                 need(stage);
                 if (elect_one()) {
-                    scores(0, stage % kStages);
-                    if (two) scores(1, stage % kStages);
+                    scores(stage % kStages);
                     tc_commit(&bars.kv_empty[stage % kStages]);
                     if (pc.t0 + 1 == pc.t1) tc_commit(&bars.q_empty);
                 }
                 __syncwarp();
                 ++stage;
-                bool there = false;
+                if (n_o++ > 0) wait(&bars.o_empty[m], n_o & 1, &s_dead, p.status);
                 for (int t = pc.t0; t < pc.t1; ++t) {
-                    const bool first = t == pc.t0, last = t + 1 == pc.t1;
+                    const bool last = t + 1 == pc.t1;
                     const uint32_t sv = stage % kStages, sk = (stage + 1) % kStages;
-                    if (!there) {
-                        need(stage);
-                        if (!last) need(stage + 1);
-                    }
+                    need(stage);
                     // slots past the context's end may hold any bits, and their weights are 0
-                    const int live = pc.pL - t * kKeys;
+                    // (either warp writes the same zeros before its products)
+                    const int live = pc.L - t * kKeys;
                     if (live < kKeys) {
                         uint4* v = reinterpret_cast<uint4*>(ring + sv * kTileBytes);
                         for (int i = lane; i < kTileBytes / 16; i += 32) {
@@ -513,40 +553,22 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_c
                         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                         __syncwarp();
                     }
-                    const uint64_t b = dv + (uint64_t)(sv * kTileBytes >> 4);
-                    auto values = [&](int m) {
-#pragma unroll
-                        for (int s = 0; s < 8; ++s)
-                            tc_mma_ts(tmem + 256 + m * 128, tmem + m * 128 + s * 8, b + s * (uint64_t)(4096 >> 4), id_o,
-                                      !first || s > 0);
-                        if (last) tc_commit(&bars.o_full[m]);
-                    };
-                    if (first && n_o++ > 0) wait(&bars.o_empty[0], n_o & 1, &s_dead, p.status);
-                    wait(&bars.p_full[0], n_p++ & 1, &s_dead, p.status);
+                    if (!last) need(stage + 1);
+                    wait(&bars.p_full[m], n_p++ & 1, &s_dead, p.status);
                     fence_after();
                     if (elect_one()) {
-                        values(0);
-                        if (!last) scores(0, sk);
-                    }
-                    __syncwarp();
-                    if (two) {
-                        if (first && n_o1++ > 0) wait(&bars.o_empty[1], n_o1 & 1, &s_dead, p.status);
-                        wait(&bars.p_full[1], n_p1++ & 1, &s_dead, p.status);
-                        fence_after();
-                        if (elect_one()) {
-                            values(1);
-                            if (!last) scores(1, sk);
-                        }
-                        __syncwarp();
-                    }
-                    if (elect_one()) {
+                        const uint64_t b = dv + (uint64_t)(sv * kTileBytes >> 4);
+#pragma unroll
+                        for (int s = 0; s < 8; ++s)
+                            tc_mma_ts(t_o, t_s + s * 8, b + s * (uint64_t)(4096 >> 4), id_o, t > pc.t0 || s > 0);
+                        if (last) tc_commit(&bars.o_full[m]);
+                        else scores(sk);
                         tc_commit(&bars.kv_empty[sv]);
                         if (!last) tc_commit(&bars.kv_empty[sk]);
                         if (t + 2 == pc.t1) tc_commit(&bars.q_empty);
                     }
                     __syncwarp();
                     stage += last ? 1 : 2;
-                    there = !last && __all_sync(0xffffffffu, landed(stage) && (t + 2 == pc.t1 || landed(stage + 1)));
                 }
             }
             // every product is complete before tensor memory is given back
@@ -574,7 +596,7 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_c
         }
         uint32_t n_s[2] = {0, 0}, n_o[2] = {0, 0};
         while (pc.next()) {
-            const size_t out_at = ((size_t)(pc.pstart + pc.token0) * p.Hq + (size_t)pc.ph * p.G) * kD + part * 32;
+            const size_t out_at = ((size_t)(pc.start + pc.token0) * p.Hq + (size_t)pc.h * p.G) * kD + part * 32;
             const int halves = pc.tokens * p.G > kHalf ? 2 : 1;
             if (pc.tiles == 0) {   // no key at all
                 const uint32_t zero[8] = {0, 0, 0, 0, 0, 0, 0, 0};
@@ -611,7 +633,8 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_c
                         // maximum of the tile is found and the weights are taken again.
                         uint32_t w[16];
                         float sum;
-                        auto weights = [&] {
+#pragma unroll 1
+                        for (bool again = false;; again = true) {
                             const uint64_t c2 = f2_pack(c, c), n2 = f2_pack(neg[m], neg[m]);
                             uint64_t sums[2] = {0ull, 0ull};
 #pragma unroll
@@ -625,9 +648,7 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_c
                             float a0, a1;
                             f2_unpack(f2_add(sums[0], sums[1]), a0, a1);
                             sum = a0 + a1;
-                        };
-                        weights();
-                        if (__builtin_expect(pair_any(pair, !(sum <= kMostSum) || m_run[m] == kNegInf), 0)) {
+                            if (again || !pair_any(pair, !(sum <= kMostSum) || m_run[m] == kNegInf)) break;
                             const float mh = top_of(s);
                             const float mw = fmaxf(mh, __shfl_xor_sync(0xffffffffu, mh, 16));
                             if (lane < 16) s_top[sw][lane] = mw;
@@ -649,7 +670,6 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_c
                                     tmem_st16<32>(t_o + q * 16, o);
                                 }
                             }
-                            weights();
                         }
                         tmem_st16<16>(t_s + (sw >> 3) * 32, w);
                         l_run[m] += sum;
@@ -710,7 +730,7 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_c
                 if (lane == 0) mbar_arrive(&bars.o_empty[m]);
             }
             if (!whole && threadIdx.x == kFirstSoftmax * 32)
-                p.slots[slot] = make_int4(pc.pb, pc.ph, pc.pi, (pc.t0 == 0 ? kLeads : 0) | (pc.t1 == pc.tiles ? kEnds : 0));
+                p.slots[slot] = make_int4(pc.b, pc.h, pc.i, (pc.t0 == 0 ? kLeads : 0) | (pc.t1 == pc.tiles ? kEnds : 0));
         }
     }
     fence_before();
