@@ -39,7 +39,7 @@ constexpr int kRows = 256;                         // query rows of a block
 constexpr int kHalf = 128;                         // ... of one of its two MMA tiles
 constexpr int kKeys = 128;                         // keys of a tile
 constexpr int kThreads = 640;
-constexpr int kMmaWarp = 0, kKvWarp = 1, kQWarp = 2, kMmaWarp1 = 3, kFirstSoftmax = 4;
+constexpr int kMmaWarp = 0, kKvWarp = 1, kQWarp = 2, kFirstSoftmax = 4;   // (warp 3: products)
 constexpr int kStages = 5;
 constexpr int kTileBytes = kKeys * kD * 2;
 constexpr int kQBytes = kRows * kD * 2;
@@ -54,7 +54,7 @@ struct ChunkParams {
     const int32_t* page_table;
     __nv_bfloat16* out;
     int* status;
-    int4* slots;               // [2 grid]: request, head, block, flags of the pieces of cut blocks
+    int4* slots;               // [2 grid], the pieces of cut blocks: first row of q, KV head, tokens, flags
     float2* part_ml;           // [2 grid, rows] maximum (in powers of two) and sum
     float* part_o;             // [2 grid, rows, 128], divided by the sum
     int b0, nb;                // requests of this launch
@@ -64,7 +64,7 @@ struct ChunkParams {
     int rows;                  // rows of a slot
     float scale_log2;
 };
-constexpr int kLeads = 1, kEnds = 2;               // flags of a piece: it has its block's first tile, last tile
+constexpr int kUsed = 1, kEnds = 2;                // flags of a slot: it holds a piece, which has its block's last tile
 
 // a / b for a >= 0, b > 0
 __device__ __forceinline__ long long quotient(long long a, long long b) { return div_pos(a, b); }
@@ -286,6 +286,12 @@ __device__ __forceinline__ float top_of(const float (&s)[32]) {
     for (int j = 0; j < 4; ++j) a[j] = fmaxf(a[j], s[28 + j]);
     return fmaxf(max3(a[0], a[1], a[2]), a[3]);
 }
+// 1 / x, within an ulp
+__device__ __forceinline__ float rcp(float x) {
+    float y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
 // 32 bytes at once
 __device__ __forceinline__ void store32(void* p, const uint32_t (&r)[8]) {
     asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]),
@@ -345,7 +351,9 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_c
     __shared__ Bars bars;
     __shared__ long long s_part[kThreads / 32];
     __shared__ Begin s_begin;
-    __shared__ float s_top[16][16], s_sum[16][16];   // a warp's rows' maxima and sums, for the warp of the other keys
+    // for the warp of the other keys: a warp's rows' sums of the first half; of the second,
+    // and maxima before
+    __shared__ float s_row[2][16][16];
     __shared__ uint32_t s_tmem;
     __shared__ volatile int s_dead;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -408,7 +416,7 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_c
         if (lane >= d) upto += x;
     }
     if (lane == 31) s_part[warp] = upto;
-    if (threadIdx.x < 2) p.slots[2 * blockIdx.x + threadIdx.x] = make_int4(-1, 0, 0, 0);
+    if (threadIdx.x < 2) p.slots[2 * blockIdx.x + threadIdx.x] = make_int4(0, 0, 0, 0);
     if (blockIdx.x == 0 && threadIdx.x == 0 && p.b0 == 0) *p.status = 0;
     fence_before();
     __syncthreads();
@@ -629,12 +637,37 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_c
                         const int lim = pc.keys - (pc.tokens - 1 - min(token[m], pc.tokens - 1)) - t * kKeys - part * 32;
                         if (__builtin_expect(lim < 32, 0)) hide(s, lim);
                         // The weights by the maximum so far.  A sum within 2^8 says that no score
-                        // passed it by more than 8; otherwise, and where there is none, the
-                        // maximum of the tile is found and the weights are taken again.
+                        // passed it by more than 8; otherwise, and in a piece's first tile, the
+                        // maximum of the tile is found before the weights are taken.
                         uint32_t w[16];
                         float sum;
 #pragma unroll 1
-                        for (bool again = false;; again = true) {
+                        for (bool find = t == pc.t0;; find = true) {
+                            if (find) {
+                                const float mh = top_of(s);
+                                const float mw = fmaxf(mh, __shfl_xor_sync(0xffffffffu, mh, 16));
+                                pair_sync(pair);   // (what was there has been read)
+                                if (lane < 16) s_row[1][sw][lane] = mw;
+                                pair_sync(pair);
+                                const float mt = fmaxf(m_run[m], fmaxf(mw, s_row[1][sw ^ 8][lane & 15]));
+                                pair_sync(pair);
+                                const float alpha = mt > m_run[m] ? ex2((m_run[m] - mt) * c) : 1.f;   // (0 where there was none)
+                                m_run[m] = mt;
+                                neg[m] = mt == kNegInf ? 0.f : -mt * c - kPShift;
+                                l_run[m] *= alpha;
+                                if (t != pc.t0) {
+                                    // P V of the tile before is complete (see above)
+#pragma unroll 1
+                                    for (int q = 0; q < 2; ++q) {
+                                        uint32_t o[16];
+                                        tmem_ld16<32>(t_o + q * 16, o);
+                                        tmem_ld_done(o);
+#pragma unroll
+                                        for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * alpha);
+                                        tmem_st16<32>(t_o + q * 16, o);
+                                    }
+                                }
+                            }
                             const uint64_t c2 = f2_pack(c, c), n2 = f2_pack(neg[m], neg[m]);
                             uint64_t sums[2] = {0ull, 0ull};
 #pragma unroll
@@ -648,31 +681,17 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_c
                             float a0, a1;
                             f2_unpack(f2_add(sums[0], sums[1]), a0, a1);
                             sum = a0 + a1;
-                            if (again || !pair_any(pair, !(sum <= kMostSum) || m_run[m] == kNegInf)) break;
-                            const float mh = top_of(s);
-                            const float mw = fmaxf(mh, __shfl_xor_sync(0xffffffffu, mh, 16));
-                            if (lane < 16) s_top[sw][lane] = mw;
-                            pair_sync(pair);
-                            const float mt = fmaxf(m_run[m], fmaxf(mw, s_top[sw ^ 8][lane & 15]));
-                            const float alpha = mt > m_run[m] ? ex2((m_run[m] - mt) * c) : 1.f;   // (0 where there was none)
-                            m_run[m] = mt;
-                            neg[m] = mt == kNegInf ? 0.f : -mt * c - kPShift;
-                            l_run[m] *= alpha;
-                            if (t != pc.t0) {
-                                // P V of the tile before is complete (see above)
-#pragma unroll 1
-                                for (int q = 0; q < 2; ++q) {
-                                    uint32_t o[16];
-                                    tmem_ld16<32>(t_o + q * 16, o);
-                                    tmem_ld_done(o);
-#pragma unroll
-                                    for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * alpha);
-                                    tmem_st16<32>(t_o + q * 16, o);
-                                }
-                            }
+                            if (find || !pair_any(pair, !(sum <= kMostSum) || m_run[m] == kNegInf)) break;
                         }
                         tmem_st16<16>(t_s + (sw >> 3) * 32, w);
                         l_run[m] += sum;
+                        if (t + 1 == pc.t1) {
+                            // the row's sum in this warp, for the other, which reads it when the
+                            // last products are complete
+                            const float l = l_run[m] + __shfl_xor_sync(0xffffffffu, l_run[m], 16);
+                            if (lane < 16) s_row[m][sw][lane] = l;
+                            l_run[m] = l;
+                        }
                         tmem_st_done();
                     }
                     fence_before();
@@ -690,12 +709,8 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_c
                 ++n_o[m];
                 fence_after();
                 if (any[m]) {
-                    float l = l_run[m];
-                    l += __shfl_xor_sync(0xffffffffu, l, 16);
-                    if (lane < 16) s_sum[sw][lane] = l;
-                    pair_sync(pair);
-                    l += s_sum[sw ^ 8][lane & 15];
-                    const float inv = l > 0.f ? 1.f / l : 0.f;
+                    const float l = l_run[m] + s_row[m][sw ^ 8][lane & 15];
+                    const float inv = l > 0.f ? rcp(l) : 0.f;
                     float o[32];
                     tmem_ld32<32>(t_row + 256 + m * 128 + (sw >> 3) * 64, o);
                     tmem_ld_done(o);
@@ -723,14 +738,13 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_c
                                 p.part_ml[row] = make_float2(m_run[m] == kNegInf ? kNegInf : m_run[m] * c, l);
                         }
                     }
-                    pair_sync(pair);   // (its sums have been read)
                 }
                 fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&bars.o_empty[m]);
             }
             if (!whole && threadIdx.x == kFirstSoftmax * 32)
-                p.slots[slot] = make_int4(pc.b, pc.h, pc.i, (pc.t0 == 0 ? kLeads : 0) | (pc.t1 == pc.tiles ? kEnds : 0));
+                p.slots[slot] = make_int4(pc.start + pc.token0, pc.h, pc.tokens, kUsed | (pc.t1 == pc.tiles ? kEnds : 0));
         }
     }
     fence_before();
@@ -741,59 +755,75 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_c
 }
 
 // ------------------------------------------------------------------ the join
-// CTA (c, y): the block that begins in main CTA c and ends in a later one, rows 32 y
-// and on, a row a warp at a time: the pieces' outputs weighted by their sums.
-constexpr int kJoinThreads = 256;
-constexpr int kJoinRows = 32;
+// CTA (c, y): the block that begins in main CTA c and ends in a later one, rows 16 y
+// and on, a row a warp at a time: the pieces' outputs weighted by their sums.  (Four
+// warps of 32 registers and no shared memory: a CTA finds room beside one of the main
+// kernel, and is there when that leaves.)
+constexpr int kJoinThreads = 128;
+constexpr int kJoinRows = 16;
 
-__global__ void __launch_bounds__(kJoinThreads) chunk_join_kernel(const ChunkParams p, int grid) {
-    __shared__ int s_slot[2];
+__global__ void __launch_bounds__(kJoinThreads, 16) chunk_join_kernel(const ChunkParams p, int grid) {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int cta = blockIdx.x, first = 2 * cta + 1;
     wait_prior_grid();
     allow_dependent_launch();
-    const int first = 2 * blockIdx.x + 1;
+    // the pieces behind are the first ones of the CTAs behind (of those that have one), up
+    // to the one that ends the block
     const int4 head = __ldcg(p.slots + first);
-    if (head.x < 0) return;
-    int start, n, L;
-    p.batch.rows_of(head.x, start, n, L);
-    const int token0 = head.z * p.block_tokens;
-    const int rows = min(n - token0, p.block_tokens) * p.G;
-    if ((int)blockIdx.y * kJoinRows >= rows) return;
-    // its other pieces are the first ones of the CTAs behind (those that have one), up to
-    // the one that ends the block
-    if (threadIdx.x < 32) {
-        int last = -1;
-        for (int c = blockIdx.x + 1; last < 0 && c < grid; c += 32) {
-            const int at = c + (int)threadIdx.x;
-            const bool ends = at < grid && (__ldcg(p.slots + 2 * at).x >= 0) && (__ldcg(p.slots + 2 * at).w & kEnds);
-            const unsigned found = __ballot_sync(0xffffffffu, ends);
-            if (found) last = c + __ffs(found) - 1;
-        }
-        if (threadIdx.x == 0) s_slot[0] = last;
+    int flags = cta + 1 + lane < grid ? __ldcg(&p.slots[2 * (cta + 1 + lane)].w) : 0;
+    const int rows = head.z * p.G;
+    if (!(head.w & kUsed) || (int)blockIdx.y * kJoinRows >= rows) return;
+    int last = cta;            // the CTA with the block's end
+    for (int c = cta + 1; last == cta && c < grid; c += 32) {
+        if (c > cta + 1) flags = c + lane < grid ? __ldcg(&p.slots[2 * (c + lane)].w) : 0;
+        const unsigned ends = __ballot_sync(0xffffffffu, flags & kEnds);
+        if (ends) last = c + __ffs(ends) - 1;
     }
-    __syncthreads();
-    const int last = s_slot[0];
-    if (last < 0) return;   // (a wait gave up; the status says so)
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (last == cta) return;   // (a wait gave up; the status says so)
     for (int r = blockIdx.y * kJoinRows + warp; r < min(rows, ((int)blockIdx.y + 1) * kJoinRows); r += kJoinThreads / 32) {
-        float4 o = __ldcg(reinterpret_cast<const float4*>(p.part_o + ((size_t)first * p.rows + r) * kD) + lane);
-        float2 ml = __ldcg(p.part_ml + (size_t)first * p.rows + r);
-        for (int c = blockIdx.x + 1; c <= last; ++c) {
-            if (__ldcg(p.slots + 2 * c).x < 0) continue;
-            const size_t at = (size_t)(2 * c) * p.rows + r;
-            const float2 x = __ldcg(p.part_ml + at);
-            const float4 y = __ldcg(reinterpret_cast<const float4*>(p.part_o + at * kD) + lane);
-            const float top = fmaxf(ml.x, x.x);
-            if (top == kNegInf) continue;
-            const float a = ml.y * ex2(ml.x - top), b = x.y * ex2(x.x - top), inv = a + b > 0.f ? 1.f / (a + b) : 0.f;
-            const float fa = a * inv, fb = b * inv;
-            o.x = o.x * fa + y.x * fb;
-            o.y = o.y * fa + y.y * fb;
-            o.z = o.z * fa + y.z * fb;
-            o.w = o.w * fa + y.w * fb;
-            ml = make_float2(top, a + b);
+        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+        float top = kNegInf, total = 0.f;
+        // the first piece, then those behind: two at a time
+        for (int c = cta; c <= last; c += 2) {
+            float2 ml[2];
+            float4 x[2];
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                const int at = c + k == cta ? first : 2 * (c + k);
+                const bool there = c + k <= last && (__ldcg(&p.slots[at].w) & kUsed);
+                ml[k] = make_float2(kNegInf, 0.f);
+                x[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+                if (there) {
+                    ml[k] = __ldcg(p.part_ml + (size_t)at * p.rows + r);
+                    x[k] = __ldcg(reinterpret_cast<const float4*>(p.part_o + ((size_t)at * p.rows + r) * kD) + lane);
+                }
+            }
+            const float most = max3(top, ml[0].x, ml[1].x);
+            if (most == kNegInf) continue;
+            // (outputs are divided by their sums already)
+            float f = total * ex2(top - most);
+            float w[2], sum = f;
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                w[k] = ml[k].y * ex2(ml[k].x - most);
+                sum += w[k];
+            }
+            const float inv = sum > 0.f ? rcp(sum) : 0.f;
+            f *= inv;
+            o = make_float4(o.x * f, o.y * f, o.z * f, o.w * f);
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                const float g = w[k] * inv;
+                o.x = fmaf(x[k].x, g, o.x);
+                o.y = fmaf(x[k].y, g, o.y);
+                o.z = fmaf(x[k].z, g, o.z);
+                o.w = fmaf(x[k].w, g, o.w);
+            }
+            top = most;
+            total = sum;
         }
-        const int token = token0 + r / p.G;
-        uint2* dst = reinterpret_cast<uint2*>(p.out + ((size_t)(start + token) * p.Hq + (size_t)head.y * p.G + r % p.G) * kD);
+        uint2* dst = reinterpret_cast<uint2*>(
+            p.out + ((size_t)(head.x + r / p.G) * p.Hq + (size_t)head.y * p.G + r % p.G) * kD);
         dst[lane] = make_uint2(pack_bf16x2(o.x, o.y), pack_bf16x2(o.z, o.w));
     }
 }
