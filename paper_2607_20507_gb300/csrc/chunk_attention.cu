@@ -46,6 +46,7 @@ constexpr int kQBytes = kRows * kD * 2;
 constexpr int kSmem = kQBytes + kStages * kTileBytes;
 constexpr int kSmallQRows = 32;                    // blocks of few rows bring in no more than these
 constexpr int kBeginKeys = 128;                    // what beginning and ending a block costs, in keys
+constexpr int kCutKeys = 3;                        // keys a row, up to which a range ends at a block's end instead
 constexpr int kMaxBatch = 1024;                    // requests of a launch
 constexpr float kMostSum = 0x1p-56f;               // 2^8 times 2^-kPShift
 
@@ -351,6 +352,7 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_c
     __shared__ Bars bars;
     __shared__ long long s_part[kThreads / 32];
     __shared__ Begin s_begin;
+    __shared__ int s_move[2];
     // for the warp of the other keys: a warp's rows' sums of the first half; of the second,
     // and maxima before
     __shared__ float s_row[2][16][16];
@@ -373,6 +375,7 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_c
     if (threadIdx.x == 3 * 32) {
         s_dead = 0;
         s_begin.b = -1;
+        s_move[0] = s_move[1] = 0;
         for (int i = 0; i < kStages; ++i) {
             mbar_init(&bars.kv_full[i], 1);
             mbar_init(&bars.kv_empty[i], 2);
@@ -430,23 +433,33 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_c
     // the first CTAs take one more of what is over
     const long long each = quotient(total, gridDim.x);
     const int over = (int)(total - each * gridDim.x), cta = blockIdx.x;
-    const long long lo = each * cta + min(cta, over), size = each + (cta < over);
+    const long long lo = each * cta + min(cta, over), hi = lo + each + (cta < over);
+    // A cut block's piece is written and read again in fp32 (256 rows: 5 to 10 us at either
+    // end, 10 tiles' time): an end that is near one of its block's moves there, for both
+    // CTAs that it parts.
 #pragma unroll
     for (int e = 0; e < kEach; ++e) {
-        const long long in = lo - at;
-        if (size > 0 && in >= 0 && in < weight[e] * p.Hkv) {
-            Begin& a = own[e];
+#pragma unroll
+        for (int end = 0; end < 2; ++end) {
+            const long long in = (end ? hi : lo) - at;
+            if (in < 0 || in >= weight[e] * p.Hkv) continue;
+            Begin a = own[e];
             a.h = (int)quotient(in, weight[e]);
             const long long x = in - a.h * weight[e];
             const Blocks blocks(a.n, a.L, p.block_tokens);
             a.i = blocks.at(x);
             a.off = (int)(x - blocks.before(a.i));
-            s_begin = a;
+            const int after = (int)(blocks.before(a.i + 1) - x);
+            const int most = kCutKeys * p.G * min(a.n - a.i * p.block_tokens, p.block_tokens);
+            const int move = min(a.off, after) > most ? 0 : a.off <= after ? -a.off : after;
+            a.off += move;
+            s_move[end] = move;
+            if (end == 0) s_begin = a;
         }
         at += weight[e] * p.Hkv;
     }
     __syncthreads();
-    Pieces pc(p, s_begin, size);
+    Pieces pc(p, s_begin, hi + s_move[1] - (lo + s_move[0]));
     const uint32_t ring_at = smem_u32(ring);
 
     if (warp < kFirstSoftmax) {
