@@ -2,10 +2,13 @@
 // values appended to the paged cache in bf16 or in 4 bits (cs_rope_kv_append,
 // cs_packed_rope_kv_append; the formulas are in cachespec.h).
 //
-// A token is one CTA's: eight threads take a head's row of 128 dims, each two 16-byte
-// vectors whose dims pair up with each other (or, of neighbouring pairs and of dims
-// that do not turn, with themselves), so that a thread's cosines and sines are the
-// same in every head and are read once.
+// A warp takes a token's heads, four at a time: eight threads a row of 128 dims, each
+// two 16-byte vectors whose dims pair up with each other (or, of neighbouring pairs and
+// of dims that do not turn, with themselves), so that a thread's cosines and sines are
+// the same in every head, are read once and multiplied by the norm's weights once.
+// Where tokens are few their heads are spread over several warps.  The next heads are
+// on their way in while four are turned, and the first ones while the token's request,
+// length and page are looked up.
 #include "cs_internal.h"
 #include "packed.cuh"
 #include "ragged.cuh"
@@ -15,7 +18,9 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kRowThreads = 8;                      // threads of a head's row
-constexpr int kRowsAtOnce = kThreads / kRowThreads;
+constexpr int kRows = 32 / kRowThreads;             // heads that a warp takes at once
+constexpr int kWarpsPerSm = 24;                     // resident ones
+constexpr float kLarge = 0x1p60f, kSmall = 0x1p-60f;   // between them quotients go without a division
 
 struct RopeParams {
     RaggedBatch batch;
@@ -32,6 +37,7 @@ struct RopeParams {
     float eps;
     int Hq, Hkv, rot, n_positions;
     int ps_log2, max_pages, P;
+    int parts;                 // warps of a token
 };
 
 __device__ __forceinline__ void unpack8(const uint4& w, float (&x)[8]) {
@@ -48,8 +54,8 @@ __device__ __forceinline__ uint4 pack8(const float (&x)[8]) {
 
 // Half a group (eight dims; the neighbouring thread has the other half) of a row of a
 // packed cache, by the rule of cs_packed_kv_append.
-__device__ __forceinline__ void store_half_group(const float (&x0)[8], float head, uint8_t* codes, uint8_t* scales,
-                                                 size_t row, int chunk) {
+__device__ __forceinline__ void store_half_group(const float (&x0)[8], float head, bool put, uint8_t* codes,
+                                                 uint8_t* scales, size_t row, int chunk) {
     float x[8], top = 0.f;
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
@@ -59,26 +65,119 @@ __device__ __forceinline__ void store_half_group(const float (&x0)[8], float hea
     top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
     const uint32_t scale = to_e4m3(fminf(__fdiv_rn(top, __fmul_rn(6.f, head)), 448.f));
     const float unit = __fmul_rn(f16_lo(scales_f16x2(scale)), head);
+    if (top < kLarge && unit > kSmall && unit < kLarge) {
+        // x / unit correctly rounded from the correctly rounded reciprocal: one step from
+        // x * (1 / unit) with the remainder (Markstein, 1990)
+        const float inv = __frcp_rn(unit);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) x[j] = unit > 0.f ? __fdiv_rn(x[j], unit) : 0.f;
+        for (int j = 0; j < 8; ++j) {
+            const float q = __fmul_rn(x[j], inv);
+            x[j] = __fmaf_rn(-__fmaf_rn(q, unit, -x[j]), inv, q);
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[j] = unit > 0.f ? __fdiv_rn(x[j], unit) : 0.f;
+    }
     uint32_t c = 0;
 #pragma unroll
     for (int j = 0; j < 4; ++j) c |= to_e2m1x2(x[2 * j], x[2 * j + 1]) << (8 * j);
-    if (!codes) return;
+    if (!put) return;
     *reinterpret_cast<uint32_t*>(codes + row * kPackCodeBytes + chunk * 4) = c;
     if ((chunk & 1) == 0) scales[row * kPackGroups + chunk / 2] = (uint8_t)scale;
 }
 
+// What a thread does to its sixteen dims x and y: x <- (x xx - y xy), y <- (y yy + x yx),
+// times 1 / rms where there is a norm; pairs as the kernel has them.
+template <bool kNeighbours>
+struct Turn {
+    // halves: x[j] pairs with y[j]; neighbours: x[2j] with x[2j+1], y[2j] with y[2j+1]
+    float xx[8], xy[8], yy[8], yx[8];
+    __device__ __forceinline__ Turn(const float (&cosv)[8], const float (&sinv)[8], const uint4* norm, int c0, int c1) {
+        float u[8], v[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) u[j] = v[j] = 1.f;
+        if (norm) {
+            unpack8(norm[c0], u);
+            unpack8(norm[c1], v);
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            if constexpr (kNeighbours) {
+                // cosv, sinv: of the four pairs of x, then those of y; xx, xy are x's, yy, yx y's
+                const float c = cosv[j / 2], s = sinv[j / 2], d = cosv[4 + j / 2], e = sinv[4 + j / 2];
+                xx[j] = u[j] * c;
+                xy[j] = u[j ^ 1] * (j & 1 ? -s : s);
+                yy[j] = v[j] * d;
+                yx[j] = v[j ^ 1] * (j & 1 ? -e : e);
+            } else {
+                xx[j] = u[j] * cosv[j];
+                xy[j] = v[j] * sinv[j];
+                yy[j] = v[j] * cosv[j];
+                yx[j] = u[j] * sinv[j];
+            }
+        }
+    }
+    __device__ __forceinline__ void operator()(float (&x)[8], float (&y)[8], float inv) const {
+        float a[8], b[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            if constexpr (kNeighbours) {
+                a[j] = x[j] * xx[j] - x[j ^ 1] * xy[j];
+                b[j] = y[j] * yy[j] - y[j ^ 1] * yx[j];
+            } else {
+                a[j] = x[j] * xx[j] - y[j] * xy[j];
+                b[j] = y[j] * yy[j] + x[j] * yx[j];
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            x[j] = a[j] * inv;
+            y[j] = b[j] * inv;
+        }
+    }
+};
+
+// The eight threads' row as 1 / rms (1 where there is no norm)
+__device__ __forceinline__ float inverse_rms(const float (&x)[8], const float (&y)[8], bool norm, float eps) {
+    if (!norm) return 1.f;
+    float sum = 0.f;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) sum += x[j] * x[j] + y[j] * y[j];
+#pragma unroll
+    for (int m = 1; m < kRowThreads; m *= 2) sum += __shfl_xor_sync(0xffffffffu, sum, m);
+    return rsqrtf(sum * (1.f / 128) + eps);
+}
+
 template <bool kPacked, bool kNeighbours>
-__global__ void __launch_bounds__(kThreads) rope_append_kernel(const RopeParams p) {
-    const int t = threadIdx.x & (kRowThreads - 1), lane = threadIdx.x & 31;
-    const int64_t token = blockIdx.x;
+__global__ void __launch_bounds__(kThreads, 3) rope_append_kernel(const RopeParams p) {
+    const int lane = threadIdx.x & 31, t = lane & (kRowThreads - 1);
+    const unsigned task = blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5);
+    const int64_t token = task / p.parts;
+    const int part = (int)(task - (unsigned)token * p.parts);
     // the thread's two vectors of a row, and whether they turn
     const int turning = p.rot / 16;     // threads whose vectors do
     const bool turns = t < turning;
     const int c0 = turns ? t : t + turning, c1 = turns ? t + turning : t + 8;
     wait_prior_grid();
     allow_dependent_launch();
+    if (token >= p.batch.tokens) return;
+
+    // fours of heads: those of q, of k, of v; this warp's are part, part + parts, ..
+    const int fours_q = (p.Hq + kRows - 1) / kRows, fours_k = (p.Hkv + kRows - 1) / kRows;
+    const int fours = fours_q + 2 * fours_k;
+    const int sub = lane / kRowThreads;
+    uint4 w0 = make_uint4(0, 0, 0, 0), w1 = w0;
+    auto fetch = [&](int four) {
+        const bool is_q = four < fours_q, is_v = four >= fours_q + fours_k;
+        const int h = (is_q ? four : is_v ? four - fours_q - fours_k : four - fours_q) * kRows + sub;
+        if (four >= fours || h >= (is_q ? p.Hq : p.Hkv)) return;
+        const __nv_bfloat16* from = is_q ? p.q + token * p.q_stride : is_v ? p.v + token * p.v_stride : p.k + token * p.k_stride;
+        const uint4* src = reinterpret_cast<const uint4*>(from + h * 128);
+        w0 = __ldcg(src + c0);
+        w1 = __ldcg(src + c1);
+    };
+    int four = part;
+    fetch(four);
     const int b = p.batch.request_of((int)token, lane);
     if (b < 0) return;
     int start, n, L;
@@ -88,8 +187,6 @@ __global__ void __launch_bounds__(kThreads) rope_append_kernel(const RopeParams 
     if (at < 0 || at >= p.n_positions) return;
     int page = -1;
     if (key >= 0) page = __ldcg(p.page_table + (size_t)b * p.max_pages + (key >> p.ps_log2));
-    const bool stored = page >= 0 && page < p.P;
-
     // the cosines and sines of pairs 8t .. 8t+7, or (neighbouring dims) of the four of
     // either vector
     float cosv[8], sinv[8];
@@ -107,81 +204,66 @@ __global__ void __launch_bounds__(kThreads) rope_append_kernel(const RopeParams 
         *reinterpret_cast<float4*>(sinv) = *reinterpret_cast<const float4*>(row + i0);
         *reinterpret_cast<float4*>(sinv + 4) = *reinterpret_cast<const float4*>(row + i1);
     }
-    const int rows = p.Hq + 2 * p.Hkv;
-    const int first_row = threadIdx.x / kRowThreads, first_of_warp = first_row & ~3;
-    for (int r0 = 0; r0 + first_of_warp < rows; r0 += kRowsAtOnce) {
-        const int r = r0 + first_row;
-        const bool live = r < rows;
-        const bool is_q = r < p.Hq, is_v = r >= p.Hq + p.Hkv;
-        const int h = is_q ? r : is_v ? r - p.Hq - p.Hkv : r - p.Hq;
-        const __nv_bfloat16* from = is_q ? p.q + token * p.q_stride : is_v ? p.v + token * p.v_stride : p.k + token * p.k_stride;
-        uint4 w0 = make_uint4(0, 0, 0, 0), w1 = w0;
-        if (live) {
-            const uint4* src = reinterpret_cast<const uint4*>(from + h * 128);
-            w0 = __ldcg(src + c0);
-            w1 = __ldcg(src + c1);
-        }
-        float x[8], y[8];
-        unpack8(w0, x);
-        unpack8(w1, y);
-        const uint4* norm = is_v ? nullptr : is_q ? p.q_norm : p.k_norm;
-        float sum = 0.f;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) sum += x[j] * x[j] + y[j] * y[j];
-#pragma unroll
-        for (int m = 1; m < kRowThreads; m *= 2) sum += __shfl_xor_sync(0xffffffffu, sum, m);
-        if (norm) {
-            const float inv = rsqrtf(sum * (1.f / 128) + p.eps);
-            float u[8], v[8];
-            unpack8(norm[c0], u);
-            unpack8(norm[c1], v);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                x[j] *= inv * u[j];
-                y[j] *= inv * v[j];
+    if (four < fours_q) {
+        const Turn<kNeighbours> turn(cosv, sinv, p.q_norm, c0, c1);
+        uint4* const out = reinterpret_cast<uint4*>(p.q_out + token * p.q_out_stride);
+        for (; four < fours_q; four += p.parts) {
+            const uint4 a = w0, c = w1;
+            fetch(four + p.parts);
+            float x[8], y[8];
+            unpack8(a, x);
+            unpack8(c, y);
+            turn(x, y, inverse_rms(x, y, p.q_norm != nullptr, p.eps));
+            const int h = four * kRows + sub;
+            if (h < p.Hq) {
+                out[h * 16 + c0] = pack8(x);
+                out[h * 16 + c1] = pack8(y);
             }
         }
-        if (!is_v && turns) {
-            if constexpr (kNeighbours) {
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const float a = x[2 * j], c = x[2 * j + 1], d = y[2 * j], e = y[2 * j + 1];
-                    x[2 * j] = a * cosv[j] - c * sinv[j];
-                    x[2 * j + 1] = c * cosv[j] + a * sinv[j];
-                    y[2 * j] = d * cosv[4 + j] - e * sinv[4 + j];
-                    y[2 * j + 1] = e * cosv[4 + j] + d * sinv[4 + j];
-                }
-            } else {
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const float a = x[j], c = y[j];
-                    x[j] = a * cosv[j] - c * sinv[j];
-                    y[j] = c * cosv[j] + a * sinv[j];
-                }
+    }
+    if (page < 0 || page >= p.P) return;
+    const size_t slot0 = (((size_t)page * p.Hkv) << p.ps_log2) + (key & ((1 << p.ps_log2) - 1));   // of head 0
+    if (four < fours_q + fours_k) {
+        const Turn<kNeighbours> turn(cosv, sinv, p.k_norm, c0, c1);
+        for (; four < fours_q + fours_k; four += p.parts) {
+            const uint4 a = w0, c = w1;
+            fetch(four + p.parts);
+            float x[8], y[8];
+            unpack8(a, x);
+            unpack8(c, y);
+            turn(x, y, inverse_rms(x, y, p.k_norm != nullptr, p.eps));
+            const int h = (four - fours_q) * kRows + sub;
+            const size_t slot = slot0 + ((size_t)h << p.ps_log2);
+            if constexpr (kPacked) {
+                const bool put = h < p.Hkv;
+                const float head = put && p.k_head ? __ldcg(p.k_head + h) : 1.f;
+                store_half_group(x, head, put, static_cast<uint8_t*>(p.k_rows), p.k_scales, slot, c0);
+                store_half_group(y, head, put, static_cast<uint8_t*>(p.k_rows), p.k_scales, slot, c1);
+            } else if (h < p.Hkv) {
+                uint4* dst = reinterpret_cast<uint4*>(p.k_rows) + slot * 16;
+                dst[c0] = pack8(x);
+                dst[c1] = pack8(y);
             }
         }
-        const size_t slot = ((((size_t)(stored ? page : 0) * p.Hkv + h) << p.ps_log2) + (key & ((1 << p.ps_log2) - 1)));
-        if (live && is_q) {
-            uint4* dst = reinterpret_cast<uint4*>(p.q_out + token * p.q_out_stride + h * 128);
-            dst[c0] = pack8(x);
-            dst[c1] = pack8(y);
-        } else if (!kPacked && live && stored) {
-            // (values as they are, whatever their bits)
-            uint4* dst = reinterpret_cast<uint4*>(is_v ? p.v_rows : p.k_rows) + slot * 16;
-            dst[c0] = is_v ? w0 : pack8(x);
-            dst[c1] = is_v ? w1 : pack8(y);
-        }
+    }
+    for (; four < fours; four += p.parts) {
+        const uint4 a = w0, c = w1;
+        fetch(four + p.parts);
+        const int h = (four - fours_q - fours_k) * kRows + sub;
+        const size_t slot = slot0 + ((size_t)h << p.ps_log2);
         if constexpr (kPacked) {
-            // (a warp has rows of q and of k: neighbours have one row)
-            if (__any_sync(0xffffffffu, live && !is_q)) {
-                const bool put = live && !is_q && stored;
-                const float* heads = is_v ? p.v_head : p.k_head;
-                const float head = put && heads ? __ldcg(heads + h) : 1.f;
-                uint8_t* codes = put ? static_cast<uint8_t*>(is_v ? p.v_rows : p.k_rows) : nullptr;
-                uint8_t* scales = is_v ? p.v_scales : p.k_scales;
-                store_half_group(x, head, codes, scales, slot, c0);
-                store_half_group(y, head, codes, scales, slot, c1);
-            }
+            const bool put = h < p.Hkv;
+            const float head = put && p.v_head ? __ldcg(p.v_head + h) : 1.f;
+            float x[8], y[8];
+            unpack8(a, x);
+            unpack8(c, y);
+            store_half_group(x, head, put, static_cast<uint8_t*>(p.v_rows), p.v_scales, slot, c0);
+            store_half_group(y, head, put, static_cast<uint8_t*>(p.v_rows), p.v_scales, slot, c1);
+        } else if (h < p.Hkv) {
+            // (as they are, whatever their bits)
+            uint4* dst = reinterpret_cast<uint4*>(p.v_rows) + slot * 16;
+            dst[c0] = a;
+            dst[c1] = c;
         }
     }
 }
@@ -211,7 +293,14 @@ cs_status launch(const cs_attn_dims& d, const cs_rope_dims& r, RopeParams& p, bo
     p.P = d.num_pages;
     auto kern = packed ? (r.interleaved ? rope_append_kernel<true, true> : rope_append_kernel<true, false>)
                        : (r.interleaved ? rope_append_kernel<false, true> : rope_append_kernel<false, false>);
-    const cudaError_t e = launch_dependent(kern, dim3((unsigned)r.tokens), dim3(kThreads), 0, stream, p);
+    // as many warps as there is room for, each a token's share of fours
+    const int fours = (p.Hq + kRows - 1) / kRows + 2 * ((p.Hkv + kRows - 1) / kRows);
+    const long long room = (long long)current_sm_count() * kWarpsPerSm;
+    p.parts = (int)((room + r.tokens - 1) / r.tokens);
+    p.parts = p.parts < fours ? p.parts : fours;
+    const long long tasks = (long long)r.tokens * p.parts;
+    const cudaError_t e = launch_dependent(kern, dim3((unsigned)((tasks + kThreads / 32 - 1) / (kThreads / 32))),
+                                           dim3(kThreads), 0, stream, p);
     return e == cudaSuccess ? CS_OK : cuda_fail(e, "rope_append_kernel launch");
 }
 
