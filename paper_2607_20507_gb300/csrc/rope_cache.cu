@@ -92,8 +92,23 @@ template <bool kNeighbours>
 struct Turn {
     // halves: x[j] pairs with y[j]; neighbours: x[2j] with x[2j+1], y[2j] with y[2j+1]
     float xx[8], xy[8], yy[8], yx[8];
-    __device__ __forceinline__ Turn(const float (&cosv)[8], const float (&sinv)[8], const uint4* norm, int c0, int c1) {
-        float u[8], v[8];
+    // row: the position's cosines and sines, or NULL for dims that do not turn
+    __device__ __forceinline__ Turn(const float* row, int rot, const uint4* norm, int c0, int c1) {
+        // the cosines and sines of pairs 8t .. 8t+7, or (neighbouring dims) of the four of
+        // either vector
+        float cosv[8], sinv[8], u[8], v[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            cosv[j] = 1.f;
+            sinv[j] = 0.f;
+        }
+        if (row) {
+            const int i0 = kNeighbours ? 4 * c0 : 8 * c0, i1 = kNeighbours ? 4 * c1 : 8 * c0 + 4;
+            *reinterpret_cast<float4*>(cosv) = *reinterpret_cast<const float4*>(row + i0);
+            *reinterpret_cast<float4*>(cosv + 4) = *reinterpret_cast<const float4*>(row + i1);
+            *reinterpret_cast<float4*>(sinv) = *reinterpret_cast<const float4*>(row + rot / 2 + i0);
+            *reinterpret_cast<float4*>(sinv + 4) = *reinterpret_cast<const float4*>(row + rot / 2 + i1);
+        }
 #pragma unroll
         for (int j = 0; j < 8; ++j) u[j] = v[j] = 1.f;
         if (norm) {
@@ -166,8 +181,9 @@ __global__ void __launch_bounds__(kThreads, 3) rope_append_kernel(const RopePara
     const int fours_q = (p.Hq + kRows - 1) / kRows, fours_k = (p.Hkv + kRows - 1) / kRows;
     const int fours = fours_q + 2 * fours_k;
     const int sub = lane / kRowThreads;
-    uint4 w0 = make_uint4(0, 0, 0, 0), w1 = w0;
-    auto fetch = [&](int four) {
+    // the next four and the one behind it
+    uint4 w0 = make_uint4(0, 0, 0, 0), w1 = w0, n0 = w0, n1 = w0;
+    auto fetch = [&](int four, uint4& w0, uint4& w1) {
         const bool is_q = four < fours_q, is_v = four >= fours_q + fours_k;
         const int h = (is_q ? four : is_v ? four - fours_q - fours_k : four - fours_q) * kRows + sub;
         if (four >= fours || h >= (is_q ? p.Hq : p.Hkv)) return;
@@ -177,7 +193,15 @@ __global__ void __launch_bounds__(kThreads, 3) rope_append_kernel(const RopePara
         w1 = __ldcg(src + c1);
     };
     int four = part;
-    fetch(four);
+    fetch(four, w0, w1);
+    fetch(four + p.parts, n0, n1);
+    auto advance = [&](uint4& a, uint4& c) {
+        a = w0;
+        c = w1;
+        w0 = n0;
+        w1 = n1;
+        fetch(four + 2 * p.parts, n0, n1);
+    };
     const int b = p.batch.request_of((int)token, lane);
     if (b < 0) return;
     int start, n, L;
@@ -187,29 +211,13 @@ __global__ void __launch_bounds__(kThreads, 3) rope_append_kernel(const RopePara
     if (at < 0 || at >= p.n_positions) return;
     int page = -1;
     if (key >= 0) page = __ldcg(p.page_table + (size_t)b * p.max_pages + (key >> p.ps_log2));
-    // the cosines and sines of pairs 8t .. 8t+7, or (neighbouring dims) of the four of
-    // either vector
-    float cosv[8], sinv[8];
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        cosv[j] = 1.f;
-        sinv[j] = 0.f;
-    }
-    if (turns) {
-        const float* row = p.cos_sin + (size_t)at * p.rot;
-        const int i0 = kNeighbours ? 4 * c0 : 8 * t, i1 = kNeighbours ? 4 * c1 : 8 * t + 4;
-        *reinterpret_cast<float4*>(cosv) = *reinterpret_cast<const float4*>(row + i0);
-        *reinterpret_cast<float4*>(cosv + 4) = *reinterpret_cast<const float4*>(row + i1);
-        row += p.rot / 2;
-        *reinterpret_cast<float4*>(sinv) = *reinterpret_cast<const float4*>(row + i0);
-        *reinterpret_cast<float4*>(sinv + 4) = *reinterpret_cast<const float4*>(row + i1);
-    }
+    const float* const row = turns ? p.cos_sin + (size_t)at * p.rot : nullptr;
     if (four < fours_q) {
-        const Turn<kNeighbours> turn(cosv, sinv, p.q_norm, c0, c1);
+        const Turn<kNeighbours> turn(row, p.rot, p.q_norm, c0, c1);
         uint4* const out = reinterpret_cast<uint4*>(p.q_out + token * p.q_out_stride);
         for (; four < fours_q; four += p.parts) {
-            const uint4 a = w0, c = w1;
-            fetch(four + p.parts);
+            uint4 a, c;
+            advance(a, c);
             float x[8], y[8];
             unpack8(a, x);
             unpack8(c, y);
@@ -224,10 +232,10 @@ __global__ void __launch_bounds__(kThreads, 3) rope_append_kernel(const RopePara
     if (page < 0 || page >= p.P) return;
     const size_t slot0 = (((size_t)page * p.Hkv) << p.ps_log2) + (key & ((1 << p.ps_log2) - 1));   // of head 0
     if (four < fours_q + fours_k) {
-        const Turn<kNeighbours> turn(cosv, sinv, p.k_norm, c0, c1);
+        const Turn<kNeighbours> turn(row, p.rot, p.k_norm, c0, c1);
         for (; four < fours_q + fours_k; four += p.parts) {
-            const uint4 a = w0, c = w1;
-            fetch(four + p.parts);
+            uint4 a, c;
+            advance(a, c);
             float x[8], y[8];
             unpack8(a, x);
             unpack8(c, y);
@@ -247,8 +255,8 @@ __global__ void __launch_bounds__(kThreads, 3) rope_append_kernel(const RopePara
         }
     }
     for (; four < fours; four += p.parts) {
-        const uint4 a = w0, c = w1;
-        fetch(four + p.parts);
+        uint4 a, c;
+        advance(a, c);
         const int h = (four - fours_q - fours_k) * kRows + sub;
         const size_t slot = slot0 + ((size_t)h << p.ps_log2);
         if constexpr (kPacked) {
@@ -296,8 +304,8 @@ cs_status launch(const cs_attn_dims& d, const cs_rope_dims& r, RopeParams& p, bo
     // as many warps as there is room for, each a token's share of fours
     const int fours = (p.Hq + kRows - 1) / kRows + 2 * ((p.Hkv + kRows - 1) / kRows);
     const long long room = (long long)current_sm_count() * kWarpsPerSm;
-    p.parts = (int)((room + r.tokens - 1) / r.tokens);
-    p.parts = p.parts < fours ? p.parts : fours;
+    p.parts = (int)(room / r.tokens);
+    p.parts = p.parts < 1 ? 1 : p.parts < fours ? p.parts : fours;
     const long long tasks = (long long)r.tokens * p.parts;
     const cudaError_t e = launch_dependent(kern, dim3((unsigned)((tasks + kThreads / 32 - 1) / (kThreads / 32))),
                                            dim3(kThreads), 0, stream, p);
