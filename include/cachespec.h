@@ -539,7 +539,8 @@ cs_status cs_packed_verify_attention(const cs_attn_dims* dims, const void* q, co
  *              computed and what stands in their place in outputs stays.
  *   strides    rows of q, new_k and new_v may lie apart, as where a projection wrote
  *              queries, keys and values side by side: elements from one token's heads
- *              to the next token's, a multiple of 8; the heads of a token lie together.
+ *              to the next token's, a multiple of 8 up to 2^30; the heads of a token lie
+ *              together.
  *
  * cs_rope_kv_append: cs_kv_append with the position rotation on the way.  For the
  * row of each token, at rotation position t = positions[row], or its key position

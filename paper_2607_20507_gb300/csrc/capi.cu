@@ -208,8 +208,8 @@ cs_status check_ragged_pointers(const cs_attn_dims* d, int32_t tokens, const int
 }
 
 cs_status check_stride(const char* name, int64_t stride, int heads) {
-    if (stride < (int64_t)heads * 128 || stride % 8 != 0 || stride > (1LL << 36))
-        return fail(CS_ERR_INVALID_ARG, "%s %lld is not a multiple of 8 from %lld to 2^36", name, (long long)stride,
+    if (stride < (int64_t)heads * 128 || stride % 8 != 0 || stride > (1LL << 30))
+        return fail(CS_ERR_INVALID_ARG, "%s %lld is not a multiple of 8 from %lld to 2^30", name, (long long)stride,
                     (long long)heads * 128);
     return CS_OK;
 }

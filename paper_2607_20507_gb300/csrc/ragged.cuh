@@ -24,8 +24,9 @@ struct RaggedBatch {
         count = max(0, min(__ldcg(q_starts + b + 1), tokens) - start);
     }
 
-    // The request that token t belongs to (the whole warp asks for one token); -1: none.
-    // 32 places of the array at a time: two loads up to 1024 requests.
+    // The request that token t may belong to (the whole warp asks for one token), the last
+    // one that does not begin behind it; -1: none.  Whether it does, its rows say.  32 places
+    // of the array at a time: two loads up to 1024 requests.
     __device__ __forceinline__ int request_of(int t, int lane) const {
         if (!q_starts) return t / n < B ? t / n : -1;
         int lo = 0, len = B + 1;   // the last b with q_starts[b] <= t lies in [lo, lo + len), if anywhere
@@ -38,7 +39,7 @@ struct RaggedBatch {
             lo += last * step;
             len = min(step, len - last * step);
         }
-        return lo < B && __ldcg(q_starts + lo) <= t && t < __ldcg(q_starts + lo + 1) ? lo : -1;
+        return lo < B ? lo : -1;
     }
 };
 

@@ -16,10 +16,10 @@
 namespace cs {
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 128;
 constexpr int kRowThreads = 8;                      // threads of a head's row
 constexpr int kRows = 32 / kRowThreads;             // heads that a warp takes at once
-constexpr int kWarpsPerSm = 24;                     // resident ones
+constexpr int kWarpsPerSm = 12;                     // that tokens are spread over, where they are few
 constexpr float kLarge = 0x1p60f, kSmall = 0x1p-60f;   // between them quotients go without a division
 
 struct RopeParams {
@@ -33,33 +33,50 @@ struct RopeParams {
     uint8_t *k_scales, *v_scales;
     const float *k_head, *v_head;
     const int32_t* page_table;
-    int64_t q_stride, k_stride, v_stride, q_out_stride;
+    uint32_t q_stride, k_stride, v_stride, q_out_stride;   // (elements)
     float eps;
     int Hq, Hkv, rot, n_positions;
     int ps_log2, max_pages, P;
     int parts;                 // warps of a token
 };
 
-__device__ __forceinline__ void unpack8(const uint4& w, float (&x)[8]) {
+// Eight values as four pairs
+struct Eight {
+    uint64_t v[4];
+};
+__device__ __forceinline__ Eight unpack8(const uint4& w) {
     const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+    Eight x;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) x.v[j] = f2_pack(__uint_as_float(u[j] << 16), __uint_as_float(u[j] & 0xffff0000u));
+    return x;
+}
+__device__ __forceinline__ uint4 pack8(const Eight& x) {
+    uint32_t u[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-        x[2 * j] = __uint_as_float(u[j] << 16);
-        x[2 * j + 1] = __uint_as_float(u[j] & 0xffff0000u);
+        float a, b;
+        f2_unpack(x.v[j], a, b);
+        u[j] = pack_bf16x2(a, b);
     }
+    return make_uint4(u[0], u[1], u[2], u[3]);
 }
-__device__ __forceinline__ uint4 pack8(const float (&x)[8]) {
-    return make_uint4(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7]));
+__device__ __forceinline__ uint64_t swapped(uint64_t v) {
+    float a, b;
+    f2_unpack(v, a, b);
+    return f2_pack(b, a);
 }
 
 // Half a group (eight dims; the neighbouring thread has the other half) of a row of a
 // packed cache, by the rule of cs_packed_kv_append.
-__device__ __forceinline__ void store_half_group(const float (&x0)[8], float head, bool put, uint8_t* codes,
+__device__ __forceinline__ void store_half_group(const Eight& x0, float head, bool put, uint8_t* codes,
                                                  uint8_t* scales, size_t row, int chunk) {
     float x[8], top = 0.f;
 #pragma unroll
+    for (int j = 0; j < 4; ++j) f2_unpack(x0.v[j], x[2 * j], x[2 * j + 1]);
+#pragma unroll
     for (int j = 0; j < 8; ++j) {
-        x[j] = x0[j] != x0[j] ? 0.f : x0[j];
+        if (x[j] != x[j]) x[j] = 0.f;
         top = fmaxf(top, fabsf(x[j]));
     }
     top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
@@ -86,12 +103,12 @@ __device__ __forceinline__ void store_half_group(const float (&x0)[8], float hea
     if ((chunk & 1) == 0) scales[row * kPackGroups + chunk / 2] = (uint8_t)scale;
 }
 
-// What a thread does to its sixteen dims x and y: x <- (x xx - y xy), y <- (y yy + x yx),
-// times 1 / rms where there is a norm; pairs as the kernel has them.
+// What a thread does to its sixteen dims x and y: x <- x xx + y xy, y <- y yy + x yx (or,
+// of neighbouring dims, x <- x xx + x' xy with the pairs of x swapped, and the same of y),
+// times 1 / rms where there is a norm.
 template <bool kNeighbours>
 struct Turn {
-    // halves: x[j] pairs with y[j]; neighbours: x[2j] with x[2j+1], y[2j] with y[2j+1]
-    float xx[8], xy[8], yy[8], yx[8];
+    Eight xx, xy, yy, yx;
     // row: the position's cosines and sines, or NULL for dims that do not turn
     __device__ __forceinline__ Turn(const float* row, int rot, const uint4* norm, int c0, int c1) {
         // the cosines and sines of pairs 8t .. 8t+7, or (neighbouring dims) of the four of
@@ -99,7 +116,7 @@ struct Turn {
         float cosv[8], sinv[8], u[8], v[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            cosv[j] = 1.f;
+            cosv[j] = u[j] = v[j] = 1.f;
             sinv[j] = 0.f;
         }
         if (row) {
@@ -109,73 +126,74 @@ struct Turn {
             *reinterpret_cast<float4*>(sinv) = *reinterpret_cast<const float4*>(row + rot / 2 + i0);
             *reinterpret_cast<float4*>(sinv + 4) = *reinterpret_cast<const float4*>(row + rot / 2 + i1);
         }
-#pragma unroll
-        for (int j = 0; j < 8; ++j) u[j] = v[j] = 1.f;
         if (norm) {
-            unpack8(norm[c0], u);
-            unpack8(norm[c1], v);
+            const Eight a = unpack8(norm[c0]), b = unpack8(norm[c1]);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                f2_unpack(a.v[j], u[2 * j], u[2 * j + 1]);
+                f2_unpack(b.v[j], v[2 * j], v[2 * j + 1]);
+            }
         }
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
+        for (int j = 0; j < 4; ++j) {
+            const int i = 2 * j, k = 2 * j + 1;
             if constexpr (kNeighbours) {
-                // cosv, sinv: of the four pairs of x, then those of y; xx, xy are x's, yy, yx y's
-                const float c = cosv[j / 2], s = sinv[j / 2], d = cosv[4 + j / 2], e = sinv[4 + j / 2];
-                xx[j] = u[j] * c;
-                xy[j] = u[j ^ 1] * (j & 1 ? -s : s);
-                yy[j] = v[j] * d;
-                yx[j] = v[j ^ 1] * (j & 1 ? -e : e);
+                xx.v[j] = f2_pack(u[i] * cosv[j], u[k] * cosv[j]);
+                xy.v[j] = f2_pack(u[k] * -sinv[j], u[i] * sinv[j]);
+                yy.v[j] = f2_pack(v[i] * cosv[4 + j], v[k] * cosv[4 + j]);
+                yx.v[j] = f2_pack(v[k] * -sinv[4 + j], v[i] * sinv[4 + j]);
             } else {
-                xx[j] = u[j] * cosv[j];
-                xy[j] = v[j] * sinv[j];
-                yy[j] = v[j] * cosv[j];
-                yx[j] = u[j] * sinv[j];
+                xx.v[j] = f2_pack(u[i] * cosv[i], u[k] * cosv[k]);
+                xy.v[j] = f2_pack(v[i] * -sinv[i], v[k] * -sinv[k]);
+                yy.v[j] = f2_pack(v[i] * cosv[i], v[k] * cosv[k]);
+                yx.v[j] = f2_pack(u[i] * sinv[i], u[k] * sinv[k]);
             }
         }
     }
-    __device__ __forceinline__ void operator()(float (&x)[8], float (&y)[8], float inv) const {
-        float a[8], b[8];
+    __device__ __forceinline__ void operator()(Eight& x, Eight& y, bool norm, float eps) const {
+        Eight a, b;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            if constexpr (kNeighbours) {
-                a[j] = x[j] * xx[j] - x[j ^ 1] * xy[j];
-                b[j] = y[j] * yy[j] - y[j ^ 1] * yx[j];
-            } else {
-                a[j] = x[j] * xx[j] - y[j] * xy[j];
-                b[j] = y[j] * yy[j] + x[j] * yx[j];
+        for (int j = 0; j < 4; ++j) {
+            const uint64_t xo = kNeighbours ? swapped(x.v[j]) : y.v[j], yo = kNeighbours ? swapped(y.v[j]) : x.v[j];
+            a.v[j] = f2_fma(x.v[j], xx.v[j], f2_mul(xo, xy.v[j]));
+            b.v[j] = f2_fma(y.v[j], yy.v[j], f2_mul(yo, yx.v[j]));
+        }
+        if (norm) {   // (the eight threads of the row)
+            uint64_t sq = f2_mul(x.v[0], x.v[0]);
+#pragma unroll
+            for (int j = 1; j < 4; ++j) sq = f2_fma(x.v[j], x.v[j], sq);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) sq = f2_fma(y.v[j], y.v[j], sq);
+            float s0, s1;
+            f2_unpack(sq, s0, s1);
+            float sum = s0 + s1;
+#pragma unroll
+            for (int m = 1; m < kRowThreads; m *= 2) sum += __shfl_xor_sync(0xffffffffu, sum, m);
+            const float inv = rsqrtf(sum * (1.f / 128) + eps);
+            const uint64_t inv2 = f2_pack(inv, inv);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                a.v[j] = f2_mul(a.v[j], inv2);
+                b.v[j] = f2_mul(b.v[j], inv2);
             }
         }
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            x[j] = a[j] * inv;
-            y[j] = b[j] * inv;
-        }
+        x = a;
+        y = b;
     }
 };
 
-// The eight threads' row as 1 / rms (1 where there is no norm)
-__device__ __forceinline__ float inverse_rms(const float (&x)[8], const float (&y)[8], bool norm, float eps) {
-    if (!norm) return 1.f;
-    float sum = 0.f;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) sum += x[j] * x[j] + y[j] * y[j];
-#pragma unroll
-    for (int m = 1; m < kRowThreads; m *= 2) sum += __shfl_xor_sync(0xffffffffu, sum, m);
-    return rsqrtf(sum * (1.f / 128) + eps);
-}
-
 template <bool kPacked, bool kNeighbours>
-__global__ void __launch_bounds__(kThreads, 3) rope_append_kernel(const RopeParams p) {
+__global__ void __launch_bounds__(kThreads, 5) rope_append_kernel(const RopeParams p) {
     const int lane = threadIdx.x & 31, t = lane & (kRowThreads - 1);
-    const unsigned task = blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5);
-    const int64_t token = task / p.parts;
-    const int part = (int)(task - (unsigned)token * p.parts);
+    const uint32_t token = blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5);
+    const int part = blockIdx.y;
     // the thread's two vectors of a row, and whether they turn
     const int turning = p.rot / 16;     // threads whose vectors do
     const bool turns = t < turning;
     const int c0 = turns ? t : t + turning, c1 = turns ? t + turning : t + 8;
     wait_prior_grid();
     allow_dependent_launch();
-    if (token >= p.batch.tokens) return;
+    if (token >= (uint32_t)p.batch.tokens) return;
 
     // fours of heads: those of q, of k, of v; this warp's are part, part + parts, ..
     const int fours_q = (p.Hq + kRows - 1) / kRows, fours_k = (p.Hkv + kRows - 1) / kRows;
@@ -185,10 +203,11 @@ __global__ void __launch_bounds__(kThreads, 3) rope_append_kernel(const RopePara
     uint4 w0 = make_uint4(0, 0, 0, 0), w1 = w0, n0 = w0, n1 = w0;
     auto fetch = [&](int four, uint4& w0, uint4& w1) {
         const bool is_q = four < fours_q, is_v = four >= fours_q + fours_k;
-        const int h = (is_q ? four : is_v ? four - fours_q - fours_k : four - fours_q) * kRows + sub;
-        if (four >= fours || h >= (is_q ? p.Hq : p.Hkv)) return;
-        const __nv_bfloat16* from = is_q ? p.q + token * p.q_stride : is_v ? p.v + token * p.v_stride : p.k + token * p.k_stride;
-        const uint4* src = reinterpret_cast<const uint4*>(from + h * 128);
+        const int head = (four - (is_q ? 0 : is_v ? fours_q + fours_k : fours_q)) * kRows + sub;
+        if (head >= (is_q ? p.Hq : p.Hkv)) return;
+        const __nv_bfloat16* from = is_q ? p.q : is_v ? p.v : p.k;
+        const uint32_t stride = is_q ? p.q_stride : is_v ? p.v_stride : p.k_stride;
+        const uint4* src = reinterpret_cast<const uint4*>(from + (uint64_t)token * stride + (uint32_t)head * 128u);
         w0 = __ldcg(src + c0);
         w1 = __ldcg(src + c1);
     };
@@ -206,6 +225,7 @@ __global__ void __launch_bounds__(kThreads, 3) rope_append_kernel(const RopePara
     if (b < 0) return;
     int start, n, L;
     p.batch.rows_of(b, start, n, L);
+    if ((unsigned)((int)token - start) >= (unsigned)n) return;
     const int key = L - n + ((int)token - start);
     const int at = p.positions ? __ldcg(p.positions + token) : key;
     if (at < 0 || at >= p.n_positions) return;
@@ -214,14 +234,12 @@ __global__ void __launch_bounds__(kThreads, 3) rope_append_kernel(const RopePara
     const float* const row = turns ? p.cos_sin + (size_t)at * p.rot : nullptr;
     if (four < fours_q) {
         const Turn<kNeighbours> turn(row, p.rot, p.q_norm, c0, c1);
-        uint4* const out = reinterpret_cast<uint4*>(p.q_out + token * p.q_out_stride);
+        uint4* const out = reinterpret_cast<uint4*>(p.q_out + (uint64_t)token * p.q_out_stride);
         for (; four < fours_q; four += p.parts) {
             uint4 a, c;
             advance(a, c);
-            float x[8], y[8];
-            unpack8(a, x);
-            unpack8(c, y);
-            turn(x, y, inverse_rms(x, y, p.q_norm != nullptr, p.eps));
+            Eight x = unpack8(a), y = unpack8(c);
+            turn(x, y, p.q_norm != nullptr, p.eps);
             const int h = four * kRows + sub;
             if (h < p.Hq) {
                 out[h * 16 + c0] = pack8(x);
@@ -236,10 +254,8 @@ __global__ void __launch_bounds__(kThreads, 3) rope_append_kernel(const RopePara
         for (; four < fours_q + fours_k; four += p.parts) {
             uint4 a, c;
             advance(a, c);
-            float x[8], y[8];
-            unpack8(a, x);
-            unpack8(c, y);
-            turn(x, y, inverse_rms(x, y, p.k_norm != nullptr, p.eps));
+            Eight x = unpack8(a), y = unpack8(c);
+            turn(x, y, p.k_norm != nullptr, p.eps);
             const int h = (four - fours_q) * kRows + sub;
             const size_t slot = slot0 + ((size_t)h << p.ps_log2);
             if constexpr (kPacked) {
@@ -262,9 +278,7 @@ __global__ void __launch_bounds__(kThreads, 3) rope_append_kernel(const RopePara
         if constexpr (kPacked) {
             const bool put = h < p.Hkv;
             const float head = put && p.v_head ? __ldcg(p.v_head + h) : 1.f;
-            float x[8], y[8];
-            unpack8(a, x);
-            unpack8(c, y);
+            const Eight x = unpack8(a), y = unpack8(c);
             store_half_group(x, head, put, static_cast<uint8_t*>(p.v_rows), p.v_scales, slot, c0);
             store_half_group(y, head, put, static_cast<uint8_t*>(p.v_rows), p.v_scales, slot, c1);
         } else if (h < p.Hkv) {
@@ -287,10 +301,10 @@ cs_status launch(const cs_attn_dims& d, const cs_rope_dims& r, RopeParams& p, bo
     p.batch = RaggedBatch{ctx_lens, q_starts, d.batch, r.tokens, q_starts ? 0 : r.tokens / d.batch,
                           d.max_pages_per_seq * d.page_size};
     p.page_table = page_table;
-    p.q_stride = r.q_stride;
-    p.k_stride = r.k_stride;
-    p.v_stride = r.v_stride;
-    p.q_out_stride = r.q_out_stride;
+    p.q_stride = (uint32_t)r.q_stride;
+    p.k_stride = (uint32_t)r.k_stride;
+    p.v_stride = (uint32_t)r.v_stride;
+    p.q_out_stride = (uint32_t)r.q_out_stride;
     p.eps = r.norm_eps;
     p.Hq = p.q ? d.n_q_heads : 0;
     p.Hkv = d.n_kv_heads;
@@ -306,9 +320,8 @@ cs_status launch(const cs_attn_dims& d, const cs_rope_dims& r, RopeParams& p, bo
     const long long room = (long long)current_sm_count() * kWarpsPerSm;
     p.parts = (int)(room / r.tokens);
     p.parts = p.parts < 1 ? 1 : p.parts < fours ? p.parts : fours;
-    const long long tasks = (long long)r.tokens * p.parts;
-    const cudaError_t e = launch_dependent(kern, dim3((unsigned)((tasks + kThreads / 32 - 1) / (kThreads / 32))),
-                                           dim3(kThreads), 0, stream, p);
+    const dim3 grid((unsigned)((r.tokens + kThreads / 32 - 1) / (kThreads / 32)), (unsigned)p.parts);
+    const cudaError_t e = launch_dependent(kern, grid, dim3(kThreads), 0, stream, p);
     return e == cudaSuccess ? CS_OK : cuda_fail(e, "rope_append_kernel launch");
 }
 
