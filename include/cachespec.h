@@ -585,9 +585,10 @@ cs_status cs_packed_verify_attention(const cs_attn_dims* dims, const void* q, co
  *   out        bf16 [tokens, Hq, 128], dense, 16-byte aligned (must not alias the inputs)
  *   tokens     >= 0, G = Hq / Hkv at most 128
  *   workspace  at least cs_chunk_attention_workspace_bytes(dims, tokens) bytes,
- *              256-byte aligned, any initial contents; its first 4 bytes are the
- *              device status word, which every call clears first.  Calls that share
- *              one must be ordered.
+ *              256-byte aligned, ZERO-FILLED before its first use; every call that
+ *              completes leaves it ready for the next call, of whatever dims.  Its
+ *              first 4 bytes are the device status word; after a call that set it,
+ *              zero-fill it again.  Calls that share one must be ordered.
  * Slots from L_b on may hold any bits.  Keys and values in front of L_b have to be
  * finite: one that is not may reach every row of its request.
  * Arithmetic: q.K in bf16 with fp32 accumulation, the softmax in fp32, its weights
@@ -754,8 +755,7 @@ cs_status cs_logprobs(const cs_logprob_dims* dims, const void* logits, const int
  * bounded wait inside a kernel gave up, so that call's output is invalid).
  * Copies 4 bytes to the host and SYNCHRONISES `stream`.  The word is sticky
  * until the caller zero-fills the workspace again; in a workspace of
- * cs_packed_verify_attention or cs_chunk_attention it tells of the latest call
- * alone.
+ * cs_packed_verify_attention it tells of the latest call alone.
  */
 #define CS_DEVICE_WAIT_TIMEOUT 1
 cs_status cs_read_device_status(const void* workspace, int32_t* status_out, cs_stream_t stream);

@@ -291,7 +291,7 @@ def attn_dims(q: torch.Tensor, k_pages: torch.Tensor, page_table: torch.Tensor,
 # stream may share it, and calls on two streams may not.  They stay for the
 # process's life (a captured graph holds their addresses).
 _workspaces: dict = {}
-_WITH_STATUS = ("attn", "tree_attn", "route")   # whose first word has to start at zero
+_WITH_STATUS = ("attn", "tree_attn", "route", "chunk_attn")   # whose first word has to start at zero
 
 
 def _made_on(stream: int, device):

@@ -6,8 +6,9 @@
 // keys into tiles of 128.  A block weighs its keys and what it costs to begin and
 // end one; a persistent grid of one CTA an SM takes equal contiguous ranges of the
 // whole weight, whatever the requests' sizes: blocks are cut between tiles where the
-// ranges end, and a second kernel joins the pieces of cut blocks.  The weights have
-// closed forms, so a CTA finds its range from the lengths alone.
+// ranges end, and the CTA that comes to the end of a cut block's pieces last joins them.
+// The weights have closed forms, so a CTA finds its range, and who has the rest of a
+// block, from the lengths alone.
 //
 // A CTA (twenty warps):
 //   warps 4-19      softmax, of query rows 0-127 and then 128-255 of a tile: a warp takes
@@ -45,8 +46,8 @@ constexpr int kTileBytes = kKeys * kD * 2;
 constexpr int kQBytes = kRows * kD * 2;
 constexpr int kSmem = kQBytes + kStages * kTileBytes;
 constexpr int kSmallQRows = 32;                    // blocks of few rows bring in no more than these
-constexpr int kBeginKeys = 128;                    // what beginning and ending a block costs, in keys
-constexpr int kCutKeys = 3;                        // keys a row, up to which a range ends at a block's end instead
+constexpr int kBeginKeys = 208;                    // what beginning and ending a block costs, in keys
+constexpr int kCutKeys = 320, kCutRow = 2;         // a range's end moves by so many keys, and so many a row, to a block's
 constexpr int kMaxBatch = 1024;                    // requests of a launch
 constexpr float kMostSum = 0x1p-56f;               // 2^8 times 2^-kPShift
 
@@ -55,17 +56,24 @@ struct ChunkParams {
     const int32_t* page_table;
     __nv_bfloat16* out;
     int* status;
-    int4* slots;               // [2 grid], the pieces of cut blocks: first row of q, KV head, tokens, flags
-    float2* part_ml;           // [2 grid, rows] maximum (in powers of two) and sum
-    float* part_o;             // [2 grid, rows, 128], divided by the sum
+    // cut blocks, by the CTA that one begins in: how many of its tiles are done (0 between
+    // calls); and of their pieces, by the CTA, the one that it goes on with and the one that
+    // it begins: rows' maxima (in powers of two) and sums, and outputs divided by the sums
+    int* done;                 // [grid]
+    // or, where a second kernel joins them: first row of q, KV head, tokens, flags
+    int4* slots;               // [2 grid]
+    float2* part_ml;           // [2 grid, rows]
+    float* part_o;             // [2 grid, rows, 128]
     int b0, nb;                // requests of this launch
     int Hq, Hkv, G, ps, ps_log2, max_pages, P;
     int block_tokens;          // whole tokens of a block
     int small_tokens;          // ... of the small query box
     int rows;                  // rows of a slot
+    bool join_here;            // the last to come joins a block's pieces
     float scale_log2;
 };
 constexpr int kUsed = 1, kEnds = 2;                // flags of a slot: it holds a piece, which has its block's last tile
+constexpr int kJoinBlocks = 2;                     // at least grid / 2 blocks: they are joined in the kernel
 
 // a / b for a >= 0, b > 0
 __device__ __forceinline__ long long quotient(long long a, long long b) { return div_pos(a, b); }
@@ -106,6 +114,32 @@ __device__ __forceinline__ int tile_at(int x, int keys) {
     return min(tiles, max(0, x - kBeginKeys + kKeys / 2) / kKeys);
 }
 
+// Where a range's end at place x of a block's weight w moves: to an end of the block that
+// is near.  (A cut block's pieces but one are written and read again in fp32; and rows are
+// what that costs.)
+__device__ __forceinline__ int moved(int x, int w, int rows) {
+    return min(x, w - x) > kCutKeys + kCutRow * rows ? x : 2 * x <= w ? 0 : w;
+}
+
+// The ends of the ranges inside one block: its beginning in the whole weight, its weight
+// and rows; equal ranges of `each`, the first `over` of them by one more.
+struct Cuts {
+    long long x0, each;
+    int w, rows, over;
+    // where CTA c's range begins in the block (0, w: in front of it, behind it)
+    __device__ __forceinline__ int begin_of(int c) const {
+        const long long x = each * c + min(c, over) - x0;
+        return x <= 0 ? 0 : x >= w ? w : moved((int)x, w, rows);
+    }
+    // the CTA that the block begins in
+    __device__ __forceinline__ int first() const {
+        const long long more = (each + 1) * over;
+        int c = x0 < more ? (int)quotient(x0, each + 1) : over + (int)quotient(x0 - more, each);
+        while (begin_of(c + 1) == 0) ++c;
+        return c;
+    }
+};
+
 // Where a CTA's range begins.
 struct Begin {
     int b, h, i;               // request of the launch, KV head, block
@@ -123,7 +157,8 @@ struct Pieces {
     // the piece: tiles [t0, t1) of `tiles`, the block's keys and tokens, its request, KV
     // head and place
     int t0, t1, tiles, keys, token0, tokens;
-    int b, h, i, L, start;
+    int b, h, L, start;
+    int off, end;              // its part of the block's weight
 
     __device__ __forceinline__ Pieces(const ChunkParams& p_, const Begin& begin, long long size)
         : p(p_), at(begin), count(0), left(begin.b >= 0 ? size : 0), next_start(0), next_n(0), next_L(0) {
@@ -146,9 +181,10 @@ struct Pieces {
             const bool there = t1 > t0 || (tiles == 0 && at.off == 0);
             b = p.b0 + at.b;
             h = at.h;
-            i = at.i;
             L = at.L;
             start = at.start;
+            off = at.off;
+            end = at.off + take;
             left -= take;
             at.off = 0;
             if (left > 0 && ++at.i == count) {
@@ -320,6 +356,8 @@ __device__ __forceinline__ bool pair_any(int id, bool x) {
         : "memory");
     return r != 0;
 }
+// All softmax warps.
+__device__ __forceinline__ void all_sync() { asm volatile("barrier.cta.sync 9, 512;" ::: "memory"); }
 __device__ __forceinline__ void pair_sync(int id) { asm volatile("barrier.cta.sync %0, 64;" ::"r"(id) : "memory"); }
 
 struct Bars {
@@ -352,7 +390,8 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_c
     __shared__ Bars bars;
     __shared__ long long s_part[kThreads / 32];
     __shared__ Begin s_begin;
-    __shared__ int s_move[2];
+    __shared__ int s_move[2], s_over, s_join;
+    __shared__ long long s_each, s_lo;
     // for the warp of the other keys: a warp's rows' sums of the first half; of the second,
     // and maxima before
     __shared__ float s_row[2][16][16];
@@ -419,8 +458,7 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_c
         if (lane >= d) upto += x;
     }
     if (lane == 31) s_part[warp] = upto;
-    if (threadIdx.x < 2) p.slots[2 * blockIdx.x + threadIdx.x] = make_int4(0, 0, 0, 0);
-    if (blockIdx.x == 0 && threadIdx.x == 0 && p.b0 == 0) *p.status = 0;
+    if (threadIdx.x < 2 && !p.join_here) p.slots[2 * blockIdx.x + threadIdx.x] = make_int4(0, 0, 0, 0);
     fence_before();
     __syncthreads();
     fence_after();
@@ -434,9 +472,13 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_c
     const long long each = quotient(total, gridDim.x);
     const int over = (int)(total - each * gridDim.x), cta = blockIdx.x;
     const long long lo = each * cta + min(cta, over), hi = lo + each + (cta < over);
-    // A cut block's piece is written and read again in fp32 (256 rows: 5 to 10 us at either
-    // end, 10 tiles' time): an end that is near one of its block's moves there, for both
-    // CTAs that it parts.
+    if (threadIdx.x == 0) {
+        s_each = each;
+        s_over = over;
+        s_lo = lo;
+    }
+    // An end that is near one of its block's moves there (moved()), for both CTAs that it
+    // parts.
 #pragma unroll
     for (int e = 0; e < kEach; ++e) {
 #pragma unroll
@@ -450,10 +492,9 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_c
             a.i = blocks.at(x);
             a.off = (int)(x - blocks.before(a.i));
             const int after = (int)(blocks.before(a.i + 1) - x);
-            const int most = kCutKeys * p.G * min(a.n - a.i * p.block_tokens, p.block_tokens);
-            const int move = min(a.off, after) > most ? 0 : a.off <= after ? -a.off : after;
-            a.off += move;
-            s_move[end] = move;
+            const int to = moved(a.off, a.off + after, p.G * min(a.n - a.i * p.block_tokens, p.block_tokens));
+            s_move[end] = to - a.off;
+            a.off = to;
             if (end == 0) s_begin = a;
         }
         at += weight[e] * p.Hkv;
@@ -651,13 +692,14 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_c
                         if (__builtin_expect(lim < 32, 0)) hide(s, lim);
                         // The weights by the maximum so far.  A sum within 2^8 says that no score
                         // passed it by more than 8; otherwise, and in a piece's first tile, the
-                        // maximum of the tile is found before the weights are taken.
+                        // row's maximum of the tile is found before the weights are taken.
                         uint32_t w[16];
                         float sum;
+                        bool need = true;   // (of this thread's row: the others' maxima stay)
 #pragma unroll 1
                         for (bool find = t == pc.t0;; find = true) {
                             if (find) {
-                                const float mh = top_of(s);
+                                const float mh = need ? top_of(s) : kNegInf;
                                 const float mw = fmaxf(mh, __shfl_xor_sync(0xffffffffu, mh, 16));
                                 pair_sync(pair);   // (what was there has been read)
                                 if (lane < 16) s_row[1][sw][lane] = mw;
@@ -694,7 +736,8 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_c
                             float a0, a1;
                             f2_unpack(f2_add(sums[0], sums[1]), a0, a1);
                             sum = a0 + a1;
-                            if (find || !pair_any(pair, !(sum <= kMostSum) || m_run[m] == kNegInf)) break;
+                            need = !(sum <= kMostSum) || m_run[m] == kNegInf;
+                            if (find || !pair_any(pair, need)) break;
                         }
                         tmem_st16<16>(t_s + (sw >> 3) * 32, w);
                         l_run[m] += sum;
@@ -713,22 +756,19 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_c
                 }
             }
             // ---- the piece's end
-            const bool whole = pc.t0 == 0 && pc.t1 == pc.tiles;
-            const size_t slot = 2 * (size_t)blockIdx.x + (pc.t0 == 0);
+            if (pc.t0 == 0 && pc.t1 == pc.tiles) {
 #pragma unroll
-            for (int m = 0; m < 2; ++m) {
-                if (m == halves) break;
-                wait(&bars.o_full[m], n_o[m] & 1, &s_dead, p.status);
-                ++n_o[m];
-                fence_after();
-                if (any[m]) {
-                    const float l = l_run[m] + s_row[m][sw ^ 8][lane & 15];
-                    const float inv = l > 0.f ? rcp(l) : 0.f;
-                    float o[32];
-                    tmem_ld32<32>(t_row + 256 + m * 128 + (sw >> 3) * 64, o);
-                    tmem_ld_done(o);
-                    if (token[m] < pc.tokens) {
-                        if (whole) {
+                for (int m = 0; m < 2; ++m) {
+                    if (m == halves) break;
+                    wait(&bars.o_full[m], n_o[m]++ & 1, &s_dead, p.status);
+                    fence_after();
+                    if (any[m]) {
+                        const float l = l_run[m] + s_row[m][sw ^ 8][lane & 15];
+                        const float inv = l > 0.f ? rcp(l) : 0.f;
+                        float o[32];
+                        tmem_ld32<32>(t_row + 256 + m * 128 + (sw >> 3) * 64, o);
+                        tmem_ld_done(o);
+                        if (token[m] < pc.tokens) {
                             __nv_bfloat16* dst = p.out + out_at + ((size_t)token[m] * p.Hq + head[m]) * kD;
 #pragma unroll
                             for (int j = 0; j < 2; ++j) {
@@ -738,26 +778,126 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_c
                                     r[e] = pack_bf16x2(o[16 * j + 2 * e] * inv, o[16 * j + 2 * e + 1] * inv);
                                 store32(dst + j * 16, r);
                             }
-                        } else {
-                            const size_t row = slot * p.rows + m * kHalf + lane0 + (lane & 15);
+                        }
+                    }
+                    fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&bars.o_empty[m]);
+                }
+                continue;
+            }
+            // A cut block's piece is left in fp32, but for the one that comes last: it joins
+            // them, its own still in tensor memory, in the order of their tiles (so the result
+            // does not go by who came last).
+            const bool begins = pc.off == 0;   // (then it is the last piece of the CTA's range, else the first)
+            const int mine = 2 * blockIdx.x + begins;
+            const long long x0 = begins ? s_lo + s_each + ((int)blockIdx.x < s_over) + s_move[1] - pc.end : s_lo + s_move[0] - pc.off;
+            const Cuts cuts{x0, s_each, pc.keys + kBeginKeys, pc.tokens * p.G, s_over};
+            const int first_cta = begins ? (int)blockIdx.x : cuts.first();
+            bool join = false;
+            if (p.join_here) {
+                if (threadIdx.x == kFirstSoftmax * 32) {
+                    s_join = __ldcg(p.done + first_cta) + pc.t1 - pc.t0 == pc.tiles;
+                    __threadfence();
+                }
+                all_sync();
+                join = s_join;
+            } else if (threadIdx.x == kFirstSoftmax * 32) {
+                p.slots[mine] = make_int4(pc.start + pc.token0, pc.h, pc.tokens, kUsed | (pc.t1 == pc.tiles ? kEnds : 0));
+            }
+#pragma unroll 1
+            for (int again = 0;; ++again) {
+#pragma unroll 1
+                for (int m = 0; m < halves; ++m) {
+                    if (again == 0) wait(&bars.o_full[m], (m ? n_o[1] : n_o[0]) & 1, &s_dead, p.status);
+                    fence_after();
+                    if (!(m ? any[1] : any[0])) continue;
+                    const float l = (m ? l_run[1] : l_run[0]) + s_row[m][sw ^ 8][lane & 15];
+                    const float top = m ? m_run[1] : m_run[0];
+                    const float inv = l > 0.f ? rcp(l) : 0.f;
+                    const int row = m * kHalf + lane0 + (lane & 15), token_ = m ? token[1] : token[0];
+                    const float2 ml = make_float2(top == kNegInf ? kNegInf : top * c, l);
+#pragma unroll 1
+                    for (int q = 0; q < 2; ++q) {   // 16 dims
+                        uint32_t w[16];
+                        tmem_ld16<32>(t_row + 256 + m * 128 + (sw >> 3) * 64 + q * 16, w);
+                        tmem_ld_done(w);
+                        if (token_ >= pc.tokens) continue;
+                        float o[16];
 #pragma unroll
-                            for (int j = 0; j < 4; ++j) {
-                                uint32_t r[8];
+                        for (int e = 0; e < 16; ++e) o[e] = __uint_as_float(w[e]) * inv;
+                        if (join) {
+                            float sum[16];
+                            float2 all = make_float2(kNegInf, 0.f);
 #pragma unroll
-                                for (int e = 0; e < 8; ++e) r[e] = __float_as_uint(o[8 * j + e] * inv);
-                                store32(p.part_o + row * kD + part * 32 + j * 8, r);
+                            for (int e = 0; e < 16; ++e) sum[e] = 0.f;
+                            int x = 0;
+#pragma unroll 1
+                            for (int cta = first_cta; x < cuts.w; ++cta) {
+                                const int y = cuts.begin_of(cta + 1);
+                                const bool there = tile_at(x, pc.keys) < tile_at(y, pc.keys);
+                                x = y;
+                                if (!there) continue;
+                                const int slot = 2 * cta + (cta == first_cta);
+                                const size_t at_row = (size_t)slot * p.rows + row;
+                                const float* from = p.part_o + at_row * kD + part * 32 + q * 16;
+                                const float2 z = slot == mine ? ml : __ldcg(p.part_ml + at_row);
+                                float4 v[4];
+#pragma unroll
+                                for (int j = 0; j < 4; ++j) {
+                                    v[j] = make_float4(o[4 * j], o[4 * j + 1], o[4 * j + 2], o[4 * j + 3]);
+                                    if (slot != mine) v[j] = __ldcg(reinterpret_cast<const float4*>(from) + j);
+                                }
+                                const float most = fmaxf(all.x, z.x);
+                                const float f = most == kNegInf ? 0.f : ex2(all.x - most);
+                                const float g = most == kNegInf ? 0.f : ex2(z.x - most) * z.y;
+                                all = make_float2(most, all.y * f + g);
+#pragma unroll
+                                for (int j = 0; j < 4; ++j) {
+                                    sum[4 * j] = fmaf(v[j].x, g, sum[4 * j] * f);
+                                    sum[4 * j + 1] = fmaf(v[j].y, g, sum[4 * j + 1] * f);
+                                    sum[4 * j + 2] = fmaf(v[j].z, g, sum[4 * j + 2] * f);
+                                    sum[4 * j + 3] = fmaf(v[j].w, g, sum[4 * j + 3] * f);
+                                }
                             }
-                            if (part == 0)
-                                p.part_ml[row] = make_float2(m_run[m] == kNegInf ? kNegInf : m_run[m] * c, l);
+                            const float r = all.y > 0.f ? rcp(all.y) : 0.f;
+#pragma unroll
+                            for (int e = 0; e < 16; ++e) o[e] = sum[e] * r;
+                        }
+                        uint32_t r[8];
+                        if (join) {
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) r[e] = pack_bf16x2(o[2 * e], o[2 * e + 1]);
+                            store32(p.out + out_at + ((size_t)token_ * (p.Hq - p.G) + row) * kD + q * 16, r);
+                        } else {
+                            const size_t at_row = (size_t)mine * p.rows + row;
+#pragma unroll
+                            for (int j = 0; j < 2; ++j) {
+#pragma unroll
+                                for (int e = 0; e < 8; ++e) r[e] = __float_as_uint(o[8 * j + e]);
+                                store32(p.part_o + at_row * kD + part * 32 + q * 16 + j * 8, r);
+                            }
+                            if (part == 0 && q == 0) p.part_ml[at_row] = ml;
                         }
                     }
                 }
-                fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(&bars.o_empty[m]);
+                if (join || again || !p.join_here) break;
+                __threadfence();
+                all_sync();
+                if (threadIdx.x == kFirstSoftmax * 32) {
+                    s_join = atomicAdd(p.done + first_cta, pc.t1 - pc.t0) + pc.t1 - pc.t0 == pc.tiles;
+                    __threadfence();
+                }
+                all_sync();
+                join = s_join;
+                if (!join) break;
             }
-            if (!whole && threadIdx.x == kFirstSoftmax * 32)
-                p.slots[slot] = make_int4(pc.start + pc.token0, pc.h, pc.tokens, kUsed | (pc.t1 == pc.tiles ? kEnds : 0));
+            if (join && threadIdx.x == kFirstSoftmax * 32) p.done[first_cta] = 0;
+            fence_before();
+            __syncwarp();
+            ++n_o[0];
+            if (halves == 2) ++n_o[1];
+            if (lane < halves) mbar_arrive(&bars.o_empty[lane]);
         }
     }
     fence_before();
@@ -768,69 +908,77 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_c
 }
 
 // ------------------------------------------------------------------ the join
-// CTA (c, y): the block that begins in main CTA c and ends in a later one, rows 16 y
-// and on, a row a warp at a time: the pieces' outputs weighted by their sums.  (Four
-// warps of 32 registers and no shared memory: a CTA finds room beside one of the main
-// kernel, and is there when that leaves.)
+// Where blocks are few and have many pieces, CTA (c, y) joins those of the block that
+// begins in main CTA c and ends in a later one, rows 16 y and on, a row a warp at a time:
+// a lane a piece for the weights, then the outputs weighted by them, four on their way
+// at once.  (Four warps of 32 registers and no shared memory: a CTA finds room beside one
+// of the main kernel, and is there when that leaves.)
 constexpr int kJoinThreads = 128;
 constexpr int kJoinRows = 16;
 
 __global__ void __launch_bounds__(kJoinThreads, 16) chunk_join_kernel(const ChunkParams p, int grid) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int cta = blockIdx.x, first = 2 * cta + 1;
+    const int cta = blockIdx.x;
     wait_prior_grid();
     allow_dependent_launch();
-    // the pieces behind are the first ones of the CTAs behind (of those that have one), up
-    // to the one that ends the block
-    const int4 head = __ldcg(p.slots + first);
-    int flags = cta + 1 + lane < grid ? __ldcg(&p.slots[2 * (cta + 1 + lane)].w) : 0;
+    // the pieces behind the first are the first ones of the CTAs behind (of those that have
+    // one), up to the one that ends the block
+    auto flags_of = [&](int c) { return c < grid ? __ldcg(&p.slots[2 * c + (c == cta)].w) : 0; };
+    const int4 head = __ldcg(p.slots + 2 * cta + 1);
+    const int flags = flags_of(cta + lane);
     const int rows = head.z * p.G;
     if (!(head.w & kUsed) || (int)blockIdx.y * kJoinRows >= rows) return;
     int last = cta;            // the CTA with the block's end
-    for (int c = cta + 1; last == cta && c < grid; c += 32) {
-        if (c > cta + 1) flags = c + lane < grid ? __ldcg(&p.slots[2 * (c + lane)].w) : 0;
-        const unsigned ends = __ballot_sync(0xffffffffu, flags & kEnds);
+    for (int c = cta; last == cta && c < grid; c += 32) {
+        const unsigned ends = __ballot_sync(0xffffffffu, (c == cta ? flags : flags_of(c + lane)) & kEnds);
         if (ends) last = c + __ffs(ends) - 1;
     }
     if (last == cta) return;   // (a wait gave up; the status says so)
     for (int r = blockIdx.y * kJoinRows + warp; r < min(rows, ((int)blockIdx.y + 1) * kJoinRows); r += kJoinThreads / 32) {
         float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
         float top = kNegInf, total = 0.f;
-        // the first piece, then those behind: two at a time
-        for (int c = cta; c <= last; c += 2) {
-            float2 ml[2];
-            float4 x[2];
+        for (int c = cta; c <= last; c += 32) {
+            const int used = c + lane <= last ? (c == cta ? flags : flags_of(c + lane)) & kUsed : 0;
+            const float2 ml = used ? __ldcg(p.part_ml + (size_t)(2 * (c + lane) + (c + lane == cta)) * p.rows + r)
+                                   : make_float2(kNegInf, 0.f);
+            float most = ml.x;
 #pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                const int at = c + k == cta ? first : 2 * (c + k);
-                const bool there = c + k <= last && (__ldcg(&p.slots[at].w) & kUsed);
-                ml[k] = make_float2(kNegInf, 0.f);
-                x[k] = make_float4(0.f, 0.f, 0.f, 0.f);
-                if (there) {
-                    ml[k] = __ldcg(p.part_ml + (size_t)at * p.rows + r);
-                    x[k] = __ldcg(reinterpret_cast<const float4*>(p.part_o + ((size_t)at * p.rows + r) * kD) + lane);
-                }
-            }
-            const float most = max3(top, ml[0].x, ml[1].x);
+            for (int d = 16; d > 0; d /= 2) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, d));
+            most = fmaxf(most, top);
             if (most == kNegInf) continue;
             // (outputs are divided by their sums already)
-            float f = total * ex2(top - most);
-            float w[2], sum = f;
+            float w = ml.y * ex2(ml.x - most), sum = w;
 #pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                w[k] = ml[k].y * ex2(ml[k].x - most);
-                sum += w[k];
-            }
+            for (int d = 16; d > 0; d /= 2) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+            float f = total * ex2(top - most);
+            sum += f;
             const float inv = sum > 0.f ? rcp(sum) : 0.f;
             f *= inv;
+            w *= inv;
             o = make_float4(o.x * f, o.y * f, o.z * f, o.w * f);
+            unsigned left = __ballot_sync(0xffffffffu, used);
+            while (left) {
+                float4 x[4];
+                float g[4];
 #pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                const float g = w[k] * inv;
-                o.x = fmaf(x[k].x, g, o.x);
-                o.y = fmaf(x[k].y, g, o.y);
-                o.z = fmaf(x[k].z, g, o.z);
-                o.w = fmaf(x[k].w, g, o.w);
+                for (int k = 0; k < 4; ++k) {
+                    const int at = left ? __ffs(left) - 1 : 0;
+                    g[k] = __shfl_sync(0xffffffffu, w, at);
+                    x[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+                    if (left)
+                        x[k] = __ldcg(reinterpret_cast<const float4*>(
+                                          p.part_o + ((size_t)(2 * (c + at) + (c + at == cta)) * p.rows + r) * kD) + lane);
+                    else
+                        g[k] = 0.f;
+                    left &= left - 1;
+                }
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    o.x = fmaf(x[k].x, g[k], o.x);
+                    o.y = fmaf(x[k].y, g[k], o.y);
+                    o.z = fmaf(x[k].z, g[k], o.z);
+                    o.w = fmaf(x[k].w, g[k], o.w);
+                }
             }
             top = most;
             total = sum;
@@ -884,14 +1032,15 @@ cs_status encode_rows(CUtensorMap* map, const void* q, const cs_attn_dims& d, in
 
 struct Layout {
     int rows;
-    size_t slots, ml, o, bytes;
+    size_t done, slots, ml, o, bytes;
 };
 size_t align_up(size_t x) { return (x + 255) / 256 * 256; }
 Layout layout(const cs_attn_dims& d, int tokens, int grid) {
     Layout l;
     const long long all = (long long)tokens * (d.n_q_heads / d.n_kv_heads);
     l.rows = all < kRows ? (int)all : kRows;
-    l.slots = 256;
+    l.done = 256;
+    l.slots = align_up(l.done + sizeof(int) * grid);
     l.ml = align_up(l.slots + sizeof(int4) * 2 * grid);
     l.o = align_up(l.ml + sizeof(float2) * 2 * grid * l.rows);
     l.bytes = align_up(l.o + sizeof(float) * kD * 2 * grid * l.rows);
@@ -917,6 +1066,7 @@ cs_status launch_chunk_attention(const cs_attn_dims& d, const void* q, int64_t q
     p.page_table = page_table;
     p.out = static_cast<__nv_bfloat16*>(out);
     p.status = reinterpret_cast<int*>(ws);
+    p.done = reinterpret_cast<int*>(ws + l.done);
     p.slots = reinterpret_cast<int4*>(ws + l.slots);
     p.part_ml = reinterpret_cast<float2*>(ws + l.ml);
     p.part_o = reinterpret_cast<float*>(ws + l.o);
@@ -949,11 +1099,16 @@ cs_status launch_chunk_attention(const cs_attn_dims& d, const void* q, int64_t q
             if (dev >= 0 && dev < 64) done[dev] = true;
         }
     }
+    // As many blocks as there may be (the lengths are the device's): with few of them each
+    // has many pieces, and joining them is work for the whole card.
+    const long long by_tokens = (tokens + p.block_tokens - 1) / p.block_tokens;
+    p.join_here = kJoinBlocks * p.Hkv * (by_tokens > d.batch ? by_tokens : d.batch < tokens ? d.batch : tokens) >= grid;
     for (p.b0 = 0; p.b0 < d.batch; p.b0 += kMaxBatch) {
         p.nb = d.batch - p.b0 < kMaxBatch ? d.batch - p.b0 : kMaxBatch;
         cudaError_t e = launch_dependent(chunk_attention_kernel, dim3(grid), dim3(kThreads), (size_t)kSmem, stream, mk, mv,
                                          mq, ms, p);
         if (e != cudaSuccess) return cuda_fail(e, "chunk_attention_kernel launch");
+        if (p.join_here) continue;
         e = launch_dependent(chunk_join_kernel, dim3(grid, (l.rows + kJoinRows - 1) / kJoinRows), dim3(kJoinThreads), 0, stream,
                              p, grid);
         if (e != cudaSuccess) return cuda_fail(e, "chunk_join_kernel launch");

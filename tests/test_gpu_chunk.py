@@ -174,14 +174,19 @@ def test_twice_is_the_same_and_the_status_is_clean():
     assert binding.cs_read_device_status(binding.chunk_attention_workspace(dims, args[0].shape[0], DEV)) == 0
 
 
-def test_a_workspace_of_any_contents():
+def test_a_workspace_of_its_own_is_left_ready():
+    """Zero-filled once; calls of other shapes in between find it as they need it."""
     args = batch([300, 1, 77, 1], [500, 5000, 0, 31], 16, 2, 16)
-    first = binding.cs_chunk_attention(*args)
-    dims = binding.chunk_attn_dims(args[0], args[1], args[3])
-    n = binding.load_library().cs_chunk_attention_workspace_bytes(dims, args[0].shape[0])
-    ws = torch.full((n,), 0xFF, dtype=torch.uint8, device=DEV)
-    for _ in range(2):
+    other = batch([1] * 40 + [500], [3000] * 41, 8, 1, 32, junk=False)
+    first, second = binding.cs_chunk_attention(*args), binding.cs_chunk_attention(*other)
+    sizes = []
+    for a in (args, other):
+        dims = binding.chunk_attn_dims(a[0], a[1], a[3])
+        sizes.append(binding.load_library().cs_chunk_attention_workspace_bytes(dims, a[0].shape[0]))
+    ws = torch.zeros((max(sizes),), dtype=torch.uint8, device=DEV)
+    for _ in range(3):
         assert torch.equal(binding.cs_chunk_attention(*args, workspace=ws), first)
+        assert torch.equal(binding.cs_chunk_attention(*other, workspace=ws), second)
     assert binding.cs_read_device_status(ws) == 0
 
 
