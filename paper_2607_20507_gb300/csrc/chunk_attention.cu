@@ -47,7 +47,7 @@ constexpr int kQBytes = kRows * kD * 2;
 constexpr int kSmem = kQBytes + kStages * kTileBytes;
 constexpr int kSmallQRows = 32;                    // blocks of few rows bring in no more than these
 constexpr int kBeginKeys = 208;                    // what beginning and ending a block costs, in keys
-constexpr int kCutKeys = 320, kCutRow = 2;         // a range's end moves by so many keys, and so many a row, to a block's
+constexpr int kCutKeys = 384, kCutRow = 2;         // a range's end moves by so many keys, and so many a row, to a block's
 constexpr int kMaxBatch = 1024;                    // requests of a launch
 constexpr float kMostSum = 0x1p-56f;               // 2^8 times 2^-kPShift
 
@@ -75,27 +75,30 @@ struct ChunkParams {
 constexpr int kUsed = 1, kEnds = 2;                // flags of a slot: it holds a piece, which has its block's last tile
 constexpr int kJoinBlocks = 2;                     // at least grid / 2 blocks: they are joined in the kernel
 
-// a / b for a >= 0, b > 0
-__device__ __forceinline__ long long quotient(long long a, long long b) { return div_pos(a, b); }
+// Weights are W: 32 bits where the whole of a call's is sure to fit (the schedule is
+// then half as long), else 64.
+__device__ __forceinline__ uint32_t quotient(uint32_t a, uint32_t b) { return a / b; }
+__device__ __forceinline__ uint64_t quotient(uint64_t a, uint64_t b) { return (uint64_t)div_pos((long long)a, (long long)b); }
 
 // A request's blocks: block i has tokens [i T, min(n, (i+1) T)) and the keys in front
 // of and at the last of them; it weighs its keys + kBeginKeys.
+template <typename W>
 struct Blocks {
     int n, L, T, count;
     __device__ __forceinline__ Blocks(int n_, int L_, int T_) : n(n_), L(L_), T(T_), count((n_ + T_ - 1) / T_) {}
     // the weight of blocks 0 .. i-1
-    __device__ __forceinline__ long long before(int i) const {
-        const long long first = (long long)L - n;   // keys in front of the new tokens
+    __device__ __forceinline__ W before(int i) const {
+        const int first = L - n;   // keys in front of the new tokens
         const int full = min(i, count - 1);
         // blocks without a key (more new tokens than keys): all in front
-        const int none = first < 0 ? min(full, (int)(n - L) / T) : 0;
-        const long long a = none, b = full;
-        long long w = (b - a) * first + T * ((b * (b + 1) - a * (a + 1)) / 2) + (long long)full * kBeginKeys;
+        const int none = first < 0 ? min(full, -first / T) : 0;
+        const W a = none, b = full;
+        W w = (b - a) * (W)(long long)first + T * ((b * (b + 1) - a * (a + 1)) / 2) + b * kBeginKeys;
         if (i == count) w += L + kBeginKeys;
         return w;
     }
     // the block that place x of the whole weight lies in
-    __device__ __forceinline__ int at(long long x) const {
+    __device__ __forceinline__ int at(W x) const {
         // i (a + T / 2) + i^2 T / 2 = x, nearly; then exactly
         const float a = (float)(L - n) + kBeginKeys + 0.5f * (float)T, y = (float)x;
         int i = L < n ? 0 : (int)(2.f * y / (a + sqrtf(a * a + 2.f * (float)T * y)));
@@ -123,17 +126,19 @@ __device__ __forceinline__ int moved(int x, int w, int rows) {
 
 // The ends of the ranges inside one block: its beginning in the whole weight, its weight
 // and rows; equal ranges of `each`, the first `over` of them by one more.
+template <typename W>
 struct Cuts {
-    long long x0, each;
-    int w, rows, over;
+    W x0, each;
+    int w, rows;
+    int over;
     // where CTA c's range begins in the block (0, w: in front of it, behind it)
     __device__ __forceinline__ int begin_of(int c) const {
-        const long long x = each * c + min(c, over) - x0;
-        return x <= 0 ? 0 : x >= w ? w : moved((int)x, w, rows);
+        const W x = each * c + min(c, over);
+        return x <= x0 ? 0 : x - x0 >= (W)w ? w : moved((int)(x - x0), w, rows);
     }
     // the CTA that the block begins in
     __device__ __forceinline__ int first() const {
-        const long long more = (each + 1) * over;
+        const W more = (each + 1) * over;
         int c = x0 < more ? (int)quotient(x0, each + 1) : over + (int)quotient(x0 - more, each);
         while (begin_of(c + 1) == 0) ++c;
         return c;
@@ -148,11 +153,12 @@ struct Begin {
 };
 
 // One piece after the other of a CTA's range; every warp goes through them by itself.
+template <typename W>
 struct Pieces {
     const ChunkParams& p;
     Begin at;                  // where the next piece begins
     int count;                 // blocks of its request
-    long long left;            // what is left of the range
+    W left;                    // what is left of the range
     int next_start, next_n, next_L;   // the request behind (read early)
     // the piece: tiles [t0, t1) of `tiles`, the block's keys and tokens, its request, KV
     // head and place
@@ -160,7 +166,7 @@ struct Pieces {
     int b, h, L, start;
     int off, end;              // its part of the block's weight
 
-    __device__ __forceinline__ Pieces(const ChunkParams& p_, const Begin& begin, long long size)
+    __device__ __forceinline__ Pieces(const ChunkParams& p_, const Begin& begin, W size)
         : p(p_), at(begin), count(0), left(begin.b >= 0 ? size : 0), next_start(0), next_n(0), next_L(0) {
         if (left > 0) arrive();
     }
@@ -175,7 +181,7 @@ struct Pieces {
             tokens = min(at.n - token0, p.block_tokens);
             keys = max(0, at.L - at.n + token0 + tokens);
             tiles = (keys + kKeys - 1) / kKeys;
-            const int w = keys + kBeginKeys - at.off, take = left < w ? (int)left : w;
+            const int w = keys + kBeginKeys - at.off, take = left < (W)w ? (int)left : w;
             t0 = tile_at(at.off, keys);
             t1 = tile_at(at.off + take, keys);
             const bool there = t1 > t0 || (tiles == 0 && at.off == 0);
@@ -380,6 +386,7 @@ __device__ __forceinline__ void wait(uint64_t* bar, uint32_t parity, volatile in
     __syncwarp();
 }
 
+template <typename W>
 __global__ void __launch_bounds__(kThreads, 1)
 chunk_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
                        const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_q_small,
@@ -388,10 +395,10 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_c
     uint8_t* const sq = smem;                      // [dim half][row][128 B]
     uint8_t* const ring = smem + kQBytes;
     __shared__ Bars bars;
-    __shared__ long long s_part[kThreads / 32];
+    __shared__ W s_part[kThreads / 32];
     __shared__ Begin s_begin;
     __shared__ int s_move[2], s_over, s_join;
-    __shared__ long long s_each, s_lo;
+    __shared__ W s_each, s_lo;
     // for the warp of the other keys: a warp's rows' sums of the first half; of the second,
     // and maxima before
     __shared__ float s_row[2][16][16];
@@ -436,25 +443,31 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_c
     wait_prior_grid();
     allow_dependent_launch();
 
-    // ---- the range: two requests a thread, their weights' running sum
-    constexpr int kEach = (kMaxBatch + kThreads - 1) / kThreads;
-    long long weight[kEach], mine = 0;   // (of one KV head)
-    Begin own[kEach];
-#pragma unroll
-    for (int e = 0; e < kEach; ++e) {
-        own[e].b = threadIdx.x * kEach + e;
-        weight[e] = 0;
-        if (own[e].b < p.nb) {
-            p.batch.rows_of(p.b0 + own[e].b, own[e].start, own[e].n, own[e].L);
-            const Blocks blocks(own[e].n, own[e].L, p.block_tokens);
-            if (own[e].n > 0) weight[e] = blocks.before(blocks.count);
-        }
-        mine += weight[e] * p.Hkv;
+    // ---- the range: requests' weights, and their running sum.  Half of the threads look
+    // for where it begins, the others for where it ends.
+    constexpr int kHalfThreads = kThreads / 2, kEach = (kMaxBatch + kHalfThreads - 1) / kHalfThreads;
+    const bool looks_for_end = threadIdx.x >= kHalfThreads;
+    const int each_ = p.nb <= kHalfThreads ? 1 : kEach, b0 = (threadIdx.x - (looks_for_end ? kHalfThreads : 0)) * each_;
+    W mine = 0;
+    Begin own{-1, 0, 0, 0, 0, 0, 0};
+    W weight = 0;              // (of one KV head, of the last request looked at)
+    auto look = [&](int b) {
+        own.b = b;
+        weight = 0;
+        if (b >= p.nb) return;
+        p.batch.rows_of(p.b0 + b, own.start, own.n, own.L);
+        const Blocks<W> blocks(own.n, own.L, p.block_tokens);
+        if (own.n > 0) weight = blocks.before(blocks.count);
+    };
+#pragma unroll 1
+    for (int e = 0; e < each_; ++e) {
+        look(b0 + e);
+        mine += weight * p.Hkv;
     }
-    long long upto = mine;
+    W upto = mine;
 #pragma unroll
     for (int d = 1; d < 32; d *= 2) {
-        const long long x = __shfl_up_sync(0xffffffffu, upto, d);
+        const W x = __shfl_up_sync(0xffffffffu, upto, d);
         if (lane >= d) upto += x;
     }
     if (lane == 31) s_part[warp] = upto;
@@ -463,15 +476,22 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_c
     __syncthreads();
     fence_after();
     const uint32_t tmem = s_tmem;
-    long long total = 0, at = upto - mine;
-    for (int w = 0; w < kThreads / 32; ++w) {
-        if (w < warp) at += s_part[w];
-        total += s_part[w];
+    // the warps' sums, by half
+    constexpr int kWarps = kThreads / 64;
+    W sums = lane < kWarps ? s_part[(looks_for_end ? kWarps : 0) + lane] : 0;
+#pragma unroll
+    for (int d = 1; d < 16; d *= 2) {
+        const W x = __shfl_up_sync(0xffffffffu, sums, d);
+        if (lane >= d) sums += x;
     }
+    const W total = __shfl_sync(0xffffffffu, sums, kWarps - 1);
+    const int before = warp - (looks_for_end ? kWarps : 0);
+    const W front = __shfl_sync(0xffffffffu, sums, before > 0 ? before - 1 : 0);
+    W at = upto - mine + (before > 0 ? front : 0);
     // the first CTAs take one more of what is over
-    const long long each = quotient(total, gridDim.x);
+    const W each = quotient(total, (W)gridDim.x);
     const int over = (int)(total - each * gridDim.x), cta = blockIdx.x;
-    const long long lo = each * cta + min(cta, over), hi = lo + each + (cta < over);
+    const W lo = each * cta + min(cta, over), hi = lo + each + (cta < over);
     if (threadIdx.x == 0) {
         s_each = each;
         s_over = over;
@@ -479,28 +499,31 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_c
     }
     // An end that is near one of its block's moves there (moved()), for both CTAs that it
     // parts.
-#pragma unroll
-    for (int e = 0; e < kEach; ++e) {
-#pragma unroll
-        for (int end = 0; end < 2; ++end) {
-            const long long in = (end ? hi : lo) - at;
-            if (in < 0 || in >= weight[e] * p.Hkv) continue;
-            Begin a = own[e];
-            a.h = (int)quotient(in, weight[e]);
-            const long long x = in - a.h * weight[e];
-            const Blocks blocks(a.n, a.L, p.block_tokens);
-            a.i = blocks.at(x);
-            a.off = (int)(x - blocks.before(a.i));
-            const int after = (int)(blocks.before(a.i + 1) - x);
-            const int to = moved(a.off, a.off + after, p.G * min(a.n - a.i * p.block_tokens, p.block_tokens));
-            s_move[end] = to - a.off;
-            a.off = to;
-            if (end == 0) s_begin = a;
+    const W want = looks_for_end ? hi : lo;
+    if (want >= at && want - at < mine) {
+#pragma unroll 1
+        for (int e = 0; e < each_; ++e) {
+            if (each_ > 1) look(b0 + e);
+            const W in = want - at;
+            if (want >= at && in < weight * p.Hkv) {
+                own.h = (int)quotient(in, weight);
+                const W x = in - own.h * weight;
+                const Blocks<W> blocks(own.n, own.L, p.block_tokens);
+                own.i = blocks.at(x);
+                const W front_ = blocks.before(own.i);
+                own.off = (int)(x - front_);
+                const int keys = max(0, own.L - own.n + min(own.n, (own.i + 1) * p.block_tokens));
+                const int to = moved(own.off, keys + kBeginKeys, p.G * min(own.n - own.i * p.block_tokens, p.block_tokens));
+                s_move[looks_for_end] = to - own.off;
+                own.off = to;
+                if (!looks_for_end) s_begin = own;
+                break;
+            }
+            at += weight * p.Hkv;
         }
-        at += weight[e] * p.Hkv;
     }
     __syncthreads();
-    Pieces pc(p, s_begin, hi + s_move[1] - (lo + s_move[0]));
+    Pieces<W> pc(p, s_begin, hi + s_move[1] - (lo + s_move[0]));
     const uint32_t ring_at = smem_u32(ring);
 
     if (warp < kFirstSoftmax) {
@@ -791,8 +814,8 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_c
             // does not go by who came last).
             const bool begins = pc.off == 0;   // (then it is the last piece of the CTA's range, else the first)
             const int mine = 2 * blockIdx.x + begins;
-            const long long x0 = begins ? s_lo + s_each + ((int)blockIdx.x < s_over) + s_move[1] - pc.end : s_lo + s_move[0] - pc.off;
-            const Cuts cuts{x0, s_each, pc.keys + kBeginKeys, pc.tokens * p.G, s_over};
+            const W x0 = begins ? s_lo + s_each + ((int)blockIdx.x < s_over) + s_move[1] - pc.end : s_lo + s_move[0] - pc.off;
+            const Cuts<W> cuts{x0, s_each, pc.keys + kBeginKeys, pc.tokens * p.G, s_over};
             const int first_cta = begins ? (int)blockIdx.x : cuts.first();
             bool join = false;
             if (p.join_here) {
@@ -1088,24 +1111,30 @@ cs_status launch_chunk_attention(const cs_attn_dims& d, const void* q, int64_t q
     if (st == CS_OK) st = encode_rows(&mq, q, d, tokens, q_stride, p.block_tokens);
     if (st == CS_OK) st = encode_rows(&ms, q, d, tokens, q_stride, p.small_tokens);
     if (st != CS_OK) return st;
+    // whether the weight of all blocks is sure to fit 32 bits
+    const long long most_blocks = (tokens + p.block_tokens - 1) / p.block_tokens + (long long)d.batch;
+    const bool wide = (p.batch.max_keys + (long long)kBeginKeys) * p.Hkv > 0x7fffffffLL / most_blocks;
+    auto kern = wide ? chunk_attention_kernel<uint64_t> : chunk_attention_kernel<uint32_t>;
     {
-        static std::atomic<bool> done[64];
+        static std::atomic<bool> done[2][64];
         int dev = 0;
         cudaError_t e = cudaGetDevice(&dev);
         if (e != cudaSuccess) return cuda_fail(e, "cudaGetDevice");
-        if (dev < 0 || dev >= 64 || !done[dev]) {
-            e = cudaFuncSetAttribute(chunk_attention_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
+        if (dev < 0 || dev >= 64 || !done[wide][dev]) {
+            e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
             if (e != cudaSuccess) return cuda_fail(e, "cudaFuncSetAttribute(chunk_attention_kernel)");
-            if (dev >= 0 && dev < 64) done[dev] = true;
+            if (dev >= 0 && dev < 64) done[wide][dev] = true;
         }
     }
     // As many blocks as there may be (the lengths are the device's): with few of them each
     // has many pieces, and joining them is work for the whole card.
     const long long by_tokens = (tokens + p.block_tokens - 1) / p.block_tokens;
-    p.join_here = kJoinBlocks * p.Hkv * (by_tokens > d.batch ? by_tokens : d.batch < tokens ? d.batch : tokens) >= grid;
+    // (Nor is there anything to join where no context is long enough for a cut.)
+    const bool uncut = p.batch.max_keys + kBeginKeys <= 2 * (kCutKeys + kCutRow * p.G);
+    p.join_here = uncut || kJoinBlocks * p.Hkv * (by_tokens > d.batch ? by_tokens : d.batch < tokens ? d.batch : tokens) >= grid;
     for (p.b0 = 0; p.b0 < d.batch; p.b0 += kMaxBatch) {
         p.nb = d.batch - p.b0 < kMaxBatch ? d.batch - p.b0 : kMaxBatch;
-        cudaError_t e = launch_dependent(chunk_attention_kernel, dim3(grid), dim3(kThreads), (size_t)kSmem, stream, mk, mv,
+        cudaError_t e = launch_dependent(kern, dim3(grid), dim3(kThreads), (size_t)kSmem, stream, mk, mv,
                                          mq, ms, p);
         if (e != cudaSuccess) return cuda_fail(e, "chunk_attention_kernel launch");
         if (p.join_here) continue;
