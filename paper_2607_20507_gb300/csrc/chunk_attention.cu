@@ -48,6 +48,7 @@ constexpr int kSmem = kQBytes + kStages * kTileBytes;
 constexpr int kSmallQRows = 32;                    // blocks of few rows bring in no more than these
 constexpr int kBeginKeys = 208;                    // what beginning and ending a block costs, in keys
 constexpr int kCutKeys = 384, kCutRow = 2;         // a range's end moves by so many keys, and so many a row, to a block's
+constexpr int kLeast = 128, kLeastRow = 2;         // a CTA's share where blocks are few: so many keys, and so many a row
 constexpr int kMaxBatch = 1024;                    // requests of a launch
 constexpr float kMostSum = 0x1p-56f;               // 2^8 times 2^-kPShift
 
@@ -70,6 +71,7 @@ struct ChunkParams {
     int small_tokens;          // ... of the small query box
     int rows;                  // rows of a slot
     bool join_here;            // the last to come joins a block's pieces
+    int least;                 // of a CTA's share
     float scale_log2;
 };
 constexpr int kUsed = 1, kEnds = 2;                // flags of a slot: it holds a piece, which has its block's last tile
@@ -488,10 +490,12 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_c
     const int before = warp - (looks_for_end ? kWarps : 0);
     const W front = __shfl_sync(0xffffffffu, sums, before > 0 ? before - 1 : 0);
     W at = upto - mine + (before > 0 ? front : 0);
-    // the first CTAs take one more of what is over
-    const W each = quotient(total, (W)gridDim.x);
-    const int over = (int)(total - each * gridDim.x), cta = blockIdx.x;
-    const W lo = each * cta + min(cta, over), hi = lo + each + (cta < over);
+    // the first CTAs take one more of what is over; with few blocks only as many work as
+    // have a share that is worth a piece's join
+    const W ctas = min((W)gridDim.x, max((W)1, quotient(total, (W)p.least)));
+    const W each = quotient(total, ctas);
+    const int over = (int)(total - each * ctas), cta = min((int)blockIdx.x, (int)ctas);
+    const W lo = each * cta + min(cta, over), hi = blockIdx.x < ctas ? lo + each + (cta < over) : lo;
     if (threadIdx.x == 0) {
         s_each = each;
         s_over = over;
@@ -1132,6 +1136,7 @@ cs_status launch_chunk_attention(const cs_attn_dims& d, const void* q, int64_t q
     // (Nor is there anything to join where no context is long enough for a cut.)
     const bool uncut = p.batch.max_keys + kBeginKeys <= 2 * (kCutKeys + kCutRow * p.G);
     p.join_here = uncut || kJoinBlocks * p.Hkv * (by_tokens > d.batch ? by_tokens : d.batch < tokens ? d.batch : tokens) >= grid;
+    p.least = p.join_here ? 1 : kLeast + kLeastRow * p.rows;
     for (p.b0 = 0; p.b0 < d.batch; p.b0 += kMaxBatch) {
         p.nb = d.batch - p.b0 < kMaxBatch ? d.batch - p.b0 : kMaxBatch;
         cudaError_t e = launch_dependent(kern, dim3(grid), dim3(kThreads), (size_t)kSmem, stream, mk, mv,
