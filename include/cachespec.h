@@ -536,7 +536,9 @@ cs_status cs_packed_verify_attention(const cs_attn_dims* dims, const void* q, co
  *   q_starts   int32 [B + 1], not decreasing, from 0 on at most `tokens`; or NULL:
  *              tokens / B rows a request (B has to divide tokens).  Rows in front of
  *              q_starts[0] and from q_starts[B] on belong to nobody: they are not
- *              computed and what stands in their place in outputs stays.
+ *              computed and what stands in their place in outputs stays.  (Entries
+ *              that decrease: the calls stay within their arrays, results and the
+ *              workspace of cs_chunk_attention are undefined.)
  *   strides    rows of q, new_k and new_v may lie apart, as where a projection wrote
  *              queries, keys and values side by side: elements from one token's heads
  *              to the next token's, a multiple of 8 up to 2^30; the heads of a token lie

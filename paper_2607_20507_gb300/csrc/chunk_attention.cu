@@ -132,7 +132,7 @@ template <typename W>
 struct Cuts {
     W x0, each;
     int w, rows;
-    int over;
+    int over, ctas;
     // where CTA c's range begins in the block (0, w: in front of it, behind it)
     __device__ __forceinline__ int begin_of(int c) const {
         const W x = each * c + min(c, over);
@@ -142,8 +142,8 @@ struct Cuts {
     __device__ __forceinline__ int first() const {
         const W more = (each + 1) * over;
         int c = x0 < more ? (int)quotient(x0, each + 1) : over + (int)quotient(x0 - more, each);
-        while (begin_of(c + 1) == 0) ++c;
-        return c;
+        while (c + 1 < ctas && begin_of(c + 1) == 0) ++c;
+        return min(c, ctas - 1);
     }
 };
 
@@ -375,6 +375,9 @@ struct Bars {
     uint64_t drained;
 };
 
+// Whether no wait of the block has given up, the same answer in the whole warp.
+__device__ __forceinline__ bool alive(volatile int* dead) { return !__any_sync(0xffffffffu, *dead); }
+
 // Waits for the phase of the given parity, the whole warp; any wait returns at once
 // after one of the block has given up.  (What follows then works on whatever is there,
 // within the same bounds, to the end, and the status says so: no warp leaves before
@@ -553,8 +556,9 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_c
 #pragma unroll
                     for (int v = 0; v < 2; ++v) {
                         const uint32_t st = at_stage % kStages, round = at_stage / kStages;
-                        ++at_stage;
                         if (round > 0) wait(&bars.kv_empty[st], (round - 1) & 1, &s_dead, p.status);
+                        if (!alive(&s_dead)) break;   // (nothing more into a stage that may be in use)
+                        ++at_stage;
                         if (lane == 0) mbar_arrive_expect_tx(&bars.kv_full[st], (uint32_t)live * box * (kD * 2));
                         __syncwarp();
                         if (lane < live)
@@ -573,6 +577,7 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_c
             while (pc.next()) {
                 if (pc.tiles == 0) continue;
                 if (piece > 0) wait(&bars.q_empty, (piece - 1) & 1, &s_dead, p.status);
+                if (!alive(&s_dead)) break;
                 ++piece;
                 const bool few = pc.tokens <= p.small_tokens;
                 const int box = few ? p.small_tokens : p.block_tokens;
@@ -819,7 +824,7 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_c
             const bool begins = pc.off == 0;   // (then it is the last piece of the CTA's range, else the first)
             const int mine = 2 * blockIdx.x + begins;
             const W x0 = begins ? s_lo + s_each + ((int)blockIdx.x < s_over) + s_move[1] - pc.end : s_lo + s_move[0] - pc.off;
-            const Cuts<W> cuts{x0, s_each, pc.keys + kBeginKeys, pc.tokens * p.G, s_over};
+            const Cuts<W> cuts{x0, s_each, pc.keys + kBeginKeys, pc.tokens * p.G, s_over, (int)gridDim.x};
             const int first_cta = begins ? (int)blockIdx.x : cuts.first();
             bool join = false;
             if (p.join_here) {
@@ -860,7 +865,7 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_c
                             for (int e = 0; e < 16; ++e) sum[e] = 0.f;
                             int x = 0;
 #pragma unroll 1
-                            for (int cta = first_cta; x < cuts.w; ++cta) {
+                            for (int cta = first_cta; x < cuts.w && cta < cuts.ctas; ++cta) {
                                 const int y = cuts.begin_of(cta + 1);
                                 const bool there = tile_at(x, pc.keys) < tile_at(y, pc.keys);
                                 x = y;

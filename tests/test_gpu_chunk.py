@@ -99,6 +99,31 @@ def test_a_chunk_behind_a_long_context():
     check(batch([700], [9000], 16, 2, 16, junk=False))
 
 
+@pytest.mark.parametrize("ns,before,hq,hkv", [
+    ([1] * 100, [20] * 99 + [60000], 8, 2),                        # one context over many CTAs, among short ones
+    ([1] * 90, [3000 + 37 * b for b in range(90)], 16, 2),
+    ([300] * 12, [2000] * 12, 16, 4),                              # whole blocks of rows
+    ([256, 1, 700] * 6, [100, 9000, 1500] * 6, 4, 4),
+    ([3, 40] * 20, [6000 - 150 * b for b in range(40)], 28, 4),
+])
+def test_blocks_cut_between_ctas(ns, before, hq, hkv):
+    """Whoever comes last joins the pieces of a block, in the same order."""
+    args = batch(ns, before, hq, hkv, 16, junk=False)
+    out = check(args)
+    for _ in range(5):
+        assert torch.equal(binding.cs_chunk_attention(*args), out)
+
+
+def test_a_page_table_of_many_columns():
+    """The schedule's weights in 64 bits, where a call's might not fit 32: the same results."""
+    for ns, before in (([1, 300, 7, 0, 1, 64, 1, 2] * 2, [5000, 20, 900, 3, 1, 0, 16000, 300] * 2), ([300, 1], [9000, 20000])):
+        q, k, v, table, lens, starts = batch(ns, before, 16, 2, 256, junk=False)
+        out = check((q, k, v, table, lens, starts))
+        wide = torch.full((len(ns), 1 << 22), -1, dtype=torch.int32, device=DEV)
+        wide[:, :table.shape[1]] = table
+        assert torch.equal(binding.cs_chunk_attention(q, k, v, wide, lens, starts), out)
+
+
 def test_uniform_rows_need_no_starts():
     q, k, v, table, lens, starts = batch([4] * 6, [9, 0, 200, 33, 64, 1], 8, 2, 16)
     assert torch.equal(binding.cs_chunk_attention(q, k, v, table, lens), binding.cs_chunk_attention(q, k, v, table, lens, starts))
