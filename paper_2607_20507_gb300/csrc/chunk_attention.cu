@@ -78,7 +78,8 @@ struct ChunkParams {
     int small_tokens;          // ... of the small query box
     int rows;                  // rows of a slot
     bool join_here;            // the last to come joins a block's pieces
-    int least;                 // of a CTA's share
+    int least;                 // of a CTA's share, 0: whatever it is
+    HostDivisor by_block, by_grid;   // quotients by block_tokens, by the grid
     float scale_log2;
 };
 constexpr int kUsed = 1, kEnds = 2;                // flags of a slot: it holds a piece, which has its block's last tile
@@ -94,7 +95,8 @@ __device__ __forceinline__ uint64_t quotient(uint64_t a, uint64_t b) { return (u
 template <typename W>
 struct Blocks {
     int n, L, T, count;
-    __device__ __forceinline__ Blocks(int n_, int L_, int T_) : n(n_), L(L_), T(T_), count((n_ + T_ - 1) / T_) {}
+    __device__ __forceinline__ Blocks(int n_, int L_, const HostDivisor& T_)
+        : n(n_), L(L_), T((int)T_.d), count((int)T_((uint32_t)n_ + T_.d - 1)) {}
     // the weight of blocks 0 .. i-1
     __device__ __forceinline__ W before(int i) const {
         const int first = L - n;   // keys in front of the new tokens
@@ -156,7 +158,7 @@ struct Cuts {
 
 // Where a CTA's range begins.
 struct Begin {
-    int b, h, i;               // request of the launch, KV head, block
+    int b, h, i, count;        // request of the launch, KV head, block of as many
     int start, n, L;           // the request's rows and length
     int off;                   // how far into the block's weight
 };
@@ -166,9 +168,7 @@ template <typename W>
 struct Pieces {
     const ChunkParams& p;
     Begin at;                  // where the next piece begins
-    int count;                 // blocks of its request
     W left;                    // what is left of the range
-    int next_start, next_n, next_L;   // the request behind (read early)
     // the piece: tiles [t0, t1) of `tiles`, the block's keys and tokens, its request, KV
     // head and place
     int t0, t1, tiles, keys, token0, tokens;
@@ -176,13 +176,7 @@ struct Pieces {
     int off, end;              // its part of the block's weight
 
     __device__ __forceinline__ Pieces(const ChunkParams& p_, const Begin& begin, W size)
-        : p(p_), at(begin), count(0), left(begin.b >= 0 ? size : 0), next_start(0), next_n(0), next_L(0) {
-        if (left > 0) arrive();
-    }
-    __device__ __forceinline__ void arrive() {
-        count = (at.n + p.block_tokens - 1) / p.block_tokens;
-        if (at.b + 1 < p.nb) p.batch.rows_of(p.b0 + at.b + 1, next_start, next_n, next_L);
-    }
+        : p(p_), at(begin), left(begin.b >= 0 ? size : 0) {}
     // false: no more
     __device__ __forceinline__ bool next() {
         while (left > 0) {
@@ -202,17 +196,13 @@ struct Pieces {
             end = at.off + take;
             left -= take;
             at.off = 0;
-            if (left > 0 && ++at.i == count) {
+            if (left > 0 && ++at.i == at.count) {
                 at.i = 0;
                 if (++at.h == p.Hkv) {
                     at.h = 0;
-                    do {
-                        ++at.b;
-                        at.start = next_start;
-                        at.n = next_n;
-                        at.L = next_L;
-                        if (at.b < p.nb) arrive();
-                    } while (at.n == 0 && at.b < p.nb);
+                    at.n = 0;
+                    while (at.n == 0 && ++at.b < p.nb) p.batch.rows_of(p.b0 + at.b, at.start, at.n, at.L);
+                    at.count = (int)p.by_block((uint32_t)at.n + p.by_block.d - 1);
                     if (at.b >= p.nb) left = 0;
                 }
             }
@@ -461,14 +451,15 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_c
     const bool looks_for_end = threadIdx.x >= kHalfThreads;
     const int each_ = p.nb <= kHalfThreads ? 1 : kEach, b0 = (threadIdx.x - (looks_for_end ? kHalfThreads : 0)) * each_;
     W mine = 0;
-    Begin own{-1, 0, 0, 0, 0, 0, 0};
+    Begin own{-1, 0, 0, 0, 0, 0, 0, 0};
     W weight = 0;              // (of one KV head, of the last request looked at)
     auto look = [&](int b) {
         own.b = b;
         weight = 0;
         if (b >= p.nb) return;
         p.batch.rows_of(p.b0 + b, own.start, own.n, own.L);
-        const Blocks<W> blocks(own.n, own.L, p.block_tokens);
+        const Blocks<W> blocks(own.n, own.L, p.by_block);
+        own.count = blocks.count;
         if (own.n > 0) weight = blocks.before(blocks.count);
     };
 #pragma unroll 1
@@ -502,8 +493,8 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_c
     W at = upto - mine + (before > 0 ? front : 0);
     // the first CTAs take one more of what is over; with few blocks only as many work as
     // have a share that is worth a piece's join
-    const W ctas = min((W)gridDim.x, max((W)1, quotient(total, (W)p.least)));
-    const W each = quotient(total, ctas);
+    const W ctas = p.least ? min((W)gridDim.x, max((W)1, quotient(total, (W)p.least))) : gridDim.x;
+    const W each = sizeof(W) == 4 && !p.least ? p.by_grid((uint32_t)total) : quotient(total, ctas);
     const int over = (int)(total - each * ctas), cta = min((int)blockIdx.x, (int)ctas);
     const W lo = each * cta + min(cta, over), hi = blockIdx.x < ctas ? lo + each + (cta < over) : lo;
     if (threadIdx.x == 0) {
@@ -522,7 +513,7 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_c
             if (want >= at && in < weight * p.Hkv) {
                 own.h = (int)quotient(in, weight);
                 const W x = in - own.h * weight;
-                const Blocks<W> blocks(own.n, own.L, p.block_tokens);
+                const Blocks<W> blocks(own.n, own.L, p.by_block);
                 own.i = blocks.at(x);
                 const W front_ = blocks.before(own.i);
                 own.off = (int)(x - front_);
@@ -1117,6 +1108,8 @@ cs_status launch_chunk_attention(const cs_attn_dims& d, const void* q, int64_t q
     p.max_pages = d.max_pages_per_seq;
     p.P = d.num_pages;
     p.block_tokens = kRows / p.G;
+    p.by_block = HostDivisor::of((uint32_t)p.block_tokens);
+    p.by_grid = HostDivisor::of((uint32_t)grid);
     p.small_tokens = p.G < kSmallQRows ? kSmallQRows / p.G : 1;
     p.rows = l.rows;
     p.scale_log2 = (d.sm_scale > 0.f ? d.sm_scale : 1.0f / sqrtf((float)kD)) * 1.4426950408889634f;
@@ -1148,7 +1141,7 @@ cs_status launch_chunk_attention(const cs_attn_dims& d, const void* q, int64_t q
     // (Nor is there anything to join where no context is long enough for a cut.)
     const bool uncut = p.batch.max_keys + kBeginKeys <= 2 * (kCutKeys + kCutRow * p.G);
     p.join_here = uncut || kJoinBlocks * p.Hkv * (by_tokens > d.batch ? by_tokens : d.batch < tokens ? d.batch : tokens) >= grid;
-    p.least = p.join_here ? 1 : kLeast + kLeastRow * p.rows;
+    p.least = p.join_here ? 0 : kLeast + kLeastRow * p.rows;
     for (p.b0 = 0; p.b0 < d.batch; p.b0 += kMaxBatch) {
         p.nb = d.batch - p.b0 < kMaxBatch ? d.batch - p.b0 : kMaxBatch;
         cudaError_t e = launch_dependent(kern, dim3(grid), dim3(kThreads), (size_t)kSmem, stream, mk, mv,

@@ -6,6 +6,22 @@
 
 namespace cs {
 
+// Quotients by a divisor that the host knows, of numbers below 2^31: one high product
+// and a shift (Granlund and Montgomery, 1994).
+struct HostDivisor {
+    uint32_t d, mul;
+    int shift;
+    static HostDivisor of(uint32_t d) {
+        HostDivisor x{d, 0, 0};
+        while ((1ull << x.shift) < d) ++x.shift;
+        if (x.shift > 0) x.mul = (uint32_t)(((1ull << (31 + x.shift)) + d - 1) / d);
+        return x;
+    }
+    __device__ __forceinline__ uint32_t operator()(uint32_t n) const {
+        return shift > 0 ? __umulhi(n, mul) >> (shift - 1) : n;
+    }
+};
+
 struct RaggedBatch {
     const int32_t* ctx_lens;   // [B]
     const int32_t* q_starts;   // [B + 1], or NULL: n rows each
