@@ -343,8 +343,7 @@ __device__ __forceinline__ void store32(void* p, const uint32_t (&r)[8]) {
 
 // (one lane)
 __device__ __forceinline__ void wait_lane(uint64_t* bar, uint32_t parity, volatile int* dead, int* status) {
-    if (mbar_try_wait(bar, parity)) return;
-    if (!*dead && !mbar_wait_bounded(bar, parity)) {
+    if (!mbar_try_wait(bar, parity) && !*dead && !mbar_wait_bounded(bar, parity)) {
         *dead = 1;
         atomicOr(status, CS_DEVICE_WAIT_TIMEOUT);
     }
@@ -380,8 +379,7 @@ __device__ __forceinline__ bool alive(volatile int* dead) { return !__any_sync(0
 // within the same bounds, to the end, and the status says so: no warp leaves before
 // another that it meets at a barrier.)
 __device__ __forceinline__ void wait(uint64_t* bar, uint32_t parity, volatile int* dead, int* status) {
-    if (mbar_try_wait(bar, parity)) return;
-    if (!*dead && !mbar_wait_bounded(bar, parity)) {
+    if (!mbar_try_wait(bar, parity) && !*dead && !mbar_wait_bounded(bar, parity)) {
         *dead = 1;
         atomicOr(status, CS_DEVICE_WAIT_TIMEOUT);
     }
@@ -673,7 +671,8 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_c
         // Of these, warps w and w + 8 take lanes 32 (w % 4) + 16 (w / 4 % 2) .. of either half, the
         // first keys 0-63 of a tile, the second 64-127; threads i and i + 16 share a row,
         // 32 keys each (and as many dims of O).  The two warps agree at a barrier of their
-        // own whether the weights stand, after which each may write over the other's scores.
+        // own whether the weights stand, after which each may write over the other's scores
+        // (which that has read).
         const int sw = warp - kFirstSoftmax;
         const int part = (sw >> 3) * 2 + (lane >> 4);     // the thread's quarter of keys and dims
         const int lane0 = (sw & 3) * 32 + ((sw >> 2) & 1) * 16;
