@@ -397,7 +397,8 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_c
     __shared__ Bars bars;
     __shared__ W s_part[kThreads / 32];
     __shared__ Begin s_begin;
-    __shared__ int s_move[2], s_over, s_join;
+    __shared__ int s_move[2], s_over;
+    __shared__ int s_join[2];                      // of the range's first piece, and of its last
     __shared__ W s_each, s_lo;
     // for the warp of the other keys: a warp's rows' sums of the first half; of the second,
     // and maxima before
@@ -826,11 +827,11 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_c
             bool join = false;
             if (p.join_here) {
                 if (threadIdx.x == kFirstSoftmax * 32) {
-                    s_join = __ldcg(p.done + first_cta) + pc.t1 - pc.t0 == pc.tiles;
+                    s_join[begins] = __ldcg(p.done + first_cta) + pc.t1 - pc.t0 == pc.tiles;
                     __threadfence();
                 }
                 all_sync();
-                join = s_join;
+                join = s_join[begins];
             } else if (threadIdx.x == kFirstSoftmax * 32) {
                 p.slots[mine] = make_int4(pc.start + pc.token0, pc.h, pc.tokens, kUsed | (pc.t1 == pc.tiles ? kEnds : 0));
             }
@@ -914,11 +915,11 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_c
                 __threadfence();
                 all_sync();
                 if (threadIdx.x == kFirstSoftmax * 32) {
-                    s_join = atomicAdd(p.done + first_cta, pc.t1 - pc.t0) + pc.t1 - pc.t0 == pc.tiles;
+                    s_join[begins] = atomicAdd(p.done + first_cta, pc.t1 - pc.t0) + pc.t1 - pc.t0 == pc.tiles;
                     __threadfence();
                 }
                 all_sync();
-                join = s_join;
+                join = s_join[begins];
                 if (!join) break;
             }
             if (join && threadIdx.x == kFirstSoftmax * 32) p.done[first_cta] = 0;
