@@ -108,12 +108,15 @@ __device__ __forceinline__ void store_half_group(const Eight& x0, float head, bo
 
 // What a thread does to its sixteen dims x and y: x <- x xx + y xy, y <- y yy + x yx (or,
 // of neighbouring dims, x <- x xx + x' xy with the pairs of x swapped, and the same of y),
-// times 1 / rms where there is a norm.
+// times 1 / rms where there is a norm.  Dims that do not turn see nothing of their
+// partners (0 times an infinity is no 0).
 template <bool kNeighbours>
 struct Turn {
     Eight xx, xy, yy, yx;
+    uint64_t seen;             // of the other dims' bits
     // row: the position's cosines and sines, or NULL for dims that do not turn
     __device__ __forceinline__ Turn(const float* row, int rot, const uint4* norm, int c0, int c1) {
+        seen = row ? ~0ull : 0ull;
         // the cosines and sines of pairs 8t .. 8t+7, or (neighbouring dims) of the four of
         // either vector
         float cosv[8], sinv[8], u[8], v[8];
@@ -151,13 +154,15 @@ struct Turn {
                 yy.v[j] = f2_pack(v[i] * cosv[i], v[k] * cosv[k]);
                 yx.v[j] = f2_pack(u[i] * sinv[i], u[k] * sinv[k]);
             }
+            if (!row) xy.v[j] = yx.v[j] = 0x8000000080000000ull;   // -0: what it is added to stays
         }
     }
     __device__ __forceinline__ void operator()(Eight& x, Eight& y, bool norm, float eps) const {
         Eight a, b;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            const uint64_t xo = kNeighbours ? swapped(x.v[j]) : y.v[j], yo = kNeighbours ? swapped(y.v[j]) : x.v[j];
+            const uint64_t xo = (kNeighbours ? swapped(x.v[j]) : y.v[j]) & seen;
+            const uint64_t yo = (kNeighbours ? swapped(y.v[j]) : x.v[j]) & seen;
             a.v[j] = f2_fma(x.v[j], xx.v[j], f2_mul(xo, xy.v[j]));
             b.v[j] = f2_fma(y.v[j], yy.v[j], f2_mul(yo, yx.v[j]));
         }

@@ -191,6 +191,26 @@ def test_values_keep_their_bits_and_a_row_that_is_not_finite_is_its_own():
 
 
 # --------------------------------------------------------------- the packed cache
+@pytest.mark.parametrize("rot", [32, 64, 96])
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_dims_that_do_not_turn_stay_whatever_stands_beside_them(rot, interleaved):
+    qkv, turns, _, table, lens, starts, P = batch([3, 30], [4, 0], 4, 2, 16, rot, seed=3)
+    pools = [torch.zeros((P, 2, 16, 128), dtype=torch.bfloat16, device=DEV) for _ in range(2)]
+    clean = binding.cs_rope_kv_append(*qkv, turns, *pools, table, lens, starts, interleaved=interleaved)
+    clean_k = pools[0].clone()
+    for x in qkv[:2]:
+        x[1::2, :, rot::5], x[1::2, :, rot + 1::5], x[1::2, :, rot + 2::7], x[1::2, :, rot + 3::7] = math.inf, -0.0, -math.inf, 3e38
+    got = binding.cs_rope_kv_append(*qkv, turns, *pools, table, lens, starts, interleaved=interleaved)
+    assert torch.equal(got[..., :rot], clean[..., :rot]) and torch.equal(pools[0][..., :rot], clean_k[..., :rot])
+    assert torch.equal(got[..., rot:].view(torch.int16), qkv[0][..., rot:].contiguous().view(torch.int16))
+    for b, row, _, j in ref.rows_of(starts.tolist(), lens.tolist(), 2, 33, table.shape[1] * 16):
+        put = pools[0][int(table[b, j // 16]), :, j % 16, rot:]
+        assert torch.equal(put.view(torch.int16), qkv[1][row, :, rot:].contiguous().view(torch.int16))
+    qkv[0][0, 0, rot + 9] = math.nan
+    again = binding.cs_rope_kv_append(*qkv, turns, *pools, table, lens, starts, interleaved=interleaved)
+    assert (again.isnan()).nonzero().tolist() == [[0, 0, rot + 9]]
+
+
 def packed_pool(P, H, ps, heads, seed=0):
     rng = np.random.default_rng(seed)
     scales = [torch.from_numpy((2.0 ** rng.uniform(-3, 1, H)).astype(np.float32)).to(DEV) for _ in range(2)] if heads else [None] * 2
