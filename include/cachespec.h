@@ -564,7 +564,8 @@ cs_status cs_packed_verify_attention(const cs_attn_dims* dims, const void* q, co
  *   positions  int32 [tokens] or NULL.  For token trees: a node's depth below the
  *              root counts, not its slot.
  *   q_norm, k_norm   bf16 [128], 16-byte aligned, or NULL
- *   q_out      bf16 [tokens, Hq, 128], 16-byte aligned; may be q itself (with its stride)
+ *   q_out      bf16 [tokens, Hq, 128], 16-byte aligned; may be q itself (with its stride; another
+ *              one is refused), and must not overlap any other input
  *   rope->tokens         at most 2^31 - 1
  *   rope->rot_dim        32, 64, 96 or 128
  * A token whose rotation position lies outside [0, n_positions) is left out: its

@@ -238,6 +238,8 @@ cs_status check_rope(const cs_attn_dims* d, const cs_rope_dims* r, const void* q
         return st;
     *nothing = d->batch == 0 || r->tokens == 0;
     if (*nothing) return CS_OK;
+    if (q && q == q_out && r->tokens > 1 && r->q_stride != r->q_out_stride)
+        return fail(CS_ERR_INVALID_ARG, "q_out is q with another stride");
     st = check_ragged_pointers(d, r->tokens, page_table, ctx_lens, q_starts);
     if (st != CS_OK) return st;
     if (!new_k || !new_v || !cos_sin) return fail(CS_ERR_INVALID_ARG, "a tensor pointer is NULL");

@@ -110,6 +110,11 @@ def test_append_refuses_arguments(lib, call):
     assert call(lib, dims(batch=0), k=None) == OK and call(lib, r=turns(tokens=0), k=None) == OK
 
 
+@pytest.mark.parametrize("call", [append, packed])
+def test_append_refuses_queries_in_place_with_another_stride(lib, call):
+    assert call(lib, r=turns(q_stride=8192)) == BAD and call(lib, r=turns(q_out_stride=4104)) == BAD
+
+
 def test_append_refuses_pools(lib):
     assert append(lib, kp=None) == BAD and append(lib, vp=FAKE + 8) == BAD
     for name in ("k_codes", "k_scales", "v_codes", "v_scales"):
