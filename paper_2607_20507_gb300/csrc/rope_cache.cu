@@ -6,9 +6,12 @@
 // two 16-byte vectors whose dims pair up with each other (or, of neighbouring pairs and
 // of dims that do not turn, with themselves), so that a thread's cosines and sines are
 // the same in every head, are read once and multiplied by the norm's weights once.
-// Where tokens are few their heads are spread over several warps (as many as make 12 an
-// SM: a token's look-ups cost a warp as much as three fours of heads, and 64 trees of 21
-// nodes took 7.1 us so, 8.3 with 20 and 12.5 with 24).  Two fours are on their way in
+// Where tokens are few their heads are spread over several warps, as many as make 8 an SM:
+// a token's look-ups cost a warp as much as three fours of heads, and so the CTAs of two
+// launches fit beside each other (200 tokens of 64 / 8 heads: 4.2 us, 4.6 with 6 and 6.0
+// with 12; 400: 5.4, 6.1, 6.7).  Where that leaves a warp more than twelve fours, 18 an SM,
+// all that runs at once (1344 tokens: 11.4 us, 14.1 with 8, 13.7 with 28; of 128 / 8 heads:
+// 21, 29.5 and 25).  Two fours are on their way in
 // while one is turned, and the first while the token's request, length and page are
 // looked up.  28,932 tokens of 64 / 8 heads, normed (1.2 GB in and out): 200-207 us, 5.8 TB/s
 // or more, bound by the memory (one four ahead: 208; one CTA a token, its heads in turn: 296).
@@ -22,7 +25,8 @@ namespace {
 constexpr int kThreads = 128;
 constexpr int kRowThreads = 8;                      // threads of a head's row
 constexpr int kRows = 32 / kRowThreads;             // heads that a warp takes at once
-constexpr int kWarpsPerSm = 12;                     // that tokens are spread over, where they are few
+constexpr int kWarpsPerSm = 8;                      // that tokens are spread over, where they are few
+constexpr int kMostWarpsPerSm = 18, kLongShare = 12;   // so many, where a warp's fours would be more
 constexpr float kLarge = 0x1p60f, kSmall = 0x1p-60f;   // between them quotients go without a division
 
 struct RopeParams {
@@ -325,9 +329,12 @@ cs_status launch(const cs_attn_dims& d, const cs_rope_dims& r, RopeParams& p, bo
                        : (r.interleaved ? rope_append_kernel<false, true> : rope_append_kernel<false, false>);
     // as many warps as there is room for, each a token's share of fours
     const int fours = (p.Hq + kRows - 1) / kRows + 2 * ((p.Hkv + kRows - 1) / kRows);
-    const long long room = (long long)current_sm_count() * kWarpsPerSm;
-    p.parts = (int)(room / r.tokens);
-    p.parts = p.parts < 1 ? 1 : p.parts < fours ? p.parts : fours;
+    auto spread = [&](int warps) {
+        const long long parts = (long long)current_sm_count() * warps / r.tokens;
+        return parts < 1 ? 1 : parts < fours ? (int)parts : fours;
+    };
+    p.parts = spread(kWarpsPerSm);
+    if ((fours + p.parts - 1) / p.parts > kLongShare) p.parts = spread(kMostWarpsPerSm);
     const dim3 grid((unsigned)((r.tokens + kThreads / 32 - 1) / (kThreads / 32)), (unsigned)p.parts);
     const cudaError_t e = launch_dependent(kern, grid, dim3(kThreads), 0, stream, p);
     return e == cudaSuccess ? CS_OK : cuda_fail(e, "rope_append_kernel launch");
