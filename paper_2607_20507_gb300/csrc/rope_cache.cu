@@ -9,9 +9,10 @@
 // Where tokens are few their heads are spread over several warps, as many as make 8 an SM:
 // a token's look-ups cost a warp as much as three fours of heads, and so the CTAs of two
 // launches fit beside each other (200 tokens of 64 / 8 heads: 4.2 us, 4.6 with 6 and 6.0
-// with 12; 400: 5.4, 6.1, 6.7).  Where that leaves a warp more than twelve fours, 18 an SM,
-// all that runs at once (1344 tokens: 11.4 us, 14.1 with 8, 13.7 with 28; of 128 / 8 heads:
-// 21, 29.5 and 25).  Two fours are on their way in
+// with 12; 400: 5.4, 6.1, 6.7).  Where that leaves a warp more than twelve fours, by the
+// fewest rounds of 20 warps an SM times what each takes (1344 tokens of 64 / 8 heads, two
+// warps each: 11.4 us, 14.1 with one, 13.7 with three; 2000: 19.3 with one, 20.6 with two,
+// 17.7 with three; 4000: 39.6 with one, 36.4 with two).  Two fours are on their way in
 // while one is turned, and the first while the token's request, length and page are
 // looked up.  28,932 tokens of 64 / 8 heads, normed (1.2 GB in and out): 200-207 us, 5.8 TB/s
 // or more, bound by the memory (one four ahead: 208; one CTA a token, its heads in turn: 296).
@@ -26,7 +27,9 @@ constexpr int kThreads = 128;
 constexpr int kRowThreads = 8;                      // threads of a head's row
 constexpr int kRows = 32 / kRowThreads;             // heads that a warp takes at once
 constexpr int kWarpsPerSm = 8;                      // that tokens are spread over, where they are few
-constexpr int kMostWarpsPerSm = 18, kLongShare = 12;   // so many, where a warp's fours would be more
+constexpr int kLongShare = 12;                      // fours of a warp that count as many
+constexpr int kLookUp = 3;                          // fours that look-ups cost as much as
+constexpr int kCtasPerSm = 5;
 constexpr float kLarge = 0x1p60f, kSmall = 0x1p-60f;   // between them quotients go without a division
 
 struct RopeParams {
@@ -195,7 +198,7 @@ struct Turn {
 };
 
 template <bool kPacked, bool kNeighbours>
-__global__ void __launch_bounds__(kThreads, 5) rope_append_kernel(const RopeParams p) {
+__global__ void __launch_bounds__(kThreads, kCtasPerSm) rope_append_kernel(const RopeParams p) {
     const int lane = threadIdx.x & 31, t = lane & (kRowThreads - 1);
     const uint32_t token = blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5);
     const int part = blockIdx.y;
@@ -329,12 +332,20 @@ cs_status launch(const cs_attn_dims& d, const cs_rope_dims& r, RopeParams& p, bo
                        : (r.interleaved ? rope_append_kernel<false, true> : rope_append_kernel<false, false>);
     // as many warps as there is room for, each a token's share of fours
     const int fours = (p.Hq + kRows - 1) / kRows + 2 * ((p.Hkv + kRows - 1) / kRows);
-    auto spread = [&](int warps) {
-        const long long parts = (long long)current_sm_count() * warps / r.tokens;
-        return parts < 1 ? 1 : parts < fours ? (int)parts : fours;
-    };
-    p.parts = spread(kWarpsPerSm);
-    if ((fours + p.parts - 1) / p.parts > kLongShare) p.parts = spread(kMostWarpsPerSm);
+    const long long sms = current_sm_count(), room = sms * kWarpsPerSm / r.tokens;
+    p.parts = room < 1 ? 1 : room < fours ? (int)room : fours;
+    auto share = [&](int parts) { return (fours + parts - 1) / parts; };
+    if (share(p.parts) > kLongShare) {
+        const long long at_once = sms * kCtasPerSm * (kThreads / 32);
+        long long best = 0;
+        for (int parts = p.parts; share(parts) > kLookUp; ++parts) {
+            const long long cost = (r.tokens * (long long)parts + at_once - 1) / at_once * (kLookUp + share(parts));
+            if (best == 0 || cost < best) {
+                best = cost;
+                p.parts = parts;
+            }
+        }
+    }
     const dim3 grid((unsigned)((r.tokens + kThreads / 32 - 1) / (kThreads / 32)), (unsigned)p.parts);
     const cudaError_t e = launch_dependent(kern, grid, dim3(kThreads), 0, stream, p);
     return e == cudaSuccess ? CS_OK : cuda_fail(e, "rope_append_kernel launch");

@@ -120,7 +120,7 @@ def test_many_requests():
     check([(3 * b) % 4 for b in range(1300)], [b % 19 for b in range(1300)], 2, 1, 8)
 
 
-@pytest.mark.parametrize("hq,hkv", [(128, 8), (64, 3), (12, 4)])
+@pytest.mark.parametrize("hq,hkv", [(128, 8), (63, 3), (12, 4)])
 def test_heads_spread_over_warps(hq, hkv):
     check([300, 0, 1, 249], [3, 9, 100, 0], hq, hkv, 16, norm=True)
 
