@@ -28,12 +28,13 @@
 // Every wait on a barrier is bounded; one that gives up sets the status word.
 //
 // What bounds it: a tile of 256 rows and 128 keys takes 2900 cycles, of which its products
-// are 2048 (the case above: 1170-1245 us, 1545-1645 TFLOP/s); single tokens over long
+// are 2048 (the case above: 1150-1210 us, 1590-1670 TFLOP/s); single tokens over long
 // contexts the memory (128 requests, contexts to 8192: 366-371 us, 6.6 TB/s); short calls
-// their start (5 us to the first tile) and 2.5 us a block.
+// their start (5 us to the first tile), 4.2 us a block, and how even the ranges are.
 #include <cudaTypedefs.h>
 #include <math.h>
 
+#include <algorithm>
 #include <atomic>
 
 #include "cs_internal.h"
@@ -53,9 +54,17 @@ constexpr int kTileBytes = kKeys * kD * 2;
 constexpr int kQBytes = kRows * kD * 2;
 constexpr int kSmem = kQBytes + kStages * kTileBytes;
 constexpr int kSmallQRows = 32;                    // blocks of few rows bring in no more than these
-constexpr int kBeginKeys = 208;                    // what beginning and ending a block costs, in keys
-constexpr int kCutKeys = 384, kCutRow = 2;         // a range's end moves by so many keys, and so many a row, to a block's
-constexpr int kLeast = 128, kLeastRow = 2;         // a CTA's share where blocks are few: so many keys, and so many a row
+// What beginning and ending a block costs, in keys (pieces of 256 rows took 4.2 us and 1.45
+// a tile; 208 instead: 8192 tokens 372 us, 360 so).
+constexpr int kBeginKeys = 288;
+// A range's end moves by so many keys, and so many a row, to a block's beginning or end;
+// contexts of up to kUncut keys are not cut.  A cut costs its two CTAs 4 and 7 us for 252
+// rows.  (24 requests, four of 301-512 new tokens: 90 us; with 384 and 2 a row either way
+// 94, without moves 91 but 777 tokens 23 for 17.  One token over 1023, 4095 keys: 11.5 and
+// 15.4 us; with 400 to the end too 14.9 and 18.2; 512 keys in pieces 11.3, 9.3 whole.)
+constexpr int kCutKeys = 400, kCutBack = 128, kCutRow = 1, kUncut = 640;
+static_assert(kCutKeys + kCutRow >= kBeginKeys + kKeys / 2 && kCutBack >= kKeys / 2, "every piece of a cut block has a tile");
+constexpr int kLeast = 192, kLeastRow = 2;         // a CTA's share where blocks are few: so many keys, and so many a row
 constexpr int kMaxBatch = 1024;                    // requests of a launch
 constexpr float kMostSum = 0x1p-56f;               // 2^8 times 2^-kPShift
 
@@ -78,6 +87,7 @@ struct ChunkParams {
     int small_tokens;          // ... of the small query box
     int rows;                  // rows of a slot
     bool join_here;            // the last to come joins a block's pieces
+    int cut_back;              // see moved()
     int least;                 // of a CTA's share, 0: whatever it is
     HostDivisor by_block, by_grid;   // quotients by block_tokens, by the grid
     float scale_log2;
@@ -129,10 +139,11 @@ __device__ __forceinline__ int tile_at(int x, int keys) {
 }
 
 // Where a range's end at place x of a block's weight w moves: to an end of the block that
-// is near.  (A cut block's pieces but one are written and read again in fp32; and rows are
-// what that costs.)
-__device__ __forceinline__ int moved(int x, int w, int rows) {
-    return min(x, w - x) > kCutKeys + kCutRow * rows ? x : 2 * x <= w ? 0 : w;
+// is near.  (A cut block's pieces but one are written and read again in fp32, and rows are
+// what that costs.  In front a block's beginning counts too.)
+__device__ __forceinline__ int moved(int x, int w, int rows, int back) {
+    const bool early = x <= kCutKeys + kCutRow * rows, late = w - x <= back + kCutRow * rows;
+    return early && (!late || 2 * x <= w) ? 0 : late ? w : x;
 }
 
 // The ends of the ranges inside one block: its beginning in the whole weight, its weight
@@ -141,11 +152,11 @@ template <typename W>
 struct Cuts {
     W x0, each;
     int w, rows;
-    int over, ctas;
+    int over, ctas, back;
     // where CTA c's range begins in the block (0, w: in front of it, behind it)
     __device__ __forceinline__ int begin_of(int c) const {
         const W x = each * c + min(c, over);
-        return x <= x0 ? 0 : x - x0 >= (W)w ? w : moved((int)(x - x0), w, rows);
+        return x <= x0 ? 0 : x - x0 >= (W)w ? w : moved((int)(x - x0), w, rows, back);
     }
     // the CTA that the block begins in
     __device__ __forceinline__ int first() const {
@@ -334,6 +345,17 @@ __device__ __forceinline__ float rcp(float x) {
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
+// Of a count that CTAs hand on what they wrote by
+__device__ __forceinline__ int load_acquire(const int* p) {
+    int x;
+    asm volatile("ld.acquire.gpu.global.s32 %0, [%1];" : "=r"(x) : "l"(p) : "memory");
+    return x;
+}
+__device__ __forceinline__ int add_acq_rel(int* p, int n) {
+    int x;
+    asm volatile("atom.add.acq_rel.gpu.global.s32 %0, [%1], %2;" : "=r"(x) : "l"(p), "r"(n) : "memory");
+    return x;
+}
 // 32 bytes at once
 __device__ __forceinline__ void store32(void* p, const uint32_t (&r)[8]) {
     asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]),
@@ -517,7 +539,7 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_c
                 const W front_ = blocks.before(own.i);
                 own.off = (int)(x - front_);
                 const int keys = max(0, own.L - own.n + min(own.n, (own.i + 1) * p.block_tokens));
-                const int to = moved(own.off, keys + kBeginKeys, p.G * min(own.n - own.i * p.block_tokens, p.block_tokens));
+                const int to = moved(own.off, keys + kBeginKeys, p.G * min(own.n - own.i * p.block_tokens, p.block_tokens), p.cut_back);
                 s_move[looks_for_end] = to - own.off;
                 own.off = to;
                 if (!looks_for_end) s_begin = own;
@@ -822,13 +844,12 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_c
             const bool begins = pc.off == 0;   // (then it is the last piece of the CTA's range, else the first)
             const int mine = 2 * blockIdx.x + begins;
             const W x0 = begins ? s_lo + s_each + ((int)blockIdx.x < s_over) + s_move[1] - pc.end : s_lo + s_move[0] - pc.off;
-            const Cuts<W> cuts{x0, s_each, pc.keys + kBeginKeys, pc.tokens * p.G, s_over, (int)gridDim.x};
+            const Cuts<W> cuts{x0, s_each, pc.keys + kBeginKeys, pc.tokens * p.G, s_over, (int)gridDim.x, p.cut_back};
             const int first_cta = begins ? (int)blockIdx.x : cuts.first();
             bool join = false;
             if (p.join_here) {
                 if (threadIdx.x == kFirstSoftmax * 32) {
-                    s_join[begins] = __ldcg(p.done + first_cta) + pc.t1 - pc.t0 == pc.tiles;
-                    __threadfence();
+                    s_join[begins] = load_acquire(p.done + first_cta) + pc.t1 - pc.t0 == pc.tiles;
                 }
                 all_sync();
                 join = s_join[begins];
@@ -846,6 +867,9 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_c
                     const float top = m ? m_run[1] : m_run[0];
                     const float inv = l > 0.f ? rcp(l) : 0.f;
                     const int row = m * kHalf + lane0 + (lane & 15), token_ = m ? token[1] : token[0];
+                    // pieces that this kernel joins: as the threads hold them, 16 rows and 64
+                    // dims a warp, [4 dims][thread]
+                    const size_t held = (size_t)(row >> 4) * (16 * kD) + (sw >> 3) * (8 * kD) + lane * 4;
                     const float2 ml = make_float2(top == kNegInf ? kNegInf : top * c, l);
 #pragma unroll 1
                     for (int q = 0; q < 2; ++q) {   // 16 dims
@@ -870,13 +894,13 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_c
                                 if (!there) continue;
                                 const int slot = 2 * cta + (cta == first_cta);
                                 const size_t at_row = (size_t)slot * p.rows + row;
-                                const float* from = p.part_o + at_row * kD + part * 32 + q * 16;
+                                const float* from = p.part_o + (size_t)slot * p.rows * kD + held + q * 512;
                                 const float2 z = slot == mine ? ml : __ldcg(p.part_ml + at_row);
                                 float4 v[4];
 #pragma unroll
                                 for (int j = 0; j < 4; ++j) {
                                     v[j] = make_float4(o[4 * j], o[4 * j + 1], o[4 * j + 2], o[4 * j + 3]);
-                                    if (slot != mine) v[j] = __ldcg(reinterpret_cast<const float4*>(from) + j);
+                                    if (slot != mine) v[j] = __ldcg(reinterpret_cast<const float4*>(from + j * 128));
                                 }
                                 const float most = fmaxf(all.x, z.x);
                                 const float f = most == kNegInf ? 0.f : ex2(all.x - most);
@@ -901,6 +925,14 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_c
                             store32(p.out + out_at + ((size_t)token_ * (p.Hq - p.G) + row) * kD + q * 16, r);
                         } else {
                             const size_t at_row = (size_t)mine * p.rows + row;
+                            if (p.join_here) {
+                                float* to = p.part_o + (size_t)mine * p.rows * kD + held + q * 512;
+#pragma unroll
+                                for (int j = 0; j < 4; ++j)
+                                    __stcg(reinterpret_cast<float4*>(to + j * 128), make_float4(o[4 * j], o[4 * j + 1], o[4 * j + 2], o[4 * j + 3]));
+                                if (part == 0 && q == 0) p.part_ml[at_row] = ml;
+                                continue;
+                            }
 #pragma unroll
                             for (int j = 0; j < 2; ++j) {
 #pragma unroll
@@ -912,12 +944,9 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_c
                     }
                 }
                 if (join || again || !p.join_here) break;
-                __threadfence();
-                all_sync();
-                if (threadIdx.x == kFirstSoftmax * 32) {
-                    s_join[begins] = atomicAdd(p.done + first_cta, pc.t1 - pc.t0) + pc.t1 - pc.t0 == pc.tiles;
-                    __threadfence();
-                }
+                all_sync();   // (with which the piece is the thread's to hand on)
+                if (threadIdx.x == kFirstSoftmax * 32)
+                    s_join[begins] = add_acq_rel(p.done + first_cta, pc.t1 - pc.t0) + pc.t1 - pc.t0 == pc.tiles;
                 all_sync();
                 join = s_join[begins];
                 if (!join) break;
@@ -1068,7 +1097,7 @@ size_t align_up(size_t x) { return (x + 255) / 256 * 256; }
 Layout layout(const cs_attn_dims& d, int tokens, int grid) {
     Layout l;
     const long long all = (long long)tokens * (d.n_q_heads / d.n_kv_heads);
-    l.rows = all < kRows ? (int)all : kRows;
+    l.rows = all < kRows ? ((int)all + 15) / 16 * 16 : kRows;   // (a warp's, whole)
     l.done = 256;
     l.slots = align_up(l.done + sizeof(int) * grid);
     l.ml = align_up(l.slots + sizeof(int4) * 2 * grid);
@@ -1139,8 +1168,10 @@ cs_status launch_chunk_attention(const cs_attn_dims& d, const void* q, int64_t q
     // has many pieces, and joining them is work for the whole card.
     const long long by_tokens = (tokens + p.block_tokens - 1) / p.block_tokens;
     // (Nor is there anything to join where no context is long enough for a cut.)
-    const bool uncut = p.batch.max_keys + kBeginKeys <= 2 * (kCutKeys + kCutRow * p.G);
+    const bool uncut = p.batch.max_keys <= kUncut;
+    p.cut_back = uncut ? 1 << 30 : kCutBack;
     p.join_here = uncut || kJoinBlocks * p.Hkv * (by_tokens > d.batch ? by_tokens : d.batch < tokens ? d.batch : tokens) >= grid;
+    if (!p.join_here) p.rows = (int)std::min((long long)kRows, (long long)tokens * p.G);
     p.least = p.join_here ? 0 : kLeast + kLeastRow * p.rows;
     for (p.b0 = 0; p.b0 < d.batch; p.b0 += kMaxBatch) {
         p.nb = d.batch - p.b0 < kMaxBatch ? d.batch - p.b0 : kMaxBatch;
