@@ -114,6 +114,17 @@ def test_blocks_cut_between_ctas(ns, before, hq, hkv):
         assert torch.equal(binding.cs_chunk_attention(*args), out)
 
 
+@pytest.mark.parametrize("n", [1, 3, 70])
+@pytest.mark.parametrize("L", [544, 639, 640, 641, 657, 720, 817, 832, 833, 960, 1100, 1301])
+def test_few_blocks_of_lengths_that_are_just_cut(L, n):
+    check(batch([n], [L - n], 8, 2, 16, seed=L + n, spare=0))
+
+
+def test_one_context_of_many_pieces_beside_many_short_ones():
+    ns = [1] * 40 + [2] + [1] * 39
+    check(batch(ns, [63 + b for b in range(40)] + [20001] + [63] * 39, 4, 1, 64, seed=7))
+
+
 def test_a_page_table_of_many_columns():
     """The schedule's weights in 64 bits, where a call's might not fit 32: the same results."""
     for ns, before in (([1, 300, 7, 0, 1, 64, 1, 2] * 2, [5000, 20, 900, 3, 1, 0, 16000, 300] * 2), ([300, 1], [9000, 20000])):
