@@ -224,6 +224,8 @@ struct Pieces {
 };
 
 // ------------------------------------------------------------- tensor memory
+// All of these are a whole warp's at once: after threads went ways of their own, and after
+// a barrier.cta (which does not bring a warp together), __syncwarp() comes first.
 // 16 lanes, twice: threads 0-15 have lanes l .. l+15 of the address at its columns,
 // threads 16-31 the same lanes kSplit columns on (32 or 16 columns a thread).
 template <int kSplit>
@@ -764,6 +766,7 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_c
                                 l_run[m] *= alpha;
                                 if (t != pc.t0) {
                                     // P V of the tile before is complete (see above)
+                                    __syncwarp();
 #pragma unroll 1
                                     for (int q = 0; q < 2; ++q) {
                                         uint32_t o[16];
@@ -791,6 +794,7 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_c
                             need = !(sum <= kMostSum) || m_run[m] == kNegInf;
                             if (find || !pair_any(pair, need)) break;
                         }
+                        __syncwarp();
                         tmem_st16<16>(t_s + (sw >> 3) * 32, w);
                         l_run[m] += sum;
                         if (t + 1 == pc.t1) {
@@ -799,6 +803,7 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_c
                             const float l = l_run[m] + __shfl_xor_sync(0xffffffffu, l_run[m], 16);
                             if (lane < 16) s_row[m][sw][lane] = l;
                             l_run[m] = l;
+                            __syncwarp();
                         }
                         tmem_st_done();
                     }
@@ -874,72 +879,73 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_c
 #pragma unroll 1
                     for (int q = 0; q < 2; ++q) {   // 16 dims
                         uint32_t w[16];
+                        __syncwarp();
                         tmem_ld16<32>(t_row + 256 + m * 128 + (sw >> 3) * 64 + q * 16, w);
                         tmem_ld_done(w);
-                        if (token_ >= pc.tokens) continue;
-                        float o[16];
+                        if (token_ < pc.tokens) {
+                            float o[16];
 #pragma unroll
-                        for (int e = 0; e < 16; ++e) o[e] = __uint_as_float(w[e]) * inv;
-                        if (join) {
-                            float sum[16];
-                            float2 all = make_float2(kNegInf, 0.f);
+                            for (int e = 0; e < 16; ++e) o[e] = __uint_as_float(w[e]) * inv;
+                            if (join) {
+                                float sum[16];
+                                float2 all = make_float2(kNegInf, 0.f);
 #pragma unroll
-                            for (int e = 0; e < 16; ++e) sum[e] = 0.f;
-                            int x = 0;
+                                for (int e = 0; e < 16; ++e) sum[e] = 0.f;
+                                int x = 0;
 #pragma unroll 1
-                            for (int cta = first_cta; x < cuts.w && cta < cuts.ctas; ++cta) {
-                                const int y = cuts.begin_of(cta + 1);
-                                const bool there = tile_at(x, pc.keys) < tile_at(y, pc.keys);
-                                x = y;
-                                if (!there) continue;
-                                const int slot = 2 * cta + (cta == first_cta);
-                                const size_t at_row = (size_t)slot * p.rows + row;
-                                const float* from = p.part_o + (size_t)slot * p.rows * kD + held + q * 512;
-                                const float2 z = slot == mine ? ml : __ldcg(p.part_ml + at_row);
-                                float4 v[4];
+                                for (int cta = first_cta; x < cuts.w && cta < cuts.ctas; ++cta) {
+                                    const int y = cuts.begin_of(cta + 1);
+                                    const bool there = tile_at(x, pc.keys) < tile_at(y, pc.keys);
+                                    x = y;
+                                    if (!there) continue;
+                                    const int slot = 2 * cta + (cta == first_cta);
+                                    const size_t at_row = (size_t)slot * p.rows + row;
+                                    const float* from = p.part_o + (size_t)slot * p.rows * kD + held + q * 512;
+                                    const float2 z = slot == mine ? ml : __ldcg(p.part_ml + at_row);
+                                    float4 v[4];
 #pragma unroll
-                                for (int j = 0; j < 4; ++j) {
-                                    v[j] = make_float4(o[4 * j], o[4 * j + 1], o[4 * j + 2], o[4 * j + 3]);
-                                    if (slot != mine) v[j] = __ldcg(reinterpret_cast<const float4*>(from + j * 128));
+                                    for (int j = 0; j < 4; ++j) {
+                                        v[j] = make_float4(o[4 * j], o[4 * j + 1], o[4 * j + 2], o[4 * j + 3]);
+                                        if (slot != mine) v[j] = __ldcg(reinterpret_cast<const float4*>(from + j * 128));
+                                    }
+                                    const float most = fmaxf(all.x, z.x);
+                                    const float f = most == kNegInf ? 0.f : ex2(all.x - most);
+                                    const float g = most == kNegInf ? 0.f : ex2(z.x - most) * z.y;
+                                    all = make_float2(most, all.y * f + g);
+#pragma unroll
+                                    for (int j = 0; j < 4; ++j) {
+                                        sum[4 * j] = fmaf(v[j].x, g, sum[4 * j] * f);
+                                        sum[4 * j + 1] = fmaf(v[j].y, g, sum[4 * j + 1] * f);
+                                        sum[4 * j + 2] = fmaf(v[j].z, g, sum[4 * j + 2] * f);
+                                        sum[4 * j + 3] = fmaf(v[j].w, g, sum[4 * j + 3] * f);
+                                    }
                                 }
-                                const float most = fmaxf(all.x, z.x);
-                                const float f = most == kNegInf ? 0.f : ex2(all.x - most);
-                                const float g = most == kNegInf ? 0.f : ex2(z.x - most) * z.y;
-                                all = make_float2(most, all.y * f + g);
+                                const float r = all.y > 0.f ? rcp(all.y) : 0.f;
 #pragma unroll
-                                for (int j = 0; j < 4; ++j) {
-                                    sum[4 * j] = fmaf(v[j].x, g, sum[4 * j] * f);
-                                    sum[4 * j + 1] = fmaf(v[j].y, g, sum[4 * j + 1] * f);
-                                    sum[4 * j + 2] = fmaf(v[j].z, g, sum[4 * j + 2] * f);
-                                    sum[4 * j + 3] = fmaf(v[j].w, g, sum[4 * j + 3] * f);
+                                for (int e = 0; e < 16; ++e) o[e] = sum[e] * r;
+                                uint32_t r8[8];
+#pragma unroll
+                                for (int e = 0; e < 8; ++e) r8[e] = pack_bf16x2(o[2 * e], o[2 * e + 1]);
+                                store32(p.out + out_at + ((size_t)token_ * (p.Hq - p.G) + row) * kD + q * 16, r8);
+                            } else {
+                                const size_t at_row = (size_t)mine * p.rows + row;
+                                if (p.join_here) {
+                                    float* to = p.part_o + (size_t)mine * p.rows * kD + held + q * 512;
+#pragma unroll
+                                    for (int j = 0; j < 4; ++j)
+                                        __stcg(reinterpret_cast<float4*>(to + j * 128),
+                                               make_float4(o[4 * j], o[4 * j + 1], o[4 * j + 2], o[4 * j + 3]));
+                                } else {
+#pragma unroll
+                                    for (int j = 0; j < 2; ++j) {
+                                        uint32_t r8[8];
+#pragma unroll
+                                        for (int e = 0; e < 8; ++e) r8[e] = __float_as_uint(o[8 * j + e]);
+                                        store32(p.part_o + at_row * kD + part * 32 + q * 16 + j * 8, r8);
+                                    }
                                 }
-                            }
-                            const float r = all.y > 0.f ? rcp(all.y) : 0.f;
-#pragma unroll
-                            for (int e = 0; e < 16; ++e) o[e] = sum[e] * r;
-                        }
-                        uint32_t r[8];
-                        if (join) {
-#pragma unroll
-                            for (int e = 0; e < 8; ++e) r[e] = pack_bf16x2(o[2 * e], o[2 * e + 1]);
-                            store32(p.out + out_at + ((size_t)token_ * (p.Hq - p.G) + row) * kD + q * 16, r);
-                        } else {
-                            const size_t at_row = (size_t)mine * p.rows + row;
-                            if (p.join_here) {
-                                float* to = p.part_o + (size_t)mine * p.rows * kD + held + q * 512;
-#pragma unroll
-                                for (int j = 0; j < 4; ++j)
-                                    __stcg(reinterpret_cast<float4*>(to + j * 128), make_float4(o[4 * j], o[4 * j + 1], o[4 * j + 2], o[4 * j + 3]));
                                 if (part == 0 && q == 0) p.part_ml[at_row] = ml;
-                                continue;
                             }
-#pragma unroll
-                            for (int j = 0; j < 2; ++j) {
-#pragma unroll
-                                for (int e = 0; e < 8; ++e) r[e] = __float_as_uint(o[8 * j + e]);
-                                store32(p.part_o + at_row * kD + part * 32 + q * 16 + j * 8, r);
-                            }
-                            if (part == 0 && q == 0) p.part_ml[at_row] = ml;
                         }
                     }
                 }
@@ -962,8 +968,10 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_c
     fence_before();
     __syncthreads();
     fence_after();
-    if (warp == kMmaWarp)
+    if (warp == kMmaWarp) {
+        __syncwarp();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
+    }
 }
 
 // ------------------------------------------------------------------ the join

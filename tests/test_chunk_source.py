@@ -1,0 +1,44 @@
+"""Rules that the chunk attention kernel keeps, read in its source (no GPU)."""
+import pathlib
+import re
+
+import paper_2607_20507_gb300 as package
+
+SOURCE = pathlib.Path(package.__file__).parent / "csrc" / "chunk_attention.cu"
+
+ALIGNED = re.compile(r"\btmem_(ld32|ld16|st16|ld_done|st_done)\b|tcgen05\.(alloc|dealloc)")
+# what may leave the threads of a warp apart: a branch by lane or by row, and barriers of several warps (which bring
+# threads together, but not so that an aligned instruction may follow)
+PARTS = re.compile(r"if \(lane|if \(!?token|if \(threadIdx|\b(pair_sync|pair_any|all_sync|hide|mbar_wait_bounded)\(|__syncthreads\(\)|__shfl")
+TOGETHER = re.compile(r"__syncwarp\(\)|\bwait\(&bars")
+
+
+def kernel():
+    text = SOURCE.read_text()
+    body = text[text.index("chunk_attention_kernel(const"):text.index("// ---", text.index("tcgen05.dealloc"))]
+    return [re.sub(r"//.*", "", line) for line in body.split("\n")]
+
+
+def test_warps_are_together_at_instructions_of_whole_warps():
+    """tcgen05.ld, st, wait, alloc and dealloc are .sync.aligned: all threads of the warp execute the same one.  In the
+    order of the source, nothing that may leave a warp's threads apart stands between them and the last __syncwarp (wait()
+    ends with one)."""
+    apart, seen = False, 0
+    for line in kernel():
+        if TOGETHER.search(line):
+            apart = False
+        if ALIGNED.search(line):
+            seen += 1
+            assert not apart, line.strip()
+        if PARTS.search(line):
+            apart = True
+    assert seen >= 12
+
+
+def test_no_thread_leaves_a_round_that_ends_with_such_an_instruction():
+    """Inside the loops over a piece's dims a thread without a row passes over its stores; it does not go on by itself."""
+    text = "\n".join(kernel())
+    assert not re.search(r"if \((token|lane)[^\n]*\)\s*(continue|break);", text)
+    end = text[text.index("for (int again = 0;;"):]
+    loop = end[end.index("for (int q = 0; q < 2; ++q)"):]
+    assert re.match(r"[^;]*;[^;]*;[^;]*;\s*__syncwarp\(\);\s*tmem_ld16", loop)
