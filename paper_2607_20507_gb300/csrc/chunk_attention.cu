@@ -359,10 +359,21 @@ __device__ __forceinline__ int add_acq_rel(int* p, int n) {
     return x;
 }
 // 32 bytes at once
-__device__ __forceinline__ void store32(void* p, const uint32_t (&r)[8]) {
+__device__ __forceinline__ void store32(float* p, const uint32_t (&r)[8]) {
     asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]),
                  "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
                  : "memory");
+}
+// 32 bytes of an output, which is aligned to 16; kWide: to 32.  (8 prompts, 32 heads each: 111.0
+// us at once, 114.5 as two stores, each half a sector; by a branch in the kernel 112.6.)
+template <bool kWide>
+__device__ __forceinline__ void store_out(__nv_bfloat16* p, const uint32_t (&r)[8]) {
+    if constexpr (kWide) {
+        store32(reinterpret_cast<float*>(p), r);
+    } else {
+        reinterpret_cast<uint4*>(p)[0] = make_uint4(r[0], r[1], r[2], r[3]);
+        reinterpret_cast<uint4*>(p)[1] = make_uint4(r[4], r[5], r[6], r[7]);
+    }
 }
 
 // (one lane)
@@ -410,7 +421,8 @@ __device__ __forceinline__ void wait(uint64_t* bar, uint32_t parity, volatile in
     __syncwarp();
 }
 
-template <typename W>
+// kWide: out is aligned to 32 bytes
+template <typename W, bool kWide>
 __global__ void __launch_bounds__(kThreads, 1)
 chunk_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
                        const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_q_small,
@@ -720,7 +732,7 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_c
                 for (int m = 0; m < 2; ++m)
                     if (token[m] < pc.tokens)
                         for (int j = 0; j < 2; ++j)
-                            store32(p.out + out_at + ((size_t)token[m] * p.Hq + head[m]) * kD + j * 16, zero);
+                            store_out<kWide>(p.out + out_at + ((size_t)token[m] * p.Hq + head[m]) * kD + j * 16, zero);
                 continue;
             }
             // the maximum that the weights go by, what takes a score to its weight's exponent,
@@ -833,7 +845,7 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_c
 #pragma unroll
                                 for (int e = 0; e < 8; ++e)
                                     r[e] = pack_bf16x2(o[16 * j + 2 * e] * inv, o[16 * j + 2 * e + 1] * inv);
-                                store32(dst + j * 16, r);
+                                store_out<kWide>(dst + j * 16, r);
                             }
                         }
                     }
@@ -926,7 +938,7 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_c
                                 uint32_t r8[8];
 #pragma unroll
                                 for (int e = 0; e < 8; ++e) r8[e] = pack_bf16x2(o[2 * e], o[2 * e + 1]);
-                                store32(p.out + out_at + ((size_t)token_ * (p.Hq - p.G) + row) * kD + q * 16, r8);
+                                store_out<kWide>(p.out + out_at + ((size_t)token_ * (p.Hq - p.G) + row) * kD + q * 16, r8);
                             } else {
                                 const size_t at_row = (size_t)mine * p.rows + row;
                                 if (p.join_here) {
@@ -1160,16 +1172,19 @@ cs_status launch_chunk_attention(const cs_attn_dims& d, const void* q, int64_t q
     // whether the weight of all blocks is sure to fit 32 bits
     const long long most_blocks = (tokens + p.block_tokens - 1) / p.block_tokens + (long long)d.batch;
     const bool wide = (p.batch.max_keys + (long long)kBeginKeys) * p.Hkv > 0x7fffffffLL / most_blocks;
-    auto kern = wide ? chunk_attention_kernel<uint64_t> : chunk_attention_kernel<uint32_t>;
+    const bool wide_out = reinterpret_cast<uintptr_t>(out) % 32 == 0;
+    auto kern = wide_out ? (wide ? chunk_attention_kernel<uint64_t, true> : chunk_attention_kernel<uint32_t, true>)
+                         : (wide ? chunk_attention_kernel<uint64_t, false> : chunk_attention_kernel<uint32_t, false>);
     {
-        static std::atomic<bool> done[2][64];
+        static std::atomic<bool> done[4][64];
+        const int which = 2 * wide_out + wide;
         int dev = 0;
         cudaError_t e = cudaGetDevice(&dev);
         if (e != cudaSuccess) return cuda_fail(e, "cudaGetDevice");
-        if (dev < 0 || dev >= 64 || !done[wide][dev]) {
+        if (dev < 0 || dev >= 64 || !done[which][dev]) {
             e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
             if (e != cudaSuccess) return cuda_fail(e, "cudaFuncSetAttribute(chunk_attention_kernel)");
-            if (dev >= 0 && dev < 64) done[wide][dev] = true;
+            if (dev >= 0 && dev < 64) done[which][dev] = true;
         }
     }
     // As many blocks as there may be (the lengths are the device's): with few of them each

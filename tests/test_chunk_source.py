@@ -42,3 +42,15 @@ def test_no_thread_leaves_a_round_that_ends_with_such_an_instruction():
     end = text[text.index("for (int again = 0;;"):]
     loop = end[end.index("for (int q = 0; q < 2; ++q)"):]
     assert re.match(r"[^;]*;[^;]*;[^;]*;\s*__syncwarp\(\);\s*tmem_ld16", loop)
+
+
+def test_wide_stores_go_where_32_byte_alignment_is_known():
+    """Stores of 32 bytes: to the workspace, which is aligned to 256, and to an output in the kernel for such outputs, which
+    the host takes by the address.  An output is promised 16."""
+    text = SOURCE.read_text()
+    assert len(re.findall(r"\.global\.v8\.", text)) == 1 and "void store32(float* p" in text
+    assert re.findall(r"\bstore32\((?!float\* p)([^,]+),", text) == [
+        "reinterpret_cast<float*>(p)", "p.part_o + at_row * kD + part * 32 + q * 16 + j * 8"]
+    assert re.search(r"if constexpr \(kWide\) \{\s*store32\(reinterpret_cast<float\*>\(p\)", text)
+    assert "wide_out = reinterpret_cast<uintptr_t>(out) % 32 == 0" in text
+    assert len(re.findall(r"\bstore_out<kWide>\(", text)) == 3
