@@ -594,10 +594,10 @@ cs_status cs_packed_verify_attention(const cs_attn_dims* dims, const void* q, co
  *              zero-fill it again.  Calls that share one must be ordered.
  * Slots from L_b on may hold any bits.  Keys and values in front of L_b have to be
  * finite: one that is not may reach every row of its request.
- * Arithmetic: q.K in bf16 with fp32 accumulation, the softmax in fp32, its weights
- * rounded to bf16 for the product with V, which is summed in fp32 (the sum that
- * divides it is that of the unrounded weights); scaled by 2^-64 on the way as in
- * cs_verify_attention, so that every finite V gives a finite output.
+ * Arithmetic: that of cs_verify_attention.  q.K in bf16 with fp32 accumulation, the
+ * softmax in fp32, its weights as two bf16 terms (about 16 bits) for the product with
+ * V, which is summed in fp32; scaled by 2^-64 on the way, so that every finite V gives
+ * a finite output.
  *
  * Return CS_ERR_INVALID_ARG (null pointer, misalignment, bad dimension, stride or
  * count), CS_ERR_UNSUPPORTED (head_dim != 128, page size, rot_dim, G > 128, a pool of

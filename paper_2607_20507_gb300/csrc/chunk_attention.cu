@@ -14,22 +14,29 @@
 //   warps 4-19      softmax, of query rows 0-127 and then 128-255 of a tile: a warp takes
 //                   16 rows and half of a tile's keys, two threads a row;
 //   warps 0, 3      issue the products of either: S = Q K^T (M 128, N 128 keys, 8 steps of 16
-//                   dims) and O += P V (N 128 dims, 8 steps of 16 keys), tcgen05 with
-//                   S, P (over S) and O in tensor memory: 2 x (128 + 128) columns;
+//                   dims) and O += P V (N 128 dims, 8 steps of 16 keys for either term of P),
+//                   tcgen05 with S, P (over S) and O in tensor memory: 2 x (128 + 128) columns;
 //   warp 1          brings K and V tiles (TMA, one box a page piece) into a ring of
 //                   five 32 KB stages;
 //   warp 2          brings a block's query rows (TMA).
 // The products of one half run while the softmax of the other does, and a half's S of
 // the next tile being complete says that P V of this one is too (a thread's products
 // complete in order), so O may be rescaled then.  The running maximum moves only for a
-// growth of more than 2^8.  Either query tile has an issuing warp of its own: the queue of
-// products is short, and what one warp does between its products showed (4096 tokens
-// over 12288, 64 / 8 heads: 1270 us with one, 1189 with two).
+// growth of more than 2^8.  P is the sum of two bf16 terms, as in verify attention: one alone
+// leaves 2e-3 + 1e-2 |out| in rows of few keys whose values cancel, and adds 1.5e-3 to an
+// output's error everywhere, where its own rounding is 1.7e-3 (2-norms).  The second term is
+// half as much again of products (4096 tokens over 12288, 64 / 8 heads: 1590-1620 us, 1190
+// without; prompts of 129 to 1024 tokens, 32 heads each: 128 and 111; single tokens over
+// contexts to 8192: 377-387 and 372).  Skipping it where every weight is small against its row's
+// sum so far gave 1335-1400 in the first of these, but 117 for 108 in mixed batches and 137 for
+// 128: what decides it stands between the scores and the weights.  Either query tile has an issuing warp of its own: the queue of
+// products is short, and what one warp does between its products showed (the first of these:
+// 1270 us with one, 1189 with two, before the second term).
 // Every wait on a barrier is bounded; one that gives up sets the status word.
 //
-// What bounds it: a tile of 256 rows and 128 keys takes 2900 cycles, of which its products
-// are 2048 (the case above: 1150-1210 us, 1590-1670 TFLOP/s); single tokens over long
-// contexts the memory (128 requests, contexts to 8192: 366-371 us, 6.6 TB/s); short calls
+// What bounds it: the products of a tile of 256 rows and 128 keys are 3072 cycles, and come at
+// 1.8 PFLOP/s (the first case above), what a library product has here; single tokens over
+// long contexts the memory (128 requests, contexts to 8192: 6.4 TB/s); short calls
 // their start (5 us to the first tile), 4.2 us a block, and how even the ranges are.
 #include <cudaTypedefs.h>
 #include <math.h>
@@ -66,7 +73,7 @@ constexpr int kCutKeys = 400, kCutBack = 128, kCutRow = 1, kUncut = 640;
 static_assert(kCutKeys + kCutRow >= kBeginKeys + kKeys / 2 && kCutBack >= kKeys / 2, "every piece of a cut block has a tile");
 constexpr int kLeast = 192, kLeastRow = 2;         // a CTA's share where blocks are few: so many keys, and so many a row
 constexpr int kMaxBatch = 1024;                    // requests of a launch
-constexpr float kMostSum = 0x1p-56f;               // 2^8 times 2^-kPShift
+constexpr float kMostOver = 8.f - kPShift;         // weights are at most 2^8 times 2^-kPShift
 
 struct ChunkParams {
     RaggedBatch batch;
@@ -686,8 +693,8 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_c
                     if (elect_one()) {
                         const uint64_t b = dv + (uint64_t)(sv * kTileBytes >> 4);
 #pragma unroll
-                        for (int s = 0; s < 8; ++s)
-                            tc_mma_ts(t_o, t_s + s * 8, b + s * (uint64_t)(4096 >> 4), id_o, t > pc.t0 || s > 0);
+                        for (int s = 0; s < 16; ++s)   // (16 keys' first terms, their second)
+                            tc_mma_ts(t_o, t_s + s * 8, b + (s >> 1) * (uint64_t)(4096 >> 4), id_o, t > pc.t0 || s > 0);
                         if (last) tc_commit(&bars.o_full[m]);
                         else scores(sk);
                         tc_commit(&bars.kv_empty[sv]);
@@ -707,9 +714,9 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_c
         // ------------------------------------------- softmax, four threads a row
         // Of these, warps w and w + 8 take lanes 32 (w % 4) + 16 (w / 4 % 2) .. of either half, the
         // first keys 0-63 of a tile, the second 64-127; threads i and i + 16 share a row,
-        // 32 keys each (and as many dims of O).  The two warps agree at a barrier of their
-        // own whether the weights stand, after which each may write over the other's scores
-        // (which that has read).
+        // 32 keys each (and as many dims of O).  A thread's weights lie over its own scores: of 16
+        // keys the first terms, then the second.  The two warps agree at a barrier of their own
+        // whether the maxima stand.
         const int sw = warp - kFirstSoftmax;
         const int part = (sw >> 3) * 2 + (lane >> 4);     // the thread's quarter of keys and dims
         const int lane0 = (sw & 3) * 32 + ((sw >> 2) & 1) * 16;
@@ -756,59 +763,55 @@ chunk_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_c
                         // keys that the row sees, from this thread's first one on
                         const int lim = pc.keys - (pc.tokens - 1 - min(token[m], pc.tokens - 1)) - t * kKeys - part * 32;
                         if (__builtin_expect(lim < 32, 0)) hide(s, lim);
-                        // The weights by the maximum so far.  A sum within 2^8 says that no score
-                        // passed it by more than 8; otherwise, and in a piece's first tile, the
-                        // row's maximum of the tile is found before the weights are taken.
-                        uint32_t w[16];
-                        float sum;
-                        bool need = true;   // (of this thread's row: the others' maxima stay)
+                        // The weights go by the maximum so far, unless a score of the pair's rows passes
+                        // it by more than 8 (in powers of two), or there is none yet.
+                        const float mh = top_of(s);
+                        const bool need = !(fmaf(mh, c, neg[m]) <= kMostOver) || m_run[m] == kNegInf;
+                        if (t == pc.t0 || pair_any(pair, need)) {
+                            const float own = need ? mh : kNegInf;   // (the others' maxima stay)
+                            const float mw = fmaxf(own, __shfl_xor_sync(0xffffffffu, own, 16));
+                            pair_sync(pair);   // (what was there has been read)
+                            if (lane < 16) s_row[1][sw][lane] = mw;
+                            pair_sync(pair);
+                            const float mt = fmaxf(m_run[m], fmaxf(mw, s_row[1][sw ^ 8][lane & 15]));
+                            pair_sync(pair);
+                            const float alpha = mt > m_run[m] ? ex2((m_run[m] - mt) * c) : 1.f;   // (0 where there was none)
+                            m_run[m] = mt;
+                            neg[m] = mt == kNegInf ? 0.f : -mt * c - kPShift;
+                            l_run[m] *= alpha;
+                            if (t != pc.t0) {
+                                // P V of the tile before is complete (see above)
+                                __syncwarp();
 #pragma unroll 1
-                        for (bool find = t == pc.t0;; find = true) {
-                            if (find) {
-                                const float mh = need ? top_of(s) : kNegInf;
-                                const float mw = fmaxf(mh, __shfl_xor_sync(0xffffffffu, mh, 16));
-                                pair_sync(pair);   // (what was there has been read)
-                                if (lane < 16) s_row[1][sw][lane] = mw;
-                                pair_sync(pair);
-                                const float mt = fmaxf(m_run[m], fmaxf(mw, s_row[1][sw ^ 8][lane & 15]));
-                                pair_sync(pair);
-                                const float alpha = mt > m_run[m] ? ex2((m_run[m] - mt) * c) : 1.f;   // (0 where there was none)
-                                m_run[m] = mt;
-                                neg[m] = mt == kNegInf ? 0.f : -mt * c - kPShift;
-                                l_run[m] *= alpha;
-                                if (t != pc.t0) {
-                                    // P V of the tile before is complete (see above)
-                                    __syncwarp();
-#pragma unroll 1
-                                    for (int q = 0; q < 2; ++q) {
-                                        uint32_t o[16];
-                                        tmem_ld16<32>(t_o + q * 16, o);
-                                        tmem_ld_done(o);
+                                for (int q = 0; q < 2; ++q) {
+                                    uint32_t o[16];
+                                    tmem_ld16<32>(t_o + q * 16, o);
+                                    tmem_ld_done(o);
 #pragma unroll
-                                        for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * alpha);
-                                        tmem_st16<32>(t_o + q * 16, o);
-                                    }
+                                    for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * alpha);
+                                    tmem_st16<32>(t_o + q * 16, o);
                                 }
                             }
-                            const uint64_t c2 = f2_pack(c, c), n2 = f2_pack(neg[m], neg[m]);
-                            uint64_t sums[2] = {0ull, 0ull};
+                        }
+                        const uint64_t c2 = f2_pack(c, c), n2 = f2_pack(neg[m], neg[m]);
+                        uint64_t sums[2] = {0ull, 0ull};
+                        __syncwarp();
 #pragma unroll
-                            for (int e = 0; e < 16; ++e) {
+                        for (int q = 0; q < 2; ++q) {   // 16 keys
+                            uint32_t w[16];
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) {
                                 float x0, x1;
-                                f2_unpack(f2_fma(f2_pack(s[2 * e], s[2 * e + 1]), c2, n2), x0, x1);
+                                f2_unpack(f2_fma(f2_pack(s[16 * q + 2 * e], s[16 * q + 2 * e + 1]), c2, n2), x0, x1);
                                 const float p0 = ex2(x0), p1 = ex2(x1);
                                 sums[e & 1] = f2_add(sums[e & 1], f2_pack(p0, p1));
-                                w[e] = pack_bf16x2(p0, p1);
+                                split_bf16x2(p0, p1, w[e], w[8 + e]);
                             }
-                            float a0, a1;
-                            f2_unpack(f2_add(sums[0], sums[1]), a0, a1);
-                            sum = a0 + a1;
-                            need = !(sum <= kMostSum) || m_run[m] == kNegInf;
-                            if (find || !pair_any(pair, need)) break;
+                            tmem_st16<32>(t_s + (sw >> 3) * 64 + q * 16, w);
                         }
-                        __syncwarp();
-                        tmem_st16<16>(t_s + (sw >> 3) * 32, w);
-                        l_run[m] += sum;
+                        float a0, a1;
+                        f2_unpack(f2_add(sums[0], sums[1]), a0, a1);
+                        l_run[m] += a0 + a1;
                         if (t + 1 == pc.t1) {
                             // the row's sum in this warp, for the other, which reads it when the
                             // last products are complete

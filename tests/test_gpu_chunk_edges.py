@@ -42,3 +42,46 @@ def test_arrays_aligned_to_16_bytes(ns, before, which):
         k, v = shifted(k), shifted(v)
     got = binding.cs_chunk_attention(q, k, v, table, lens, starts, out=out)
     assert got is out and torch.equal(got, expect)
+
+
+def fine(args):
+    """The framework's bound of attention outputs; and the output's rounding (half a step, 2^-8 of the value) with scores,
+    weights and sums in 16 bits and more: weights of two bf16 terms are off by at most 2^-16 of themselves, fp32 scores of
+    128 products by 128 * 2^-24 of some 10, sums of up to 4000 weights by a good deal less than 4000 * 2^-24: 2^-11
+    together.  (Weights of one bf16 term are off by up to 2^-8.)"""
+    out = binding.cs_chunk_attention(*args)
+    expect, size = ref.attention(*args)
+    off = (out.double() - expect).abs()
+    assert not (off > 2e-3 + 1e-2 * expect.abs()).any()
+    assert not (off > 1.01 * 2.0 ** -8 * expect.abs() + 2.0 ** -11 * size).any()
+
+
+@pytest.mark.parametrize("L", [1, 2, 3, 5, 9, 17, 33, 128, 129])
+@pytest.mark.parametrize("hq,hkv", [(8, 2), (32, 1)])
+def test_weights_of_few_keys_are_not_rounded_to_bf16(L, hq, hkv):
+    fine(batch([1] * 150, [L - 1] * 150, hq, hkv, 16, seed=L))
+
+
+def test_the_first_rows_of_prompts():
+    fine(batch([17, 40, 130, 9] * 12, [0] * 48, 16, 4, 16, seed=5))
+
+
+@pytest.mark.parametrize("ns,before", [WHOLE, BY_KERNEL, BY_LAST, ([1] * 60 + [90], [500] * 60 + [3500])])
+def test_weights_of_longer_contexts_and_of_cut_blocks(ns, before):
+    fine(batch(ns, before, 16, 4, 16, seed=9, junk=False))
+
+
+@pytest.mark.parametrize("heavy", [2, 3, 7])
+@pytest.mark.parametrize("growing", [False, True])
+def test_a_few_keys_that_outweigh_the_others(heavy, growing):
+    """Scores of a few keys anywhere in a long context stand 16 above the others', all alike or each above the last."""
+    ns, before = [1, 200, 3], [5000, 1200, 2600]
+    q, k, v, table, lens, starts = batch(ns, before, 8, 2, 16, seed=heavy, junk=False)
+    q[:, :, 0] = 16.0
+    k[..., 0] = 0.0
+    gen = torch.Generator().manual_seed(heavy)
+    for b, L in enumerate(lens.tolist()):
+        for i, j in enumerate(sorted(torch.randperm(before[b], generator=gen)[:heavy].tolist())):
+            # 16 * 11.25 / sqrt(128) = 15.9; growing: a step of 0.5 is 0.7 of a score
+            k[table[b, j // 16], :, j % 16, 0] = 11.25 + (0.5 * i if growing else 0)
+    fine((q, k, v, table, lens, starts))
