@@ -1027,7 +1027,9 @@ __global__ void __launch_bounds__(kJoinThreads, 16) chunk_join_kernel(const Chun
 #pragma unroll
             for (int d = 16; d > 0; d /= 2) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, d));
             most = fmaxf(most, top);
-            if (most == kNegInf) continue;
+            // (no score of these is a number, or there is none; NaN scores leave a NaN sum and
+            // outputs, which are the result)
+            if (most == kNegInf && !__any_sync(0xffffffffu, ml.y != 0.f)) continue;
             // (outputs are divided by their sums already)
             float w = ml.y * ex2(ml.x - most), sum = w;
 #pragma unroll

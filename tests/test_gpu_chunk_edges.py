@@ -85,3 +85,21 @@ def test_a_few_keys_that_outweigh_the_others(heavy, growing):
             # 16 * 11.25 / sqrt(128) = 15.9; growing: a step of 0.5 is 0.7 of a score
             k[table[b, j // 16], :, j % 16, 0] = 11.25 + (0.5 * i if growing else 0)
     fine((q, k, v, table, lens, starts))
+
+
+@pytest.mark.parametrize("ns,before", [WHOLE, BY_KERNEL, BY_LAST])
+@pytest.mark.parametrize("bad", [math.nan, math.inf])
+def test_rows_that_are_not_finite_stay_so_and_alone(ns, before, bad):
+    """In whole blocks and in either join: one entry of a few query rows is NaN, or infinite (scores of both signs)."""
+    q, k, v, table, lens, starts = batch(ns, before, 16, 4, 16, seed=3, junk=False)
+    clean = binding.cs_chunk_attention(q, k, v, table, lens, starts)
+    hit = torch.zeros(clean.shape[:2], dtype=torch.bool, device=DEV)
+    for b, n in enumerate(ns):
+        if n:
+            hit[int(starts[b]) + n // 2, (5 * b + 3) % 16] = True
+            hit[int(starts[b]) + n - 1, 15] = True
+    q = q.contiguous()
+    q[..., 7][hit] = bad
+    got = binding.cs_chunk_attention(q, k, v, table, lens, starts)
+    assert torch.equal(got[~hit], clean[~hit])
+    assert torch.isnan(got[hit]).all()
