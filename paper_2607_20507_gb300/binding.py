@@ -292,6 +292,7 @@ def attn_dims(q: torch.Tensor, k_pages: torch.Tensor, page_table: torch.Tensor,
 # process's life (a captured graph holds their addresses).
 _workspaces: dict = {}
 _WITH_STATUS = ("attn", "tree_attn", "route", "chunk_attn")   # whose first word has to start at zero
+_WITH_COUNTS = ("chunk_attn",)                                # and words that results depend on
 
 
 def _made_on(stream: int, device):
@@ -317,15 +318,18 @@ def _workspace_of(kind: str, device, n: int, stream: int | None = None):
     ws = _workspaces.get(key)
     if ws is not None:
         return ws, True
-    if kind in _WITH_STATUS and stream == here and device.type == "cuda" and torch.cuda.is_current_stream_capturing():
-        # a zero fill would become a part of the graph, so a captured call takes
-        # the workspace of the calls before the capture (with whose stream the
-        # graph's replays have to be ordered)
-        for (k, d, _, m), ws in list(_workspaces.items()):
-            if (k, d, m) == (kind, device, n):
-                return ws, False
     with _made_on(stream, device):
+        captured = kind in _WITH_STATUS and device.type == "cuda" and torch.cuda.is_current_stream_capturing()
+        if captured:
+            # a zero fill would become a part of the graph, so a captured call takes
+            # the workspace of the calls before the capture (with whose stream the
+            # graph's replays have to be ordered)
+            for (k, d, _, m), ws in list(_workspaces.items()):
+                if (k, d, m) == (kind, device, n):
+                    return ws, False
         ws = (torch.zeros if kind in _WITH_STATUS else torch.empty)(max(n, 256), dtype=torch.uint8, device=device)
+    if captured and kind in _WITH_COUNTS:
+        return ws, False   # the fill is the graph's: for nobody else is this memory zero
     return _workspaces.setdefault(key, ws), True
 
 
@@ -920,11 +924,16 @@ def chunk_attn_dims(q: torch.Tensor, k_pages: torch.Tensor, page_table: torch.Te
     return AttnDims(page_table.shape[0], q.shape[1], Hkv, D, ps, page_table.shape[1], P, float(sm_scale))
 
 
+def _chunk_workspace_bytes(lib, d: AttnDims, tokens: int) -> int:
+    """Of the default workspace: what 256 tokens need, which is what all larger calls do, so that a stream has one
+    for whatever calls, and one call before a capture has made it for all calls in it."""
+    return max(lib.cs_chunk_attention_workspace_bytes(ctypes.byref(d), t) for t in (tokens, 256))
+
+
 def chunk_attention_workspace(dims: AttnDims, tokens: int, device, stream: int | None = None) -> torch.Tensor:
-    """The default workspace of the (current) stream's calls of cs_chunk_attention with these dims: after one,
-    cs_read_device_status of it tells whether it finished normally."""
-    n = load_library().cs_chunk_attention_workspace_bytes(ctypes.byref(dims), int(tokens))
-    return _cached_workspace("chunk_attn", device, n, stream)
+    """The default workspace of the (current) stream's calls of cs_chunk_attention: after one, cs_read_device_status of
+    it tells whether it finished normally."""
+    return _cached_workspace("chunk_attn", device, _chunk_workspace_bytes(load_library(), dims, int(tokens)), stream)
 
 
 def cs_chunk_attention(q, k_pages, v_pages, page_table, ctx_lens, q_starts=None, out=None, workspace=None,
@@ -954,8 +963,7 @@ def cs_chunk_attention(q, k_pages, v_pages, page_table, ctx_lens, q_starts=None,
     T = q.shape[0]
     with torch.cuda.device(dev):
         if workspace is None:
-            n = lib.cs_chunk_attention_workspace_bytes(ctypes.byref(d), int(T))
-            workspace = _cached_workspace("chunk_attn", dev, n, stream)
+            workspace = _cached_workspace("chunk_attn", dev, _chunk_workspace_bytes(lib, d, int(T)), stream)
         st = lib.cs_chunk_attention(ctypes.byref(d), q.data_ptr(), q_stride, int(T), k_pages.data_ptr(),
                                     v_pages.data_ptr(), page_table.data_ptr(), ctx_lens.data_ptr(), _ptr(q_starts),
                                     out.data_ptr(), workspace.data_ptr(), workspace.nbytes,

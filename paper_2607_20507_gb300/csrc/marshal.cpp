@@ -18,6 +18,7 @@
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <algorithm>
 #include <map>
 #include <tuple>
 
@@ -734,7 +735,8 @@ CALL(chunk_attention, 10)
                          (int32_t)k->size(2), (int32_t)table->size(1), (int32_t)k->size(0), scale};
     const c10::cuda::CUDAGuard guard(dev);
     Scratch ws;
-    const size_t bytes = a[7] == Py_None ? cs_chunk_attention_workspace_bytes(&d, T) : 0;
+    // (binding.py's size, the same for whatever calls)
+    const size_t bytes = a[7] == Py_None ? std::max(cs_chunk_attention_workspace_bytes(&d, T), cs_chunk_attention_workspace_bytes(&d, 256)) : 0;
     if (!workspace(a[7], kChunkAttn, dev, bytes, s, &ws)) Py_RETURN_NONE;
     at::Tensor out;
     const cs_status st = launch([&] {

@@ -1,5 +1,8 @@
 """Chunk attention where it can go wrong: alignment, rows that are not finite, few keys, workspaces of captured calls."""
 import math
+import pathlib
+import subprocess
+import sys
 
 import pytest
 import torch
@@ -103,3 +106,90 @@ def test_rows_that_are_not_finite_stay_so_and_alone(ns, before, bad):
     got = binding.cs_chunk_attention(q, k, v, table, lens, starts)
     assert torch.equal(got[~hit], clean[~hit])
     assert torch.isnan(got[hit]).all()
+
+
+def own_workspace(args):
+    dims = binding.chunk_attn_dims(args[0], args[1], args[3])
+    n = binding.load_library().cs_chunk_attention_workspace_bytes(dims, args[0].shape[0])
+    return torch.zeros((n,), dtype=torch.uint8, device=DEV)
+
+
+def test_one_default_workspace_for_whatever_calls():
+    sizes = [([1], [20], 8, 1), ([3, 1], [20, 5], 28, 4), ([300, 7], [0, 100], 32, 32), ([1] * 40, [9] * 40, 64, 8)]
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        all_ = [batch(ns, before, hq, hkv, 16) for ns, before, hq, hkv in sizes]
+        got = {binding.chunk_attention_workspace(binding.chunk_attn_dims(a[0], a[1], a[3]), a[0].shape[0], DEV).data_ptr()
+               for a in all_}
+        held = sum(k[0] == "chunk_attn" and k[2] == side.cuda_stream for k in binding._workspaces)
+        for a in all_:
+            check(a)
+        assert len(got) == 1
+        assert sum(k[0] == "chunk_attn" and k[2] == side.cuda_stream for k in binding._workspaces) == held == 1
+    side.synchronize()
+
+
+def test_graphs_of_other_token_counts_after_one_call():
+    """Captured after one call of another size, with no fill in the graphs, and replayed in the other order."""
+    x = [batch(ns, before, 16, 4, 16, seed=i, junk=False) for i, (ns, before) in enumerate((
+        ([1] * 90, [3000 + 37 * b for b in range(90)]), ([1] * 60, [5000] * 60), ([300] * 12, [2000] * 12)))]
+    expect = [binding.cs_chunk_attention(*a, workspace=own_workspace(a)) for a in x]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        binding.cs_chunk_attention(*x[0])
+    graphs, outs = [], [torch.full_like(e, 3.0) for e in expect]
+    before = {k: v.data_ptr() for k, v in binding._workspaces.items()}
+    for a, out in zip(x[1:], outs[1:]):
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1], stream=side):
+            binding.cs_chunk_attention(*a, out=out)
+    assert {k: v.data_ptr() for k, v in binding._workspaces.items()} == before
+    for i in (1, 0, 1, 0):
+        outs[i + 1].fill_(3.0)
+        torch.cuda.synchronize()
+        graphs[i].replay()
+        torch.cuda.synchronize()
+        assert torch.equal(outs[i + 1], expect[i + 1])
+
+
+ALONE = """
+import sys
+sys.path[:0] = ["tests"]
+import torch
+from test_gpu_chunk_edges import BY_LAST, DEV, batch, binding, own_workspace
+a = batch(*BY_LAST, 16, 4, 16, junk=False)
+expect = binding.cs_chunk_attention(*a, workspace=own_workspace(a))
+out = torch.full_like(expect, 3.0)
+side, pool = torch.cuda.Stream(), torch.cuda.graph_pool_handle()
+side.wait_stream(torch.cuda.current_stream())
+first, second = torch.cuda.CUDAGraph(), torch.cuda.CUDAGraph()
+with torch.cuda.graph(first, pool=pool, stream=side):      # (its memory is free again at the end, with what is in it)
+    torch.full((128 << 20,), 7, dtype=torch.uint8, device=DEV)
+first.replay()
+torch.cuda.synchronize()
+with torch.cuda.graph(second, pool=pool, stream=side):     # the process's first call with a default workspace
+    %s
+for k in range(2):
+    for how in ("eager", "replayed"):
+        out.fill_(3.0)
+        torch.cuda.synchronize()
+        if how == "eager":
+            with torch.cuda.stream(side):
+                binding.cs_chunk_attention(*a, out=out)
+        else:
+            second.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, expect), (k, how)
+print("fine")
+"""
+
+
+@pytest.mark.parametrize("call", ["binding.cs_chunk_attention(*a, out=out)",
+                                  "binding.cs_chunk_attention(*a, out=out, stream=side.cuda_stream)"])
+def test_a_workspace_made_while_capturing_is_the_graph_s(call):
+    """In a process of its own: the first call is a captured one, an eager one on the same stream comes before the first
+    replay.  What the graph's memory held before is not zero."""
+    r = subprocess.run([sys.executable, "-c", ALONE % call], cwd=pathlib.Path(__file__).parent.parent, capture_output=True,
+                       text=True, timeout=300)
+    assert r.returncode == 0 and r.stdout.strip() == "fine", r.stderr[-2000:]
