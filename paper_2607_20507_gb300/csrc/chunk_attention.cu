@@ -168,9 +168,11 @@ struct Cuts {
     // the CTA that the block begins in
     __device__ __forceinline__ int first() const {
         const W more = (each + 1) * over;
-        int c = x0 < more ? (int)quotient(x0, each + 1) : over + (int)quotient(x0 - more, each);
+        const W at = x0 < more ? quotient(x0, each + 1) : over + quotient(x0 - more, each);
+        // (where starts decrease the weights may not fit: still one of the grid)
+        int c = at < (W)ctas ? (int)at : ctas - 1;
         while (c + 1 < ctas && begin_of(c + 1) == 0) ++c;
-        return min(c, ctas - 1);
+        return c;
     }
 };
 

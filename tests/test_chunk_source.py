@@ -54,3 +54,26 @@ def test_wide_stores_go_where_32_byte_alignment_is_known():
     assert re.search(r"if constexpr \(kWide\) \{\s*store32\(reinterpret_cast<float\*>\(p\)", text)
     assert "wide_out = reinterpret_cast<uintptr_t>(out) % 32 == 0" in text
     assert len(re.findall(r"\bstore_out<kWide>\(", text)) == 3
+
+
+def test_the_place_of_a_count_is_one_of_the_grid():
+    """Cuts::first() names the word in which a block's finished tiles are counted.  Where starts decrease, rows count several
+    times and the weights may pass their type, so its quotient may be anything: it is bounded before it becomes an int (a
+    quotient of 2^31 or more by a small share would be a negative one)."""
+    text = SOURCE.read_text()
+    first = text[text.index("int first() const {"):]
+    first = first[:first.index("\n    }\n")]
+    assert re.search(r"const W at = .*quotient\(.*quotient\(", first) and not re.search(r"\(int\)\s*quotient", first)
+    assert "int c = at < (W)ctas ? (int)at : ctas - 1;" in first and "return c;" in first
+    # a model of it: any place of the weight, any share, 32 bits
+    mask = (1 << 32) - 1
+    for each in (0, 1, 2, 7, 1 << 20, mask):
+        for over in (0, 1, 151):
+            for x0 in (0, 1, 150, 1 << 31, mask - 1, mask):
+                more = (each + 1) * over & mask
+                if x0 < more:
+                    at = x0 // ((each + 1) & mask) if (each + 1) & mask else mask
+                else:
+                    at = over + ((x0 - more) // each if each else mask) & mask
+                c = at if at < 152 else 151
+                assert 0 <= c < 152
