@@ -77,3 +77,24 @@ def test_the_place_of_a_count_is_one_of_the_grid():
                     at = over + ((x0 - more) // each if each else mask) & mask
                 c = at if at < 152 else 151
                 assert 0 <= c < 152
+
+
+def test_every_wait_is_bounded_and_every_role_comes_to_the_end():
+    """Waits on mbarriers: wait() and wait_lane(), which go on to the bounded one that the self-test lets run out and raise the
+    block's flag, and that one itself.  No thread leaves the kernel early, so that all meet the last barrier, with the products
+    of either issuing warp and the copies of the producers complete, before tensor memory is given back."""
+    text = SOURCE.read_text()
+    body = "\n".join(kernel())
+    assert not re.search(r"mbar_(try|test)_wait|mbarrier\.(try|test)_wait", body)
+    for name in ("wait_lane", "wait"):
+        f = text[text.index(f"void {name}(uint64_t* bar"):]
+        assert "if (!mbar_try_wait(bar, parity) && !*dead && !mbar_wait_bounded(bar, parity))" in f[:f.index("\n}\n")]
+    assert "!mbar_wait_bounded(" in (SOURCE.parent / "selftest.cu").read_text()
+    look = body[body.index("auto look = [&](int b) {"):]      # (a function of its own)
+    assert body.count("return;") == look[:look.index("};")].count("return;") == 1 and "exit;" not in body
+    end = body[body.rindex("__syncthreads()"):]
+    assert "tcgen05.dealloc" in end and body.index("mbar_wait_bounded(&bars.drained, 0)") < body.rindex("__syncthreads()")
+    roles = body[body.index("if (warp == kKvWarp) {"):]
+    producers = roles[:roles.index("const int m = warp == kMmaWarp")]
+    assert producers.count("if (!alive(&s_dead)) break;") == 2     # nothing more into places that may be in use
+    assert "mbar_wait_bounded(&bars.kv_full" in producers and "mbar_wait_bounded(&bars.q_full" in producers
