@@ -870,8 +870,10 @@ def cs_rope_kv_append(q, new_k, new_v, cos_sin, k_pages, v_pages, page_table, ct
                       stream: int | None = None):
     """Turn the queries and keys of new tokens by their positions and append keys and values to the page pools (in
     place).  q bf16 [tokens, Hq, 128] or None, new_k / new_v [tokens, Hkv, 128], whose tokens may lie apart; request b's
-    are the rows q_starts[b] .. q_starts[b+1] - 1 (None: as many each).  cos_sin fp32 [positions, rot_dim].  Returns
-    q_out.  See include/cachespec.h."""
+    are the rows q_starts[b] .. q_starts[b+1] - 1 (None: as many each).  cos_sin fp32 [positions, rot_dim]: it has to
+    reach every position, for a token past it is left out, in silence, its key, value and query unwritten.  Returns
+    q_out (where it is made here, rows of tokens left out and of no request hold anything).  See
+    include/cachespec.h."""
     r = (_fast or _load_fast()).rope_kv_append(q, new_k, new_v, cos_sin, k_pages, v_pages, page_table, ctx_lens, q_starts,
                                                positions, q_norm, k_norm, norm_eps, interleaved, q_out, stream)
     if r is not None:
@@ -940,7 +942,8 @@ def cs_chunk_attention(q, k_pages, v_pages, page_table, ctx_lens, q_starts=None,
                        sm_scale: float = 0.0, stream: int | None = None):
     """Attention of every request's newest tokens over the paged cache, causal among them.  q bf16 [tokens, Hq, 128],
     whose tokens may lie apart; request b's are the rows q_starts[b] .. q_starts[b+1] - 1 (None: as many each).
-    Returns ``out`` (bf16 [tokens, Hq, 128]; rows of no request stay as they are).  See include/cachespec.h."""
+    Returns ``out`` (bf16 [tokens, Hq, 128]; rows of no request stay as they are: anything, where it is made here).
+    See include/cachespec.h."""
     r = (_fast or _load_fast()).chunk_attention(q, k_pages, v_pages, page_table, ctx_lens, q_starts, out, workspace,
                                                 sm_scale, stream)
     if r is not None:

@@ -22,22 +22,24 @@
 // The products of one half run while the softmax of the other does, and a half's S of
 // the next tile being complete says that P V of this one is too (a thread's products
 // complete in order), so O may be rescaled then.  The running maximum moves only for a
-// growth of more than 2^8.  P is the sum of two bf16 terms, as in verify attention: one alone
-// leaves 2e-3 + 1e-2 |out| in rows of few keys whose values cancel, and adds 1.5e-3 to an
-// output's error everywhere, where its own rounding is 1.7e-3 (2-norms).  The second term is
-// half as much again of products (4096 tokens over 12288, 64 / 8 heads: 1590-1620 us, 1190
-// without; prompts of 129 to 1024 tokens, 32 heads each: 128 and 111; single tokens over
-// contexts to 8192: 377-387 and 372).  Skipping it where every weight is small against its row's
-// sum so far gave 1335-1400 in the first of these, but 117 for 108 in mixed batches and 137 for
-// 128: what decides it stands between the scores and the weights.  Either query tile has an issuing warp of its own: the queue of
-// products is short, and what one warp does between its products showed (the first of these:
-// 1270 us with one, 1189 with two, before the second term).
+// growth of more than 2^8.  Either query tile has an issuing warp of its own: the queue of
+// products is short, and what one warp does between its products showed (with one term of
+// P, 4096 tokens over 12288, 64 / 8 heads: 1270 us with one, 1189 with two).
+// P is the sum of two bf16 terms, as in verify attention: one alone leaves 2e-3 + 1e-2 |out|
+// in rows of few keys whose values cancel, and adds 1.5e-3 to an output's error everywhere,
+// where its own rounding is 1.7e-3 (2-norms).  The second term is half as much again of
+// products (the same case: 1550-1620 us, 1190 without it; prompts of 129 to 1024 tokens, 32
+// heads each: 128 and 111; single tokens over contexts to 8192: 385 and 372).  Skipping it
+// where every weight is small against its row's sum so far gave 1335-1400 in the first of
+// these, but 137 in the second, and 117 instead of 108 in mixed batches: what decides it
+// stands between the scores and the weights.
 // Every wait on a barrier is bounded; one that gives up sets the status word.
 //
-// What bounds it: the products of a tile of 256 rows and 128 keys are 3072 cycles, and come at
-// 1.8 PFLOP/s (the first case above), what a library product has here; single tokens over
-// long contexts the memory (128 requests, contexts to 8192: 6.4 TB/s); short calls
-// their start (5 us to the first tile), 4.2 us a block, and how even the ranges are.
+// What bounds it: the products of a tile of 256 rows and 128 keys, 3072 cycles; in the first
+// case above all of them come at 1.8 PFLOP/s, what a library product has here.  Single tokens
+// over long contexts: the memory (128 requests, contexts to 8192: 6.4 TB/s), and the chain of
+// a tile of one query tile.  Short calls: their start (5 us to the first tile), 4.2 us a
+// block, and how even the ranges are.
 #include <cudaTypedefs.h>
 #include <math.h>
 
@@ -61,14 +63,16 @@ constexpr int kTileBytes = kKeys * kD * 2;
 constexpr int kQBytes = kRows * kD * 2;
 constexpr int kSmem = kQBytes + kStages * kTileBytes;
 constexpr int kSmallQRows = 32;                    // blocks of few rows bring in no more than these
-// What beginning and ending a block costs, in keys (pieces of 256 rows took 4.2 us and 1.45
-// a tile; 208 instead: 8192 tokens 372 us, 360 so).
+// What beginning and ending a block costs, in keys (pieces of 256 rows take 4.2 us and 2 a
+// tile; 208 instead: 8 prompts 129 us, 127 so).
 constexpr int kBeginKeys = 288;
-// A range's end moves by so many keys, and so many a row, to a block's beginning or end;
-// contexts of up to kUncut keys are not cut.  A cut costs its two CTAs 4 and 7 us for 252
-// rows.  (24 requests, four of 301-512 new tokens: 90 us; with 384 and 2 a row either way
-// 94, without moves 91 but 777 tokens 23 for 17.  One token over 1023, 4095 keys: 11.5 and
-// 15.4 us; with 400 to the end too 14.9 and 18.2; 512 keys in pieces 11.3, 9.3 whole.)
+// A range's end moves by so many keys, and so many a row, to a block's beginning or end; a
+// call whose page table holds no more than kUncut keys a row has no cuts.  A cut costs its two
+// CTAs 4 and 7 us for 252 rows.  (24 requests, four of 301-512 new tokens: 107 us; with 384
+// and 2 a row either way 110; with 352, 64 and none a row 108, but 777 tokens 27 for 19.  One
+// token over 1023, 4095 keys: 12.5 and 16.0 us; with 400 to the end too 18 and 21; over 512
+// keys in pieces 10.9, 10.5 whole.  Where the table is wider, leaving contexts of up to kUncut
+// keys whole was no gain: over 512 keys 12.2, 11.3 so; 8 requests of 400 13.4, 15.0 so.)
 constexpr int kCutKeys = 400, kCutBack = 128, kCutRow = 1, kUncut = 640;
 static_assert(kCutKeys + kCutRow >= kBeginKeys + kKeys / 2 && kCutBack >= kKeys / 2, "every piece of a cut block has a tile");
 constexpr int kLeast = 192, kLeastRow = 2;         // a CTA's share where blocks are few: so many keys, and so many a row
