@@ -35,7 +35,7 @@
 // stands between the scores and the weights.
 // Every wait on a barrier is bounded; one that gives up sets the status word.
 //
-// What bounds it: the products of a tile of 256 rows and 128 keys, 3072 cycles; in the first
+// What bounds it: the products of a tile of 256 rows and 128 keys, 3 x 1024 cycles; in the first
 // case above all of them come at 1.8 PFLOP/s, what a library product has here.  Single tokens
 // over long contexts: the memory (128 requests, contexts to 8192: 6.4 TB/s), and the chain of
 // a tile of one query tile.  Short calls: their start (5 us to the first tile), 4.2 us a
